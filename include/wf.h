@@ -334,6 +334,109 @@ int wf_encoder_logmel(wf_encoder* e, const float* audio, float* mel, void* strea
 int wf_encoder_release(wf_encoder* e);
 const char* wf_encoder_last_error(wf_encoder* e);
 
+/*
+ * Operators without a handle: beam search's choice and page tables, and acoustic
+ * keys and values held in 4 bits.  They keep to the conventions above: checks on the
+ * host before anything is enqueued, work on the caller's stream (of the current
+ * device, which holds every buffer), no device memory but the caller's, no host
+ * synchronisation, so they may be captured into a HIP graph.  Messages of refused
+ * calls: wf_last_error(NULL).  A workspace serves one call at a time.  What device
+ * arrays hold is checked on the device, as each call states.
+ */
+
+/*
+ * Beam selection: for each of n requests, the k best continuations of its beams.
+ * Candidate (b, v) scores scores[r][b] + log softmax(logits row (r, b))[v], computed in
+ * 64 bits from exponentials in 32 and rounded to 32 once.  Candidates come best first,
+ * equal ones by lower beam, then lower token.
+ * logits: device, fp32 or bf16 (dtype WF_F32 or WF_BF16); row (r, b) starts
+ *   r * req_stride + b * beam_stride elements in and holds n_vocab values.
+ * scores: device fp32 [n, beams], each beam's cumulative log-probability (-inf: the
+ *   beam is empty and offers nothing).
+ * suppress: device uint8 [n_vocab] (1 = the token counts as logit -inf) or NULL.
+ * out_score fp32, out_beam int32, out_token int32: device [n, k].  Where a request has
+ * fewer than k candidates above -inf, the rest are -inf, -1, -1.  A row that holds a
+ * NaN or +inf among its unsuppressed values, and a beam whose score is NaN or +inf,
+ * offers nothing.
+ * 1 <= n <= 65535, 1 <= beams <= 16, 1 <= k <= 32, 1 <= n_vocab <= 2^20, strides >= 0.
+ * Errors: WF_EINVAL, WF_ESIZE (workspace), WF_EHIP.
+ */
+int wf_beam_select_workspace_bytes(int n, int beams, int n_vocab, int k, size_t* bytes);
+int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t beam_stride, const float* scores,
+                   const uint8_t* suppress, int n, int beams, int n_vocab, int k, float* out_score, int32_t* out_beam,
+                   int32_t* out_token, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Page tables after a choice of beams: beam j of request r continues beam
+ * parents[r][j], whose lens[r] positions it keeps.  It takes over the parent's pages;
+ * pages that are full are shared.  The page of the next position, lens[r] / page_tokens,
+ * is each beam's own: where it is part-filled, the first beam that keeps it goes on in
+ * it and every other one gets a fresh page with its contents; where it would be empty,
+ * every beam gets a fresh page.  Fresh pages are the pages of the request's pool, in
+ * the pool's order, that no kept table entry names.  Entries past a beam's last page,
+ * and every entry of a beam whose parent is not in [0, beams), name the pool's first
+ * page, so that reading ahead stays inside the cache.
+ * cache: device, 16-byte aligned: n_regions regions region_stride bytes apart (keys and
+ *   values of every block), each of n_pages pages of page_bytes (multiples of 16).
+ * tables, new_tables: device int32 [n, beams, max_pages], not the same memory.
+ * parents: device int32 [n, beams]; lens: device int32 [n], taken as the nearest of
+ *   [0, max_pages * page_tokens].
+ * pool: device int32 [n, pool_pages], distinct pages that belong to the request alone;
+ *   pool_pages >= beams * max_pages always holds enough fresh ones.
+ * A page number outside [0, n_pages) is carried over and never read or written.
+ * 1 <= n <= 65535, 1 <= beams <= 16, n_pages <= 2^18, 1 <= n_regions <= 65535.
+ * Errors: WF_EINVAL, WF_EHIP.
+ */
+int wf_cache_reorder(void* cache, int n_regions, size_t region_stride, int n_pages, size_t page_bytes,
+                     const int32_t* tables, int32_t* new_tables, int n, int beams, int max_pages, int page_tokens,
+                     const int32_t* parents, const int32_t* lens, const int32_t* pool, int pool_pages, void* stream);
+
+/*
+ * Acoustic keys and values in 4 bits: per entry (a request's memory) n_frames frames of
+ * n_head heads of 64 dims.  Elements are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives; to the nearest, ties to the even code) in blocks of 32 with a power-of-two
+ * scale: the smallest 2^e, e >= -120, with max |x| <= 6 * 2^e.  A key's blocks are dims
+ * 0..31 and 32..63 of a frame, a value's are 32 frames (32 g .. 32 g + 31) of one dim.  A
+ * block that holds a NaN or an infinity stands for NaN throughout; magnitudes of
+ * 3.5 * 2^126 (2.98e38) and more stand for infinity (4 * 2^126).  4.25 bits an element:
+ * 2176 bytes per head and 32 frames, in an order of the library's own.
+ * data: device, 16-byte aligned, wf_kv4_bytes(entries, n_head, n_frames) bytes.
+ * 1 <= entries <= 65535, 1 <= n_head <= 65535, 1 <= n_frames <= 2^20.
+ */
+typedef struct wf_kv4 {
+  void* data;
+  int32_t entries;
+  int32_t n_head;
+  int32_t n_frames;
+} wf_kv4;
+int wf_kv4_bytes(int entries, int n_head, int n_frames, size_t* bytes);
+/*
+ * Store keys and values of entries [slot0, slot0 + n), whole entries.
+ * k, v: device, fp32 or bf16; element (r, f, h, d) lies r * stride[0] + f * stride[1] +
+ *   h * stride[2] + d elements in (strides >= 0, host arrays of three).
+ * lens: device int32 [n], the frames of each that are given, taken as the nearest of
+ *   [0, n_frames], or NULL (all).  Frames past them are not read and hold zeros.
+ */
+int wf_kv4_store(const wf_kv4* c, int slot0, int n, const void* k, const int64_t* k_stride, const void* v,
+                 const int64_t* v_stride, int dtype, const int32_t* lens, void* stream);
+/* The values that entries [slot0, slot0 + n) hold: k, v device [n, n_frames, n_head, 64]
+ * in dtype (every one is exact in both). */
+int wf_kv4_load(const wf_kv4* c, int slot0, int n, void* k, void* v, int dtype, void* stream);
+/*
+ * Attention of `rows` query rows of each of n requests over the first lens[r] frames of
+ * its entry slot0 + r: softmax(q k^T / 8) v, without a mask (cross-attention).  Query
+ * values enter the products exactly, probabilities exactly (fp32) or to 2^-16 relative
+ * (bf16), the softmax and all sums are fp32.  A request of no frames gets zeros.
+ * q: device, fp32 or bf16; element (r, i, h, d) lies r * q_stride[0] + i * q_stride[1] +
+ *   h * q_stride[2] + d elements in (strides >= 0, a host array of three): a request's beams
+ *   or the rows of a pass are its rows.
+ * lens: device int32 [n], taken as the nearest of [0, n_frames], or NULL (all).
+ * out: device [n, rows, n_head, 64] in the same type.  1 <= rows <= 2^20.
+ */
+int wf_kv4_attend_workspace_bytes(const wf_kv4* c, int n, int rows, size_t* bytes);
+int wf_kv4_attend(const wf_kv4* c, int slot0, int n, const void* q, const int64_t* q_stride, int rows, int dtype,
+                  const int32_t* lens, void* out, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,9 @@ EXPORTS = ["wf_workspace_bytes", "wf_weight_count", "wf_weight_numel", "wf_init_
            "wf_step", "wf_step_noalloc", "wf_debug_ptr", "wf_set_debug", "wf_profile_enable", "wf_profile_summary", "wf_status",
            "wf_release", "wf_strerror", "wf_last_error", "wf_rng_words_host", "wf_rng_words_device",
            "wf_encoder_workspace_bytes", "wf_encoder_weight_count", "wf_encoder_weight_numel", "wf_encoder_init",
-           "wf_encoder_run", "wf_encoder_logmel", "wf_encoder_release", "wf_encoder_last_error"]
+           "wf_encoder_run", "wf_encoder_logmel", "wf_encoder_release", "wf_encoder_last_error",
+           "wf_beam_select_workspace_bytes", "wf_beam_select", "wf_cache_reorder", "wf_kv4_bytes", "wf_kv4_store",
+           "wf_kv4_load", "wf_kv4_attend_workspace_bytes", "wf_kv4_attend"]
 
 
 class WfConfig(ctypes.Structure):
@@ -41,6 +43,11 @@ class WfEncoderConfig(ctypes.Structure):
     _fields_ = [("n_mels", ctypes.c_int32), ("n_ctx", ctypes.c_int32), ("d_model", ctypes.c_int32),
                 ("n_head", ctypes.c_int32), ("n_layer", ctypes.c_int32), ("d_ff", ctypes.c_int32),
                 ("n_fft", ctypes.c_int32), ("hop", ctypes.c_int32), ("sample_rate", ctypes.c_int32)]
+
+
+class WfKv4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("entries", ctypes.c_int32), ("n_head", ctypes.c_int32),
+                ("n_frames", ctypes.c_int32)]
 
 
 class WfError(RuntimeError):
@@ -59,7 +66,8 @@ def load_library(path=LIB_PATH):
         raise WfError(f"{path} not found: build the HIP library first (python -m paper_2609_32869_amd.build)")
     lib = ctypes.CDLL(path)
     P, I, Z, U64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint64
-    cfgp = ctypes.POINTER(WfConfig)
+    I64, I64p = ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)
+    cfgp, kv4p = ctypes.POINTER(WfConfig), ctypes.POINTER(WfKv4)
     sig = {
         "wf_workspace_bytes": [cfgp, ctypes.POINTER(Z)],
         "wf_weight_count": [cfgp, ctypes.POINTER(I)],
@@ -90,6 +98,14 @@ def load_library(path=LIB_PATH):
         "wf_encoder_logmel": [P, P, P, P],
         "wf_encoder_release": [P],
         "wf_encoder_last_error": [P],
+        "wf_beam_select_workspace_bytes": [I, I, I, I, ctypes.POINTER(Z)],
+        "wf_beam_select": [P, I, I64, I64, P, P, I, I, I, I, P, P, P, P, Z, P],
+        "wf_cache_reorder": [P, I, Z, I, Z, P, P, I, I, I, I, P, P, P, I, P],
+        "wf_kv4_bytes": [I, I, I, ctypes.POINTER(Z)],
+        "wf_kv4_store": [kv4p, I, I, P, I64p, P, I64p, I, P, P],
+        "wf_kv4_load": [kv4p, I, I, P, P, I, P],
+        "wf_kv4_attend_workspace_bytes": [kv4p, I, I, ctypes.POINTER(Z)],
+        "wf_kv4_attend": [kv4p, I, I, P, I64p, I, I, P, P, P, Z, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

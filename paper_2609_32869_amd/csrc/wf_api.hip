@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "wf_internal.h"
+#include "wf_ops.h"
 
 using namespace wf;
 
@@ -48,6 +49,16 @@ char* scratch_of(int dev) {
 }
 
 thread_local std::string g_err;
+}  // namespace
+
+namespace wf {
+int op_fail(int code, const char* msg) {
+  g_err = msg;
+  return code;
+}
+}  // namespace wf
+
+namespace {
 
 int fail(Handle* h, int code, const std::string& msg) {
   if (h) h->err = msg;

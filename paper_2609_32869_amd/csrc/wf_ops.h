@@ -1,0 +1,96 @@
+// Argument blocks and launchers of the stateless operators (internal): beam selection
+// and page reordering (k_beam.hip), the 4-bit acoustic cache (k_kv4.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <string>
+
+#include "wf_common.h"
+
+namespace wf {
+
+// Records the message of a call without a handle (wf_last_error(NULL)); returns code.
+int op_fail(int code, const char* msg);
+
+// ---------------------------------------------------------------- beam selection
+constexpr int kMaxBeams = 16;       // beams of one request
+constexpr int kMaxCand = 32;        // candidates kept per request
+constexpr int kMaxVocab = 1 << 20;  // columns of a logits row
+struct BeamSelectArgs {
+  const void* logits;  // element (r, b, v) at r * sr + b * sb + v
+  int bf16_logits;
+  long long sr, sb;
+  const float* scores;      // (r, b) at r * beams + b
+  const uint8_t* suppress;  // [vocab] nonzero: the column is left out, or null
+  int n, beams, vocab, k;
+  // per logits row (r * beams + b): the row's k best as (logit, column), its log of the sum of exponentials
+  float* pv;
+  int* pi;
+  double* lse;
+  float* out_score;  // [n][k]
+  int* out_beam;
+  int* out_token;
+};
+void beam_select(const BeamSelectArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- page tables after a choice of beams
+constexpr int kMaxPages = 1 << 18;  // pages of a cache (a bit each in LDS)
+struct ReorderArgs {
+  char* cache;  // [regions] of region_stride bytes, each n_pages pages of page_bytes
+  int regions;
+  size_t region_stride, page_bytes;
+  int n_pages;
+  const int* tables;   // (r, b, c) at r * tr + b * tb + c
+  int* new_tables;     // likewise, other memory
+  long long tr, tb;
+  const int* parents;  // [n][beams]
+  const int* lens;     // [n]
+  const int* pool;     // [n][pool_pages]
+  int n, beams, max_pages, pool_pages, page_tokens;
+};
+void cache_reorder(const ReorderArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- acoustic keys and values in 4 bits
+// Per (entry, head), groups of 32 frames one after the other, kKv4Group bytes each: the
+// keys' and the values' codes in the order in which a wave's lanes multiply them, then
+// their scales' biased exponents (0xff: the block stands for NaN).
+//   keys    lane l = 16 kg + n, byte 8 t + j: dims 16 kg + 2 j, + 1 of frame 16 t + n
+//   values  lane l = 16 kg + n, byte 4 dt + j: frames 8 kg + 2 j, + 1 of dim 16 dt + n
+//   scales  keys: byte 32 half + 2 n + t: dims 32 half .. + 31 of frame 16 t + n;
+//           values: byte 4 n + dt: dim 16 dt + n
+// Low nibble first.  A wave reads a group's codes as two 16-byte loads per lane.
+constexpr int kKv4Frames = 32;
+constexpr int kKv4Values = 1024, kKv4KeyScale = 2048, kKv4ValueScale = 2112, kKv4Group = 2176;
+constexpr int kKv4MaxFrames = 1 << 20;
+inline int kv4_groups(int frames) { return (frames + kKv4Frames - 1) / kKv4Frames; }
+struct Kv4 {
+  uint8_t* base;
+  int n_head, groups, frames;
+};
+struct Kv4StoreArgs {
+  Kv4 c;
+  const void *k, *v;  // element (r, f, h, d) at r * sr + f * sf + h * sh + d
+  int bf16_src;
+  long long kr, kf, kh, vr, vf, vh;
+  const int* lens;  // [n] or null
+  int slot0, n;
+  int vec;  // rows may be read 16 bytes at a time
+};
+void kv4_store(const Kv4StoreArgs& a, hipStream_t st);
+struct Kv4LoadArgs {
+  Kv4 c;
+  void *k, *v;  // [n][frames][n_head][64]
+  int bf16_out, slot0, n;
+};
+void kv4_load(const Kv4LoadArgs& a, hipStream_t st);
+struct Kv4AttendArgs {
+  Kv4 c;
+  const void* q;  // element (r, i, h, d) at r * sr + i * si + h * sh + d
+  long long sr, si, sh;
+  int bf16_q, vec;
+  void* out;  // [n][rows][n_head][64], the query's type
+  const int* lens;
+  int slot0, n, rows;
+};
+void kv4_attend(const Kv4AttendArgs& a, hipStream_t st);
+
+}  // namespace wf

@@ -20,7 +20,7 @@ def beam_select(logits, scores, k, suppress=None):
             if not np.isfinite(s) or np.isnan(row).any() or np.isposinf(row).any() or np.isneginf(row).all():
                 continue
             m = row.max()
-            every[b] = s + (row - (m + np.log(np.exp(row - m).sum())))
+            every[b] = s + ((row - m) - np.log(np.exp(row - m).sum()))
         order = np.argsort(-every, axis=None, kind="stable")[:k]
         for j, i in enumerate(order):
             if every.flat[i] > -np.inf:

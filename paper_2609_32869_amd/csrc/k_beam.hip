@@ -1,103 +1,315 @@
 // Beam search: the k best continuations over a request's beams and vocabulary, and the
 // page tables of the beams that were chosen.
+#include <algorithm>
+
 #include "wf_ops.h"
 
 namespace wf {
 
 // ---------------------------------------------------------------- selection
 // score(b, v) = s_b + x_bv - log sum_u exp(x_bu).  A beam's order over v is the order of
-// its logits, so each row keeps its k best logits; the beams meet in 64-bit scores.
+// its logits, so the row kernel keeps the k best logits of each piece of a row beside the
+// piece's maximum and sum of exponentials; the beams meet in 64-bit scores in the merge.
+//
+// Row kernel: a block per (piece of kBeamPiece columns, row), one read of the logits into
+// registers, 32 per thread.  The k-th best of a wave's 64 per-lane bests, found bit by bit
+// with ballots, bounds the k-th best of the piece from below: the best of the four waves'
+// bounds leaves a handful of survivors (k lanes a wave at most), which are ranked by
+// counting.  Values as order-preserving integers; equal ones by column, so that any
+// number of ties stays within the survivors' array.
+constexpr int kBeamRegs = 32;
+constexpr int kBeamPiece = 256 * kBeamRegs;
+constexpr int kBeamList = 4 * kBeamRegs * kMaxCand;  // survivors at most: four waves of k lanes
 
+// Larger value, larger integer; NaN and -inf (no candidates) at 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return !(x > -INFINITY) ? 0u : u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o); }
+
+// r-th largest of the active lanes' words (r <= their number); afterwards r is its rank
+// among the lanes that hold it, and those are the active ones.
+__device__ __forceinline__ uint32_t wave_kth(uint32_t w, bool& active, int& r) {
+  uint32_t t = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const int c = __popcll(__ballot(active && (w >> bit) == (t >> bit | 1u)));
+    if (c >= r) t |= 1u << bit;
+    else r -= c;
+  }
+  active = active && w == t;
+  return t;
+}
+
+// 8 consecutive logits from column v on; columns past the row and suppressed ones are
+// -inf.  Rows start anywhere (every second bf16 row of an odd vocabulary lies off 4
+// bytes), so the loads are 16 bytes at the elements' alignment: columns are grouped by
+// number, not by address, and rows of equal values have equal sums.
+__device__ __forceinline__ void ld8_any(const float* p, float* o) { __builtin_memcpy(o, p, 32); }
+__device__ __forceinline__ void ld8_any(const bf16* p, float* o) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = __uint_as_float(u[i] << 16);
+    o[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
 template <typename T>
-__device__ __forceinline__ float logit(const T* x, const uint8_t* sup, int v) {
-  return sup && sup[v] ? -INFINITY : to_f(x[v]);
+__device__ __forceinline__ void logits8(const T* x, const uint8_t* sup, int v, int vocab, float* o) {
+  if (v + 8 <= vocab) {
+    ld8_any(x + v, o);
+    if (sup) {
+      uint64_t m;
+      __builtin_memcpy(&m, sup + v, 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (m >> (8 * e) & 255) o[e] = -INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = v + e;
+      o[e] = c < vocab && !(sup && sup[c]) ? to_f(x[c]) : -INFINITY;
+    }
+  }
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
-  __shared__ float sv[256];
-  __shared__ int si[256];
-  __shared__ double sd[256];
-  const int row = blockIdx.x, r = row / a.beams, b = row % a.beams, t = threadIdx.x;
+  __shared__ uint32_t lo[kBeamList];
+  __shared__ int lc[kBeamList];
+  __shared__ uint32_t tv[4], ti[4];
+  __shared__ float wm[4];
+  __shared__ double ws[4];
+  __shared__ int count;
+  const int row = blockIdx.x, r = row / a.beams, b = row % a.beams, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb;
-  float last = INFINITY;
-  int li = -1;
-  for (int j = 0; j < a.k; ++j) {
-    float bv = -INFINITY;
-    int bi = a.vocab;
-    for (int v = t; v < a.vocab; v += 256) {
-      const float y = logit(x, a.suppress, v);
-      if ((y < last || (y == last && v > li)) && y > -INFINITY && better(y, v, bv, bi)) {
-        bv = y;
-        bi = v;
-      }
+  const int v0 = blockIdx.y * kBeamPiece + 8 * t;
+  if (t == 0) count = 0;
+  float y[kBeamRegs];
+#pragma unroll
+  for (int i = 0; i < kBeamRegs / 8; ++i) logits8(x, a.suppress, v0 + 2048 * i, a.vocab, y + 8 * i);
+  // maximum and sum of exponentials, eight at a time in 32 bits, then 64
+  float m = -INFINITY;
+  uint32_t best = 0;
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < kBeamRegs; ++i) {
+    m = fmaxf(m, y[i]);
+    const uint32_t o = order_of(y[i]);
+    if (o > best) {  // the first of equal values
+      best = o;
+      at = v0 + 2048 * (i / 8) + i % 8;
     }
-    sv[t] = bv;
-    si[t] = bi;
-    __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-      if (t < o && better(sv[t + o], si[t + o], sv[t], si[t])) {
-        sv[t] = sv[t + o];
-        si[t] = si[t + o];
-      }
-      __syncthreads();
+  }
+  const float base = m == -INFINITY ? 0.f : m;
+  double sum = 0;
+#pragma unroll
+  for (int i = 0; i < kBeamRegs; i += 8) {
+    float p = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p += __expf(y[i + e] - base);
+    sum += (double)p;
+  }
+  const float M = wave_max(m);
+  // rescaled to the wave's maximum; a lane of no values adds nothing, a NaN stays
+  sum *= (double)__expf((m == -INFINITY ? M : m) - (M == -INFINITY ? 0.f : M));
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+  // the wave's bound: its k-th best lane
+  int need = a.k;
+  bool active = best != 0;
+  uint32_t bound = 0, col = ~0u;
+  if (__popcll(__ballot(active)) >= need) {
+    bound = wave_kth(best, active, need);
+    if (need < __popcll(__ballot(active))) col = ~wave_kth(~(uint32_t)at, active, need);  // lowest columns first
+  }
+  if (lane == 0) {
+    tv[w] = bound;
+    ti[w] = col;
+    wm[w] = M;
+    ws[w] = sum;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (tv[i] > bound || (tv[i] == bound && ti[i] < col)) {
+      bound = tv[i];
+      col = ti[i];
     }
-    last = sv[0];
-    li = si[0];
-    __syncthreads();
-    if (j == 0) {
-      double sum = 0;
-      for (int v = t; v < a.vocab; v += 256) {
-        const float y = logit(x, a.suppress, v);
-        if (!(y == -INFINITY)) sum += (double)expf(y - last);
-      }
-      sd[t] = sum;
-      __syncthreads();
-      for (int o = 128; o > 0; o >>= 1) {
-        if (t < o) sd[t] += sd[t + o];
-        __syncthreads();
-      }
-      if (t == 0) a.lse[row] = (double)last + log(sd[0]);
+#pragma unroll
+  for (int i = 0; i < kBeamRegs; ++i) {
+    const uint32_t o = order_of(y[i]);
+    const int c = v0 + 2048 * (i / 8) + i % 8;
+    if (o != 0 && (o > bound || (o == bound && (uint32_t)c <= col))) {
+      const int j = atomicAdd(&count, 1);
+      lo[j] = o;
+      lc[j] = c;
     }
-    if (t == 0) {
-      a.pv[(size_t)row * a.k + j] = last;
-      a.pi[(size_t)row * a.k + j] = li;
+  }
+  __syncthreads();
+  const size_t piece = (size_t)row * gridDim.y + blockIdx.y;
+  const int n = count;
+  for (int i = t; i < n; i += 256) {
+    const uint32_t o = lo[i];
+    const int c = lc[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += lo[j] > o || (lo[j] == o && lc[j] < c);
+    if (rank < a.k) {
+      a.pv[piece * a.k + rank] = value_of(o);
+      a.pi[piece * a.k + rank] = c;
     }
-    if (li >= a.vocab) {  // nothing left (uniform)
-      last = -INFINITY;
-      li = a.vocab;
-    }
+  }
+  for (int i = n + t; i < a.k; i += 256) {
+    a.pv[piece * a.k + i] = -INFINITY;
+    a.pi[piece * a.k + i] = -1;
+  }
+  if (t == 0) {
+    float mm = wm[0];
+    for (int i = 1; i < 4; ++i) mm = fmaxf(mm, wm[i]);
+    double total = 0;
+    for (int i = 0; i < 4; ++i)
+      total += ws[i] * (double)__expf((wm[i] == -INFINITY ? mm : wm[i]) - (mm == -INFINITY ? 0.f : mm));
+    a.pm[piece] = mm;
+    a.ps[piece] = total;
   }
 }
 
-__global__ void __launch_bounds__(64) k_beam_merge(BeamSelectArgs a) {
-  const int r = blockIdx.x;
-  if (threadIdx.x != 0) return;
-  int at[kMaxBeams];
-  for (int b = 0; b < a.beams; ++b) at[b] = 0;
-  for (int j = 0; j < a.k; ++j) {
-    double best = -INFINITY;
-    int bb = -1;
-    for (int b = 0; b < a.beams; ++b) {
-      if (at[b] >= a.k) continue;
-      const size_t row = (size_t)r * a.beams + b;
-      const double s = (double)a.scores[row] + ((double)a.pv[row * a.k + at[b]] - a.lse[row]);
-      if (s > best && s < INFINITY) {
-        best = s;
-        bb = b;
+// Merge: a block per request.  16 lanes a row join its pieces' sums; then the pieces'
+// candidates by 64-bit score.  A wave's k-th best lane (scores rounded to 32 bits, which
+// keeps the order) bounds the k-th best again; more survivors than the array holds, which
+// takes that many equal scores, are chosen one by one.
+constexpr int kMergeList = 2048;
+// ties: order = beam * 2^20 + column
+__device__ __forceinline__ bool ahead(double s, int o, double t, int p) { return s > t || (s == t && o < p); }
+
+__global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
+  __shared__ double top[kMaxBeams], rest[kMaxBeams], ls[kMergeList], bs[4];
+  __shared__ int lo[kMergeList], bo[4], count;
+  __shared__ uint32_t tv[4];
+  const int r = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
+  if (t == 0) count = 0;
+  {
+    const int b = min(t >> 4, a.beams - 1);
+    const size_t row = (size_t)r * a.beams + b;
+    float m = -INFINITY;
+    for (int p = t & 15; p < np; p += 16) m = fmaxf(m, a.pm[row * np + p]);
+    m = max16(m);
+    double s = 0;
+    for (int p = t & 15; p < np; p += 16) {
+      const float pm = a.pm[row * np + p];
+      const double ps = a.ps[row * np + p];
+      s += pm == -INFINITY && ps == 0 ? 0 : ps * exp((double)pm - (double)m);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o);
+    const float sc = a.scores[row];
+    // score = (x - m) + (s_b - log sum): the difference is exact enough at any magnitude; NaN where the row or the
+    // beam offers nothing
+    if ((t & 15) == 0 && t >> 4 < a.beams) {
+      top[b] = m;
+      rest[b] = sc < INFINITY ? (double)sc - log(s) : NAN;
+    }
+  }
+  __syncthreads();
+  const int per = np * a.k, total = a.beams * per;
+  const size_t first = (size_t)r * total;
+  // score and order of candidate i; false: none
+  auto cand = [&](int i, double& s, int& o) {
+    const int b = i / per, c = a.pi[first + i];
+    s = ((double)a.pv[first + i] - top[b]) + rest[b];
+    o = b << 20 | c;
+    return c >= 0 && s > -INFINITY;
+  };
+  uint32_t best = 0;
+  for (int i = t; i < total; i += 256) {
+    double s;
+    int o;
+    if (cand(i, s, o)) best = max(best, order_of((float)s));
+  }
+  int need = a.k;
+  bool active = best != 0;
+  uint32_t bound = 0;
+  if (__popcll(__ballot(active)) >= need) bound = wave_kth(best, active, need);
+  if (lane == 0) tv[w] = bound;
+  __syncthreads();
+  bound = max(max(tv[0], tv[1]), max(tv[2], tv[3]));
+  for (int i = t; i < total; i += 256) {
+    double s;
+    int o;
+    if (cand(i, s, o) && order_of((float)s) >= bound) {
+      const int j = atomicAdd(&count, 1);
+      if (j < kMergeList) {
+        ls[j] = s;
+        lo[j] = o;
       }
     }
-    a.out_score[(size_t)r * a.k + j] = (float)best;
-    a.out_beam[(size_t)r * a.k + j] = bb;
-    a.out_token[(size_t)r * a.k + j] = bb < 0 ? -1 : a.pi[((size_t)r * a.beams + bb) * a.k + at[bb]];
-    if (bb >= 0) ++at[bb];
+  }
+  __syncthreads();
+  const int n = count;
+  auto put = [&](int rank, double s, int o) {
+    a.out_score[(size_t)r * a.k + rank] = (float)s;
+    a.out_beam[(size_t)r * a.k + rank] = o < 0 ? -1 : o >> 20;
+    a.out_token[(size_t)r * a.k + rank] = o < 0 ? -1 : o & ((1 << 20) - 1);
+  };
+  if (n <= kMergeList) {
+    for (int i = t; i < n; i += 256) {
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += ahead(ls[j], lo[j], ls[i], lo[i]);
+      if (rank < a.k) put(rank, ls[i], lo[i]);
+    }
+    for (int i = n + t; i < a.k; i += 256) put(i, -INFINITY, -1);
+    return;
+  }
+  double ps = INFINITY;
+  int po = -1;
+  for (int j = 0; j < a.k; ++j) {
+    double s1 = -INFINITY;
+    int o1 = 0x7fffffff;
+    for (int i = t; i < total; i += 256) {
+      double s;
+      int o;
+      if (cand(i, s, o) && ahead(ps, po, s, o) && ahead(s, o, s1, o1)) {
+        s1 = s;
+        o1 = o;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double s2 = __shfl_xor(s1, o);
+      const int o2 = __shfl_xor(o1, o);
+      if (ahead(s2, o2, s1, o1)) {
+        s1 = s2;
+        o1 = o2;
+      }
+    }
+    if (lane == 0) {
+      bs[w] = s1;
+      bo[w] = o1;
+    }
+    __syncthreads();
+    for (int i = 0; i < 4; ++i)
+      if (ahead(bs[i], bo[i], s1, o1)) {
+        s1 = bs[i];
+        o1 = bo[i];
+      }
+    ps = s1;
+    po = o1;
+    if (t == 0) put(j, s1, o1);
+    __syncthreads();
   }
 }
+
+int beam_pieces(int vocab) { return (vocab + kBeamPiece - 1) / kBeamPiece; }
 
 void beam_select(const BeamSelectArgs& a, hipStream_t st) {
-  if (a.bf16_logits) k_beam_rows<bf16><<<a.n * a.beams, 256, 0, st>>>(a);
-  else k_beam_rows<float><<<a.n * a.beams, 256, 0, st>>>(a);
-  k_beam_merge<<<a.n, 64, 0, st>>>(a);
+  const int np = beam_pieces(a.vocab);
+  const dim3 grid(a.n * a.beams, np);
+  if (a.bf16_logits) k_beam_rows<bf16><<<grid, 256, 0, st>>>(a);
+  else k_beam_rows<float><<<grid, 256, 0, st>>>(a);
+  k_beam_merge<<<a.n, 256, 0, st>>>(a, np);
 }
 
 // ---------------------------------------------------------------- page tables
@@ -106,71 +318,84 @@ void beam_select(const BeamSelectArgs& a, hipStream_t st) {
 // is one beam's own: the first beam that keeps a part-filled page goes on in it, every
 // other one gets the pool's next unreferenced page and a copy.
 //
-// Grid (region, request).  Every block works the request's pages out for itself (a few
-// hundred table entries, a bit per page of the cache in LDS); the first one writes the
-// tables, each copies the pages of its region.
-__global__ void __launch_bounds__(256) k_cache_reorder(ReorderArgs a) {
+// Grid (region x part of a page, request).  Every block works the request's pages out for
+// itself (a few hundred table entries, a bit per page of the cache in LDS), so that one
+// launch does it all.  The first block writes the tables, each copies its part of the
+// copied pages in its region.
+constexpr int kReorderThreads = 256;
+__global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a, int parts) {
   __shared__ unsigned used[kMaxPages / 32];
-  __shared__ int2 copy[kMaxBeams];  // (source, destination), destination -1: none
+  __shared__ int parent[kMaxBeams], mine[kMaxBeams], fresh[kMaxBeams];
+  __shared__ int2 copy[kMaxBeams];  // (source, destination)
+  __shared__ int ncopy;
   const int r = blockIdx.y, t = threadIdx.x;
   const bool lead = blockIdx.x == 0;
-  for (int i = t; i < (a.n_pages + 31) / 32; i += 256) used[i] = 0;
-  __syncthreads();
-  const int len = (int)min((long long)max(a.lens[r], 0), (long long)a.max_pages * a.page_tokens);
-  const int last = len / a.page_tokens, part = len % a.page_tokens, kept = last + (part ? 1 : 0);
   const int* T = a.tables + r * a.tr;
   int* N = a.new_tables + r * a.tr;
   const int* pool = a.pool + (size_t)r * a.pool_pages;
-  const int* parents = a.parents + (size_t)r * a.beams;
-  for (int j = 0; j < a.beams; ++j) {
-    const int p = parents[j];
-    const bool live = p >= 0 && p < a.beams;
-    for (int c = t; c < a.max_pages; c += 256) {
-      const int page = live && c < kept ? T[p * a.tb + c] : pool[0];
-      if (lead) N[j * a.tb + c] = page;
-      if (live && c < kept && page >= 0 && page < a.n_pages) atomicOr(&used[page >> 5], 1u << (page & 31));
-    }
+  // independent loads first
+  const int p0 = pool[0], q0 = pool[min(t, a.pool_pages - 1)], raw = a.lens[r];
+  if (t < kMaxBeams) {
+    const int p = t < a.beams ? a.parents[(size_t)r * a.beams + t] : -1;
+    parent[t] = p < a.beams ? p : -1;
+    fresh[t] = -1;
+  }
+  for (int i = t; i < (a.n_pages + 31) / 32; i += kReorderThreads) used[i] = 0;
+  __syncthreads();
+  const int len = (int)min((long long)max(raw, 0), (long long)a.max_pages * a.page_tokens);
+  const int last = len / a.page_tokens, part = len % a.page_tokens, kept = last + (part ? 1 : 0);
+  const int entries = a.beams * (lead ? a.max_pages : kept), width = lead ? a.max_pages : max(kept, 1);
+  for (int i = t; i < entries; i += kReorderThreads) {
+    const int j = i / width, c = i - j * width, p = parent[j];
+    const bool keep = p >= 0 && c < kept;
+    const int page = keep ? T[p * a.tb + c] : p0;
+    if (keep && page >= 0 && page < a.n_pages) atomicOr(&used[page >> 5], 1u << (page & 31));
+    if (keep && c == last) mine[j] = page;
+    if (lead && !(c == last && p >= 0)) N[j * a.tb + c] = page;
   }
   __syncthreads();
-  if (t == 0) {
-    int at = 0;
-    for (int j = 0; j < a.beams; ++j) {
-      const int p = parents[j];
-      int2 cp = make_int2(-1, -1);
-      if (p >= 0 && p < a.beams && last < a.max_pages) {
-        bool need = part == 0;
-        const int mine = T[p * a.tb + last];
-        for (int i = 0; i < j && !need; ++i) {
-          const int pi = parents[i];
-          need = pi >= 0 && pi < a.beams && T[pi * a.tb + last] == mine;
-        }
-        if (need) {
-          int page = -1;
-          for (; at < a.pool_pages && page < 0; ++at) {
-            const int q = pool[at];
-            if (q >= 0 && q < a.n_pages && !(used[q >> 5] >> (q & 31) & 1)) page = q;
-          }
-          if (page >= 0) {
-            if (lead) N[j * a.tb + last] = page;
-            if (part && mine >= 0 && mine < a.n_pages) cp = make_int2(mine, page);
-          }
-        }
-      }
-      copy[j] = cp;
+  if (t < 64) {  // the first wave: which beams need a page, and the pool's free ones in order
+    const int j = min(t, a.beams - 1);
+    bool need = t < a.beams && parent[j] >= 0 && last < a.max_pages, again = false;
+    if (need && part)
+      for (int i = 0; i < j; ++i) again = again || (parent[i] >= 0 && mine[i] == mine[j]);
+    need = need && (part == 0 || again);
+    const uint64_t below = ((uint64_t)1 << t) - 1, who = __ballot(need);
+    const int want = __popcll(who), rank = __popcll(who & below);
+    for (int i0 = 0, found = 0; i0 < a.pool_pages && found < want; i0 += 64) {
+      const int i = i0 + t;
+      const int q = i0 == 0 ? q0 : i < a.pool_pages ? pool[i] : -1;
+      const bool free = i < a.pool_pages && q >= 0 && q < a.n_pages && !(used[max(q, 0) >> 5] >> (q & 31) & 1);
+      const uint64_t m = __ballot(free);
+      const int f = found + __popcll(m & below);
+      if (free && f < want) fresh[f] = q;
+      found += __popcll(m);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // fresh[] was written by other lanes
+    const int page = need ? fresh[rank] : -1;
+    const bool moved = need && page >= 0 && part && mine[j] >= 0 && mine[j] < a.n_pages;
+    const uint64_t mv = __ballot(moved);
+    if (moved) copy[__popcll(mv & below)] = make_int2(mine[j], page);
+    if (t == 0) ncopy = __popcll(mv);
+    if (lead && t < a.beams && parent[j] >= 0 && last < a.max_pages)
+      N[j * a.tb + last] = need ? (page >= 0 ? page : part ? mine[j] : p0) : mine[j];
   }
   __syncthreads();
-  char* base = a.cache + (size_t)blockIdx.x * a.region_stride;
-  for (int j = 0; j < a.beams; ++j) {
-    if (copy[j].y < 0) continue;
+  const int nc = ncopy, region = blockIdx.x / parts, share = blockIdx.x % parts;
+  char* base = a.cache + (size_t)region * a.region_stride;
+  const size_t per = a.page_bytes / 16, i0 = per * share / parts, i1 = per * (share + 1) / parts;
+  for (int j = 0; j < nc; ++j) {
     const uint4* s = reinterpret_cast<const uint4*>(base + (size_t)copy[j].x * a.page_bytes);
     uint4* d = reinterpret_cast<uint4*>(base + (size_t)copy[j].y * a.page_bytes);
-    for (size_t i = t; i < a.page_bytes / 16; i += 256) d[i] = s[i];
+    for (size_t i = i0 + t; i < i1; i += kReorderThreads) d[i] = s[i];
   }
 }
 
 void cache_reorder(const ReorderArgs& a, hipStream_t st) {
-  k_cache_reorder<<<dim3(a.regions, a.n), 256, 0, st>>>(a);
+  // pages cut into parts of at least 4 KB until about four blocks per compute unit copy
+  const long long have = (long long)a.regions * a.n;
+  int parts = (int)std::max<long long>(1, std::min<long long>(1024 / have, (long long)(a.page_bytes / 4096)));
+  k_cache_reorder<<<dim3((unsigned)(a.regions * parts), a.n), kReorderThreads, 0, st>>>(a, parts);
 }
 
 }  // namespace wf

@@ -39,14 +39,16 @@ int check_dtype(int dtype, size_t& e) {
 }
 
 struct SelectSpace {
-  size_t pv, pi, lse, total;
+  size_t ps, pm, pv, pi, total;
 };
-SelectSpace select_space(size_t rows, size_t k) {
+SelectSpace select_space(int n, int beams, int vocab, int k) {
+  const size_t pieces = (size_t)n * beams * beam_pieces(vocab);
   SelectSpace s;
-  s.lse = 0;
-  s.pv = up256(rows * 8);
-  s.pi = s.pv + up256(rows * k * 4);
-  s.total = s.pi + up256(rows * k * 4);
+  s.ps = 0;
+  s.pm = up256(pieces * 8);
+  s.pv = s.pm + up256(pieces * 4);
+  s.pi = s.pv + up256(pieces * k * 4);
+  s.total = s.pi + up256(pieces * k * 4);
   return s;
 }
 int check_select(int n, int beams, int vocab, int k) {
@@ -90,7 +92,7 @@ int wf_beam_select_workspace_bytes(int n, int beams, int n_vocab, int k, size_t*
   return guarded([&] {
     if (int r = check_select(n, beams, n_vocab, k)) return r;
     if (!bytes) return bad("null bytes");
-    *bytes = select_space((size_t)n * beams, k).total;
+    *bytes = select_space(n, beams, n_vocab, k).total;
     return WF_OK;
   });
 }
@@ -108,7 +110,7 @@ int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t be
     if (req_stride < 0 || beam_stride < 0 || req_stride > ((int64_t)1 << 40) || beam_stride > ((int64_t)1 << 40))
       return bad("stride out of range");
     if (!workspace || !aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
-    const SelectSpace s = select_space((size_t)n * beams, k);
+    const SelectSpace s = select_space(n, beams, n_vocab, k);
     if (ws_bytes < s.total) return op_fail(WF_ESIZE, "workspace too small");
     char* w = static_cast<char*>(workspace);
     BeamSelectArgs a{};
@@ -122,7 +124,8 @@ int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t be
     a.beams = beams;
     a.vocab = n_vocab;
     a.k = k;
-    a.lse = reinterpret_cast<double*>(w + s.lse);
+    a.ps = reinterpret_cast<double*>(w + s.ps);
+    a.pm = reinterpret_cast<float*>(w + s.pm);
     a.pv = reinterpret_cast<float*>(w + s.pv);
     a.pi = reinterpret_cast<int*>(w + s.pi);
     a.out_score = out_score;

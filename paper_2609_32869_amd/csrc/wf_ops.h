@@ -22,14 +22,17 @@ struct BeamSelectArgs {
   const float* scores;      // (r, b) at r * beams + b
   const uint8_t* suppress;  // [vocab] nonzero: the column is left out, or null
   int n, beams, vocab, k;
-  // per logits row (r * beams + b): the row's k best as (logit, column), its log of the sum of exponentials
+  // per piece of a logits row ((r * beams + b) * pieces + piece): its k best as (logit, column; -1: none),
+  // its maximum and its sum of exponentials relative to that
   float* pv;
   int* pi;
-  double* lse;
+  float* pm;
+  double* ps;
   float* out_score;  // [n][k]
   int* out_beam;
   int* out_token;
 };
+int beam_pieces(int vocab);  // pieces of a row
 void beam_select(const BeamSelectArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- page tables after a choice of beams

@@ -7,65 +7,94 @@ of the tensors' device) and returns without waiting; workspaces and results come
 PyTorch's allocator, so concurrent calls and captured graphs each have their own.
 """
 import ctypes
+import functools
 
 import torch
 
-from .binding import WF_BF16, WF_F32, WfError, WfKv4, _ptr, load_library
+from .binding import WF_BF16, WF_F32, WfError, WfKv4, load_library
 
 _DTYPES = {torch.float32: WF_F32, torch.bfloat16: WF_BF16}
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
-def _check(lib, rc):
+def _check(rc):
     if rc != 0:
+        lib = load_library()
         msg = lib.wf_last_error(None)
         raise WfError(f"{lib.wf_strerror(rc).decode()} ({rc}): {msg.decode() if msg else ''}")
 
 
-def _need(ok, what):
-    if not ok:
-        raise WfError(f"invalid argument (-1): {what}")
+def _refuse(what):
+    raise WfError(f"invalid argument (-1): {what}")
 
 
-def _tensor(t, name, dtypes, shape=None, device=None, contiguous=True):
-    """Refuse a tensor of another kind; shape entries of None match any size."""
-    _need(isinstance(t, torch.Tensor), f"{name} must be a tensor")
-    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
-    _need(t.dtype in dtypes, f"{name} must be {' or '.join(str(d)[6:] for d in dtypes)}, not {str(t.dtype)[6:]}")
-    if shape is not None:
-        _need(t.dim() == len(shape) and all(s is None or s == g for s, g in zip(shape, t.shape)),
-              f"{name} must have shape {tuple('any' if s is None else s for s in shape)}, not {tuple(t.shape)}")
-    _need(t.is_cuda, f"{name} must be on the GPU")
-    _need(device is None or t.device == device, f"{name} is on another device")
-    _need(not contiguous or t.is_contiguous(), f"{name} must be contiguous")
-    return t
+def _tensor(t, name, dtype, shape, device):
+    """Refuse what is not a contiguous GPU tensor of this type, shape and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor):
+            _refuse(f"{name} must be a tensor")
+        if t.dtype != dtype:
+            _refuse(f"{name} must be {str(dtype)[6:]}, not {str(t.dtype)[6:]}")
+        if t.shape != shape:
+            _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        if t.device != device:
+            _refuse(f"{name} must be on {device}, not {t.device}")
+        _refuse(f"{name} must be contiguous")
+
+
+def _gpu(t, name, dims):
+    """The device of a GPU tensor of `dims` axes."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(f"{name} must be a tensor on the GPU")
+    if t.dim() != dims:
+        _refuse(f"{name} must have {dims} axes, not {t.dim()}")
+    return t.device
+
+
+def _type(t, name):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(f"{name} must be float32 or bfloat16, not {str(t.dtype)[6:]}")
+    return code
 
 
 class _On:
-    """The tensors' device made current and a stream of it, for the length of a call."""
+    """Where a call's work goes: `device` made current, `stream` or the current stream of it.  Memory from `empty` is
+    reused only behind the work that a given stream still has for it."""
+
+    __slots__ = ("device", "stream", "given", "back")
 
     def __init__(self, device, stream):
-        _need(stream is None or stream.device == device, "stream is of another device than the tensors")
-        self.guard, self.device, self.stream = torch.cuda.device(device), device, stream
+        self.device, self.given, self.back = device, None, None
+        if stream is not None:
+            if stream.device != device:
+                _refuse("stream is of another device than the tensors")
+            self.given = stream
 
     def __enter__(self):
-        self.guard.__enter__()
-        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        self.other = self.stream is not None and s != torch.cuda.current_stream(self.device)
-        self.s = s
+        here = torch.cuda.current_device()
+        if here != self.device.index:
+            self.back = here
+            torch.cuda.set_device(self.device)
+        self.stream = (self.given or torch.cuda.current_stream()).cuda_stream
         return self
 
     def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
-
-    def ptr(self):
-        return ctypes.c_void_p(self.s.cuda_stream)
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
 
     def empty(self, shape, dtype):
-        """Memory for this call's work: freed or reused only behind it on its stream."""
         t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other:
-            t.record_stream(self.s)
+        if self.given is not None:
+            t.record_stream(self.given)
         return t
+
+
+@functools.lru_cache(maxsize=256)
+def _select_bytes(n, beams, vocab, k):
+    nbytes = ctypes.c_size_t()
+    _check(load_library().wf_beam_select_workspace_bytes(n, beams, vocab, k, ctypes.byref(nbytes)))
+    return nbytes.value
 
 
 def beam_select(logits, scores, k, suppress=None, stream=None):
@@ -75,23 +104,24 @@ def beam_select(logits, scores, k, suppress=None, stream=None):
     suppress: uint8 [vocab] or None.  Returns (score fp32, beam int32, token int32), each [n, k].
     """
     lib = load_library()
-    _tensor(logits, "logits", tuple(_DTYPES), (None, None, None), contiguous=False)
+    dev = _gpu(logits, "logits", 3)
+    dtype = _type(logits, "logits")
     n, beams, vocab = logits.shape
-    dev = logits.device
-    _need(vocab <= 1 or logits.stride(2) == 1, "logits must be contiguous along the vocabulary")
-    _tensor(scores, "scores", torch.float32, (n, beams), dev)
+    sr, sb, sv = logits.stride()
+    if vocab > 1 and sv != 1:
+        _refuse("logits must be contiguous along the vocabulary")
+    _tensor(scores, "scores", _F32, (n, beams), dev)
     if suppress is not None:
-        _tensor(suppress, "suppress", torch.uint8, (vocab,), dev)
+        _tensor(suppress, "suppress", _U8, (vocab,), dev)
     k = int(k)
-    nbytes = ctypes.c_size_t()
-    _check(lib, lib.wf_beam_select_workspace_bytes(n, beams, vocab, k, ctypes.byref(nbytes)))
+    nbytes = _select_bytes(n, beams, vocab, k)
     with _On(dev, stream) as on:
-        score, beam = on.empty((n, k), torch.float32), on.empty((n, k), torch.int32)
-        token, ws = on.empty((n, k), torch.int32), on.empty(nbytes.value, torch.uint8)
-        _check(lib, lib.wf_beam_select(_ptr(logits), _DTYPES[logits.dtype], logits.stride(0), logits.stride(1), _ptr(scores),
-                                       _ptr(suppress), n, beams, vocab, k, _ptr(score), _ptr(beam), _ptr(token), _ptr(ws),
-                                       nbytes.value, on.ptr()))
-    return score, beam, token
+        score, beam, token = on.empty((3, n, k), _I32).unbind()
+        ws = on.empty(nbytes, _U8)
+        _check(lib.wf_beam_select(logits.data_ptr(), dtype, sr, sb, scores.data_ptr(),
+                                  None if suppress is None else suppress.data_ptr(), n, beams, vocab, k, score.data_ptr(),
+                                  beam.data_ptr(), token.data_ptr(), ws.data_ptr(), nbytes, on.stream))
+    return score.view(_F32), beam, token
 
 
 def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=None):
@@ -102,22 +132,32 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
     Returns the new tables.
     """
     lib = load_library()
-    _need(isinstance(cache, torch.Tensor) and cache.is_cuda, "cache must be a tensor on the GPU")
-    _need(cache.dim() >= 3 and cache.is_contiguous() and cache.numel() > 0, "cache must be contiguous [regions, pages, ...]")
-    dev = cache.device
-    _tensor(tables, "tables", torch.int32, (None, None, None), dev)
+    if not isinstance(cache, torch.Tensor) or not cache.is_cuda or cache.dim() < 3 or not cache.is_contiguous():
+        _refuse("cache must be a contiguous tensor [regions, pages, ...] on the GPU")
+    dev = _gpu(tables, "tables", 3)
     n, beams, max_pages = tables.shape
-    _tensor(parents, "parents", torch.int32, (n, beams), dev)
-    _tensor(lens, "lens", torch.int32, (n,), dev)
-    _tensor(pool, "pool", torch.int32, (n, None), dev)
+    if dev != cache.device:
+        _refuse("tables must be on the cache's device")
+    if pool.dim() != 2:
+        _refuse("pool must have 2 axes")
+    pool_pages = pool.shape[1]
+    _tensor(tables, "tables", _I32, (n, beams, max_pages), dev)
+    _tensor(parents, "parents", _I32, (n, beams), dev)
+    _tensor(lens, "lens", _I32, (n,), dev)
+    _tensor(pool, "pool", _I32, (n, pool_pages), dev)
     regions, pages = cache.shape[:2]
-    page = cache[0, 0].numel() * cache.element_size()
+    if regions == 0 or pages == 0:
+        _refuse("cache must hold a page")
+    region = cache.numel() // regions * cache.element_size()
     with _On(dev, stream) as on:
-        new = on.empty((n, beams, max_pages), torch.int32)
-        _check(lib, lib.wf_cache_reorder(_ptr(cache), regions, pages * page, pages, page, _ptr(tables), _ptr(new), n, beams,
-                                         max_pages, int(page_tokens), _ptr(parents), _ptr(lens), _ptr(pool), pool.shape[1],
-                                         on.ptr()))
+        new = on.empty((n, beams, max_pages), _I32)
+        _check(lib.wf_cache_reorder(cache.data_ptr(), regions, region, pages, region // pages, tables.data_ptr(), new.data_ptr(),
+                                    n, beams, max_pages, int(page_tokens), parents.data_ptr(), lens.data_ptr(),
+                                    pool.data_ptr(), pool_pages, on.stream))
     return new
+
+
+_Strides = ctypes.c_int64 * 3
 
 
 class AcousticCache4:
@@ -127,52 +167,70 @@ class AcousticCache4:
         self.lib = load_library()
         self.entries, self.n_head, self.n_frames = int(entries), int(n_head), int(n_frames)
         nbytes = ctypes.c_size_t()
-        _check(self.lib, self.lib.wf_kv4_bytes(self.entries, self.n_head, self.n_frames, ctypes.byref(nbytes)))
-        self.data = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
-        _need(self.data.is_cuda, "device must be a GPU")
+        _check(self.lib.wf_kv4_bytes(self.entries, self.n_head, self.n_frames, ctypes.byref(nbytes)))
+        self.data = torch.empty(nbytes.value, dtype=_U8, device=device)
+        if not self.data.is_cuda:
+            _refuse("device must be a GPU")
         self.device = self.data.device
-        self.c = WfKv4(self.data.data_ptr(), self.entries, self.n_head, self.n_frames)
+        self._c = WfKv4(self.data.data_ptr(), self.entries, self.n_head, self.n_frames)
+        self._ref = ctypes.byref(self._c)
+        self._spaces = {}  # workspace bytes of (n, rows)
 
     def _lens(self, lens, n):
-        if lens is not None:
-            _tensor(lens, "lens", torch.int32, (n,), self.device)
-        return _ptr(lens)
+        if lens is None:
+            return None
+        _tensor(lens, "lens", _I32, (n,), self.device)
+        return lens.data_ptr()
 
-    def _rows(self, t, name, shape, dtypes=tuple(_DTYPES)):
-        _tensor(t, name, dtypes, shape, self.device, contiguous=False)
-        _need(t.stride(3) == 1, f"{name} must be contiguous along its last axis")
-        return (ctypes.c_int64 * 3)(*t.stride()[:3])
+    def _rows(self, t, name, axis1):
+        """Type and strides of [n, axis1 (None: any), n_head, 64] with the last axis contiguous."""
+        if _gpu(t, name, 4) != self.device:
+            _refuse(f"{name} must be on {self.device}, not {t.device}")
+        shape = t.shape
+        if shape[2] != self.n_head or shape[3] != 64 or (axis1 is not None and shape[1] != axis1):
+            _refuse(f"{name} must have shape (n, {'rows' if axis1 is None else axis1}, {self.n_head}, 64), not {tuple(shape)}")
+        s = t.stride()
+        if s[3] != 1:
+            _refuse(f"{name} must be contiguous along its last axis")
+        return _type(t, name), _Strides(*s[:3])
 
     def store(self, slot0, k, v, lens=None, stream=None):
         """Entries slot0 .. from k, v: fp32 or bf16 [n, n_frames, n_head, 64] (any strides but the last), of which the
         first lens[r] frames (int32 [n], None: all) are given and the others hold zeros."""
-        shape = (None, self.n_frames, self.n_head, 64)
-        ks = self._rows(k, "k", shape)
-        vs = self._rows(v, "v", (k.shape[0],) + shape[1:], k.dtype)
+        dtype, ks = self._rows(k, "k", self.n_frames)
+        vtype, vs = self._rows(v, "v", self.n_frames)
+        n = k.shape[0]
+        if vtype != dtype or v.shape[0] != n:
+            _refuse("v must have k's type and shape")
         with _On(self.device, stream) as on:
-            _check(self.lib, self.lib.wf_kv4_store(ctypes.byref(self.c), int(slot0), k.shape[0], _ptr(k), ks, _ptr(v), vs,
-                                                   _DTYPES[k.dtype], self._lens(lens, k.shape[0]), on.ptr()))
+            _check(self.lib.wf_kv4_store(self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype,
+                                         self._lens(lens, n), on.stream))
 
     def load(self, slot0, n, dtype=torch.float32, stream=None):
         """The keys and values that entries slot0 .. slot0 + n - 1 hold: two tensors [n, n_frames, n_head, 64]."""
-        _need(dtype in _DTYPES, "dtype must be float32 or bfloat16")
-        _need(0 < n <= self.entries and 0 <= slot0 <= self.entries - n, "entries out of range")
+        if dtype not in _DTYPES:
+            _refuse("dtype must be float32 or bfloat16")
+        if not (0 < n <= self.entries and 0 <= slot0 <= self.entries - n):
+            _refuse("entries out of range")
         with _On(self.device, stream) as on:
             k = on.empty((n, self.n_frames, self.n_head, 64), dtype)
             v = on.empty((n, self.n_frames, self.n_head, 64), dtype)
-            _check(self.lib, self.lib.wf_kv4_load(ctypes.byref(self.c), int(slot0), n, _ptr(k), _ptr(v), _DTYPES[dtype],
-                                                  on.ptr()))
+            _check(self.lib.wf_kv4_load(self._ref, int(slot0), n, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], on.stream))
         return k, v
 
     def attend(self, slot0, q, lens=None, stream=None):
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, n_head, 64], any strides but the last) over the first lens[r]
         frames (int32 [n], None: all) of entries slot0 ..: [n, rows, n_head, 64] in q's type."""
-        qs = self._rows(q, "q", (None, None, self.n_head, 64))
+        dtype, qs = self._rows(q, "q", None)
         n, rows = q.shape[:2]
-        nbytes = ctypes.c_size_t()
-        _check(self.lib, self.lib.wf_kv4_attend_workspace_bytes(ctypes.byref(self.c), n, rows, ctypes.byref(nbytes)))
+        need = self._spaces.get((n, rows))
+        if need is None:
+            nbytes = ctypes.c_size_t()
+            _check(self.lib.wf_kv4_attend_workspace_bytes(self._ref, n, rows, ctypes.byref(nbytes)))
+            need = self._spaces[n, rows] = nbytes.value
         with _On(self.device, stream) as on:
-            out, ws = on.empty((n, rows, self.n_head, 64), q.dtype), on.empty(max(nbytes.value, 1), torch.uint8)
-            _check(self.lib, self.lib.wf_kv4_attend(ctypes.byref(self.c), int(slot0), n, _ptr(q), qs, rows, _DTYPES[q.dtype],
-                                                    self._lens(lens, n), _ptr(out), _ptr(ws), nbytes.value, on.ptr()))
+            out = on.empty((n, rows, self.n_head, 64), q.dtype)
+            ws = on.empty(need, _U8).data_ptr() if need else None
+            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, self._lens(lens, n),
+                                          out.data_ptr(), ws, need, on.stream))
         return out

@@ -415,7 +415,8 @@ int wf_kv4_bytes(int entries, int n_head, int n_frames, size_t* bytes);
  * k, v: device, fp32 or bf16; element (r, f, h, d) lies r * stride[0] + f * stride[1] +
  *   h * stride[2] + d elements in (strides >= 0, host arrays of three).
  * lens: device int32 [n], the frames of each that are given, taken as the nearest of
- *   [0, n_frames], or NULL (all).  Frames past them are not read and hold zeros.
+ *   [0, n_frames], or NULL (all).  What k and v hold past them is not used; the cache
+ *   holds zeros there.
  */
 int wf_kv4_store(const wf_kv4* c, int slot0, int n, const void* k, const int64_t* k_stride, const void* v,
                  const int64_t* v_stride, int dtype, const int32_t* lens, void* stream);

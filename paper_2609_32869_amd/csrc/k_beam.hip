@@ -12,33 +12,56 @@ namespace wf {
 // piece's maximum and sum of exponentials; the beams meet in 64-bit scores in the merge.
 //
 // Row kernel: a block per (piece of kBeamPiece columns, row), one read of the logits into
-// registers, 32 per thread.  The k-th best of a wave's 64 per-lane bests, found bit by bit
-// with ballots, bounds the k-th best of the piece from below: the best of the four waves'
-// bounds leaves a handful of survivors (k lanes a wave at most), which are ranked by
-// counting.  Values as order-preserving integers; equal ones by column, so that any
-// number of ties stays within the survivors' array.
+// registers, 32 per thread.  At least k lanes of a wave hold a value of at least the k-th
+// best of the 64 per-lane maxima, so that maximum, found with ballots to as many bits as
+// leave few lanes above it, bounds the piece's k-th best from below; the best of the four
+// waves' bounds leaves a handful of survivors (KL lanes a wave at most), which are ranked by
+// counting.  Equal values by column, so that any number of ties stays within the array.
 constexpr int kBeamRegs = 32;
 constexpr int kBeamPiece = 256 * kBeamRegs;
-constexpr int kBeamList = 4 * kBeamRegs * kMaxCand;  // survivors at most: four waves of k lanes
 
-// Larger value, larger integer; NaN and -inf (no candidates) at 0.
+// Larger value, larger integer, both zeros alike; NaN and -inf (no candidates) at 0.
 __device__ __forceinline__ uint32_t order_of(float x) {
-  const uint32_t u = __float_as_uint(x);
+  const uint32_t u = __float_as_uint(x + 0.f);  // -0 + 0 = +0
   return !(x > -INFINITY) ? 0u : u >> 31 ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o); }
 
-// r-th largest of the active lanes' words (r <= their number); afterwards r is its rank
-// among the lanes that hold it, and those are the active ones.
-__device__ __forceinline__ uint32_t wave_kth(uint32_t w, bool& active, int& r) {
-  uint32_t t = 0;
-  for (int bit = 31; bit >= 0; --bit) {
+// Bits of the r-th largest of the active lanes' words, from `high` down to `low`, appended to
+// t; r becomes the rank among the lanes that hold those bits.
+template <int high, int low>
+__device__ __forceinline__ void wave_kth(uint32_t w, bool active, uint32_t& t, int& r) {
+#pragma unroll
+  for (int bit = high; bit >= low; --bit) {
     const int c = __popcll(__ballot(active && (w >> bit) == (t >> bit | 1u)));
-    if (c >= r) t |= 1u << bit;
-    else r -= c;
+    const bool up = c >= r;
+    t = up ? t | 1u << bit : t;
+    r = up ? r : r - c;
   }
-  active = active && w == t;
-  return t;
+}
+// sum over a row of 16 lanes by DPP moves of the two halves, in every lane of the row
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sum16d(double v) {
+  v += dpp_d<kDppXor1>(v);
+  v += dpp_d<kDppXor2>(v);
+  v += dpp_d<kDppHalfMirror>(v);
+  return v + dpp_d<kDppMirror>(v);
+}
+__device__ __forceinline__ double lane_d(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(u >> 32), l);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// whole-wave sum, uniform result
+__device__ __forceinline__ double wave_sum_d(double v) {
+  v = sum16d(v);
+  return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
 }
 
 // 8 consecutive logits from column v on; columns past the row and suppressed ones are
@@ -76,56 +99,58 @@ __device__ __forceinline__ void logits8(const T* x, const uint8_t* sup, int v, i
   }
 }
 
-template <typename T>
+// KL: lanes of a wave that survive at most, k <= KL
+template <typename T, int KL>
 __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
-  __shared__ uint32_t lo[kBeamList];
-  __shared__ int lc[kBeamList];
+  constexpr int kSeg = KL * kBeamRegs;  // a wave's survivors
+  __shared__ __align__(16) uint64_t keys[4 * kSeg];
   __shared__ uint32_t tv[4], ti[4];
   __shared__ float wm[4];
   __shared__ double ws[4];
-  __shared__ int count;
+  __shared__ int wn[4];
   const int row = blockIdx.x, r = row / a.beams, b = row % a.beams, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb;
   const int v0 = blockIdx.y * kBeamPiece + 8 * t;
-  if (t == 0) count = 0;
   float y[kBeamRegs];
 #pragma unroll
   for (int i = 0; i < kBeamRegs / 8; ++i) logits8(x, a.suppress, v0 + 2048 * i, a.vocab, y + 8 * i);
-  // maximum and sum of exponentials, eight at a time in 32 bits, then 64
   float m = -INFINITY;
-  uint32_t best = 0;
-  int at = 0;
 #pragma unroll
-  for (int i = 0; i < kBeamRegs; ++i) {
-    m = fmaxf(m, y[i]);
-    const uint32_t o = order_of(y[i]);
-    if (o > best) {  // the first of equal values
-      best = o;
-      at = v0 + 2048 * (i / 8) + i % 8;
+  for (int i = 0; i < kBeamRegs; ++i) m = fmaxf(m, y[i]);
+  // the wave's bound (0: fewer than k lanes hold anything)
+  const uint32_t best = order_of(m);
+  bool active = best != 0;
+  uint32_t bound = 0, col = ~0u;
+  if (__popcll(__ballot(active)) >= a.k) {
+    int need = a.k;
+    wave_kth<31, 16>(best, active, bound, need);
+    if (__popcll(__ballot(best >= bound)) > KL) wave_kth<15, 0>(best, active, bound, need);
+    if (__popcll(__ballot(best >= bound)) > KL) {  // more equal maxima than that: the first of them by column
+      int at = 0;
+#pragma unroll
+      for (int i = kBeamRegs - 1; i >= 0; --i)
+        if (y[i] == m) at = v0 + 2048 * (i / 8) + i % 8;
+      uint32_t inv = 0;
+      active = best == bound;
+      wave_kth<31, 0>(~(uint32_t)at, active, inv, need);
+      col = ~inv;
     }
   }
+  // sum of exponentials relative to the lane's maximum, eight at a time in 32 bits, then 64
+  constexpr float log2e = 1.44269504088896f;
   const float base = m == -INFINITY ? 0.f : m;
   double sum = 0;
 #pragma unroll
   for (int i = 0; i < kBeamRegs; i += 8) {
     float p = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p += __expf(y[i + e] - base);
+    for (int e = 0; e < 8; ++e) p += __builtin_amdgcn_exp2f((y[i + e] - base) * log2e);
     sum += (double)p;
   }
+  // to the wave's maximum; a lane of no values holds 0, or NaN, which stays
   const float M = wave_max(m);
-  // rescaled to the wave's maximum; a lane of no values adds nothing, a NaN stays
-  sum *= (double)__expf((m == -INFINITY ? M : m) - (M == -INFINITY ? 0.f : M));
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-  // the wave's bound: its k-th best lane
-  int need = a.k;
-  bool active = best != 0;
-  uint32_t bound = 0, col = ~0u;
-  if (__popcll(__ballot(active)) >= need) {
-    bound = wave_kth(best, active, need);
-    if (need < __popcll(__ballot(active))) col = ~wave_kth(~(uint32_t)at, active, need);  // lowest columns first
-  }
+  if (m != -INFINITY) sum *= (double)__builtin_amdgcn_exp2f((m - M) * log2e);
+  sum = wave_sum_d(sum);
   if (lane == 0) {
     tv[w] = bound;
     ti[w] = col;
@@ -139,27 +164,50 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
       bound = tv[i];
       col = ti[i];
     }
+  int mine = 0;  // the wave's survivors so far
+  if (__ballot(best >= max(bound, 1u)) != 0) {
+    const float least = value_of(bound);
 #pragma unroll
-  for (int i = 0; i < kBeamRegs; ++i) {
-    const uint32_t o = order_of(y[i]);
-    const int c = v0 + 2048 * (i / 8) + i % 8;
-    if (o != 0 && (o > bound || (o == bound && (uint32_t)c <= col))) {
-      const int j = atomicAdd(&count, 1);
-      lo[j] = o;
-      lc[j] = c;
+    for (int i = 0; i < kBeamRegs; ++i) {
+      const int cc = v0 + 2048 * (i / 8) + i % 8;
+      const bool in = bound == 0 ? y[i] > -INFINITY : y[i] > least || (y[i] == least && (uint32_t)cc <= col);
+      const uint64_t mask = __ballot(in);
+      if (mask != 0) {  // uniform
+        if (in) keys[w * kSeg + mine + __popcll(mask & (((uint64_t)1 << lane) - 1))] = (uint64_t)order_of(y[i]) << 32 | (uint32_t)~cc;
+        mine += __popcll(mask);
+      }
     }
   }
+  if (lane == 0) wn[w] = mine;
   __syncthreads();
   const size_t piece = (size_t)row * gridDim.y + blockIdx.y;
-  const int n = count;
+  // rank by counting larger keys (a larger value, then a lower column)
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) n += wn[i];
   for (int i = t; i < n; i += 256) {
-    const uint32_t o = lo[i];
-    const int c = lc[i];
+    int s = i, q = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (q == j && s >= wn[j]) {
+        s -= wn[j];
+        q = j + 1;
+      }
+    const uint64_t key = keys[q * kSeg + s];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += lo[j] > o || (lo[j] == o && lc[j] < c);
+    for (int j = 0; j < 4; ++j) {
+      const int e = wn[j];
+      for (int u = 0; u < e; u += 4) {  // entries past e lie in the segment (kSeg is a multiple of 4) and do not count
+        uint64_t z[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) z[d] = keys[j * kSeg + u + d];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) rank += u + d < e && z[d] > key;
+      }
+    }
     if (rank < a.k) {
-      a.pv[piece * a.k + rank] = value_of(o);
-      a.pi[piece * a.k + rank] = c;
+      a.pv[piece * a.k + rank] = value_of((uint32_t)(key >> 32));
+      a.pi[piece * a.k + rank] = (int)~(uint32_t)key;
     }
   }
   for (int i = n + t; i < a.k; i += 256) {
@@ -178,10 +226,11 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
 }
 
 // Merge: a block per request.  16 lanes a row join its pieces' sums; then the pieces'
-// candidates by 64-bit score.  A wave's k-th best lane (scores rounded to 32 bits, which
-// keeps the order) bounds the k-th best again; more survivors than the array holds, which
-// takes that many equal scores, are chosen one by one.
-constexpr int kMergeList = 2048;
+// candidates by 64-bit score, the first four of a thread held in registers.  The k-th best of a
+// wave's lanes (scores rounded to 32 bits, which keeps the order, to 16 bits of that)
+// bounds the k-th best again; more survivors than the array holds, which takes that many
+// nearly equal scores, are chosen one by one.
+constexpr int kMergeList = 1024, kMergeRegs = 4;
 // ties: order = beam * 2^20 + column
 __device__ __forceinline__ bool ahead(double s, int o, double t, int p) { return s > t || (s == t && o < p); }
 
@@ -190,62 +239,79 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
   __shared__ int lo[kMergeList], bo[4], count;
   __shared__ uint32_t tv[4];
   const int r = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (t == 0) count = 0;
-  {
-    const int b = min(t >> 4, a.beams - 1);
-    const size_t row = (size_t)r * a.beams + b;
-    float m = -INFINITY;
-    for (int p = t & 15; p < np; p += 16) m = fmaxf(m, a.pm[row * np + p]);
-    m = max16(m);
-    double s = 0;
-    for (int p = t & 15; p < np; p += 16) {
-      const float pm = a.pm[row * np + p];
-      const double ps = a.ps[row * np + p];
-      s += pm == -INFINITY && ps == 0 ? 0 : ps * exp((double)pm - (double)m);
-    }
+  const int per = np * a.k, total = a.beams * per;
+  const size_t first = (size_t)r * total;
+  float xv[kMergeRegs];
+  int xi[kMergeRegs];
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o);
-    const float sc = a.scores[row];
+  for (int i = 0; i < kMergeRegs; ++i) {
+    const size_t at = first + min(t + 256 * i, total - 1);
+    xv[i] = a.pv[at];
+    xi[i] = a.pi[at];
+  }
+  {
+    const int b = min(t >> 4, a.beams - 1), p0 = t & 15;
+    const size_t row = ((size_t)r * a.beams + b) * np;
+    const float sc = a.scores[(size_t)r * a.beams + b], m0 = a.pm[row + min(p0, np - 1)];
+    const double s0 = a.ps[row + min(p0, np - 1)];
+    float m = m0;
+    for (int p = p0 + 16; p < np; p += 16) m = fmaxf(m, a.pm[row + p]);
+    m = max16(m);
+    auto part = [&](float pm, double ps) { return pm == -INFINITY && ps == 0 ? 0 : ps * exp((double)pm - (double)m); };
+    double s = p0 < np ? part(m0, s0) : 0;
+    for (int p = p0 + 16; p < np; p += 16) s += part(a.pm[row + p], a.ps[row + p]);
+    s = sum16d(s);
     // score = (x - m) + (s_b - log sum): the difference is exact enough at any magnitude; NaN where the row or the
     // beam offers nothing
-    if ((t & 15) == 0 && t >> 4 < a.beams) {
+    if (p0 == 0 && t >> 4 < a.beams) {
       top[b] = m;
       rest[b] = sc < INFINITY ? (double)sc - log(s) : NAN;
     }
   }
+  if (t == 0) count = 0;
   __syncthreads();
-  const int per = np * a.k, total = a.beams * per;
-  const size_t first = (size_t)r * total;
-  // score and order of candidate i; false: none
-  auto cand = [&](int i, double& s, int& o) {
-    const int b = i / per, c = a.pi[first + i];
-    s = ((double)a.pv[first + i] - top[b]) + rest[b];
+  // score and order of candidate i, whose logit and column are x and c; false: none
+  auto score = [&](int i, float x, int c, double& s, int& o) {
+    const int b = min(i, total - 1) / per;
+    s = ((double)x - top[b]) + rest[b];
     o = b << 20 | c;
-    return c >= 0 && s > -INFINITY;
+    return i < total && c >= 0 && s > -INFINITY;
   };
+  double rs[kMergeRegs];
+  int ro[kMergeRegs];
+  bool rl[kMergeRegs];
   uint32_t best = 0;
-  for (int i = t; i < total; i += 256) {
+#pragma unroll
+  for (int i = 0; i < kMergeRegs; ++i) {
+    rl[i] = score(t + 256 * i, xv[i], xi[i], rs[i], ro[i]);
+    if (rl[i]) best = max(best, order_of((float)rs[i]));
+  }
+  for (int i = t + 256 * kMergeRegs; i < total; i += 256) {
     double s;
     int o;
-    if (cand(i, s, o)) best = max(best, order_of((float)s));
+    if (score(i, a.pv[first + i], a.pi[first + i], s, o)) best = max(best, order_of((float)s));
   }
-  int need = a.k;
-  bool active = best != 0;
+  const bool active = best != 0;
   uint32_t bound = 0;
-  if (__popcll(__ballot(active)) >= need) bound = wave_kth(best, active, need);
+  int need = a.k;
+  if (__popcll(__ballot(active)) >= need) wave_kth<31, 16>(best, active, bound, need);
   if (lane == 0) tv[w] = bound;
   __syncthreads();
   bound = max(max(tv[0], tv[1]), max(tv[2], tv[3]));
-  for (int i = t; i < total; i += 256) {
+  auto keep = [&](double s, int o) {
+    const int j = atomicAdd(&count, 1);
+    if (j < kMergeList) {
+      ls[j] = s;
+      lo[j] = o;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kMergeRegs; ++i)
+    if (rl[i] && order_of((float)rs[i]) >= bound) keep(rs[i], ro[i]);
+  for (int i = t + 256 * kMergeRegs; i < total; i += 256) {
     double s;
     int o;
-    if (cand(i, s, o) && order_of((float)s) >= bound) {
-      const int j = atomicAdd(&count, 1);
-      if (j < kMergeList) {
-        ls[j] = s;
-        lo[j] = o;
-      }
-    }
+    if (score(i, a.pv[first + i], a.pi[first + i], s, o) && order_of((float)s) >= bound) keep(s, o);
   }
   __syncthreads();
   const int n = count;
@@ -256,9 +322,21 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
   };
   if (n <= kMergeList) {
     for (int i = t; i < n; i += 256) {
+      const double s = ls[i];
+      const int o = lo[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) rank += ahead(ls[j], lo[j], ls[i], lo[i]);
-      if (rank < a.k) put(rank, ls[i], lo[i]);
+      for (int j = 0; j < n; j += 4) {  // entries past n lie in the array and do not count
+        double z[4];
+        int q[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          z[d] = ls[j + d];
+          q[d] = lo[j + d];
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) rank += j + d < n && ahead(z[d], q[d], s, o);
+      }
+      if (rank < a.k) put(rank, s, o);
     }
     for (int i = n + t; i < a.k; i += 256) put(i, -INFINITY, -1);
     return;
@@ -271,7 +349,7 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
     for (int i = t; i < total; i += 256) {
       double s;
       int o;
-      if (cand(i, s, o) && ahead(ps, po, s, o) && ahead(s, o, s1, o1)) {
+      if (score(i, a.pv[first + i], a.pi[first + i], s, o) && ahead(ps, po, s, o) && ahead(s, o, s1, o1)) {
         s1 = s;
         o1 = o;
       }
@@ -307,8 +385,13 @@ int beam_pieces(int vocab) { return (vocab + kBeamPiece - 1) / kBeamPiece; }
 void beam_select(const BeamSelectArgs& a, hipStream_t st) {
   const int np = beam_pieces(a.vocab);
   const dim3 grid(a.n * a.beams, np);
-  if (a.bf16_logits) k_beam_rows<bf16><<<grid, 256, 0, st>>>(a);
-  else k_beam_rows<float><<<grid, 256, 0, st>>>(a);
+  auto rows = [&](auto tag) {
+    using T = decltype(tag);
+    if (a.k <= 16) k_beam_rows<T, 16><<<grid, 256, 0, st>>>(a);
+    else k_beam_rows<T, kMaxCand><<<grid, 256, 0, st>>>(a);
+  };
+  if (a.bf16_logits) rows(bf16{});
+  else rows(0.f);
   k_beam_merge<<<a.n, 256, 0, st>>>(a, np);
 }
 

@@ -5,6 +5,8 @@
 // (keys: 32 of a frame's 64 dims; values: 32 frames of one dim), so the eight elements
 // that a lane gives a matrix instruction have one scale and one instruction turns two
 // codes and the scale into two bf16 values, exactly.
+#include <algorithm>
+
 #include "wf_operand.h"
 #include "wf_ops.h"
 
@@ -45,33 +47,78 @@ __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0
 __device__ __forceinline__ float scale_f(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // ---------------------------------------------------------------- store
-// A wave per (entry, head, 32-frame group); frames at or beyond the request's length are
-// not read and stand for zero.
+// A wave per (entry, head, 32-frame group).  Every load is issued before the first use and
+// without a condition (frames at or beyond the length re-read the last given one, or the
+// first, and count as zero).
+template <int N>
+__device__ __forceinline__ void ld_vals(const float* p, int vec, float* o) {
+  if (vec) {
+#pragma unroll
+    for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(o + j) = *reinterpret_cast<const float4*>(p + j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = p[j];
+  }
+}
+// bf16: raw bits, two values a word
+template <int N>
+__device__ __forceinline__ void ld_bits(const bf16* p, int vec, uint32_t* o) {
+  if (vec) {
+    if constexpr (N == 4) *reinterpret_cast<uint2*>(o) = *reinterpret_cast<const uint2*>(p);
+    else
+#pragma unroll
+      for (int j = 0; j < N / 2; j += 4) *reinterpret_cast<uint4*>(o + j) = *reinterpret_cast<const uint4*>(p + 2 * j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) o[j / 2] = (uint32_t)p[j].u | (uint32_t)p[j + 1].u << 16;
+  }
+}
+// N consecutive source elements as they were loaded, converted where they are used.
+template <typename T, int N>
+struct Raw;
+template <int N>
+struct Raw<float, N> {
+  float v[N];
+  __device__ __forceinline__ void load(const float* p, int vec) { ld_vals<N>(p, vec, v); }
+  __device__ __forceinline__ float get(int j) const { return v[j]; }
+};
+template <int N>
+struct Raw<bf16, N> {
+  uint32_t v[N / 2];
+  __device__ __forceinline__ void load(const bf16* p, int vec) { ld_bits<N>(p, vec, v); }
+  __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16); }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
   const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, r = blockIdx.z;
   if (g >= a.c.groups) return;
-  const int len = a.lens ? min(max(a.lens[r], 0), a.c.frames) : a.c.frames;
+  const int len = a.lens ? min(max(a.lens[r], 0), a.c.frames) : a.c.frames, top = max(len - 1, 0);
   uint8_t* out = a.c.base + (((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups + g) * kKv4Group;
-  const T* K = reinterpret_cast<const T*>(a.k) + r * a.kr + head * a.kh;
-  const T* V = reinterpret_cast<const T*>(a.v) + r * a.vr + head * a.vh;
+  const T* K = reinterpret_cast<const T*>(a.k) + r * a.kr + head * a.kh + 16 * kg;
+  const T* V = reinterpret_cast<const T*>(a.v) + r * a.vr + head * a.vh + 4 * n;
+  Raw<T, 16> k[2];
+  Raw<T, 4> v[8];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) k[t].load(K + min(g * 32 + 16 * t + n, top) * a.kf, a.vec);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j].load(V + min(g * 32 + 8 * kg + j, top) * a.vf, a.vec);
+  uint2 kc[2];
+  uint32_t ks[2], vc[4], vs = 0;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int f = g * 32 + 16 * t + n;
+    const bool in = g * 32 + 16 * t + n < len;
     float x[16];
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      x[j] = f < len ? to_f(K[(long long)f * a.kf + 16 * kg + j]) : 0.f;
+      x[j] = in ? k[t].get(j) : 0.f;
       m = umax(m, mag(x[j]));
     }
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-    const uint32_t sb = scale_of(__uint_as_float(m));
-    const float s = scale_f(sb);
-    uint2 c = make_uint2(codes8(x, s), codes8(x + 8, s));
-    *reinterpret_cast<uint2*>(out + 16 * lane + 8 * t) = c;
-    if ((kg & 1) == 0) out[kKv4KeyScale + 32 * (kg >> 1) + 2 * n + t] = (uint8_t)sb;
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));  // the block's other 16 dims
+    ks[t] = scale_of(__uint_as_float(m));
+    kc[t] = make_uint2(codes8(x, scale_f(ks[t])), codes8(x + 8, scale_f(ks[t])));
   }
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) {
@@ -79,16 +126,19 @@ __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int f = g * 32 + 8 * kg + j;
-      x[j] = f < len ? to_f(V[(long long)f * a.vf + 16 * dt + n]) : 0.f;
+      x[j] = g * 32 + 8 * kg + j < len ? v[j].get(dt) : 0.f;
       m = umax(m, mag(x[j]));
     }
     m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
     m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
     const uint32_t sb = scale_of(__uint_as_float(m));
-    *reinterpret_cast<uint32_t*>(out + kKv4Values + 16 * lane + 4 * dt) = codes8(x, scale_f(sb));
-    if (kg == 0) out[kKv4ValueScale + 4 * n + dt] = (uint8_t)sb;
+    vc[dt] = codes8(x, scale_f(sb));
+    vs |= sb << (8 * dt);
   }
+  *reinterpret_cast<uint4*>(out + 16 * lane) = make_uint4(kc[0].x, kc[0].y, kc[1].x, kc[1].y);
+  *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = make_uint4(vc[0], vc[1], vc[2], vc[3]);
+  if ((kg & 1) == 0) *reinterpret_cast<uint16_t*>(out + kKv4KeyScale + 32 * (kg >> 1) + 2 * n) = (uint16_t)(ks[0] | ks[1] << 8);
+  if (kg == 0) *reinterpret_cast<uint32_t*>(out + kKv4ValueScale + 4 * n) = vs;
 }
 
 void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
@@ -98,36 +148,47 @@ void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- load
+// A wave per (entry, head, 32-frame group), the store's lanes.
+__device__ __forceinline__ void st8(float* p, bf16x8 x) {
+  *reinterpret_cast<float4*>(p) = make_float4((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4((float)x[4], (float)x[5], (float)x[6], (float)x[7]);
+}
+__device__ __forceinline__ void st8(bf16* p, bf16x8 x) { *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, x); }
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void st4(float* p, bf16x4 x) {
+  *reinterpret_cast<float4*>(p) = make_float4((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
+}
+__device__ __forceinline__ void st4(bf16* p, bf16x4 x) { *reinterpret_cast<uint2*>(p) = __builtin_bit_cast(uint2, x); }
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_load(Kv4LoadArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
   const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, r = blockIdx.z;
   if (g >= a.c.groups) return;
   const uint8_t* in = a.c.base + (((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups + g) * kKv4Group;
-  T* K = reinterpret_cast<T*>(a.k);
-  T* V = reinterpret_cast<T*>(a.v);
-  auto at = [&](int f, int d) { return (((size_t)r * a.c.frames + f) * a.c.n_head + head) * kHeadDim + d; };
+  const uint4 k = *reinterpret_cast<const uint4*>(in + 16 * lane), v = *reinterpret_cast<const uint4*>(in + kKv4Values + 16 * lane);
+  const uint32_t ks = *reinterpret_cast<const uint16_t*>(in + kKv4KeyScale + 32 * (kg >> 1) + 2 * n);
+  const uint32_t vs = *reinterpret_cast<const uint32_t*>(in + kKv4ValueScale + 4 * n);
+  const size_t pitch = (size_t)a.c.n_head * kHeadDim, at = ((size_t)r * a.c.frames + g * 32) * pitch + head * kHeadDim;
+  T* K = reinterpret_cast<T*>(a.k) + at + 16 * kg;
+  T* V = reinterpret_cast<T*>(a.v) + at + 4 * n;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int f = g * 32 + 16 * t + n;
-    const float s = scale_f(in[kKv4KeyScale + 32 * (kg >> 1) + 2 * n + t]);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bf16x8 x = values8(*reinterpret_cast<const uint32_t*>(in + 16 * lane + 8 * t + 4 * h), s);
-      if (f < a.c.frames)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) K[at(f, 16 * kg + 8 * h + j)] = from_f<T>((float)x[j]);
+    const int f = 16 * t + n;
+    const float s = scale_f(t ? ks >> 8 : ks & 255);
+    if (g * 32 + f < a.c.frames) {
+      st8(K + f * pitch, values8(t ? k.z : k.x, s));
+      st8(K + f * pitch + 8, values8(t ? k.w : k.y, s));
     }
   }
+  bf16x8 x[4];
+  const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt) {
-    const bf16x8 x = values8(*reinterpret_cast<const uint32_t*>(in + kKv4Values + 16 * lane + 4 * dt),
-                             scale_f(in[kKv4ValueScale + 4 * n + dt]));
+  for (int dt = 0; dt < 4; ++dt) x[dt] = values8(vw[dt], scale_f(vs >> (8 * dt) & 255));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int f = g * 32 + 8 * kg + j;
-      if (f < a.c.frames) V[at(f, 16 * dt + n)] = from_f<T>((float)x[j]);
-    }
+  for (int j = 0; j < 8; ++j) {
+    const int f = 8 * kg + j;
+    if (g * 32 + f < a.c.frames) st4(V + f * pitch, bf16x4{x[0][j], x[1][j], x[2][j], x[3][j]});
   }
 }
 
@@ -138,7 +199,17 @@ void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- attention
-// Block (head, request, 16 query rows), four waves; a wave takes every fourth group.
+// Block (head, request, chunk of the groups) x (16 query rows), NW waves; a wave takes
+// steps of KS groups, the next step's codes in flight while it multiplies the current one.
+//   scores   S^T = K q^T per 16-frame tile (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets
+//            row n of frames 4 kg .. + 3
+//   softmax  running maximum and sum per row, one rescaling per step; powers of two, the
+//            maximum held times log2(e) so that numerator and rescaling use one rounding
+//   values   O^T = V^T P^T per group: two lane swaps turn the group's two score tiles into
+//            the operand (lane: row n, frames 8 kg .. + 7)
+//   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for
+//            the merge kernel
+
 // bf16 terms of a query value (fp32: exact) and of a probability (fp32 output: exact;
 // bf16 output: 2^-16 relative, against the output's own 2^-9).
 template <typename T>
@@ -161,111 +232,245 @@ __device__ __forceinline__ floatx4 mfma_terms(bf16x8 x, const bf16x8 (&t)[N], fl
   for (int i = 0; i < N; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, t[i], acc, 0, 0, 0);
   return acc;
 }
+__device__ __forceinline__ float swap_max(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float swap_sum(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_kv4_attend(Kv4AttendArgs a) {
-  constexpr int QT = Terms<T>::q, PT = Terms<T>::p;
-  __shared__ float wm[4][16], wl[4][16], wo[4][16][68];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kg = lane >> 4;
-  const int head = blockIdx.x, r = blockIdx.y, row = blockIdx.z * 16 + n;
-  const int len = a.lens ? min(max(a.lens[r], 0), a.c.frames) : a.c.frames;
-  const uint8_t* in = a.c.base + ((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups * kKv4Group;
-  bf16x8 qt[2][QT];
-  {
-    const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(row, a.rows - 1) * a.si + head * a.sh + 16 * kg;
+// Codes and scales of KS groups.
+template <int KS>
+struct KvStep {
+  uint4 k[KS], v[KS];
+  uint32_t ks[KS], vs[KS];
+};
+// Groups g .. g + KS - 1 (those from `end` on re-read group end - 1, masked below).
+template <int KS>
+__device__ __forceinline__ void kv_load(const uint8_t* in, int g, int end, KvStep<KS>& s) {
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = row < a.rows ? 0.125f * to_f(q[8 * h + j]) : 0.f;
-      split_terms<QT>(x, qt[h]);
-    }
+  for (int u = 0; u < KS; ++u) {
+    const uint8_t* p = in + (size_t)min(g + u, end - 1) * kKv4Group;
+    s.k[u] = *reinterpret_cast<const uint4*>(p + 16 * lane);
+    s.v[u] = *reinterpret_cast<const uint4*>(p + kKv4Values + 16 * lane);
+    s.ks[u] = *reinterpret_cast<const uint16_t*>(p + kKv4KeyScale + 32 * (kg >> 1) + 2 * n);
+    s.vs[u] = *reinterpret_cast<const uint32_t*>(p + kKv4ValueScale + 4 * n);
   }
-  float m = -INFINITY, l = 0.f;
+}
+constexpr float kLog2e = 1.44269504088896f;
+// A row's running state: maximum of the scores times log2(e), the lane's share of the sum, O^T.
+struct RowState {
+  float m, l;
   floatx4 o[4];
+};
+template <int KS, int QT, int PT>
+__device__ __forceinline__ void kv_step(const KvStep<KS>& c, int g, int len, const bf16x8 (&qt)[2][QT], RowState& st) {
+  const int kg = (threadIdx.x & 63) >> 4;
+  floatx4 s[2 * KS];
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int g = w; g * 32 < len; g += 4) {
-    const uint8_t* p = in + (size_t)g * kKv4Group;
-    const uint4 kc = *reinterpret_cast<const uint4*>(p + 16 * lane), vc = *reinterpret_cast<const uint4*>(p + kKv4Values + 16 * lane);
-    const uint32_t ks = *reinterpret_cast<const uint16_t*>(p + kKv4KeyScale + 32 * (kg >> 1) + 2 * n);
-    const uint32_t vs = *reinterpret_cast<const uint32_t*>(p + kKv4ValueScale + 4 * n);
-    floatx4 s[2];
-    float mx = -INFINITY;
+  for (int t = 0; t < 2 * KS; ++t) {
+    const int u = t >> 1;
+    const float sc = scale_f(t & 1 ? c.ks[u] >> 8 : c.ks[u] & 255);
+    s[t] = mfma_terms<QT>(values8(t & 1 ? c.k[u].w : c.k[u].y, sc), qt[1],
+                          mfma_terms<QT>(values8(t & 1 ? c.k[u].z : c.k[u].x, sc), qt[0], floatx4{0.f, 0.f, 0.f, 0.f}));
+  }
+  if ((g + KS) * kKv4Frames > len) {  // uniform: the last step
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float sc = scale_f(ks >> (8 * t) & 255);
-      const bf16x8 k0 = values8(t ? kc.z : kc.x, sc), k1 = values8(t ? kc.w : kc.y, sc);
-      floatx4 acc = mfma_terms<QT>(k1, qt[1], mfma_terms<QT>(k0, qt[0], floatx4{0.f, 0.f, 0.f, 0.f}));
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (g * 32 + 16 * t + 4 * kg + i >= len) acc[i] = -INFINITY;
-        mx = fmaxf(mx, acc[i]);
-      }
-      s[t] = acc;
-    }
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float mn = fmaxf(m, mx), f = m == -INFINITY ? 0.f : __expf(m - mn);
-    const float base = mn == -INFINITY ? 0.f : mn;
-    m = mn;
-    l *= f;
+      for (int i = 0; i < 4; ++i)
+        if (g * kKv4Frames + 16 * t + 4 * kg + i >= len) s[t][i] = -INFINITY;
+  }
+  float mx = -INFINITY;
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) o[dt] *= f;
-    float pb[8];
+  for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
+  const float m = fmaxf(st.m, swap_max(mx) * kLog2e), base = m == -INFINITY ? 0.f : m;
+  const float f = __builtin_amdgcn_exp2f(st.m - base);  // 0 at first
+  st.m = m;
+  float l = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[t][i] = __expf(s[t][i] - base);
-        l += s[t][i];
-      }
+  for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[0][i]), __float_as_uint(s[1][i]), false, false);
+      s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], kLog2e, -base));
+      l += s[t][i];
+    }
+  st.l = fmaf(st.l, f, l);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) st.o[dt] *= f;
+#pragma unroll
+  for (int u = 0; u < KS; ++u) {
+    float pb[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[2 * u][i]), __float_as_uint(s[2 * u + 1][i]), false, false);
       const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
       pb[i] = __uint_as_float(y[0]);
       pb[4 + i] = __uint_as_float(y[1]);
     }
     bf16x8 pt[PT];
     split_terms<PT>(pb, pt);
-    const uint32_t vw[4] = {vc.x, vc.y, vc.z, vc.w};
+    const uint32_t vw[4] = {c.v[u].x, c.v[u].y, c.v[u].z, c.v[u].w};
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-      const bf16x8 v = values8(vw[dt], scale_f(vs >> (8 * dt) & 255));
-      o[dt] = mfma_terms<PT>(v, pt, o[dt]);
-    }
-  }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (lane < 16) {
-    wm[w][lane] = m;
-    wl[w][lane] = l;
-  }
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) wo[w][n][16 * dt + 4 * kg + i] = o[dt][i];
-  __syncthreads();
-  for (int t = threadIdx.x; t < 16 * 64; t += 256) {
-    const int i = t >> 6, d = t & 63, out_row = blockIdx.z * 16 + i;
-    if (out_row >= a.rows) break;
-    float M = wm[0][i], L = 0.f, O = 0.f;
-    for (int j = 1; j < 4; ++j) M = fmaxf(M, wm[j][i]);
-    for (int j = 0; j < 4; ++j) {
-      const float f = wm[j][i] == -INFINITY && wl[j][i] == 0.f ? 0.f : __expf(wm[j][i] - M);
-      L = fmaf(f, wl[j][i], L);
-      O = fmaf(f, wo[j][i][d], O);
-    }
-    reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + out_row) * a.c.n_head + head) * kHeadDim + d] =
-        from_f<T>(L == 0.f ? 0.f : O / L);
+    for (int dt = 0; dt < 4; ++dt)
+      st.o[dt] = mfma_terms<PT>(values8(vw[dt], scale_f(c.vs[u] >> (8 * dt) & 255)), pt, st.o[dt]);
   }
 }
 
-void kv4_attend(const Kv4AttendArgs& a, hipStream_t st) {
-  const dim3 grid(a.c.n_head, a.n, (a.rows + 15) / 16);
-  if (a.bf16_q) k_kv4_attend<bf16><<<grid, 256, 0, st>>>(a);
-  else k_kv4_attend<float><<<grid, 256, 0, st>>>(a);
+// The lane's 16 query values (dims 16 kg ..) of row `row`, times 1 / sqrt(64).
+template <typename T>
+__device__ __forceinline__ void q_load(const Kv4AttendArgs& a, int r, int row, int head, float* x) {
+  const int kg = (threadIdx.x & 63) >> 4;
+  const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(row, a.rows - 1) * a.si + head * a.sh + 16 * kg;
+  if (a.vec) {
+#pragma unroll
+    for (int j = 0; j < 16; j += 8) ld8(q + j, x + j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = to_f(q[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j) x[j] = row < a.rows ? 0.125f * x[j] : 0.f;
+}
+
+constexpr int kKv4Record = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
+
+template <typename T, int NW, int KS>
+__global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
+  constexpr int QT = Terms<T>::q, PT = Terms<T>::p, S = NW * KS;
+  __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kg = lane >> 4;
+  const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, row = blockIdx.z * 16 + n;
+  const int len = a.lens ? min(max(a.lens[r], 0), a.c.frames) : a.c.frames;
+  const uint8_t* in = a.c.base + ((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups * kKv4Group;
+  const int end = min((chunk + 1) * a.cgroups, (len + kKv4Frames - 1) / kKv4Frames);
+  const int lim = min(len, end * kKv4Frames);  // a step that reaches past the chunk holds its last group again
+  int g = chunk * a.cgroups + w * KS;
+  RowState st;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) st.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (g < end) {
+    KvStep<KS> A, B;
+    kv_load<KS>(in, g, end, A);
+    float x[16];
+    q_load<T>(a, r, row, head, x);
+    bf16x8 qt[2][QT];
+    split_terms<QT>(x, qt[0]);
+    split_terms<QT>(x + 8, qt[1]);
+    for (;;) {
+      kv_load<KS>(in, g + S, end, B);
+      kv_step<KS, QT, PT>(A, g, lim, qt, st);
+      g += S;
+      if (g >= end) break;
+      kv_load<KS>(in, g + S, end, A);
+      kv_step<KS, QT, PT>(B, g, lim, qt, st);
+      g += S;
+      if (g >= end) break;
+    }
+  }
+  const float l = swap_sum(st.l);
+  if (lane < 16) {
+    wm[w][lane] = st.m;
+    wl[w][lane] = l;
+  }
+  // value tile dt holds dims 4 m + dt: o[dt][i] of the lane is dim 16 kg + 4 i + dt
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<floatx4*>(&wo[w][n][16 * kg + 4 * i]) = floatx4{st.o[0][i], st.o[1][i], st.o[2][i], st.o[3][i]};
+  __syncthreads();
+  const int nr = min(16, a.rows - (int)blockIdx.z * 16);
+  for (int t = threadIdx.x; t < nr * 64; t += NW * 64) {
+    const int i = t >> 6, d = t & 63;
+    float M = wm[0][i], L = 0.f, O = 0.f;
+#pragma unroll
+    for (int j = 1; j < NW; ++j) M = fmaxf(M, wm[j][i]);
+    const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+      const float f = __builtin_amdgcn_exp2f(wm[j][i] - base);  // 0 for a wave of no frames
+      L = fmaf(f, wl[j][i], L);
+      O = fmaf(f, wo[j][i][d], O);
+    }
+    if (a.nchunk == 1) {
+      reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + blockIdx.z * 16 + i) * a.c.n_head + head) * kHeadDim + d] =
+          from_f<T>(L == 0.f ? 0.f : O / L);
+    } else {
+      float* rec = a.part + ((((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk + chunk) * kKv4Record;
+      rec[32 + t] = O;
+      if (d == 0) {
+        rec[i] = M;
+        rec[16 + i] = L;
+      }
+    }
+  }
+}
+
+// Joins the chunks of one (head, request, 16 rows): a thread per (row, 4 dims).
+template <typename T>
+__global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
+  const int head = blockIdx.x, r = blockIdx.y, t = threadIdx.x, i = t >> 4, d = 4 * (t & 15), row = blockIdx.z * 16 + i;
+  if (row >= a.rows) return;
+  const float* rec = a.part + (((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk * kKv4Record;
+  float M = -INFINITY, L = 0.f;
+  floatx4 O = {0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < a.nchunk; ++c) M = fmaxf(M, rec[(size_t)c * kKv4Record + i]);
+  const float base = M == -INFINITY ? 0.f : M;
+  for (int c = 0; c < a.nchunk; ++c) {
+    const float* p = rec + (size_t)c * kKv4Record;
+    const float f = __builtin_amdgcn_exp2f(p[i] - base);
+    L = fmaf(f, p[16 + i], L);
+    O += f * *reinterpret_cast<const floatx4*>(p + 32 + i * 64 + d);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + row) * a.c.n_head + head) * kHeadDim + d + e] =
+        from_f<T>(L == 0.f ? 0.f : O[e] / L);
+}
+
+int kv4_chunks(int n, int rows, int n_head, int frames) {
+  const long long pairs = (long long)n * n_head * ((rows + 15) / 16), groups = kv4_groups(frames);
+  if (groups <= 64 || pairs >= 512) return 1;
+  return (int)std::max<long long>(1, std::min<long long>(1024 / pairs, groups / 16));
+}
+size_t kv4_workspace(int n, int rows, int n_head, int frames) {
+  const int nc = kv4_chunks(n, rows, n_head, frames);
+  return nc == 1 ? 0 : (size_t)n * n_head * ((rows + 15) / 16) * nc * kKv4Record * 4;
+}
+
+template <typename T, int NW, int KS>
+static void attend_launch(const Kv4AttendArgs& a, hipStream_t st) {
+  const int tiles = (a.rows + 15) / 16;
+  k_kv4_attend<T, NW, KS><<<dim3(a.c.n_head * a.nchunk, a.n, tiles), NW * 64, 0, st>>>(a);
+  if (a.nchunk > 1) k_kv4_merge<T><<<dim3(a.c.n_head, a.n, tiles), 256, 0, st>>>(a);
+}
+template <typename T>
+static void attend_type(const Kv4AttendArgs& a, hipStream_t st) {
+#ifdef WF_ATT_NW
+  attend_launch<T, WF_ATT_NW, WF_ATT_KS>(a, st);
+#else
+  const long long pairs = (long long)a.n * a.c.n_head * ((a.rows + 15) / 16);
+  if (a.nchunk > 1 || pairs >= 512) attend_launch<T, 4, 2>(a, st);
+  else if (pairs >= 128) attend_launch<T, 8, 2>(a, st);
+  else attend_launch<T, 16, 2>(a, st);
+#endif
+}
+void kv4_attend(const Kv4AttendArgs& a0, hipStream_t st) {
+  Kv4AttendArgs a = a0;
+  a.nchunk = kv4_chunks(a.n, a.rows, a.c.n_head, a.c.frames);
+  a.cgroups = (a.c.groups + a.nchunk - 1) / a.nchunk;
+  if (a.bf16_q) attend_type<bf16>(a, st);
+  else attend_type<float>(a, st);
 }
 
 }  // namespace wf

@@ -246,7 +246,7 @@ int wf_kv4_attend_workspace_bytes(const wf_kv4* c, int n, int rows, size_t* byte
     if (int r = check_range(c, 0, n)) return r;
     if (rows < 1 || rows > (1 << 20)) return bad("rows must be in [1, 2^20]");
     if (!bytes) return bad("null bytes");
-    *bytes = 0;
+    *bytes = kv4_workspace(n, rows, c->n_head, c->n_frames);
     return WF_OK;
   });
 }
@@ -278,6 +278,7 @@ int wf_kv4_attend(const wf_kv4* c, int slot0, int n, const void* q, const int64_
     a.slot0 = slot0;
     a.n = n;
     a.rows = rows;
+    a.part = static_cast<float*>(workspace);
     kv4_attend(a, static_cast<hipStream_t>(stream));
     return launched();
   });

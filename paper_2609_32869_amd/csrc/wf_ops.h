@@ -57,9 +57,9 @@ void cache_reorder(const ReorderArgs& a, hipStream_t st);
 // keys' and the values' codes in the order in which a wave's lanes multiply them, then
 // their scales' biased exponents (0xff: the block stands for NaN).
 //   keys    lane l = 16 kg + n, byte 8 t + j: dims 16 kg + 2 j, + 1 of frame 16 t + n
-//   values  lane l = 16 kg + n, byte 4 dt + j: frames 8 kg + 2 j, + 1 of dim 16 dt + n
+//   values  lane l = 16 kg + n, byte 4 dt + j: frames 8 kg + 2 j, + 1 of dim 4 n + dt
 //   scales  keys: byte 32 half + 2 n + t: dims 32 half .. + 31 of frame 16 t + n;
-//           values: byte 4 n + dt: dim 16 dt + n
+//           values: a byte per dim
 // Low nibble first.  A wave reads a group's codes as two 16-byte loads per lane.
 constexpr int kKv4Frames = 32;
 constexpr int kKv4Values = 1024, kKv4KeyScale = 2048, kKv4ValueScale = 2112, kKv4Group = 2176;
@@ -93,7 +93,10 @@ struct Kv4AttendArgs {
   void* out;  // [n][rows][n_head][64], the query's type
   const int* lens;
   int slot0, n, rows;
+  float* part;  // chunk records (nchunk > 1)
+  int nchunk, cgroups;  // chunks of the groups and groups of a chunk (set by the launcher)
 };
+size_t kv4_workspace(int n, int rows, int n_head, int frames);
 void kv4_attend(const Kv4AttendArgs& a, hipStream_t st);
 
 }  // namespace wf

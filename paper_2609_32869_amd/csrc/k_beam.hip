@@ -1,6 +1,7 @@
 // Beam search: the k best continuations over a request's beams and vocabulary, and the
 // page tables of the beams that were chosen.
 #include <algorithm>
+#include <type_traits>
 
 #include "wf_ops.h"
 
@@ -64,37 +65,62 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
 }
 
-// 8 consecutive logits from column v on; columns past the row and suppressed ones are
-// -inf.  Rows start anywhere (every second bf16 row of an odd vocabulary lies off 4
-// bytes), so the loads are 16 bytes at the elements' alignment: columns are grouped by
-// number, not by address, and rows of equal values have equal sums.
-__device__ __forceinline__ void ld8_any(const float* p, float* o) { __builtin_memcpy(o, p, 32); }
-__device__ __forceinline__ void ld8_any(const bf16* p, float* o) {
-  uint4 v;
-  __builtin_memcpy(&v, p, 16);
-  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    o[2 * i] = __uint_as_float(u[i] << 16);
-    o[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-  }
-}
+// 8 consecutive logits or suppression bytes.  Rows start anywhere (every second bf16 row of
+// an odd vocabulary lies off 4 bytes), so the loads are 16 bytes at the elements'
+// alignment: columns are grouped by number, not by address, and rows of equal values have
+// equal sums.
 template <typename T>
-__device__ __forceinline__ void logits8(const T* x, const uint8_t* sup, int v, int vocab, float* o) {
-  if (v + 8 <= vocab) {
-    ld8_any(x + v, o);
-    if (sup) {
-      uint64_t m;
-      __builtin_memcpy(&m, sup + v, 8);
+struct Eight {
+  T v[8];
+  __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
+};
+
+// The thread's 32 logits: eights at columns v0 + 2048 i.  The eights' loads are issued
+// together, without a condition (those that reach past the row read its last eight
+// columns); the row's last, partial eight is then read by element.  Columns past the row
+// and suppressed ones are -inf.
+template <typename T>
+__device__ __forceinline__ void load_logits(const T* x, const uint8_t* sup, int v0, int vocab, float* y) {
+  constexpr int N = kBeamRegs / 8;
+  if (vocab >= 8) {
+    Eight<T> e[N];
+    uint64_t m[N] = {};
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (m >> (8 * e) & 255) o[e] = -INFINITY;
+    for (int i = 0; i < N; ++i) e[i].load(x + min(v0 + 2048 * i, vocab - 8));
+    if (sup) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) __builtin_memcpy(&m[i], sup + min(v0 + 2048 * i, vocab - 8), 8);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool in = v0 + 2048 * i + 8 <= vocab;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[8 * i + j] = in ? to_f(e[i].v[j]) : -INFINITY;
+    }
+    if (sup) {
+#pragma unroll
+      for (int i = 0; i < kBeamRegs; ++i)
+        if (m[i / 8] >> (8 * (i % 8)) & 255) y[i] = -INFINITY;
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = v + e;
-      o[e] = c < vocab && !(sup && sup[c]) ? to_f(x[c]) : -INFINITY;
+    for (int i = 0; i < kBeamRegs; ++i) y[i] = -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int v = v0 + 2048 * i;
+    if (v < vocab && v + 8 > vocab) {  // one thread of the row
+      T e[8];
+      uint8_t m[8] = {};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) e[j] = x[min(v + j, vocab - 1)];
+      if (sup) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m[j] = sup[min(v + j, vocab - 1)];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[8 * i + j] = v + j < vocab && m[j] == 0 ? to_f(e[j]) : -INFINITY;
     }
   }
 }
@@ -112,8 +138,7 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
   const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb;
   const int v0 = blockIdx.y * kBeamPiece + 8 * t;
   float y[kBeamRegs];
-#pragma unroll
-  for (int i = 0; i < kBeamRegs / 8; ++i) logits8(x, a.suppress, v0 + 2048 * i, a.vocab, y + 8 * i);
+  load_logits(x, a.suppress, v0, a.vocab, y);
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kBeamRegs; ++i) m = fmaxf(m, y[i]);
@@ -166,17 +191,22 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
     }
   int mine = 0;  // the wave's survivors so far
   if (__ballot(best >= max(bound, 1u)) != 0) {
-    const float least = value_of(bound);
+    const float least = bound == 0 ? -__FLT_MAX__ : value_of(bound);
+    auto gather = [&](auto ties) {
 #pragma unroll
-    for (int i = 0; i < kBeamRegs; ++i) {
-      const int cc = v0 + 2048 * (i / 8) + i % 8;
-      const bool in = bound == 0 ? y[i] > -INFINITY : y[i] > least || (y[i] == least && (uint32_t)cc <= col);
-      const uint64_t mask = __ballot(in);
-      if (mask != 0) {  // uniform
-        if (in) keys[w * kSeg + mine + __popcll(mask & (((uint64_t)1 << lane) - 1))] = (uint64_t)order_of(y[i]) << 32 | (uint32_t)~cc;
-        mine += __popcll(mask);
+      for (int i = 0; i < kBeamRegs; ++i) {
+        const int cc = v0 + 2048 * (i / 8) + i % 8;
+        bool in = y[i] >= least;
+        if constexpr (decltype(ties)::value) in = in && (y[i] > least || (uint32_t)cc <= col);
+        const uint64_t mask = __ballot(in);
+        if (mask != 0) {  // uniform
+          if (in) keys[w * kSeg + mine + __popcll(mask & (((uint64_t)1 << lane) - 1))] = (uint64_t)order_of(y[i]) << 32 | (uint32_t)~cc;
+          mine += __popcll(mask);
+        }
       }
-    }
+    };
+    if (col == ~0u) gather(std::false_type{});
+    else gather(std::true_type{});
   }
   if (lane == 0) wn[w] = mine;
   __syncthreads();

@@ -98,6 +98,13 @@ __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
   uint8_t* out = a.c.base + (((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups + g) * kKv4Group;
   const T* K = reinterpret_cast<const T*>(a.k) + r * a.kr + head * a.kh + 16 * kg;
   const T* V = reinterpret_cast<const T*>(a.v) + r * a.vr + head * a.vh + 4 * n;
+  if (g * 32 >= len) {  // uniform: nothing given (scales of 2^-120, as a block of zeros has)
+    const uint4 z = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(out + 16 * lane) = z;
+    *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = z;
+    if (lane < 32) *reinterpret_cast<uint32_t*>(out + kKv4KeyScale + 4 * lane) = 0x07070707u;
+    return;
+  }
   Raw<T, 16> k[2];
   Raw<T, 4> v[8];
 #pragma unroll
@@ -199,8 +206,8 @@ void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- attention
-// Block (head, request, chunk of the groups) x (16 query rows), NW waves; a wave takes
-// steps of KS groups, the next step's codes in flight while it multiplies the current one.
+// Block (head, request, chunk of the groups) x (16 query rows), eight waves; a wave takes
+// steps of two groups, the next step's codes in flight while it multiplies the current one.
 //   scores   S^T = K q^T per 16-frame tile (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets
 //            row n of frames 4 kg .. + 3
 //   softmax  running maximum and sum per row, one rescaling per step; powers of two, the
@@ -342,11 +349,15 @@ __device__ __forceinline__ void q_load(const Kv4AttendArgs& a, int r, int row, i
   for (int j = 0; j < 16; ++j) x[j] = row < a.rows ? 0.125f * x[j] : 0.f;
 }
 
+// Waves a block and groups a step.  us per launch (fp32, 20 heads; 1 x 9 rows, 96 x 9 rows of 1,500 frames, one
+// row of 131,072; 16 x 5 rows in bf16): 8 waves of 2: 8.5, 52, 43, 10.7; of 1: 8.9, 52, 43, 10.6; of 3: 8.5, 73, 49,
+// 11.4; 4 waves of 2: 9.3, 52, 45, 11.4; 16 of 2: 8.9, 77, 53, 11.5.
+constexpr int kAttWaves = 8, kAttStep = 2;
 constexpr int kKv4Record = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
 
-template <typename T, int NW, int KS>
-__global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
-  constexpr int QT = Terms<T>::q, PT = Terms<T>::p, S = NW * KS;
+template <typename T>
+__global__ void __launch_bounds__(kAttWaves * 64) k_kv4_attend(Kv4AttendArgs a) {
+  constexpr int QT = Terms<T>::q, PT = Terms<T>::p, NW = kAttWaves, KS = kAttStep, S = NW * KS;
   __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kg = lane >> 4;
   const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, row = blockIdx.z * 16 + n;
@@ -416,30 +427,70 @@ __global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
   }
 }
 
-// Joins the chunks of one (head, request, 16 rows): a thread per (row, 4 dims).
+// Joins the chunks of one row of a (head, request): 16 threads (4 dims each) take every
+// sixteenth chunk, so that a few loads per thread are in flight at once, and meet in LDS.
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
-  const int head = blockIdx.x, r = blockIdx.y, t = threadIdx.x, i = t >> 4, d = 4 * (t & 15), row = blockIdx.z * 16 + i;
-  if (row >= a.rows) return;
-  const float* rec = a.part + (((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk * kKv4Record;
+  __shared__ float wm[16], wl[16], wo[16][64];
+  const int head = blockIdx.x, r = blockIdx.y, row = blockIdx.z, tile = row >> 4, i = row & 15, tiles = (a.rows + 15) >> 4;
+  const int t = threadIdx.x, q = t >> 4, d = 4 * (t & 15);
+  const float* rec = a.part + (((size_t)r * tiles + tile) * a.c.n_head + head) * a.nchunk * kKv4Record;
   float M = -INFINITY, L = 0.f;
   floatx4 O = {0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < a.nchunk; ++c) M = fmaxf(M, rec[(size_t)c * kKv4Record + i]);
-  const float base = M == -INFINITY ? 0.f : M;
-  for (int c = 0; c < a.nchunk; ++c) {
-    const float* p = rec + (size_t)c * kKv4Record;
-    const float f = __builtin_amdgcn_exp2f(p[i] - base);
-    L = fmaf(f, p[16 + i], L);
-    O += f * *reinterpret_cast<const floatx4*>(p + 32 + i * 64 + d);
-  }
+  constexpr int U = 4;
+  for (int c0 = q; c0 < a.nchunk; c0 += 16 * U) {
+    float m[U], l[U];
+    floatx4 o[U];
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + row) * a.c.n_head + head) * kHeadDim + d + e] =
-        from_f<T>(L == 0.f ? 0.f : O[e] / L);
+    for (int u = 0; u < U; ++u) {
+      const float* p = rec + (size_t)min(c0 + 16 * u, a.nchunk - 1) * kKv4Record;
+      m[u] = p[i];
+      l[u] = p[16 + i];
+      o[u] = *reinterpret_cast<const floatx4*>(p + 32 + i * 64 + d);
+    }
+    float Mn = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + 16 * u < a.nchunk) Mn = fmaxf(Mn, m[u]);
+    const float base = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - base);
+    M = Mn;
+    L *= f0;
+    O *= f0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (c0 + 16 * u < a.nchunk) {
+        const float f = __builtin_amdgcn_exp2f(m[u] - base);
+        L = fmaf(f, l[u], L);
+        O += f * o[u];
+      }
+    }
+  }
+  *reinterpret_cast<floatx4*>(&wo[q][d]) = O;
+  if (d == 0) {
+    wm[q] = M;
+    wl[q] = L;
+  }
+  __syncthreads();
+  if (t < 64) {
+    float m = wm[0], l = 0.f, o = 0.f;
+#pragma unroll
+    for (int j = 1; j < 16; ++j) m = fmaxf(m, wm[j]);
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float f = __builtin_amdgcn_exp2f(wm[j] - base);
+      l = fmaf(f, wl[j], l);
+      o = fmaf(f, wo[j][t], o);
+    }
+    reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + row) * a.c.n_head + head) * kHeadDim + t] = from_f<T>(l == 0.f ? 0.f : o / l);
+  }
 }
 
 int kv4_chunks(int n, int rows, int n_head, int frames) {
   const long long pairs = (long long)n * n_head * ((rows + 15) / 16), groups = kv4_groups(frames);
+#ifdef WF_CH
+  return (int)std::max<long long>(1, std::min<long long>(WF_CH / pairs, groups / 16));
+#endif
   if (groups <= 64 || pairs >= 512) return 1;
   return (int)std::max<long long>(1, std::min<long long>(1024 / pairs, groups / 16));
 }
@@ -448,29 +499,18 @@ size_t kv4_workspace(int n, int rows, int n_head, int frames) {
   return nc == 1 ? 0 : (size_t)n * n_head * ((rows + 15) / 16) * nc * kKv4Record * 4;
 }
 
-template <typename T, int NW, int KS>
+template <typename T>
 static void attend_launch(const Kv4AttendArgs& a, hipStream_t st) {
   const int tiles = (a.rows + 15) / 16;
-  k_kv4_attend<T, NW, KS><<<dim3(a.c.n_head * a.nchunk, a.n, tiles), NW * 64, 0, st>>>(a);
-  if (a.nchunk > 1) k_kv4_merge<T><<<dim3(a.c.n_head, a.n, tiles), 256, 0, st>>>(a);
-}
-template <typename T>
-static void attend_type(const Kv4AttendArgs& a, hipStream_t st) {
-#ifdef WF_ATT_NW
-  attend_launch<T, WF_ATT_NW, WF_ATT_KS>(a, st);
-#else
-  const long long pairs = (long long)a.n * a.c.n_head * ((a.rows + 15) / 16);
-  if (a.nchunk > 1 || pairs >= 512) attend_launch<T, 4, 2>(a, st);
-  else if (pairs >= 128) attend_launch<T, 8, 2>(a, st);
-  else attend_launch<T, 16, 2>(a, st);
-#endif
+  k_kv4_attend<T><<<dim3(a.c.n_head * a.nchunk, a.n, tiles), kAttWaves * 64, 0, st>>>(a);
+  if (a.nchunk > 1) k_kv4_merge<T><<<dim3(a.c.n_head, a.n, a.rows), 256, 0, st>>>(a);
 }
 void kv4_attend(const Kv4AttendArgs& a0, hipStream_t st) {
   Kv4AttendArgs a = a0;
   a.nchunk = kv4_chunks(a.n, a.rows, a.c.n_head, a.c.frames);
   a.cgroups = (a.c.groups + a.nchunk - 1) / a.nchunk;
-  if (a.bf16_q) attend_type<bf16>(a, st);
-  else attend_type<float>(a, st);
+  if (a.bf16_q) attend_launch<bf16>(a, st);
+  else attend_launch<float>(a, st);
 }
 
 }  // namespace wf

@@ -11,6 +11,8 @@ import functools
 
 import torch
 
+from torch._C import _cuda_getCurrentRawStream as _raw_stream  # torch.cuda.current_stream() without its objects (2.7 us)
+
 from .binding import WF_BF16, WF_F32, WfError, WfKv4, load_library
 
 _DTYPES = {torch.float32: WF_F32, torch.bfloat16: WF_BF16}
@@ -58,36 +60,25 @@ def _type(t, name):
     return code
 
 
-class _On:
-    """Where a call's work goes: `device` made current, `stream` or the current stream of it.  Memory from `empty` is
-    reused only behind the work that a given stream still has for it."""
+def _enqueue(device, stream, call):
+    """call(raw stream, empty) with `device` current.  empty(shape, dtype): memory that is reused only behind the work
+    that the call's stream has for it."""
+    index = device.index
+    if stream is None:
+        raw, empty = _raw_stream(index), functools.partial(torch.empty, device=device)
+    else:
+        if stream.device != device:
+            _refuse("stream is of another device than the tensors")
+        raw = stream.cuda_stream
 
-    __slots__ = ("device", "stream", "given", "back")
-
-    def __init__(self, device, stream):
-        self.device, self.given, self.back = device, None, None
-        if stream is not None:
-            if stream.device != device:
-                _refuse("stream is of another device than the tensors")
-            self.given = stream
-
-    def __enter__(self):
-        here = torch.cuda.current_device()
-        if here != self.device.index:
-            self.back = here
-            torch.cuda.set_device(self.device)
-        self.stream = (self.given or torch.cuda.current_stream()).cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
-
-    def empty(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.given is not None:
-            t.record_stream(self.given)
-        return t
+        def empty(shape, dtype):
+            t = torch.empty(shape, dtype=dtype, device=device)
+            t.record_stream(stream)
+            return t
+    if torch.cuda.current_device() == index:
+        return call(raw, empty)
+    with torch.cuda.device(index):
+        return call(raw, empty)
 
 
 @functools.lru_cache(maxsize=256)
@@ -115,12 +106,17 @@ def beam_select(logits, scores, k, suppress=None, stream=None):
         _tensor(suppress, "suppress", _U8, (vocab,), dev)
     k = int(k)
     nbytes = _select_bytes(n, beams, vocab, k)
-    with _On(dev, stream) as on:
-        score, beam, token = on.empty((3, n, k), _I32).unbind()
-        ws = on.empty(nbytes, _U8)
+
+    def call(raw, empty):
+        out = empty((3, n, k), dtype=_I32)
+        ws = empty(nbytes, dtype=_U8)
+        p, step = out.data_ptr(), 4 * n * k
         _check(lib.wf_beam_select(logits.data_ptr(), dtype, sr, sb, scores.data_ptr(),
-                                  None if suppress is None else suppress.data_ptr(), n, beams, vocab, k, score.data_ptr(),
-                                  beam.data_ptr(), token.data_ptr(), ws.data_ptr(), nbytes, on.stream))
+                                  None if suppress is None else suppress.data_ptr(), n, beams, vocab, k, p, p + step,
+                                  p + 2 * step, ws.data_ptr(), nbytes, raw))
+        return out
+
+    score, beam, token = _enqueue(dev, stream, call).unbind()
     return score.view(_F32), beam, token
 
 
@@ -149,12 +145,15 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
     if regions == 0 or pages == 0:
         _refuse("cache must hold a page")
     region = cache.numel() // regions * cache.element_size()
-    with _On(dev, stream) as on:
-        new = on.empty((n, beams, max_pages), _I32)
+
+    def call(raw, empty):
+        new = empty((n, beams, max_pages), dtype=_I32)
         _check(lib.wf_cache_reorder(cache.data_ptr(), regions, region, pages, region // pages, tables.data_ptr(), new.data_ptr(),
                                     n, beams, max_pages, int(page_tokens), parents.data_ptr(), lens.data_ptr(),
-                                    pool.data_ptr(), pool_pages, on.stream))
-    return new
+                                    pool.data_ptr(), pool_pages, raw))
+        return new
+
+    return _enqueue(dev, stream, call)
 
 
 _Strides = ctypes.c_int64 * 3
@@ -202,9 +201,9 @@ class AcousticCache4:
         n = k.shape[0]
         if vtype != dtype or v.shape[0] != n:
             _refuse("v must have k's type and shape")
-        with _On(self.device, stream) as on:
-            _check(self.lib.wf_kv4_store(self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype,
-                                         self._lens(lens, n), on.stream))
+        lens = self._lens(lens, n)
+        _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv4_store(
+            self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, lens, raw)))
 
     def load(self, slot0, n, dtype=torch.float32, stream=None):
         """The keys and values that entries slot0 .. slot0 + n - 1 hold: two tensors [n, n_frames, n_head, 64]."""
@@ -212,11 +211,14 @@ class AcousticCache4:
             _refuse("dtype must be float32 or bfloat16")
         if not (0 < n <= self.entries and 0 <= slot0 <= self.entries - n):
             _refuse("entries out of range")
-        with _On(self.device, stream) as on:
-            k = on.empty((n, self.n_frames, self.n_head, 64), dtype)
-            v = on.empty((n, self.n_frames, self.n_head, 64), dtype)
-            _check(self.lib.wf_kv4_load(self._ref, int(slot0), n, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], on.stream))
-        return k, v
+
+        def call(raw, empty):
+            k = empty((n, self.n_frames, self.n_head, 64), dtype=dtype)
+            v = empty((n, self.n_frames, self.n_head, 64), dtype=dtype)
+            _check(self.lib.wf_kv4_load(self._ref, int(slot0), n, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], raw))
+            return k, v
+
+        return _enqueue(self.device, stream, call)
 
     def attend(self, slot0, q, lens=None, stream=None):
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, n_head, 64], any strides but the last) over the first lens[r]
@@ -228,9 +230,13 @@ class AcousticCache4:
             nbytes = ctypes.c_size_t()
             _check(self.lib.wf_kv4_attend_workspace_bytes(self._ref, n, rows, ctypes.byref(nbytes)))
             need = self._spaces[n, rows] = nbytes.value
-        with _On(self.device, stream) as on:
-            out = on.empty((n, rows, self.n_head, 64), q.dtype)
-            ws = on.empty(need, _U8).data_ptr() if need else None
-            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, self._lens(lens, n),
-                                          out.data_ptr(), ws, need, on.stream))
-        return out
+        lens = self._lens(lens, n)
+
+        def call(raw, empty):
+            out = empty((n, rows, self.n_head, 64), dtype=q.dtype)
+            ws = empty(need, dtype=_U8) if need else None
+            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, lens, out.data_ptr(),
+                                          ws.data_ptr() if need else None, need, raw))
+            return out
+
+        return _enqueue(self.device, stream, call)

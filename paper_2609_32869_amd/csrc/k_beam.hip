@@ -13,13 +13,16 @@ namespace wf {
 // piece's maximum and sum of exponentials; the beams meet in 64-bit scores in the merge.
 //
 // Row kernel: a block per (piece of kBeamPiece columns, row), one read of the logits into
-// registers, 32 per thread.  At least k lanes of a wave hold a value of at least the k-th
-// best of the 64 per-lane maxima, so that maximum, found with ballots to as many bits as
-// leave few lanes above it, bounds the piece's k-th best from below; the best of the four
-// waves' bounds leaves a handful of survivors (KL lanes a wave at most), which are ranked by
-// counting.  Equal values by column, so that any number of ties stays within the array.
-constexpr int kBeamRegs = 32;
-constexpr int kBeamPiece = 256 * kBeamRegs;
+// registers, 32 per thread, a wave's columns together.  With the block's lanes in k groups
+// or more, the least of the groups' maxima bounds the piece's k-th best from below; the
+// few values that reach it go to LDS and are ranked by counting.  Where a wave has more of
+// them than its KL * R places (near-equal logits), the wave's own bound is the k-th best of
+// its lanes' maxima, found bit by bit with ballots, equal ones by column: KL lanes at most,
+// any number of ties.
+// 768 rows of 51,864 logits: fp32 32 us, the copy rate of 4.9 TB/s; bf16 33 us, bound by the
+// vector instructions (a logit costs five: one to convert, four for its exponential, and
+// a wave as many again besides).  64 logits a thread: 34 and 41 us, fewer waves a SIMD.
+constexpr int kBeamRegs = 32, kBeamPiece = 256 * kBeamRegs;
 
 // Larger value, larger integer, both zeros alike; NaN and -inf (no candidates) at 0.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -39,6 +42,11 @@ __device__ __forceinline__ void wave_kth(uint32_t w, bool active, uint32_t& t, i
     t = up ? t | 1u << bit : t;
     r = up ? r : r - c;
   }
+}
+__device__ __forceinline__ float max8(float v) {  // over 8 lanes, in each of them
+  v = fmaxf(v, dpp<kDppXor1>(v));
+  v = fmaxf(v, dpp<kDppXor2>(v));
+  return fmaxf(v, dpp<kDppHalfMirror>(v));
 }
 // sum over a row of 16 lanes by DPP moves of the two halves, in every lane of the row
 template <int CTRL>
@@ -75,138 +83,171 @@ struct Eight {
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
 };
 
-// The thread's 32 logits: eights at columns v0 + 2048 i.  The eights' loads are issued
-// together, without a condition (those that reach past the row read its last eight
-// columns); the row's last, partial eight is then read by element.  Columns past the row
-// and suppressed ones are -inf.
-template <typename T>
+// The thread's R logits: eights from columns v0 + 512 i on, of which the row's last, partial
+// one is read as the row's last eight columns (eight_at) and keeps those that are its own.
+// The loads are issued together, without a condition.  Columns past the row and suppressed
+// ones are -inf.
+__device__ __forceinline__ int eight_at(int v, int vocab) { return max(min(v, vocab - 8), 0); }
+template <typename T, int R>
 __device__ __forceinline__ void load_logits(const T* x, const uint8_t* sup, int v0, int vocab, float* y) {
-  constexpr int N = kBeamRegs / 8;
+  constexpr int N = R / 8;
   if (vocab >= 8) {
     Eight<T> e[N];
-    uint64_t m[N] = {};
 #pragma unroll
-    for (int i = 0; i < N; ++i) e[i].load(x + min(v0 + 2048 * i, vocab - 8));
-    if (sup) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) __builtin_memcpy(&m[i], sup + min(v0 + 2048 * i, vocab - 8), 8);
-    }
+    for (int i = 0; i < N; ++i) e[i].load(x + eight_at(v0 + 512 * i, vocab));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const bool in = v0 + 2048 * i + 8 <= vocab;
+    for (int i = 0; i < R; ++i) y[i] = to_f(e[i / 8].v[i % 8]);
+  } else {  // a row shorter than an eight
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[8 * i + j] = in ? to_f(e[i].v[j]) : -INFINITY;
-    }
-    if (sup) {
-#pragma unroll
-      for (int i = 0; i < kBeamRegs; ++i)
-        if (m[i / 8] >> (8 * (i % 8)) & 255) y[i] = -INFINITY;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kBeamRegs; ++i) y[i] = -INFINITY;
+    for (int i = 0; i < R; ++i) y[i] = i < 8 ? to_f(x[min(i, vocab - 1)]) : -INFINITY;
   }
+  if (__builtin_amdgcn_readfirstlane(v0) + 64 * R > vocab) {  // the row's last columns
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int v = v0 + 2048 * i;
-    if (v < vocab && v + 8 > vocab) {  // one thread of the row
-      T e[8];
-      uint8_t m[8] = {};
+    for (int i = 0; i < R; ++i) {
+      const int v = v0 + 512 * (i / 8), c = eight_at(v, vocab) + i % 8;
+      if (c < v || c >= vocab) y[i] = -INFINITY;
+    }
+  }
+  if (sup) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = x[min(v + j, vocab - 1)];
-      if (sup) {
+    for (int i = 0; i < N; ++i) {
+      const uint8_t* p = sup + eight_at(v0 + 512 * i, vocab);
+      uint64_t m = 0;
+      if (vocab >= 8) __builtin_memcpy(&m, p, 8);
+      else
+        for (int j = 0; j < vocab; ++j) m |= (uint64_t)p[j] << (8 * j);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m[j] = sup[min(v + j, vocab - 1)];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[8 * i + j] = v + j < vocab && m[j] == 0 ? to_f(e[j]) : -INFINITY;
+      for (int j = 0; j < 8; ++j)
+        if (m >> (8 * j) & 255) y[8 * i + j] = -INFINITY;
     }
   }
 }
 
-// KL: lanes of a wave that survive at most, k <= KL
+// KL: groups of the block's lanes, and lanes of a wave that survive at most; k <= KL
 template <typename T, int KL>
 __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
-  constexpr int kSeg = KL * kBeamRegs;  // a wave's survivors
+  constexpr int R = kBeamRegs, kSeg = KL * R;  // a wave's survivors
   __shared__ __align__(16) uint64_t keys[4 * kSeg];
-  __shared__ uint32_t tv[4], ti[4];
-  __shared__ float wm[4];
+  __shared__ float gm[KL], wm[4];
   __shared__ double ws[4];
   __shared__ int wn[4];
-  const int row = blockIdx.x, r = row / a.beams, b = row % a.beams, t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int r = blockIdx.x, b = blockIdx.z, row = r * a.beams + b, t = threadIdx.x, lane = t & 63;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb;
-  const int v0 = blockIdx.y * kBeamPiece + 8 * t;
-  float y[kBeamRegs];
-  load_logits(x, a.suppress, v0, a.vocab, y);
+  const int v0 = blockIdx.y * 256 * R + w * 64 * R + 8 * lane;
+  float y[R];
+  load_logits<T, R>(x, a.suppress, v0, a.vocab, y);
   float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kBeamRegs; ++i) m = fmaxf(m, y[i]);
-  // the wave's bound (0: fewer than k lanes hold anything)
-  const uint32_t best = order_of(m);
-  bool active = best != 0;
-  uint32_t bound = 0, col = ~0u;
-  if (__popcll(__ballot(active)) >= a.k) {
-    int need = a.k;
-    wave_kth<31, 16>(best, active, bound, need);
-    if (__popcll(__ballot(best >= bound)) > KL) wave_kth<15, 0>(best, active, bound, need);
-    if (__popcll(__ballot(best >= bound)) > KL) {  // more equal maxima than that: the first of them by column
-      int at = 0;
-#pragma unroll
-      for (int i = kBeamRegs - 1; i >= 0; --i)
-        if (y[i] == m) at = v0 + 2048 * (i / 8) + i % 8;
-      uint32_t inv = 0;
-      active = best == bound;
-      wave_kth<31, 0>(~(uint32_t)at, active, inv, need);
-      col = ~inv;
-    }
+  for (int i = 0; i < R; ++i) m = fmaxf(m, y[i]);
+  // maxima of the block's KL groups of 256 / KL lanes
+  {
+    const float g = KL == 16 ? max16(m) : max8(m);
+    if (lane % (256 / KL) == 0) gm[t / (256 / KL)] = g;
   }
-  // sum of exponentials relative to the lane's maximum, eight at a time in 32 bits, then 64
+  // sum of exponentials relative to the lane's maximum, eight at a time in 32 bits, then 64.  Powers of two, m log2(e)
+  // rounded once and what that took put back on the sum; huge logits, whose product overflows, by difference
   constexpr float log2e = 1.44269504088896f;
   const float base = m == -INFINITY ? 0.f : m;
   double sum = 0;
+  if (__ballot(fabsf(base) > 1e30f) == 0) {
+    const float mc = base * log2e, took = fmaf(base, log2e, -mc);
 #pragma unroll
-  for (int i = 0; i < kBeamRegs; i += 8) {
-    float p = 0.f;
+    for (int i = 0; i < R; i += 8) {
+      float p = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p += __builtin_amdgcn_exp2f((y[i + e] - base) * log2e);
-    sum += (double)p;
+      for (int e = 0; e < 8; ++e) p += __builtin_amdgcn_exp2f(fmaf(y[i + e], log2e, -mc));
+      sum += (double)p;
+    }
+    sum *= (double)__builtin_amdgcn_exp2f(-took);
+  } else {
+#pragma unroll
+    for (int i = 0; i < R; i += 8) {
+      float p = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p += __builtin_amdgcn_exp2f((y[i + e] - base) * log2e);
+      sum += (double)p;
+    }
   }
   // to the wave's maximum; a lane of no values holds 0, or NaN, which stays
   const float M = wave_max(m);
   if (m != -INFINITY) sum *= (double)__builtin_amdgcn_exp2f((m - M) * log2e);
   sum = wave_sum_d(sum);
   if (lane == 0) {
-    tv[w] = bound;
-    ti[w] = col;
     wm[w] = M;
     ws[w] = sum;
   }
   __syncthreads();
+  // the least of KL groups' maxima, or of half or a quarter as many groups where k allows it
+  float g[KL];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (tv[i] > bound || (tv[i] == bound && ti[i] < col)) {
-      bound = tv[i];
-      col = ti[i];
+  for (int i = 0; i < KL; ++i) g[i] = gm[i];
+  float least = INFINITY;
+  if (a.k <= KL / 4) {
+#pragma unroll
+    for (int i = 0; i < KL; i += 4) least = fminf(least, fmaxf(fmaxf(g[i], g[i + 1]), fmaxf(g[i + 2], g[i + 3])));
+  } else if (a.k <= KL / 2) {
+#pragma unroll
+    for (int i = 0; i < KL; i += 2) least = fminf(least, fmaxf(g[i], g[i + 1]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < KL; ++i) least = fminf(least, g[i]);
+  }
+  least = fmaxf(least, -__FLT_MAX__);  // a group of no values: every value is kept
+  uint64_t lanes = __ballot(m >= least);
+  uint32_t col = ~0u;
+  int over = 0;
+  if (__popcll(lanes) > KL) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) over += __popcll(__ballot(y[i] >= least));
+  }
+  if (over > kSeg) {
+    const uint32_t best = order_of(m);
+    uint32_t bound = 0;
+    int need = a.k;
+    bool active = best != 0;
+    wave_kth<31, 0>(best, active, bound, need);
+    least = value_of(bound);
+    lanes = __ballot(m >= least);
+    if (__popcll(lanes) > KL) {  // more equal maxima than that: the first of them by column
+      int at = 0;
+#pragma unroll
+      for (int i = R - 1; i >= 0; --i)
+        if (y[i] == m) at = eight_at(v0 + 512 * (i / 8), a.vocab) + i % 8;
+      uint32_t inv = 0;
+      active = best == bound;
+      wave_kth<31, 0>(~(uint32_t)at, active, inv, need);
+      col = ~inv;
+      lanes = __ballot(m > least || (m == least && (uint32_t)at <= col));
     }
-  int mine = 0;  // the wave's survivors so far
-  if (__ballot(best >= max(bound, 1u)) != 0) {
-    const float least = bound == 0 ? -__FLT_MAX__ : value_of(bound);
+  }
+  // the wave's survivors: value and place first, as little as possible per value, then made into keys in place
+  int mine = 0;
+  if (lanes != 0) {
+    uint2* seg = reinterpret_cast<uint2*>(keys + w * kSeg);
     auto gather = [&](auto ties) {
 #pragma unroll
-      for (int i = 0; i < kBeamRegs; ++i) {
-        const int cc = v0 + 2048 * (i / 8) + i % 8;
+      for (int i = 0; i < R; ++i) {
         bool in = y[i] >= least;
-        if constexpr (decltype(ties)::value) in = in && (y[i] > least || (uint32_t)cc <= col);
+        if constexpr (decltype(ties)::value)
+          in = in && (y[i] > least || (uint32_t)(eight_at(v0 + 512 * (i / 8), a.vocab) + i % 8) <= col);
         const uint64_t mask = __ballot(in);
-        if (mask != 0) {  // uniform
-          if (in) keys[w * kSeg + mine + __popcll(mask & (((uint64_t)1 << lane) - 1))] = (uint64_t)order_of(y[i]) << 32 | (uint32_t)~cc;
+        if (mask != 0) {  // uniform, and rare
+          const int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, mine));
+          if (in) seg[at] = make_uint2(__float_as_uint(y[i]), i << 6 | lane);
           mine += __popcll(mask);
         }
       }
     };
     if (col == ~0u) gather(std::false_type{});
     else gather(std::true_type{});
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int u = lane; u < mine; u += 64) {
+      const uint2 e = seg[u];
+      const int i = e.y >> 6, v = v0 - 8 * lane + 8 * (int)(e.y & 63) + 512 * (i / 8), c = eight_at(v, a.vocab) + i % 8;
+      keys[w * kSeg + u] = (uint64_t)order_of(__uint_as_float(e.x)) << 32 | (uint32_t)~c;
+    }
   }
   if (lane == 0) wn[w] = mine;
   __syncthreads();
@@ -414,14 +455,14 @@ int beam_pieces(int vocab) { return (vocab + kBeamPiece - 1) / kBeamPiece; }
 
 void beam_select(const BeamSelectArgs& a, hipStream_t st) {
   const int np = beam_pieces(a.vocab);
-  const dim3 grid(a.n * a.beams, np);
-  auto rows = [&](auto tag) {
+  const dim3 grid(a.n, np, a.beams);
+  auto launch = [&](auto tag) {
     using T = decltype(tag);
     if (a.k <= 16) k_beam_rows<T, 16><<<grid, 256, 0, st>>>(a);
     else k_beam_rows<T, kMaxCand><<<grid, 256, 0, st>>>(a);
   };
-  if (a.bf16_logits) rows(bf16{});
-  else rows(0.f);
+  if (a.bf16_logits) launch(bf16{});
+  else launch(0.f);
   k_beam_merge<<<a.n, 256, 0, st>>>(a, np);
 }
 

@@ -23,9 +23,11 @@
  *    one request.  Per-slot decoding state (cache length, anchor, counters,
  *    done flag) lives on the device, so steps never synchronise with the host.
  *  - Storage type (wf_config.dtype): WF_F32 stores weights, acoustic memory and
- *    all caches in fp32; WF_BF16 stores them in bf16.  Activations, residual
- *    stream, LayerNorm, softmax, GELU, logits and all accumulation are fp32 in
- *    both.
+ *    all caches in fp32; WF_BF16 stores them in bf16.  WF_BF16_KV4 is WF_BF16 with
+ *    the acoustic keys and values of target and drafter in 4 bits (the form of wf_kv4
+ *    below, rounded from their bf16 values; large-v3: 71 MB a slot instead of 265).
+ *    Activations, residual stream, LayerNorm, softmax, GELU, logits and all
+ *    accumulation are fp32 in each.
  *  - Token ids are int32.
  */
 #ifndef WF_H
@@ -46,6 +48,7 @@ extern "C" {
 
 #define WF_F32 0
 #define WF_BF16 1
+#define WF_BF16_KV4 2 /* wf_config.dtype: WF_BF16 with the acoustic keys and values in 4 bits */
 
 /* Device status word bits (wf_status). */
 #define WF_STATUS_NONFINITE_LOGITS 0x1u  /* a verified row's logits had NaN/Inf */
@@ -87,7 +90,7 @@ typedef struct wf_config {
   int32_t n_tap;
   int32_t taps[WF_MAX_TAPS];
   int32_t eos_id;           /* end-of-transcript id, or -1 for none */
-  int32_t dtype;            /* WF_F32 or WF_BF16 */
+  int32_t dtype;            /* WF_F32, WF_BF16 or WF_BF16_KV4 */
   int32_t max_batch;        /* number of slots */
   int32_t draft_flags;      /* WF_DRAFT_* bits (0: the paper's drafter); n_draft_layer
                                sets the depth (2 in the paper, 5 in Table A4) */
@@ -227,7 +230,9 @@ int wf_step_noalloc(wf_handle* h, int slot0, int n, int k_max, const int32_t* dr
  * sampling), 1 = draft logits of the last draft [max_batch, block_k+1,
  * n_vocab] fp32 (row j >= 1 is mask j; same condition), 2 = per-slot state
  * int32 [max_batch, 16] (0 L, 1 anchor, 2 emitted, 3 max_new, 4 done,
- * 5 step), 3 = last drafted tokens int32 [max_batch, block_k].
+ * 5 step), 3 = last drafted tokens int32 [max_batch, block_k], 4 = acoustic keys and
+ * values (WF_BF16_KV4: per block, target then drafter, the data of a wf_kv4 of
+ * max_batch entries).
  */
 int wf_debug_ptr(wf_handle* h, int which, void** ptr);
 int wf_set_debug(wf_handle* h, int enable);

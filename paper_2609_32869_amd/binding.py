@@ -15,7 +15,7 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libwf.so")
 
-WF_F32, WF_BF16 = 0, 1
+WF_F32, WF_BF16, WF_BF16_KV4 = 0, 1, 2
 WF_MAX_TAPS = 8
 WF_STATUS_NONFINITE_LOGITS = 0x1
 WF_STATUS_POSITION_OVERFLOW = 0x2
@@ -135,8 +135,11 @@ def rng_words_device(seed, purpose, slot, step, pos, n, stream=None):
     return out
 
 
-def make_config(cfg, max_batch):
-    """WfConfig from a model-shape object (attributes as in wf_fixtures.ModelConfig)."""
+def make_config(cfg, max_batch, acoustic_bits=16):
+    """WfConfig from a model-shape object (attributes as in wf_fixtures.ModelConfig); acoustic_bits 4: bf16 storage
+    with the acoustic keys and values in 4 bits."""
+    if acoustic_bits not in (4, 16) or (acoustic_bits == 4 and cfg.dtype != "bf16"):
+        raise WfError("acoustic_bits must be 16, or 4 with bf16 storage")
     c = WfConfig()
     c.n_layer, c.d_model, c.n_head, c.d_ff = cfg.n_layer, cfg.d_model, cfg.n_head, cfg.d_ff
     c.n_vocab, c.n_ctx, c.n_frames = cfg.n_vocab, cfg.n_ctx, cfg.n_frames
@@ -144,7 +147,7 @@ def make_config(cfg, max_batch):
     for i, t in enumerate(cfg.taps):
         c.taps[i] = t
     c.eos_id = cfg.eos_id
-    c.dtype = WF_BF16 if cfg.dtype == "bf16" else WF_F32
+    c.dtype = WF_F32 if cfg.dtype != "bf16" else WF_BF16 if acoustic_bits == 16 else WF_BF16_KV4
     c.max_batch = max_batch
     c.draft_flags = getattr(cfg, "draft_flags", 0)
     return c
@@ -171,11 +174,12 @@ def to_device_storage(arr, dtype, device="cuda"):
 class WhisperFlash:
     """One libwf handle over a workspace tensor it owns."""
 
-    def __init__(self, cfg, max_batch, weights, stream=None):
-        """weights: device tensors in manifest order (storage type)."""
+    def __init__(self, cfg, max_batch, weights, stream=None, acoustic_bits=16):
+        """weights: device tensors in manifest order (storage type); acoustic_bits: of the acoustic keys and values
+        (16, or 4 with bf16 storage)."""
         self.lib = load_library()
         self.cfg = cfg
-        self.ccfg = make_config(cfg, max_batch)
+        self.ccfg = make_config(cfg, max_batch, acoustic_bits)
         self.max_batch = max_batch
         self.K = cfg.block_k
         nbytes = ctypes.c_size_t()
@@ -192,9 +196,9 @@ class WhisperFlash:
         self.h = h
 
     @classmethod
-    def from_host(cls, cfg, max_batch, ordered_arrays, stream=None):
+    def from_host(cls, cfg, max_batch, ordered_arrays, stream=None, acoustic_bits=16):
         dev = [to_device_storage(a, cfg.dtype) for a in ordered_arrays]
-        obj = cls(cfg, max_batch, dev, stream)
+        obj = cls(cfg, max_batch, dev, stream, acoustic_bits)
         torch.cuda.synchronize()
         del dev
         return obj

@@ -1554,6 +1554,10 @@ void Ops<S>::attn_cross(const CrossArgs& a, int n, hipStream_t st) {
     else launch_merge<S, false>(a, n, st);
   }
 }
+void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st) {
+  if (a.op.w != nullptr) launch_merge<bf16, true>(a, n, st);
+  else launch_merge<bf16, false>(a, n, st);
+}
 
 template void Ops<float>::attn_self(const AttnArgs&, int, hipStream_t);
 template void Ops<bf16>::attn_self(const AttnArgs&, int, hipStream_t);

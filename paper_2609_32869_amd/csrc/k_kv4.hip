@@ -89,6 +89,16 @@ struct Raw<bf16, N> {
   __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16); }
 };
 
+// A group's codes and scales, each lane its own.
+__device__ __forceinline__ void put_group(uint8_t* out, const uint2 (&kc)[2], const uint32_t (&ks)[2], const uint32_t (&vc)[4],
+                                          uint32_t vs) {
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
+  *reinterpret_cast<uint4*>(out + 16 * lane) = make_uint4(kc[0].x, kc[0].y, kc[1].x, kc[1].y);
+  *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = make_uint4(vc[0], vc[1], vc[2], vc[3]);
+  if ((kg & 1) == 0) *reinterpret_cast<uint16_t*>(out + kKv4KeyScale + 32 * (kg >> 1) + 2 * n) = (uint16_t)(ks[0] | ks[1] << 8);
+  if (kg == 0) *reinterpret_cast<uint32_t*>(out + kKv4ValueScale + 4 * n) = vs;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
@@ -142,10 +152,7 @@ __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
     vc[dt] = codes8(x, scale_f(sb));
     vs |= sb << (8 * dt);
   }
-  *reinterpret_cast<uint4*>(out + 16 * lane) = make_uint4(kc[0].x, kc[0].y, kc[1].x, kc[1].y);
-  *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = make_uint4(vc[0], vc[1], vc[2], vc[3]);
-  if ((kg & 1) == 0) *reinterpret_cast<uint16_t*>(out + kKv4KeyScale + 32 * (kg >> 1) + 2 * n) = (uint16_t)(ks[0] | ks[1] << 8);
-  if (kg == 0) *reinterpret_cast<uint32_t*>(out + kKv4ValueScale + 4 * n) = vs;
+  put_group(out, kc, ks, vc, vs);
 }
 
 void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
@@ -205,6 +212,89 @@ void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
   else k_kv4_load<float><<<grid, 256, 0, st>>>(a);
 }
 
+// ---------------------------------------------------------------- a decoder's keys and values
+// The same codes from and to the request-time product's layout, whose values lie
+// transposed: a lane's eight frames of a dim are 16 consecutive bytes.  Grid z: layers
+// (pack) or entries (unpack).
+__global__ void __launch_bounds__(256) k_kv4_pack(Kv4PackArgs a) {
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
+  const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, H = a.c.n_head, F = a.c.frames;
+  if (g >= a.c.groups) return;
+  const bf16* src = a.kv + (size_t)blockIdx.z * a.stride;
+  const bf16* K = src + (size_t)head * F * kHeadDim + 16 * kg;
+  const bf16* V = src + ((size_t)H * F + (size_t)head * a.vt_frames) * kHeadDim;
+  uint8_t* out = a.c.base + blockIdx.z * a.layer + (((size_t)a.slot0 * H + head) * a.c.groups + g) * kKv4Group;
+  Raw<bf16, 16> k[2];
+  Raw<bf16, 8> v[4];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) k[t].load(K + (size_t)min(g * 32 + 16 * t + n, F - 1) * kHeadDim, 1);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) v[dt].load(V + vt_index(4 * n + dt, g * 32 + 8 * kg), 1);
+  uint2 kc[2];
+  uint32_t ks[2], vc[4], vs = 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    float x[16];
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      x[j] = g * 32 + 16 * t + n < F ? k[t].get(j) : 0.f;
+      m = umax(m, mag(x[j]));
+    }
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
+    ks[t] = scale_of(__uint_as_float(m));
+    kc[t] = make_uint2(codes8(x, scale_f(ks[t])), codes8(x + 8, scale_f(ks[t])));
+  }
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) {
+    float x[8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = g * 32 + 8 * kg + j < F ? v[dt].get(j) : 0.f;
+      m = umax(m, mag(x[j]));
+    }
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
+    const uint32_t sb = scale_of(__uint_as_float(m));
+    vc[dt] = codes8(x, scale_f(sb));
+    vs |= sb << (8 * dt);
+  }
+  put_group(out, kc, ks, vc, vs);
+}
+void kv4_pack(const Kv4PackArgs& a, hipStream_t st) {
+  k_kv4_pack<<<dim3((a.c.groups + 3) / 4, a.c.n_head, a.layers), 256, 0, st>>>(a);
+}
+
+__global__ void __launch_bounds__(256) k_kv4_unpack(Kv4PackArgs a) {
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
+  const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, slot = a.slot0 + blockIdx.z, H = a.c.n_head, F = a.c.frames;
+  if (g >= a.c.groups) return;
+  const uint8_t* in = a.c.base + (((size_t)slot * H + head) * a.c.groups + g) * kKv4Group;
+  const uint4 k = *reinterpret_cast<const uint4*>(in + 16 * lane), v = *reinterpret_cast<const uint4*>(in + kKv4Values + 16 * lane);
+  const uint32_t ks = *reinterpret_cast<const uint16_t*>(in + kKv4KeyScale + 32 * (kg >> 1) + 2 * n);
+  const uint32_t vs = *reinterpret_cast<const uint32_t*>(in + kKv4ValueScale + 4 * n);
+  bf16* dst = a.kv + (size_t)slot * a.stride;
+  bf16* K = dst + (size_t)head * F * kHeadDim + 16 * kg;
+  bf16* V = dst + ((size_t)H * F + (size_t)head * a.vt_frames) * kHeadDim;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int f = g * 32 + 16 * t + n;
+    const float s = scale_f(t ? ks >> 8 : ks & 255);
+    if (f < F) {
+      st8(K + (size_t)f * kHeadDim, values8(t ? k.z : k.x, s));
+      st8(K + (size_t)f * kHeadDim + 8, values8(t ? k.w : k.y, s));
+    }
+  }
+  const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)  // frames past the last are zeros, as the layout has them
+    st8(V + vt_index(4 * n + dt, g * 32 + 8 * kg), values8(vw[dt], scale_f(vs >> (8 * dt) & 255)));
+}
+void kv4_unpack(const Kv4PackArgs& a, hipStream_t st) {
+  k_kv4_unpack<<<dim3((a.c.groups + 3) / 4, a.c.n_head, a.n), 256, 0, st>>>(a);
+}
+
 // ---------------------------------------------------------------- attention
 // Block (head, request, chunk of the groups) x (16 query rows), eight waves; a wave takes
 // steps of two groups, the next step's codes in flight while it multiplies the current one.
@@ -218,10 +308,13 @@ void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
 //            the merge kernel
 
 // bf16 terms of a query value (fp32: exact) and of a probability (fp32 output: exact;
-// bf16 output: 2^-16 relative, against the output's own 2^-9).
-template <typename T>
+// bf16 output: 2^-16 relative, against the output's own 2^-9).  A decoder step's operands
+// hold an fp32 value to 2^-16 themselves: two terms of each.
+enum { KV4_ROWS = 0, KV4_OPERAND = 1, KV4_RECORDS = 2 };
+template <typename T, int OUT>
 struct Terms {
-  static constexpr int q = sizeof(T) == 4 ? 3 : 1, p = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int q = sizeof(T) == 2 ? 1 : OUT == KV4_ROWS ? 3 : 2;
+  static constexpr int p = sizeof(T) == 2 || OUT != KV4_ROWS ? 2 : 3;
 };
 // Eight values as N bf16 terms.
 template <int N>
@@ -355,9 +448,10 @@ __device__ __forceinline__ void q_load(const Kv4AttendArgs& a, int r, int row, i
 constexpr int kAttWaves = 8, kAttStep = 2;
 constexpr int kKv4Record = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
 
-template <typename T>
-__global__ void __launch_bounds__(kAttWaves * 64) k_kv4_attend(Kv4AttendArgs a) {
-  constexpr int QT = Terms<T>::q, PT = Terms<T>::p, NW = kAttWaves, KS = kAttStep, S = NW * KS;
+template <typename T, int OUT, int NW = kAttWaves, int KS = kAttStep>
+__global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
+  constexpr int QT = Terms<T, OUT>::q, PT = Terms<T, OUT>::p, S = NW * KS;
+  StampScope stamp_scope(OUT == KV4_ROWS ? nullptr : a.stamp, NW * 64);
   __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kg = lane >> 4;
   const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, row = blockIdx.z * 16 + n;
@@ -413,7 +507,16 @@ __global__ void __launch_bounds__(kAttWaves * 64) k_kv4_attend(Kv4AttendArgs a) 
       L = fmaf(f, wl[j][i], L);
       O = fmaf(f, wo[j][i][d], O);
     }
-    if (a.nchunk == 1) {
+    if constexpr (OUT == KV4_OPERAND) {
+      put_op<bf16>(a.op, a.nsplit, a.R9, a.row0 + r * a.orr + i * a.ori, head * kHeadDim + d, O / L);
+    } else if constexpr (OUT == KV4_RECORDS) {
+      float* rec = a.part + (((size_t)r * a.c.n_head + head) * a.nchunk + chunk) * kXrPart;
+      rec[32 + t] = O;
+      if (d == 0) {
+        rec[i] = M * 0.693147180559945f;  // the merge's powers of e
+        rec[16 + i] = L;
+      }
+    } else if (a.nchunk == 1) {
       reinterpret_cast<T*>(a.out)[(((size_t)r * a.rows + blockIdx.z * 16 + i) * a.c.n_head + head) * kHeadDim + d] =
           from_f<T>(L == 0.f ? 0.f : O / L);
     } else {
@@ -488,9 +591,6 @@ __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
 
 int kv4_chunks(int n, int rows, int n_head, int frames) {
   const long long pairs = (long long)n * n_head * ((rows + 15) / 16), groups = kv4_groups(frames);
-#ifdef WF_CH
-  return (int)std::max<long long>(1, std::min<long long>(WF_CH / pairs, groups / 16));
-#endif
   if (groups <= 64 || pairs >= 512) return 1;
   return (int)std::max<long long>(1, std::min<long long>(1024 / pairs, groups / 16));
 }
@@ -502,7 +602,7 @@ size_t kv4_workspace(int n, int rows, int n_head, int frames) {
 template <typename T>
 static void attend_launch(const Kv4AttendArgs& a, hipStream_t st) {
   const int tiles = (a.rows + 15) / 16;
-  k_kv4_attend<T><<<dim3(a.c.n_head * a.nchunk, a.n, tiles), kAttWaves * 64, 0, st>>>(a);
+  k_kv4_attend<T, KV4_ROWS><<<dim3(a.c.n_head * a.nchunk, a.n, tiles), kAttWaves * 64, 0, st>>>(a);
   if (a.nchunk > 1) k_kv4_merge<T><<<dim3(a.c.n_head, a.n, a.rows), 256, 0, st>>>(a);
 }
 void kv4_attend(const Kv4AttendArgs& a0, hipStream_t st) {
@@ -511,6 +611,21 @@ void kv4_attend(const Kv4AttendArgs& a0, hipStream_t st) {
   a.cgroups = (a.c.groups + a.nchunk - 1) / a.nchunk;
   if (a.bf16_q) attend_launch<bf16>(a, st);
   else attend_launch<float>(a, st);
+}
+
+void kv4_attend_operand(const Kv4AttendArgs& a0, hipStream_t st) {
+  Kv4AttendArgs a = a0;
+  a.nchunk = 1;
+  a.cgroups = a.c.groups;
+  k_kv4_attend<float, KV4_OPERAND><<<dim3(a.c.n_head, a.n, (a.rows + 15) / 16), kAttWaves * 64, 0, st>>>(a);
+}
+// Four waves of a group each: the chunks of 128 frames that the step of one slot takes.
+void kv4_attend_records(const Kv4AttendArgs& a0, hipStream_t st) {
+  static_assert(kXrPart == 32 + kRows * 64, "records hold nine rows");
+  Kv4AttendArgs a = a0;
+  a.cgroups = cross_mx_chunk(1) / kKv4Frames;
+  a.nchunk = cross_mx_chunks(1, a.c.frames);
+  k_kv4_attend<float, KV4_RECORDS, 4, 1><<<dim3(a.c.n_head * a.nchunk, a.n), 256, 0, st>>>(a);
 }
 
 }  // namespace wf

@@ -12,7 +12,6 @@
 #include <vector>
 
 #include "wf_internal.h"
-#include "wf_ops.h"
 
 using namespace wf;
 
@@ -74,11 +73,14 @@ int fail(Handle* h, int code, const std::string& msg) {
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-size_t elt_bytes(const wf_config& c) { return c.dtype == WF_BF16 ? 2 : 4; }
+size_t elt_bytes(const wf_config& c) { return bf16_storage(c) ? 2 : 4; }
 
 int check_config(const wf_config* c, std::string& why) {
   if (!c) { why = "null config"; return WF_EINVAL; }
-  if (c->dtype != WF_F32 && c->dtype != WF_BF16) { why = "dtype must be WF_F32 or WF_BF16"; return WF_EINVAL; }
+  if (c->dtype != WF_F32 && c->dtype != WF_BF16 && c->dtype != WF_BF16_KV4) {
+    why = "dtype must be WF_F32, WF_BF16 or WF_BF16_KV4";
+    return WF_EINVAL;
+  }
   if (c->n_head <= 0 || c->d_model != c->n_head * kHeadDim) { why = "head width must be 64"; return WF_EINVAL; }
   if (c->d_model > 2048) { why = "d_model must be <= 2048"; return WF_EINVAL; }
   if (c->n_layer <= 0 || c->n_draft_layer <= 0) { why = "layer counts must be positive"; return WF_EINVAL; }
@@ -124,7 +126,7 @@ constexpr size_t kNoLn = ~(size_t)0;
 
 std::vector<ManEntry> manifest(const wf_config& c, const Layout& L, std::vector<Mat>* mats = nullptr) {
   const size_t d = c.d_model, F = c.d_ff;
-  const bool frag = c.dtype == WF_BF16;
+  const bool frag = bf16_storage(c);
   std::vector<ManEntry> m;
   std::vector<Mat> mm;
   // start a streamed matrix (bf16 storage only); returns its index for the entries
@@ -212,11 +214,11 @@ int compute_layout(const wf_config& c, Layout& L, bool many_rows) {
   L.pages_per_slot = c.n_ctx / kPage;
   // column blocks of the vocabulary head: 32-column tiles (bf16, batch 1), 64-column
   // GEMM blocks (bf16, several slots) or 16-column tiles (fp32)
-  L.nsplit_op = c.dtype != WF_BF16 ? 1 : c.max_batch == 1 ? 3 : 2;
-  L.head_blocks = c.dtype != WF_BF16 ? (int)((V + 15) / 16) : L.nsplit_op == 3 ? (int)((V + 31) / 32) : (int)((V + 63) / 64);
+  L.nsplit_op = !bf16_storage(c) ? 1 : c.max_batch == 1 ? 3 : 2;
+  L.head_blocks = !bf16_storage(c) ? (int)((V + 15) / 16) : L.nsplit_op == 3 ? (int)((V + 31) / 32) : (int)((V + 63) / 64);
   // raw bf16 matrices are staged at init in the cross K/V region before reordering
   L.stage_bytes = 0;
-  if (c.dtype == WF_BF16) {
+  if (bf16_storage(c)) {
     const size_t big = std::max({V * d, 3 * d * d, F * d, (size_t)c.n_tap * d * d});
     L.stage_bytes = big * eb;
   }
@@ -229,8 +231,8 @@ int compute_layout(const wf_config& c, Layout& L, bool many_rows) {
   L.status = region(256);
   L.aux = region(4 * B * 4);
   L.weights = region(w * eb);
-  L.xkv = region(std::max((size_t)(c.n_layer + c.n_draft_layer) * B * xkv_slot_elems(c.dtype == WF_BF16, c.n_frames, (int)d) * eb,
-                          L.stage_bytes));
+  const size_t layers = c.n_layer + c.n_draft_layer, xslot = xkv_slot_elems(bf16_storage(c), c.n_frames, (int)d) * eb;
+  L.xkv = region(std::max(kv4_storage(c) ? layers * kv4_layer_bytes(c) : layers * B * xslot, L.stage_bytes));
   L.skv = region((size_t)c.n_layer * 2 * B * L.pages_per_slot * H * kPage * kHeadDim * eb);
   L.hkv = region((size_t)c.n_draft_layer * 2 * B * H * c.n_ctx * kHeadDim * eb);
   // matrix operands: 3 bf16 terms per fp32 value as extra rows at batch 1, 2 terms as
@@ -267,13 +269,13 @@ int compute_layout(const wf_config& c, Layout& L, bool many_rows) {
   // batch 1 with bf16 storage: the second MLP product is split over k into
   // partial sums that the residual update reduces (about 240 blocks of 64 columns)
   L.fc2_split = 0;
-  if (c.dtype == WF_BF16 && L.nsplit_op == 3 && d <= (size_t)kLnFoldMaxK) {
+  if (bf16_storage(c) && L.nsplit_op == 3 && d <= (size_t)kLnFoldMaxK) {
     const int tiles64 = (int)((d + 63) / 64), ksteps = (int)(F / 32);
     L.fc2_split = std::max(1, std::min({kRlnMaxPartsHost, 240 / tiles64, ksteps}));
   }
   const int nparts = std::max({L.fc2_split, L.nsplit_op == 2 ? kFc2SplitBatch : 0, 1});
   L.part = region((size_t)nparts * R9 * d * 4);
-  const size_t xrec = c.dtype == WF_BF16 ? B * H * (size_t)cross_mx_chunks(1, c.n_frames) : 0;  // 1 slot: the smallest chunks
+  const size_t xrec = bf16_storage(c) ? B * H * (size_t)cross_mx_chunks(1, c.n_frames) : 0;  // 1 slot: the smallest chunks
   L.xpart = region(std::max((size_t)kXrMaxPartials, xrec) * kXrPart * 4);
   // fp32 storage: blocks of 16 columns, each taking all rows, split over k likewise (at most
   // kRlnRowParts buffers, which the row-per-block reduction takes): 384 columns are 24
@@ -288,10 +290,11 @@ int compute_layout(const wf_config& c, Layout& L, bool many_rows) {
     if (L.fc2_split) L.fc2_part = L.xpart;
   }
   L.lncd = region(L.nsplit_op == 3 ? cw * 4 : 0);
+  L.xtmp = region(kv4_storage(c) ? kv4_tmp_slots(c) * xslot : 0);
   L.stamps = region((size_t)kStampSlots * kStampWords * 8);
   // prompt pass over many rows: every prompt of a call up to kPreMaxRows rows, the
   // operands as bf16 planes
-  L.pre_rows = many_rows && c.dtype == WF_BF16 ? (int)std::min(B * (size_t)c.n_ctx, (size_t)kPreMaxRows) : 0;
+  L.pre_rows = many_rows && bf16_storage(c) ? (int)std::min(B * (size_t)c.n_ctx, (size_t)kPreMaxRows) : 0;
   const size_t PR = L.pre_rows, pb = (size_t)L.nsplit_op * 2;
   L.pre_h = region(PR * d * 4);
   L.pre_q = region(PR * d * 4);
@@ -403,13 +406,17 @@ struct Runner {
     }
     f(stamp);
   }
-  double eb() const { return c.dtype == WF_BF16 ? 2.0 : 4.0; }
+  double eb() const { return bf16_storage(c) ? 2.0 : 4.0; }
 
   const S* W(size_t off) const { return h->at<const S>(L.weights) + off; }
   float* F32(size_t off) const { return h->at<float>(off); }
   int* I32(size_t off) const { return h->at<int>(off); }
-  size_t xkv_slot() const { return xkv_slot_elems(c.dtype == WF_BF16, c.n_frames, c.d_model); }
-  int vt_frames() const { return c.dtype == WF_BF16 ? xkv_vt_frames(c.n_frames) : 0; }
+  size_t xkv_slot() const { return xkv_slot_elems(bf16_storage(c), c.n_frames, c.d_model); }
+  int vt_frames() const { return bf16_storage(c) ? xkv_vt_frames(c.n_frames) : 0; }
+  bool kv4() const { return kv4_storage(c); }
+  Kv4 kv4_layer(int l) const {
+    return Kv4{h->at<uint8_t>(L.xkv) + l * kv4_layer_bytes(c), c.n_head, kv4_groups(c.n_frames), c.n_frames};
+  }
   S* xkv_layer(int l) const { return h->at<S>(L.xkv) + (size_t)l * c.max_batch * xkv_slot(); }
   S* skv_layer(int l) const {
     return h->at<S>(L.skv) + (size_t)l * 2 * kv_stride();
@@ -419,7 +426,7 @@ struct Runner {
     return h->at<S>(L.hkv) + ((size_t)dl * 2 + kv) * c.max_batch * c.n_head * c.n_ctx * kHeadDim;
   }
 
-  bool frag() const { return c.dtype == WF_BF16; }
+  bool frag() const { return bf16_storage(c); }
   // Operand buffer at `off` with row length K, in the order read by products whose
   // weights have 32-column (wide) or 16-column tiles.
   Operand op(size_t off, int K, bool wide) const {
@@ -588,11 +595,11 @@ struct Runner {
     a.nsplit = L.nsplit_op;
     a.R9 = R9();
     a.vt_frames = vt_frames();
-    if (c.dtype == WF_BF16 && op.w == nullptr && cross_by_pair(n, c.n_head, c.n_frames)) {
+    if (bf16_storage(c) && op.w == nullptr && cross_by_pair(n, c.n_head, c.n_frames)) {
       a.by_pair = 1;
       a.chunk = kXpChunk;
       a.nchunk = (c.n_frames + kXpChunk - 1) / kXpChunk;
-    } else if (c.dtype == WF_BF16) {
+    } else if (bf16_storage(c)) {
       a.chunk = cross_mx_chunk(n);
       a.nchunk = cross_mx_chunks(n, c.n_frames);
     } else {
@@ -600,9 +607,48 @@ struct Runner {
     }
     a.part = F32(L.xpart);
     const double wbytes = op.w ? (double)c.d_model * c.d_model * eb() : 0.0;  // fused output product
+    if (kv4()) {
+      cross_kv4(a, n, layer, wbytes);
+      return;
+    }
     launch("attn_cross", 2.0 * c.n_head * c.n_frames * kHeadDim * eb() * n + wbytes, [&](unsigned long long* sp) {
       a.stamp = sp;
       Ops<S>::attn_cross(a, n, st);
+    });
+  }
+
+  // The same over keys and values held in 4 bits.  One slot with the fused output product:
+  // the 128-frame chunks' records and their merge, as in bf16; else a block per (head,
+  // slot) writes the next product's operand.
+  void cross_kv4(CrossArgs a, int n, int layer, double wbytes) {
+    Kv4AttendArgs t{};
+    t.c = kv4_layer(layer);
+    t.q = a.q + (size_t)a.slot0 * kRows * a.ldq;
+    t.sr = (long long)kRows * a.ldq;
+    t.si = a.ldq;
+    t.sh = kHeadDim;
+    t.vec = 1;
+    t.slot0 = a.slot0;
+    t.n = n;
+    t.rows = kRows;
+    t.op = a.out;
+    t.nsplit = a.nsplit;
+    t.R9 = a.R9;
+    t.row0 = a.slot0 * kRows;
+    t.orr = kRows;
+    t.ori = 1;
+    t.part = a.part;
+    const double bytes = (double)kKv4Group * t.c.groups * c.n_head * n + wbytes;
+    launch("attn_cross", bytes, [&](unsigned long long* sp) {
+      t.stamp = sp;
+      if (a.op.w == nullptr) {
+        kv4_attend_operand(t, st);
+      } else {
+        kv4_attend_records(t, st);
+        a.stamp = sp;
+        a.nchunk = cross_mx_chunks(1, c.n_frames);
+        attn_cross_merge(a, n, st);
+      }
     });
   }
 
@@ -912,7 +958,25 @@ struct Runner {
           a.n_head = c.n_head;
           a.vt_frames = vt_frames();
           a.scale = 1.f;
-          mm(a, MM_XKV, count, st);
+          if (!kv4()) {
+            mm(a, MM_XKV, count, st);
+            return;
+          }
+          // 4 bits: as many layers at a time as the transit buffer holds, then packed
+          const int most = kv4_tmp_slots(c);
+          const bf16 *w0 = a.B, *b0 = a.bias;
+          for (int l0 = 0; l0 < count; l0 += most) {
+            const int nl = std::min(most, count - l0);
+            a.B = w0 + l0 * a.sB;
+            a.bias = b0 + l0 * a.sBias;
+            a.out = h->at<bf16>(L.xtmp);
+            a.sO = (long long)xkv_slot();
+            mm(a, MM_XKV, nl, st);
+            Kv4PackArgs k{};
+            k.c = kv4_layer(first + l0); k.layer = kv4_layer_bytes(c); k.kv = h->at<bf16>(L.xtmp); k.stride = xkv_slot();
+            k.vt_frames = vt_frames(); k.slot0 = slot; k.n = 1; k.layers = nl;
+            kv4_pack(k, st);
+          }
         };
         group(0, c.n_layer, L.tb);
         if (!(c.draft_flags & WF_DRAFT_NO_AUDIO)) group(c.n_layer, c.n_draft_layer, L.db);
@@ -1012,7 +1076,13 @@ struct Runner {
         int ks = product("gemv_o", PRE_PART, A, b.w_o, b.b_o, d, d, part, d, nullptr);
         reduce(ks, b.b_o, b.ln2_g, b.ln2_b, true);
         product("gemv_q2", PRE_STORE, A, b.w_q2, b.b_q2, d, d, q, d, nullptr);
-        attend(true, xkv_layer(l), nullptr);
+        if (kv4()) {  // the pass's slots' keys and values of this block, as the attention reads them
+          Kv4PackArgs k{};
+          k.c = kv4_layer(l); k.kv = h->at<bf16>(L.xtmp); k.stride = xkv_slot(); k.vt_frames = vt_frames();
+          k.slot0 = plan.parts[ps.part0].slot; k.n = plan.parts[ps.part0 + ps.nparts - 1].slot - k.slot0 + 1; k.layers = 1;
+          kv4_unpack(k, st);
+        }
+        attend(true, kv4() ? h->at<S>(L.xtmp) : xkv_layer(l), nullptr);
         ks = product("gemv_o", PRE_PART, A, b.w_o2, b.b_o2, d, d, part, d, nullptr);
         reduce(ks, b.b_o2, b.ln3_g, b.ln3_b, true);
         product("gemv_fc1", PRE_GELU, A, b.w_fc1, b.b_fc1, F, d, nullptr, 0, Af, nullptr, true);
@@ -1117,7 +1187,7 @@ int dispatch(Handle* h, hipStream_t st, Fn&& fn) {
     h->nstamp = 0;
     stamp_init(h->at<unsigned long long>(h->lay.stamps), kStampSlots, st);
   }
-  if (h->cfg.dtype == WF_BF16) {
+  if (bf16_storage(h->cfg)) {
     fn(static_cast<bf16*>(nullptr));
   } else {
     fn(static_cast<float*>(nullptr));
@@ -1255,7 +1325,7 @@ int wf_init_weights(wf_handle** out, const wf_config* cfg, const void* const* we
     e = hipMemsetAsync(stage, 0, L.stage_bytes, st);
     if (e != hipSuccess) return cleanup(WF_EHIP, std::string("hipMemsetAsync: ") + hipGetErrorString(e));
   }
-  if (cfg->dtype == WF_BF16 && L.nsplit_op == 3 && (size_t)cfg->d_model <= (size_t)kLnFoldMaxK) {
+  if (bf16_storage(*cfg) && L.nsplit_op == 3 && (size_t)cfg->d_model <= (size_t)kLnFoldMaxK) {
     // the heads' column sums, from the caller's row-major embedding (manifest entry
     // 0), now that both final LayerNorms are in place
     float* cols = h->at<float>(L.lncd);
@@ -1282,7 +1352,7 @@ int wf_encode_memory_set(wf_handle* hh, int slot0, int n, const void* mem, void*
   Handle* h = reinterpret_cast<Handle*>(hh);
   if (int r = check_batch(h, slot0, n, false)) return r;
   if (!mem) return fail(h, WF_EINVAL, "null memory");
-  if (h->cfg.dtype == WF_BF16) {
+  if (bf16_storage(h->cfg)) {
     if (reinterpret_cast<uintptr_t>(mem) & 15) return fail(h, WF_EINVAL, "acoustic memory must be 16-byte aligned");
     MmArgs a{};
     a.M = h->cfg.n_frames; a.N = 2 * h->cfg.d_model; a.K = a.lda = a.ldb = h->cfg.d_model;
@@ -1455,6 +1525,7 @@ int wf_debug_ptr(wf_handle* hh, int which, void** ptr) {
     case 1: *ptr = h->at<void>(h->lay.dlogits); break;
     case 2: *ptr = h->at<void>(h->lay.state); break;
     case 3: *ptr = h->at<void>(h->lay.draft); break;
+    case 4: *ptr = h->at<void>(h->lay.xkv); break;
     default: return fail(h, WF_EINVAL, "unknown debug view");
   }
   return WF_OK;

@@ -10,6 +10,7 @@
 #include "../../include/wf.h"
 #include "wf_common.h"
 #include "wf_kernels.h"
+#include "wf_ops.h"
 
 namespace wf {
 
@@ -31,6 +32,7 @@ struct Layout {
   size_t a_d16, a_d32, a_f16, a_tap16, h, qkv, hp, kvh, hv, hi, tok, g, gmax, draft, lasth, logits, dlogits, part;
   size_t hm, hs, tmax, tsum, dmax, dsum, sst, spart;  // sampling: normalisers and draw partials
   size_t xpart;   // chunked cross-attention: partial records
+  size_t xtmp;    // 4-bit acoustic K/V: bf16 keys and values on their way in (encode) and out (prompt pass)
   size_t lncd;    // LayerNorm column sums of the folded products (batch 1, bf16)
   size_t stamps;  // launch timing slots (profiling)
   // prompt pass over many rows (bf16): residual rows, queries, operands, partial
@@ -116,6 +118,16 @@ struct Handle {
   // bytes of the per-call buffers (what wf_step_noalloc places in the static scratch)
   size_t transient_bytes() const { return lay.lncd - lay.a_d16; }
 };
+
+// bf16 storage, with the acoustic keys and values in bf16 or in 4 bits
+inline bool bf16_storage(const wf_config& c) { return c.dtype != WF_F32; }
+inline bool kv4_storage(const wf_config& c) { return c.dtype == WF_BF16_KV4; }
+// bytes of one block's 4-bit acoustic keys and values, all slots
+inline size_t kv4_layer_bytes(const wf_config& c) {
+  return (size_t)c.max_batch * c.n_head * kv4_groups(c.n_frames) * kKv4Group;
+}
+// slots (or layers of one slot) that xtmp holds
+inline int kv4_tmp_slots(const wf_config& c) { return c.max_batch < 4 ? 4 : c.max_batch; }
 
 // many_rows: with the buffers of the many-row prompt pass (bf16 storage)
 int compute_layout(const wf_config& c, Layout& L, bool many_rows = true);

@@ -212,6 +212,9 @@ inline void cross_chunks(int pairs, int n_frames, int& nchunk, int& chunk) {
   nchunk = (n_frames + ch - 1) / ch;
 }
 
+// Merge of the chunk records in a.part (with the fused output product if a.op is set).
+void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st);
+
 struct LnArgs {
   const float* x;  // [rows][d]
   const void* g;

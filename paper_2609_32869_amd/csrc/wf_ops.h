@@ -5,6 +5,7 @@
 #include <string>
 
 #include "wf_common.h"
+#include "wf_kernels.h"
 
 namespace wf {
 
@@ -85,6 +86,19 @@ struct Kv4LoadArgs {
   int bf16_out, slot0, n;
 };
 void kv4_load(const Kv4LoadArgs& a, hipStream_t st);
+// A decoder's acoustic keys and values: packed from, and unpacked to, the bf16 layout of
+// the request-time product (keys [head][frame][64], values [head][frame / 256][dim][256]).
+struct Kv4PackArgs {
+  Kv4 c;              // of the first layer
+  size_t layer;       // bytes from one layer's cache to the next's
+  bf16* kv;           // entry (or layer) i at i * stride elements
+  size_t stride;
+  int vt_frames;
+  int slot0, n;       // entries; layers: pack only
+  int layers;         // pack: layers of one entry (n 1); unpack: 1
+};
+void kv4_pack(const Kv4PackArgs& a, hipStream_t st);
+void kv4_unpack(const Kv4PackArgs& a, hipStream_t st);
 struct Kv4AttendArgs {
   Kv4 c;
   const void* q;  // element (r, i, h, d) at r * sr + i * si + h * sh + d
@@ -95,8 +109,17 @@ struct Kv4AttendArgs {
   int slot0, n, rows;
   float* part;  // chunk records (nchunk > 1)
   int nchunk, cgroups;  // chunks of the groups and groups of a chunk (set by the launcher)
+  // a decoder step's output rows: row i of request r is operand row row0 + r * orr + i * ori
+  Operand op;
+  int nsplit, R9, row0, orr, ori;
+  unsigned long long* stamp;  // launch timing slot (profiled calls), or null
 };
 size_t kv4_workspace(int n, int rows, int n_head, int frames);
 void kv4_attend(const Kv4AttendArgs& a, hipStream_t st);
+// A decoder step's rows (fp32 queries as two bf16 terms, like the step's other products):
+// into the next product's operand, or as the records of cross_mx_chunks(1) chunks for
+// attn_cross_merge (one request of at most nine rows).
+void kv4_attend_operand(const Kv4AttendArgs& a, hipStream_t st);
+void kv4_attend_records(const Kv4AttendArgs& a, hipStream_t st);
 
 }  // namespace wf

@@ -1,0 +1,154 @@
+"""Handles whose acoustic keys and values are held in 4 bits (WF_BF16_KV4): draft, verify and
+prompt passes against the oracle on the values that the handle holds, and those values against
+the oracle's own keys and values."""
+import numpy as np
+import pytest
+import torch
+
+import lockstep
+from lockstep import Lockstep
+from oracle import OracleOpts, Target, Drafter
+from oracle import operators as plain
+from wf_fixtures import MICRO, make_memory, make_prefix, make_weights
+
+pytestmark = pytest.mark.gpu
+TOL = 2e-2   # bf16 storage, as the other parity tests
+SMALL = MICRO.with_(name="micro-kv4", dtype="bf16", n_vocab=501, n_frames=77)
+
+
+def held(eng, cfg, layer, slot):
+    """Keys and values [F, d] of one block and slot that the handle holds."""
+    import ctypes
+    from paper_2609_32869_amd.binding import WfKv4
+    lib, F, H = eng.lib, cfg.n_frames, cfg.n_head
+    base, per = ctypes.c_void_p(), ctypes.c_size_t()
+    assert lib.wf_debug_ptr(eng.h, 4, ctypes.byref(base)) == 0
+    assert lib.wf_kv4_bytes(eng.max_batch, H, F, ctypes.byref(per)) == 0
+    c = WfKv4(base.value + layer * per.value, eng.max_batch, H, F)
+    k, v = (torch.empty((F, H, 64), device="cuda") for _ in range(2))
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.wf_kv4_load(ctypes.byref(c), slot, 1, k.data_ptr(), v.data_ptr(), 0, stream) == 0
+    torch.cuda.synchronize()
+    return [t.cpu().numpy().reshape(F, H * 64) for t in (k, v)]
+
+
+class OnHeld:
+    """The oracle's cross-attention on what the engine holds: patches the engine's width and the oracle's keys and
+    values (whose own are kept to compare)."""
+
+    def __init__(self, monkeypatch, cfg):
+        self.engine, self.own, self.slot = None, [], 0
+        build = lockstep.build_engine
+
+        def engine(c, W, max_batch):
+            arrays = [W.values[name] for name, _ in W.order]
+            self.engine = lockstep.WhisperFlash.from_host(c, max_batch, arrays, acoustic_bits=4)
+            return self.engine
+        assert build is not engine
+        monkeypatch.setattr(lockstep, "build_engine", engine)
+        target_kv, drafter_kv = Target.cross_kv, Drafter.cross_kv
+
+        def of_target(t, mem):
+            self.own.append((self.slot, 0, target_kv(t, mem)))
+            return [held(self.engine, cfg, l, self.slot) for l in range(cfg.n_layer)]
+
+        def of_drafter(d, mem):
+            self.own.append((self.slot, cfg.n_layer, drafter_kv(d, mem)))
+            out = [held(self.engine, cfg, cfg.n_layer + l, self.slot) for l in range(cfg.n_draft_layer)]
+            self.slot += 1
+            return out
+        monkeypatch.setattr(Target, "cross_kv", of_target)
+        monkeypatch.setattr(Drafter, "cross_kv", of_drafter)
+
+    def check_values(self, cfg):
+        """The held values are the oracle's bf16 keys and values in 4 bits.  A product whose bf16 rounding differs (one
+        in a few hundred: fp32 sums in another order) may take the neighbouring code where it lies at a border (a bf16
+        step is 2^-8 of it, codes are at least 2^-2 apart) or move a block's scale; so few values differ, by two codes
+        of the larger scale at most: half the block's largest value, 4 of 6."""
+        for slot, first, kv in self.own:
+            for l, (k, v) in enumerate(kv):
+                F, d = k.shape
+                own = plain.kv4_values(k.reshape(1, F, d // 64, 64), v.reshape(1, F, d // 64, 64), [F])
+                for g, w in zip(held(self.engine, cfg, first + l, slot), own):
+                    w = w.reshape(F, d)
+                    far = np.abs(g - w)
+                    assert (far > 0).mean() < 0.01
+                    assert far.max() <= 0.75 * np.abs(w).max()
+
+
+@pytest.mark.parametrize("batch", [1, 2, 5])
+def test_steps_against_the_oracle(monkeypatch, batch):
+    cfg = SMALL
+    W = make_weights(cfg)
+    on = OnHeld(monkeypatch, cfg)
+    prompts = [make_prefix(cfg, s, 5 + 9 * s) for s in range(batch)]   # one and more nine-row passes, and the many-row pass
+    ls = Lockstep(cfg, W, prompts, [30] * batch, TOL, OracleOpts(dtype=np.float32, kv_bf16=True))
+    on.check_values(cfg)
+    for _ in range(3):
+        ls.step()
+    ls.verify_only()
+    print(f"kv4 b{batch}: max |dlogit| draft {ls.max_dlogit:.3e} target {ls.max_tlogit:.3e}, near ties {ls.near_ties}")
+    assert ls.eng.status() == 0
+    ls.close()
+
+
+@pytest.mark.parametrize("d_model,batch,frames", [(512, 1, 1500), (768, 3, 300), (1408, 1, 40)])
+def test_other_widths(monkeypatch, d_model, batch, frames):
+    """8, 12 and 22 heads (the widest without the fused output product), a whole window's frames."""
+    cfg = SMALL.with_(name=f"kv4-{d_model}", d_model=d_model, n_head=d_model // 64, d_ff=2 * d_model, n_frames=frames)
+    W = make_weights(cfg)
+    on = OnHeld(monkeypatch, cfg)
+    prompts = [make_prefix(cfg, s, 30 - 6 * s) for s in range(batch)]
+    ls = Lockstep(cfg, W, prompts, [20] * batch, TOL, OracleOpts(dtype=np.float32, kv_bf16=True))
+    on.check_values(cfg)
+    ls.step()
+    ls.step()
+    print(f"kv4 d{d_model}: max |dlogit| draft {ls.max_dlogit:.3e} target {ls.max_tlogit:.3e}, near ties {ls.near_ties}")
+    ls.close()
+
+
+def test_graph_and_noalloc_steps_match():
+    """The eager step, its graph and the step without allocation give the same logits to the order of their atomic
+    adds (fp32 sums of 20 terms and fewer: 1e-4 of logits of order 1)."""
+    cfg = SMALL
+    W = make_weights(cfg)
+    arrays = [W.values[n] for n, _ in W.order]
+    mem = torch.stack([lockstep.to_device_storage(make_memory(cfg, 0), "bf16")])
+    prompt = torch.from_numpy(make_prefix(cfg, 0, 40)[None].copy()).cuda()
+    ovr = torch.randint(0, cfg.n_vocab, (1, 8), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    logs = []
+    for kind in ("eager", "graph", "noalloc"):
+        eng = lockstep.WhisperFlash.from_host(cfg, 1, arrays, acoustic_bits=4)
+        eng.encode_memory_set(0, mem)
+        eng.prefill(0, prompt, [40], [20])
+        eng.set_debug(True)
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            outs = eng._outs(1)
+            for _ in range(2):
+                if kind == "noalloc":
+                    eng.step_noalloc(0, 1, draft_override=ovr, outs=outs)
+                else:
+                    eng.step(0, 1, draft_override=ovr, outs=outs, use_graph=kind == "graph")
+        s.synchronize()
+        logs.append((eng.target_logits()[0, 0].clone() if kind != "noalloc" else None, outs[0].clone(), outs[1].clone()))
+        eng.close()
+    assert (logs[0][0] - logs[1][0]).abs().max() < 1e-4
+    for x in logs[1:]:
+        assert torch.equal(x[1], logs[0][1]) and torch.equal(x[2], logs[0][2])
+
+
+def test_memory_shrinks_and_fp32_is_refused():
+    import ctypes
+    from paper_2609_32869_amd import WfError, make_config, load_library
+    from wf_fixtures import LARGE_V3
+    lib, sizes = load_library(), []
+    for bits in (16, 4):
+        n = ctypes.c_size_t()
+        assert lib.wf_workspace_bytes(ctypes.byref(make_config(LARGE_V3, 96, bits)), ctypes.byref(n)) == 0
+        sizes.append(n.value)
+    assert sizes[0] - sizes[1] > 96 * 185e6
+    with pytest.raises(WfError):
+        make_config(MICRO, 1, 4)
+    with pytest.raises(WfError):
+        make_config(SMALL, 1, 8)

@@ -224,6 +224,42 @@ int wf_step_noalloc(wf_handle* h, int slot0, int n, int k_max, const int32_t* dr
                     int32_t* n_out, int32_t* n_acc, int32_t* done, void* stream);
 
 /*
+ * Beam search: n requests of `beams` hypotheses each on slots [slot0, slot0 + n * beams);
+ * beam b of request r is slot slot0 + b * n + r, so the requests' leaders (b = 0) are the
+ * first n slots.  The leaders have their acoustic memory set and their prompts prefilled
+ * (wf_encode_memory_set, wf_prefill); the beams share the leader's acoustic memory, and
+ * pages of the self-attention cache are shared until two beams part within one.
+ *
+ * wf_beam_begin starts a search from the leaders' prompts (their first tokens and anything
+ * decoded since are dropped).  last_tokens: device int32 [n], each prompt's last token;
+ * max_new: host int32 [n], >= 1, tokens at most; length_penalty >= 0: hypotheses rank by
+ * score / length^length_penalty (0: by score).  workspace: device, 256-byte aligned,
+ * wf_beam_bytes(h, n, beams) bytes, held until wf_beam_end.  Synchronises the stream.
+ *
+ * wf_beam_step extends every unfinished request by one token: the target over the beams'
+ * newest tokens (no drafter), the 2 * beams best continuations (wf_beam_select), of which
+ * in order those that end with eos_id become finished hypotheses and the others beams,
+ * until there are `beams` of them, then the page tables (wf_cache_reorder).  A request is done
+ * with `beams` finished hypotheses, max_new tokens, or a full context.  done: device
+ * int32 [n] or NULL.  use_graph as in wf_step.
+ *
+ * wf_beam_end writes the hypotheses, best first, and gives the slots back (empty: they
+ * need wf_prefill again): the finished ones and, where those are fewer than `beams`, the
+ * best unfinished.  tokens: device int32 [n, beams, len_max] (-1 past the end, longer ones
+ * are cut), eos_id included; lens: device int32 [n, beams] (0: none); scores: device fp32
+ * [n, beams], cumulative log-probabilities (-inf: none).
+ *
+ * While a search holds a slot, other calls on it return WF_ESTATE; sampling (temperature
+ * > 0) and a search exclude each other.  1 <= beams <= 16.
+ * Errors: WF_EINVAL, WF_ESTATE, WF_ESIZE, WF_EHIP.
+ */
+int wf_beam_bytes(wf_handle* h, int n, int beams, size_t* bytes);
+int wf_beam_begin(wf_handle* h, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
+                  float length_penalty, void* workspace, size_t ws_bytes, void* stream);
+int wf_beam_step(wf_handle* h, int slot0, int32_t* done, int use_graph, void* stream);
+int wf_beam_end(wf_handle* h, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream);
+
+/*
  * Debug views for tests: device pointers into the workspace (valid until
  * wf_release).  which: 0 = target logits of the last verify [max_batch,
  * block_k+1, n_vocab] fp32 (written when wf_set_debug(h, 1) or when

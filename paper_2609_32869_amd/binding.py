@@ -27,7 +27,7 @@ EXPORTS = ["wf_workspace_bytes", "wf_weight_count", "wf_weight_numel", "wf_init_
            "wf_release", "wf_strerror", "wf_last_error", "wf_rng_words_host", "wf_rng_words_device",
            "wf_encoder_workspace_bytes", "wf_encoder_weight_count", "wf_encoder_weight_numel", "wf_encoder_init",
            "wf_encoder_run", "wf_encoder_logmel", "wf_encoder_release", "wf_encoder_last_error",
-           "wf_beam_select_workspace_bytes", "wf_beam_select", "wf_cache_reorder", "wf_kv4_bytes", "wf_kv4_store",
+           "wf_beam_bytes", "wf_beam_begin", "wf_beam_step", "wf_beam_end", "wf_beam_select_workspace_bytes", "wf_beam_select", "wf_cache_reorder", "wf_kv4_bytes", "wf_kv4_store",
            "wf_kv4_load", "wf_kv4_attend_workspace_bytes", "wf_kv4_attend"]
 
 
@@ -98,6 +98,10 @@ def load_library(path=LIB_PATH):
         "wf_encoder_logmel": [P, P, P, P],
         "wf_encoder_release": [P],
         "wf_encoder_last_error": [P],
+        "wf_beam_bytes": [P, I, I, ctypes.POINTER(Z)],
+        "wf_beam_begin": [P, I, I, I, P, ctypes.POINTER(ctypes.c_int32), ctypes.c_float, P, Z, P],
+        "wf_beam_step": [P, I, P, I, P],
+        "wf_beam_end": [P, I, P, I, P, P, P],
         "wf_beam_select_workspace_bytes": [I, I, I, I, ctypes.POINTER(Z)],
         "wf_beam_select": [P, I, I64, I64, P, P, I, I, I, I, P, P, P, P, Z, P],
         "wf_cache_reorder": [P, I, Z, I, Z, P, P, I, I, I, I, P, P, P, I, P],
@@ -182,6 +186,7 @@ class WhisperFlash:
         self.ccfg = make_config(cfg, max_batch, acoustic_bits)
         self.max_batch = max_batch
         self.K = cfg.block_k
+        self.searches = {}  # beam searches by first slot: requests, beams, workspace
         nbytes = ctypes.c_size_t()
         self._check(self.lib.wf_workspace_bytes(ctypes.byref(self.ccfg), ctypes.byref(nbytes)))
         self.ws = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
@@ -270,6 +275,53 @@ class WhisperFlash:
         self._check(self.lib.wf_step_noalloc(self.h, slot0, n, k_max, _ptr(draft_override), _ptr(out), _ptr(n_out),
                                              _ptr(n_acc), _ptr(done), _stream(stream)))
         return out, n_out, n_acc, done
+
+    # ---- beam search (beam b of request r is slot slot0 + b * n + r)
+    def beam_begin(self, slot0, beams, last_tokens, max_new, length_penalty=1.0, stream=None):
+        """last_tokens: device int32 [n], the last prompt token of each prefilled leader; max_new: sequence of ints."""
+        n = last_tokens.shape[0]
+        nbytes = ctypes.c_size_t()
+        self._check(self.lib.wf_beam_bytes(self.h, n, beams, ctypes.byref(nbytes)))
+        ws = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        M = (ctypes.c_int32 * n)(*[int(x) for x in max_new])
+        self._check(self.lib.wf_beam_begin(self.h, slot0, n, beams, _ptr(last_tokens), M, float(length_penalty), _ptr(ws),
+                                           nbytes.value, _stream(stream)))
+        self.searches[slot0] = (n, beams, ws)
+
+    def beam_step(self, slot0, done=None, use_graph=False, stream=None):
+        """One token more for every unfinished request; done: device int32 [n] to write, or None."""
+        self._check(self.lib.wf_beam_step(self.h, slot0, _ptr(done), 1 if use_graph else 0, _stream(stream)))
+        return done
+
+    def beam_end(self, slot0, len_max=None, stream=None):
+        """(tokens int32 [n, beams, len_max], lens int32 [n, beams], scores fp32 [n, beams]), best hypothesis first."""
+        if slot0 not in self.searches:
+            raise WfError("invalid state (-2): no beam search begins at this slot")
+        n, beams, ws = self.searches[slot0]
+        len_max = self.cfg.n_ctx if len_max is None else len_max
+        tokens = torch.empty((n, beams, len_max), dtype=torch.int32, device="cuda")
+        lens = torch.empty((n, beams), dtype=torch.int32, device="cuda")
+        scores = torch.empty((n, beams), dtype=torch.float32, device="cuda")
+        self._check(self.lib.wf_beam_end(self.h, slot0, _ptr(tokens), len_max, _ptr(lens), _ptr(scores), _stream(stream)))
+        if stream is not None:
+            for t in (tokens, lens, scores, ws):
+                t.record_stream(stream)
+        del self.searches[slot0]
+        return tokens, lens, scores
+
+    def beam_search(self, slot0, tokens, lens, max_new, beams, length_penalty=1.0, use_graph=False, poll=8):
+        """A whole search from prompts (arguments as in prefill; the leaders' acoustic memory is set): prefill, steps
+        until every request is done (looked at every `poll` steps), hypotheses as in beam_end."""
+        n = tokens.shape[0]
+        self.prefill(slot0, tokens, lens, max_new)
+        last = tokens.gather(1, torch.tensor([[int(x) - 1] for x in lens], device=tokens.device)).view(n).contiguous()
+        self.beam_begin(slot0, beams, last, max_new, length_penalty)
+        done = torch.zeros(n, dtype=torch.int32, device="cuda")
+        for step in range(self.cfg.n_ctx):
+            self.beam_step(slot0, done, use_graph)
+            if step % poll == poll - 1 and bool(done.all()):
+                break
+        return self.beam_end(slot0)
 
     def set_debug(self, on):
         self._check(self.lib.wf_set_debug(self.h, 1 if on else 0))

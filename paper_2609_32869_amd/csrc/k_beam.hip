@@ -453,6 +453,19 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
 
 int beam_pieces(int vocab) { return (vocab + kBeamPiece - 1) / kBeamPiece; }
 
+static size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+size_t beam_space_bytes(int n, int beams, int vocab, int k) {
+  const size_t pieces = (size_t)n * beams * beam_pieces(vocab);
+  return up256(pieces * 8) + up256(pieces * 4) + 2 * up256(pieces * k * 4);
+}
+void beam_space(BeamSelectArgs& a, char* space) {
+  const size_t pieces = (size_t)a.n * a.beams * beam_pieces(a.vocab);
+  a.ps = reinterpret_cast<double*>(space);
+  a.pm = reinterpret_cast<float*>(space += up256(pieces * 8));
+  a.pv = reinterpret_cast<float*>(space += up256(pieces * 4));
+  a.pi = reinterpret_cast<int*>(space += up256(pieces * a.k * 4));
+}
+
 void beam_select(const BeamSelectArgs& a, hipStream_t st) {
   const int np = beam_pieces(a.vocab);
   const dim3 grid(a.n, np, a.beams);
@@ -485,7 +498,7 @@ __global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a
   const int r = blockIdx.y, t = threadIdx.x;
   const bool lead = blockIdx.x == 0;
   const int* T = a.tables + r * a.tr;
-  int* N = a.new_tables + r * a.tr;
+  int* N = a.new_tables + r * a.nr;
   const int* pool = a.pool + (size_t)r * a.pool_pages;
   // independent loads first
   const int p0 = pool[0], q0 = pool[min(t, a.pool_pages - 1)], raw = a.lens[r];
@@ -505,7 +518,7 @@ __global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a
     const int page = keep ? T[p * a.tb + c] : p0;
     if (keep && page >= 0 && page < a.n_pages) atomicOr(&used[page >> 5], 1u << (page & 31));
     if (keep && c == last) mine[j] = page;
-    if (lead && !(c == last && p >= 0)) N[j * a.tb + c] = page;
+    if (lead && !(c == last && p >= 0)) N[j * a.nb + c] = page;
   }
   __syncthreads();
   if (t < 64) {  // the first wave: which beams need a page, and the pool's free ones in order
@@ -532,7 +545,7 @@ __global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a
     if (moved) copy[__popcll(mv & below)] = make_int2(mine[j], page);
     if (t == 0) ncopy = __popcll(mv);
     if (lead && t < a.beams && parent[j] >= 0 && last < a.max_pages)
-      N[j * a.tb + last] = need ? (page >= 0 ? page : part ? mine[j] : p0) : mine[j];
+      N[j * a.nb + last] = need ? (page >= 0 ? page : part ? mine[j] : p0) : mine[j];
   }
   __syncthreads();
   const int nc = ncopy, region = blockIdx.x / parts, share = blockIdx.x % parts;
@@ -551,5 +564,174 @@ void cache_reorder(const ReorderArgs& a, hipStream_t st) {
   int parts = (int)std::max<long long>(1, std::min<long long>(1024 / have, (long long)(a.page_bytes / 4096)));
   k_cache_reorder<<<dim3((unsigned)(a.regions * parts), a.n), kReorderThreads, 0, st>>>(a, parts);
 }
+
+// ---------------------------------------------------------------- beam search on a handle's slots
+// A block per request; what a request decides is a few dozen dependent choices of one
+// thread, everything per beam or page is spread over the block.
+
+// Every beam starts on the leader's prompt with its last token unread (the first step
+// reads it and gives the first choice); only beam 0 runs until then.
+__global__ void __launch_bounds__(256) k_beam_begin(BeamArgs a) {
+  const int r = blockIdx.x, t = threadIdx.x, B = a.beams, P = a.pages, leader = a.slot0 + r;
+  const int* lead = a.state + leader * kStateInts;
+  const int L = lead[ST_LEN] - 1, anchor = a.last[r];
+  __syncthreads();  // the leader's state is read before it is written
+  for (int i = t; i < B * P; i += 256) {
+    const int b = i / P, j = i - b * P;
+    a.pool[(size_t)r * B * P + i] = j * a.max_batch + a.slot0 + b * a.n + r;
+    a.page_table[(size_t)(a.slot0 + b * a.n + r) * P + j] = j * a.max_batch + leader;
+  }
+  if (t < B) {
+    int* st = a.state + (a.slot0 + t * a.n + r) * kStateInts;
+    st[ST_L] = L;
+    st[ST_ANCHOR] = anchor;
+    st[ST_EMITTED] = 0;
+    st[ST_MAX_NEW] = 1 << 30;  // the search keeps its own budget
+    st[ST_DONE] = t > 0;
+    st[ST_STEP] = 0;
+    st[ST_NV] = 0;
+    st[ST_HN] = 0;
+    st[ST_LEN] = L + 1;
+    st[ST_LIVE] = 1;
+    a.scores[r * B + t] = t == 0 ? 0.f : -INFINITY;
+    a.parents[r * B + t] = 0;
+  }
+  if (t == 0) {
+    int* q = a.req + r * kBeamReq;
+    q[BR_L] = L;
+    q[BR_STEPS] = 0;
+    q[BR_FIN] = 0;
+    q[BR_DONE] = 0;
+    q[BR_MAX_NEW] = a.max_new[r];
+    q[BR_LIVE] = 1;
+  }
+}
+void beam_begin(const BeamArgs& a, hipStream_t st) { k_beam_begin<<<a.n, 256, 0, st>>>(a); }
+
+// After the selection: candidates in order, those that end with the end-of-transcript token
+// become finished hypotheses and the others beams, until there are as many beams.  Leaves
+// the tables as they were for the reordering.
+__global__ void __launch_bounds__(256) k_beam_advance(BeamArgs a) {
+  __shared__ int par[kMaxBeams], tok[kMaxBeams], fin_all;
+  __shared__ float sc[kMaxBeams];
+  const int r = blockIdx.x, t = threadIdx.x, B = a.beams, P = a.pages;
+  int* q = a.req + r * kBeamReq;
+  const bool was_done = q[BR_DONE] != 0;
+  const int L = q[BR_L], step = q[BR_STEPS];
+  for (int i = t; i < B * P; i += 256) {
+    const int b = i / P;
+    a.tables[(size_t)r * B * P + i] = a.page_table[(size_t)(a.slot0 + b * a.n + r) * P + (i - b * P)];
+  }
+  if (t < B) par[t] = -1;
+  __syncthreads();
+  if (t == 0 && !was_done) {
+    int live = 0, nf = q[BR_FIN];
+    for (int j = 0; j < a.k && live < B; ++j) {
+      const int b = a.cand_beam[r * a.k + j], v = a.cand_token[r * a.k + j];
+      const float s = a.cand_score[r * a.k + j];
+      if (b < 0) break;
+      if (v == a.eos) {
+        if (nf < B) {
+          a.fscore[r * B + nf] = s;
+          a.fstep[r * B + nf] = step;
+          a.fbeam[r * B + nf] = b;
+          ++nf;
+        }
+      } else {
+        par[live] = b;
+        tok[live] = v;
+        sc[live] = s;
+        ++live;
+      }
+    }
+    const bool done = nf >= B || live == 0 || step + 1 >= q[BR_MAX_NEW] || L + 1 >= a.n_ctx;
+    q[BR_L] = L + 1;
+    q[BR_STEPS] = step + 1;
+    q[BR_FIN] = nf;
+    q[BR_DONE] = done;
+    q[BR_LIVE] = live;
+    fin_all = done;
+  }
+  __syncthreads();
+  if (!was_done && t < B) {
+    const bool on = par[t] >= 0;
+    int* st = a.state + (a.slot0 + t * a.n + r) * kStateInts;
+    st[ST_L] = L + 1;
+    if (on) st[ST_ANCHOR] = tok[t];
+    st[ST_DONE] = !on || fin_all;
+    st[ST_STEP] = step + 1;
+    a.scores[r * B + t] = on ? sc[t] : -INFINITY;
+    const size_t at = ((size_t)step * a.n + r) * B + t;
+    a.bt[at] = on ? tok[t] : -1;
+    a.bp[at] = par[t];
+  }
+  if (t < B) a.parents[r * B + t] = was_done ? -1 : par[t];
+  if (t == 0) {
+    a.lens[r] = L + 1;
+    if (a.done) a.done[r] = was_done || fin_all;
+  }
+}
+void beam_advance(const BeamArgs& a, hipStream_t st) { k_beam_advance<<<a.n, 256, 0, st>>>(a); }
+
+// The hypotheses, best first by score / length^penalty: the finished ones and, where those
+// are fewer than the beams, the best live ones.  Then the slots are given back.
+__global__ void __launch_bounds__(256) k_beam_end(BeamArgs a) {
+  __shared__ float sc[kMaxBeams], val[kMaxBeams];
+  __shared__ int hs[kMaxBeams], hb[kMaxBeams], he[kMaxBeams], order[kMaxBeams], nh;
+  const int r = blockIdx.x, t = threadIdx.x, B = a.beams, P = a.pages;
+  const int* q = a.req + r * kBeamReq;
+  if (t == 0) {
+    int n = 0;
+    for (int i = 0; i < q[BR_FIN]; ++i, ++n) {  // the path of fbeam up to the step before, then the closing token
+      sc[n] = a.fscore[r * B + i];
+      hs[n] = a.fstep[r * B + i] - 1;
+      hb[n] = a.fbeam[r * B + i];
+      he[n] = 1;
+    }
+    if (q[BR_STEPS] > 0)
+      for (int b = 0; b < q[BR_LIVE] && n < B; ++b, ++n) {  // beams come best first
+        sc[n] = a.scores[r * B + b];
+        hs[n] = q[BR_STEPS] - 1;
+        hb[n] = b;
+        he[n] = 0;
+      }
+    for (int i = 0; i < n; ++i) {
+      val[i] = sc[i] / powf((float)(hs[i] + 1 + he[i]), a.length_penalty);
+      int j = i;
+      for (; j > 0 && val[order[j - 1]] < val[i]; --j) order[j] = order[j - 1];
+      order[j] = i;
+    }
+    nh = n;
+  }
+  __syncthreads();
+  if (t < B) {
+    int* out = a.tokens + ((size_t)r * B + t) * a.len_max;
+    int len = 0;
+    if (t < nh) {
+      const int h = order[t];
+      int b = hb[h];
+      len = hs[h] + 1 + he[h];
+      if (he[h] && len - 1 < a.len_max) out[len - 1] = a.eos;
+      for (int s = hs[h]; s >= 0; --s) {
+        const size_t at = ((size_t)s * a.n + r) * B + b;
+        if (s < a.len_max) out[s] = a.bt[at];
+        b = a.bp[at];
+      }
+    }
+    for (int s = len; s < a.len_max; ++s) out[s] = -1;
+    a.out_len[r * B + t] = len;
+    a.out_score[r * B + t] = t < nh ? sc[order[t]] : -INFINITY;
+  }
+  for (int i = t; i < B * P; i += 256) {
+    const int b = i / P, j = i - b * P, slot = a.slot0 + b * a.n + r;
+    a.page_table[(size_t)slot * P + j] = j * a.max_batch + slot;
+  }
+  if (t < B) {
+    int* st = a.state + (a.slot0 + t * a.n + r) * kStateInts;
+    st[ST_LIVE] = 0;
+    st[ST_DONE] = 1;
+  }
+}
+void beam_end(const BeamArgs& a, hipStream_t st) { k_beam_end<<<a.n, 256, 0, st>>>(a); }
 
 }  // namespace wf

@@ -11,8 +11,6 @@ namespace {
 
 int bad(const char* msg) { return op_fail(WF_EINVAL, msg); }
 
-size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 int launched() {
@@ -38,19 +36,6 @@ int check_dtype(int dtype, size_t& e) {
   return WF_OK;
 }
 
-struct SelectSpace {
-  size_t ps, pm, pv, pi, total;
-};
-SelectSpace select_space(int n, int beams, int vocab, int k) {
-  const size_t pieces = (size_t)n * beams * beam_pieces(vocab);
-  SelectSpace s;
-  s.ps = 0;
-  s.pm = up256(pieces * 8);
-  s.pv = s.pm + up256(pieces * 4);
-  s.pi = s.pv + up256(pieces * k * 4);
-  s.total = s.pi + up256(pieces * k * 4);
-  return s;
-}
 int check_select(int n, int beams, int vocab, int k) {
   if (n < 1 || n > kMaxGrid) return bad("n must be in [1, 65535]");
   if (beams < 1 || beams > kMaxBeams) return bad("beams must be in [1, 16]");
@@ -92,7 +77,7 @@ int wf_beam_select_workspace_bytes(int n, int beams, int n_vocab, int k, size_t*
   return guarded([&] {
     if (int r = check_select(n, beams, n_vocab, k)) return r;
     if (!bytes) return bad("null bytes");
-    *bytes = select_space(n, beams, n_vocab, k).total;
+    *bytes = beam_space_bytes(n, beams, n_vocab, k);
     return WF_OK;
   });
 }
@@ -110,9 +95,7 @@ int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t be
     if (req_stride < 0 || beam_stride < 0 || req_stride > ((int64_t)1 << 40) || beam_stride > ((int64_t)1 << 40))
       return bad("stride out of range");
     if (!workspace || !aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
-    const SelectSpace s = select_space(n, beams, n_vocab, k);
-    if (ws_bytes < s.total) return op_fail(WF_ESIZE, "workspace too small");
-    char* w = static_cast<char*>(workspace);
+    if (ws_bytes < beam_space_bytes(n, beams, n_vocab, k)) return op_fail(WF_ESIZE, "workspace too small");
     BeamSelectArgs a{};
     a.logits = logits;
     a.bf16_logits = dtype == WF_BF16;
@@ -124,10 +107,7 @@ int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t be
     a.beams = beams;
     a.vocab = n_vocab;
     a.k = k;
-    a.ps = reinterpret_cast<double*>(w + s.ps);
-    a.pm = reinterpret_cast<float*>(w + s.pm);
-    a.pv = reinterpret_cast<float*>(w + s.pv);
-    a.pi = reinterpret_cast<int*>(w + s.pi);
+    beam_space(a, static_cast<char*>(workspace));
     a.out_score = out_score;
     a.out_beam = out_beam;
     a.out_token = out_token;
@@ -164,8 +144,8 @@ int wf_cache_reorder(void* cache, int n_regions, size_t region_stride, int n_pag
     a.n_pages = n_pages;
     a.tables = tables;
     a.new_tables = new_tables;
-    a.tb = max_pages;
-    a.tr = (long long)beams * max_pages;
+    a.tb = a.nb = max_pages;
+    a.tr = a.nr = (long long)beams * max_pages;
     a.parents = parents;
     a.lens = lens;
     a.pool = pool;

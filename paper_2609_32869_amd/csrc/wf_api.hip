@@ -355,6 +355,48 @@ PrePlan pre_plan(const Handle* h, int slot0, int n, const int32_t* lens, int max
   return pl;
 }
 
+// A search's buffers: n requests of B beams over `steps` positions.
+BeamSpace beam_layout(const Handle* h, int n, int B) {
+  BeamSpace s{};
+  size_t o = 0;
+  auto region = [&](size_t bytes) { size_t r = o; o = align_up(o + bytes, 256); return r; };
+  const size_t nb = (size_t)n * B, P = h->lay.pages_per_slot, steps = h->cfg.n_ctx;
+  s.req = region((size_t)n * kBeamReq * 4);
+  s.scores = region(nb * 4);
+  s.cs = region(2 * nb * 4);
+  s.cb = region(2 * nb * 4);
+  s.ct = region(2 * nb * 4);
+  s.parents = region(nb * 4);
+  s.lens = region((size_t)n * 4);
+  s.pool = region(nb * P * 4);
+  s.tables = region(nb * P * 4);
+  s.bt = region(steps * nb * 4);
+  s.bp = region(steps * nb * 4);
+  s.fscore = region(nb * 4);
+  s.fstep = region(nb * 4);
+  s.fbeam = region(nb * 4);
+  s.last = region((size_t)n * 4);
+  s.max_new = region((size_t)n * 4);
+  s.select_bytes = beam_space_bytes(n, B, h->cfg.n_vocab, 2 * B);
+  s.select = region(s.select_bytes);
+  s.total = o;
+  return s;
+}
+BeamArgs beam_args(const Handle* h, const BeamSearch& bs) {
+  auto i32 = [&](size_t off) { return reinterpret_cast<int*>(bs.ws + off); };
+  auto f32 = [&](size_t off) { return reinterpret_cast<float*>(bs.ws + off); };
+  const BeamSpace& s = bs.sp;
+  BeamArgs g{};
+  g.state = h->at<int>(h->lay.state); g.page_table = h->at<int>(h->lay.page_table);
+  g.slot0 = bs.slot0; g.n = bs.n; g.beams = bs.beams; g.pages = h->lay.pages_per_slot; g.max_batch = h->cfg.max_batch;
+  g.eos = h->cfg.eos_id; g.n_ctx = h->cfg.n_ctx; g.k = 2 * bs.beams;
+  g.req = i32(s.req); g.scores = f32(s.scores); g.cand_score = f32(s.cs); g.cand_beam = i32(s.cb); g.cand_token = i32(s.ct);
+  g.parents = i32(s.parents); g.lens = i32(s.lens); g.pool = i32(s.pool); g.tables = i32(s.tables);
+  g.bt = i32(s.bt); g.bp = i32(s.bp); g.fscore = f32(s.fscore); g.fstep = i32(s.fstep); g.fbeam = i32(s.fbeam);
+  g.last = i32(s.last); g.max_new = i32(s.max_new); g.length_penalty = bs.length_penalty;
+  return g;
+}
+
 template <typename S>
 struct Runner {
   Handle* h;
@@ -366,6 +408,7 @@ struct Runner {
   // The LayerNorm operand of the next product was already written by the
   // residual reduction (Ad16 for a block's first product, Ad32 for the head).
   bool ln_ready = false;
+  int share = 0;  // beams: leaders whose acoustic memory the slots of the pass share (see CrossArgs)
   int tap_next = -1;  // drafter tap the next folded q|k|v product writes from its rows (-1: none)
 
   // The LayerNorm that follows a block: the next block's first one, or the final
@@ -595,6 +638,7 @@ struct Runner {
     a.nsplit = L.nsplit_op;
     a.R9 = R9();
     a.vt_frames = vt_frames();
+    a.share = share;
     if (bf16_storage(c) && op.w == nullptr && cross_by_pair(n, c.n_head, c.n_frames)) {
       a.by_pair = 1;
       a.chunk = kXpChunk;
@@ -638,7 +682,14 @@ struct Runner {
     t.orr = kRows;
     t.ori = 1;
     t.part = a.part;
-    const double bytes = (double)kKv4Group * t.c.groups * c.n_head * n + wbytes;
+    if (a.share && a.op.w == nullptr) {
+      // a request's beams are the rows: each slot's first row, all on the leader's memory
+      t.n = a.share;
+      t.rows = n / a.share;
+      t.si = (long long)a.share * kRows * a.ldq;
+      t.ori = a.share * kRows;
+    }
+    const double bytes = (double)kKv4Group * t.c.groups * c.n_head * t.n + wbytes;
     launch("attn_cross", bytes, [&](unsigned long long* sp) {
       t.stamp = sp;
       if (a.op.w == nullptr) {
@@ -927,6 +978,45 @@ struct Runner {
     history_apply(slot0, n);
   }
 
+  // One step of a beam search: the target over every beam's newest token, the choice of
+  // the next beams, their bookkeeping and their page tables.
+  void beam_step(const BeamSearch& bs, int* done) {
+    const int slot0 = bs.slot0, n = bs.n, B = bs.beams, total = n * B, P = L.pages_per_slot;
+    auto at = [&](size_t off) { return bs.ws + off; };
+    BeginArgs ba{};
+    ba.state = I32(L.state); ba.draft = I32(L.draft); ba.tok = I32(L.tok); ba.emb = W(L.tok_emb); ba.emb_kind = wk(true); ba.pos = W(L.pos_emb);
+    ba.h = F32(L.h); ba.slot0 = slot0; ba.d = c.d_model; ba.n_vocab = c.n_vocab; ba.n_ctx = c.n_ctx;
+    ba.block_k = c.block_k; ba.k_max = 0;
+    ba.page_table = I32(L.page_table); ba.pages_per_slot = P;
+    ba.status = h->at<unsigned>(L.status);
+    launch("begin", 0, [&](unsigned long long*) { Ops<S>::verify_begin(ba, total, st); });
+    share = n;
+    target_forward(slot0, total);
+    share = 0;
+    head(slot0, total, F32(L.h), L.lnf_g, L.lnf_b, F32(L.logits));
+    BeamSelectArgs sa{};
+    sa.logits = F32(L.logits) + (size_t)slot0 * kRows * c.n_vocab;
+    sa.sr = (long long)kRows * c.n_vocab;
+    sa.sb = (long long)n * kRows * c.n_vocab;
+    sa.scores = reinterpret_cast<const float*>(at(bs.sp.scores)); sa.suppress = h->suppress;
+    sa.n = n; sa.beams = B; sa.vocab = c.n_vocab; sa.k = 2 * B;
+    beam_space(sa, at(bs.sp.select));
+    sa.out_score = reinterpret_cast<float*>(at(bs.sp.cs)); sa.out_beam = reinterpret_cast<int*>(at(bs.sp.cb));
+    sa.out_token = reinterpret_cast<int*>(at(bs.sp.ct));
+    launch("beam_select", 4.0 * total * c.n_vocab, [&](unsigned long long*) { beam_select(sa, st); });
+    BeamArgs g = beam_args(h, bs);
+    g.done = done;
+    launch("beam_advance", 0, [&](unsigned long long*) { beam_advance(g, st); });
+    ReorderArgs ra{};
+    ra.cache = h->at<char>(L.skv); ra.regions = 2 * c.n_layer; ra.region_stride = kv_stride() * sizeof(S);
+    ra.page_bytes = (size_t)c.n_head * kPage * kHeadDim * sizeof(S); ra.n_pages = c.max_batch * P;
+    ra.tables = g.tables; ra.tr = (long long)B * P; ra.tb = P;
+    ra.new_tables = I32(L.page_table) + (size_t)slot0 * P; ra.nr = P; ra.nb = (long long)n * P;
+    ra.parents = g.parents; ra.lens = g.lens; ra.pool = g.pool; ra.n = n; ra.beams = B; ra.max_pages = P;
+    ra.pool_pages = B * P; ra.page_tokens = kPage;
+    launch("cache_reorder", 0, [&](unsigned long long*) { cache_reorder(ra, st); });
+  }
+
   // The history already holds every verified position: each verify writes the
   // drafter history of its rows after the acceptance (Appendix A.2), so any
   // sequence of verify and draft calls sees a complete history.
@@ -1203,9 +1293,43 @@ int dispatch(Handle* h, hipStream_t st, Fn&& fn) {
   return WF_OK;
 }
 
+// Replay the graph of `key`, captured from enqueue() on first use.
+template <typename F>
+int replay(Handle* h, const GraphKey& key, hipStream_t st, F&& enqueue) {
+  if (!st) return fail(h, WF_EINVAL, "graph replay needs a non-null stream");
+  auto it = h->graphs.find(key);
+  if (it == h->graphs.end()) {
+    h->cap_recs.clear();
+    HIPCK(h, hipStreamBeginCapture(st, hipStreamCaptureModeThreadLocal));
+    h->capturing = true;
+    int r = enqueue();
+    h->capturing = false;
+    hipGraph_t g = nullptr;
+    hipError_t e = hipStreamEndCapture(st, &g);
+    auto drop_recs = [&] { h->cap_recs.clear(); };
+    if (r) { if (g) (void)hipGraphDestroy(g); drop_recs(); return r; }
+    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipStreamEndCapture: ") + hipGetErrorString(e)); }
+    hipGraphExec_t ex = nullptr;
+    e = hipGraphInstantiate(&ex, g, nullptr, nullptr, 0);
+    (void)hipGraphDestroy(g);
+    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipGraphInstantiate: ") + hipGetErrorString(e)); }
+    it = h->graphs.emplace(key, ex).first;
+    if (key.prof) h->graph_recs[key] = h->cap_recs;
+    h->cap_recs.clear();
+  }
+  HIPCK(h, hipGraphLaunch(it->second, st));
+  if (key.prof) {  // profiled replay: read this replay's launch durations now
+    HIPCK(h, hipStreamSynchronize(st));
+    return collect_stamps(h, h->graph_recs[key]);
+  }
+  return WF_OK;
+}
+
 int check_batch(Handle* h, int slot0, int n, bool need_live) {
   if (!h) return fail(nullptr, WF_EINVAL, "null handle");
-  if (n < 1 || slot0 < 0 || slot0 + n > h->cfg.max_batch) return fail(h, WF_EINVAL, "slot range out of bounds");
+  if (n < 1 || slot0 < 0 || slot0 > h->cfg.max_batch - n) return fail(h, WF_EINVAL, "slot range out of bounds");
+  for (int s = slot0; s < slot0 + n; ++s)
+    if (h->beam[s]) return fail(h, WF_ESTATE, "slot belongs to a beam search");
   if (need_live)
     for (int s = slot0; s < slot0 + n; ++s)
       if (!h->live[s]) return fail(h, WF_ESTATE, "slot not prefilled");
@@ -1281,6 +1405,7 @@ int wf_init_weights(wf_handle** out, const wf_config* cfg, const void* const* we
   h->ws = static_cast<char*>(workspace);
   h->ws_bytes = ws_bytes;
   h->live.assign(cfg->max_batch, 0);
+  h->beam.assign(cfg->max_batch, 0);
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto cleanup = [&](int code, const std::string& msg) { delete h; return fail(nullptr, code, msg); };
   {
@@ -1459,34 +1584,8 @@ int wf_step(wf_handle* hh, int slot0, int n, int k_max, const int32_t* ovr, int3
   if (k_max < 0 || k_max > h->cfg.block_k) return fail(h, WF_EINVAL, "k_max out of range");
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!use_graph) return step_enqueue(h, slot0, n, k_max, ovr, out, n_out, n_acc, done, st);
-  if (!st) return fail(h, WF_EINVAL, "graph replay needs a non-null stream");
   GraphKey key{slot0, n, k_max, ovr, out, n_out, n_acc, done, h->prof};
-  auto it = h->graphs.find(key);
-  if (it == h->graphs.end()) {
-    h->cap_recs.clear();
-    HIPCK(h, hipStreamBeginCapture(st, hipStreamCaptureModeThreadLocal));
-    h->capturing = true;
-    int r = step_enqueue(h, slot0, n, k_max, ovr, out, n_out, n_acc, done, st);
-    h->capturing = false;
-    hipGraph_t g = nullptr;
-    hipError_t e = hipStreamEndCapture(st, &g);
-    auto drop_recs = [&] { h->cap_recs.clear(); };
-    if (r) { if (g) (void)hipGraphDestroy(g); drop_recs(); return r; }
-    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipStreamEndCapture: ") + hipGetErrorString(e)); }
-    hipGraphExec_t ex = nullptr;
-    e = hipGraphInstantiate(&ex, g, nullptr, nullptr, 0);
-    (void)hipGraphDestroy(g);
-    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipGraphInstantiate: ") + hipGetErrorString(e)); }
-    it = h->graphs.emplace(key, ex).first;
-    if (key.prof) h->graph_recs[key] = h->cap_recs;
-    h->cap_recs.clear();
-  }
-  HIPCK(h, hipGraphLaunch(it->second, st));
-  if (key.prof) {  // profiled replay: read this replay's launch durations now
-    HIPCK(h, hipStreamSynchronize(st));
-    return collect_stamps(h, h->graph_recs[key]);
-  }
-  return WF_OK;
+  return replay(h, key, st, [&] { return step_enqueue(h, slot0, n, k_max, ovr, out, n_out, n_acc, done, st); });
 }
 
 int wf_step_noalloc(wf_handle* hh, int slot0, int n, int k_max, const int32_t* ovr, int32_t* out, int32_t* n_out,
@@ -1515,6 +1614,94 @@ int wf_step_noalloc(wf_handle* hh, int slot0, int n, int k_max, const int32_t* o
   h->scratch = nullptr;
   h->prof = prof;
   return r;
+}
+
+// ---------------------------------------------------------------- beam search
+static int beam_check(Handle* h, int slot0, int n, int beams) {
+  if (!h) return fail(nullptr, WF_EINVAL, "null handle");
+  if (beams < 1 || beams > kMaxBeams) return fail(h, WF_EINVAL, "beams must be in [1, 16]");
+  if (n < 1 || slot0 < 0 || n > h->cfg.max_batch / beams || slot0 > h->cfg.max_batch - n * beams)
+    return fail(h, WF_EINVAL, "the beams' slots are out of bounds");
+  if (h->cfg.n_vocab > kMaxVocab) return fail(h, WF_EINVAL, "n_vocab must be <= 2^20");
+  return WF_OK;
+}
+
+int wf_beam_bytes(wf_handle* hh, int n, int beams, size_t* bytes) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  if (int r = beam_check(h, 0, n, beams)) return r;
+  if (!bytes) return fail(h, WF_EINVAL, "null bytes");
+  *bytes = beam_layout(h, n, beams).total;
+  return WF_OK;
+}
+
+int wf_beam_begin(wf_handle* hh, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
+                  float length_penalty, void* workspace, size_t ws_bytes, void* stream) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  if (int r = beam_check(h, slot0, n, beams)) return r;
+  if (int r = check_batch(h, slot0, n * beams, false)) return r;
+  if (int r = check_batch(h, slot0, n, true)) return r;
+  if (!last_tokens || !max_new) return fail(h, WF_EINVAL, "null argument");
+  for (int r = 0; r < n; ++r)
+    if (max_new[r] < 1) return fail(h, WF_EINVAL, "max_new must be >= 1");
+  if (!(length_penalty >= 0.f) || std::isinf(length_penalty)) return fail(h, WF_EINVAL, "length_penalty must be finite and >= 0");
+  if (h->temperature > 0.f) return fail(h, WF_ESTATE, "a beam search needs temperature 0");
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(h, WF_EINVAL, "workspace must be 256-byte aligned");
+  BeamSearch bs{slot0, n, beams, length_penalty, static_cast<char*>(workspace), beam_layout(h, n, beams)};
+  if (ws_bytes < bs.sp.total) return fail(h, WF_ESIZE, "workspace too small");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  HIPCK(h, hipMemcpyAsync(bs.ws + bs.sp.last, last_tokens, (size_t)n * 4, hipMemcpyDeviceToDevice, st));
+  HIPCK(h, hipMemcpyAsync(bs.ws + bs.sp.max_new, max_new, (size_t)n * 4, hipMemcpyHostToDevice, st));
+  beam_begin(beam_args(h, bs), st);
+  HIPCK(h, hipGetLastError());
+  HIPCK(h, hipStreamSynchronize(st));
+  h->searches[slot0] = bs;
+  for (int s = slot0; s < slot0 + n * beams; ++s) h->beam[s] = 1;
+  return WF_OK;
+}
+
+int wf_beam_step(wf_handle* hh, int slot0, int32_t* done, int use_graph, void* stream) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  if (!h) return fail(nullptr, WF_EINVAL, "null handle");
+  auto it = h->searches.find(slot0);
+  if (it == h->searches.end()) return fail(h, WF_ESTATE, "no beam search begins at this slot");
+  if (h->temperature > 0.f) return fail(h, WF_ESTATE, "a beam search needs temperature 0");
+  const BeamSearch& bs = it->second;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto enqueue = [&] {
+    return dispatch(h, st, [&](auto* tag) {
+      using S = std::remove_pointer_t<decltype(tag)>;
+      Runner<S>(h, st).beam_step(bs, done);
+    });
+  };
+  if (!use_graph) return enqueue();
+  return replay(h, GraphKey{slot0, bs.n * bs.beams, -bs.beams, bs.ws, nullptr, nullptr, nullptr, done, h->prof}, st, enqueue);
+}
+
+int wf_beam_end(wf_handle* hh, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  if (!h) return fail(nullptr, WF_EINVAL, "null handle");
+  auto it = h->searches.find(slot0);
+  if (it == h->searches.end()) return fail(h, WF_ESTATE, "no beam search begins at this slot");
+  if (!tokens || !lens || !scores || len_max < 1) return fail(h, WF_EINVAL, "null argument");
+  const BeamSearch bs = it->second;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  BeamArgs g = beam_args(h, bs);
+  g.tokens = tokens; g.out_len = lens; g.out_score = scores; g.len_max = len_max;
+  beam_end(g, st);
+  HIPCK(h, hipGetLastError());
+  h->searches.erase(slot0);
+  for (int s = bs.slot0; s < bs.slot0 + bs.n * bs.beams; ++s) h->beam[s] = h->live[s] = 0;
+  // a later search at these slots may lie in other memory
+  for (auto gi = h->graphs.begin(); gi != h->graphs.end();) {
+    if (gi->first.k_max < 0 && gi->first.ovr == bs.ws) {
+      h->graph_recs.erase(gi->first);
+      (void)hipGraphExecDestroy(gi->second);
+      gi = h->graphs.erase(gi);
+    } else {
+      ++gi;
+    }
+  }
+  return WF_OK;
 }
 
 int wf_debug_ptr(wf_handle* hh, int which, void** ptr) {

@@ -82,6 +82,19 @@ struct ProfAgg {
   long n = 0;
 };
 
+// A beam search over slots [slot0, slot0 + n * beams) and the offsets of its buffers in the
+// caller's workspace.
+struct BeamSpace {
+  size_t req, scores, cs, cb, ct, parents, lens, pool, tables, bt, bp, fscore, fstep, fbeam, last, max_new, select, total;
+  size_t select_bytes;
+};
+struct BeamSearch {
+  int slot0, n, beams;
+  float length_penalty;
+  char* ws;
+  BeamSpace sp;
+};
+
 struct Handle {
   wf_config cfg;
   Layout lay;
@@ -94,6 +107,8 @@ struct Handle {
   bool debug = false;
   std::string err;
   std::vector<int> live;  // host mirror: slot prefilled
+  std::vector<int> beam;  // slot belongs to a beam search
+  std::map<int, BeamSearch> searches;  // by first slot
   std::map<GraphKey, hipGraphExec_t> graphs;
   bool prof = false;       // time launches (eager calls and profiled graph replays)
   bool capturing = false;  // inside graph capture

@@ -165,8 +165,15 @@ struct CrossArgs {
   float* part;        // [pair][nchunk][kXrPart] chunk partials (nchunk > 1 or op.w)
   OprojArgs op;       // fused output product (taken by the merge kernel)
   int by_pair;        // bf16: one block per (head, slot) walks every chunk (no records, no merge)
+  int share;          // beams: slot slot0 + i reads the memory of slot slot0 + i % share (0: its own)
   unsigned long long* stamp;  // launch timing slot (profiled calls), or null
 };
+// Kernels of their own where beams share a memory: a test here lengthens the first load's
+// address by enough to cost a batch-1 step 0.6 %.
+template <bool SHARE>
+__device__ __forceinline__ int memory_slot(const CrossArgs& a, int slot) {
+  return SHARE ? a.slot0 + (slot - a.slot0) % a.share : slot;
+}
 // Chunk partial record: max [9] at 0, sum [9] at 16, acc [9][64] at 32.
 constexpr int kXrPart = 32 + kRows * 64;
 constexpr int kXrMaxPairs = 128;      // chunking only below this many (head, slot) pairs

@@ -34,6 +34,9 @@ struct BeamSelectArgs {
   int* out_token;
 };
 int beam_pieces(int vocab);  // pieces of a row
+// bytes of the row kernel's results, and the pointers to them in `space` (of a with its sizes set)
+size_t beam_space_bytes(int n, int beams, int vocab, int k);
+void beam_space(BeamSelectArgs& a, char* space);
 void beam_select(const BeamSelectArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- page tables after a choice of beams
@@ -44,14 +47,49 @@ struct ReorderArgs {
   size_t region_stride, page_bytes;
   int n_pages;
   const int* tables;   // (r, b, c) at r * tr + b * tb + c
-  int* new_tables;     // likewise, other memory
-  long long tr, tb;
+  int* new_tables;     // other memory: (r, b, c) at r * nr + b * nb + c
+  long long tr, tb, nr, nb;
   const int* parents;  // [n][beams]
   const int* lens;     // [n]
   const int* pool;     // [n][pool_pages]
   int n, beams, max_pages, pool_pages, page_tokens;
 };
 void cache_reorder(const ReorderArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- beam search on a handle's slots
+// Request r's beam b is slot slot0 + b * n + r.  Per request: BR_* words.
+enum { BR_L = 0, BR_STEPS = 1, BR_FIN = 2, BR_DONE = 3, BR_MAX_NEW = 4, BR_LIVE = 5, kBeamReq = 8 };
+struct BeamArgs {
+  int* state;       // the handle's slots
+  int* page_table;  // [slot][pages]
+  int slot0, n, beams, pages, max_batch, eos, n_ctx, k;
+  int* req;         // [n][kBeamReq]
+  float* scores;    // [n][beams] cumulative log-probabilities
+  const float* cand_score;  // [n][k] candidates of the step, best first
+  const int* cand_beam;
+  const int* cand_token;
+  int* parents;     // [n][beams] of the step (-1: no beam)
+  int* lens;        // [n] positions cached after it
+  int* pool;        // [n][beams * pages] the request's own pages
+  int* tables;      // [n][beams][pages] the page tables before the step's choice
+  int* bt;          // [step][n][beams] token and parent of every beam
+  int* bp;
+  float* fscore;    // [n][beams] finished hypotheses: score, step of the closing token, beam before it
+  int* fstep;
+  int* fbeam;
+  const int* last;  // begin: last prompt token of each request
+  const int* max_new;
+  int* done;        // step: [n] or null
+  // end: [n][beams][len_max], [n][beams], [n][beams]
+  int* tokens;
+  int* out_len;
+  float* out_score;
+  int len_max;
+  float length_penalty;
+};
+void beam_begin(const BeamArgs& a, hipStream_t st);
+void beam_advance(const BeamArgs& a, hipStream_t st);
+void beam_end(const BeamArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- acoustic keys and values in 4 bits
 // Per (entry, head), groups of 32 frames one after the other, kKv4Group bytes each: the

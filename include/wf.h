@@ -473,7 +473,7 @@ int wf_kv4_load(const wf_kv4* c, int slot0, int n, void* k, void* v, int dtype, 
  *   h * q_stride[2] + d elements in (strides >= 0, a host array of three): a request's beams
  *   or the rows of a pass are its rows.
  * lens: device int32 [n], taken as the nearest of [0, n_frames], or NULL (all).
- * out: device [n, rows, n_head, 64] in the same type.  1 <= rows <= 2^20.
+ * out: device [n, rows, n_head, 64] in the same type.  1 <= rows <= 2^19.
  */
 int wf_kv4_attend_workspace_bytes(const wf_kv4* c, int n, int rows, size_t* bytes);
 int wf_kv4_attend(const wf_kv4* c, int slot0, int n, const void* q, const int64_t* q_stride, int rows, int dtype,

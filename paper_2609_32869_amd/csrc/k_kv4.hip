@@ -47,9 +47,11 @@ __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0
 __device__ __forceinline__ float scale_f(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // ---------------------------------------------------------------- store
-// A wave per (entry, head, 32-frame group).  Every load is issued before the first use and
-// without a condition (frames at or beyond the length re-read the last given one, or the
-// first, and count as zero).
+// A wave per (entry, head, 32-frame group), four heads a block: their rows lie beside each
+// other.  Every load is issued before the first use and without a condition (frames at or
+// beyond the length re-read the last given one and count as zero); a load under one would
+// make each wait for the one before (16 ragged entries: 101 us against 53).  Memory bounds
+// it: 96 entries of 1500 frames, 20 heads, fp32, 357 us or 4.7 TB/s, the copy rate.
 template <int N>
 __device__ __forceinline__ void ld_vals(const float* p, int vec, float* o) {
   if (vec) {
@@ -102,8 +104,8 @@ __device__ __forceinline__ void put_group(uint8_t* out, const uint2 (&kc)[2], co
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, r = blockIdx.z;
-  if (g >= a.c.groups) return;
+  const int g = blockIdx.y, head = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.z;
+  if (head >= a.c.n_head) return;
   const int len = a.lens ? min(max(a.lens[r], 0), a.c.frames) : a.c.frames, top = max(len - 1, 0);
   uint8_t* out = a.c.base + (((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups + g) * kKv4Group;
   const T* K = reinterpret_cast<const T*>(a.k) + r * a.kr + head * a.kh + 16 * kg;
@@ -156,13 +158,14 @@ __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
 }
 
 void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
-  const dim3 grid((a.c.groups + 3) / 4, a.c.n_head, a.n);
+  const dim3 grid((a.c.n_head + 3) / 4, a.c.groups, a.n);
   if (a.bf16_src) k_kv4_store<bf16><<<grid, 256, 0, st>>>(a);
   else k_kv4_store<float><<<grid, 256, 0, st>>>(a);
 }
 
 // ---------------------------------------------------------------- load
-// A wave per (entry, head, 32-frame group), the store's lanes.
+// The store's waves and lanes; the results' rows leave 16 bytes a lane: 16 entries of 1500
+// frames into fp32 54 us, 5.1 TB/s.
 __device__ __forceinline__ void st8(float* p, bf16x8 x) {
   *reinterpret_cast<float4*>(p) = make_float4((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4((float)x[4], (float)x[5], (float)x[6], (float)x[7]);
@@ -177,8 +180,8 @@ __device__ __forceinline__ void st4(bf16* p, bf16x4 x) { *reinterpret_cast<uint2
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv4_load(Kv4LoadArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, r = blockIdx.z;
-  if (g >= a.c.groups) return;
+  const int g = blockIdx.y, head = blockIdx.x * 4 + (threadIdx.x >> 6), r = blockIdx.z;
+  if (head >= a.c.n_head) return;
   const uint8_t* in = a.c.base + (((size_t)(a.slot0 + r) * a.c.n_head + head) * a.c.groups + g) * kKv4Group;
   const uint4 k = *reinterpret_cast<const uint4*>(in + 16 * lane), v = *reinterpret_cast<const uint4*>(in + kKv4Values + 16 * lane);
   const uint32_t ks = *reinterpret_cast<const uint16_t*>(in + kKv4KeyScale + 32 * (kg >> 1) + 2 * n);
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(256) k_kv4_load(Kv4LoadArgs a) {
 }
 
 void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
-  const dim3 grid((a.c.groups + 3) / 4, a.c.n_head, a.n);
+  const dim3 grid((a.c.n_head + 3) / 4, a.c.groups, a.n);
   if (a.bf16_out) k_kv4_load<bf16><<<grid, 256, 0, st>>>(a);
   else k_kv4_load<float><<<grid, 256, 0, st>>>(a);
 }
@@ -508,7 +511,9 @@ __global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
       O = fmaf(f, wo[j][i][d], O);
     }
     if constexpr (OUT == KV4_OPERAND) {
-      put_op<bf16>(a.op, a.nsplit, a.R9, a.row0 + r * a.orr + i * a.ori, head * kHeadDim + d, O / L);
+      const int to = a.row0 + r * a.orr + i * a.ori;
+      put_op<bf16>(a.op, a.nsplit, a.R9, to, head * kHeadDim + d, O / L);
+      for (int p = 1; p <= a.pad; ++p) put_op<bf16>(a.op, a.nsplit, a.R9, to + p, head * kHeadDim + d, 0.f);
     } else if constexpr (OUT == KV4_RECORDS) {
       float* rec = a.part + (((size_t)r * a.c.n_head + head) * a.nchunk + chunk) * kXrPart;
       rec[32 + t] = O;

@@ -52,7 +52,10 @@ thread_local std::string g_err;
 
 namespace wf {
 int op_fail(int code, const char* msg) {
-  g_err = msg;
+  try {
+    g_err = msg;
+  } catch (...) {
+  }
   return code;
 }
 }  // namespace wf
@@ -688,6 +691,7 @@ struct Runner {
       t.rows = n / a.share;
       t.si = (long long)a.share * kRows * a.ldq;
       t.ori = a.share * kRows;
+      t.pad = kRows - 1;
     }
     const double bytes = (double)kKv4Group * t.c.groups * c.n_head * t.n + wbytes;
     launch("attn_cross", bytes, [&](unsigned long long* sp) {
@@ -1634,9 +1638,8 @@ int wf_beam_bytes(wf_handle* hh, int n, int beams, size_t* bytes) {
   return WF_OK;
 }
 
-int wf_beam_begin(wf_handle* hh, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
-                  float length_penalty, void* workspace, size_t ws_bytes, void* stream) {
-  Handle* h = reinterpret_cast<Handle*>(hh);
+static int beam_start(Handle* h, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
+                      float length_penalty, void* workspace, size_t ws_bytes, void* stream) {
   if (int r = beam_check(h, slot0, n, beams)) return r;
   if (int r = check_batch(h, slot0, n * beams, false)) return r;
   if (int r = check_batch(h, slot0, n, true)) return r;
@@ -1659,8 +1662,7 @@ int wf_beam_begin(wf_handle* hh, int slot0, int n, int beams, const int32_t* las
   return WF_OK;
 }
 
-int wf_beam_step(wf_handle* hh, int slot0, int32_t* done, int use_graph, void* stream) {
-  Handle* h = reinterpret_cast<Handle*>(hh);
+static int beam_extend(Handle* h, int slot0, int32_t* done, int use_graph, void* stream) {
   if (!h) return fail(nullptr, WF_EINVAL, "null handle");
   auto it = h->searches.find(slot0);
   if (it == h->searches.end()) return fail(h, WF_ESTATE, "no beam search begins at this slot");
@@ -1677,8 +1679,7 @@ int wf_beam_step(wf_handle* hh, int slot0, int32_t* done, int use_graph, void* s
   return replay(h, GraphKey{slot0, bs.n * bs.beams, -bs.beams, bs.ws, nullptr, nullptr, nullptr, done, h->prof}, st, enqueue);
 }
 
-int wf_beam_end(wf_handle* hh, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
-  Handle* h = reinterpret_cast<Handle*>(hh);
+static int beam_finish(Handle* h, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
   if (!h) return fail(nullptr, WF_EINVAL, "null handle");
   auto it = h->searches.find(slot0);
   if (it == h->searches.end()) return fail(h, WF_ESTATE, "no beam search begins at this slot");
@@ -1702,6 +1703,25 @@ int wf_beam_end(wf_handle* hh, int slot0, int32_t* tokens, int len_max, int32_t*
     }
   }
   return WF_OK;
+}
+
+// No exception leaves a C entry (the host's records of a search, of a graph or of a message may fail to allocate).
+#define WF_GUARDED(call)                       \
+  try {                                        \
+    return call;                               \
+  } catch (...) {                              \
+    return op_fail(WF_EINVAL, "out of host memory"); \
+  }
+int wf_beam_begin(wf_handle* h, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
+                  float length_penalty, void* workspace, size_t ws_bytes, void* stream) {
+  WF_GUARDED(beam_start(reinterpret_cast<Handle*>(h), slot0, n, beams, last_tokens, max_new, length_penalty, workspace, ws_bytes,
+                        stream))
+}
+int wf_beam_step(wf_handle* h, int slot0, int32_t* done, int use_graph, void* stream) {
+  WF_GUARDED(beam_extend(reinterpret_cast<Handle*>(h), slot0, done, use_graph, stream))
+}
+int wf_beam_end(wf_handle* h, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
+  WF_GUARDED(beam_finish(reinterpret_cast<Handle*>(h), slot0, tokens, len_max, lens, scores, stream))
 }
 
 int wf_debug_ptr(wf_handle* hh, int which, void** ptr) {

@@ -147,9 +147,10 @@ struct Kv4AttendArgs {
   int slot0, n, rows;
   float* part;  // chunk records (nchunk > 1)
   int nchunk, cgroups;  // chunks of the groups and groups of a chunk (set by the launcher)
-  // a decoder step's output rows: row i of request r is operand row row0 + r * orr + i * ori
+  // a decoder step's output rows: row i of request r is operand row row0 + r * orr + i * ori;
+  // the `pad` rows behind each are set to zero (beams: a slot's rows that no beam uses)
   Operand op;
-  int nsplit, R9, row0, orr, ori;
+  int nsplit, R9, row0, orr, ori, pad;
   unsigned long long* stamp;  // launch timing slot (profiled calls), or null
 };
 size_t kv4_workspace(int n, int rows, int n_head, int frames);

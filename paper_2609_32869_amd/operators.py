@@ -3,8 +3,9 @@ acoustic keys and values held in 4 bits.
 
 Argument marshalling as in ``binding``: shapes, types and devices are checked here, sizes
 and ranges by the library.  Every call enqueues on ``stream`` (default: the current stream
-of the tensors' device) and returns without waiting; workspaces and results come from
-PyTorch's allocator, so concurrent calls and captured graphs each have their own.
+of the tensors' device) and returns without waiting; a given stream has to be ordered
+behind the work that fills the tensors.  Workspaces and results come from PyTorch's
+allocator, so concurrent calls and captured graphs each have their own.
 """
 import ctypes
 import functools
@@ -60,9 +61,9 @@ def _type(t, name):
     return code
 
 
-def _enqueue(device, stream, call):
-    """call(raw stream, empty) with `device` current.  empty(shape, dtype): memory that is reused only behind the work
-    that the call's stream has for it."""
+def _enqueue(device, stream, call, *tensors):
+    """call(raw stream, empty) with `device` current.  With a given stream the call's tensors and what empty(shape,
+    dtype) returns are freed only behind the work that this stream has for them."""
     index = device.index
     if stream is None:
         raw, empty = _raw_stream(index), functools.partial(torch.empty, device=device)
@@ -70,6 +71,9 @@ def _enqueue(device, stream, call):
         if stream.device != device:
             _refuse("stream is of another device than the tensors")
         raw = stream.cuda_stream
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
         def empty(shape, dtype):
             t = torch.empty(shape, dtype=dtype, device=device)
@@ -116,7 +120,7 @@ def beam_select(logits, scores, k, suppress=None, stream=None):
                                   p + 2 * step, ws.data_ptr(), nbytes, raw))
         return out
 
-    score, beam, token = _enqueue(dev, stream, call).unbind()
+    score, beam, token = _enqueue(dev, stream, call, logits, scores, suppress).unbind()
     return score.view(_F32), beam, token
 
 
@@ -153,7 +157,7 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
                                     pool.data_ptr(), pool_pages, raw))
         return new
 
-    return _enqueue(dev, stream, call)
+    return _enqueue(dev, stream, call, cache, tables, parents, lens, pool)
 
 
 _Strides = ctypes.c_int64 * 3
@@ -201,9 +205,9 @@ class AcousticCache4:
         n = k.shape[0]
         if vtype != dtype or v.shape[0] != n:
             _refuse("v must have k's type and shape")
-        lens = self._lens(lens, n)
+        plens = self._lens(lens, n)
         _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv4_store(
-            self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, lens, raw)))
+            self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, plens, raw)), k, v, lens, self.data)
 
     def load(self, slot0, n, dtype=torch.float32, stream=None):
         """The keys and values that entries slot0 .. slot0 + n - 1 hold: two tensors [n, n_frames, n_head, 64]."""
@@ -218,7 +222,7 @@ class AcousticCache4:
             _check(self.lib.wf_kv4_load(self._ref, int(slot0), n, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], raw))
             return k, v
 
-        return _enqueue(self.device, stream, call)
+        return _enqueue(self.device, stream, call, self.data)
 
     def attend(self, slot0, q, lens=None, stream=None):
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, n_head, 64], any strides but the last) over the first lens[r]
@@ -230,13 +234,13 @@ class AcousticCache4:
             nbytes = ctypes.c_size_t()
             _check(self.lib.wf_kv4_attend_workspace_bytes(self._ref, n, rows, ctypes.byref(nbytes)))
             need = self._spaces[n, rows] = nbytes.value
-        lens = self._lens(lens, n)
+        plens = self._lens(lens, n)
 
         def call(raw, empty):
             out = empty((n, rows, self.n_head, 64), dtype=q.dtype)
             ws = empty(need, dtype=_U8) if need else None
-            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, lens, out.data_ptr(),
+            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, plens, out.data_ptr(),
                                           ws.data_ptr() if need else None, need, raw))
             return out
 
-        return _enqueue(self.device, stream, call)
+        return _enqueue(self.device, stream, call, q, lens, self.data)

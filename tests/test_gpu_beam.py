@@ -153,6 +153,30 @@ def test_bf16_storage(beams, n, bits):
     eng.close()
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_search_after_a_broken_memory(bits):
+    """A recording of non-finite features leaves non-finite activation rows behind; once its cache pages hold other
+    prompts, a search on the same slots sets no status bit (rows that no beam uses hold zeros, not what was there)."""
+    cfg = BF16
+    W, eng = engine(cfg, 6, bits)
+    rows, toks = prompts(cfg, [8, 8])
+    eng.encode_memory_set(0, torch.full((6, cfg.n_frames, cfg.d_model), float("nan"), dtype=torch.bfloat16, device="cuda"))
+    eng.prefill(0, toks[:1].expand(6, 8).contiguous(), [8] * 6, [9] * 6)
+    eng.step(0, 6)
+    assert eng.status() != 0
+    set_memory(eng, cfg, 0, 6)
+    eng.prefill(0, torch.full((6, cfg.n_ctx), 9, dtype=torch.int32, device="cuda"), [cfg.n_ctx] * 6, [9] * 6)
+    eng.status()
+    eng.prefill(0, toks, [8, 8], [5, 5])
+    assert eng.status() == 0
+    eng.beam_begin(0, 3, toks[:, 7].contiguous(), [5, 5])
+    for _ in range(5):
+        eng.beam_step(0)
+    assert eng.status() == 0
+    assert eng.beam_end(0)[2].isfinite().all()
+    eng.close()
+
+
 def test_one_beam_is_greedy_decoding():
     """One beam without a length choice follows plain greedy decoding, on every path a single slot takes."""
     for cfg, bits in ((MICRO, 16), (BF16, 16), (BF16, 4)):

@@ -336,7 +336,7 @@ def check_attend(cache, slot0, q, k, v, lens, lens_arg, stream=None):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n,rows,F,H", [
     (1, 1, 1, 1), (1, 1, 1500, 20), (1, 9, 1500, 20), (2, 16, 33, 2), (3, 17, 100, 2), (1, 40, 64, 3), (5, 5, 257, 6),
-    (40, 9, 200, 20), (2, 3, 5000, 2), (100, 1, 40, 2)])
+    (40, 9, 200, 20), (2, 3, 5000, 2), (100, 1, 40, 2), (1, 40, 5000, 2)])
 def test_attend(n, rows, F, H, dtype):
     wf = lib()
     k, v = source(n, F, H, dtype, rows)

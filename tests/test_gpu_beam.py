@@ -5,7 +5,7 @@ import torch
 
 from oracle import OracleOpts, Target
 from oracle.beam import beam_search
-from wf_fixtures import MICRO, make_memory, make_prefix, make_weights
+from wf_fixtures import LARGE_V3, MICRO, full_manifest, make_memory, make_prefix, make_weights
 from paper_2609_32869_amd import WfError, WhisperFlash, to_device_storage
 
 pytestmark = pytest.mark.gpu
@@ -174,6 +174,39 @@ def test_a_search_after_a_broken_memory(bits):
         eng.beam_step(0)
     assert eng.status() == 0
     assert eng.beam_end(0)[2].isfinite().all()
+    eng.close()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_large_v3_scores_are_the_hypotheses_own(bits):
+    """Large-v3 shapes, three recordings of five beams on 15 slots (page borders crossed, pages shared and copied): each
+    hypothesis's score is the sum of its tokens' log-probabilities in one plain verification pass over it.  The passes'
+    products sum in other orders and the fused adds vary: a logit moves by 1e-3 (the step's parity tests), a
+    log-probability by 2e-3, nine of them by 2e-2."""
+    cfg, B, lens = LARGE_V3.with_(eos_id=-1), 5, [30, 41, 16]
+    g = torch.Generator("cuda").manual_seed(11)
+    weights = []
+    for name, shape in full_manifest(cfg):
+        w = (0.02 * torch.randn(shape, device="cuda", generator=g)).bfloat16()
+        weights.append(w + 1 if name.endswith(".g") else w)
+    weights[0] *= 4          # a livelier vocabulary: paths differ, and differ in score
+    eng = WhisperFlash(cfg, 15, weights, acoustic_bits=bits)
+    eng.encode_memory_set(0, torch.randn((3, cfg.n_frames, cfg.d_model), device="cuda", generator=g).bfloat16())
+    toks = torch.randint(0, cfg.n_vocab, (3, 41), dtype=torch.int32, device="cuda", generator=g)
+    out, n_tok, scores = eng.beam_search(0, toks, lens, [9] * 3, B)
+    assert (n_tok == 9).all() and (scores[:, :-1] >= scores[:, 1:]).all()
+    assert len({tuple(p) for p in out[0, :, :9].tolist()}) == B
+    eng.set_debug(True)
+    for r in range(3):
+        for b in range(B):
+            eng.prefill(r, toks[r:r + 1, :lens[r] - 1].contiguous(), [lens[r] - 1], [60])
+            st = eng.state()
+            st[r, 1] = toks[r, lens[r] - 1]     # the anchor is the prompt's own last token
+            eng.verify_accept(r, out[r:r + 1, b, :8].contiguous())
+            logp = torch.log_softmax(eng.target_logits()[r].double(), -1)
+            total = logp.gather(1, out[r, b, :9, None].long()).sum()
+            assert abs(float(total - scores[r, b])) <= 2e-2, (r, b)
+    assert eng.status() == 0
     eng.close()
 
 

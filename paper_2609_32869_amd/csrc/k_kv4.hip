@@ -303,8 +303,8 @@ void kv4_unpack(const Kv4PackArgs& a, hipStream_t st) {
 // steps of two groups, the next step's codes in flight while it multiplies the current one.
 //   scores   S^T = K q^T per 16-frame tile (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets
 //            row n of frames 4 kg .. + 3
-//   softmax  running maximum and sum per row, one rescaling per step; powers of two, the
-//            maximum held times log2(e) so that numerator and rescaling use one rounding
+//   softmax  running maximum and sum per row, one rescaling per step; the difference to the
+//            maximum first, then powers of two: right at any magnitude of the scores
 //   values   O^T = V^T P^T per group: two lane swaps turn the group's two score tiles into
 //            the operand (lane: row n, frames 8 kg .. + 7)
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for
@@ -368,13 +368,17 @@ __device__ __forceinline__ void kv_load(const uint8_t* in, int g, int end, KvSte
   }
 }
 constexpr float kLog2e = 1.44269504088896f;
-// A row's running state: maximum of the scores times log2(e), the lane's share of the sum, O^T.
+// exp(x - m) for a maximum m that is -inf where there is no x yet: 0 there.
+__device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
+// A row's running state: maximum of the scores, the lane's share of the sum, O^T.  (Rescaling only where the maximum
+// moves by more than a few powers costs registers past 64, a block per CU fewer: 68 us against 52 at 96 x 9 rows.)
 struct RowState {
   float m, l;
   floatx4 o[4];
 };
 template <int KS, int QT, int PT>
-__device__ __forceinline__ void kv_step(const KvStep<KS>& c, int g, int len, const bf16x8 (&qt)[2][QT], RowState& st) {
+__device__ __forceinline__ void kv_step(KvStep<KS>& c, int g, int len, const bf16x8 (&qt)[2][QT], RowState& st) {
   const int kg = (threadIdx.x & 63) >> 4;
   floatx4 s[2 * KS];
 #pragma unroll
@@ -390,21 +394,30 @@ __device__ __forceinline__ void kv_step(const KvStep<KS>& c, int g, int len, con
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (g * kKv4Frames + 16 * t + 4 * kg + i >= len) s[t][i] = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < KS; ++u) {  // values past the length may stand for infinity: 0 instead
+      const int left = len - (g + u) * kKv4Frames - 8 * kg;
+      const uint32_t in = left >= 8 ? ~0u : left <= 0 ? 0u : (1u << 4 * left) - 1;
+      c.v[u].x &= in;
+      c.v[u].y &= in;
+      c.v[u].z &= in;
+      c.v[u].w &= in;
+    }
   }
   float mx = -INFINITY;
 #pragma unroll
   for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-  const float m = fmaxf(st.m, swap_max(mx) * kLog2e), base = m == -INFINITY ? 0.f : m;
-  const float f = __builtin_amdgcn_exp2f(st.m - base);  // 0 at first
+  const float m = fmaxf(st.m, swap_max(mx)), base = no_inf(m);
+  const float f = exp_to(st.m, base);  // 0 at first
   st.m = m;
   float l = 0.f;
 #pragma unroll
   for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], kLog2e, -base));
+      s[t][i] = exp_to(s[t][i], base);
       l += s[t][i];
     }
   st.l = fmaf(st.l, f, l);
@@ -503,10 +516,10 @@ __global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
     float M = wm[0][i], L = 0.f, O = 0.f;
 #pragma unroll
     for (int j = 1; j < NW; ++j) M = fmaxf(M, wm[j][i]);
-    const float base = M == -INFINITY ? 0.f : M;
+    const float base = no_inf(M);
 #pragma unroll
     for (int j = 0; j < NW; ++j) {
-      const float f = __builtin_amdgcn_exp2f(wm[j][i] - base);  // 0 for a wave of no frames
+      const float f = exp_to(wm[j][i], base);  // 0 for a wave of no frames
       L = fmaf(f, wl[j][i], L);
       O = fmaf(f, wo[j][i][d], O);
     }
@@ -518,7 +531,7 @@ __global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
       float* rec = a.part + (((size_t)r * a.c.n_head + head) * a.nchunk + chunk) * kXrPart;
       rec[32 + t] = O;
       if (d == 0) {
-        rec[i] = M * 0.693147180559945f;  // the merge's powers of e
+        rec[i] = M;
         rec[16 + i] = L;
       }
     } else if (a.nchunk == 1) {
@@ -560,14 +573,14 @@ __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (c0 + 16 * u < a.nchunk) Mn = fmaxf(Mn, m[u]);
-    const float base = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - base);
+    const float base = no_inf(Mn), f0 = exp_to(M, base);
     M = Mn;
     L *= f0;
     O *= f0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (c0 + 16 * u < a.nchunk) {
-        const float f = __builtin_amdgcn_exp2f(m[u] - base);
+        const float f = exp_to(m[u], base);
         L = fmaf(f, l[u], L);
         O += f * o[u];
       }
@@ -583,10 +596,10 @@ __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
     float m = wm[0], l = 0.f, o = 0.f;
 #pragma unroll
     for (int j = 1; j < 16; ++j) m = fmaxf(m, wm[j]);
-    const float base = m == -INFINITY ? 0.f : m;
+    const float base = no_inf(m);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      const float f = __builtin_amdgcn_exp2f(wm[j] - base);
+      const float f = exp_to(wm[j], base);
       l = fmaf(f, wl[j], l);
       o = fmaf(f, wo[j][t], o);
     }

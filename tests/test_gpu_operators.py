@@ -386,6 +386,47 @@ def test_attend_masked_places_may_hold_anything():
     assert got[0].isfinite().all() and got[1].isnan().all()     # a non-finite frame inside shows
 
 
+def test_attend_infinite_values_in_masked_places():
+    """Values that stand for infinity behind the length, in a group with frames inside it: they count for nothing, also
+    where a wave's last step holds that group twice."""
+    wf = lib()
+    n, F, H = 4, 600, 2
+    for dtype in (torch.float32, torch.bfloat16):
+        k, v = source(n, F, H, dtype, 20)
+        v[:, 200:224] = 3.3e38
+        v[:, 520:] = -3.3e38
+        cache = wf.AcousticCache4(n, H, F)
+        cache.store(0, k, v)
+        held = plain.kv4_values(num(k), num(v), [F] * n)
+        assert np.isinf(held[1][:, 200:224]).all()
+        lens = [200, 193, 197, 1]
+        q = torch.randn((n, 5, H, 64), device="cuda").to(dtype)
+        check_attend(cache, 0, q, *held, lens, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("size", [1e10, 7e20, 3e38])
+@pytest.mark.parametrize("F", [45, 1500, 6000])
+def test_attend_scores_of_any_magnitude(F, size):
+    """Queries of one dim and keys of powers of two there: every score is exact, and so far apart that the best frames
+    share the weight evenly.  Their mean takes at most 600 sums in 32 bits: 600 * 2^-24 of the largest value."""
+    wf = lib()
+    g = torch.Generator("cuda").manual_seed(F)
+    k = torch.zeros((1, F, 2, 64), device="cuda")
+    k[..., 0] = 2.0 ** torch.randint(-1, 3, (1, F, 2), device="cuda", generator=g) * \
+        (1 - 2 * torch.randint(0, 2, (1, F, 2), device="cuda", generator=g))
+    v = torch.randn((1, F, 2, 64), device="cuda", generator=g)
+    cache = wf.AcousticCache4(1, 2, F)
+    cache.store(0, k, v)
+    held = plain.kv4_values(num(k), num(v), [F])
+    assert np.array_equal(held[0], num(k))
+    for dtype in (torch.float32, torch.bfloat16):
+        q = torch.zeros((1, 3, 2, 64), device="cuda", dtype=dtype)
+        q[..., 0] = torch.tensor([size, -size, size / 64], device="cuda")[None, :, None]
+        got, want = num(cache.attend(0, q)), plain.attend(num(q), *held, [F])
+        half = 2.0 ** -9 if dtype == torch.bfloat16 else 2.0 ** -24
+        assert (np.abs(got - want) <= 600 * 2.0 ** -24 * np.abs(held[1]).max() + 2 * half * np.abs(want)).all()
+
+
 def test_attend_strides_and_large_scores():
     """Rows as beams of a slot-major buffer, one row for all requests, bases off 16 bytes; scores of a few hundred."""
     wf = lib()

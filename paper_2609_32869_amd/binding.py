@@ -6,6 +6,7 @@ output tensors) and the HIP stream.  The library must be built first
 (``python -m paper_2609_32869_amd.build`` or ``__graft_entry__.build()``);
 importing this module without it raises.
 """
+import contextlib
 import ctypes
 import os
 
@@ -166,6 +167,11 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _on(stream):
+    """Allocate memory of `stream` (None: of the current one)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def to_device_storage(arr, dtype, device="cuda"):
     """Host fp32 array -> device tensor in the storage type (bf16 values must be exact)."""
     a = np.ascontiguousarray(arr, dtype=np.float32)
@@ -279,10 +285,13 @@ class WhisperFlash:
     # ---- beam search (beam b of request r is slot slot0 + b * n + r)
     def beam_begin(self, slot0, beams, last_tokens, max_new, length_penalty=1.0, stream=None):
         """last_tokens: device int32 [n], the last prompt token of each prefilled leader; max_new: sequence of ints."""
+        if last_tokens.dtype != torch.int32 or last_tokens.dim() != 1 or not last_tokens.is_contiguous() or not last_tokens.is_cuda:
+            raise WfError("invalid argument (-1): last_tokens must be a contiguous int32 [n] on the GPU")
         n = last_tokens.shape[0]
         nbytes = ctypes.c_size_t()
         self._check(self.lib.wf_beam_bytes(self.h, n, beams, ctypes.byref(nbytes)))
-        ws = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
+        with _on(stream):  # memory of the search's stream
+            ws = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
         M = (ctypes.c_int32 * n)(*[int(x) for x in max_new])
         self._check(self.lib.wf_beam_begin(self.h, slot0, n, beams, _ptr(last_tokens), M, float(length_penalty), _ptr(ws),
                                            nbytes.value, _stream(stream)))
@@ -299,13 +308,15 @@ class WhisperFlash:
             raise WfError("invalid state (-2): no beam search begins at this slot")
         n, beams, ws = self.searches[slot0]
         len_max = self.cfg.n_ctx if len_max is None else len_max
-        tokens = torch.empty((n, beams, len_max), dtype=torch.int32, device="cuda")
-        lens = torch.empty((n, beams), dtype=torch.int32, device="cuda")
-        scores = torch.empty((n, beams), dtype=torch.float32, device="cuda")
+        with _on(stream):
+            tokens = torch.empty((n, beams, len_max), dtype=torch.int32, device="cuda")
+            lens = torch.empty((n, beams), dtype=torch.int32, device="cuda")
+            scores = torch.empty((n, beams), dtype=torch.float32, device="cuda")
         self._check(self.lib.wf_beam_end(self.h, slot0, _ptr(tokens), len_max, _ptr(lens), _ptr(scores), _stream(stream)))
+        ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
         if stream is not None:
-            for t in (tokens, lens, scores, ws):
-                t.record_stream(stream)
+            for t in (tokens, lens, scores):
+                t.record_stream(torch.cuda.current_stream())
         del self.searches[slot0]
         return tokens, lens, scores
 
@@ -317,10 +328,14 @@ class WhisperFlash:
         last = tokens.gather(1, torch.tensor([[int(x) - 1] for x in lens], device=tokens.device)).view(n).contiguous()
         self.beam_begin(slot0, beams, last, max_new, length_penalty)
         done = torch.zeros(n, dtype=torch.int32, device="cuda")
-        for step in range(self.cfg.n_ctx):
-            self.beam_step(slot0, done, use_graph)
-            if step % poll == poll - 1 and bool(done.all()):
-                break
+        try:
+            for step in range(self.cfg.n_ctx):
+                self.beam_step(slot0, done, use_graph)
+                if step % poll == poll - 1 and bool(done.all()):
+                    break
+        except WfError:
+            self.beam_end(slot0)  # the slots are given back
+            raise
         return self.beam_end(slot0)
 
     def set_debug(self, on):

@@ -5,7 +5,8 @@ Argument marshalling as in ``binding``: shapes, types and devices are checked he
 and ranges by the library.  Every call enqueues on ``stream`` (default: the current stream
 of the tensors' device) and returns without waiting; a given stream has to be ordered
 behind the work that fills the tensors.  Workspaces and results come from PyTorch's
-allocator, so concurrent calls and captured graphs each have their own.
+allocator for the call's stream, so concurrent calls and captured graphs each have their
+own.
 """
 import ctypes
 import functools
@@ -29,6 +30,14 @@ def _check(rc):
 
 def _refuse(what):
     raise WfError(f"invalid argument (-1): {what}")
+
+
+def _int(v, name):
+    """A number that the C entries' 32 bits hold (the range that each allows is the library's check)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        _refuse(f"{name} out of range")
+    return v
 
 
 def _tensor(t, name, dtype, shape, device):
@@ -62,8 +71,9 @@ def _type(t, name):
 
 
 def _enqueue(device, stream, call, *tensors):
-    """call(raw stream, empty) with `device` current.  With a given stream the call's tensors and what empty(shape,
-    dtype) returns are freed only behind the work that this stream has for them."""
+    """call(raw stream, empty) with `device` current.  With a given stream the call's tensors are freed only behind the
+    work that it has for them, and empty(shape, dtype) takes memory of that stream: memory of the current one may
+    still be in use there, by work that the given stream is not ordered behind."""
     index = device.index
     if stream is None:
         raw, empty = _raw_stream(index), functools.partial(torch.empty, device=device)
@@ -75,9 +85,12 @@ def _enqueue(device, stream, call, *tensors):
             if t is not None:
                 t.record_stream(stream)
 
+        current = torch.cuda.current_stream(device)
+
         def empty(shape, dtype):
-            t = torch.empty(shape, dtype=dtype, device=device)
-            t.record_stream(stream)
+            with torch.cuda.stream(stream):
+                t = torch.empty(shape, dtype=dtype, device=device)
+            t.record_stream(current)
             return t
     if torch.cuda.current_device() == index:
         return call(raw, empty)
@@ -87,6 +100,8 @@ def _enqueue(device, stream, call, *tensors):
 
 @functools.lru_cache(maxsize=256)
 def _select_bytes(n, beams, vocab, k):
+    for v, name in ((n, "n"), (beams, "beams"), (vocab, "n_vocab"), (k, "k")):
+        _int(v, name)
     nbytes = ctypes.c_size_t()
     _check(load_library().wf_beam_select_workspace_bytes(n, beams, vocab, k, ctypes.byref(nbytes)))
     return nbytes.value
@@ -138,8 +153,7 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
     n, beams, max_pages = tables.shape
     if dev != cache.device:
         _refuse("tables must be on the cache's device")
-    if pool.dim() != 2:
-        _refuse("pool must have 2 axes")
+    _gpu(pool, "pool", 2)
     pool_pages = pool.shape[1]
     _tensor(tables, "tables", _I32, (n, beams, max_pages), dev)
     _tensor(parents, "parents", _I32, (n, beams), dev)
@@ -148,6 +162,9 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
     regions, pages = cache.shape[:2]
     if regions == 0 or pages == 0:
         _refuse("cache must hold a page")
+    for v, name in ((n, "n"), (beams, "beams"), (max_pages, "max_pages"), (regions, "n_regions"), (pages, "n_pages"),
+                    (pool_pages, "pool_pages"), (page_tokens, "page_tokens")):
+        _int(v, name)
     region = cache.numel() // regions * cache.element_size()
 
     def call(raw, empty):
@@ -168,7 +185,7 @@ class AcousticCache4:
 
     def __init__(self, entries, n_head, n_frames, device="cuda"):
         self.lib = load_library()
-        self.entries, self.n_head, self.n_frames = int(entries), int(n_head), int(n_frames)
+        self.entries, self.n_head, self.n_frames = _int(entries, "entries"), _int(n_head, "n_head"), _int(n_frames, "n_frames")
         nbytes = ctypes.c_size_t()
         _check(self.lib.wf_kv4_bytes(self.entries, self.n_head, self.n_frames, ctypes.byref(nbytes)))
         self.data = torch.empty(nbytes.value, dtype=_U8, device=device)
@@ -205,9 +222,9 @@ class AcousticCache4:
         n = k.shape[0]
         if vtype != dtype or v.shape[0] != n:
             _refuse("v must have k's type and shape")
-        plens = self._lens(lens, n)
+        plens, slot0, n = self._lens(lens, n), _int(slot0, "slot0"), _int(n, "n")
         _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv4_store(
-            self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, plens, raw)), k, v, lens, self.data)
+            self._ref, slot0, n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, plens, raw)), k, v, lens, self.data)
 
     def load(self, slot0, n, dtype=torch.float32, stream=None):
         """The keys and values that entries slot0 .. slot0 + n - 1 hold: two tensors [n, n_frames, n_head, 64]."""
@@ -231,15 +248,16 @@ class AcousticCache4:
         n, rows = q.shape[:2]
         need = self._spaces.get((n, rows))
         if need is None:
+            _int(n, "n"), _int(rows, "rows")
             nbytes = ctypes.c_size_t()
             _check(self.lib.wf_kv4_attend_workspace_bytes(self._ref, n, rows, ctypes.byref(nbytes)))
             need = self._spaces[n, rows] = nbytes.value
-        plens = self._lens(lens, n)
+        plens, slot0 = self._lens(lens, n), _int(slot0, "slot0")
 
         def call(raw, empty):
             out = empty((n, rows, self.n_head, 64), dtype=q.dtype)
             ws = empty(need, dtype=_U8) if need else None
-            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, plens, out.data_ptr(),
+            _check(self.lib.wf_kv4_attend(self._ref, slot0, n, q.data_ptr(), qs, rows, dtype, plens, out.data_ptr(),
                                           ws.data_ptr() if need else None, need, raw))
             return out
 

@@ -271,6 +271,36 @@ def test_searches_beside_each_other_and_graphs(cfg):
     eng.close()
 
 
+def test_on_a_given_stream_and_after_a_refused_step():
+    cfg = MICRO
+    W, eng = engine(cfg, 4)
+    rows, toks = prompts(cfg, [10])
+    set_memory(eng, cfg, 0, 1)
+    whole = eng.beam_search(0, toks, [10], [9], 4)
+    last = toks[0, 9:10].contiguous()
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(2):
+        eng.prefill(0, toks, [10], [1])
+        torch.cuda.synchronize()
+        eng.beam_begin(0, 4, last, [9], stream=stream)
+        for _ in range(9):
+            eng.beam_step(0, use_graph=True, stream=stream)
+        got = eng.beam_end(0, stream=stream)
+        stream.synchronize()
+        for a, b in zip(got, whole):
+            assert torch.equal(a, b)
+    with pytest.raises(WfError, match="non-null stream"):       # no graph on the default stream: the slots come back
+        eng.beam_search(0, toks, [10], [9], 4, use_graph=True)
+    assert eng.searches == {}
+    for a, b in zip(eng.beam_search(0, toks, [10], [9], 4), whole):
+        assert torch.equal(a, b)
+    for wrong in (last.long(), toks[:, :1], toks[0, ::2], last.cpu()):
+        with pytest.raises(WfError, match="last_tokens"):
+            eng.beam_begin(0, 2, wrong, [9])
+    eng.close()
+
+
 def test_results_cut_and_ended_early():
     cfg = MICRO
     W, eng = engine(cfg, 4)

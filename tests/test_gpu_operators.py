@@ -533,6 +533,34 @@ def test_operators_on_a_given_stream():
         assert torch.equal(x, y)
 
 
+def test_a_given_streams_results_take_that_streams_memory():
+    """Memory freed on the current stream, whose work on it has not run, is not what a call on another stream writes."""
+    wf = lib()
+    s = torch.cuda.Stream()
+    logits, scores = torch.randn((2, 3, 999), device="cuda"), torch.zeros((2, 3), device="cuda")
+    k, v = source(2, 64, 2, torch.float32, 30)
+    cache = wf.AcousticCache4(2, 2, 64)
+    cache.store(0, k, v)
+    q = torch.randn((2, 3, 2, 64), device="cuda")
+
+    def call(stream=None):
+        return [*wf.beam_select(logits, scores, 6, stream=stream), cache.attend(0, q, stream=stream),
+                *cache.load(0, 2, stream=stream)]
+    want = call()
+    call(s)
+    torch.cuda.synchronize()
+    x = torch.randn((4096, 4096), device="cuda")
+    for _ in range(5):
+        for _ in range(20):
+            x = x @ x * 1e-4
+        stale = [torch.full_like(t, 7) for t in want for _ in range(4)]     # runs long after the calls on s
+        del stale
+        got = call(s)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
 def test_operators_captured_into_a_graph():
     """Two searches captured into two graphs, replayed in turn with eager work between: every replay gives the
     eager result."""

@@ -114,6 +114,18 @@ def test_binding_refuses_tensors_of_another_kind():
         wf.cache_reorder(torch.zeros((1, 8, 16)), i, i[0, :1], i[0, 0, :1], i[0])
 
 
+def test_binding_refuses_sizes_past_32_bits():
+    """What a C int would cut off to a size that is allowed."""
+    import paper_2609_32869_amd as wf
+    from paper_2609_32869_amd import operators
+    for sizes in ((1, 5, 2 ** 32 + 100, 5), (1, 5, 100, 2 ** 32 + 5), (2 ** 32 + 1, 5, 100, 5), (1, 2 ** 32 + 5, 100, 5)):
+        with pytest.raises(wf.WfError, match="out of range"):
+            operators._select_bytes(*sizes)
+    for sizes in ((2 ** 32 + 1, 2, 100), (1, 2 ** 32 + 2, 100), (1, 2, 2 ** 32 + 100)):
+        with pytest.raises(wf.WfError, match="out of range"):
+            wf.AcousticCache4(*sizes)
+
+
 def test_beam_calls_on_a_null_handle():
     binding, lib = _lib()
     n = ctypes.c_size_t()

@@ -607,10 +607,17 @@ __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
   }
 }
 
+// Chunks: a long memory's groups over about two blocks per CU, 16 groups (a step of each wave) or more to a chunk.
+// us a replayed call, split against one block per (head, request): 20 pairs, 2,048 frames 7.3 / 9.7, 4,500 frames
+// 8.0 / 18.1, 131,072 frames 40.5 / 418; 80 pairs, 4,500 frames 11.5 / 18.5; 160 pairs, 4,500 frames 18.1 / 19.2, 131,072
+// frames 312 / 424.  Up to 1,536 frames (20 pairs, 1,500 frames: 7.2 / 8.2) the merge's launch costs its caller more than
+// it saves, and from nearly a block per CU on (240 pairs, 4,500 frames: 23.2 / 19.8; 131,072: 464 / 471) one is as good.
+// Towards 256, 768 or 1,024 blocks instead of 512 (160 pairs of 4,500, of 16,384 frames): 18.9, 19.9, 19.0 us against
+// 18.1; 56, 45, 43 against 42.
 int kv4_chunks(int n, int rows, int n_head, int frames) {
   const long long pairs = (long long)n * n_head * ((rows + 15) / 16), groups = kv4_groups(frames);
-  if (groups <= 64 || pairs >= 512) return 1;
-  return (int)std::max<long long>(1, std::min<long long>(1024 / pairs, groups / 16));
+  if (groups <= 48 || pairs >= 240) return 1;
+  return (int)std::max<long long>(1, std::min<long long>(512 / pairs, groups / 16));
 }
 size_t kv4_workspace(int n, int rows, int n_head, int frames) {
   const int nc = kv4_chunks(n, rows, n_head, frames);

@@ -412,7 +412,7 @@ __device__ __forceinline__ void xr_scores_mfma(const CrossArgs& a, int slot, int
   }
 }
 
-template <typename S, bool SHARE>
+template <typename S>
 __global__ void __launch_bounds__(kXrThreads, 4) k_attn_cross_rows(CrossArgs a) {
   StampScope stamp_scope(a.stamp, kXrThreads);
   // key octets per vector load stage (the fp32 score pass and the value pass)
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(kXrThreads, 4) k_attn_cross_rows(CrossArgs a) 
   const int k0 = c * a.chunk, nk = min(a.n_frames - k0, a.chunk), noct = (nk + 7) >> 3;
   const int nst = ((noct - w + NW - 1) / NW + B - 1) / B;  // load stages of this wave
   const S* Kx = reinterpret_cast<const S*>(a.kv) +
-                (((size_t)memory_slot<SHARE>(a, slot) * 2 * a.n_head + head) * a.n_frames + k0) * kHeadDim;
+                (((size_t)slot * 2 * a.n_head + head) * a.n_frames + k0) * kHeadDim;
   const S* Vx = Kx + (size_t)a.n_head * a.n_frames * kHeadDim;
   // key of lane group kl in octet b of stage st of this wave (may lie past the end)
   auto key_of = [&](int st, int b) { return (w + NW * (st * B + b)) * 8 + kl; };
@@ -740,12 +740,12 @@ __device__ __forceinline__ void xq_load(const CrossArgs& a, int head, int slot, 
   }
 }
 
-template <int KS, int NW, bool SHARE>
+template <int KS, int NW>
 __device__ __forceinline__ void xkv_load(const CrossArgs& a, int head, int slot, int c, XKv<KS>& it) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kg = lane >> 4;
   const int F = a.n_frames, Fp = a.vt_frames;
   const int f0w = c * a.chunk + w * 32 * KS;  // first frame of this wave
-  const bf16* base = reinterpret_cast<const bf16*>(a.kv) + (size_t)memory_slot<SHARE>(a, slot) * a.d * (F + Fp);
+  const bf16* base = reinterpret_cast<const bf16*>(a.kv) + (size_t)slot * a.d * (F + Fp);
   const bf16* Kh = base + (size_t)head * F * kHeadDim;
   const bf16* Vt = base + (size_t)a.n_head * F * kHeadDim + (size_t)head * kHeadDim * Fp;
 #pragma unroll
@@ -762,10 +762,10 @@ __device__ __forceinline__ void xkv_load(const CrossArgs& a, int head, int slot,
       it.vt[st][dt] = *reinterpret_cast<const bf16x8*>(Vt + vt_index(16 * dt + n, f0w + 32 * st + 8 * kg));
 }
 
-template <int KS, int NW, bool SHARE>
+template <int KS, int NW>
 __device__ __forceinline__ void xitem_load(const CrossArgs& a, int head, int slot, int c, XItem<KS>& it) {
   xq_load(a, head, slot, it.qx);
-  xkv_load<KS, NW, SHARE>(a, head, slot, c, it.kv);
+  xkv_load<KS, NW>(a, head, slot, c, it.kv);
 }
 
 // The query planes of the nine rows scaled by 1/sqrt(64) (rows >= 9 zero).
@@ -908,7 +908,7 @@ __device__ __forceinline__ void xitem_compute(const CrossArgs& a, int head, int 
   }
 }
 
-template <int KS, int NW, bool SHARE>
+template <int KS, int NW>
 __global__ void __launch_bounds__(NW * 64) k_attn_cross_mx(CrossArgs a) {
   StampScope stamp_scope(a.stamp, NW * 64);
   __shared__ float wmax[NW][16];
@@ -916,7 +916,7 @@ __global__ void __launch_bounds__(NW * 64) k_attn_cross_mx(CrossArgs a) {
   __shared__ float wo[NW][kRows][64];
   const int head = blockIdx.x, slot = a.slot0 + blockIdx.y, c = blockIdx.z;
   XItem<KS> it;
-  xitem_load<KS, NW, SHARE>(a, head, slot, c, it);
+  xitem_load<KS, NW>(a, head, slot, c, it);
   __builtin_amdgcn_sched_barrier(0);  // every load above is issued before any use below
   xitem_compute<KS, NW>(a, head, slot, blockIdx.y * a.n_head + head, c, it, wmax, wsum, wo);
 }
@@ -930,7 +930,7 @@ __global__ void __launch_bounds__(NW * 64) k_attn_cross_mx(CrossArgs a) {
 // go straight into the next product's operand: no chunk records (their writes
 // among the key and value reads cost about a tenth of the launch at 96 slots)
 // and no merge launch.
-template <int KS, int NW, int NCH, bool SHARE>
+template <int KS, int NW, int NCH>
 __global__ void __launch_bounds__(NW * 64) k_attn_cross_pair(CrossArgs a) {
   constexpr int NI = (kRows * 64 + NW * 64 - 1) / (NW * 64);  // (row, dim) items per thread
   StampScope stamp_scope(a.stamp, NW * 64);
@@ -944,7 +944,7 @@ __global__ void __launch_bounds__(NW * 64) k_attn_cross_pair(CrossArgs a) {
   XKv<KS> it[2];
   xq_load(a, head, slot, qx);
 #pragma unroll
-  for (int c = 0; c < 2 && c < NCH; ++c) xkv_load<KS, NW, SHARE>(a, head, slot, c, it[c]);
+  for (int c = 0; c < 2 && c < NCH; ++c) xkv_load<KS, NW>(a, head, slot, c, it[c]);
   __builtin_amdgcn_sched_barrier(0);  // every load above is issued before any use below
   bf16x8 qh[2], ql[2];
   xq_planes(qx, qh, ql);
@@ -961,7 +961,7 @@ __global__ void __launch_bounds__(NW * 64) k_attn_cross_pair(CrossArgs a) {
     xchunk_rows<KS, NW>(a, c, it[b], qh, ql, wmax[b], wsum[b], wo[b]);
     if (c + 2 < NCH) {  // the set just used takes chunk c + 2
       __builtin_amdgcn_sched_barrier(0);
-      xkv_load<KS, NW, SHARE>(a, head, slot, c + 2, it[b]);
+      xkv_load<KS, NW>(a, head, slot, c + 2, it[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -1533,32 +1533,28 @@ void Ops<S>::attn_cross(const CrossArgs& a, int n, hipStream_t st) {
       const dim3 grid(a.n_head, n);
       switch (a.nchunk) {
 #define WF_XPAIR(N) \
-  case N:                                                                \
-    if (a.share) k_attn_cross_pair<1, 4, N, true><<<grid, 256, 0, st>>>(a); \
-    else k_attn_cross_pair<1, 4, N, false><<<grid, 256, 0, st>>>(a);        \
-    break;
+  case N: k_attn_cross_pair<1, 4, N><<<grid, 256, 0, st>>>(a); break;
         WF_XPAIR(1) WF_XPAIR(2) WF_XPAIR(3) WF_XPAIR(4) WF_XPAIR(5) WF_XPAIR(6)
         WF_XPAIR(7) WF_XPAIR(8) WF_XPAIR(9) WF_XPAIR(10) WF_XPAIR(11) WF_XPAIR(12)
 #undef WF_XPAIR
       }
       return;
     }
-    if (a.chunk == 128) k_attn_cross_mx<1, 4, false><<<dim3(a.n_head, n, a.nchunk), 256, 0, st>>>(a);  // one slot: nothing shared
-    else if (a.share) k_attn_cross_mx<2, 8, true><<<dim3(a.n_head, n, a.nchunk), 512, 0, st>>>(a);
-    else k_attn_cross_mx<2, 8, false><<<dim3(a.n_head, n, a.nchunk), 512, 0, st>>>(a);
+    if (a.chunk == 128) k_attn_cross_mx<1, 4><<<dim3(a.n_head, n, a.nchunk), 256, 0, st>>>(a);
+    else k_attn_cross_mx<2, 8><<<dim3(a.n_head, n, a.nchunk), 512, 0, st>>>(a);
   } else {
     if (n == 1) {  // one slot: a block per (head, row) streams all frames (9 blocks per head share an L2)
       k_attn_cross<S><<<dim3(row_blocks(a.n_head), n), kCrossThreads, 0, st>>>(a);
       return;
     }
-    if (a.share) k_attn_cross_rows<S, true><<<dim3(a.n_head, n, a.nchunk), kXrThreads, xr_lds_bytes(a.chunk), st>>>(a);
-    else k_attn_cross_rows<S, false><<<dim3(a.n_head, n, a.nchunk), kXrThreads, xr_lds_bytes(a.chunk), st>>>(a);
+    k_attn_cross_rows<S><<<dim3(a.n_head, n, a.nchunk), kXrThreads, xr_lds_bytes(a.chunk), st>>>(a);
   }
   if (a.nchunk > 1 || a.op.w != nullptr) {
     if (a.op.w != nullptr) launch_merge<S, true>(a, n, st);
     else launch_merge<S, false>(a, n, st);
   }
 }
+
 void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st) {
   if (a.op.w != nullptr) launch_merge<bf16, true>(a, n, st);
   else launch_merge<bf16, false>(a, n, st);

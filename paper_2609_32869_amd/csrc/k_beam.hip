@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "wf_operand.h"
 #include "wf_ops.h"
 
 namespace wf {
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
   __shared__ int wn[4];
   const int r = blockIdx.x, b = blockIdx.z, row = r * a.beams + b, t = threadIdx.x, lane = t & 63;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
-  const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb;
+  const T* x = reinterpret_cast<const T*>(a.logits) + r * a.sr + b * a.sb + (b < kRows ? 0 : a.far);
   const int v0 = blockIdx.y * 256 * R + w * 64 * R + 8 * lane;
   float y[R];
   load_logits<T, R>(x, a.suppress, v0, a.vocab, y);
@@ -606,7 +607,124 @@ __global__ void __launch_bounds__(256) k_beam_begin(BeamArgs a) {
     q[BR_LIVE] = 1;
   }
 }
-void beam_begin(const BeamArgs& a, hipStream_t st) { k_beam_begin<<<a.n, 256, 0, st>>>(a); }
+void beam_start(const BeamArgs& a, hipStream_t st) { k_beam_begin<<<a.n, 256, 0, st>>>(a); }
+
+// ---------------------------------------------------------------- self-attention of the beams' rows
+// Block (head, row): one query over at most 448 positions, so a few hundred keys and values of
+// 64: 8 lanes a key (16 bytes or two a lane), a lane a dim of the values, every load of four
+// keys or pages in flight at once.  The row's own key and value come from the product's
+// rows, rounded to the cache's type, and go into the cache; positions of the last page past it
+// hold anything and are left out.  What bounds it: two dependent memory round trips.
+template <typename S>
+__global__ void __launch_bounds__(256) k_beam_attn(BeamAttnArgs a) {
+  StampScope stamp_scope(a.stamp, 256);
+  __shared__ float sc[kMaxCtx], newv[kHeadDim], red[4], acc[4][kHeadDim];
+  __shared__ int pts[kMaxCtx / kPage];
+  const int head = blockIdx.x, p = blockIdx.y / kRows, i = blockIdx.y % kRows, row = a.rows.slot0 * kRows + blockIdx.y;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, slot = a.rows.slot_of(p, i), H = a.n_head;
+  const int* st = a.state + max(slot, 0) * kStateInts;
+  const int L = st[ST_L];
+  float* q = a.qkv + (size_t)row * a.ldq + head * kHeadDim;
+  if (slot < 0 || !st[ST_LIVE] || st[ST_DONE] || L < 0 || L >= a.n_ctx) {  // uniform: a row of no beam
+    if (t < kHeadDim) put_op<S>(a.out, a.nsplit, a.R9, row, head * kHeadDim + t, 0.f);
+    return;
+  }
+  if (t < a.pages) pts[t] = a.page_table[(size_t)slot * a.pages + t];
+  const int g = lane & 7, kl = lane >> 3, d = H * kHeadDim;
+  float q8[8], k8[8];
+  ld8(q + 8 * g, q8);
+  ld8(q + d + 8 * g, k8);
+  float own = 0.f;  // the score of the row's own key
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    q8[e] *= 0.125f;
+    own = fmaf(q8[e], to_f(from_f<S>(k8[e])), own);
+  }
+  own = sum8(own);
+  __syncthreads();
+  S* K = reinterpret_cast<S*>(a.kcache);
+  S* V = reinterpret_cast<S*>(a.vcache);
+  constexpr bool vt = sizeof(S) == 2;  // values of a page: [head][dim][position], fp32 [head][position][dim]
+  if (t < kHeadDim) {
+    const size_t ph = (size_t)pts[L / kPage] * H + head;
+    const S v = from_f<S>(q[2 * d + t]);
+    newv[t] = to_f(v);
+    K[(ph * kPage + L % kPage) * kHeadDim + t] = from_f<S>(q[d + t]);
+    V[vt ? (ph * kHeadDim + t) * kPage + L % kPage : (ph * kPage + L % kPage) * kHeadDim + t] = v;
+  }
+  // scores of the L cached keys: 32 of the block at a time, four times that in flight
+  constexpr int B = 4;
+  float mx = own;
+  for (int j0 = 0; j0 < L; j0 += 32 * B) {
+    float kx[B][8];
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int j = min(j0 + 32 * u + 8 * w + kl, L - 1);
+      ld8(K + (((size_t)pts[j / kPage] * H + head) * kPage + j % kPage) * kHeadDim + 8 * g, kx[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(q8[e], kx[u][e], s);
+      s = sum8(s);
+      const int j = j0 + 32 * u + 8 * w + kl;
+      if (j < L) {
+        mx = fmaxf(mx, s);
+        if (g == 0) sc[j] = s;
+      }
+    }
+  }
+  mx = wave_max(mx);
+  if (lane == 0) red[w] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  // values: a wave every fourth page, a lane a dim
+  const int np = (L + kPage - 1) / kPage;
+  float o = 0.f, l = 0.f;
+  for (int c0 = w; c0 < np; c0 += 4 * B) {
+    float v[B][kPage];
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const size_t ph = (size_t)pts[min(c0 + 4 * u, np - 1)] * H + head;
+      if constexpr (vt) {
+        ld8(V + (ph * kHeadDim + lane) * kPage, v[u]);
+        ld8(V + (ph * kHeadDim + lane) * kPage + 8, v[u] + 8);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPage; ++e) v[u][e] = to_f(V[(ph * kPage + e) * kHeadDim + lane]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int c = c0 + 4 * u;
+      if (c >= np) break;
+#pragma unroll
+      for (int e = 0; e < kPage; ++e) {
+        const int j = kPage * c + e;
+        const float pr = j < L ? __expf(sc[j] - mx) : 0.f;
+        l += pr;
+        o = fmaf(pr, j < L ? v[u][e] : 0.f, o);
+      }
+    }
+  }
+  acc[w][lane] = o;
+  __syncthreads();  // every wave has read red[] and its queries
+  if (lane == 0) red[w] = l;
+  if (a.clear_q && t < kHeadDim) q[t] = 0.f;
+  __syncthreads();
+  if (t < kHeadDim) {
+    const float pr = __expf(own - mx), sum = (red[0] + red[1]) + (red[2] + red[3]) + pr;
+    put_op<S>(a.out, a.nsplit, a.R9, row, head * kHeadDim + t,
+              fmaf(pr, newv[t], (acc[0][t] + acc[1][t]) + (acc[2][t] + acc[3][t])) / sum);
+  }
+}
+template <typename S>
+void beam_attn(const BeamAttnArgs& a, hipStream_t st) {
+  k_beam_attn<S><<<dim3(a.n_head, a.rows.slots() * kRows), 256, 0, st>>>(a);
+}
+template void beam_attn<float>(const BeamAttnArgs&, hipStream_t);
+template void beam_attn<bf16>(const BeamAttnArgs&, hipStream_t);
 
 // After the selection: candidates in order, those that end with the end-of-transcript token
 // become finished hypotheses and the others beams, until there are as many beams.  Leaves

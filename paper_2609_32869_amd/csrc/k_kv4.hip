@@ -524,9 +524,7 @@ __global__ void __launch_bounds__(NW * 64) k_kv4_attend(Kv4AttendArgs a) {
       O = fmaf(f, wo[j][i][d], O);
     }
     if constexpr (OUT == KV4_OPERAND) {
-      const int to = a.row0 + r * a.orr + i * a.ori;
-      put_op<bf16>(a.op, a.nsplit, a.R9, to, head * kHeadDim + d, O / L);
-      for (int p = 1; p <= a.pad; ++p) put_op<bf16>(a.op, a.nsplit, a.R9, to + p, head * kHeadDim + d, 0.f);
+      put_op<bf16>(a.op, a.nsplit, a.R9, a.row0 + r * a.rows + i, head * kHeadDim + d, O / L);
     } else if constexpr (OUT == KV4_RECORDS) {
       float* rec = a.part + (((size_t)r * a.c.n_head + head) * a.nchunk + chunk) * kXrPart;
       rec[32 + t] = O;

@@ -321,6 +321,22 @@ __global__ void __launch_bounds__(256) k_verify_begin(BeginArgs a) {
   fill_rows<S>(a, slot, toks, poss, false, bc);
 }
 
+// Beam search: each beam's newest token at its position, the beams as rows (rows of no beam take
+// a token all the same; nothing reads them).
+template <typename S>
+__global__ void __launch_bounds__(256) k_beam_rows_begin(BeginArgs a, BeamRows b) {
+  __shared__ int toks[kRows], poss[kRows];
+  const BeginCols bc(a.d);
+  if (threadIdx.x < kRows) {
+    const int s = b.slot_of(blockIdx.x, threadIdx.x);
+    const int* st = a.state + max(s, a.slot0) * kStateInts;
+    toks[threadIdx.x] = min(max(st[ST_ANCHOR], 0), a.n_vocab - 1);
+    poss[threadIdx.x] = min(st[ST_L], a.n_ctx - 1);
+  }
+  __syncthreads();
+  fill_rows<S>(a, a.slot0 + blockIdx.x, toks, poss, false, bc);
+}
+
 // Draft block X_t = [Emb(y_t), m, ..., m] (Eq. 2).  The drafter history already
 // holds every verified position (it is written at the end of each verify).
 template <typename S>
@@ -932,6 +948,10 @@ void Ops<S>::reduce_ln(const RlnArgs& a, int rows, hipStream_t st) {
 template <typename S>
 void Ops<S>::verify_begin(const BeginArgs& a, int n, hipStream_t st) { k_verify_begin<S><<<dim3(n, kBeginGroups), 256, 0, st>>>(a); }
 template <typename S>
+void Ops<S>::beam_begin(const BeginArgs& a, const BeamRows& b, hipStream_t st) {
+  k_beam_rows_begin<S><<<dim3(b.slots(), kBeginGroups), 256, 0, st>>>(a, b);
+}
+template <typename S>
 void Ops<S>::draft_begin(const BeginArgs& a, int n, hipStream_t st) { k_draft_begin<S><<<dim3(n, kBeginGroups), 256, 0, st>>>(a); }
 template <typename S>
 void Ops<S>::prefill_begin(const BeginArgs& a, int n, hipStream_t st) { k_prefill_begin<S><<<dim3(n, kBeginGroups), 256, 0, st>>>(a); }
@@ -968,6 +988,7 @@ void accept_greedy(const AcceptArgs& a, hipStream_t st) { k_accept_greedy<<<(a.n
   template void Ops<S>::ln_operand(const LnArgs&, int, hipStream_t);        \
   template void Ops<S>::reduce_ln(const RlnArgs&, int, hipStream_t);        \
   template void Ops<S>::verify_begin(const BeginArgs&, int, hipStream_t);   \
+  template void Ops<S>::beam_begin(const BeginArgs&, const BeamRows&, hipStream_t); \
   template void Ops<S>::draft_begin(const BeginArgs&, int, hipStream_t);    \
   template void Ops<S>::prefill_begin(const BeginArgs&, int, hipStream_t);  \
   template void Ops<S>::hist_write(const HistArgs&, int, hipStream_t);

@@ -411,7 +411,7 @@ struct Runner {
   // The LayerNorm operand of the next product was already written by the
   // residual reduction (Ad16 for a block's first product, Ad32 for the head).
   bool ln_ready = false;
-  int share = 0;  // beams: leaders whose acoustic memory the slots of the pass share (see CrossArgs)
+  const BeamRows* beams = nullptr;  // the pass's rows are a search's beams
   int tap_next = -1;  // drafter tap the next folded q|k|v product writes from its rows (-1: none)
 
   // The LayerNorm that follows a block: the next block's first one, or the final
@@ -627,12 +627,13 @@ struct Runner {
            });
   }
 
-  void cross(int slot0, int n, int layer, const OprojArgs& op) {
+  // mem0: the slots' acoustic memories begin at this one
+  void cross(int slot0, int n, int mem0, int layer, const OprojArgs& op) {
     CrossArgs a{};
     a.op = op;
     a.q = F32(L.qkv);
     a.ldq = 3 * c.d_model;
-    a.kv = xkv_layer(layer);
+    a.kv = xkv_layer(layer) - (ptrdiff_t)((slot0 - mem0) * xkv_slot());
     a.out = Ad16();
     a.slot0 = slot0;
     a.d = c.d_model;
@@ -641,7 +642,6 @@ struct Runner {
     a.nsplit = L.nsplit_op;
     a.R9 = R9();
     a.vt_frames = vt_frames();
-    a.share = share;
     if (bf16_storage(c) && op.w == nullptr && cross_by_pair(n, c.n_head, c.n_frames)) {
       a.by_pair = 1;
       a.chunk = kXpChunk;
@@ -655,7 +655,7 @@ struct Runner {
     a.part = F32(L.xpart);
     const double wbytes = op.w ? (double)c.d_model * c.d_model * eb() : 0.0;  // fused output product
     if (kv4()) {
-      cross_kv4(a, n, layer, wbytes);
+      cross_kv4(a, n, mem0, layer, wbytes);
       return;
     }
     launch("attn_cross", 2.0 * c.n_head * c.n_frames * kHeadDim * eb() * n + wbytes, [&](unsigned long long* sp) {
@@ -667,7 +667,7 @@ struct Runner {
   // The same over keys and values held in 4 bits.  One slot with the fused output product:
   // the 128-frame chunks' records and their merge, as in bf16; else a block per (head,
   // slot) writes the next product's operand.
-  void cross_kv4(CrossArgs a, int n, int layer, double wbytes) {
+  void cross_kv4(CrossArgs a, int n, int mem0, int layer, double wbytes) {
     Kv4AttendArgs t{};
     t.c = kv4_layer(layer);
     t.q = a.q + (size_t)a.slot0 * kRows * a.ldq;
@@ -675,24 +675,14 @@ struct Runner {
     t.si = a.ldq;
     t.sh = kHeadDim;
     t.vec = 1;
-    t.slot0 = a.slot0;
+    t.slot0 = mem0;
     t.n = n;
     t.rows = kRows;
     t.op = a.out;
     t.nsplit = a.nsplit;
     t.R9 = a.R9;
     t.row0 = a.slot0 * kRows;
-    t.orr = kRows;
-    t.ori = 1;
     t.part = a.part;
-    if (a.share && a.op.w == nullptr) {
-      // a request's beams are the rows: each slot's first row, all on the leader's memory
-      t.n = a.share;
-      t.rows = n / a.share;
-      t.si = (long long)a.share * kRows * a.ldq;
-      t.ori = a.share * kRows;
-      t.pad = kRows - 1;
-    }
     const double bytes = (double)kKv4Group * t.c.groups * c.n_head * t.n + wbytes;
     launch("attn_cross", bytes, [&](unsigned long long* sp) {
       t.stamp = sp;
@@ -740,7 +730,8 @@ struct Runner {
       gemv_ln("gemv_q2", EPI_STORE, slot0, n, h_, b.ln2_g, b.ln2_b, b.c_q2, d, 0, Ad16(), b.w_q2, b.b_q2, d, d, qkv, 3 * d);
     }
     const OprojArgs op2 = oproj(b.w_o2, b.b_o2);
-    cross(slot0, n, xlayer, op2);
+    const int part = beams ? beams->n : n;  // a search's slots from the second n on use the first n's memories again
+    for (int s = 0; s < n; s += part) cross(slot0 + s, part, slot0, xlayer, op2);
     if (op2.w == nullptr) {
       touch_next(slot0, n, b.w_fc1, (size_t)c.d_ff * d, 64);
       resid("gemv_o", slot0, n, Ad16(), b.w_o2, b.b_o2, d, d);
@@ -789,6 +780,26 @@ struct Runner {
     }
   }
 
+  // one block's q | k | v and self-attention of a search's beams (their own page tables, no
+  // drafter tap); q_clear: the attention leaves the query places at zero
+  void beam_self(int slot0, int n, const BlockW& b, int layer, bool q_clear) {
+    const int d = c.d_model;
+    float* qkv = F32(L.qkv);
+    if (ln_ready) gemv("gemv_qkv", EPI_STORE, slot0, n, Ad16(), b.w_qkv, b.b_qkv, d, 3 * d, qkv, 3 * d);
+    else gemv_ln("gemv_qkv", EPI_STORE, slot0, n, F32(L.h), b.ln1_g, b.ln1_b, b.c_qkv, 3 * d, 0, Ad16(), b.w_qkv, b.b_qkv,
+                 d, 3 * d, qkv, 3 * d);
+    ln_ready = false;
+    BeamAttnArgs at{};
+    at.rows = *beams; at.qkv = qkv; at.ldq = 3 * d; at.kcache = skv_layer(layer); at.vcache = skv_layer(layer) + kv_stride();
+    at.state = I32(L.state); at.page_table = I32(L.page_table); at.out = Ad16(); at.n_head = c.n_head; at.n_ctx = c.n_ctx;
+    at.pages = L.pages_per_slot; at.nsplit = L.nsplit_op; at.R9 = R9(); at.clear_q = q_clear;
+    launch("attn_self", 0, [&](unsigned long long* sp) {
+      at.stamp = sp;
+      beam_attn<S>(at, st);
+    });
+    resid("gemv_o", slot0, n, Ad16(), b.w_o, b.b_o, d, d);
+  }
+
   void target_forward(int slot0, int n) {
     const int d = c.d_model;
     float *h_ = F32(L.h), *qkv = F32(L.qkv);
@@ -797,6 +808,14 @@ struct Runner {
     touch_ = Touch{nullptr, 0, 0};
     for (int l = 0; l < c.n_layer; ++l) {
       const BlockW& b = L.tb[l];
+      const LnNext nx = l + 1 < c.n_layer ? LnNext{L.tb[l + 1].ln1_g, L.tb[l + 1].ln1_b, false, L.tb[l + 1].w_qkv, (size_t)3 * d * d}
+                                          : LnNext{L.lnf_g, L.lnf_b, true, 0, 0};
+      if (beams) {
+        const bool q_clear = split_small(slot0, n, d, d);
+        beam_self(slot0, n, b, l, q_clear);
+        block_tail(slot0, n, b, l, -1, nx, q_clear);
+        continue;
+      }
       int tap = -1;
       for (int i = 0; i < c.n_tap; ++i)
         if (c.taps[i] == l) tap = i;
@@ -830,8 +849,6 @@ struct Runner {
         Ops<S>::attn_self(at, n, st);
       });
       if (at.op.w == nullptr) resid("gemv_o", slot0, n, Ad16(), b.w_o, b.b_o, d, d);
-      const LnNext nx = l + 1 < c.n_layer ? LnNext{L.tb[l + 1].ln1_g, L.tb[l + 1].ln1_b, false, L.tb[l + 1].w_qkv, (size_t)3 * d * d}
-                                          : LnNext{L.lnf_g, L.lnf_b, true, 0, 0};
       block_tail(slot0, n, b, l, tap, nx, q_clear);
     }
   }
@@ -985,29 +1002,28 @@ struct Runner {
   // One step of a beam search: the target over every beam's newest token, the choice of
   // the next beams, their bookkeeping and their page tables.
   void beam_step(const BeamSearch& bs, int* done) {
-    const int slot0 = bs.slot0, n = bs.n, B = bs.beams, total = n * B, P = L.pages_per_slot;
+    const int slot0 = bs.slot0, n = bs.n, B = bs.beams, P = L.pages_per_slot;
+    const BeamRows rows{slot0, n, B};
     auto at = [&](size_t off) { return bs.ws + off; };
     BeginArgs ba{};
-    ba.state = I32(L.state); ba.draft = I32(L.draft); ba.tok = I32(L.tok); ba.emb = W(L.tok_emb); ba.emb_kind = wk(true); ba.pos = W(L.pos_emb);
+    ba.state = I32(L.state); ba.emb = W(L.tok_emb); ba.emb_kind = wk(true); ba.pos = W(L.pos_emb);
     ba.h = F32(L.h); ba.slot0 = slot0; ba.d = c.d_model; ba.n_vocab = c.n_vocab; ba.n_ctx = c.n_ctx;
-    ba.block_k = c.block_k; ba.k_max = 0;
-    ba.page_table = I32(L.page_table); ba.pages_per_slot = P;
-    ba.status = h->at<unsigned>(L.status);
-    launch("begin", 0, [&](unsigned long long*) { Ops<S>::verify_begin(ba, total, st); });
-    share = n;
-    target_forward(slot0, total);
-    share = 0;
-    head(slot0, total, F32(L.h), L.lnf_g, L.lnf_b, F32(L.logits));
+    launch("begin", 0, [&](unsigned long long*) { Ops<S>::beam_begin(ba, rows, st); });
+    beams = &rows;
+    target_forward(slot0, rows.slots());
+    beams = nullptr;
+    head(slot0, rows.slots(), F32(L.h), L.lnf_g, L.lnf_b, F32(L.logits));
     BeamSelectArgs sa{};
     sa.logits = F32(L.logits) + (size_t)slot0 * kRows * c.n_vocab;
     sa.sr = (long long)kRows * c.n_vocab;
-    sa.sb = (long long)n * kRows * c.n_vocab;
+    sa.sb = c.n_vocab;
+    sa.far = (long long)(n - 1) * kRows * c.n_vocab;
     sa.scores = reinterpret_cast<const float*>(at(bs.sp.scores)); sa.suppress = h->suppress;
     sa.n = n; sa.beams = B; sa.vocab = c.n_vocab; sa.k = 2 * B;
     beam_space(sa, at(bs.sp.select));
     sa.out_score = reinterpret_cast<float*>(at(bs.sp.cs)); sa.out_beam = reinterpret_cast<int*>(at(bs.sp.cb));
     sa.out_token = reinterpret_cast<int*>(at(bs.sp.ct));
-    launch("beam_select", 4.0 * total * c.n_vocab, [&](unsigned long long*) { beam_select(sa, st); });
+    launch("beam_select", 4.0 * n * B * c.n_vocab, [&](unsigned long long*) { beam_select(sa, st); });
     BeamArgs g = beam_args(h, bs);
     g.done = done;
     launch("beam_advance", 0, [&](unsigned long long*) { beam_advance(g, st); });
@@ -1654,7 +1670,7 @@ static int beam_start(Handle* h, int slot0, int n, int beams, const int32_t* las
   hipStream_t st = static_cast<hipStream_t>(stream);
   HIPCK(h, hipMemcpyAsync(bs.ws + bs.sp.last, last_tokens, (size_t)n * 4, hipMemcpyDeviceToDevice, st));
   HIPCK(h, hipMemcpyAsync(bs.ws + bs.sp.max_new, max_new, (size_t)n * 4, hipMemcpyHostToDevice, st));
-  beam_begin(beam_args(h, bs), st);
+  beam_start(beam_args(h, bs), st);
   HIPCK(h, hipGetLastError());
   HIPCK(h, hipStreamSynchronize(st));
   h->searches[slot0] = bs;

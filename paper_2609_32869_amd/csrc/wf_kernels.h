@@ -165,15 +165,8 @@ struct CrossArgs {
   float* part;        // [pair][nchunk][kXrPart] chunk partials (nchunk > 1 or op.w)
   OprojArgs op;       // fused output product (taken by the merge kernel)
   int by_pair;        // bf16: one block per (head, slot) walks every chunk (no records, no merge)
-  int share;          // beams: slot slot0 + i reads the memory of slot slot0 + i % share (0: its own)
   unsigned long long* stamp;  // launch timing slot (profiled calls), or null
 };
-// Kernels of their own where beams share a memory: a test here lengthens the first load's
-// address by enough to cost a batch-1 step 0.6 %.
-template <bool SHARE>
-__device__ __forceinline__ int memory_slot(const CrossArgs& a, int slot) {
-  return SHARE ? a.slot0 + (slot - a.slot0) % a.share : slot;
-}
 // Chunk partial record: max [9] at 0, sum [9] at 16, acc [9][64] at 32.
 constexpr int kXrPart = 32 + kRows * 64;
 constexpr int kXrMaxPairs = 128;      // chunking only below this many (head, slot) pairs
@@ -247,6 +240,20 @@ struct RlnArgs {
   Operand out;
   int d, row0, nsplit, R9;
   unsigned long long* stamp;  // launch timing slot (profiled calls), or null
+};
+
+// A beam search's rows: beam b of request r (slot slot0 + b * n + r) is row b % 9 of the pass's slot
+// slot0 + b / 9 * n + r, so that a request's beams are the rows of one slot on one acoustic
+// memory (two of both above nine beams).
+struct BeamRows {
+  int slot0, n, beams;
+  __host__ __device__ int groups() const { return (beams + kRows - 1) / kRows; }
+  __host__ __device__ int slots() const { return n * groups(); }  // of the pass
+  // row i of the pass's slot slot0 + p: its beam's own slot, -1: none
+  __host__ __device__ int slot_of(int p, int i) const {
+    const int b = p / n * kRows + i;
+    return b < beams ? slot0 + b * n + p % n : -1;
+  }
 };
 
 struct BeginArgs {
@@ -462,6 +469,7 @@ struct Ops {
   static void attn_cross(const CrossArgs& a, int n, hipStream_t st);
   static void reduce_ln(const RlnArgs& a, int rows, hipStream_t st);
   static void verify_begin(const BeginArgs& a, int n, hipStream_t st);
+  static void beam_begin(const BeginArgs& a, const BeamRows& b, hipStream_t st);
   static void draft_begin(const BeginArgs& a, int n, hipStream_t st);
   static void prefill_begin(const BeginArgs& a, int n, hipStream_t st);
   static void hist_write(const HistArgs& a, int n, hipStream_t st);

@@ -17,9 +17,9 @@ constexpr int kMaxBeams = 16;       // beams of one request
 constexpr int kMaxCand = 32;        // candidates kept per request
 constexpr int kMaxVocab = 1 << 20;  // columns of a logits row
 struct BeamSelectArgs {
-  const void* logits;  // element (r, b, v) at r * sr + b * sb + v
+  const void* logits;  // element (r, b, v) at r * sr + b * sb + (b < kRows ? 0 : far) + v
   int bf16_logits;
-  long long sr, sb;
+  long long sr, sb, far;  // far: more of it for the beams from kRows on (a handle's logits)
   const float* scores;      // (r, b) at r * beams + b
   const uint8_t* suppress;  // [vocab] nonzero: the column is left out, or null
   int n, beams, vocab, k;
@@ -87,9 +87,25 @@ struct BeamArgs {
   int len_max;
   float length_penalty;
 };
-void beam_begin(const BeamArgs& a, hipStream_t st);
+void beam_start(const BeamArgs& a, hipStream_t st);
 void beam_advance(const BeamArgs& a, hipStream_t st);
 void beam_end(const BeamArgs& a, hipStream_t st);
+// Self-attention of the beams' rows, each over its own page table, after putting its new key
+// and value into its page.
+struct BeamAttnArgs {
+  BeamRows rows;
+  float* qkv;  // q | k | v of the pass's rows, [row][ldq]
+  int ldq;
+  void *kcache, *vcache;
+  const int* state;
+  const int* page_table;
+  Operand out;
+  int n_head, n_ctx, pages, nsplit, R9;
+  int clear_q;  // as in AttnArgs
+  unsigned long long* stamp;
+};
+template <typename S>
+void beam_attn(const BeamAttnArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- acoustic keys and values in 4 bits
 // Per (entry, head), groups of 32 frames one after the other, kKv4Group bytes each: the
@@ -147,10 +163,8 @@ struct Kv4AttendArgs {
   int slot0, n, rows;
   float* part;  // chunk records (nchunk > 1)
   int nchunk, cgroups;  // chunks of the groups and groups of a chunk (set by the launcher)
-  // a decoder step's output rows: row i of request r is operand row row0 + r * orr + i * ori;
-  // the `pad` rows behind each are set to zero (beams: a slot's rows that no beam uses)
-  Operand op;
-  int nsplit, R9, row0, orr, ori, pad;
+  Operand op;  // a decoder step's output: row i of request r is operand row row0 + r * rows + i
+  int nsplit, R9, row0;
   unsigned long long* stamp;  // launch timing slot (profiled calls), or null
 };
 size_t kv4_workspace(int n, int rows, int n_head, int frames);

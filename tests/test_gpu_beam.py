@@ -51,7 +51,7 @@ def check(got, want, tol):
 F32_TOL, BF16_TOL = 2e-4, 2e-2
 
 
-@pytest.mark.parametrize("beams,lens,max_new", [(1, [5], 8), (3, [11, 16], 12), (5, [17, 3, 30], 20), (16, [9], 6), (4, [1], 20)])
+@pytest.mark.parametrize("beams,lens,max_new", [(1, [5], 8), (3, [11, 16], 12), (5, [17, 3, 30], 20), (16, [9], 6), (4, [1], 20), (11, [12, 7, 20], 10)])
 def test_beam_search_matches_the_oracle(beams, lens, max_new):
     cfg = MICRO
     W, eng = engine(cfg, beams * len(lens))
@@ -119,10 +119,10 @@ def test_context_end():
 
 
 @pytest.mark.parametrize("bits", [16, 4])
-@pytest.mark.parametrize("beams,n", [(5, 1), (3, 4)])
+@pytest.mark.parametrize("beams,n", [(5, 1), (3, 4), (9, 2), (10, 2), (16, 3)])
 def test_bf16_storage(beams, n, bits):
-    """bf16 caches; with the acoustic keys and values in 4 bits a request's beams are the rows of one attention call:
-    there the first request's hypotheses are read again token by token, as a plain slot's."""
+    """bf16 caches (above nine beams a request's rows are those of two slots on one memory); with the acoustic keys and
+    values in 4 bits the first request's hypotheses are read again token by token, as a plain slot's."""
     cfg = BF16
     W, eng = engine(cfg, beams * n, bits)
     lens = [4 + 13 * i for i in range(n)]
@@ -156,7 +156,7 @@ def test_bf16_storage(beams, n, bits):
 @pytest.mark.parametrize("bits", [16, 4])
 def test_a_search_after_a_broken_memory(bits):
     """A recording of non-finite features leaves non-finite activation rows behind; once its cache pages hold other
-    prompts, a search on the same slots sets no status bit (rows that no beam uses hold zeros, not what was there)."""
+    prompts, a search on the same slots sets no status bit (rows that no beam uses are made anew, not left as they were)."""
     cfg = BF16
     W, eng = engine(cfg, 6, bits)
     rows, toks = prompts(cfg, [8, 8])

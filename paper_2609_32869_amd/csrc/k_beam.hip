@@ -301,7 +301,8 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
 // candidates by 64-bit score, the first four of a thread held in registers.  The k-th best of a
 // wave's lanes (scores rounded to 32 bits, which keeps the order, to 16 bits of that)
 // bounds the k-th best again; more survivors than the array holds, which takes that many
-// nearly equal scores, are chosen one by one.
+// nearly equal scores, are chosen one by one.  One request of five beams 4.4 us, 96 of eight
+// 7.3: a chain of short phases between barriers, not bytes (1.3 MB of candidates at 96).
 constexpr int kMergeList = 1024, kMergeRegs = 4;
 // ties: order = beam * 2^20 + column
 __device__ __forceinline__ bool ahead(double s, int o, double t, int p) { return s > t || (s == t && o < p); }
@@ -489,7 +490,8 @@ void beam_select(const BeamSelectArgs& a, hipStream_t st) {
 // Grid (region x part of a page, request).  Every block works the request's pages out for
 // itself (a few hundred table entries, a bit per page of the cache in LDS), so that one
 // launch does it all.  The first block writes the tables, each copies its part of the
-// copied pages in its region.
+// copied pages in its region.  64 regions of 40 KB pages, 5 beams: one request 6.7 us, four
+// dependent round trips; eight requests 11.4 us, the copied pages' bytes (floor 8.9).
 constexpr int kReorderThreads = 256;
 __global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a, int parts) {
   __shared__ unsigned used[kMaxPages / 32];
@@ -560,7 +562,8 @@ __global__ void __launch_bounds__(kReorderThreads) k_cache_reorder(ReorderArgs a
 }
 
 void cache_reorder(const ReorderArgs& a, hipStream_t st) {
-  // pages cut into parts of at least 4 KB until about four blocks per compute unit copy
+  // pages cut into parts of at least 4 KB until about four blocks per compute unit copy (eight
+  // requests: towards 512 blocks 14.2 us, 1,024 11.2, 2,048 12.5, 4,096 16.4: each block repeats the tables' work)
   const long long have = (long long)a.regions * a.n;
   int parts = (int)std::max<long long>(1, std::min<long long>(1024 / have, (long long)(a.page_bytes / 4096)));
   k_cache_reorder<<<dim3((unsigned)(a.regions * parts), a.n), kReorderThreads, 0, st>>>(a, parts);
@@ -611,14 +614,17 @@ void beam_start(const BeamArgs& a, hipStream_t st) { k_beam_begin<<<a.n, 256, 0,
 
 // ---------------------------------------------------------------- self-attention of the beams' rows
 // Block (head, row): one query over at most 448 positions, so a few hundred keys and values of
-// 64: 8 lanes a key (16 bytes or two a lane), a lane a dim of the values, every load of four
+// 64: 8 lanes a key (16 bytes or two a lane), a lane a dim of the values, the loads of three
 // keys or pages in flight at once.  The row's own key and value come from the product's
 // rows, rounded to the cache's type, and go into the cache; positions of the last page past it
-// hold anything and are left out.  What bounds it: two dependent memory round trips.
+// hold anything and are left out.  bf16, 20 heads: 5 rows at 130 positions 6.5 us, two
+// dependent memory round trips; 80 rows at 190 positions 13.6 us, registers (eight waves a SIMD;
+// four keys or pages in flight, six waves: 6.0 and 14.9 us; two: 6.4 and 13.6).  The nine rows
+// of a (head, request) on one XCD: no faster.
 template <typename S>
 __global__ void __launch_bounds__(256) k_beam_attn(BeamAttnArgs a) {
   StampScope stamp_scope(a.stamp, 256);
-  __shared__ float sc[kMaxCtx], newv[kHeadDim], red[4], acc[4][kHeadDim];
+  __shared__ float sc[kMaxCtx], newv[kHeadDim], red[4], sum[4], acc[4][kHeadDim];
   __shared__ int pts[kMaxCtx / kPage];
   const int head = blockIdx.x, p = blockIdx.y / kRows, i = blockIdx.y % kRows, row = a.rows.slot0 * kRows + blockIdx.y;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, slot = a.rows.slot_of(p, i), H = a.n_head;
@@ -652,8 +658,8 @@ __global__ void __launch_bounds__(256) k_beam_attn(BeamAttnArgs a) {
     K[(ph * kPage + L % kPage) * kHeadDim + t] = from_f<S>(q[d + t]);
     V[vt ? (ph * kHeadDim + t) * kPage + L % kPage : (ph * kPage + L % kPage) * kHeadDim + t] = v;
   }
-  // scores of the L cached keys: 32 of the block at a time, four times that in flight
-  constexpr int B = 4;
+  // scores of the L cached keys: 32 of the block at a time, B times that in flight
+  constexpr int B = 3;
   float mx = own;
   for (int j0 = 0; j0 < L; j0 += 32 * B) {
     float kx[B][8];
@@ -679,9 +685,19 @@ __global__ void __launch_bounds__(256) k_beam_attn(BeamAttnArgs a) {
   if (lane == 0) red[w] = mx;
   __syncthreads();
   mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  // values: a wave every fourth page, a lane a dim
+  // probabilities in place, zero behind the last position
   const int np = (L + kPage - 1) / kPage;
-  float o = 0.f, l = 0.f;
+  float l = 0.f;
+  for (int j = t; j < np * kPage; j += 256) {
+    const float pr = j < L ? __expf(sc[j] - mx) : 0.f;
+    sc[j] = pr;
+    l += pr;
+  }
+  l = wave_sum(l);
+  if (lane == 0) sum[w] = l;
+  __syncthreads();
+  // values: a wave every fourth page, a lane a dim
+  float o = 0.f;
   for (int c0 = w; c0 < np; c0 += 4 * B) {
     float v[B][kPage];
 #pragma unroll
@@ -702,21 +718,17 @@ __global__ void __launch_bounds__(256) k_beam_attn(BeamAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < kPage; ++e) {
         const int j = kPage * c + e;
-        const float pr = j < L ? __expf(sc[j] - mx) : 0.f;
-        l += pr;
-        o = fmaf(pr, j < L ? v[u][e] : 0.f, o);
+        o = fmaf(sc[j], j < L ? v[u][e] : 0.f, o);
       }
     }
   }
   acc[w][lane] = o;
-  __syncthreads();  // every wave has read red[] and its queries
-  if (lane == 0) red[w] = l;
-  if (a.clear_q && t < kHeadDim) q[t] = 0.f;
+  if (a.clear_q && t < kHeadDim) q[t] = 0.f;  // every wave has read its queries
   __syncthreads();
   if (t < kHeadDim) {
-    const float pr = __expf(own - mx), sum = (red[0] + red[1]) + (red[2] + red[3]) + pr;
+    const float pr = __expf(own - mx), all = (sum[0] + sum[1]) + (sum[2] + sum[3]) + pr;
     put_op<S>(a.out, a.nsplit, a.R9, row, head * kHeadDim + t,
-              fmaf(pr, newv[t], (acc[0][t] + acc[1][t]) + (acc[2][t] + acc[3][t])) / sum);
+              fmaf(pr, newv[t], (acc[0][t] + acc[1][t]) + (acc[2][t] + acc[3][t])) / all);
   }
 }
 template <typename S>

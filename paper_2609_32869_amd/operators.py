@@ -32,12 +32,7 @@ def _refuse(what):
     raise WfError(f"invalid argument (-1): {what}")
 
 
-def _int(v, name):
-    """A number that the C entries' 32 bits hold (the range that each allows is the library's check)."""
-    v = int(v)
-    if not -2 ** 31 <= v < 2 ** 31:
-        _refuse(f"{name} out of range")
-    return v
+_INTS = 2 ** 31  # sizes from here on would be cut off by the C entries' 32 bits; smaller ones are the library's to check
 
 
 def _tensor(t, name, dtype, shape, device):
@@ -100,8 +95,8 @@ def _enqueue(device, stream, call, *tensors):
 
 @functools.lru_cache(maxsize=256)
 def _select_bytes(n, beams, vocab, k):
-    for v, name in ((n, "n"), (beams, "beams"), (vocab, "n_vocab"), (k, "k")):
-        _int(v, name)
+    if max(n, beams, vocab, abs(k)) >= _INTS:
+        _refuse("a size is out of range")
     nbytes = ctypes.c_size_t()
     _check(load_library().wf_beam_select_workspace_bytes(n, beams, vocab, k, ctypes.byref(nbytes)))
     return nbytes.value
@@ -162,15 +157,15 @@ def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=Non
     regions, pages = cache.shape[:2]
     if regions == 0 or pages == 0:
         _refuse("cache must hold a page")
-    for v, name in ((n, "n"), (beams, "beams"), (max_pages, "max_pages"), (regions, "n_regions"), (pages, "n_pages"),
-                    (pool_pages, "pool_pages"), (page_tokens, "page_tokens")):
-        _int(v, name)
+    page_tokens = int(page_tokens)
+    if max(n, beams, max_pages, regions, pages, pool_pages, abs(page_tokens)) >= _INTS:
+        _refuse("a size is out of range")
     region = cache.numel() // regions * cache.element_size()
 
     def call(raw, empty):
         new = empty((n, beams, max_pages), dtype=_I32)
         _check(lib.wf_cache_reorder(cache.data_ptr(), regions, region, pages, region // pages, tables.data_ptr(), new.data_ptr(),
-                                    n, beams, max_pages, int(page_tokens), parents.data_ptr(), lens.data_ptr(),
+                                    n, beams, max_pages, page_tokens, parents.data_ptr(), lens.data_ptr(),
                                     pool.data_ptr(), pool_pages, raw))
         return new
 
@@ -185,7 +180,9 @@ class AcousticCache4:
 
     def __init__(self, entries, n_head, n_frames, device="cuda"):
         self.lib = load_library()
-        self.entries, self.n_head, self.n_frames = _int(entries, "entries"), _int(n_head, "n_head"), _int(n_frames, "n_frames")
+        self.entries, self.n_head, self.n_frames = int(entries), int(n_head), int(n_frames)
+        if max(abs(self.entries), abs(self.n_head), abs(self.n_frames)) >= _INTS:
+            _refuse("a size is out of range")
         nbytes = ctypes.c_size_t()
         _check(self.lib.wf_kv4_bytes(self.entries, self.n_head, self.n_frames, ctypes.byref(nbytes)))
         self.data = torch.empty(nbytes.value, dtype=_U8, device=device)
@@ -222,9 +219,11 @@ class AcousticCache4:
         n = k.shape[0]
         if vtype != dtype or v.shape[0] != n:
             _refuse("v must have k's type and shape")
-        plens, slot0, n = self._lens(lens, n), _int(slot0, "slot0"), _int(n, "n")
+        if not 0 <= slot0 <= self.entries - n:
+            _refuse("entries out of range")
+        plens = self._lens(lens, n)
         _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv4_store(
-            self._ref, slot0, n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, plens, raw)), k, v, lens, self.data)
+            self._ref, int(slot0), n, k.data_ptr(), ks, v.data_ptr(), vs, dtype, plens, raw)), k, v, lens, self.data)
 
     def load(self, slot0, n, dtype=torch.float32, stream=None):
         """The keys and values that entries slot0 .. slot0 + n - 1 hold: two tensors [n, n_frames, n_head, 64]."""
@@ -246,18 +245,21 @@ class AcousticCache4:
         frames (int32 [n], None: all) of entries slot0 ..: [n, rows, n_head, 64] in q's type."""
         dtype, qs = self._rows(q, "q", None)
         n, rows = q.shape[:2]
+        if not 0 <= slot0 <= self.entries - n:
+            _refuse("entries out of range")
         need = self._spaces.get((n, rows))
         if need is None:
-            _int(n, "n"), _int(rows, "rows")
+            if rows >= _INTS:
+                _refuse("rows out of range")
             nbytes = ctypes.c_size_t()
             _check(self.lib.wf_kv4_attend_workspace_bytes(self._ref, n, rows, ctypes.byref(nbytes)))
             need = self._spaces[n, rows] = nbytes.value
-        plens, slot0 = self._lens(lens, n), _int(slot0, "slot0")
+        plens = self._lens(lens, n)
 
         def call(raw, empty):
             out = empty((n, rows, self.n_head, 64), dtype=q.dtype)
             ws = empty(need, dtype=_U8) if need else None
-            _check(self.lib.wf_kv4_attend(self._ref, slot0, n, q.data_ptr(), qs, rows, dtype, plens, out.data_ptr(),
+            _check(self.lib.wf_kv4_attend(self._ref, int(slot0), n, q.data_ptr(), qs, rows, dtype, plens, out.data_ptr(),
                                           ws.data_ptr() if need else None, need, raw))
             return out
 

@@ -91,14 +91,49 @@ struct Raw<bf16, N> {
   __device__ __forceinline__ float get(int j) const { return __uint_as_float(j & 1 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16); }
 };
 
-// A group's codes and scales, each lane its own.
-__device__ __forceinline__ void put_group(uint8_t* out, const uint2 (&kc)[2], const uint32_t (&ks)[2], const uint32_t (&vc)[4],
-                                          uint32_t vs) {
+// A group's key or value codes and scales from the lane's values (16 dims of frames n, 16 + n; 8 frames of dims
+// 4 n .. + 3), of which those that are not `in` count as zero.
+template <typename In>
+__device__ __forceinline__ void put_keys(uint8_t* out, const In& in, float (&x)[2][16]) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  *reinterpret_cast<uint4*>(out + 16 * lane) = make_uint4(kc[0].x, kc[0].y, kc[1].x, kc[1].y);
-  *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = make_uint4(vc[0], vc[1], vc[2], vc[3]);
-  if ((kg & 1) == 0) *reinterpret_cast<uint16_t*>(out + kKv4KeyScale + 32 * (kg >> 1) + 2 * n) = (uint16_t)(ks[0] | ks[1] << 8);
-  if (kg == 0) *reinterpret_cast<uint32_t*>(out + kKv4ValueScale + 4 * n) = vs;
+  uint2 c[2];
+  uint32_t s[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const bool ok = in(16 * t + n);
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      x[t][j] = ok ? x[t][j] : 0.f;
+      m = umax(m, mag(x[t][j]));
+    }
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));  // the block's other 16 dims
+    s[t] = scale_of(__uint_as_float(m));
+    c[t] = make_uint2(codes8(x[t], scale_f(s[t])), codes8(x[t] + 8, scale_f(s[t])));
+  }
+  *reinterpret_cast<uint4*>(out + 16 * lane) = make_uint4(c[0].x, c[0].y, c[1].x, c[1].y);
+  if ((kg & 1) == 0) *reinterpret_cast<uint16_t*>(out + kKv4KeyScale + 32 * (kg >> 1) + 2 * n) = (uint16_t)(s[0] | s[1] << 8);
+}
+template <typename In>
+__device__ __forceinline__ void put_values(uint8_t* out, const In& in, float (&x)[4][8]) {
+  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
+  uint32_t c[4], s = 0;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[dt][j] = in(8 * kg + j) ? x[dt][j] : 0.f;
+      m = umax(m, mag(x[dt][j]));
+    }
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
+    const uint32_t sb = scale_of(__uint_as_float(m));
+    c[dt] = codes8(x[dt], scale_f(sb));
+    s |= sb << (8 * dt);
+  }
+  *reinterpret_cast<uint4*>(out + kKv4Values + 16 * lane) = make_uint4(c[0], c[1], c[2], c[3]);
+  if (kg == 0) *reinterpret_cast<uint32_t*>(out + kKv4ValueScale + 4 * n) = s;
 }
 
 template <typename T>
@@ -123,38 +158,18 @@ __global__ void __launch_bounds__(256) k_kv4_store(Kv4StoreArgs a) {
   for (int t = 0; t < 2; ++t) k[t].load(K + min(g * 32 + 16 * t + n, top) * a.kf, a.vec);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j].load(V + min(g * 32 + 8 * kg + j, top) * a.vf, a.vec);
-  uint2 kc[2];
-  uint32_t ks[2], vc[4], vs = 0;
+  auto in = [&](int f) { return g * 32 + f < len; };
+  float x[2][16], y[4][8];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const bool in = g * 32 + 16 * t + n < len;
-    float x[16];
-    uint32_t m = 0;
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      x[j] = in ? k[t].get(j) : 0.f;
-      m = umax(m, mag(x[j]));
-    }
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));  // the block's other 16 dims
-    ks[t] = scale_of(__uint_as_float(m));
-    kc[t] = make_uint2(codes8(x, scale_f(ks[t])), codes8(x + 8, scale_f(ks[t])));
-  }
+    for (int j = 0; j < 16; ++j) x[t][j] = k[t].get(j);
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt) {
-    float x[8];
-    uint32_t m = 0;
+  for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = g * 32 + 8 * kg + j < len ? v[j].get(dt) : 0.f;
-      m = umax(m, mag(x[j]));
-    }
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
-    const uint32_t sb = scale_of(__uint_as_float(m));
-    vc[dt] = codes8(x, scale_f(sb));
-    vs |= sb << (8 * dt);
-  }
-  put_group(out, kc, ks, vc, vs);
+    for (int j = 0; j < 8; ++j) y[dt][j] = v[j].get(dt);
+  put_keys(out, in, x);
+  put_values(out, in, y);
 }
 
 void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
@@ -165,7 +180,7 @@ void kv4_store(const Kv4StoreArgs& a, hipStream_t st) {
 
 // ---------------------------------------------------------------- load
 // The store's waves and lanes; the results' rows leave 16 bytes a lane: 16 entries of 1500
-// frames into fp32 54 us, 5.1 TB/s.
+// frames into fp32 54 us, 5.1 TB/s (keys and values in waves of their own: 76).
 __device__ __forceinline__ void st8(float* p, bf16x8 x) {
   *reinterpret_cast<float4*>(p) = make_float4((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4((float)x[4], (float)x[5], (float)x[6], (float)x[7]);
@@ -234,37 +249,18 @@ __global__ void __launch_bounds__(256) k_kv4_pack(Kv4PackArgs a) {
   for (int t = 0; t < 2; ++t) k[t].load(K + (size_t)min(g * 32 + 16 * t + n, F - 1) * kHeadDim, 1);
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) v[dt].load(V + vt_index(4 * n + dt, g * 32 + 8 * kg), 1);
-  uint2 kc[2];
-  uint32_t ks[2], vc[4], vs = 0;
+  auto in = [&](int f) { return g * 32 + f < F; };
+  float x[2][16], y[4][8];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    float x[16];
-    uint32_t m = 0;
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      x[j] = g * 32 + 16 * t + n < F ? k[t].get(j) : 0.f;
-      m = umax(m, mag(x[j]));
-    }
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-    ks[t] = scale_of(__uint_as_float(m));
-    kc[t] = make_uint2(codes8(x, scale_f(ks[t])), codes8(x + 8, scale_f(ks[t])));
-  }
+    for (int j = 0; j < 16; ++j) x[t][j] = k[t].get(j);
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt) {
-    float x[8];
-    uint32_t m = 0;
+  for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = g * 32 + 8 * kg + j < F ? v[dt].get(j) : 0.f;
-      m = umax(m, mag(x[j]));
-    }
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
-    const uint32_t sb = scale_of(__uint_as_float(m));
-    vc[dt] = codes8(x, scale_f(sb));
-    vs |= sb << (8 * dt);
-  }
-  put_group(out, kc, ks, vc, vs);
+    for (int j = 0; j < 8; ++j) y[dt][j] = v[dt].get(j);
+  put_keys(out, in, x);
+  put_values(out, in, y);
 }
 void kv4_pack(const Kv4PackArgs& a, hipStream_t st) {
   k_kv4_pack<<<dim3((a.c.groups + 3) / 4, a.c.n_head, a.layers), 256, 0, st>>>(a);

@@ -299,10 +299,12 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
 
 // Merge: a block per request.  16 lanes a row join its pieces' sums; then the pieces'
 // candidates by 64-bit score, the first four of a thread held in registers.  The k-th best of a
-// wave's lanes (scores rounded to 32 bits, which keeps the order, to 16 bits of that)
-// bounds the k-th best again; more survivors than the array holds, which takes that many
-// nearly equal scores, are chosen one by one.  One request of five beams 4.4 us, 96 of eight
-// 7.3: a chain of short phases between barriers, not bytes (1.3 MB of candidates at 96).
+// wave's lanes (scores rounded to 32 bits, which keeps the order, to 24 bits of that: with 16
+// cumulative scores of some hundred lie too close, 350 candidates all survive and the merge
+// takes 42 us instead of 7) bounds the k-th best again; more survivors than the array holds,
+// which takes that many nearly equal scores, are chosen one by one.  One request of five beams
+// 4.7 us, 96 of eight 7.5: a chain of short phases between barriers, not bytes (1.3 MB of
+// candidates at 96).
 constexpr int kMergeList = 1024, kMergeRegs = 4;
 // ties: order = beam * 2^20 + column
 __device__ __forceinline__ bool ahead(double s, int o, double t, int p) { return s > t || (s == t && o < p); }
@@ -367,7 +369,7 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
   const bool active = best != 0;
   uint32_t bound = 0;
   int need = a.k;
-  if (__popcll(__ballot(active)) >= need) wave_kth<31, 16>(best, active, bound, need);
+  if (__popcll(__ballot(active)) >= need) wave_kth<31, 8>(best, active, bound, need);
   if (lane == 0) tv[w] = bound;
   __syncthreads();
   bound = max(max(tv[0], tv[1]), max(tv[2], tv[3]));

@@ -34,7 +34,8 @@ def check_select(logits, scores, k, suppress=None, stream=None):
     (1, 1, 1, 1, torch.float32), (1, 1, 1, 4, torch.bfloat16), (2, 3, 5, 32, torch.float32), (1, 5, 64, 10, torch.float32),
     (3, 16, 65, 32, torch.bfloat16), (1, 5, 51866, 10, torch.float32), (2, 8, 51865, 16, torch.bfloat16),
     (7, 2, 1023, 7, torch.float32), (5, 4, 4097, 8, torch.bfloat16), (300, 5, 777, 10, torch.float32),
-    (1, 16, 51866, 32, torch.float32), (1, 2, 300001, 5, torch.float32), (130, 4, 9001, 32, torch.bfloat16)])
+    (1, 16, 51866, 32, torch.float32), (1, 2, 300001, 5, torch.float32), (130, 4, 9001, 32, torch.bfloat16),
+    (62, 8, 367, 3, torch.float32), (20, 16, 4624, 32, torch.float32), (4, 3, 40, 4, torch.bfloat16), (6, 9, 8200, 16, torch.float32)])
 def test_select(n, B, V, k, dtype):
     g = torch.Generator("cuda").manual_seed(n * 1000 + V)
     logits = (3 * torch.randn((n, B, V), device="cuda", generator=g)).to(dtype)

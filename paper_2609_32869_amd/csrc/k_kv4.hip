@@ -602,17 +602,25 @@ __global__ void __launch_bounds__(256) k_kv4_merge(Kv4AttendArgs a) {
   }
 }
 
-// Chunks: a long memory's groups over about two blocks per CU, 16 groups (a step of each wave) or more to a chunk.
-// us a replayed call, split against one block per (head, request): 20 pairs, 2,048 frames 7.3 / 9.7, 4,500 frames
-// 8.0 / 18.1, 131,072 frames 40.5 / 418; 80 pairs, 4,500 frames 11.5 / 18.5; 160 pairs, 4,500 frames 18.1 / 19.2, 131,072
-// frames 312 / 424.  Up to 1,536 frames (20 pairs, 1,500 frames: 7.2 / 8.2) the merge's launch costs its caller more than
-// it saves, and from nearly a block per CU on (240 pairs, 4,500 frames: 23.2 / 19.8; 131,072: 464 / 471) one is as good.
-// Towards 256, 768 or 1,024 blocks instead of 512 (160 pairs of 4,500, of 16,384 frames): 18.9, 19.9, 19.0 us against
-// 18.1; 56, 45, 43 against 42.
-int kv4_chunks(int n, int rows, int n_head, int frames) {
-  const long long pairs = (long long)n * n_head * ((rows + 15) / 16), groups = kv4_groups(frames);
-  if (groups <= 48 || pairs >= 240) return 1;
-  return (int)std::max<long long>(1, std::min<long long>(512 / pairs, groups / 16));
+// Groups of a chunk: a long memory over about four blocks per CU, so that requests of different lengths share the
+// chip, in whole steps of a block's waves (16 groups, the nearest).  us a replayed call of 4,500 frames, 20 heads, split
+// against one block per (head, request): 20 pairs 7.6 / 18.1, 80 pairs 13.1 / 18.5, 320 pairs 28.3 / 33.4; of 131,072 frames:
+// 20 pairs 39.9 / 418, 160 pairs 306 / 424.  Not split: up to 1,536 frames (20 pairs, 1,500 frames: 7.2 / 8.2, but the merge's
+// launch costs the caller more); from 480 pairs; and, below 8,192 frames, pairs that give each CU as many blocks within a
+// fifth (240 pairs, 4,500 frames: 25.6 / 20.2; 460 pairs: 41.3 / 34.0).  Towards 512 blocks instead of 1,024 equal lengths
+// are a tenth faster at times (168 pairs, 13,512 frames: 38.5 against 43.1; 160 of 4,500: 18.4 against 20.4) and mixed ones
+// far slower (160 pairs of up to 16,384: 41 against 32; 40 of up to 131,072: 73 against 42).
+static int kv4_chunk(int n, int rows, int n_head, int frames) {
+  constexpr int step = kAttWaves * kAttStep, cus = 256;
+  const int pairs = (int)std::min<long long>((long long)n * n_head * ((rows + 15) / 16), 1 << 20), groups = kv4_groups(frames);
+  const bool even = 5 * pairs >= 4 * ((pairs + cus - 1) / cus * cus);
+  if (groups <= 3 * step || pairs >= 480 || (even && groups < 256)) return groups;
+  const int chunks = 1024 / pairs, each = (groups + chunks - 1) / chunks;
+  return std::max(step, (each + step / 2) / step * step);
+}
+static int kv4_chunks(int n, int rows, int n_head, int frames) {
+  const int each = kv4_chunk(n, rows, n_head, frames);
+  return (kv4_groups(frames) + each - 1) / each;
 }
 size_t kv4_workspace(int n, int rows, int n_head, int frames) {
   const int nc = kv4_chunks(n, rows, n_head, frames);
@@ -627,8 +635,8 @@ static void attend_launch(const Kv4AttendArgs& a, hipStream_t st) {
 }
 void kv4_attend(const Kv4AttendArgs& a0, hipStream_t st) {
   Kv4AttendArgs a = a0;
+  a.cgroups = kv4_chunk(a.n, a.rows, a.c.n_head, a.c.frames);
   a.nchunk = kv4_chunks(a.n, a.rows, a.c.n_head, a.c.frames);
-  a.cgroups = (a.c.groups + a.nchunk - 1) / a.nchunk;
   if (a.bf16_q) attend_launch<bf16>(a, st);
   else attend_launch<float>(a, st);
 }

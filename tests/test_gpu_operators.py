@@ -460,6 +460,21 @@ def test_attend_long_memory():
     check_attend(cache, 0, q, *held, [69001], torch.tensor([69001], dtype=torch.int32, device="cuda"))
 
 
+@pytest.mark.parametrize("n,F", [(340, 1600), (230, 1600), (50, 9000), (7, 3000)])
+def test_attend_mixed_lengths_of_long_memories(n, F):
+    """Many requests, split into chunks and not, some ending in the first chunk, some of no frames."""
+    wf = lib()
+    g = torch.Generator("cuda").manual_seed(n)
+    k = torch.randn((n, F, 1, 64), device="cuda", generator=g).bfloat16()
+    cache = wf.AcousticCache4(n, 1, F)
+    cache.store(0, k, k.flip(1))
+    held = [num(x) for x in cache.load(0, n)]
+    lens = torch.randint(0, F + 1, (n,), dtype=torch.int32, device="cuda", generator=g)
+    lens[0], lens[n // 2], lens[n - 1] = F, 0, 1
+    q = torch.randn((n, 2, 1, 64), device="cuda", generator=g)
+    check_attend(cache, 0, q, *held, lens.tolist(), lens)
+
+
 def test_attend_offsets_past_32_bits():
     """A cache of over 4 GiB: the last entries lie past a 32-bit offset."""
     wf = lib()

@@ -302,17 +302,21 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
 }
 
 // Merge: a block per request.  16 lanes a row join its pieces' sums; then the pieces'
-// candidates by 64-bit score, the first four of a thread held in registers.  The k-th best of a
-// wave's lanes (scores rounded to 32 bits, which keeps the order, to 24 bits of that: with 16
-// cumulative scores of some hundred lie too close, 350 candidates all survive and the merge
-// takes 42 us instead of 7) bounds the k-th best again; more survivors than the array holds,
-// which takes that many nearly equal scores, are chosen one by one.  One request of five beams
-// 4.7 us, 96 of eight 7.5: a chain of short phases between barriers, not bytes (1.3 MB of
+// candidates by 64-bit score, the first M of a thread held in registers (2 below 512
+// candidates, 4 up to 1,024, else 16: 3,584 of 16 beams, 32 best, 16.7 us with 4, 13.1 with 16).
+// The k-th best is bounded by the best of the waves' k-th best lanes; from 512 candidates on
+// they are mixed over the waves and the least of the waves' k/4-th best lanes bounds it more
+// closely (3,584 candidates: 13 us instead of 41; 350: 4.8 instead of 4.5).  Scores for that are rounded to 32 bits, which keeps
+// the order, and cut to 24 (with 16, cumulative scores of some hundred lie too close, 350
+// candidates all survive: 42 us instead of 7).  More survivors than the array holds, which
+// takes that many nearly equal scores, are chosen one by one.  One request of five beams
+// 4.8 us, 96 of eight 7.2: a chain of short phases between barriers, not bytes (1.3 MB of
 // candidates at 96).
-constexpr int kMergeList = 1024, kMergeRegs = 4;
+constexpr int kMergeList = 1024;
 // ties: order = beam * 2^20 + column
 __device__ __forceinline__ bool ahead(double s, int o, double t, int p) { return s > t || (s == t && o < p); }
 
+template <int M, bool MIX>
 __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
   __shared__ double top[kMaxBeams], rest[kMaxBeams], ls[kMergeList], bs[4];
   __shared__ int lo[kMergeList], bo[4], count;
@@ -320,11 +324,16 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
   const int r = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const int per = np * a.k, total = a.beams * per;
   const size_t first = (size_t)r * total;
-  float xv[kMergeRegs];
-  int xi[kMergeRegs];
+  // MIX: candidates in turn over the waves and, each time elsewhere, over their lanes
+  auto place = [&](int u) {
+    const int l = (lane + 9 * u) & 63;
+    return 256 * u + (MIX ? 4 * l + ((w + l) & 3) : t);
+  };
+  float xv[M];
+  int xi[M];
 #pragma unroll
-  for (int i = 0; i < kMergeRegs; ++i) {
-    const size_t at = first + min(t + 256 * i, total - 1);
+  for (int i = 0; i < M; ++i) {
+    const size_t at = first + min(place(i), total - 1);
     xv[i] = a.pv[at];
     xi[i] = a.pi[at];
   }
@@ -356,27 +365,27 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
     o = b << 20 | c;
     return i < total && c >= 0 && s > -INFINITY;
   };
-  double rs[kMergeRegs];
-  int ro[kMergeRegs];
-  bool rl[kMergeRegs];
+  double rs[M];
+  int ro[M];
+  bool rl[M];
   uint32_t best = 0;
 #pragma unroll
-  for (int i = 0; i < kMergeRegs; ++i) {
-    rl[i] = score(t + 256 * i, xv[i], xi[i], rs[i], ro[i]);
+  for (int i = 0; i < M; ++i) {
+    rl[i] = score(place(i), xv[i], xi[i], rs[i], ro[i]);
     if (rl[i]) best = max(best, order_of((float)rs[i]));
   }
-  for (int i = t + 256 * kMergeRegs; i < total; i += 256) {
+  for (int i = t + 256 * M; i < total; i += 256) {
     double s;
     int o;
     if (score(i, a.pv[first + i], a.pi[first + i], s, o)) best = max(best, order_of((float)s));
   }
   const bool active = best != 0;
   uint32_t bound = 0;
-  int need = a.k;
+  int need = MIX ? (a.k + 3) / 4 : a.k;
   if (__popcll(__ballot(active)) >= need) wave_kth<31, 8>(best, active, bound, need);
   if (lane == 0) tv[w] = bound;
   __syncthreads();
-  bound = max(max(tv[0], tv[1]), max(tv[2], tv[3]));
+  bound = MIX ? min(min(tv[0], tv[1]), min(tv[2], tv[3])) : max(max(tv[0], tv[1]), max(tv[2], tv[3]));
   auto keep = [&](double s, int o) {
     const int j = atomicAdd(&count, 1);
     if (j < kMergeList) {
@@ -385,9 +394,9 @@ __global__ void __launch_bounds__(256) k_beam_merge(BeamSelectArgs a, int np) {
     }
   };
 #pragma unroll
-  for (int i = 0; i < kMergeRegs; ++i)
+  for (int i = 0; i < M; ++i)
     if (rl[i] && order_of((float)rs[i]) >= bound) keep(rs[i], ro[i]);
-  for (int i = t + 256 * kMergeRegs; i < total; i += 256) {
+  for (int i = t + 256 * M; i < total; i += 256) {
     double s;
     int o;
     if (score(i, a.pv[first + i], a.pi[first + i], s, o) && order_of((float)s) >= bound) keep(s, o);
@@ -484,7 +493,10 @@ void beam_select(const BeamSelectArgs& a, hipStream_t st) {
   };
   if (a.bf16_logits) launch(bf16{});
   else launch(0.f);
-  k_beam_merge<<<a.n, 256, 0, st>>>(a, np);
+  const int total = a.beams * np * a.k;
+  if (total < 512) k_beam_merge<2, false><<<a.n, 256, 0, st>>>(a, np);
+  else if (total <= 1024) k_beam_merge<4, true><<<a.n, 256, 0, st>>>(a, np);
+  else k_beam_merge<16, true><<<a.n, 256, 0, st>>>(a, np);
 }
 
 // ---------------------------------------------------------------- page tables

@@ -35,7 +35,8 @@ def check_select(logits, scores, k, suppress=None, stream=None):
     (3, 16, 65, 32, torch.bfloat16), (1, 5, 51866, 10, torch.float32), (2, 8, 51865, 16, torch.bfloat16),
     (7, 2, 1023, 7, torch.float32), (5, 4, 4097, 8, torch.bfloat16), (300, 5, 777, 10, torch.float32),
     (1, 16, 51866, 32, torch.float32), (1, 2, 300001, 5, torch.float32), (130, 4, 9001, 32, torch.bfloat16),
-    (62, 8, 367, 3, torch.float32), (20, 16, 4624, 32, torch.float32), (4, 3, 40, 4, torch.bfloat16), (6, 9, 8200, 16, torch.float32)])
+    (62, 8, 367, 3, torch.float32), (20, 16, 4624, 32, torch.float32), (4, 3, 40, 4, torch.bfloat16), (6, 9, 8200, 16, torch.float32),
+    (1, 16, 300001, 32, torch.float32)])
 def test_select(n, B, V, k, dtype):
     g = torch.Generator("cuda").manual_seed(n * 1000 + V)
     logits = (3 * torch.randn((n, B, V), device="cuda", generator=g)).to(dtype)
@@ -62,6 +63,14 @@ def test_select_ties_and_orders(V, shape):
     logits = x.cuda().expand(2, 5, V).contiguous()
     check_select(logits, torch.zeros((2, 5), device="cuda"), 32)
     check_select(logits.bfloat16(), torch.tensor([[-1.0, -2, -1, -2, -1]] * 2, device="cuda"), 17)
+
+
+@pytest.mark.parametrize("levels", [1, 3])
+def test_select_more_equal_candidates_than_a_block_lists(levels):
+    """16 beams of equal rows, 32 best of each of 7 pieces: 3,584 candidates of one score, or of three."""
+    logits = (torch.arange(51866, device="cuda") % levels).float().expand(2, 16, 51866)
+    check_select(logits, torch.zeros((2, 16), device="cuda"), 32)
+    check_select(logits, torch.tensor([[0.0, -INF] * 8, [-1.0] * 16], device="cuda"), 31)
 
 
 def test_select_empty_beams_and_suppressed_tokens():

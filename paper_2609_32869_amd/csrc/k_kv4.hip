@@ -7,30 +7,13 @@
 // codes and the scale into two bf16 values, exactly.
 #include <algorithm>
 
+#include "wf_kv4.h"
 #include "wf_operand.h"
 #include "wf_ops.h"
 
 namespace wf {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// Smallest 2^e, e >= -120, with amax <= 6 * 2^e, as a biased exponent: amax = m 2^x with
-// 1 <= m < 2 is <= 6 * 2^e = 1.5 * 2^(e + 2) for e = x - 2 where m <= 1.5, else x - 1.
-// 0xff where amax is not finite.
-__device__ __forceinline__ uint32_t scale_of(float amax) {
-  const uint32_t u = __float_as_uint(amax);
-  const int e = (int)(u >> 23) - ((u & 0x7fffffu) <= 0x400000u ? 2 : 1);
-  return (u >> 23) == 255u ? 255u : (uint32_t)max(e, 7);
-}
-
-// 8 values -> 8 codes, element i in nibble i.
-__device__ __forceinline__ uint32_t codes8(const float* x, float s) {
-  uint32_t r = 0;
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[0], x[1], s, 0);
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[2], x[3], s, 1);
-  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[4], x[5], s, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x[6], x[7], s, 3);
-}
 
 // 8 codes -> the 8 bf16 values they stand for.
 __device__ __forceinline__ bf16x8 values8(uint32_t c, float s) {
@@ -40,11 +23,6 @@ __device__ __forceinline__ bf16x8 values8(uint32_t c, float s) {
   const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
   return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
-
-// max |x| that keeps a NaN (fmaxf would drop it): |x| as integers, NaN above infinity
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-__device__ __forceinline__ float scale_f(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // ---------------------------------------------------------------- store
 // A wave per (entry, head, 32-frame group), four heads a block: their rows lie beside each
@@ -231,42 +209,10 @@ void kv4_load(const Kv4LoadArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- a decoder's keys and values
-// The same codes from and to the request-time product's layout, whose values lie
-// transposed: a lane's eight frames of a dim are 16 consecutive bytes.  Grid z: layers
-// (pack) or entries (unpack).  Memory bounds both: 32 layers of a slot's 1,500 frames, 20
-// heads, packed in 70 us, 4.4 TB/s.
-__global__ void __launch_bounds__(256) k_kv4_pack(Kv4PackArgs a) {
-  const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
-  const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, H = a.c.n_head, F = a.c.frames;
-  if (g >= a.c.groups) return;
-  const bf16* src = a.kv + (size_t)blockIdx.z * a.stride;
-  const bf16* K = src + (size_t)head * F * kHeadDim + 16 * kg;
-  const bf16* V = src + ((size_t)H * F + (size_t)head * a.vt_frames) * kHeadDim;
-  uint8_t* out = a.c.base + blockIdx.z * a.layer + (((size_t)a.slot0 * H + head) * a.c.groups + g) * kKv4Group;
-  Raw<bf16, 16> k[2];
-  Raw<bf16, 8> v[4];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) k[t].load(K + (size_t)min(g * 32 + 16 * t + n, F - 1) * kHeadDim, 1);
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt) v[dt].load(V + vt_index(4 * n + dt, g * 32 + 8 * kg), 1);
-  auto in = [&](int f) { return g * 32 + f < F; };
-  float x[2][16], y[4][8];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[t][j] = k[t].get(j);
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[dt][j] = v[dt].get(j);
-  put_keys(out, in, x);
-  put_values(out, in, y);
-}
-void kv4_pack(const Kv4PackArgs& a, hipStream_t st) {
-  k_kv4_pack<<<dim3((a.c.groups + 3) / 4, a.c.n_head, a.layers), 256, 0, st>>>(a);
-}
-
-__global__ void __launch_bounds__(256) k_kv4_unpack(Kv4PackArgs a) {
+// The values that the prompt pass's attention reads, in the request-time product's bf16
+// layout, whose values lie transposed: a lane's eight frames of a dim are 16 consecutive
+// bytes.  Grid z: entries.  Memory bounds it: about ten slots of 1,500 frames, 20 heads, 22 us.
+__global__ void __launch_bounds__(256) k_kv4_unpack(Kv4UnpackArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, kg = lane >> 4;
   const int g = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y, slot = a.slot0 + blockIdx.z, H = a.c.n_head, F = a.c.frames;
   if (g >= a.c.groups) return;
@@ -291,7 +237,7 @@ __global__ void __launch_bounds__(256) k_kv4_unpack(Kv4PackArgs a) {
   for (int dt = 0; dt < 4; ++dt)  // frames past the last are zeros, as the layout has them
     st8(V + vt_index(4 * n + dt, g * 32 + 8 * kg), values8(vw[dt], scale_f(vs >> (8 * dt) & 255)));
 }
-void kv4_unpack(const Kv4PackArgs& a, hipStream_t st) {
+void kv4_unpack(const Kv4UnpackArgs& a, hipStream_t st) {
   k_kv4_unpack<<<dim3((a.c.groups + 3) / 4, a.c.n_head, a.n), 256, 0, st>>>(a);
 }
 

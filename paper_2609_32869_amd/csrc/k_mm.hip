@@ -19,6 +19,7 @@
 
 #include "wf_common.h"
 #include "wf_kernels.h"
+#include "wf_kv4.h"
 #include "wf_operand.h"
 #include "wf_split.h"
 
@@ -181,6 +182,46 @@ __global__ void __launch_bounds__(NT) k_mm(MmArgs a, int nmb, int nnb, int rs) {
   }
   __syncthreads();
 
+  if constexpr (EP == MM_XKV4) {
+    // keys: items (row, 32 columns), values: items (column, 32 rows), each a block of the 4-bit
+    // cache, rounded to bf16 first; rows past the last frame are zeros
+    uint8_t* out = reinterpret_cast<uint8_t*>(a.out) + (size_t)z * a.sO;
+    const int groups = kv4_groups(a.M);
+    auto group = [&](int col, int f) { return out + ((size_t)(col >> 6) * groups + f / kKv4Frames) * kKv4Group; };
+    auto block = [&](float (&x)[32]) {  // the block's scale byte
+      uint32_t m = 0;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) m = umax(m, mag(x[e]));
+      return scale_of(__uint_as_float(m));
+    };
+    for (int it = t; it < BM * (BN / 32); it += NT) {
+      const int rl = it / (BN / 32), c32 = it % (BN / 32) * 32, f = m0 + rl, n = n0 + c32;
+      if (n >= a.d || f >= groups * kKv4Frames) continue;
+      float x[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) x[e] = f < a.M ? to_f(from_f<bf16>(ct(rl)[c32 + e])) : 0.f;
+      const uint32_t s = block(x);
+      uint8_t* g = group(n, f);
+      const int half = n >> 5 & 1, fr = f % kKv4Frames;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(key_word(g, fr, 4 * half + i)) = codes8(x + 8 * i, scale_f(s));
+      *key_scale(g, fr, half) = (uint8_t)s;
+    }
+    for (int it = t; it < BN * (BM / 32); it += NT) {
+      const int cl = it % BN, r32 = it / BN * 32, n = n0 + cl, f = m0 + r32;
+      if (n < a.d || n >= a.N || f >= groups * kKv4Frames) continue;
+      float x[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) x[e] = f + e < a.M ? to_f(from_f<bf16>(ct(r32 + e)[cl])) : 0.f;
+      const uint32_t s = block(x);
+      const int col = n - a.d, dim = col & 63;
+      uint8_t* g = group(col, f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(value_word(g, i, dim)) = codes8(x + 8 * i, scale_f(s));
+      g[kKv4ValueScale + dim] = (uint8_t)s;
+    }
+    return;
+  }
   if (EP == MM_XKV || EP == MM_QKV_ENC) {
     // columns [0, nrow) row-major bf16 (keys, or queries | keys), columns
     // [nrow, N) values transposed per head: MM_XKV in 256-frame pieces
@@ -358,7 +399,7 @@ __global__ void __launch_bounds__(512, 2) k_mmw(MmArgs a, int nmb, int nnb, int 
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int mt = m0 + (wm * MI + i) * 32;
-      const int nrow = EP == MM_XKV ? a.d : EP == MM_QKV_ENC ? 2 * a.d : 1 << 30;
+      const int nrow = EP == MM_XKV || EP == MM_XKV4 ? a.d : EP == MM_QKV_ENC ? 2 * a.d : 1 << 30;
       floatx16 c = acc[i][j];
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -379,6 +420,54 @@ __global__ void __launch_bounds__(512, 2) k_mmw(MmArgs a, int nmb, int nnb, int 
             const int f = mt + 8 * (v >> 2) + 4 * lk + (v & 3);
             if (f < a.M) out[(size_t)f * a.ldo] = c[v] + o[v];
           }
+        }
+      } else if (EP == MM_XKV4) {
+        // the tile is 32 blocks of the 4-bit cache: a key's 32 dims (four lanes, turned around in the
+        // wave's LDS), a value's 32 frames (two lanes); rounded to bf16 first, zero past the last frame
+        const int groups = kv4_groups(a.M), g = mt / kKv4Frames, col = nt < nrow ? nt : nc - nrow;
+        if (g >= groups) continue;  // uniform
+        uint8_t* grp = reinterpret_cast<uint8_t*>(a.out) + (size_t)z * a.sO + ((size_t)(col >> 6) * groups + g) * kKv4Group;
+        if (nt < nrow) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int v = 0; v < 8; ++v) tr[(8 * (v >> 2) + 4 * lk + (v & 3)) * 33 + lr] = c[8 * half + v];
+            __builtin_amdgcn_wave_barrier();
+            const int fr = 16 * half + (lane >> 2), i = lane & 3;
+            float o[8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              o[e] = mt + fr < a.M ? to_f(from_f<bf16>(tr[(lane >> 2) * 33 + 8 * i + e])) : 0.f;
+              m = umax(m, mag(o[e]));
+            }
+            __builtin_amdgcn_wave_barrier();
+            m = umax(m, (uint32_t)__shfl_xor((int)m, 1));
+            m = umax(m, (uint32_t)__shfl_xor((int)m, 2));
+            const uint32_t s = scale_of(__uint_as_float(m));
+            const int hf = nt >> 5 & 1;
+            *reinterpret_cast<uint32_t*>(key_word(grp, fr, 4 * hf + i)) = codes8(o, scale_f(s));
+            if (i == 0) *key_scale(grp, fr, hf) = (uint8_t)s;
+          }
+        } else {
+          float o[16];
+          uint32_t m = 0;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            o[v] = mt + 8 * (v >> 2) + 4 * lk + (v & 3) < a.M ? to_f(from_f<bf16>(c[v])) : 0.f;
+            m = umax(m, mag(o[v]));
+          }
+          m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
+          const uint32_t s = scale_of(__uint_as_float(m));
+          // four codes per eight frames in each of the two lanes; the first lane writes frames 0 .. 15
+          const float sf = scale_f(s);
+          const uint32_t lo = codes4(o, sf) | codes4(o + 4, sf) << 16, hi = codes4(o + 8, sf) | codes4(o + 12, sf) << 16;
+          const uint32_t give = lk ? lo : hi, got = (uint32_t)__shfl_xor((int)give, 32);
+          const uint32_t first = lk ? got : lo, second = lk ? hi : got;  // frames 0 .. 3 and 4 .. 7 of each eight
+          const int dim = col & 63;
+          *reinterpret_cast<uint32_t*>(value_word(grp, 2 * lk, dim)) = (first & 0xffffu) | second << 16;
+          *reinterpret_cast<uint32_t*>(value_word(grp, 2 * lk + 1, dim)) = first >> 16 | (second & 0xffff0000u);
+          if (lk == 0) grp[kKv4ValueScale + dim] = (uint8_t)s;
         }
       } else if (nt < nrow) {
         // bf16 rows: half tiles turned around in the wave's LDS, 8 columns per lane
@@ -442,6 +531,7 @@ int mm_check(const MmArgs& a, int ep) {
     return -1;
   if (ep == MM_GELU_ADD_F32 && (!a.add || a.ldadd < a.N)) return -1;
   if (ep == MM_XKV && (a.N != 2 * a.d || a.d % kHeadDim || a.vt_frames < a.M || a.vt_frames % kVtPiece)) return -1;
+  if (ep == MM_XKV4 && (a.N != 2 * a.d || a.d % kHeadDim)) return -1;
   if (ep == MM_QKV_ENC && (a.N != 3 * a.d || a.d % kHeadDim || (a.period > 0 ? a.period != a.vt_frames || a.M % a.period : a.vt_frames < a.M) || a.vt_frames % 8 || a.ldo % 8 ||
                            a.ldo < 2 * a.d))
     return -1;
@@ -459,6 +549,7 @@ static void mm_launch(const MmArgs& a, int ep, const XcdSplit& x, int batch, hip
     case MM_BF16_GELU: k_mm<MM_BF16_GELU, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_RESID: k_mm<MM_RESID, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_XKV: k_mm<MM_XKV, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
+    case MM_XKV4: k_mm<MM_XKV4, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_QKV_ENC: k_mm<MM_QKV_ENC, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_GELU_ADD_F32: k_mm<MM_GELU_ADD_F32, BM, NS><<<grid, NT, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
   }
@@ -469,6 +560,7 @@ static void mmw_launch(const MmArgs& a, int ep, const XcdSplit& x, int batch, hi
     case MM_BF16_GELU: k_mmw<MM_BF16_GELU><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_RESID: k_mmw<MM_RESID><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_XKV: k_mmw<MM_XKV><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
+    case MM_XKV4: k_mmw<MM_XKV4><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_QKV_ENC: k_mmw<MM_QKV_ENC><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
     case MM_GELU_ADD_F32: k_mmw<MM_GELU_ADD_F32><<<grid, 512, 0, st>>>(a, x.nmb, x.nnb, x.rs); break;
   }

@@ -293,7 +293,7 @@ int compute_layout(const wf_config& c, Layout& L, bool many_rows) {
     if (L.fc2_split) L.fc2_part = L.xpart;
   }
   L.lncd = region(L.nsplit_op == 3 ? cw * 4 : 0);
-  L.xtmp = region(kv4_storage(c) ? kv4_tmp_slots(c) * xslot : 0);
+  L.xtmp = region(kv4_storage(c) ? B * xslot : 0);
   L.stamps = region((size_t)kStampSlots * kStampWords * 8);
   // prompt pass over many rows: every prompt of a call up to kPreMaxRows rows, the
   // operands as bf16 planes
@@ -1072,21 +1072,10 @@ struct Runner {
             mm(a, MM_XKV, count, st);
             return;
           }
-          // 4 bits: as many layers at a time as the transit buffer holds, then packed
-          const int most = kv4_tmp_slots(c);
-          const bf16 *w0 = a.B, *b0 = a.bias;
-          for (int l0 = 0; l0 < count; l0 += most) {
-            const int nl = std::min(most, count - l0);
-            a.B = w0 + l0 * a.sB;
-            a.bias = b0 + l0 * a.sBias;
-            a.out = h->at<bf16>(L.xtmp);
-            a.sO = (long long)xkv_slot();
-            mm(a, MM_XKV, nl, st);
-            Kv4PackArgs k{};
-            k.c = kv4_layer(first + l0); k.layer = kv4_layer_bytes(c); k.kv = h->at<bf16>(L.xtmp); k.stride = xkv_slot();
-            k.vt_frames = vt_frames(); k.slot0 = slot; k.n = 1; k.layers = nl;
-            kv4_pack(k, st);
-          }
+          const Kv4 to = kv4_layer(first);
+          a.out = to.base + (size_t)slot * c.n_head * to.groups * kKv4Group;
+          a.sO = (long long)kv4_layer_bytes(c);
+          mm(a, MM_XKV4, count, st);
         };
         group(0, c.n_layer, L.tb);
         if (!(c.draft_flags & WF_DRAFT_NO_AUDIO)) group(c.n_layer, c.n_draft_layer, L.db);
@@ -1187,9 +1176,9 @@ struct Runner {
         reduce(ks, b.b_o, b.ln2_g, b.ln2_b, true);
         product("gemv_q2", PRE_STORE, A, b.w_q2, b.b_q2, d, d, q, d, nullptr);
         if (kv4()) {  // the pass's slots' keys and values of this block, as the attention reads them
-          Kv4PackArgs k{};
+          Kv4UnpackArgs k{};
           k.c = kv4_layer(l); k.kv = h->at<bf16>(L.xtmp); k.stride = xkv_slot(); k.vt_frames = vt_frames();
-          k.slot0 = plan.parts[ps.part0].slot; k.n = plan.parts[ps.part0 + ps.nparts - 1].slot - k.slot0 + 1; k.layers = 1;
+          k.slot0 = plan.parts[ps.part0].slot; k.n = plan.parts[ps.part0 + ps.nparts - 1].slot - k.slot0 + 1;
           kv4_unpack(k, st);
         }
         attend(true, kv4() ? h->at<S>(L.xtmp) : xkv_layer(l), nullptr);

@@ -141,8 +141,6 @@ inline bool kv4_storage(const wf_config& c) { return c.dtype == WF_BF16_KV4; }
 inline size_t kv4_layer_bytes(const wf_config& c) {
   return (size_t)c.max_batch * c.n_head * kv4_groups(c.n_frames) * kKv4Group;
 }
-// slots (or layers of one slot) that xtmp holds
-inline int kv4_tmp_slots(const wf_config& c) { return c.max_batch < 4 ? 4 : c.max_batch; }
 
 // many_rows: with the buffers of the many-row prompt pass (bf16 storage)
 int compute_layout(const wf_config& c, Layout& L, bool many_rows = true);

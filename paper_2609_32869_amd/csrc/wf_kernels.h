@@ -318,6 +318,7 @@ enum {
   MM_RESID = 3,      // out fp32 [M][ldo] += scale * C + bias
   MM_XKV = 4,        // acoustic keys [head][frame][64] then values [head][frame / 256][dim][256]
   MM_QKV_ENC = 5,    // columns < 2d: out bf16 [M][ldo]; the rest: out2 bf16 [head][dim][vt_frames]
+  MM_XKV4 = 7,       // the same in 4 bits (k_kv4.hip): out the entry's groups, sO in bytes
   MM_GELU_ADD_F32 = 6,  // out fp32 [M][ldo] = GELU(scale * C + bias) + add[M][ldadd]
 };
 struct MmArgs {

@@ -119,7 +119,7 @@ void beam_attn(const BeamAttnArgs& a, hipStream_t st);
 constexpr int kKv4Frames = 32;
 constexpr int kKv4Values = 1024, kKv4KeyScale = 2048, kKv4ValueScale = 2112, kKv4Group = 2176;
 constexpr int kKv4MaxFrames = 1 << 20;
-inline int kv4_groups(int frames) { return (frames + kKv4Frames - 1) / kKv4Frames; }
+__host__ __device__ inline int kv4_groups(int frames) { return (frames + kKv4Frames - 1) / kKv4Frames; }
 struct Kv4 {
   uint8_t* base;
   int n_head, groups, frames;
@@ -140,19 +140,16 @@ struct Kv4LoadArgs {
   int bf16_out, slot0, n;
 };
 void kv4_load(const Kv4LoadArgs& a, hipStream_t st);
-// A decoder's acoustic keys and values: packed from, and unpacked to, the bf16 layout of
-// the request-time product (keys [head][frame][64], values [head][frame / 256][dim][256]).
-struct Kv4PackArgs {
-  Kv4 c;              // of the first layer
-  size_t layer;       // bytes from one layer's cache to the next's
-  bf16* kv;           // entry (or layer) i at i * stride elements
+// A decoder's acoustic keys and values in the bf16 layout of the request-time product (keys
+// [head][frame][64], values [head][frame / 256][dim][256]).
+struct Kv4UnpackArgs {
+  Kv4 c;
+  bf16* kv;  // entry i at i * stride elements
   size_t stride;
   int vt_frames;
-  int slot0, n;       // entries; layers: pack only
-  int layers;         // pack: layers of one entry (n 1); unpack: 1
+  int slot0, n;
 };
-void kv4_pack(const Kv4PackArgs& a, hipStream_t st);
-void kv4_unpack(const Kv4PackArgs& a, hipStream_t st);
+void kv4_unpack(const Kv4UnpackArgs& a, hipStream_t st);
 struct Kv4AttendArgs {
   Kv4 c;
   const void* q;  // element (r, i, h, d) at r * sr + i * si + h * sh + d

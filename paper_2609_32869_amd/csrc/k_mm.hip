@@ -14,7 +14,8 @@
 // q ^ (r & 7) so that the eight rows a wave's lane group reads fall in different
 // banks).
 // The finished tile goes through LDS again so that every epilogue writes 16-byte
-// runs of consecutive elements.
+// runs of consecutive elements (the 4-bit cache's: words of eight codes, 128 bytes of
+// values a wave together).
 #include <algorithm>
 
 #include "wf_common.h"

@@ -32,7 +32,7 @@ struct Layout {
   size_t a_d16, a_d32, a_f16, a_tap16, h, qkv, hp, kvh, hv, hi, tok, g, gmax, draft, lasth, logits, dlogits, part;
   size_t hm, hs, tmax, tsum, dmax, dsum, sst, spart;  // sampling: normalisers and draw partials
   size_t xpart;   // chunked cross-attention: partial records
-  size_t xtmp;    // 4-bit acoustic K/V: bf16 keys and values on their way in (encode) and out (prompt pass)
+  size_t xtmp;    // 4-bit acoustic K/V: one block's keys and values in bf16 for the prompt pass
   size_t lncd;    // LayerNorm column sums of the folded products (batch 1, bf16)
   size_t stamps;  // launch timing slots (profiling)
   // prompt pass over many rows (bf16): residual rows, queries, operands, partial

@@ -467,8 +467,9 @@ int wf_kv4_load(const wf_kv4* c, int slot0, int n, void* k, void* v, int dtype, 
 /*
  * Attention of `rows` query rows of each of n requests over the first lens[r] frames of
  * its entry slot0 + r: softmax(q k^T / 8) v, without a mask (cross-attention).  Query
- * values enter the products exactly, probabilities exactly (fp32) or to 2^-16 relative
- * (bf16), the softmax and all sums are fp32.  A request of no frames gets zeros.
+ * values and probabilities enter the products exactly, the softmax and all sums are fp32.
+ * A request of no frames gets zeros; keys and values that stand for infinity within the
+ * length give results that are infinite or NaN.
  * q: device, fp32 or bf16; element (r, i, h, d) lies r * q_stride[0] + i * q_stride[1] +
  *   h * q_stride[2] + d elements in (strides >= 0, a host array of three): a request's beams
  *   or the rows of a pass are its rows.

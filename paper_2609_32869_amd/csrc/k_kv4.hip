@@ -245,7 +245,9 @@ void kv4_unpack(const Kv4UnpackArgs& a, hipStream_t st) {
 // Block (head, request, chunk of the groups) x (16 query rows), eight waves; a wave takes
 // steps of two groups, the next step's codes in flight while it multiplies the current one.
 //   scores   S^T = K q^T per 16-frame tile (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets
-//            row n of frames 4 kg .. + 3
+//            row n of frames 4 kg .. + 3.  The queries' smallest terms first, so that two of
+//            the six roundings are to the score's own size (one row of 131,072 frames whose
+//            scores reach 15: off by 4.4e-7 in the 2-norm, largest first 1.7e-6)
 //   softmax  running maximum and sum per row, one rescaling per step; the difference to the
 //            maximum first, then powers of two: right at any magnitude of the scores
 //   values   O^T = V^T P^T per group: two lane swaps turn the group's two score tiles into
@@ -253,14 +255,15 @@ void kv4_unpack(const Kv4UnpackArgs& a, hipStream_t st) {
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for
 //            the merge kernel
 
-// bf16 terms of a query value (fp32: exact) and of a probability (fp32 output: exact;
-// bf16 output: 2^-16 relative, against the output's own 2^-9).  A decoder step's operands
-// hold an fp32 value to 2^-16 themselves: two terms of each.
+// bf16 terms of a query value and of a probability: as many as hold it exactly (an fp32 query three, a bf16 one one,
+// a probability three).  Two terms of a probability, 2^-17 of it, are a tenth faster with bf16 rows (16 x 5 rows of ragged
+// memories 10.7 us against 11.7) and round 0.24% of the bf16 outputs to the other side of 64 bits, three 0.017%, as sums
+// in 32 bits do.  A decoder step's operands hold an fp32 value to 2^-17 themselves: two terms of each.
 enum { KV4_ROWS = 0, KV4_OPERAND = 1, KV4_RECORDS = 2 };
 template <typename T, int OUT>
 struct Terms {
   static constexpr int q = sizeof(T) == 2 ? 1 : OUT == KV4_ROWS ? 3 : 2;
-  static constexpr int p = sizeof(T) == 2 || OUT != KV4_ROWS ? 2 : 3;
+  static constexpr int p = OUT == KV4_ROWS ? 3 : 2;
 };
 // Eight values as N bf16 terms.
 template <int N>
@@ -272,11 +275,8 @@ __device__ __forceinline__ void split_terms(const float* v, bf16x8 (&t)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) t[i] = __builtin_bit_cast(bf16x8, u[i]);
 }
-template <int N>
-__device__ __forceinline__ floatx4 mfma_terms(bf16x8 x, const bf16x8 (&t)[N], floatx4 acc) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, t[i], acc, 0, 0, 0);
-  return acc;
+__device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ float swap_max(float v) {
   const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -328,8 +328,11 @@ __device__ __forceinline__ void kv_step(KvStep<KS>& c, int g, int len, const bf1
   for (int t = 0; t < 2 * KS; ++t) {
     const int u = t >> 1;
     const float sc = scale_f(t & 1 ? c.ks[u] >> 8 : c.ks[u] & 255);
-    s[t] = mfma_terms<QT>(values8(t & 1 ? c.k[u].w : c.k[u].y, sc), qt[1],
-                          mfma_terms<QT>(values8(t & 1 ? c.k[u].z : c.k[u].x, sc), qt[0], floatx4{0.f, 0.f, 0.f, 0.f}));
+    const bf16x8 k0 = values8(t & 1 ? c.k[u].z : c.k[u].x, sc), k1 = values8(t & 1 ? c.k[u].w : c.k[u].y, sc);
+    s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = QT - 1; i >= 0; --i)
+      s[t] = mfma16(k1, qt[1][i], mfma16(k0, qt[0][i], s[t]));
   }
   if ((g + KS) * kKv4Frames > len) {  // uniform: the last step
 #pragma unroll
@@ -380,8 +383,11 @@ __device__ __forceinline__ void kv_step(KvStep<KS>& c, int g, int len, const bf1
     split_terms<PT>(pb, pt);
     const uint32_t vw[4] = {c.v[u].x, c.v[u].y, c.v[u].z, c.v[u].w};
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-      st.o[dt] = mfma_terms<PT>(values8(vw[dt], scale_f(c.vs[u] >> (8 * dt) & 255)), pt, st.o[dt]);
+    for (int dt = 0; dt < 4; ++dt) {
+      const bf16x8 x = values8(vw[dt], scale_f(c.vs[u] >> (8 * dt) & 255));
+#pragma unroll
+      for (int i = PT - 1; i >= 0; --i) st.o[dt] = mfma16(x, pt[i], st.o[dt]);
+    }
   }
 }
 
@@ -401,9 +407,9 @@ __device__ __forceinline__ void q_load(const Kv4AttendArgs& a, int r, int row, i
   for (int j = 0; j < 16; ++j) x[j] = row < a.rows ? 0.125f * x[j] : 0.f;
 }
 
-// Waves a block and groups a step.  us per launch (fp32, 20 heads; 1 x 9 rows, 96 x 9 rows of 1,500 frames, one
-// row of 131,072; 16 x 5 rows in bf16): 8 waves of 2: 8.5, 52, 43, 10.7; of 1: 8.9, 52, 43, 10.6; of 3: 8.5, 73, 49,
-// 11.4; 4 waves of 2: 9.3, 52, 45, 11.4; 16 of 2: 8.9, 77, 53, 11.5.
+// Waves a block and groups a step.  us a replayed call (20 heads; fp32 1 x 9 rows, 96 x 9 rows of 1,500 frames, one row of
+// 131,072; bf16 16 x 5 rows of ragged memories): 8 waves of 2: 8.5, 50, 39.7, 11.7; of 1: 6.9, 50, 40.3, 13.1; of 3: 8.7,
+// 61, 50, 11.2; 4 waves of 2: 7.0, 50, 41.3, 12.5; 16 of 2: 8.8, 67, 53, 11.9.
 constexpr int kAttWaves = 8, kAttStep = 2;
 constexpr int kKv4Record = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
 

@@ -441,6 +441,76 @@ def test_attend_scores_of_any_magnitude(F, size):
         assert (np.abs(got - want) <= 600 * 2.0 ** -24 * np.abs(held[1]).max() + 2 * half * np.abs(want)).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attend_probabilities_are_exact_in_the_products(dtype):
+    """Two frames of scores d and 0 and of values 6 and -6: 6 (1 - p) / (1 + p) with p = exp(-d), which for a small d is
+    what the last bits of p leave.  p is off by 2^-23 (its exponential, an ulp, and the rounding of d log2(e)), the result by
+    3 times that, and by at most six roundings to 2^-24 of 6 (three terms' sums, the sum of both, its inverse, the product):
+    under 2^-18, then half a step of the type.  (Two bf16 terms leave up to 2^-17 of p: 2^-15.4.)"""
+    wf = lib()
+    d = 2.0 ** torch.arange(-13, 1, 0.125, dtype=torch.float64)
+    q = torch.zeros((1, len(d), 1, 64), device="cuda", dtype=dtype)
+    q[0, :, 0, 0] = (8 * d).to(q)
+    k, v = torch.zeros((1, 2, 1, 64), device="cuda"), torch.full((1, 2, 1, 64), 6.0, device="cuda")
+    k[0, 0, 0, 0] = 1
+    v[0, 1] = -6
+    cache = wf.AcousticCache4(1, 1, 2)
+    cache.store(0, k, v)
+    p = np.exp(-num(q)[0, :, 0, :1] / 8)
+    want, got = 6 * (1 - p) / (1 + p), num(cache.attend(0, q))[0, :, 0]
+    half = torch.finfo(dtype).eps / 2
+    assert (np.abs(got - want) <= 2.0 ** -18 + half * want).all(), (np.abs(got - want) / (2.0 ** -18 + half * want)).max()
+
+
+def pair_errors(cache, q, k, v, F):
+    """2-norm of each (request, head) pair's error over its result's, and the largest sum of |q k| / 8 of its rows."""
+    qn, got = num(q), num(cache.attend(0, q))
+    want = plain.attend(qn, k, v, [F] * len(qn))
+    off = np.linalg.norm(got - want, axis=(1, 3)) / np.linalg.norm(want, axis=(1, 3))
+    mass = np.array([[(np.abs(qn[r, :, h]) @ np.abs(k[r, :, h]).T).max() / 8 for h in range(q.shape[2])] for r in range(len(qn))])
+    return off, mass
+
+
+@pytest.mark.parametrize("F,rows,size", [(4000, 1, 3), (1500, 9, 1), (600, 3, 8), (20000, 1, 2)])
+def test_attend_fp32_every_pair(F, rows, size):
+    """Every (request, head) pair by its own scores.  Products of query terms and codes are exact and the smaller terms'
+    sums come first, so a score is off by the two sums of its largest terms, half a step each: in the 2-norm 2^-24 * 0.4 of
+    a partial sum, which for the frames that carry the weight is up to half of mass: sqrt(2) * 0.4 * 2^-25 * mass, under
+    2^-25 * mass; the probability by as much, and 2^-21 for its exponential and the sums over the frames.  (With the largest
+    terms first, all six sums are of that size, and more is lost: 0.46 to 0.61 of 2^-24 * mass on average.)"""
+    wf = lib()
+    n, H = 6, 8
+    g = torch.Generator("cuda").manual_seed(F)
+    width = torch.exp(0.7 * torch.randn((2, H, 64), device="cuda", generator=g))
+    k, v = [torch.randn((n, F, H, 64), device="cuda", generator=g) * w for w in width]
+    cache = wf.AcousticCache4(n, H, F)
+    cache.store(0, k, v)
+    held = [num(x) for x in cache.load(0, n)]
+    q = size * torch.randn((n, rows, H, 64), device="cuda", generator=g)
+    off, mass = pair_errors(cache, q, *held, F)
+    assert (off <= 2.0 ** -25 * mass + 2.0 ** -21).all(), ((off / (2.0 ** -25 * mass + 2.0 ** -21)).max(), mass.max())
+
+
+@pytest.mark.parametrize("F", [130, 5000])
+def test_attend_fp32_exact_scores_forty_times_as_large(F):
+    """Queries of one dim, keys of a few steps there: scores are exact at any size, so what is left is the exponential's
+    difference times log2(e), half a step of up to 2^-23 * 16 (beyond 16 a weight is under 2^-23), and 2^-21 for the
+    exponential and the sums."""
+    wf = lib()
+    n, H = 3, 4
+    g = torch.Generator("cuda").manual_seed(F)
+    k = torch.zeros((n, F, H, 64), device="cuda")
+    k[..., 5] = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], device="cuda")[torch.randint(0, 8, (n, F, H), device="cuda", generator=g)]
+    v = torch.randn((n, F, H, 64), device="cuda", generator=g)
+    cache = wf.AcousticCache4(n, H, F)
+    cache.store(0, k, v)
+    held = [num(x) for x in cache.load(0, n)]
+    q = torch.zeros((n, 5, H, 64), device="cuda")
+    q[..., 5] = 40 * torch.randn((n, 5, H), device="cuda", generator=g).bfloat16()   # times a code: 10 bits
+    off, _ = pair_errors(cache, q, *held, F)
+    assert (off <= 2.0 ** -20 + 2.0 ** -21).all(), off.max()
+
+
 def test_attend_strides_and_large_scores():
     """Rows as beams of a slot-major buffer, one row for all requests, bases off 16 bytes; scores of a few hundred."""
     wf = lib()

@@ -152,11 +152,12 @@ __global__ void __launch_bounds__(256) k_beam_rows(BeamSelectArgs a) {
     if (lane % (256 / KL) == 0) gm[t / (256 / KL)] = g;
   }
   // sum of exponentials relative to the lane's maximum, eight at a time in 32 bits, then 64.  Powers of two, m log2(e)
-  // rounded once and what that took put back on the sum; huge logits, whose product overflows, by difference
+  // rounded once and what that took put back on the sum.  It took up to half a step of m log2(e), a quarter at 2^22 and
+  // at 1e10 more powers of two than there are, so larger logits go by difference
   constexpr float log2e = 1.44269504088896f;
   const float base = m == -INFINITY ? 0.f : m;
   double sum = 0;
-  if (__ballot(fabsf(base) > 1e30f) == 0) {
+  if (__ballot(fabsf(base) > 0x1p22f) == 0) {
     const float mc = base * log2e, took = fmaf(base, log2e, -mc);
 #pragma unroll
     for (int i = 0; i < R; i += 8) {

@@ -114,6 +114,41 @@ def test_select_peaked_and_far_logits():
     check_select(logits, torch.tensor([[-3.0, -3.25], [-100, -99]], device="cuda"), 4)
 
 
+HUGE = [1e6, 4.19e6, 4.2e6, 1e9, 3e9, 5e9, 1e10, 1e11, 1e12, 1e20, 9e29, 1e30, 3e38]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size", HUGE)
+def test_select_runs_of_huge_logits(size, dtype):
+    """Columns masked with a large negative value beside ordinary ones: a wave's lanes that hold nothing else, a whole wave
+    (2,048 columns), the last, partial one; a single lane (8 columns); and suppressed places with the value of either sign."""
+    g = torch.Generator("cuda").manual_seed(9)
+    V = 51866
+    logits = (3 * torch.randn((3, 2, V), device="cuda", generator=g)).to(dtype)
+    logits[0, 0, 50365:] = -size
+    logits[0, 1, 4096:6144] = -size
+    logits[1, 0, 16:24] = -size
+    logits[1, 1, 100:] = -size
+    sup = torch.zeros(V, dtype=torch.uint8, device="cuda")
+    scores = torch.tensor([[-1.0, -2], [-1.5, -1], [0, -3]], device="cuda")
+    check_select(logits, scores, 10)
+    sup[30000:40000] = 1
+    logits[2, 0, 30000:35000], logits[2, 1, 30000:40000] = size, -size
+    check_select(logits, scores, 10, sup)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("size", HUGE)
+def test_select_rows_of_huge_logits(size, sign):
+    """Whole rows about one large value: equal ones, and ones a few of its steps apart."""
+    g = torch.Generator("cuda").manual_seed(10)
+    logits = torch.full((2, 3, 9000), sign * size, device="cuda")
+    logits[:, 1, 1234] += size * 2.0 ** -20     # by itself a logit of over 30 above the rest, or next to them
+    logits[:, 2] *= 1 - 2.0 ** -24 * torch.randint(0, 3, (2, 9000), device="cuda", generator=g)
+    check_select(logits, torch.tensor([[0.0, -1, -2], [-7, -INF, -7]], device="cuda"), 6)
+    check_select(logits.bfloat16(), torch.zeros((2, 3), device="cuda"), 6)
+
+
 # ---------------------------------------------------------------- page tables
 
 def search_tables(rng, n, B, P, page_tokens, lens):

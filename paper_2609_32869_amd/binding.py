@@ -172,6 +172,24 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+def _refuse(what):
+    raise WfError(f"invalid argument (-1): {what}")
+
+
+def _tensor(t, name, dtype, shape, device):
+    """Refuse what is not a contiguous GPU tensor of this type, shape and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor):
+            _refuse(f"{name} must be a tensor")
+        if t.dtype != dtype:
+            _refuse(f"{name} must be {str(dtype)[6:]}, not {str(t.dtype)[6:]}")
+        if t.shape != shape:
+            _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        if t.device != device:
+            _refuse(f"{name} must be on {device}, not {t.device}")
+        _refuse(f"{name} must be contiguous")
+
+
 def to_device_storage(arr, dtype, device="cuda"):
     """Host fp32 array -> device tensor in the storage type (bf16 values must be exact)."""
     a = np.ascontiguousarray(arr, dtype=np.float32)
@@ -284,9 +302,9 @@ class WhisperFlash:
 
     # ---- beam search (beam b of request r is slot slot0 + b * n + r)
     def beam_begin(self, slot0, beams, last_tokens, max_new, length_penalty=1.0, stream=None):
-        """last_tokens: device int32 [n], the last prompt token of each prefilled leader; max_new: sequence of ints."""
+        """last_tokens: device int32 [n], the last prompt token of each prefilled leader; max_new: n ints."""
         if last_tokens.dtype != torch.int32 or last_tokens.dim() != 1 or not last_tokens.is_contiguous() or not last_tokens.is_cuda:
-            raise WfError("invalid argument (-1): last_tokens must be a contiguous int32 [n] on the GPU")
+            _refuse("last_tokens must be a contiguous int32 [n] on the GPU")
         n = last_tokens.shape[0]
         nbytes = ctypes.c_size_t()
         self._check(self.lib.wf_beam_bytes(self.h, n, beams, ctypes.byref(nbytes)))
@@ -299,6 +317,9 @@ class WhisperFlash:
 
     def beam_step(self, slot0, done=None, use_graph=False, stream=None):
         """One token more for every unfinished request; done: device int32 [n] to write, or None."""
+        if done is not None and slot0 in self.searches:
+            n, _, ws = self.searches[slot0]
+            _tensor(done, "done", torch.int32, (n,), ws.device)
         self._check(self.lib.wf_beam_step(self.h, slot0, _ptr(done), 1 if use_graph else 0, _stream(stream)))
         return done
 

@@ -16,7 +16,7 @@ import torch
 # torch.cuda.current_stream() and current_device() without their objects and checks (2.7 and 0.1 us)
 from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _device
 
-from .binding import WF_BF16, WF_F32, WfError, WfKv4, load_library
+from .binding import WF_BF16, WF_F32, WfError, WfKv4, _refuse, _tensor, load_library
 
 _DTYPES = {torch.float32: WF_F32, torch.bfloat16: WF_BF16}
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
@@ -29,25 +29,7 @@ def _check(rc):
         raise WfError(f"{lib.wf_strerror(rc).decode()} ({rc}): {msg.decode() if msg else ''}")
 
 
-def _refuse(what):
-    raise WfError(f"invalid argument (-1): {what}")
-
-
 _INTS = 2 ** 31  # sizes from here on would be cut off by the C entries' 32 bits; smaller ones are the library's to check
-
-
-def _tensor(t, name, dtype, shape, device):
-    """Refuse what is not a contiguous GPU tensor of this type, shape and device."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        if not isinstance(t, torch.Tensor):
-            _refuse(f"{name} must be a tensor")
-        if t.dtype != dtype:
-            _refuse(f"{name} must be {str(dtype)[6:]}, not {str(t.dtype)[6:]}")
-        if t.shape != shape:
-            _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-        if t.device != device:
-            _refuse(f"{name} must be on {device}, not {t.device}")
-        _refuse(f"{name} must be contiguous")
 
 
 def _gpu(t, name, dims):

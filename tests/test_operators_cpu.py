@@ -126,6 +126,31 @@ def test_binding_refuses_sizes_past_32_bits():
             wf.AcousticCache4(*sizes)
 
 
+class Search:
+    """A handle's beam calls without a library: which were made."""
+
+    def __new__(cls, n=2, beams=3):
+        from paper_2609_32869_amd import WhisperFlash
+        eng = WhisperFlash.__new__(WhisperFlash)
+        eng.searches, eng.made = {4: (n, beams, torch.empty(8, dtype=torch.uint8))}, []
+        eng.lib = type("Lib", (), {"wf_beam_step": lambda *a: eng.made.append("step") or 0})()
+        eng.h = None
+        return eng
+
+
+def test_beam_step_refuses_what_it_cannot_write_done_to():
+    """n whole int32 of the handle's device: anything else would be written past its end."""
+    import paper_2609_32869_amd as wf
+    eng = Search()
+    good = torch.zeros(2, dtype=torch.int32)
+    for done, what in ((good.bool(), "int32"), (good.to(torch.uint8), "int32"), (good.long(), "int32"), (good[:1], "shape"),
+                       (torch.zeros(3, dtype=torch.int32), "shape"), (good[None], "shape"), ([0, 0], "tensor"),
+                       (torch.zeros(4, dtype=torch.int32)[::2], "contiguous"), (good.to("meta"), "on cpu")):
+        with pytest.raises(wf.WfError, match=what):
+            eng.beam_step(4, done)
+    assert eng.made == []
+
+
 def test_beam_calls_on_a_null_handle():
     binding, lib = _lib()
     n = ctypes.c_size_t()

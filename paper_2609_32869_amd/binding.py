@@ -306,11 +306,14 @@ class WhisperFlash:
         if last_tokens.dtype != torch.int32 or last_tokens.dim() != 1 or not last_tokens.is_contiguous() or not last_tokens.is_cuda:
             _refuse("last_tokens must be a contiguous int32 [n] on the GPU")
         n = last_tokens.shape[0]
+        max_new = [int(x) for x in max_new]
+        if len(max_new) != n:
+            _refuse(f"max_new must hold {n} numbers, not {len(max_new)}")
         nbytes = ctypes.c_size_t()
         self._check(self.lib.wf_beam_bytes(self.h, n, beams, ctypes.byref(nbytes)))
         with _on(stream):  # memory of the search's stream
             ws = torch.empty(nbytes.value, dtype=torch.uint8, device="cuda")
-        M = (ctypes.c_int32 * n)(*[int(x) for x in max_new])
+        M = (ctypes.c_int32 * n)(*max_new)
         self._check(self.lib.wf_beam_begin(self.h, slot0, n, beams, _ptr(last_tokens), M, float(length_penalty), _ptr(ws),
                                            nbytes.value, _stream(stream)))
         self.searches[slot0] = (n, beams, ws)

@@ -151,6 +151,14 @@ def test_beam_step_refuses_what_it_cannot_write_done_to():
     assert eng.made == []
 
 
+def test_beam_begin_takes_one_budget_a_request():
+    import paper_2609_32869_amd as wf
+    last = type("T", (), {"dtype": torch.int32, "dim": lambda s: 1, "is_contiguous": lambda s: True, "is_cuda": True, "shape": (2,)})()
+    for budget in ([5], [5, 5, 5], []):
+        with pytest.raises(wf.WfError, match="max_new"):
+            Search().beam_begin(0, 3, last, budget)
+
+
 def test_beam_calls_on_a_null_handle():
     binding, lib = _lib()
     n = ctypes.c_size_t()

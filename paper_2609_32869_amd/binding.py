@@ -351,14 +351,15 @@ class WhisperFlash:
         self.prefill(slot0, tokens, lens, max_new)
         last = tokens.gather(1, torch.tensor([[int(x) - 1] for x in lens], device=tokens.device)).view(n).contiguous()
         self.beam_begin(slot0, beams, last, max_new, length_penalty)
-        done = torch.zeros(n, dtype=torch.int32, device="cuda")
         try:
+            done = torch.zeros(n, dtype=torch.int32, device="cuda")
             for step in range(self.cfg.n_ctx):
                 self.beam_step(slot0, done, use_graph)
                 if step % poll == poll - 1 and bool(done.all()):
                     break
-        except WfError:
-            self.beam_end(slot0)  # the slots are given back
+        except BaseException:
+            with contextlib.suppress(Exception):
+                self.beam_end(slot0)  # the slots are given back
             raise
         return self.beam_end(slot0)
 

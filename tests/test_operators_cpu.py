@@ -159,6 +159,28 @@ def test_beam_begin_takes_one_budget_a_request():
             Search().beam_begin(0, 3, last, budget)
 
 
+@pytest.mark.parametrize("error", [RuntimeError, KeyboardInterrupt, MemoryError])
+def test_beam_search_gives_the_slots_back_on_any_error(error):
+    from paper_2609_32869_amd import WhisperFlash
+    eng = Search()
+    ended = []
+
+    def step(*a, **k):
+        raise error("in the middle")
+    eng.prefill = lambda *a, **k: None
+    eng.beam_begin = lambda *a, **k: None
+    eng.beam_step = step
+    eng.beam_end = lambda slot0: ended.append(slot0) or (_ for _ in ()).throw(RuntimeError("and so does this"))
+    eng.cfg = type("Cfg", (), {"n_ctx": 9})()
+    zeros, torch.zeros = torch.zeros, lambda *a, **k: torch.ones(1)
+    try:
+        with pytest.raises(error, match="in the middle"):
+            WhisperFlash.beam_search(eng, 4, torch.ones((1, 3), dtype=torch.int32), [3], [5], 2)
+    finally:
+        torch.zeros = zeros
+    assert ended == [4]
+
+
 def test_beam_calls_on_a_null_handle():
     binding, lib = _lib()
     n = ctypes.c_size_t()

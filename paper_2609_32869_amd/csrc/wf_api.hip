@@ -11,6 +11,7 @@
 #include <new>
 #include <vector>
 
+#include "wf_capture.h"
 #include "wf_internal.h"
 
 using namespace wf;
@@ -1302,29 +1303,37 @@ int dispatch(Handle* h, hipStream_t st, Fn&& fn) {
   return WF_OK;
 }
 
+struct HipGraphs {
+  using Error = hipError_t;
+  using Stream = hipStream_t;
+  using Graph = hipGraph_t;
+  using Exec = hipGraphExec_t;
+  static constexpr Error ok = hipSuccess;
+  static Error begin(Stream st) { return hipStreamBeginCapture(st, hipStreamCaptureModeThreadLocal); }
+  static Error end(Stream st, Graph* g) { return hipStreamEndCapture(st, g); }
+  static Error instantiate(Exec* x, Graph g) { return hipGraphInstantiate(x, g, nullptr, nullptr, 0); }
+  static void destroy(Graph g) { (void)hipGraphDestroy(g); }
+  static void destroy_exec(Exec x) { (void)hipGraphExecDestroy(x); }
+};
+
 // Replay the graph of `key`, captured from enqueue() on first use.
 template <typename F>
 int replay(Handle* h, const GraphKey& key, hipStream_t st, F&& enqueue) {
   if (!st) return fail(h, WF_EINVAL, "graph replay needs a non-null stream");
   auto it = h->graphs.find(key);
   if (it == h->graphs.end()) {
+    auto failed = [&](const char* call, hipError_t e) { return fail(h, WF_EHIP, std::string(call) + ": " + hipGetErrorString(e)); };
     h->cap_recs.clear();
-    HIPCK(h, hipStreamBeginCapture(st, hipStreamCaptureModeThreadLocal));
-    h->capturing = true;
-    int r = enqueue();
-    h->capturing = false;
-    hipGraph_t g = nullptr;
-    hipError_t e = hipStreamEndCapture(st, &g);
-    auto drop_recs = [&] { h->cap_recs.clear(); };
-    if (r) { if (g) (void)hipGraphDestroy(g); drop_recs(); return r; }
-    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipStreamEndCapture: ") + hipGetErrorString(e)); }
-    hipGraphExec_t ex = nullptr;
-    e = hipGraphInstantiate(&ex, g, nullptr, nullptr, 0);
-    (void)hipGraphDestroy(g);
-    if (e != hipSuccess) { drop_recs(); return fail(h, WF_EHIP, std::string("hipGraphInstantiate: ") + hipGetErrorString(e)); }
-    it = h->graphs.emplace(key, ex).first;
+    Capture<HipGraphs> cap(st, h->capturing);
+    if (hipError_t e = cap.begin()) return failed("hipStreamBeginCapture", e);
+    const int r = enqueue();
+    const hipError_t e = cap.end();
+    if (r) return r;
+    if (e != hipSuccess) return failed("hipStreamEndCapture", e);
+    if (hipError_t e1 = cap.instantiate()) return failed("hipGraphInstantiate", e1);
     if (key.prof) h->graph_recs[key] = h->cap_recs;
-    h->cap_recs.clear();
+    it = h->graphs.emplace(key, cap.exec()).first;
+    cap.release();
   }
   HIPCK(h, hipGraphLaunch(it->second, st));
   if (key.prof) {  // profiled replay: read this replay's launch durations now

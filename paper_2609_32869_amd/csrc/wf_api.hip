@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "wf_capture.h"
+#include "wf_guard.h"
 #include "wf_internal.h"
 
 using namespace wf;
@@ -1719,23 +1720,20 @@ static int beam_finish(Handle* h, int slot0, int32_t* tokens, int len_max, int32
   return WF_OK;
 }
 
-// No exception leaves a C entry (the host's records of a search, of a graph or of a message may fail to allocate).
-#define WF_GUARDED(call)                       \
-  try {                                        \
-    return call;                               \
-  } catch (...) {                              \
-    return op_fail(WF_EINVAL, "out of host memory"); \
-  }
-int wf_beam_begin(wf_handle* h, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
+int wf_beam_begin(wf_handle* hh, int slot0, int n, int beams, const int32_t* last_tokens, const int32_t* max_new,
                   float length_penalty, void* workspace, size_t ws_bytes, void* stream) {
-  WF_GUARDED(beam_start(reinterpret_cast<Handle*>(h), slot0, n, beams, last_tokens, max_new, length_penalty, workspace, ws_bytes,
-                        stream))
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  return guarded(h, g_err, WF_EINVAL, [&] {
+    return beam_start(h, slot0, n, beams, last_tokens, max_new, length_penalty, workspace, ws_bytes, stream);
+  });
 }
-int wf_beam_step(wf_handle* h, int slot0, int32_t* done, int use_graph, void* stream) {
-  WF_GUARDED(beam_extend(reinterpret_cast<Handle*>(h), slot0, done, use_graph, stream))
+int wf_beam_step(wf_handle* hh, int slot0, int32_t* done, int use_graph, void* stream) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  return guarded(h, g_err, WF_EINVAL, [&] { return beam_extend(h, slot0, done, use_graph, stream); });
 }
-int wf_beam_end(wf_handle* h, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
-  WF_GUARDED(beam_finish(reinterpret_cast<Handle*>(h), slot0, tokens, len_max, lens, scores, stream))
+int wf_beam_end(wf_handle* hh, int slot0, int32_t* tokens, int len_max, int32_t* lens, float* scores, void* stream) {
+  Handle* h = reinterpret_cast<Handle*>(hh);
+  return guarded(h, g_err, WF_EINVAL, [&] { return beam_finish(h, slot0, tokens, len_max, lens, scores, stream); });
 }
 
 int wf_debug_ptr(wf_handle* hh, int which, void** ptr) {

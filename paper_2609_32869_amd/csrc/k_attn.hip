@@ -1555,10 +1555,7 @@ void Ops<S>::attn_cross(const CrossArgs& a, int n, hipStream_t st) {
   }
 }
 
-void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st) {
-  if (a.op.w != nullptr) launch_merge<bf16, true>(a, n, st);
-  else launch_merge<bf16, false>(a, n, st);
-}
+void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st) { launch_merge<bf16, true>(a, n, st); }
 
 template void Ops<float>::attn_self(const AttnArgs&, int, hipStream_t);
 template void Ops<bf16>::attn_self(const AttnArgs&, int, hipStream_t);

@@ -212,7 +212,7 @@ inline void cross_chunks(int pairs, int n_frames, int& nchunk, int& chunk) {
   nchunk = (n_frames + ch - 1) / ch;
 }
 
-// Merge of the chunk records in a.part (with the fused output product if a.op is set).
+// Merge of the chunk records in a.part with the fused output product (a.op has to be set).
 void attn_cross_merge(const CrossArgs& a, int n, hipStream_t st);
 
 struct LnArgs {

@@ -13,10 +13,15 @@ import functools
 
 import torch
 
-# torch.cuda.current_stream() and current_device() without their objects and checks (2.7 and 0.1 us)
-from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _device
-
 from .binding import WF_BF16, WF_F32, WfError, WfKv4, _refuse, _tensor, load_library
+
+try:  # torch.cuda.current_stream() and current_device() without their objects and checks (2.7 and 0.1 us)
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _device
+except ImportError:  # a PyTorch without these names
+    from torch.cuda import current_device as _device
+
+    def _raw_stream(index):
+        return torch.cuda.current_stream(index).cuda_stream
 
 _DTYPES = {torch.float32: WF_F32, torch.bfloat16: WF_BF16}
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8

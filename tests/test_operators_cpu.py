@@ -3,6 +3,8 @@ anything is enqueued (the pointers here point at nothing), workspace sizes, and 
 import ctypes
 import itertools
 import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -112,6 +114,19 @@ def test_binding_refuses_tensors_of_another_kind():
     i = torch.zeros((1, 2, 4), dtype=torch.int32)
     with pytest.raises(wf.WfError, match="on the GPU"):
         wf.cache_reorder(torch.zeros((1, 8, 16)), i, i[0, :1], i[0, 0, :1], i[0])
+
+
+def test_import_without_private_names_of_torch():
+    """The package imports where PyTorch lacks the shortcuts, and takes the stream and device by the public calls."""
+    code = ("import torch\n"
+            "for name in ('_cuda_getCurrentRawStream', '_cuda_getDevice'):\n"
+            "    if hasattr(torch._C, name): delattr(torch._C, name)\n"
+            "import paper_2609_32869_amd as wf\n"
+            "from paper_2609_32869_amd import operators\n"
+            "torch.cuda.current_stream = lambda index: type('S', (), {'cuda_stream': 70 + index})()\n"
+            "assert operators._raw_stream(3) == 73 and operators._device is torch.cuda.current_device\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=300)
 
 
 def test_binding_refuses_sizes_past_32_bits():

@@ -107,6 +107,52 @@ def test_other_widths(monkeypatch, d_model, batch, frames):
     ls.close()
 
 
+# width, target blocks, frames, rows of the tile that the target's product takes (the drafter's two blocks may take another)
+TILES = [(128, 2, 77, 64), (512, 2, 1500, 64), (384, 6, 1500, 128), (768, 12, 700, 128), (512, 12, 1500, 256), (128, 12, 1497, 256),
+         (256, 24, 257, 256), (1280, 2, 1500, 256), (384, 24, 300, 64)]
+
+
+def raw(eng, layer, slot, nbytes):
+    """A block's and slot's acoustic keys and values as the handle holds them."""
+    import ctypes
+    base = ctypes.c_void_p()
+    assert eng.lib.wf_debug_ptr(eng.h, 4, ctypes.byref(base)) == 0
+    at = base.value - eng.ws.data_ptr() + (layer * eng.max_batch + slot) * nbytes
+    return eng.ws[at:at + nbytes]
+
+
+@pytest.mark.parametrize("d,layers,frames,tile", TILES)
+def test_codes_and_scales_of_every_tile(d, layers, frames, tile):
+    """The request-time product's own rounding against the store's: a bf16 handle's keys and values put into a 4-bit cache
+    give the 4-bit handle's bytes, every one.  Each tile adds its products in the order of k, so that both handles round the
+    same sums, also where they take different tiles."""
+    from paper_2609_32869_amd import AcousticCache4
+    H = d // 64
+    cfg = SMALL.with_(name=f"kv4-tile-{d}-{layers}", n_layer=layers, d_model=d, n_head=H, d_ff=2 * d, n_frames=frames)
+    W = make_weights(cfg)
+    arrays = [W.values[n] for n, _ in W.order]
+    mem = torch.stack([lockstep.to_device_storage(make_memory(cfg, i), "bf16") for i in range(2)])
+    mem[1, frames // 2:] *= 50      # scales far apart
+    wide, four = (lockstep.WhisperFlash.from_host(cfg, 2, arrays, acoustic_bits=bits) for bits in (16, 4))
+    for eng in (wide, four):
+        eng.encode_memory_set(0, mem)
+    torch.cuda.synchronize()
+    vt = -(-frames // 512) * 512
+    cache = AcousticCache4(1, H, frames)
+    for slot in range(2):
+        for layer in range(layers + cfg.n_draft_layer):
+            x = raw(wide, layer, slot, 2 * d * (frames + vt)).view(torch.bfloat16)
+            k = x[:frames * d].view(1, H, frames, 64).transpose(1, 2)
+            v = x[frames * d:].view(H, vt // 256, 64, 256).permute(1, 3, 0, 2).reshape(1, vt, H, 64)[:, :frames]
+            assert k.isfinite().all() and k.abs().max() > 0 and v.abs().max() > 0
+            cache.store(0, k, v)
+            got = raw(four, layer, slot, cache.data.numel())
+            differ = (got != cache.data).view(-1, 2176)
+            assert not differ.any(), (layer, slot, differ.any(1).nonzero()[:4], differ.any(0).nonzero()[:4])
+    wide.close()
+    four.close()
+
+
 def test_graph_and_noalloc_steps_match():
     """The eager step, its graph and the step without allocation give the same logits to the order of their atomic
     adds (fp32 sums of 20 terms and fewer: 1e-4 of logits of order 1)."""

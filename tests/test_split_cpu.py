@@ -65,3 +65,12 @@ def test_tiles_of_large_v3(lib):
     assert [lib.tile(1536, n, 1) for n in (5120, 3840, 1280)] == [256, 256, 64]
     assert [lib.tile(6144, n, 1) for n in (5120, 3840, 1280)] == [256, 256, 256]
     assert lib.tile(1500, 1280, 4) == 128 and lib.tile(1536, 2560, 32) == 256
+
+
+def test_shapes_of_the_4_bit_rounding_take_every_tile(lib):
+    """The handles whose codes and scales are compared byte for byte take the tile that each names, all three among them."""
+    from test_gpu_kv4_handle import TILES
+    for d, layers, frames, tile in TILES:
+        assert lib.tile(frames, 2 * d, layers) == tile
+    assert {t for _, _, _, t in TILES} == {64, 128, 256}
+    assert lib.tile(1500, 2560, 32) == lib.tile(1500, 2560, 2) == 256    # large-v3's target and drafter

@@ -7,6 +7,9 @@ of the tensors' device) and returns without waiting; a given stream has to be or
 behind the work that fills the tensors.  Workspaces and results come from PyTorch's
 allocator for the call's stream, so concurrent calls and captured graphs each have their
 own.
+
+There are no backward passes.  Results of inputs that require gradients raise where a
+gradient is asked of them; what a cache stores or copies has no history.
 """
 import ctypes
 import functools
@@ -81,6 +84,33 @@ def _enqueue(device, stream, call, *tensors):
         return call(raw, empty)
 
 
+class _NoBackward(torch.autograd.Function):
+    """A result, as a function of the tensors that it came from."""
+
+    @staticmethod
+    def forward(ctx, name, result, *tensors):
+        ctx.name = name
+        return result.t
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise WfError(f"{ctx.name} has no backward pass")
+
+
+class _Held:
+    """Keeps a result out of the function's inputs: what it returns is the tensor itself."""
+
+    def __init__(self, t):
+        self.t = t
+
+
+def _without_backward(name, result, *tensors):
+    """`result`, a tensor of its own memory, which raises on backward() where one of `tensors` wants a gradient."""
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        return _NoBackward.apply(name, _Held(result), *tensors)
+    return result
+
+
 @functools.lru_cache(maxsize=256)
 def _select_bytes(n, beams, vocab, k):
     if max(n, beams, vocab, abs(k)) >= _INTS:
@@ -119,7 +149,11 @@ def beam_select(logits, scores, k, suppress=None, stream=None):
         return out
 
     score, beam, token = _enqueue(dev, stream, call, logits, scores, suppress).unbind()
-    return score.view(_F32), beam, token
+    score = score.view(_F32)
+    if logits.requires_grad or scores.requires_grad:  # not as a view, which autograd would not let change in place
+        own = torch.empty(0, dtype=_F32, device=dev).set_(score.untyped_storage(), score.storage_offset(), score.shape, score.stride())
+        score = _without_backward("beam_select", own, logits, scores)
+    return score, beam, token
 
 
 def cache_reorder(cache, tables, parents, lens, pool, page_tokens=16, stream=None):
@@ -251,4 +285,5 @@ class AcousticCache4:
                                           ws.data_ptr() if need else None, need, raw))
             return out
 
-        return _enqueue(self.device, stream, call, q, lens, self.data)
+        out = _enqueue(self.device, stream, call, q, lens, self.data)
+        return _without_backward("attend", out, q) if q.requires_grad else out

@@ -608,6 +608,32 @@ def test_attend_offsets_past_32_bits():
     check_attend(cache, entries - 2, q, *held, [F] * 2, None)
 
 
+def test_gradients_are_refused_not_lost():
+    """Inputs that require gradients give the same results, which raise on backward() also where another branch has one."""
+    wf = lib()
+    k, v = source(1, 40, 2, torch.float32, 30)
+    cache = wf.AcousticCache4(1, 2, 40)
+    cache.store(0, k, v)
+    g = torch.Generator("cuda").manual_seed(30)
+    q, x = torch.randn((1, 3, 2, 64), device="cuda", generator=g), torch.randn((1, 2, 50), device="cuda", generator=g)
+    s, w = torch.zeros((1, 2), device="cuda"), torch.ones((), device="cuda", requires_grad=True)
+    want, best = cache.attend(0, q), wf.beam_select(x, s, 4)
+    q, s, other = q.requires_grad_(), s.requires_grad_(), torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for stream in (None, other):
+        out = cache.attend(0, q, stream=stream)
+        got = wf.beam_select(x, s, 4, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out.detach(), want) and all(torch.equal(a.detach(), b) for a, b in zip(got, best))
+        assert not got[1].requires_grad and not got[2].requires_grad
+        got[0].add_(1)
+        for result, name in ((out, "attend"), (got[0], "beam_select")):
+            with pytest.raises(wf.WfError, match=f"{name} has no backward"):
+                (w * 2 + result.sum()).backward()
+    with torch.no_grad():
+        assert not cache.attend(0, q).requires_grad
+
+
 # ---------------------------------------------------------------- streams, graphs, several calls at once
 
 def one_of_each(seed, dtype=torch.float32):

@@ -116,6 +116,28 @@ def test_binding_refuses_tensors_of_another_kind():
         wf.cache_reorder(torch.zeros((1, 8, 16)), i, i[0, :1], i[0, 0, :1], i[0])
 
 
+def test_results_without_a_backward_pass():
+    """A result whose input requires a gradient is the same tensor, may be changed in place, and raises when a gradient is
+    asked of it; others, and all without autograd, are left alone."""
+    import paper_2609_32869_amd as wf
+    from paper_2609_32869_amd.operators import _without_backward
+    q, other = torch.ones(3, requires_grad=True), torch.ones(3, requires_grad=True)
+    for make in (lambda: torch.arange(3.0),
+                 lambda: torch.empty(0).set_(torch.arange(6.0).untyped_storage(), 0, (3,), (1,))):
+        out = make()
+        got = _without_backward("attend", out, q)
+        assert got.data_ptr() == out.data_ptr() and torch.equal(got.detach(), torch.arange(3.0))
+        got += 1
+        with pytest.raises(wf.WfError, match="attend has no backward pass"):
+            (got * other).sum().backward()
+        assert q.grad is None
+        plain_out = make()
+        assert _without_backward("attend", plain_out, q.detach()) is plain_out
+        with torch.no_grad():
+            assert _without_backward("attend", plain_out, q) is plain_out
+        assert not plain_out.requires_grad
+
+
 def test_import_without_private_names_of_torch():
     """The package imports where PyTorch lacks the shortcuts, and takes the stream and device by the public calls."""
     code = ("import torch\n"

@@ -381,8 +381,9 @@ const char* wf_encoder_last_error(wf_encoder* e);
  * host before anything is enqueued, work on the caller's stream (of the current
  * device, which holds every buffer), no device memory but the caller's, no host
  * synchronisation, so they may be captured into a HIP graph.  Messages of refused
- * calls: wf_last_error(NULL).  A workspace serves one call at a time.  What device
- * arrays hold is checked on the device, as each call states.
+ * calls: wf_last_error(NULL).  A workspace serves one call at a time; it and a call's
+ * outputs overlap none of the call's other arguments.  What device arrays hold is checked
+ * on the device, as each call states.
  */
 
 /*
@@ -419,7 +420,7 @@ int wf_beam_select(const void* logits, int dtype, int64_t req_stride, int64_t be
  * page, so that reading ahead stays inside the cache.
  * cache: device, 16-byte aligned: n_regions regions region_stride bytes apart (keys and
  *   values of every block), each of n_pages pages of page_bytes (multiples of 16).
- * tables, new_tables: device int32 [n, beams, max_pages], not the same memory.
+ * tables, new_tables: device int32 [n, beams, max_pages].
  * parents: device int32 [n, beams]; lens: device int32 [n], taken as the nearest of
  *   [0, max_pages * page_tokens].
  * pool: device int32 [n, pool_pages], distinct pages that belong to the request alone;

@@ -12,6 +12,11 @@ int bad(const char* msg) { return op_fail(WF_EINVAL, msg); }
 
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
 int launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? WF_OK : op_fail(WF_EHIP, hipGetErrorString(e));
@@ -117,9 +122,11 @@ int wf_cache_reorder(void* cache, int n_regions, size_t region_stride, int n_pag
   if (n_regions > 1 && region_stride / page_bytes < (size_t)n_pages) return bad("regions overlap");
   if (!aligned(tables, 4) || !aligned(new_tables, 4) || !aligned(parents, 4) || !aligned(lens, 4) || !aligned(pool, 4))
     return bad("a tensor must be aligned to its elements");
-  const size_t tb = (size_t)n * beams * max_pages * 4;
-  const uintptr_t t0 = reinterpret_cast<uintptr_t>(tables), t1 = reinterpret_cast<uintptr_t>(new_tables);
-  if (t0 < t1 + tb && t1 < t0 + tb) return bad("tables and new_tables must not share memory");
+  // every block reads all of these, and the first one of a request writes its new tables
+  const size_t nb = (size_t)n * beams, tb = nb * max_pages * 4;
+  if (overlap(new_tables, tb, tables, tb) || overlap(new_tables, tb, parents, nb * 4) || overlap(new_tables, tb, lens, (size_t)n * 4) ||
+      overlap(new_tables, tb, pool, (size_t)n * pool_pages * 4))
+    return bad("new_tables must not share memory with another argument");
   ReorderArgs a{};
   a.cache = static_cast<char*>(cache);
   a.regions = n_regions;

@@ -65,6 +65,23 @@ def test_reorder_refusals():
         "tokens": [(0, -1)], "parents": [(None, -1)], "lens": [(None, -1)], "pool": [(None, -1)], "pool_pages": [(0, -1)]})
 
 
+def test_reorder_refuses_new_tables_over_what_it_reads():
+    """Sizes 3 x 4 x 5 tables: 240 bytes; parents 48, lens 12, pool 3 x 20 words."""
+    binding, lib = _lib()
+    new = P + (1 << 16)
+    far = dict(tables=P, parents=P + 4096, lens=P + 8192, pool=P + 12288)
+    size = dict(tables=240, parents=48, lens=12, pool=240)
+
+    def call(a, tokens=16):
+        return lib.wf_cache_reorder(P << 4, 2, 1 << 20, 64, 1024, a["tables"], new, 3, 4, 5, tokens, a["parents"], a["lens"], a["pool"],
+                                    20, None)
+    for name in far:
+        for at in (new - size[name] + 4, new, new + 236):
+            assert call(dict(far, **{name: at})) == -1 and b"share memory" in lib.wf_last_error(None), (name, at)
+        for at in (new - size[name], new + 240):      # side by side: refused for another reason, a bad page size, alone
+            assert call(dict(far, **{name: at}), 0) == -1 and b"page_tokens" in lib.wf_last_error(None), (name, at)
+
+
 def test_cache4_refusals():
     binding, lib = _lib()
 

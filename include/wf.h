@@ -470,7 +470,7 @@ int wf_kv4_load(const wf_kv4* c, int slot0, int n, void* k, void* v, int dtype, 
  * its entry slot0 + r: softmax(q k^T / 8) v, without a mask (cross-attention).  Query
  * values and probabilities enter the products exactly, the softmax and all sums are fp32.
  * A request of no frames gets zeros; keys and values that stand for infinity within the
- * length give results that are infinite or NaN.
+ * length can make a row's results NaN.
  * q: device, fp32 or bf16; element (r, i, h, d) lies r * q_stride[0] + i * q_stride[1] +
  *   h * q_stride[2] + d elements in (strides >= 0, a host array of three): a request's beams
  *   or the rows of a pass are its rows.

@@ -22,9 +22,10 @@ namespace wf {
 // equal ones by column: KL lanes at most, whose values fit its KL * R places with any number of
 // ties.  Not waiting for the places to run out, a call of 62 x 8 rows of 367 logits, 3 best,
 // takes 12.4 us instead of 22.9, of 20 x 16 rows of 4,624, 32 best, 20.4 instead of 55.8.
-// 768 rows of 51,864 logits: fp32 32 us, the copy rate of 4.9 TB/s; bf16 33 us, bound by the
-// vector instructions (a logit costs five: one to convert, four for its exponential, and
-// a wave as many again besides).  64 logits a thread: 34 and 41 us, fewer waves a SIMD.
+// 768 rows of 51,864 logits: fp32 32 us, the copy rate of 4.9 TB/s.  bf16 33.6 us, half that rate: a wave's 525 vector
+// instructions (16 a logit of a lane, the exponential four of them; 32 are the exponentials themselves) take about 60% of
+// the SIMDs' time, and for half of its own a wave waits, for its logits before and at the barriers after them.  64 logits a
+// thread: 34 and 41 us, fewer waves a SIMD.
 constexpr int kBeamRegs = 32, kBeamPiece = 256 * kBeamRegs;
 
 // Larger value, larger integer, both zeros alike; NaN and -inf (no candidates) at 0.

@@ -481,6 +481,138 @@ int wf_kv4_attend_workspace_bytes(const wf_kv4* c, int n, int rows, size_t* byte
 int wf_kv4_attend(const wf_kv4* c, int slot0, int n, const void* q, const int64_t* q_stride, int rows, int dtype,
                   const int32_t* lens, void* out, void* workspace, size_t ws_bytes, void* stream);
 
+/*
+ * A decoder's self-attention, from the prompt to single tokens: rotary positions, attention
+ * over packed prompts, and a paged cache in 8 bits.  Head width 64 in the attentions; query
+ * head h reads key and value head h / (n_head / n_kv_head).
+ */
+
+/*
+ * Rotary positions.  Of each head's `width` elements the first `dims` turn in pairs, (i, i +
+ * dims / 2) or, interleaved, (2 i, 2 i + 1): (a, b) -> A (a cos t - b sin t, b cos t + a sin t)
+ * with t = 2 pi position turns[i]; the others stay.  Angles are formed in 64 bits, sines and
+ * cosines and the products in 32, results are rounded once.
+ *
+ * wf_rotary_turns fills a host table of dims / 2 turns a position, base^(-2 i / dims) / (2 pi),
+ * and the amplitude A, for `scaling`:
+ *   WF_ROTARY_PLAIN   as they are, A = 1 (factor, context, low and high are not used)
+ *   WF_ROTARY_LINEAR  divided by factor
+ *   WF_ROTARY_BASE    from base * factor^(dims / (dims - 2)); needs dims > 2
+ *   WF_ROTARY_RAMP    by parts: times w + (1 - w) / factor, w = (context turns - low) / (high - low)
+ *                     within [0, 1]: pairs that turn more than `high` times within `context`
+ *                     positions stay, those below `low` are divided; A = 0.1 ln(factor) + 1
+ * factor >= 1, base > 1 and context > 0 finite, 0 <= low < high.
+ */
+#define WF_ROTARY_PLAIN 0
+#define WF_ROTARY_LINEAR 1
+#define WF_ROTARY_BASE 2
+#define WF_ROTARY_RAMP 3
+int wf_rotary_turns(int dims, double base, int scaling, double factor, double context, double low, double high,
+                    double* turns, float* amplitude);
+/*
+ * turns: device fp64 [dims / 2].  transposed != 0 turns the other way with the same amplitude
+ * (the gradient of the rotation).  positions: device int32 [tokens], any value.
+ * rows: host array of n_rows (1 or 2: queries and keys) descriptions: element (token, head, i)
+ * of x lies token * x_stride[0] + head * x_stride[1] + i elements in, of y likewise; x and y
+ * are device memory in dtype (WF_F32 or WF_BF16).  y is x itself with equal strides (in place)
+ * or other memory; rows of y may not overlap, nor the two tensors.
+ * 0 <= tokens <= 2^28 (0: nothing is enqueued), 1 <= heads <= 65535, 2 <= dims <= width <= 4096, dims even.
+ * Errors: WF_EINVAL, WF_EHIP.
+ */
+typedef struct wf_rotary_rows {
+  const void* x;
+  void* y;
+  int64_t x_stride[2];
+  int64_t y_stride[2];
+  int32_t heads;
+} wf_rotary_rows;
+int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, int transposed, const int32_t* positions,
+              int tokens, int width, int dtype, const wf_rotary_rows* rows, int n_rows, void* stream);
+
+/*
+ * Causal attention of packed prompts: softmax(q k^T / 8) v, where row t of the sequence
+ * [starts[s], starts[s + 1]) sees its rows starts[s] .. t.  What the other rows hold, NaN and
+ * infinities included, does not reach it.
+ * q, k, v: device, fp32 or bf16; element (t, h, d) lies t * stride[0] + h * stride[1] + d
+ *   elements in (strides >= 0, host arrays of two).
+ * starts: device int32 [n + 1], not decreasing; a sequence may be empty.  Rows before starts[0]
+ *   and from starts[n] on belong to none (where starts lies outside [0, tokens], the part
+ *   inside counts; borders that decrease give results without meaning, read inside the tensors).
+ * out: device [tokens, n_head, 64] in the same type.  Rows of no sequence are set to zero
+ *   (clear != 0) or left as they are.
+ * fp32: products in 32 bits; bf16: the probabilities are rounded to bf16 for their product, sums
+ * are fp32.  A row all of whose scores are -inf gets zeros.
+ * 0 <= tokens <= 2^28 (0: nothing is enqueued), 1 <= n <= 2^24, 1 <= n_kv_head, n_head a multiple of it <= 65535.
+ * Errors: WF_EINVAL, WF_EHIP.
+ */
+int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, const int64_t* k_stride, const void* v,
+                     const int64_t* v_stride, int dtype, const int32_t* starts, int n, int tokens, int n_head,
+                     int n_kv_head, void* out, int clear, void* stream);
+
+/*
+ * Keys and values of a self-attention cache in 8 bits: n_pages pages of 16 positions of n_head
+ * (key and value) heads of 64.  Elements are e4m3 (to the nearest, ties to the even code) with
+ * one power-of-two scale for the keys and one for the values of a page and head: the smallest
+ * 2^e, e >= -100, with max |x| <= 448 * 2^e over its finite elements.  A NaN or an infinity is
+ * held as NaN.  Magnitudes from 248 * 2^120 (3.3e38) on stand for infinity, and for NaN in a
+ * page that keeps them while rows are appended to it.
+ * data: device, 16-byte aligned, n_pages records of wf_kv8_page_bytes(n_head) bytes (a multiple
+ * of 16) one after the other, in an order of the library's own: a page may be copied as bytes
+ * (wf_cache_reorder, page_tokens 16).
+ * 1 <= n_pages <= 2^24, 1 <= n_head <= 4096.
+ */
+typedef struct wf_kv8 {
+  void* data;
+  int32_t n_pages;
+  int32_t n_head;
+} wf_kv8;
+int wf_kv8_page_bytes(int n_head, size_t* bytes);
+/*
+ * Append rows: request r's first row goes to position positions[r], the others follow.
+ * Every page that gets a row is written whole: its positions before positions[r] keep the
+ * values that they stand for, rounded with the new ones to their common scale (exactly, unless
+ * the scale grows); positions behind the last row hold zeros.
+ * k, v: device, fp32 or bf16.  Packed (starts given): request r's rows are starts[r] ..
+ *   starts[r + 1] - 1 of `rows` in all, element (t, h, d) at t * stride[1] + h * stride[2] + d.
+ *   Otherwise every request has `rows` rows, of which the first counts[r] are given (NULL: all):
+ *   element (r, i, h, d) at r * stride[0] + i * stride[1] + h * stride[2] + d.
+ * starts: device int32 [n + 1], not decreasing (borders are taken as the nearest of [0, rows]),
+ *   or NULL; counts: device int32 [n], taken as the nearest of [0, rows], or NULL.  Not both.
+ * tables: device int32, entry (r, c) at r * table_stride + c, c < max_pages: the page of
+ *   positions 16 c .. 16 c + 15.  A page written belongs to one request alone.
+ * positions: device int32 [n].  Rows at positions below 0 or from 16 max_pages on, and rows
+ *   whose page number is outside [0, n_pages), are not stored.
+ * rows >= 0 (0: nothing is enqueued), packed <= 2^27, otherwise <= 2^20 and n * ((rows + 30) / 16) below
+ * 2^24; 1 <= n <= 65535, 1 <= max_pages <= 2^24.
+ * Errors: WF_EINVAL, WF_EHIP.
+ */
+int wf_kv8_store(const wf_kv8* c, int n, const void* k, const int64_t* k_stride, const void* v, const int64_t* v_stride,
+                 int dtype, int rows, const int32_t* starts, const int32_t* counts, const int32_t* tables,
+                 int64_t table_stride, int max_pages, const int32_t* positions, void* stream);
+/* The values that the first lens[r] positions (taken as the nearest of [0, 16 max_pages]) of
+ * every request's pages hold: k, v device [n, 16 max_pages, n_head, 64] in dtype, zeros behind
+ * them and where a page number is outside [0, n_pages).  n * max_pages below 2^24. */
+int wf_kv8_load(const wf_kv8* c, int n, const int32_t* tables, int64_t table_stride, int max_pages, const int32_t* lens,
+                void* k, void* v, int dtype, void* stream);
+/*
+ * Attention of `rows` rows of each of n requests: row i of request r stands at position
+ * positions[r] + i and sees positions 0 .. positions[r] + i of the request's pages:
+ * softmax(q k^T / 8) v.  Query values and probabilities enter the products exactly, the
+ * softmax and all sums are fp32.  Positions whose page number is outside [0, n_pages), and
+ * those from 16 max_pages on, are left out; a row that sees none gets zeros, as do rows from
+ * counts[r] on (device int32 [n], taken as the nearest of [0, rows], or NULL: all).  What
+ * positions hold that a row does not see does not reach it.
+ * q: device, fp32 or bf16; element (r, i, h, d) lies r * q_stride[0] + i * q_stride[1] +
+ *   h * q_stride[2] + d elements in.  n_q_head: a multiple of the cache's n_head, <= 65535.
+ * out: device [n, rows, n_q_head, 64] in the same type.
+ * 1 <= n <= 65535, 1 <= rows, rows * n_q_head / n_head <= 2^19, 1 <= max_pages <= 2^24.
+ * Errors: WF_EINVAL, WF_ESIZE (workspace), WF_EHIP.
+ */
+int wf_kv8_attend_workspace_bytes(const wf_kv8* c, int n, int rows, int n_q_head, int max_pages, size_t* bytes);
+int wf_kv8_attend(const wf_kv8* c, int n, const void* q, const int64_t* q_stride, int rows, int n_q_head, int dtype,
+                  const int32_t* tables, int64_t table_stride, int max_pages, const int32_t* positions,
+                  const int32_t* counts, void* out, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

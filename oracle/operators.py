@@ -102,3 +102,123 @@ def attend(q, k, v, lens):
             p = np.exp(s - s.max(-1, keepdims=True))
             out[r, :, h] = p @ v[r, :m, h] / p.sum(-1, keepdims=True)
     return out
+
+
+# ---------------------------------------------------------------- a decoder's self-attention
+
+def rotary_turns(dims, base=10000.0, scaling=None, factor=1.0, context=0.0, low=1.0, high=32.0):
+    """(turns a position of every pair, amplitude)."""
+    i = np.arange(dims // 2)
+    if scaling == "base":
+        base = base * factor ** (dims / (dims - 2))
+    f = base ** (-2.0 * i / dims) / (2 * np.pi)
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "ramp":
+        w = np.clip((f * context - low) / (high - low), 0, 1)
+        return f * (w + (1 - w) / factor), 0.1 * np.log(factor) + 1
+    return f, 1.0
+
+
+def rotary(x, positions, turns, amplitude, interleaved, transposed=False):
+    """x [tokens, heads, width]: the pairs of the first 2 len(turns) elements turned by positions' angles."""
+    y, d = np.array(x, np.float64), 2 * len(turns)
+    part = np.asarray(positions, np.float64)[:, None] * turns
+    angle = 2 * np.pi * (part - np.rint(part)) * (-1 if transposed else 1)
+    z = (amplitude * np.exp(1j * angle))[:, None]
+    a, b = (slice(0, d, 2), slice(1, d, 2)) if interleaved else (slice(0, d // 2), slice(d // 2, d))
+    w = (y[..., a] + 1j * y[..., b]) * z
+    y[..., a], y[..., b] = w.real, w.imag
+    return y
+
+
+def seen_attention(q, k, v, sees):
+    """softmax(q k^T / 8) v of rows q [rows, heads, 64] over k, v [keys, kv heads, 64], row i over its keys sees[i] (bool
+    [rows, keys]); rows that see none: zeros.  Also sum p |v| and the largest |q| |k| / 8 of a seen key (for bounds)."""
+    rows, H, _ = q.shape
+    G = H // k.shape[1]
+    out, spread, size = np.zeros(q.shape), np.zeros(q.shape), np.zeros((rows, H))
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    for h in range(H):
+        for i in range(rows):
+            at = np.flatnonzero(sees[i])
+            if not len(at):
+                continue
+            kk, vv = k[at, h // G], v[at, h // G]
+            s = kk @ q[i, h] / 8
+            with np.errstate(invalid="ignore", over="ignore"):
+                p = np.exp(s - s.max())
+                p = p / p.sum()
+                out[i, h], spread[i, h] = p @ vv, p @ np.abs(vv)
+            size[i, h] = (np.abs(kk) @ np.abs(q[i, h]) / 8).max()
+    return out, spread, size
+
+
+def prompt_attention(q, k, v, starts):
+    rows = np.arange(len(q))
+    first = np.full(len(q), -1)
+    for a, b in zip(starts, starts[1:]):
+        first[max(a, 0):max(b, 0)] = max(a, 0)
+    sees = (first[:, None] >= 0) & (rows[None] >= first[:, None]) & (rows[None] <= rows[:, None])
+    return seen_attention(q, k, v, sees)
+
+
+E4M3 = np.array([m * 2.0 ** -9 for m in range(8)] + [(8 + m) * 2.0 ** (e - 3) for e in range(-6, 9) for m in range(8)][:-1])
+
+
+def quantise8(x):
+    """A page's keys or values of one head [16, 64] -> the values that its codes stand for; what is not finite: NaN."""
+    fine = np.isfinite(x)
+    top = np.abs(np.where(fine, x, 0)).max()
+    e = -100
+    while top > 448 * 2.0 ** e:
+        e += 1
+    y = np.abs(np.where(fine, x, 0)) / 2.0 ** e
+    low = np.clip(np.searchsorted(E4M3, y, side="right") - 1, 0, len(E4M3) - 2)
+    below, above = y - E4M3[low], E4M3[low + 1] - y
+    code = np.where((above < below) | ((above == below) & (low % 2 == 1)), low + 1, low)
+    return np.where(fine, np.copysign(E4M3[code], x) * 2.0 ** e, np.nan)
+
+
+class PagedCache8:
+    """The values that a paged 8-bit cache stands for: k, v [pages, heads, 16, 64]."""
+
+    def __init__(self, pages, heads):
+        self.pages, self.heads = pages, heads
+        self.k, self.v = np.zeros((pages, heads, 16, 64)), np.zeros((pages, heads, 16, 64))
+
+    def store(self, k, v, tables, positions):
+        """k, v: a list of [rows, heads, 64] for every request."""
+        for r, at in enumerate(positions):
+            count = len(k[r])
+            for c in range(len(tables[r])):
+                page = int(tables[r][c])
+                a, b = max(16 * c, at, 0), min(16 * c + 16, at + count)
+                if a >= b or not 0 <= page < self.pages:
+                    continue
+                for held, new in ((self.k, k[r]), (self.v, v[r])):
+                    x = np.zeros((self.heads, 16, 64))
+                    keep = min(max(at - 16 * c, 0), 16)
+                    x[:, :keep] = held[page][:, :keep]
+                    x[:, a - 16 * c:b - 16 * c] = np.moveaxis(new[a - at:b - at], 0, 1)
+                    for h in range(self.heads):
+                        held[page][h] = quantise8(x[h])
+
+    def rows(self, table, length):
+        """(k, v [length, heads, 64], which of them lie in a page)."""
+        k, v, there = np.zeros((length, self.heads, 64)), np.zeros((length, self.heads, 64)), np.zeros(length, bool)
+        for c in range(min(len(table), -(-length // 16))):
+            page, m = int(table[c]), min(16, length - 16 * c)
+            if 0 <= page < self.pages:
+                k[16 * c:16 * c + m] = np.moveaxis(self.k[page][:, :m], 0, 1)
+                v[16 * c:16 * c + m] = np.moveaxis(self.v[page][:, :m], 0, 1)
+                there[16 * c:16 * c + m] = True
+        return k, v, there
+
+    def attend(self, q, table, at, count):
+        """One request's rows q [rows, heads, 64]."""
+        rows, most = len(q), 16 * len(table)
+        length = min(max(at + count, 0), most)
+        k, v, there = self.rows(table, length)
+        sees = (np.arange(length)[None] <= at + np.arange(rows)[:, None]) & there[None] & (np.arange(rows)[:, None] < count)
+        return seen_attention(q, k, v, sees)

@@ -29,7 +29,9 @@ EXPORTS = ["wf_workspace_bytes", "wf_weight_count", "wf_weight_numel", "wf_init_
            "wf_encoder_workspace_bytes", "wf_encoder_weight_count", "wf_encoder_weight_numel", "wf_encoder_init",
            "wf_encoder_run", "wf_encoder_logmel", "wf_encoder_release", "wf_encoder_last_error",
            "wf_beam_bytes", "wf_beam_begin", "wf_beam_step", "wf_beam_end", "wf_beam_select_workspace_bytes", "wf_beam_select", "wf_cache_reorder", "wf_kv4_bytes", "wf_kv4_store",
-           "wf_kv4_load", "wf_kv4_attend_workspace_bytes", "wf_kv4_attend"]
+           "wf_kv4_load", "wf_kv4_attend_workspace_bytes", "wf_kv4_attend",
+           "wf_rotary_turns", "wf_rotary", "wf_prompt_attend", "wf_kv8_page_bytes", "wf_kv8_store", "wf_kv8_load",
+           "wf_kv8_attend_workspace_bytes", "wf_kv8_attend"]
 
 
 class WfConfig(ctypes.Structure):
@@ -51,6 +53,15 @@ class WfKv4(ctypes.Structure):
                 ("n_frames", ctypes.c_int32)]
 
 
+class WfRotaryRows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2),
+                ("heads", ctypes.c_int32)]
+
+
+class WfKv8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("n_head", ctypes.c_int32)]
+
+
 class WfError(RuntimeError):
     pass
 
@@ -68,7 +79,8 @@ def load_library(path=LIB_PATH):
     lib = ctypes.CDLL(path)
     P, I, Z, U64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint64
     I64, I64p = ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)
-    cfgp, kv4p = ctypes.POINTER(WfConfig), ctypes.POINTER(WfKv4)
+    cfgp, kv4p, kv8p = ctypes.POINTER(WfConfig), ctypes.POINTER(WfKv4), ctypes.POINTER(WfKv8)
+    F, D = ctypes.c_float, ctypes.c_double
     sig = {
         "wf_workspace_bytes": [cfgp, ctypes.POINTER(Z)],
         "wf_weight_count": [cfgp, ctypes.POINTER(I)],
@@ -111,6 +123,14 @@ def load_library(path=LIB_PATH):
         "wf_kv4_load": [kv4p, I, I, P, P, I, P],
         "wf_kv4_attend_workspace_bytes": [kv4p, I, I, ctypes.POINTER(Z)],
         "wf_kv4_attend": [kv4p, I, I, P, I64p, I, I, P, P, P, Z, P],
+        "wf_rotary_turns": [I, D, I, D, D, D, D, ctypes.POINTER(D), ctypes.POINTER(F)],
+        "wf_rotary": [P, I, I, F, I, P, I, I, I, ctypes.POINTER(WfRotaryRows), I, P],
+        "wf_prompt_attend": [P, I64p, P, I64p, P, I64p, I, P, I, I, I, I, P, I, P],
+        "wf_kv8_page_bytes": [I, ctypes.POINTER(Z)],
+        "wf_kv8_store": [kv8p, I, P, I64p, P, I64p, I, I, P, P, P, I64, I, P, P],
+        "wf_kv8_load": [kv8p, I, P, I64, I, P, P, P, I, P],
+        "wf_kv8_attend_workspace_bytes": [kv8p, I, I, I, I, ctypes.POINTER(Z)],
+        "wf_kv8_attend": [kv8p, I, P, I64p, I, I, I, P, I64, I, P, P, P, P, Z, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

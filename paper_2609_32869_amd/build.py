@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwf.so")
 OBJDIR = os.path.join(os.path.dirname(HERE), "_build")
 SOURCES = ["k_gemv.hip", "k_attn.hip", "k_misc.hip", "k_mm.hip", "k_enc.hip", "k_pre.hip", "k_beam.hip", "k_kv4.hip",
-           "wf_api.hip", "enc_api.hip", "op_api.hip"]
+           "k_rope.hip", "k_prompt.hip", "k_kv8.hip", "wf_api.hip", "enc_api.hip", "op_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed fp32 arithmetic is kept out of every kernel
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,567 @@
+// A paged self-attention cache in 8 bits, and attention over it.
+//
+// Elements are e4m3 with a power-of-two scale for the keys and one for the values of a page (16
+// positions) and head, so one instruction turns two codes and the scale into two bf16 values,
+// exactly, and a page whose scale grows keeps its values unless they fall below the new scale's
+// smallest normal one.
+#include <algorithm>
+
+#include "wf_kv4.h"
+#include "wf_operand.h"
+#include "wf_ops.h"
+
+namespace wf {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Smallest 2^e, e >= -100, with amax <= 448 * 2^e = 1.75 * 2^(e + 8), as a biased exponent.
+__device__ __forceinline__ uint32_t scale8_of(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - ((u & 0x7fffffu) <= 0x600000u ? 8 : 7);
+  return (uint32_t)max(e, 27);
+}
+// 4 values -> 4 codes, element i in byte i; `inv` the scale's inverse.  No |x| inv passes 448.  What is
+// not finite becomes NaN.
+__device__ __forceinline__ uint32_t codes8x4(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = mag(x[j]) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : x[j] * inv;
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
+}
+// 4 codes -> the 4 values they stand for.
+__device__ __forceinline__ void values8x4(uint32_t c, float s, float* x) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+  x[0] = a[0] * s;
+  x[1] = a[1] * s;
+  x[2] = b[0] * s;
+  x[3] = b[1] * s;
+}
+__device__ __forceinline__ uint32_t mag_finite(float x) { return mag(x) >= 0x7f800000u ? 0u : mag(x); }
+// 2^(127 - byte) of a scale byte in [27, 247]
+__device__ __forceinline__ float inverse_f(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v = umax(v, (uint32_t)__shfl_xor((int)v, m));
+  return v;
+}
+
+// ---------------------------------------------------------------- store
+// A wave per (page that a request writes, head).  Lane l = 16 kg + n holds dims 16 kg .. + 15 of
+// position n's key; lane l = 32 h + 16 g + n of the values dims 4 n + 2 h, + 1 of positions 8 g .. + 7.
+// Where a request's pages lie in the grid: request r's first page has number starts[r] / 16 + 2 r
+// (packed), which leaves room for every page that its rows can touch, or r * per (padded).
+template <typename T>
+__global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
+  const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (head >= a.c.n_head) return;
+  int r, col, first, count;
+  if (a.starts) {
+    int lo = 0, hi = a.n;  // the last request whose first number is <= the block's
+    auto at = [&](int i) { return min(max(a.starts[i], 0), a.rows); };
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (at(m) / 16 + 2 * m <= (int)blockIdx.x) lo = m;
+      else hi = m;
+    }
+    r = lo;
+    first = at(r);
+    count = at(r + 1) - first;
+    col = (int)blockIdx.x - (first / 16 + 2 * r);
+  } else {
+    r = blockIdx.x / per;
+    col = blockIdx.x - r * per;
+    first = 0;
+    count = a.counts ? min(max(a.counts[r], 0), a.rows) : a.rows;
+  }
+  const long long pos = a.positions[r], begin = max(pos, 0ll);  // first position stored
+  const long long page0 = (begin >> 4) + col;                    // this wave's page of the request
+  if (col < 0 || count <= 0 || page0 >= a.max_pages || page0 * 16 >= pos + count) return;
+  const int page = a.tables[r * a.ts + page0];
+  if (page < 0 || page >= a.c.n_pages) return;
+  uint8_t* out = a.c.base + page * a.c.page + (size_t)head * kKv8Head;
+  uint8_t* sc = a.c.base + page * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head;
+  const long long skip = page0 * 16 - pos;  // row of position 0 of the page (negative: kept positions before the rows)
+  const int kept = (int)max(-skip, 0ll);    // positions [0, kept) stay, [kept, end) are rows
+  const int end = (int)min(count - skip, 16ll);
+  const T* K = reinterpret_cast<const T*>(a.k) + (a.starts ? 0 : r * a.kr) + head * a.kh;
+  const T* V = reinterpret_cast<const T*>(a.v) + (a.starts ? 0 : r * a.vr) + head * a.vh;
+  const uint32_t olds = kept ? *reinterpret_cast<const uint16_t*>(sc) : 0;
+
+  const int n = lane & 15, kg = lane >> 4;
+  float x[16];
+  if (n < kept) {
+    const uint4 c = *reinterpret_cast<const uint4*>(out + 16 * lane);
+    const float s = scale_f(olds & 255);
+    values8x4(c.x, s, x);
+    values8x4(c.y, s, x + 4);
+    values8x4(c.z, s, x + 8);
+    values8x4(c.w, s, x + 12);
+  } else if (n < end) {
+    const T* p = K + (first + skip + n) * a.ki + 16 * kg;
+    if (a.vec) {
+      ld8(p, x);
+      ld8(p + 8, x + 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = to_f(p[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = 0.f;
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) m = umax(m, mag_finite(x[j]));
+  const uint32_t ks = scale8_of(__uint_as_float(wave_umax(m)));
+  const float ki = inverse_f(ks);
+  const uint4 kc = make_uint4(codes8x4(x, ki), codes8x4(x + 4, ki), codes8x4(x + 8, ki), codes8x4(x + 12, ki));
+
+  // values: y[dd][j] = dim 4 n + 2 h + dd of position 8 g + j
+  const int h = lane >> 5, g = (lane >> 4) & 1;
+  uint8_t* vout = out + kKv8Values + 32 * (16 * g + n) + 16 * h;
+  float y[2][8];
+  if (kept > 8 * g) {
+    const uint4 c = *reinterpret_cast<const uint4*>(vout);
+    const float s = scale_f(olds >> 8);
+    values8x4(c.x, s, y[0]);
+    values8x4(c.y, s, y[0] + 4);
+    values8x4(c.z, s, y[1]);
+    values8x4(c.w, s, y[1] + 4);
+  }
+  m = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int f = 8 * g + j;
+    if (f >= kept) {
+      y[0][j] = y[1][j] = 0.f;
+      if (f < end) {
+        const T* p = V + (first + skip + f) * a.vi + 4 * n + 2 * h;
+        y[0][j] = to_f(p[0]);
+        y[1][j] = to_f(p[1]);
+      }
+    }
+    m = umax(m, umax(mag_finite(y[0][j]), mag_finite(y[1][j])));
+  }
+  const uint32_t vs = scale8_of(__uint_as_float(wave_umax(m)));
+  const float vi = inverse_f(vs);
+  *reinterpret_cast<uint4*>(out + 16 * lane) = kc;
+  *reinterpret_cast<uint4*>(vout) = make_uint4(codes8x4(y[0], vi), codes8x4(y[0] + 4, vi), codes8x4(y[1], vi), codes8x4(y[1] + 4, vi));
+  if (lane == 0) *reinterpret_cast<uint16_t*>(sc) = (uint16_t)(ks | vs << 8);
+}
+
+void kv8_store(const Kv8StoreArgs& a, hipStream_t st) {
+  const int per = (a.rows + 30) / 16;  // pages that a request's rows can touch
+  const long long units = a.starts ? a.rows / 16 + 2ll * a.n + 1 : (long long)per * a.n;
+  const dim3 grid((unsigned)units, (a.c.n_head + 3) / 4);
+  if (a.bf16_src) k_kv8_store<bf16><<<grid, 256, 0, st>>>(a, per);
+  else k_kv8_store<float><<<grid, 256, 0, st>>>(a, per);
+}
+
+// ---------------------------------------------------------------- load
+__device__ __forceinline__ void st4(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void st4(bf16* p, const float* x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
+}
+// A wave per (request, column of its table, head): lane l = 16 kg + n the key's dims 16 kg .. + 15 of position n,
+// and dims 4 n .. + 3 of the values of positions 4 kg .. + 3.
+template <typename T>
+__global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
+  const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
+  if (head >= a.c.n_head) return;
+  const int r = blockIdx.x / a.max_pages, col = blockIdx.x - r * a.max_pages;
+  const int page = a.tables[r * a.ts + col];
+  const int len = min(max(a.lens[r], 0), 16 * a.max_pages) - 16 * col;  // positions of this page
+  const bool there = page >= 0 && page < a.c.n_pages && len > 0;
+  const size_t pitch = (size_t)a.c.n_head * kHeadDim, at = (size_t)blockIdx.x * 16 * pitch + head * kHeadDim;
+  T* K = reinterpret_cast<T*>(a.k) + at;
+  T* V = reinterpret_cast<T*>(a.v) + at;
+  float x[16], y[4][4];  // y[dt][j]: dim 4 n + dt of position 4 kg + j
+  if (there) {
+    const uint8_t* in = a.c.base + page * a.c.page + (size_t)head * kKv8Head;
+    const uint32_t s = *reinterpret_cast<const uint16_t*>(a.c.base + page * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head);
+    const uint4 c = *reinterpret_cast<const uint4*>(in + 16 * lane);
+    values8x4(c.x, scale_f(s & 255), x);
+    values8x4(c.y, scale_f(s & 255), x + 4);
+    values8x4(c.z, scale_f(s & 255), x + 8);
+    values8x4(c.w, scale_f(s & 255), x + 12);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(in + kKv8Values + 32 * (16 * (kg >> 1) + n) + 8 * dt + 4 * (kg & 1));
+      values8x4(v, scale_f(s >> 8), y[dt]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 16; ++j) x[j] = there && n < len ? x[j] : 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) st4(K + n * pitch + 16 * kg + j, x + j);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool in = there && 4 * kg + j < len;
+    const float o[4] = {in ? y[0][j] : 0.f, in ? y[1][j] : 0.f, in ? y[2][j] : 0.f, in ? y[3][j] : 0.f};
+    st4(V + (4 * kg + j) * pitch + 4 * n, o);
+  }
+}
+
+void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)a.n * a.max_pages), (a.c.n_head + 3) / 4);
+  if (a.bf16_out) k_kv8_load<bf16><<<grid, 256, 0, st>>>(a);
+  else k_kv8_load<float><<<grid, 256, 0, st>>>(a);
+}
+
+// ---------------------------------------------------------------- attention
+// A key and value head's query columns are the rows of its group's heads: column c is row c / group,
+// head c % group of the group.  Block (key and value head, request, 16 columns, chunk of the
+// positions) x eight waves; a wave takes steps of 32 positions (two pages), every eighth.
+//   scores   S^T = K q^T per page (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets column n of
+//            positions 4 kg .. + 3
+//   softmax  running maximum and sum per column, one rescaling per step
+//   values   O^T = V^T P^T per step: two lane swaps turn its two score tiles into the operand
+//            (lane: column n, positions 8 kg .. + 7)
+//   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for the
+//            merge kernel
+namespace {
+constexpr float kLog2e = 1.44269504088896f;
+constexpr int kWaves = 8, kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
+
+__device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
+__device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float swap_max(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float swap_sum(float v) {
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+// Eight values as N bf16 terms (three hold an fp32 value exactly, one a bf16 value).
+template <int N>
+__device__ __forceinline__ void split_terms(const float* v, bf16x8 (&t)[N]) {
+  uint4 u[3];
+  if constexpr (N == 3) split3x8(v, u[0], u[1], u[2]);
+  else u[0] = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+#pragma unroll
+  for (int i = 0; i < N; ++i) t[i] = __builtin_bit_cast(bf16x8, u[i]);
+}
+// 8 codes -> the 8 bf16 values they stand for.
+__device__ __forceinline__ bf16x8 bf8(uint32_t lo, uint32_t hi, float s) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// The bytes of a word that are NaN codes, as 0xff each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t c) {
+  const uint32_t x = (c & 0x7f7f7f7fu) + 0x01010101u;  // bit 7 of a byte: its low seven bits are all ones
+  return ((x & 0x80808080u) >> 7) * 255u;
+}
+// The bytes of positions below `left` in the two words of eight positions.
+__device__ __forceinline__ void cut(uint32_t& lo, uint32_t& hi, int left) {
+  lo &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
+  hi &= left >= 8 ? ~0u : left <= 4 ? 0u : (1u << 8 * (left - 4)) - 1;
+}
+
+// Codes and scales of two pages; there: bit t set where page t's number is good.
+struct Step {
+  uint4 k[2], v[2];
+  uint32_t s[2], there;
+};
+struct State {
+  float m, l;
+  floatx4 o[4];
+};
+}  // namespace
+
+// Positions p0 .. p0 + 31; `lim`: this lane's column sees positions below it; all columns see those below `low`, none
+// those from `top` on.
+template <int QT, int PT>
+__device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int top, const bf16x8 (&qt)[2][QT], State& st) {
+  const int kg = (threadIdx.x & 63) >> 4;
+  floatx4 s[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float sc = scale_f(c.s[t] & 255);
+    const bf16x8 k0 = bf8(c.k[t].x, c.k[t].y, sc), k1 = bf8(c.k[t].z, c.k[t].w, sc);
+    s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = QT - 1; i >= 0; --i) s[t] = mfma16(k1, qt[1][i], mfma16(k0, qt[0][i], s[t]));
+  }
+  uint32_t vw[4][2] = {{c.v[0].x, c.v[0].y}, {c.v[0].z, c.v[0].w}, {c.v[1].x, c.v[1].y}, {c.v[1].z, c.v[1].w}};
+  const uint32_t vs = (kg >> 1 ? c.s[1] : c.s[0]) >> 8;
+  const bool masked = p0 + 32 > low || c.there != 3;
+  uint32_t odd = 0, hidden = 0;  // hidden: bit 4 t + i
+  if (masked) {  // uniform
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p0 + 16 * t + 4 * kg + i >= lim || !(c.there >> t & 1)) {
+          s[t][i] = -INFINITY;
+          hidden |= 1u << (4 * t + i);
+        }
+    const int left = c.there >> (kg >> 1) & 1 ? top - p0 - 8 * kg : 0;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      cut(vw[dt][0], vw[dt][1], left);
+      odd |= nan_bytes(vw[dt][0]) | nan_bytes(vw[dt][1]);
+    }
+  }
+  float mx = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
+  const float m = fmaxf(st.m, swap_max(mx)), base = no_inf(m);
+  const float f = exp_to(st.m, base);  // 0 at first
+  st.m = m;
+  float l = 0.f;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[t][i] = exp_to(s[t][i], base);
+      l += s[t][i];
+    }
+  st.l = fmaf(st.l, f, l);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) st.o[dt] *= f;
+  auto operand = [&](const floatx4 (&x)[2], float* pb) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[0][i]), __float_as_uint(x[1][i]), false, false);
+      const auto y = __builtin_amdgcn_permlane16_swap(u[0], u[1], false, false);
+      pb[i] = __uint_as_float(y[0]);
+      pb[4 + i] = __uint_as_float(y[1]);
+    }
+  };
+  // A NaN times a probability of 0 would reach the columns that do not see it: such values leave the
+  // product and are counted, for the columns that do, by a product of ones.
+  if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+    floatx4 sees[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sees[t][i] = hidden >> (4 * t + i) & 1 ? 0.f : 1.f;
+    float pb[8];
+    operand(sees, pb);
+    bf16x8 one[1];
+    split_terms<1>(pb, one);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+      const uint32_t n0 = nan_bytes(vw[dt][0]), n1 = nan_bytes(vw[dt][1]);
+      const bf16x8 x = bf8(n0 & 0x38383838u, n1 & 0x38383838u, 1.f);  // 0x38: the code of 1
+      const floatx4 z = mfma16(x, one[0], floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (z[i] > 0.f) st.o[dt][i] = __uint_as_float(0x7fc00000u);
+      vw[dt][0] &= ~n0;
+      vw[dt][1] &= ~n1;
+    }
+  }
+  float pb[8];
+  operand(s, pb);
+  bf16x8 pt[PT];
+  split_terms<PT>(pb, pt);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) {
+    const bf16x8 x = bf8(vw[dt][0], vw[dt][1], scale_f(vs));
+#pragma unroll
+    for (int i = PT - 1; i >= 0; --i) st.o[dt] = mfma16(x, pt[i], st.o[dt]);
+  }
+}
+
+// Position of request r's first row and its rows, as far as they matter: positions far outside the tables count as the
+// nearest that behave alike.
+__device__ __forceinline__ void kv8_rows(const Kv8AttendArgs& a, int r, int& pos, int& count) {
+  count = a.counts ? min(max(a.counts[r], 0), a.rows) : a.rows;
+  pos = min(max(a.positions[r], -(1 << 20)), 16 * a.max_pages);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
+  constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
+  __shared__ float wm[kWaves][16], wl[kWaves][16], wo[kWaves][16][68];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
+  const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, c0 = blockIdx.z * 16;
+  const int cols = a.rows * a.group, cap = 16 * a.max_pages;
+  int pos, count;
+  kv8_rows(a, r, pos, count);
+  // columns of rows from `count` on, and of rows that see nothing, run along unmasked and are written as zeros
+  const int i0 = c0 / a.group, i1 = min(min(cols, c0 + 16) - 1, count * a.group - 1) / a.group;  // rows of this tile
+  const int col = c0 + n, i = col / a.group;
+  const bool live = col < cols && i < count && pos + i >= 0;
+  const int top = c0 < count * a.group ? min(max(pos + i1 + 1, 0), cap) : 0;
+  const int low = min(max(pos + i0, 0) + 1, top), lim = live ? min(pos + i + 1, cap) : cap;
+  const int groups = (top + 31) / 32, each = (groups + a.nchunk - 1) / a.nchunk;
+  const int end = min((chunk + 1) * each, groups);
+  const int* table = a.tables + r * a.ts;
+  State st;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) st.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  auto load = [&](int g, Step& s) {
+    const int pages = (top + 15) / 16;
+    int p[2];
+    s.there = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int c = min(2 * min(g, end - 1) + t, pages - 1);
+      p[t] = __builtin_amdgcn_readfirstlane(table[c]);
+      if (p[t] >= 0 && p[t] < a.c.n_pages) s.there |= 1u << t;
+      else p[t] = 0;
+    }
+    const size_t scales = (size_t)a.c.n_head * kKv8Head + 2 * head;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t* in = a.c.base + p[t] * a.c.page;
+      s.k[t] = *reinterpret_cast<const uint4*>(in + (size_t)head * kKv8Head + 16 * lane);
+      s.s[t] = *reinterpret_cast<const uint16_t*>(in + scales);
+      if (!(s.there >> t & 1)) s.s[t] = 0x7f7f;  // another page's scales may be anything: 1
+    }
+    const uint8_t* in = a.c.base + (kg >> 1 ? p[1] : p[0]) * a.c.page + (size_t)head * kKv8Head + kKv8Values + 32 * (lane & 31);
+    s.v[0] = *reinterpret_cast<const uint4*>(in);
+    s.v[1] = *reinterpret_cast<const uint4*>(in + 16);
+  };
+  int g = chunk * each + w;
+  if (g < end) {
+    Step A, B;
+    load(g, A);
+    const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(i, a.rows - 1) * a.si +
+                 (head * a.group + col % a.group) * a.sh + 16 * kg;
+    float x[16];
+    if (a.vec) {
+      ld8(q, x);
+      ld8(q + 8, x + 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[j] = to_f(q[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = live ? 0.125f * x[j] : 0.f;
+    bf16x8 qt[2][QT];
+    split_terms<QT>(x, qt[0]);
+    split_terms<QT>(x + 8, qt[1]);
+    for (;;) {
+      load(g + kWaves, B);
+      kv8_step<QT, PT>(A, 32 * g, lim, low, top, qt, st);
+      g += kWaves;
+      if (g >= end) break;
+      load(g + kWaves, A);
+      kv8_step<QT, PT>(B, 32 * g, lim, low, top, qt, st);
+      g += kWaves;
+      if (g >= end) break;
+    }
+  }
+  const float l = swap_sum(st.l);
+  if (lane < 16) {
+    wm[w][lane] = st.m;
+    wl[w][lane] = l;
+  }
+  // value tile dt holds dims 4 m + dt: o[dt][i] of the lane is dim 16 kg + 4 i + dt
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    *reinterpret_cast<floatx4*>(&wo[w][n][16 * kg + 4 * e]) = floatx4{st.o[0][e], st.o[1][e], st.o[2][e], st.o[3][e]};
+  __syncthreads();
+  const int nc = min(16, cols - c0);
+  for (int t = threadIdx.x; t < nc * 64; t += kWaves * 64) {
+    const int c = t >> 6, d = t & 63, ci = (c0 + c) / a.group;
+    float M = wm[0][c], L = 0.f, O = 0.f;
+#pragma unroll
+    for (int j = 1; j < kWaves; ++j) M = fmaxf(M, wm[j][c]);
+    const float base = no_inf(M);
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) {
+      const float f = exp_to(wm[j][c], base);  // 0 for a wave of no positions
+      L = fmaf(f, wl[j][c], L);
+      O = fmaf(f, wo[j][c][d], O);
+    }
+    if (a.nchunk == 1) {
+      const bool some = ci < count && pos + ci >= 0 && L != 0.f;
+      reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + (c0 + c) % a.group) * kHeadDim + d] =
+          from_f<T>(some ? O / L : 0.f);
+    } else {
+      float* rec = a.part + ((((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk + chunk) * kRecord;
+      rec[32 + t] = O;
+      if (d == 0) {
+        rec[c] = M;
+        rec[16 + c] = L;
+      }
+    }
+  }
+}
+
+// Joins the chunks of one column: 16 threads (4 dims each) take every sixteenth chunk and meet in LDS.
+template <typename T>
+__global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
+  __shared__ float wm[16], wl[16], wo[16][64];
+  const int cols = a.rows * a.group, tiles = (cols + 15) >> 4;
+  const int head = blockIdx.x, r = blockIdx.y, c = blockIdx.z, tile = c >> 4, i = c & 15;
+  const int t = threadIdx.x, q = t >> 4, d = 4 * (t & 15);
+  const float* rec = a.part + (((size_t)r * tiles + tile) * a.c.n_head + head) * a.nchunk * kRecord;
+  float M = -INFINITY, L = 0.f;
+  floatx4 O = {0.f, 0.f, 0.f, 0.f};
+  for (int k = q; k < a.nchunk; k += 16) {
+    const float* p = rec + (size_t)k * kRecord;
+    const float m = p[i], Mn = fmaxf(M, m), base = no_inf(Mn), f0 = exp_to(M, base), f = exp_to(m, base);
+    M = Mn;
+    L = fmaf(f, p[16 + i], L * f0);
+    O = O * f0 + f * *reinterpret_cast<const floatx4*>(p + 32 + i * 64 + d);
+  }
+  *reinterpret_cast<floatx4*>(&wo[q][d]) = O;
+  if (d == 0) {
+    wm[q] = M;
+    wl[q] = L;
+  }
+  __syncthreads();
+  if (t < 64) {
+    float m = wm[0], l = 0.f, o = 0.f;
+#pragma unroll
+    for (int j = 1; j < 16; ++j) m = fmaxf(m, wm[j]);
+    const float base = no_inf(m);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float f = exp_to(wm[j], base);
+      l = fmaf(f, wl[j], l);
+      o = fmaf(f, wo[j][t], o);
+    }
+    int pos, count;
+    kv8_rows(a, r, pos, count);
+    const int ci = c / a.group;
+    const bool some = ci < count && pos + ci >= 0 && l != 0.f;
+    reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + c % a.group) * kHeadDim + t] =
+        from_f<T>(some ? o / l : 0.f);
+  }
+}
+
+// Chunks of the positions: towards four blocks a compute unit, each of two steps of every wave at least.
+static int kv8_chunks(int n, int rows, int group, int n_head, int max_pages) {
+  const long long blocks = (long long)n * n_head * ((rows * group + 15) / 16), groups = (max_pages + 1) / 2;
+  return (int)std::max<long long>(1, std::min<long long>(1024 / blocks, groups / (2 * kWaves)));
+}
+size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages) {
+  const int nc = kv8_chunks(n, rows, group, n_head, max_pages);
+  return nc == 1 ? 0 : (size_t)n * n_head * ((rows * group + 15) / 16) * nc * kRecord * 4;
+}
+
+template <typename T>
+static void attend_launch(const Kv8AttendArgs& a, hipStream_t st) {
+  const int cols = a.rows * a.group;
+  k_kv8_attend<T><<<dim3(a.c.n_head * a.nchunk, a.n, (cols + 15) / 16), kWaves * 64, 0, st>>>(a);
+  if (a.nchunk > 1) k_kv8_merge<T><<<dim3(a.c.n_head, a.n, cols), 256, 0, st>>>(a);
+}
+void kv8_attend(const Kv8AttendArgs& a0, hipStream_t st) {
+  Kv8AttendArgs a = a0;
+  a.nchunk = kv8_chunks(a.n, a.rows, a.group, a.c.n_head, a.max_pages);
+  if (a.bf16_q) attend_launch<bf16>(a, st);
+  else attend_launch<float>(a, st);
+}
+
+}  // namespace wf

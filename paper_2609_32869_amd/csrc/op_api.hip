@@ -1,4 +1,5 @@
 // C entries of the operators without a handle: argument checks and launches.
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/wf.h"
@@ -53,15 +54,46 @@ int check_range(const wf_kv4* c, int slot0, int n) {
 Kv4 geometry(const wf_kv4* c) {
   return Kv4{static_cast<uint8_t*>(c->data), c->n_head, kv4_groups(c->n_frames), c->n_frames};
 }
-// Strides of three axes before the last; vec: every row starts on 16 bytes.
-int check_strides(const void* p, const int64_t* s, size_t e, int& vec) {
+// Strides of the `axes` axes before the last; vec: every row starts on 16 bytes.
+int check_strides(const void* p, const int64_t* s, size_t e, int& vec, int axes = 3) {
   if (!p || !s) return bad("null argument");
   if (!aligned(p, e)) return bad("a tensor must be aligned to its elements");
-  for (int i = 0; i < 3; ++i)
+  if (!aligned(p, 16)) vec = 0;
+  for (int i = 0; i < axes; ++i) {
     if (s[i] < 0 || s[i] > ((int64_t)1 << 40)) return bad("stride out of range");
-  if (!aligned(p, 16) || (s[0] * e) % 16 || (s[1] * e) % 16 || (s[2] * e) % 16) vec = 0;
+    if ((s[i] * e) % 16) vec = 0;
+  }
   return WF_OK;
 }
+// Rows of `width` elements at t * s[0] + h * s[1] that overlap.
+bool rows_overlap(const int64_t* s, int tokens, int heads, int width) {
+  const int64_t a = tokens > 1 ? s[0] : INT64_MAX, b = heads > 1 ? s[1] : INT64_MAX;
+  if (a < width || b < width) return true;
+  if (tokens <= 1 || heads <= 1) return false;
+  return a < b ? b / a < tokens : a / b < heads;
+}
+int check_heads(int n_head, int n_kv_head) {
+  if (n_kv_head < 1 || n_head < 1 || n_head > kMaxGrid || n_head % n_kv_head)
+    return bad("n_head must be in [1, 65535] and a multiple of the key and value heads");
+  return WF_OK;
+}
+
+int check_cache8(const wf_kv8* c, bool data = true) {
+  if (!c) return bad("null cache");
+  if (c->n_pages < 1 || c->n_pages > kKv8MaxPages) return bad("n_pages must be in [1, 2^24]");
+  if (c->n_head < 1 || c->n_head > kKv8MaxHeads) return bad("n_head must be in [1, 4096]");
+  if (data && (!c->data || !aligned(c->data, 16))) return bad("cache data must be 16-byte aligned");
+  return WF_OK;
+}
+int check_tables(int n, const int32_t* tables, int64_t stride, int max_pages) {
+  if (n < 1 || n > kMaxGrid) return bad("n must be in [1, 65535]");
+  if (max_pages < 1 || max_pages > kKv8MaxPages) return bad("max_pages must be in [1, 2^24]");
+  if (!tables || !aligned(tables, 4)) return bad("tables must be aligned to its elements");
+  if (stride < 0 || stride > ((int64_t)1 << 40)) return bad("stride out of range");
+  return WF_OK;
+}
+Kv8 geometry(const wf_kv8* c) { return Kv8{static_cast<uint8_t*>(c->data), c->n_pages, c->n_head, kv8_page_bytes(c->n_head)}; }
+constexpr int kMaxUnits = (1 << 24) - 1;  // blocks of 256 threads along a grid's x
 
 }  // namespace
 
@@ -241,6 +273,226 @@ int wf_kv4_attend(const wf_kv4* c, int slot0, int n, const void* q, const int64_
   a.rows = rows;
   a.part = static_cast<float*>(workspace);
   kv4_attend(a, static_cast<hipStream_t>(stream));
+  return launched();
+}
+
+int wf_rotary_turns(int dims, double base, int scaling, double factor, double context, double low, double high,
+                    double* turns, float* amplitude) {
+  if (dims < 2 || dims > 4096 || dims % 2) return bad("dims must be even and in [2, 4096]");
+  if (!(base > 1.0) || !std::isfinite(base)) return bad("base must be above 1");
+  if (scaling < WF_ROTARY_PLAIN || scaling > WF_ROTARY_RAMP) return bad("unknown scaling");
+  if (scaling != WF_ROTARY_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return bad("factor must be 1 or more");
+  if (scaling == WF_ROTARY_BASE && dims < 4) return bad("scaling the base needs dims above 2");
+  if (scaling == WF_ROTARY_RAMP && !(context > 0.0 && std::isfinite(context))) return bad("context must be above 0");
+  if (scaling == WF_ROTARY_RAMP && !(low >= 0.0 && low < high && std::isfinite(high))) return bad("low must be in [0, high)");
+  if (!turns || !amplitude) return bad("null argument");
+  if (scaling == WF_ROTARY_BASE) base *= std::pow(factor, dims / (dims - 2.0));
+  for (int i = 0; i < dims / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / dims) / (2.0 * 3.14159265358979323846);
+    if (scaling == WF_ROTARY_LINEAR) f /= factor;
+    if (scaling == WF_ROTARY_RAMP) {
+      const double w = std::fmin(std::fmax((f * context - low) / (high - low), 0.0), 1.0);
+      f *= w + (1.0 - w) / factor;
+    }
+    turns[i] = f;
+  }
+  *amplitude = scaling == WF_ROTARY_RAMP ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return WF_OK;
+}
+
+int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, int transposed, const int32_t* positions,
+              int tokens, int width, int dtype, const wf_rotary_rows* rows, int n_rows, void* stream) {
+  size_t e;
+  if (width < 2 || width > 4096) return bad("width must be in [2, 4096]");
+  if (dims < 2 || dims > width || dims % 2) return bad("dims must be even and in [2, width]");
+  if (tokens < 0 || tokens > (1 << 28)) return bad("tokens must be in [0, 2^28]");
+  if (int r = check_dtype(dtype, e)) return r;
+  if (n_rows < 1 || n_rows > 2 || !rows) return bad("n_rows must be 1 or 2");
+  if (!turns || !positions) return bad("null argument");
+  if (!aligned(turns, 8) || !aligned(positions, 4)) return bad("a tensor must be aligned to its elements");
+  if (!std::isfinite(amplitude)) return bad("amplitude must be finite");
+  RotaryArgs a{};
+  a.turns = turns;
+  a.dims = dims;
+  a.interleaved = interleaved != 0;
+  a.transposed = transposed != 0;
+  a.width = width;
+  a.amplitude = amplitude;
+  a.positions = positions;
+  a.tokens = tokens;
+  a.bf16_data = dtype == WF_BF16;
+  a.n_rows = n_rows;
+  a.vec = 1;
+  for (int i = 0; i < n_rows; ++i) {
+    const wf_rotary_rows& w = rows[i];
+    if (w.heads < 1 || w.heads > kMaxGrid) return bad("heads must be in [1, 65535]");
+    if (int r = check_strides(w.x, w.x_stride, e, a.vec, 2)) return r;
+    if (int r = check_strides(w.y, w.y_stride, e, a.vec, 2)) return r;
+    if (rows_overlap(w.y_stride, tokens, w.heads, width)) return bad("rows of y overlap");
+    if (w.x == w.y) {
+      if ((tokens > 1 && w.x_stride[0] != w.y_stride[0]) || (w.heads > 1 && w.x_stride[1] != w.y_stride[1]))
+        return bad("in place, x and y must have equal strides");
+    } else {
+      a.copies = 1;  // of an x in place: onto itself
+    }
+    a.rows[i] = RotaryRows{w.x, w.y, w.x_stride[0], w.x_stride[1], w.y_stride[0], w.y_stride[1], w.heads};
+  }
+  if (tokens == 0) return WF_OK;
+  rotary(a, static_cast<hipStream_t>(stream));
+  return launched();
+}
+
+int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, const int64_t* k_stride, const void* v,
+                     const int64_t* v_stride, int dtype, const int32_t* starts, int n, int tokens, int n_head,
+                     int n_kv_head, void* out, int clear, void* stream) {
+  size_t e;
+  if (int r = check_dtype(dtype, e)) return r;
+  if (int r = check_heads(n_head, n_kv_head)) return r;
+  if (n < 1 || n > (1 << 24)) return bad("n must be in [1, 2^24]");
+  if (tokens < 0 || tokens > (1 << 28)) return bad("tokens must be in [0, 2^28]");
+  if (!starts || !aligned(starts, 4)) return bad("starts must be aligned to its elements");
+  PromptArgs a{};
+  a.vec = 1;
+  if (int r = check_strides(q, q_stride, e, a.vec, 2)) return r;
+  if (int r = check_strides(k, k_stride, e, a.vec, 2)) return r;
+  if (int r = check_strides(v, v_stride, e, a.vec, 2)) return r;
+  if (!out || !aligned(out, 16)) return bad("out must be 16-byte aligned");
+  if (tokens == 0) return WF_OK;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.qt = q_stride[0];
+  a.qh = q_stride[1];
+  a.kt = k_stride[0];
+  a.kh = k_stride[1];
+  a.vt = v_stride[0];
+  a.vh = v_stride[1];
+  a.bf16_data = dtype == WF_BF16;
+  a.starts = starts;
+  a.n = n;
+  a.tokens = tokens;
+  a.heads = n_head;
+  a.group = n_head / n_kv_head;
+  a.out = out;
+  a.clear = clear != 0;
+  prompt_attend(a, static_cast<hipStream_t>(stream));
+  return launched();
+}
+
+int wf_kv8_page_bytes(int n_head, size_t* bytes) {
+  const wf_kv8 c{nullptr, 1, n_head};
+  if (int r = check_cache8(&c, false)) return r;
+  if (!bytes) return bad("null bytes");
+  *bytes = kv8_page_bytes(n_head);
+  return WF_OK;
+}
+
+int wf_kv8_store(const wf_kv8* c, int n, const void* k, const int64_t* k_stride, const void* v, const int64_t* v_stride,
+                 int dtype, int rows, const int32_t* starts, const int32_t* counts, const int32_t* tables,
+                 int64_t table_stride, int max_pages, const int32_t* positions, void* stream) {
+  size_t e;
+  if (int r = check_cache8(c)) return r;
+  if (int r = check_tables(n, tables, table_stride, max_pages)) return r;
+  if (int r = check_dtype(dtype, e)) return r;
+  if (starts && counts) return bad("starts and counts exclude each other");
+  if (rows < 0 || (starts ? rows > (1 << 27) : rows > (1 << 20) || (long long)n * ((rows + 30) / 16) > kMaxUnits))
+    return bad("rows out of range");
+  Kv8StoreArgs a{};
+  a.vec = 1;
+  if (int r = check_strides(k, k_stride, e, a.vec)) return r;
+  if (int r = check_strides(v, v_stride, e, a.vec)) return r;
+  if (!aligned(starts, 4) || !aligned(counts, 4) || !positions || !aligned(positions, 4))
+    return bad("starts, counts and positions must be aligned to their elements");
+  if (rows == 0) return WF_OK;
+  a.c = geometry(c);
+  a.k = k;
+  a.v = v;
+  a.bf16_src = dtype == WF_BF16;
+  a.kr = k_stride[0];
+  a.ki = k_stride[1];
+  a.kh = k_stride[2];
+  a.vr = v_stride[0];
+  a.vi = v_stride[1];
+  a.vh = v_stride[2];
+  a.rows = rows;
+  a.starts = starts;
+  a.counts = counts;
+  a.tables = tables;
+  a.ts = table_stride;
+  a.max_pages = max_pages;
+  a.n = n;
+  a.positions = positions;
+  kv8_store(a, static_cast<hipStream_t>(stream));
+  return launched();
+}
+
+int wf_kv8_load(const wf_kv8* c, int n, const int32_t* tables, int64_t table_stride, int max_pages, const int32_t* lens,
+                void* k, void* v, int dtype, void* stream) {
+  size_t e;
+  if (int r = check_cache8(c)) return r;
+  if (int r = check_tables(n, tables, table_stride, max_pages)) return r;
+  if ((long long)n * max_pages > kMaxUnits) return bad("n * max_pages must be below 2^24");
+  if (int r = check_dtype(dtype, e)) return r;
+  if (!lens || !aligned(lens, 4)) return bad("lens must be aligned to its elements");
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return bad("outputs must be 16-byte aligned");
+  Kv8LoadArgs a{};
+  a.c = geometry(c);
+  a.tables = tables;
+  a.ts = table_stride;
+  a.max_pages = max_pages;
+  a.n = n;
+  a.lens = lens;
+  a.k = k;
+  a.v = v;
+  a.bf16_out = dtype == WF_BF16;
+  kv8_load(a, static_cast<hipStream_t>(stream));
+  return launched();
+}
+
+int wf_kv8_attend_workspace_bytes(const wf_kv8* c, int n, int rows, int n_q_head, int max_pages, size_t* bytes) {
+  if (int r = check_cache8(c, false)) return r;
+  if (n < 1 || n > kMaxGrid) return bad("n must be in [1, 65535]");
+  if (int r = check_heads(n_q_head, c->n_head)) return r;
+  const int group = n_q_head / c->n_head;
+  if (rows < 1 || rows > (1 << 19) / group) return bad("rows times a group's heads must be in [1, 2^19]");
+  if (max_pages < 1 || max_pages > kKv8MaxPages) return bad("max_pages must be in [1, 2^24]");
+  if (!bytes) return bad("null bytes");
+  *bytes = kv8_workspace(n, rows, group, c->n_head, max_pages);
+  return WF_OK;
+}
+
+int wf_kv8_attend(const wf_kv8* c, int n, const void* q, const int64_t* q_stride, int rows, int n_q_head, int dtype,
+                  const int32_t* tables, int64_t table_stride, int max_pages, const int32_t* positions,
+                  const int32_t* counts, void* out, void* workspace, size_t ws_bytes, void* stream) {
+  size_t e, need;
+  if (int r = check_cache8(c)) return r;
+  if (int r = check_tables(n, tables, table_stride, max_pages)) return r;
+  if (int r = check_dtype(dtype, e)) return r;
+  if (int r = wf_kv8_attend_workspace_bytes(c, n, rows, n_q_head, max_pages, &need)) return r;
+  Kv8AttendArgs a{};
+  a.vec = 1;
+  if (int r = check_strides(q, q_stride, e, a.vec)) return r;
+  if (!positions || !aligned(positions, 4) || !aligned(counts, 4)) return bad("positions and counts must be aligned to their elements");
+  if (!out || !aligned(out, 16)) return bad("out must be 16-byte aligned");
+  if (need > 0 && (!workspace || !aligned(workspace, 256))) return bad("workspace must be 256-byte aligned");
+  if (ws_bytes < need) return op_fail(WF_ESIZE, "workspace too small");
+  a.c = geometry(c);
+  a.q = q;
+  a.sr = q_stride[0];
+  a.si = q_stride[1];
+  a.sh = q_stride[2];
+  a.bf16_q = dtype == WF_BF16;
+  a.rows = rows;
+  a.group = n_q_head / c->n_head;
+  a.n = n;
+  a.tables = tables;
+  a.ts = table_stride;
+  a.max_pages = max_pages;
+  a.positions = positions;
+  a.counts = counts;
+  a.out = out;
+  a.part = static_cast<float*>(workspace);
+  kv8_attend(a, static_cast<hipStream_t>(stream));
   return launched();
 }
 

@@ -1,5 +1,6 @@
 // Argument blocks and launchers of the stateless operators (internal): beam selection
-// and page reordering (k_beam.hip), the 4-bit acoustic cache (k_kv4.hip).
+// and page reordering (k_beam.hip), the 4-bit acoustic cache (k_kv4.hip), rotary positions
+// (k_rope.hip), packed prompts (k_prompt.hip), the 8-bit paged cache (k_kv8.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <string>
@@ -171,5 +172,94 @@ void kv4_attend(const Kv4AttendArgs& a, hipStream_t st);
 // attn_cross_merge (one request of at most nine rows).
 void kv4_attend_operand(const Kv4AttendArgs& a, hipStream_t st);
 void kv4_attend_records(const Kv4AttendArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- rotary positions
+struct RotaryRows {
+  const void* x;  // element (t, h, i) at t * xt + h * xh + i
+  void* y;
+  long long xt, xh, yt, yh;
+  int heads;
+};
+struct RotaryArgs {
+  const double* turns;  // [dims / 2]
+  int dims, interleaved, transposed, width;
+  float amplitude;
+  const int* positions;  // [tokens]
+  int tokens, bf16_data;
+  RotaryRows rows[2];
+  int n_rows;
+  int vec;     // rows may be read and written 16 bytes at a time
+  int copies;  // elements from dims on are copied (y is not x)
+  int tb;      // tokens of a block (set by the launcher)
+};
+void rotary(const RotaryArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- attention of packed prompts
+struct PromptArgs {
+  const void *q, *k, *v;  // element (t, h, d) at t * st + h * sh + d
+  long long qt, qh, kt, kh, vt, vh;
+  int bf16_data;
+  int vec;            // rows may be read 16 bytes at a time
+  const int* starts;  // [n + 1]
+  int n, tokens, heads, group;
+  void* out;          // [tokens][heads][64]
+  int clear;          // rows of no sequence are zeroed
+};
+void prompt_attend(const PromptArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- a paged cache in 8 bits
+// A page: per head kKv8Head bytes of codes, then per head the biased exponents of its keys' and
+// its values' scale, then zeros to a multiple of 16 bytes.  Codes in the order in which a wave's
+// lanes multiply them:
+//   keys    byte 16 (16 (d / 16) + j) + d % 16: dim d of position j
+//   values  byte 1024 + 32 (16 (j / 8) + d / 4) + 8 (d % 4) + j % 8
+constexpr int kKv8Values = 1024, kKv8Head = 2048;
+constexpr int kKv8MaxPages = 1 << 24, kKv8MaxHeads = 4096;
+__host__ __device__ inline size_t kv8_page_bytes(int n_head) { return (size_t)n_head * kKv8Head + (((size_t)n_head * 2 + 15) & ~(size_t)15); }
+struct Kv8 {
+  uint8_t* base;
+  int n_pages, n_head;
+  size_t page;  // bytes of a page
+};
+struct Kv8StoreArgs {
+  Kv8 c;
+  const void *k, *v;  // element (r, i, h, d) at r * sr + i * si + h * sh + d
+  int bf16_src;
+  long long kr, ki, kh, vr, vi, vh;
+  int rows;
+  const int *starts, *counts;
+  const int* tables;
+  long long ts;
+  int max_pages, n;
+  const int* positions;
+  int vec;
+};
+void kv8_store(const Kv8StoreArgs& a, hipStream_t st);
+struct Kv8LoadArgs {
+  Kv8 c;
+  const int* tables;
+  long long ts;
+  int max_pages, n;
+  const int* lens;
+  void *k, *v;  // [n][16 max_pages][n_head][64]
+  int bf16_out;
+};
+void kv8_load(const Kv8LoadArgs& a, hipStream_t st);
+struct Kv8AttendArgs {
+  Kv8 c;
+  const void* q;  // element (r, i, h, d) at r * sr + i * si + h * sh + d
+  long long sr, si, sh;
+  int bf16_q, vec;
+  int rows, group, n;
+  const int* tables;
+  long long ts;
+  int max_pages;
+  const int *positions, *counts;
+  void* out;    // [n][rows][n_head * group][64], the query's type
+  float* part;  // chunk records (nchunk > 1)
+  int nchunk;   // set by the launcher
+};
+size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages);
+void kv8_attend(const Kv8AttendArgs& a, hipStream_t st);
 
 }  // namespace wf

@@ -1,5 +1,6 @@
-"""Operators without a handle (include/wf.h): beam selection, page-table reordering and
-acoustic keys and values held in 4 bits.
+"""Operators without a handle (include/wf.h): beam selection, page-table reordering,
+acoustic keys and values held in 4 bits, and a decoder's self-attention: rotary positions,
+attention over packed prompts and a paged cache in 8 bits.
 
 Argument marshalling as in ``binding``: shapes, types and devices are checked here, sizes
 and ranges by the library.  Every call enqueues on ``stream`` (default: the current stream
@@ -8,15 +9,15 @@ behind the work that fills the tensors.  Workspaces and results come from PyTorc
 allocator for the call's stream, so concurrent calls and captured graphs each have their
 own.
 
-There are no backward passes.  Results of inputs that require gradients raise where a
-gradient is asked of them; what a cache stores or copies has no history.
+Rotary positions have a backward pass, the others none: their results of inputs that require
+gradients raise where a gradient is asked of them; what a cache stores or copies has no history.
 """
 import ctypes
 import functools
 
 import torch
 
-from .binding import WF_BF16, WF_F32, WfError, WfKv4, _refuse, _tensor, load_library
+from .binding import WF_BF16, WF_F32, WfError, WfKv4, WfKv8, WfRotaryRows, _refuse, _tensor, load_library
 
 try:  # torch.cuda.current_stream() and current_device() without their objects and checks (2.7 and 0.1 us)
     from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _device
@@ -286,4 +287,266 @@ class AcousticCache4:
             return out
 
         out = _enqueue(self.device, stream, call, q, lens, self.data)
+        return _without_backward("attend", out, q) if q.requires_grad else out
+
+
+_Strides2 = ctypes.c_int64 * 2
+_SCALINGS = {None: 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+def _heads(t, name, axes, width=64):
+    """Device, type and strides of [..., heads, width] of `axes` axes, the last one contiguous."""
+    dev = _gpu(t, name, axes)
+    if width is not None and t.shape[-1] != width:
+        _refuse(f"{name} must have a last axis of {width}, not {t.shape[-1]}")
+    s = t.stride()
+    if s[-1] != 1 and t.shape[-1] > 1:
+        _refuse(f"{name} must be contiguous along its last axis")
+    if max(t.shape) >= _INTS:
+        _refuse("a size is out of range")
+    return dev, _type(t, name), s[:-1]
+
+
+class _Rotate(torch.autograd.Function):
+    """Rotated tensors as a function of them; the gradient turns the other way."""
+
+    @staticmethod
+    def forward(ctx, rotary, positions, transposed, stream, *tensors):
+        ctx.rotary, ctx.transposed = rotary, transposed
+        ctx.save_for_backward(positions)
+        return rotary._turn(positions, tensors, transposed, None, stream)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        (positions,) = ctx.saved_tensors
+        need = [i for i, g in enumerate(grads) if ctx.needs_input_grad[4 + i]]
+        turned = _Rotate.apply(ctx.rotary, positions, not ctx.transposed, None,
+                               *(g if g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous() for g in (grads[i] for i in need)))
+        out = [None] * len(grads)
+        for i, t in zip(need, turned):
+            out[i] = t
+        return (None, None, None, None, *out)
+
+
+class Rotary:
+    """Rotary positions of heads' first `dims` elements (wf_rotary): pairs (i, i + dims / 2) or, interleaved,
+    (2 i, 2 i + 1).  scaling for long contexts: None, "linear" or "base" by `factor`, or "ramp" (by parts, from pairs
+    that turn `low` times within `context` positions to those that turn `high` times): wf_rotary_turns."""
+
+    def __init__(self, dims, base=10000.0, interleaved=False, scaling=None, factor=1.0, context=0, low=1.0, high=32.0, device="cuda"):
+        self.lib = load_library()
+        self.dims, self.interleaved = int(dims), bool(interleaved)
+        if abs(self.dims) >= _INTS:
+            _refuse("a size is out of range")
+        if scaling not in _SCALINGS:
+            _refuse("scaling must be None, 'linear', 'base' or 'ramp'")
+        turns = (ctypes.c_double * (max(2, min(self.dims, 4096)) // 2))()
+        amplitude = ctypes.c_float()
+        _check(self.lib.wf_rotary_turns(self.dims, base, _SCALINGS[scaling], factor, context, low, high, turns, ctypes.byref(amplitude)))
+        self.amplitude = amplitude.value
+        self.turns = torch.tensor(list(turns), dtype=torch.float64, device=device)
+        if not self.turns.is_cuda:
+            _refuse("device must be a GPU")
+        self.device = self.turns.device
+
+    def rotate(self, positions, q, k=None, in_place=False, stream=None):
+        """q, and k beside it, at their positions: q, k fp32 or bf16 [tokens, heads, width] of the same tokens, width and
+        type (any strides but the last); positions int32 [tokens].  Returns new tensors, or the given ones changed in place
+        (without gradients): the rotated q, or (q, k)."""
+        tensors = (q,) if k is None else (q, k)
+        if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
+            if in_place:
+                _refuse("tensors that require gradients are not changed in place")
+            out = _Rotate.apply(self, positions, False, stream, *tensors)
+        else:
+            out = self._turn(positions, tensors, False, tensors if in_place else None, stream)
+        return out[0] if k is None else out
+
+    def _turn(self, positions, tensors, transposed, outs, stream):
+        first = tensors[0]
+        rows = (WfRotaryRows * len(tensors))()
+        for i, (t, name) in enumerate(zip(tensors, "qk")):
+            dev, dtype, strides = _heads(t, name, 3, None)
+            if dev != self.device:
+                _refuse(f"{name} must be on {self.device}, not {dev}")
+            if t.shape[0] != first.shape[0] or t.shape[2] != first.shape[2] or t.dtype != first.dtype:
+                _refuse("k must have q's tokens, width and type")
+            rows[i].x, rows[i].x_stride, rows[i].heads = t.data_ptr(), _Strides2(*strides), t.shape[1]
+        tokens, _, width = first.shape
+        _tensor(positions, "positions", _I32, (tokens,), self.device)
+
+        def call(raw, empty):
+            result = outs if outs is not None else tuple(empty(t.shape, dtype=t.dtype, device=self.device) for t in tensors)
+            for r, t in zip(rows, result):
+                r.y, r.y_stride = t.data_ptr(), _Strides2(*t.stride()[:2])
+            if tokens:
+                _check(self.lib.wf_rotary(self.turns.data_ptr(), self.dims, self.interleaved, self.amplitude, transposed,
+                                          positions.data_ptr(), tokens, width, dtype, rows, len(tensors), raw))
+            return result
+
+        result = _enqueue(self.device, stream, call, positions, self.turns, *tensors)
+        if outs is not None:  # autograd's count of changes
+            torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+        return result
+
+
+def prompt_attention(q, k, v, starts, out=None, stream=None):
+    """Causal attention of packed prompts: wf_prompt_attend.
+
+    q: fp32 or bf16 [tokens, n_head, 64]; k, v: [tokens, n_kv_head, 64] in the same type (any strides but the last);
+    starts: int32 [n + 1], sequence s holds the rows starts[s] .. starts[s + 1] - 1.  Returns [tokens, n_head, 64]: rows of
+    no sequence are zeros, or stay as they are in a given contiguous `out`.
+    """
+    lib = load_library()
+    dev, dtype, qs = _heads(q, "q", 3)
+    tokens, heads, _ = q.shape
+    strides = []
+    for t, name in ((k, "k"), (v, "v")):
+        d, code, s = _heads(t, name, 3)
+        if d != dev or code != dtype or t.shape[0] != tokens or t.shape[1] != k.shape[1]:
+            _refuse("k and v must have q's device, type and tokens, and as many heads")
+        strides.append(_Strides2(*s))
+    if _gpu(starts, "starts", 1) != dev or starts.shape[0] < 2:
+        _refuse(f"starts must hold two borders at least, on {dev}")
+    n = starts.shape[0] - 1
+    _tensor(starts, "starts", _I32, (n + 1,), dev)
+    wants = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
+    if out is not None:
+        _tensor(out, "out", q.dtype, (tokens, heads, 64), dev)
+        if wants or out.requires_grad:
+            _refuse("prompt_attention into a given tensor has no gradient")
+
+    def call(raw, empty):
+        o = out if out is not None else empty((tokens, heads, 64), dtype=q.dtype, device=dev)
+        if tokens:
+            _check(lib.wf_prompt_attend(q.data_ptr(), _Strides2(*qs), k.data_ptr(), strides[0], v.data_ptr(), strides[1], dtype,
+                                        starts.data_ptr(), n, tokens, heads, k.shape[1], o.data_ptr(), out is None, raw))
+        return o
+
+    o = _enqueue(dev, stream, call, q, k, v, starts, out)
+    if out is not None and not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+    return _without_backward("prompt_attention", o, q, k, v) if wants else o
+
+
+class PagedCache8:
+    """Self-attention keys and values in 8 bits (wf_kv8): `layers` layers of `pages` pages of 16 positions of n_head heads of
+    64.  data: uint8 [layers, pages, bytes of a page], what cache_reorder takes as its cache; requests' page numbers lie in
+    tables, int32 [n, max_pages] (rows of any stride), the same for every layer."""
+
+    PAGE = 16
+
+    def __init__(self, pages, n_head, layers=1, device="cuda"):
+        self.lib = load_library()
+        self.pages, self.n_head, self.layers = int(pages), int(n_head), int(layers)
+        if max(abs(self.pages), abs(self.n_head), abs(self.layers)) >= _INTS:
+            _refuse("a size is out of range")
+        nbytes = ctypes.c_size_t()
+        _check(self.lib.wf_kv8_page_bytes(self.n_head, ctypes.byref(nbytes)))
+        if not 1 <= self.pages <= 1 << 24 or self.layers < 1:
+            _refuse("pages must be in [1, 2^24] and layers 1 or more")
+        self.data = torch.empty((self.layers, self.pages, nbytes.value), dtype=_U8, device=device)
+        if not self.data.is_cuda:
+            _refuse("device must be a GPU")
+        self.device = self.data.device
+        base, layer = self.data.data_ptr(), self.pages * nbytes.value
+        self._c = [WfKv8(base + i * layer, self.pages, self.n_head) for i in range(self.layers)]
+        self._refs = [ctypes.byref(c) for c in self._c]
+        self._spaces = {}  # workspace bytes of (n, rows, heads, max_pages)
+
+    def _layer(self, layer):
+        if not 0 <= layer < self.layers:
+            _refuse(f"layer must be in [0, {self.layers})")
+        return self._refs[layer]
+
+    def _tables(self, tables):
+        """Requests, pages of a row and its stride."""
+        if _gpu(tables, "tables", 2) != self.device or tables.dtype != _I32:
+            _refuse(f"tables must be int32 on {self.device}")
+        n, most = tables.shape
+        if most > 1 and tables.stride(1) != 1:
+            _refuse("tables must be contiguous along its last axis")
+        if max(n, most) >= _INTS:
+            _refuse("a size is out of range")
+        return n, most, tables.stride(0)
+
+    def _vector(self, t, name, n):
+        if t is None:
+            return None
+        _tensor(t, name, _I32, (n,), self.device)
+        return t.data_ptr()
+
+    def store(self, k, v, tables, positions, starts=None, counts=None, layer=0, stream=None):
+        """Append rows to requests' pages from positions (int32 [n]) on.  k, v: fp32 or bf16, any strides but the last:
+        packed [rows, n_head, 64] with starts (int32 [n + 1]), or [n, rows, n_head, 64], of which request r's first counts[r]
+        (int32 [n], None: all) are given."""
+        ref = self._layer(layer)
+        n, most, ts = self._tables(tables)
+        axes = 4 if starts is None else 3
+        strides = []
+        for t, name in ((k, "k"), (v, "v")):
+            dev, code, s = _heads(t, name, axes)
+            if dev != self.device or t.shape != k.shape or t.dtype != k.dtype or t.shape[-2] != self.n_head:
+                _refuse(f"k and v must have equal shapes and types, {self.n_head} heads, and lie on {self.device}")
+            strides.append(_Strides(*s) if starts is None else _Strides(0, *s))
+        if starts is None and k.shape[0] != n:
+            _refuse(f"k must hold {n} requests, not {k.shape[0]}")
+        if starts is not None and counts is not None:
+            _refuse("starts and counts exclude each other")
+        pstarts, pcounts = self._vector(starts, "starts", n + 1), self._vector(counts, "counts", n)
+        if positions is None:
+            _refuse("positions must be a tensor")
+        at, rows = self._vector(positions, "positions", n), k.shape[-3]
+        if rows == 0:
+            return
+        _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv8_store(
+            ref, n, k.data_ptr(), strides[0], v.data_ptr(), strides[1], code, rows, pstarts, pcounts, tables.data_ptr(), ts, most, at,
+            raw)), k, v, tables, positions, starts, counts, self.data)
+
+    def load(self, tables, lens, dtype=torch.float32, layer=0, stream=None):
+        """The keys and values that the first lens[r] (int32 [n]) positions of requests' pages hold: two tensors
+        [n, 16 max_pages, n_head, 64], zeros behind them."""
+        ref = self._layer(layer)
+        if dtype not in _DTYPES:
+            _refuse("dtype must be float32 or bfloat16")
+        n, most, ts = self._tables(tables)
+        if lens is None:
+            _refuse("lens must be a tensor")
+        plens = self._vector(lens, "lens", n)
+
+        def call(raw, empty):
+            k = empty((n, 16 * most, self.n_head, 64), dtype=dtype, device=self.device)
+            v = empty((n, 16 * most, self.n_head, 64), dtype=dtype, device=self.device)
+            _check(self.lib.wf_kv8_load(ref, n, tables.data_ptr(), ts, most, plens, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], raw))
+            return k, v
+
+        return _enqueue(self.device, stream, call, tables, lens, self.data)
+
+    def attend(self, q, tables, positions, counts=None, layer=0, stream=None):
+        """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, heads, 64], any strides but the last; heads a multiple of the
+        cache's): row i of request r stands at positions[r] + i (int32 [n]) and sees positions up to its own.  Rows from
+        counts[r] (int32 [n], None: all) on give zeros.  Returns [n, rows, heads, 64] in q's type."""
+        ref = self._layer(layer)
+        n, most, ts = self._tables(tables)
+        dev, dtype, s = _heads(q, "q", 4)
+        if dev != self.device or q.shape[0] != n:
+            _refuse(f"q must hold {n} requests on {self.device}")
+        rows, heads = q.shape[1:3]
+        need = self._spaces.get((n, rows, heads, most))
+        if need is None:
+            nbytes = ctypes.c_size_t()
+            _check(self.lib.wf_kv8_attend_workspace_bytes(ref, n, rows, heads, most, ctypes.byref(nbytes)))
+            need = self._spaces[n, rows, heads, most] = nbytes.value
+        if positions is None:
+            _refuse("positions must be a tensor")
+        at, pcounts = self._vector(positions, "positions", n), self._vector(counts, "counts", n)
+
+        def call(raw, empty):
+            out = empty((n, rows, heads, 64), dtype=q.dtype, device=self.device)
+            ws = empty(need, dtype=_U8, device=self.device) if need else None
+            _check(self.lib.wf_kv8_attend(ref, n, q.data_ptr(), _Strides(*s), rows, heads, dtype, tables.data_ptr(), ts, most, at, pcounts,
+                                          out.data_ptr(), ws.data_ptr() if need else None, need, raw))
+            return out
+
+        out = _enqueue(self.device, stream, call, q, tables, positions, counts, self.data)
         return _without_backward("attend", out, q) if q.requires_grad else out

@@ -1,0 +1,849 @@
+"""Rotary positions, packed prompts and the 8-bit paged cache on the GPU against their plain 64-bit forms
+(oracle/operators.py)."""
+import copy
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as plain
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def lib():
+    import paper_2609_32869_amd as wf
+    return wf
+
+
+def num(t):
+    return t.detach().double().cpu().numpy()
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x).tolist(), dtype=torch.int32, device="cuda")
+
+
+def half(dtype):
+    """A rounding's largest relative error."""
+    return torch.finfo(dtype).eps / 2
+
+
+# ---------------------------------------------------------------- rotary positions
+
+def check_rotary(got, x, positions, kw, dims, transposed=False):
+    """A sine and a cosine are off by less than 2^-21 (the angle's two roundings, 2^-24 of up to pi / 4 each, and six
+    steps of a polynomial), a result by three roundings more of at most A (|a| + |b|); then one to the type."""
+    inter = kw.get("interleaved", False)
+    t, amplitude = plain.rotary_turns(dims, **{k: v for k, v in kw.items() if k != "interleaved"})
+    want = plain.rotary(num(x), positions, t, amplitude, inter, transposed)
+    size = np.abs(num(x))
+    pair = size.copy()
+    a, b = (slice(0, dims, 2), slice(1, dims, 2)) if inter else (slice(0, dims // 2), slice(dims // 2, dims))
+    pair[..., a] = pair[..., b] = size[..., a] + size[..., b]
+    pair[..., dims:] = 0
+    err = np.abs(num(got) - want)
+    assert (err <= amplitude * 2.0 ** -20 * pair + (half(x.dtype) * np.abs(want)) * (pair != 0)).all(), err.max()
+
+
+SCALINGS = [{}, dict(scaling="linear", factor=4.0), dict(scaling="base", factor=8.0), dict(scaling="ramp", factor=16.0, context=2048)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("tokens,heads,kv,width,dims", [
+    (1, 1, 1, 2, 2), (1, 20, 20, 64, 64), (7, 6, 2, 64, 32), (3, 5, 1, 63, 10), (65, 3, 3, 64, 62), (1000, 2, 2, 64, 64), (5, 4, 4, 128, 96),
+    (2, 3, 1, 4096, 4096), (33, 32, 8, 64, 48), (17, 1, 1, 80, 80), (2, 7, 7, 64, 4)])
+def test_rotary(tokens, heads, kv, width, dims, inter, dtype):
+    g = torch.Generator("cuda").manual_seed(tokens * 100 + dims)
+    kw = dict(SCALINGS[(tokens + heads + dims) % 4], interleaved=inter)
+    if dims == 2:
+        kw = dict(interleaved=inter)
+    q = torch.randn((tokens, heads, width), device="cuda", generator=g).to(dtype)
+    k = torch.randn((tokens, kv, width), device="cuda", generator=g).to(dtype)
+    at = torch.randint(0, 1 << 17, (tokens,), device="cuda", generator=g, dtype=torch.int32)
+    rot = lib().Rotary(dims, **kw)
+    a, b = rot.rotate(at, q, k)
+    check_rotary(a, q, at.cpu().numpy(), kw, dims)
+    check_rotary(b, k, at.cpu().numpy(), kw, dims)
+    assert torch.equal(rot.rotate(at, k), b)
+    assert rot.rotate(at, q, k, in_place=True)[0] is q and torch.equal(q, a) and torch.equal(k, b)
+
+
+def test_rotary_positions():
+    """Any 32-bit position: the angle's whole turns come off exactly."""
+    at = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 1 << 20, 123456789, 447, 65535]
+    x = torch.randn((len(at), 3, 64), device="cuda", generator=torch.Generator("cuda").manual_seed(0))
+    for kw in SCALINGS:
+        rot = lib().Rotary(64, **kw)
+        y = rot.rotate(i32(at), x)
+        t, amplitude = plain.rotary_turns(64, **kw)
+        # angles of far positions: 2^31 positions of up to 1 / (2 pi) turns each, to 2^-53 (three roundings): 6e-8 turns
+        want = plain.rotary(num(x), at, t, amplitude, False)
+        size = np.abs(num(x)).reshape(len(at), 3, 2, 32).sum(2, keepdims=True).repeat(2, 2).reshape(want.shape)
+        far = 2 * np.pi * 3 * 2.0 ** -53 * np.abs(np.array(at, float))[:, None, None] / (2 * np.pi)
+        assert (np.abs(num(y) - want) <= amplitude * size * (2.0 ** -20 + far)).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("offset", [0, 1, 8])
+def test_rotary_strides(dtype, offset):
+    """Slices of a projection's output, heads before tokens, rows off a 16-byte border; nothing else changes in place."""
+    g = torch.Generator("cuda").manual_seed(offset)
+    rot = lib().Rotary(64)
+    at = torch.arange(11, dtype=torch.int32, device="cuda")
+    buf = torch.randn(offset + 11 * 12 * 64 + 64, device="cuda", generator=g).to(dtype)
+    was = buf.clone()
+    qkv = buf[offset:offset + 11 * 12 * 64].view(11, 12, 64)
+    a, b = rot.rotate(at, qkv[:, :8], qkv[:, 8:10])
+    check_rotary(a, qkv[:, :8], at.cpu().numpy(), {}, 64)
+    rot.rotate(at, qkv[:, :8], qkv[:, 8:10], in_place=True)
+    assert torch.equal(qkv[:, :8], a) and torch.equal(qkv[:, 8:10], b)
+    now = was[offset:offset + 11 * 12 * 64].view(11, 12, 64)
+    now[:, :8], now[:, 8:10] = a, b
+    assert torch.equal(buf, was)
+    x = torch.randn((3, 11, 70), device="cuda", generator=g).to(dtype)[:, :, 3:67].transpose(0, 1)
+    check_rotary(rot.rotate(at, x), x, at.cpu().numpy(), {}, 64)
+    one = torch.randn((11, 1, 64), device="cuda", generator=g).to(dtype)
+    check_rotary(rot.rotate(at, one.expand(11, 5, 64)), one.expand(11, 5, 64), at.cpu().numpy(), {}, 64)
+
+
+def test_rotary_no_tokens_and_large_grids():
+    rot = lib().Rotary(2)
+    assert rot.rotate(i32([]), torch.empty((0, 3, 64), device="cuda")).shape == (0, 3, 64)
+    n = (1 << 24) + 5                                        # blocks past one axis of a grid
+    x = torch.ones((n, 1, 2), device="cuda", dtype=BF16)
+    at = torch.arange(n, dtype=torch.int32, device="cuda")
+    y = rot.rotate(at, x)
+    rows = [0, 1, 99999, 1 << 20, 1 << 24, n - 1]
+    check_rotary(y[rows], x[rows], rows, {}, 2)
+
+
+def test_rotary_offsets_past_32_bits():
+    far = (1 << 31) + 64
+    buf = torch.empty(far + 64 * 3, dtype=BF16, device="cuda")
+    x = buf.as_strided((2, 3, 64), (far, 64, 1))
+    x.copy_(torch.randn((2, 3, 64), device="cuda"))
+    want = lib().Rotary(64).rotate(i32([5, 6]), x.contiguous())
+    lib().Rotary(64).rotate(i32([5, 6]), x, in_place=True)
+    assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kw", [dict(), dict(interleaved=True, scaling="ramp", factor=4.0, context=64)])
+def test_rotary_gradient(dtype, kw):
+    """The gradient of y . w is the transposed rotation of w; against differences in fp32 (linear: exact up to rounding)."""
+    g = torch.Generator("cuda").manual_seed(1)
+    rot, at = lib().Rotary(32, **kw), i32([3, 0, 1000, 77])
+    q = torch.randn((4, 3, 64), device="cuda", generator=g).to(dtype).requires_grad_()
+    k = torch.randn((4, 1, 64), device="cuda", generator=g).to(dtype).requires_grad_()
+    wq = torch.randn((4, 3, 64), device="cuda", generator=g).to(dtype)
+    wk = torch.randn((64, 4, 1), device="cuda", generator=g).to(dtype).permute(1, 2, 0)      # a gradient of other strides
+    a, b = rot.rotate(at, q, k)
+    gq, gk = torch.autograd.grad([a, b], [q, k], [wq, wk])
+    check_rotary(gq, wq, at.cpu().numpy(), kw, 32, transposed=True)
+    check_rotary(gk, wk, at.cpu().numpy(), kw, 32, transposed=True)
+    if dtype == F32:
+        d = torch.randn(q.shape, device="cuda", generator=g)
+        up, down = (num(rot.rotate(at, (q + s * d).detach())) for s in (1, -1))
+        assert np.isclose(((up - down) * num(wq)).sum() / 2, (num(gq) * num(d)).sum(), rtol=1e-5, atol=1e-4)
+        z = wq.clone().requires_grad_()
+        (h,) = torch.autograd.grad(rot.rotate(at, q), q, z, create_graph=True)       # linear: its gradient is the rotation
+        (hz,) = torch.autograd.grad(h, z, d)
+        check_rotary(hz, d, at.cpu().numpy(), kw, 32)
+    rot.rotate(at, q).sum().backward()                       # an expanded gradient; only one tensor
+    check_rotary(q.grad, torch.ones_like(q), at.cpu().numpy(), kw, 32, transposed=True)
+    k.grad = None
+    a, b = rot.rotate(at, q.detach(), k)
+    b.sum().backward()
+    check_rotary(k.grad, torch.ones_like(k), at.cpu().numpy(), kw, 32, transposed=True)
+
+
+def test_rotary_gradient_refusals():
+    wf = lib()
+    rot, at = wf.Rotary(64), i32([1, 2])
+    q = torch.randn((2, 3, 64), device="cuda", requires_grad=True)
+    with pytest.raises(wf.WfError, match="in place"):
+        rot.rotate(at, q, in_place=True)
+    with torch.no_grad():
+        rot.rotate(at, q, in_place=True)
+    y = rot.rotate(at, q)
+    at += 1                                                  # the backward pass needs the positions as they were
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.sum().backward()
+    p = torch.randn((2, 3, 64), device="cuda", requires_grad=True)
+    x = (p * 1.0).detach().requires_grad_()
+    z = (x * x)
+    with torch.no_grad():
+        rot.rotate(at, x, in_place=True)                     # x is what z's backward pass reads
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        z.sum().backward()
+
+
+# ---------------------------------------------------------------- packed prompts
+
+def bound(want, spread, size, terms, dtype, rounded=False):
+    """A score is off by the roundings of its 64 products' sum, twice over for a split operand: 2^-17 of the sum of
+    magnitudes; probabilities by twice that, an exponential's 2^-21 and a sum of `terms` values, 2^-24 each, once for
+    the total and once for the product; rounded: probabilities in bf16.  Then one rounding to the type."""
+    share = 2 * (2.0 ** -17 * size[..., None] + 2.0 ** -21 + terms * 2.0 ** -24) + (2.0 ** -8 if rounded else 0)
+    return share * spread + half(dtype) * np.abs(want) * (1 + share)
+
+
+def check_prompt(q, k, v, starts, out=None, stream=None):
+    got = lib().prompt_attention(q, k, v, i32(starts), out=out, stream=stream)
+    want, spread, size = plain.prompt_attention(num(q), num(k), num(v), starts)
+    g = num(got)
+    if out is not None:
+        return g, want
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[np.isinf(want)], want[np.isinf(want)])
+    err = np.abs(np.where(fine, g, 0) - np.where(fine, want, 0))
+    tol = bound(np.where(fine, want, 0), np.where(np.isfinite(spread), spread, 0), size, len(q), q.dtype, q.dtype == BF16)
+    assert (err <= tol).all(), (err.max(), (err / np.maximum(tol, 1e-30)).max())
+    return g, want
+
+
+def packed(T, H, KV, dtype, seed=0, scale=1.0):
+    g = torch.Generator("cuda").manual_seed(seed + T)
+    return [(scale if h == H else 1.0) * torch.randn((T, h, 64), device="cuda", generator=g).to(dtype) for h in (H, KV, KV)]
+
+
+def borders(lens, first=0):
+    return [first + int(sum(lens[:i])) for i in range(len(lens) + 1)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens,H,KV", [
+    ([1], 1, 1), ([2], 2, 1), ([31], 2, 2), ([32], 1, 1), ([33], 3, 1), ([64], 2, 2), ([65], 2, 1), ([127], 1, 1), ([128], 2, 2), ([129], 4, 2), ([255], 1, 1),
+    ([257], 2, 1), ([300, 1, 0, 0, 7, 63, 64, 65], 4, 2), ([1] * 70, 2, 2), ([0, 0, 5, 0], 6, 1), ([100, 28, 128, 3], 2, 2), ([0], 1, 1), ([448, 224], 20, 20),
+    ([600, 520], 1, 1), ([3, 500, 2], 7, 1)])
+def test_prompt(lens, H, KV, dtype):
+    T = max(1, sum(lens))
+    check_prompt(*packed(T, H, KV, dtype), borders(lens))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_rows_of_no_sequence(dtype):
+    """Rows before the first and behind the last sequence: zeros in a new result, untouched in a given one, and whatever
+    they hold stays out of the others."""
+    for first, rest in ((3, 5), (0, 200), (130, 0), (40, 300)):
+        lens = [70, 1, 33]
+        T = first + sum(lens) + rest
+        q, k, v = packed(T, 4, 2, dtype)
+        for t in (q, k, v):
+            t[:first] = NAN
+            t[first + sum(lens):] = INF
+        starts = borders(lens, first)
+        got, _ = check_prompt(q, k, v, starts)
+        out = torch.full_like(q, 7.0)
+        same, _ = check_prompt(q, k, v, starts, out=out)
+        assert (same[:first] == 7).all() and (same[first + sum(lens):] == 7).all()
+        assert np.array_equal(same[first:first + sum(lens)], got[first:first + sum(lens)])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [40, 200, 700])
+def test_prompt_what_is_masked_may_hold_anything(dtype, T):
+    """NaN and infinities in later rows and in other sequences: rows that do not see them are as without them, those that
+    do have what the definition gives."""
+    lens = [T // 3, T - T // 3 - 5, 5]
+    starts = borders(lens)
+    for name, at, value in (("v", T // 2, NAN), ("v", T // 2, INF), ("k", T // 2, NAN), ("v", T // 3 - 1, -INF), ("v", T // 3, NAN),
+                            ("k", T - 6, INF), ("v", T - 1, INF), ("q", T // 2, NAN)):
+        x = dict(zip("qkv", packed(T, 2, 1, dtype, seed=at)))
+        clean = lib().prompt_attention(*x.values(), i32(starts))
+        x[name][at, :, 5:9] = value
+        got = lib().prompt_attention(*x.values(), i32(starts))
+        end = next(b for b in starts if b > at)
+        sees = torch.zeros(T, dtype=torch.bool)
+        sees[at:at + 1 if name == "q" else end] = True
+        assert torch.equal(got[~sees.cuda()], clean[~sees.cuda()]), (name, at, value)
+        if name == "v":
+            check_prompt(*x.values(), starts)
+            assert not torch.isfinite(got[sees.cuda()][:, :, 5:9]).any() and torch.isfinite(got[sees.cuda()][:, :, 9:]).all()
+        else:
+            assert not torch.isfinite(got[at]).any()
+    x = dict(zip("qkv", packed(T, 2, 1, dtype, seed=9)))   # both infinities: NaN where a row sees both
+    x["v"][T // 2, 0, 3], x["v"][T // 2 + 2, 0, 3], x["v"][T // 2 + 3, 0, 4] = INF, -INF, INF
+    check_prompt(*x.values(), starts)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [30.0, 1e4, 1e-30])
+def test_prompt_scores_of_any_magnitude(dtype, scale):
+    """One key takes all, or all take the same; the running maximum moves late (keys that grow along the sequence)."""
+    q, k, v = packed(333, 2, 2, dtype, scale=scale)
+    k *= torch.linspace(0.1, 1.5, 333, device="cuda")[:, None, None]
+    q, k = q.to(dtype), k.to(dtype)
+    got = num(lib().prompt_attention(q, k, v, i32([0, 333])))
+    want, spread, size = plain.prompt_attention(num(q), num(k), num(v), [0, 333])
+    # a score is off by 2^-17 of its magnitudes at most: where that is more than the gap to the next key, either may win
+    ok = 2.0 ** -17 * size < 0.01
+    assert ok.any() or scale == 1e4
+    tol = bound(want, spread, size, 333, dtype, dtype == BF16)
+    assert (np.abs(got - want) <= tol)[ok].all() and np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("offset", [0, 1, 4])
+def test_prompt_strides(dtype, offset):
+    T, H, KV = 150, 4, 2
+    g = torch.Generator("cuda").manual_seed(offset)
+    buf = torch.randn(offset + T * 8 * 64, device="cuda", generator=g).to(dtype)
+    qkv = buf[offset:].view(T, 8, 64)
+    check_prompt(qkv[:, :H], qkv[:, H:H + KV], qkv[:, H + KV:], [0, 100, 150])
+    x = torch.randn((H, T, 66), device="cuda", generator=g).to(dtype)[:, :, 1:65].transpose(0, 1)
+    y = torch.randn((T, 1, 64), device="cuda", generator=g).to(dtype).expand(T, KV, 64)
+    check_prompt(x, y, x[:, :KV], [0, 149])
+
+
+def test_prompt_offsets_past_32_bits():
+    far = (1 << 28) + 64
+    buf = torch.empty(9 * far + 256, dtype=BF16, device="cuda")
+    x = buf.as_strided((10, 4, 64), (far, 64, 1))
+    x.copy_(torch.randn((10, 4, 64), device="cuda"))
+    check_prompt(x[:, :2], x[:, 2:3], x[:, 3:], [0, 10])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_many_sequences(dtype):
+    rng = np.random.default_rng(5)
+    lens = rng.integers(0, 4, 3000).tolist()
+    check_prompt(*packed(sum(lens), 1, 1, dtype), borders(lens))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_odd_borders(dtype):
+    """Borders outside the rows count as far as they are inside; others read nothing outside the tensors."""
+    q, k, v = packed(100, 2, 1, dtype)
+    f = lib().prompt_attention
+    assert torch.equal(f(q, k, v, i32([-5, 40, 200])), f(q, k, v, i32([0, 40, 100])))
+    assert not f(q, k, v, i32([200, 300])).any() and not f(q, k, v, i32([-9, -2])).any()
+    for starts in ([50, 20, 80, 10, 100], [0, 2 ** 31 - 1, -2 ** 31, 100], [100, 0]):
+        f(q, k, v, i32(starts))
+    assert f(q[:0], k[:0], v[:0], i32([0, 0])).shape == (0, 2, 64)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_prompt_long(dtype):
+    """Rows of a long prompt, each against 64 bits."""
+    T = 9000
+    q, k, v = packed(T, 2, 1, dtype)
+    got = lib().prompt_attention(q, k, v, i32([0, T]))
+    for i in (0, 1, 4095, 4096, 7777, T - 1):
+        want, spread, size = plain.seen_attention(num(q[i:i + 1]), num(k), num(v), np.arange(T)[None] <= i)
+        assert (np.abs(num(got[i:i + 1]) - want) <= bound(want, spread, size, T, dtype, dtype == BF16)).all()
+
+
+def test_prompt_refuses_gradients():
+    wf = lib()
+    q, k, v = packed(10, 2, 1, F32)
+    k.requires_grad_()
+    y = wf.prompt_attention(q, k, v, i32([0, 10]))
+    with pytest.raises(wf.WfError, match="no backward"):
+        y.sum().backward()
+    with pytest.raises(wf.WfError, match="no gradient"):
+        wf.prompt_attention(q, k, v, i32([0, 10]), out=torch.empty_like(q))
+    with torch.no_grad():
+        assert torch.equal(wf.prompt_attention(q, k, v, i32([0, 10]), out=torch.empty_like(q)), y)
+    for bad in (dict(q=q[:, :, :32]), dict(k=k[:5]), dict(v=v.bfloat16()), dict(q=q.half()), dict(starts=i32([0])), dict(starts=i32([0, 10]).long()),
+                dict(q=q[:, :, ::2]), dict(starts=torch.zeros(2, dtype=torch.int32)), dict(out=torch.empty((9, 2, 64), device="cuda"))):
+        with pytest.raises(wf.WfError):
+            with torch.no_grad():
+                wf.prompt_attention(**dict(dict(q=q, k=k, v=v, starts=i32([0, 10])), **bad))
+
+
+# ---------------------------------------------------------------- the 8-bit paged cache
+
+def random_tables(rng, n, width, pages):
+    return rng.permutation(pages)[:n * width].reshape(n, width)
+
+
+def check_values(cache, model, tables, lens, layer=0):
+    for dtype in (F32, BF16):
+        k, v = cache.load(i32(tables), i32(lens), dtype, layer=layer)
+        for r, length in enumerate(lens):
+            m = min(max(length, 0), 16 * len(tables[r]))
+            wk, wv, _ = model.rows(tables[r], m)
+            assert np.array_equal(num(k[r, :m]), wk, equal_nan=True) and np.array_equal(num(v[r, :m]), wv, equal_nan=True)
+            assert not k[r, m:].any() and not v[r, m:].any()
+
+
+def rows_of(rng, shape, dtype, spread=1.0):
+    x = torch.from_numpy(rng.standard_normal(shape) * np.exp(spread * rng.standard_normal(shape))).to(dtype)
+    return x.cuda()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads", [1, 2, 5, 20])
+def test_cache8_appends(heads, dtype):
+    """Rows appended in steps of many sizes, values held exactly as the plain form has them after each."""
+    rng = np.random.default_rng(heads)
+    wf, n, width = lib(), 3, 6
+    cache, model = wf.PagedCache8(25, heads, layers=2), plain.PagedCache8(25, heads)
+    tables, at = random_tables(rng, n, width, 25), [0, 0, 0]
+    cache.data.fill_(0xff)                                    # what was never stored may be anything
+    for step, rows in enumerate((1, 1, 5, 9, 16, 17, 1, 33)):
+        counts = [rows, rng.integers(0, rows + 1), 0 if step % 3 == 1 else rows]
+        k, v = (rows_of(rng, (n, rows, heads, 64), dtype, 1 + step % 3) for _ in range(2))
+        cache.store(k, v, i32(tables), i32(at), counts=None if counts == [rows] * 3 else i32(counts), layer=1)
+        model.store([num(k[r, :c]) for r, c in enumerate(counts)], [num(v[r, :c]) for r, c in enumerate(counts)], tables, at)
+        at = [a + c for a, c in zip(at, counts)]
+        check_values(cache, model, tables, at, layer=1)
+    # a rollback: rows over what is there, the rest of the page gone
+    at = [max(0, a - 5) for a in at]
+    k, v = (rows_of(rng, (n, 2, heads, 64), dtype) for _ in range(2))
+    cache.store(k, v, i32(tables), i32(at), layer=1)
+    model.store(num(k), num(v), tables, at)
+    check_values(cache, model, tables, [min(16 * ((a + 2 + 15) // 16), 16 * width) for a in at], layer=1)
+    assert (cache.data[0] == 0xff).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens,at", [([1], [0]), ([0, 40, 1, 16, 15, 0], [3, 9, 31, 16, 17, 8]), ([200], [5]), ([1] * 40, list(range(40))), ([0, 0], [1, 2]),
+                                     ([47, 33, 32, 31], [0, 15, 16, 1])])
+def test_cache8_packed(lens, at, dtype):
+    rng = np.random.default_rng(sum(lens))
+    wf, n, heads, width = lib(), len(lens), 3, 15
+    cache, model = wf.PagedCache8(n * width, heads), plain.PagedCache8(n * width, heads)
+    cache.data.zero_()
+    tables = random_tables(rng, n, width, n * width)
+    k, v = (rows_of(rng, (n, 16 * width, heads, 64), dtype) for _ in range(2))
+    cache.store(k, v, i32(tables), i32([0] * n), counts=i32(at))
+    model.store([num(k[r, :a]) for r, a in enumerate(at)], [num(v[r, :a]) for r, a in enumerate(at)], tables, [0] * n)
+    starts = borders(lens)
+    k, v = (rows_of(rng, (max(1, sum(lens)), heads, 64), dtype) for _ in range(2))
+    cache.store(k, v, i32(tables), i32(at), starts=i32(starts))
+    model.store([num(k[a:b]) for a, b in zip(starts, starts[1:])], [num(v[a:b]) for a, b in zip(starts, starts[1:])], tables, at)
+    check_values(cache, model, tables, [a + c for a, c in zip(at, lens)])
+    check_values(cache, model, tables, [16 * width] * n)
+
+
+def test_cache8_extremes():
+    """The scale's borders, ties, zeros of both signs, the smallest and largest values, NaN and infinities beside others."""
+    rng = np.random.default_rng(0)
+    rows = []
+    for top in (448.0, 448.0 * (1 + 2.0 ** -20), 449.0, 1.0, 1.75, np.float32(1.7500001), 2.0 ** -100 * 448, 2.0 ** -110, 1e-38, 1e-44, 0.0, 3e38,
+                247 * 2.0 ** 120, 2.0 ** 119):
+        x = rng.standard_normal((16, 64))
+        x *= top / np.abs(x).max() if top else 0
+        x.flat[0] = top
+        x.flat[1] = -0.0
+        rows.append(x)
+    ties = (plain.E4M3[:-1] + plain.E4M3[1:]) / 2
+    x = np.zeros((16, 64))
+    x.flat[:len(ties)], x.flat[200:200 + len(ties)], x[15, 63] = ties, -ties, 448
+    rows.append(x)
+    for bad in (NAN, INF, -INF):
+        x = rng.standard_normal((16, 64))
+        x[3, 3], x[9, 50] = bad, bad
+        rows.append(x)
+    rows.append(np.full((16, 64), NAN))
+    wf, n = lib(), len(rows)
+    k = torch.from_numpy(np.stack(rows)).float().cuda()[:, :, None]
+    v = k.flip(0, 1, 3)
+    cache, model = wf.PagedCache8(n, 1), plain.PagedCache8(n, 1)
+    tables = np.arange(n)[:, None]
+    cache.store(k, v, i32(tables), i32([0] * n))
+    model.store(num(k), num(v), tables, [0] * n)
+    check_values(cache, model, tables, [16] * n)
+    cache.store(k[:, 4:9], v[:, 4:9], i32(tables), i32([11] * n))   # appended to what stands there, NaN among it
+    model.store(num(k[:, 4:9]), num(v[:, 4:9]), tables, [11] * n)
+    check_values(cache, model, tables, [16] * n)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_cache8_strides_and_places_that_are_not_there(dtype):
+    rng = np.random.default_rng(2)
+    wf = lib()
+    cache, model = wf.PagedCache8(12, 2), plain.PagedCache8(12, 2)
+    cache.data.zero_()
+    wide = np.concatenate([random_tables(rng, 3, 3, 12), np.full((3, 2), -1)], 1)
+    wide[1, 1], wide[2, 0], wide[0, 2] = -7, 12, 2 ** 31 - 1
+    tables = i32(wide)
+    buf = rows_of(rng, (3, 70, 2, 2, 66), dtype)
+    for off in (0, 1):
+        k, v = buf[:, :50, :, 0, off:off + 64], buf[:, 10:60, :, 1, off:off + 64]
+        for at in ([0, 0, 0], [-5, 3, 40], [16 * 5 - 3, -60, 2 ** 31 - 1], [-2 ** 31, 0, 16]):
+            cache.store(k, v, tables, i32(at))
+            model.store(num(k), num(v), wide, at)
+            check_values(cache, model, wide, [80, 80, 80])
+    kk, vv = buf.transpose(0, 1)[:50, :, 0, 0, :64], buf.transpose(0, 1)[:50, :, 1, 1, :64]      # packed [50, 3 as heads]
+    c3, m3 = wf.PagedCache8(12, 3), plain.PagedCache8(12, 3)
+    c3.data.zero_()
+    part = tables[:2, :3]                                        # a slice: rows further apart
+    c3.store(kk, vv, part, i32([0, 5]), starts=i32([0, 20, 50]))
+    m3.store([num(kk[:20]), num(kk[20:])], [num(vv[:20]), num(vv[20:])], wide[:2, :3], [0, 5])
+    check_values(c3, m3, wide[:2, :3], [48, 48])
+    c3.store(kk[:0], vv[:0], part, i32([0, 5]), starts=i32([0, 0, 0]))
+    for starts in ([-5, 20, 90], [30, 10, 50], [2 ** 31 - 1, 0, -2 ** 31]):
+        c3.store(kk, vv, part, i32([0, 5]), starts=i32(starts))
+    torch.cuda.synchronize()
+
+
+def check_attend(cache, model, q, tables, at, counts=None, stream=None, layer=0):
+    got = num(cache.attend(q, i32(tables), i32(at), counts=None if counts is None else i32(counts), stream=stream, layer=layer))
+    for r in range(len(q)):
+        c = q.shape[1] if counts is None else min(max(counts[r], 0), q.shape[1])
+        want, spread, size = model.attend(num(q[r]), tables[r], at[r], c)
+        bad = ~np.isfinite(want)
+        assert np.array_equal(np.isnan(got[r]), bad), (r, np.isnan(got[r]).sum(), bad.sum())
+        tol = bound(np.where(bad, 0, want), np.where(bad, 0, spread), np.nan_to_num(size), 16 * len(tables[r]), q.dtype)
+        err = np.abs(np.where(bad, 0, got[r]) - np.where(bad, 0, want))
+        assert (err <= tol).all(), (r, err.max(), (err / np.maximum(tol, 1e-30)).max())
+
+
+def filled(n, width, heads, seed=0, dtype=F32, pages=None, layers=1, layer=0, spread=0.5):
+    rng = np.random.default_rng(seed)
+    pages = pages or n * width + 2
+    cache, model = lib().PagedCache8(pages, heads, layers=layers), plain.PagedCache8(pages, heads)
+    cache.data.fill_(0xff)
+    tables = random_tables(rng, n, width, pages)
+    k, v = (rows_of(rng, (n, 16 * width, heads, 64), dtype, spread) for _ in range(2))
+    cache.store(k, v, i32(tables), i32([0] * n), layer=layer)
+    model.store(num(k), num(v), tables, [0] * n)
+    return rng, cache, model, tables
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,rows,heads,group,width,at", [
+    (1, 1, 1, 1, 1, [0]), (1, 1, 2, 1, 1, [15]), (2, 1, 2, 2, 3, [16, 47]), (3, 9, 4, 1, 4, [0, 20, 55]), (1, 1, 1, 24, 2, [31]), (2, 3, 2, 7, 5, [33, 60]),
+    (1, 17, 1, 1, 3, [31]), (1, 48, 2, 2, 6, [40]), (4, 5, 2, 4, 40, [0, 100, 511, 635]), (1, 1, 2, 4, 200, [3199]), (2, 2, 1, 8, 130, [2000, 31]),
+    (5, 1, 20, 1, 28, [0, 1, 100, 300, 447]), (1, 9, 20, 1, 28, [438]), (1, 33, 1, 5, 70, [1000])])
+def test_attend8(n, rows, heads, group, width, at, dtype):
+    rng, cache, model, tables = filled(n, width, heads, seed=rows + width, dtype=dtype)
+    q = rows_of(rng, (n, rows, heads * group, 64), dtype, 0.3)
+    check_attend(cache, model, q, tables, at)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [4, 100])
+def test_attend8_counts_and_positions(dtype, width):
+    """Rows behind the given ones, before the first position and past the tables; requests of nothing."""
+    rng, cache, model, tables = filled(5, width, 2, seed=1)
+    q = rows_of(rng, (5, 6, 4, 64), dtype, 0.3)
+    q[3] = NAN                                                # not one row of it counts
+    for counts in ([6, 3, 0, 0, 1], [6, 6, 6, -2, 9]):
+        for at in ([0, 10, 5, 3, 16 * width - 2], [-3, -6, 16 * width, 0, -2 ** 31], [16 * width - 1, 2 ** 31 - 1, -1, 7, 30]):
+            check_attend(cache, model, q, tables, at, counts)
+    q[3] = 1
+    check_attend(cache, model, q, tables, [1, 2, 3, 4, 5])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [3, 90])
+def test_attend8_bad_pages(dtype, width):
+    """Positions of pages that are not there are left out, wherever they lie; a request of such pages alone gives zeros."""
+    rng, cache, model, tables = filled(4, width, 2, seed=2)
+    cache.data[:, 0] = 0xff
+    tables[tables == 0] = -1
+    tables[0, 1], tables[1, 0], tables[1, -1], tables[2] = -1, 2 ** 31 - 1, len(cache.data[0]), -5
+    q = rows_of(rng, (4, 3, 4, 64), dtype, 0.3)
+    check_attend(cache, model, q, tables, [16 * width - 3, 20, 30, 16 * width - 20])
+    check_attend(cache, model, q, tables, [16, 0, 16 * width, 1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width,where", [(3, 20), (3, 33), (60, 900)])
+def test_attend8_what_is_masked_may_hold_anything(dtype, width, where):
+    """NaN in positions that some rows, or none, see."""
+    rng, cache, model, tables = filled(2, width, 2, seed=3)
+    q = rows_of(rng, (2, 5, 4, 64), dtype, 0.3)
+    clean = cache.attend(q, i32(tables), i32([where - 3, where - 3]))
+    x = rows_of(rng, (2, 1, 2, 64), F32)
+    x[0, :, :, 7] = NAN
+    cache.store(torch.ones_like(x), x, i32(tables), i32([where + 2, where + 2]))      # seen by no row
+    model.store(num(torch.ones_like(x)), num(x), tables, [where + 2, where + 2])
+    check_attend(cache, model, q, tables, [where - 3, where - 3])
+    cache.store(torch.ones_like(x), x, i32(tables), i32([where, where]))              # seen by the fourth row on
+    model.store(num(torch.ones_like(x)), num(x), tables, [where, where])
+    check_attend(cache, model, q, tables, [where - 3, where - 3])
+    got = cache.attend(q, i32(tables), i32([where - 3, where - 3]))
+    assert torch.equal(got[:, :3], clean[:, :3]) and torch.isnan(got[0, 3:, :, 7]).all() and torch.isfinite(got[0, :, :, 8:]).all()
+    cache.store(x, torch.ones_like(x), i32(tables), i32([where, where]))              # a key
+    model.store(num(x), num(torch.ones_like(x)), tables, [where, where])
+    check_attend(cache, model, q, tables, [where - 3, where - 3])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [6, 100])
+@pytest.mark.parametrize("size", [20.0, 300.0])
+def test_attend8_scores_of_any_magnitude(dtype, width, size):
+    rng, cache, model, tables = filled(1, width, 1, seed=4)
+    q = (rows_of(rng, (1, 4, 2, 64), F32, 0.1) * size).to(dtype)
+    check_attend(cache, model, q, tables, [16 * width - 4])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("offset", [0, 1, 4])
+def test_attend8_strides(dtype, offset):
+    rng, cache, model, tables = filled(3, 5, 2, seed=5, layers=3, layer=2)
+    buf = rows_of(rng, (offset + 3 * 4 * 12 * 64,), dtype, 0.3)
+    qkv = buf[offset:].view(3, 4, 12, 64)
+    check_attend(cache, model, qkv[:, :, :4], tables, [3, 30, 70], layer=2)
+    check_attend(cache, model, qkv.transpose(1, 2)[:, :, :4], tables, [3, 30, 60], layer=2)
+    q = rows_of(rng, (3, 1, 1, 64), dtype, 0.3).expand(3, 5, 6, 64)
+    check_attend(cache, model, q, tables, [3, 30, 60], layer=2)
+    wide = i32(np.concatenate([tables, tables], 1))
+    assert torch.equal(cache.attend(q, wide[:, :5], i32([3, 30, 60]), layer=2), cache.attend(q, i32(tables), i32([3, 30, 60]), layer=2))
+
+
+def test_cache8_offsets_past_32_bits():
+    """Pages from 4 GB on."""
+    wf = lib()
+    page = 2064
+    pages = (1 << 32) // page + 40
+    cache = wf.PagedCache8(pages, 1)
+    tables = np.array([[pages - 1, 0, pages - 20], [pages - 3, pages - 2, 5]])
+    model = plain.PagedCache8(50, 1)
+    small = np.array([[49, 0, 30], [47, 48, 5]])
+    rng = np.random.default_rng(0)
+    k, v = (rows_of(rng, (2, 48, 1, 64), BF16) for _ in range(2))
+    cache.store(k, v, i32(tables), i32([0, 0]))
+    model.store(num(k), num(v), small, [0, 0])
+    a, b = cache.load(i32(tables), i32([48, 48]))
+    for r in range(2):
+        wk, wv, _ = model.rows(small[r], 48)
+        assert np.array_equal(num(a[r]), wk) and np.array_equal(num(b[r]), wv)
+    q = rows_of(rng, (2, 2, 3, 64), F32, 0.3)
+    got = num(cache.attend(q, i32(tables), i32([46, 30])))
+    for r, at in enumerate((46, 30)):
+        want, spread, size = model.attend(num(q[r]), small[r], at, 2)
+        assert (np.abs(got[r] - want) <= bound(want, spread, size, 48, F32)).all()
+
+
+def test_attend8_long():
+    """131,072 positions: rows against 64 bits over the values that the cache holds."""
+    wf, width, heads, group = lib(), 8192, 2, 4
+    g = torch.Generator("cuda").manual_seed(0)
+    cache = wf.PagedCache8(2 * width, heads)
+    tables = torch.randperm(2 * width, generator=torch.Generator().manual_seed(1)).view(2, width).to(torch.int32).cuda()
+    k, v = (torch.randn((2, 16 * width, heads, 64), device="cuda", generator=g).to(BF16) for _ in range(2))
+    zero = torch.zeros(2, dtype=torch.int32, device="cuda")
+    cache.store(k, v, tables, zero)
+    held = cache.load(tables, torch.full_like(zero, 16 * width))
+    for rows, at in ((1, [16 * width - 1, 100001]), (9, [70000, 16 * width - 9])):
+        q = torch.randn((2, rows, heads * group, 64), device="cuda", generator=g)
+        got = num(cache.attend(q, tables, i32(at)))
+        for r in range(2):
+            kk, vv = num(held[0][r]), num(held[1][r])
+            for i in {0, rows - 1}:
+                for h in (0, 5):
+                    n = at[r] + i + 1
+                    s = kk[:n, h // group] @ num(q[r, i, h]) / 8
+                    p = np.exp(s - s.max())
+                    p /= p.sum()
+                    want = p @ vv[:n, h // group]
+                    # sums of 131,072 terms in a tree of a few hundred each: the 2-norm of the roundings, not their sum
+                    assert np.abs(got[r, i, h] - want).max() <= 2.0 ** -18 * (p @ np.abs(vv[:n, h // group])).max()
+
+
+def test_cache8_refuses():
+    wf = lib()
+    cache = wf.PagedCache8(8, 2, layers=2)
+    k = torch.zeros((2, 3, 2, 64), device="cuda")
+    t, at = i32([[0, 1], [2, 3]]), i32([0, 0])
+    q = torch.zeros((2, 3, 4, 64), device="cuda")
+    for bad in (dict(k=k[:, :, :1]), dict(v=k.bfloat16()), dict(v=k[:1]), dict(k=k[:1], v=k[:1]), dict(tables=t.long()), dict(tables=t[:1]),
+                dict(positions=at.long()), dict(positions=None), dict(counts=at, starts=i32([0, 1, 2])), dict(layer=2), dict(layer=-1), dict(counts=i32([1])),
+                dict(k=k[..., ::2], v=k[..., ::2]), dict(tables=i32([[0, 9, 1, 9], [2, 9, 3, 9]])[:, ::2]), dict(starts=i32([0, 1, 2]))):
+        with pytest.raises(wf.WfError):
+            cache.store(**dict(dict(k=k, v=k, tables=t, positions=at), **bad))
+    for bad in (dict(q=q[:, :, :3]), dict(q=q[:1]), dict(q=q.half()), dict(q=q[0]), dict(tables=t[0]), dict(positions=None), dict(layer=5), dict(q=q[:, :0])):
+        with pytest.raises(wf.WfError):
+            cache.attend(**dict(dict(q=q, tables=t, positions=at), **bad))
+    for bad in (dict(dtype=torch.half), dict(lens=None), dict(lens=i32([1]))):
+        with pytest.raises(wf.WfError):
+            cache.load(**dict(dict(tables=t, lens=at), **bad))
+    q.requires_grad_()
+    cache.store(k, k, t, at)
+    y = cache.attend(q, t, at)
+    with pytest.raises(wf.WfError, match="no backward"):
+        y.sum().backward()
+
+
+# ---------------------------------------------------------------- together
+
+def decode(seed, dtype, stream=None, steps=5):
+    """Packed prompts of three requests, then `steps` of one and three rows: rotated, stored, attended."""
+    wf, H, KV, width = lib(), 6, 2, 8
+    g = torch.Generator("cuda").manual_seed(seed)
+    lens = [37, 1, 64]
+    starts, at = i32(borders(lens)), torch.cat([torch.arange(m) for m in lens]).to(torch.int32).cuda()
+    rot, cache = wf.Rotary(64, scaling="ramp", factor=4.0, context=64), wf.PagedCache8(3 * width, KV)
+    tables = i32(np.random.default_rng(seed).permutation(3 * width).reshape(3, width))
+    x = [torch.randn((sum(lens), H + 2 * KV, 64), device="cuda", generator=g).to(dtype)]
+    x += [torch.randn((3 * (1 + 2 * (i % 2)), H + 2 * KV, 64), device="cuda", generator=g).to(dtype) for i in range(steps)]
+    torch.cuda.synchronize()
+    out, pos = [], i32(lens)
+    q, k = rot.rotate(at, x[0][:, :H], x[0][:, H:H + KV], stream=stream)
+    out.append(wf.prompt_attention(q, k, x[0][:, H + KV:], starts, stream=stream))
+    cache.store(k, x[0][:, H + KV:], tables, i32([0, 0, 0]), starts=starts, stream=stream)
+    for y in x[1:]:
+        rows = len(y) // 3
+        here = (pos[:, None] + torch.arange(rows, dtype=torch.int32, device="cuda")).flatten()
+        torch.cuda.synchronize()
+        q, k = rot.rotate(here, y[:, :H], y[:, H:H + KV], stream=stream)
+        cache.store(k.view(3, rows, KV, 64), y.view(3, rows, H + 2 * KV, 64)[:, :, H + KV:], tables, pos, stream=stream)
+        out.append(cache.attend(q.view(3, rows, H, 64), tables, pos, stream=stream))
+        pos = pos + rows
+    torch.cuda.synchronize()
+    return lens, x, out, rot
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_decoding_from_prompt_to_tokens(dtype):
+    """The whole run against the plain forms, each fed with the values of the one before."""
+    lens, x, out, rot = decode(3, dtype)
+    H, KV, width = 6, 2, 8
+    turns, amplitude = plain.rotary_turns(64, scaling="ramp", factor=4.0, context=64)
+
+    def turned(y, at):
+        z = plain.rotary(num(y[:, :H + KV]), at, turns, amplitude, False)
+        return torch.from_numpy(z).to(dtype)                   # rounded to the type as the kernel does (but for near ties)
+    at = np.concatenate([np.arange(m) for m in lens])
+    z = turned(x[0], at)
+    starts = borders(lens)
+    want, spread, size = plain.prompt_attention(num(z[:, :H]), num(z[:, H:]), num(x[0][:, H + KV:]), starts)
+    # a rotated value may round the other way: one step of its type, as an error of the scores
+    slack = 4 * half(dtype) if dtype == BF16 else 2.0 ** -18
+    assert (np.abs(num(out[0]) - want) <= bound(want, spread, size, 64, dtype, dtype == BF16) + 2 * slack * size[..., None] * spread).all()
+    model = plain.PagedCache8(3 * width, KV)
+    tables = np.random.default_rng(3).permutation(3 * width).reshape(3, width)
+    model.store([num(z[a:b, H:]) for a, b in zip(starts, starts[1:])], [num(x[0][a:b, H + KV:]) for a, b in zip(starts, starts[1:])], tables, [0, 0, 0])
+    pos = list(lens)
+    for y, got in zip(x[1:], out[1:]):
+        rows = len(y) // 3
+        z = turned(y, np.concatenate([p + np.arange(rows) for p in pos]))
+        model.store(num(z[:, H:]).reshape(3, rows, KV, 64), num(y[:, H + KV:]).reshape(3, rows, KV, 64), tables, pos)
+        for r in range(3):
+            want, spread, size = model.attend(num(z[r * rows:(r + 1) * rows, :H]), tables[r], pos[r], rows)
+            # a key that rounds the other way in 8 bits is off by one step, 2^-3 of it, of one dimension: rare, so few of
+            # a row's 64 products and of its keys; 2^-6 of the scores' magnitudes bounds what a few of them give
+            assert (np.abs(num(got[r]) - want) <= bound(want, spread, size, 128, dtype) + 2 * (slack + 2.0 ** -6) * size[..., None] * spread).all()
+        pos = [p + rows for p in pos]
+
+
+def test_beams_share_and_part_pages():
+    """cache_reorder on the 8-bit cache: beams that continue one parent read what it read, and part from there."""
+    wf, B, width, KV, layers = lib(), 3, 4, 2, 2
+    rng = np.random.default_rng(0)
+    cache = wf.PagedCache8(B * width + 4, KV, layers=layers)
+    cache.data.zero_()
+    pool = rng.permutation(B * width + 4)[:B * width].reshape(1, -1)
+    tables = i32(pool[:, :width].repeat(B, 0).reshape(1, B, width))
+    prompt = rows_of(rng, (1, 21, KV, 64), F32)
+    for layer in range(layers):
+        cache.store(prompt, prompt * 2, tables[0, :1], i32([0]), layer=layer)
+    plains = [plain.PagedCache8(width, KV) for _ in range(B)]
+    own = np.arange(width)[None]
+    for m in plains:
+        m.store(num(prompt), num(prompt * 2), own, [0])
+    at, parents = 21, [0, 0, 0]
+    for step in range(12):
+        tables = wf.cache_reorder(cache.data, tables, i32([parents]), i32([at]), i32(pool), 16)
+        plains = [copy.deepcopy(plains[p]) for p in parents]
+        k = rows_of(rng, (B, 1, KV, 64), F32)
+        for layer in range(layers):
+            cache.store(k, -k, tables[0], i32([at] * B), layer=layer)
+        for b, m in enumerate(plains):
+            m.store(num(k[b:b + 1]), num(-k[b:b + 1]), own, [at])
+        q = rows_of(rng, (B, 1, 4, 64), F32, 0.3)
+        for layer in range(layers):
+            got = num(cache.attend(q, tables[0], i32([at] * B), layer=layer))
+            for b, m in enumerate(plains):
+                want, spread, size = m.attend(num(q[b]), own[0], at, 1)
+                assert (np.abs(got[b] - want) <= bound(want, spread, size, 64, F32)).all(), (step, b)
+        at += 1
+        parents = rng.integers(0, B, B).tolist()
+
+
+def test_operators_on_streams():
+    """Several streams at once, a given stream, and the current one: the same results bit for bit."""
+    want = [decode(s, F32)[2] for s in range(3)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [decode(s, F32, stream=streams[s])[2] for s in range(3)]
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    with torch.cuda.stream(streams[0]):
+        assert all(torch.equal(x, y) for x, y in zip(decode(1, F32)[2], want[1]))
+
+
+def test_operators_captured_into_graphs():
+    """Two graphs, replayed with other inputs in between and with eager calls of the same sizes; every replay as the eager call."""
+    wf, H, KV, width, n = lib(), 8, 2, 200, 2
+    g = torch.Generator("cuda").manual_seed(0)
+    rot, cache = wf.Rotary(64), wf.PagedCache8(n * width, KV)
+    tables = torch.randperm(n * width, generator=torch.Generator().manual_seed(2)).view(n, width).to(torch.int32).cuda()
+    old = torch.randn((n, 16 * width, KV, 64), device="cuda", generator=g)
+    cache.store(old, old, tables, i32([0, 0]))
+    starts, at = i32([0, 90, 133]), torch.arange(133, dtype=torch.int32, device="cuda")
+
+    def prompt(x):
+        q, k = rot.rotate(at, x[:, :H], x[:, H:H + KV])
+        return wf.prompt_attention(q, k, x[:, H + KV:], starts)
+
+    def token(x, pos):
+        q, k = rot.rotate(pos, x[:, :H], x[:, H:H + KV])
+        cache.store(k[:, None], x[:, None, H + KV:], tables, pos)
+        return cache.attend(q[:, None], tables, pos)
+    xp, xt, pos = torch.randn((133, H + 2 * KV, 64), device="cuda"), torch.randn((n, H + 2 * KV, 64), device="cuda"), i32([1000, 3000])
+    graphs = []
+    for f, a in ((prompt, (xp,)), (token, (xt, pos)), (token, (xt, pos))):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            f(*a)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = f(*a)
+        graphs.append((graph, out, f, a))
+    for i in range(4):
+        xp.copy_(torch.randn(xp.shape, device="cuda", generator=g))
+        xt.copy_(torch.randn(xt.shape, device="cuda", generator=g))
+        pos.copy_(i32([1000 + i, 3000 - 500 * i]))
+        for graph, out, f, a in graphs:
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            assert torch.equal(got, f(*a)), i
+
+
+def test_rotary_backward_captured_beside_an_eager_graph():
+    """A forward and backward pass captured while an eager graph of other leaves of the same kind lives."""
+    wf = lib()
+    rot, at = wf.Rotary(64), i32([4, 5, 6])
+    eager = torch.randn((3, 2, 64), device="cuda", requires_grad=True)
+    alive = rot.rotate(at, eager)
+    q = torch.randn((3, 2, 64), device="cuda", requires_grad=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(rot.rotate(at, q).square().sum(), q)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        (grad,) = torch.autograd.grad((rot.rotate(at, q) ** 3 / 3).sum(), q)
+    for i in range(3):
+        with torch.no_grad():
+            q.copy_(torch.randn(q.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        (want,) = torch.autograd.grad((rot.rotate(at, q) ** 3 / 3).sum(), q)
+        assert torch.allclose(grad, want, rtol=1e-5, atol=1e-5)
+    alive.sum().backward()
+    check_rotary(eager.grad, torch.ones_like(eager), [4, 5, 6], {}, 64, transposed=True)
+
+
+def test_selfattn_results_do_not_vary():
+    first = decode(7, BF16)[2]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, decode(7, BF16)[2]))

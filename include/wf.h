@@ -512,22 +512,18 @@ int wf_rotary_turns(int dims, double base, int scaling, double factor, double co
 /*
  * turns: device fp64 [dims / 2].  transposed != 0 turns the other way with the same amplitude
  * (the gradient of the rotation).  positions: device int32 [tokens], any value.
- * rows: host array of n_rows (1 or 2: queries and keys) descriptions: element (token, head, i)
- * of x lies token * x_stride[0] + head * x_stride[1] + i elements in, of y likewise; x and y
- * are device memory in dtype (WF_F32 or WF_BF16).  y is x itself with equal strides (in place)
- * or other memory; rows of y may not overlap, nor the two tensors.
+ * q, k: device, in dtype (WF_F32 or WF_BF16); element (token, head, i) lies token * stride[0] +
+ * head * stride[1] + i elements in (strides >= 0, host arrays of two), likewise in their results
+ * q_out and k_out.  k NULL: there is none (k_stride, k_heads, k_out and k_out_stride are not used).  A result is
+ * its source itself with equal strides (in place) or other memory; its rows may not overlap, nor the
+ * two results.
  * 0 <= tokens <= 2^28 (0: nothing is enqueued), 1 <= heads <= 65535, 2 <= dims <= width <= 4096, dims even.
  * Errors: WF_EINVAL, WF_EHIP.
  */
-typedef struct wf_rotary_rows {
-  const void* x;
-  void* y;
-  int64_t x_stride[2];
-  int64_t y_stride[2];
-  int32_t heads;
-} wf_rotary_rows;
 int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, int transposed, const int32_t* positions,
-              int tokens, int width, int dtype, const wf_rotary_rows* rows, int n_rows, void* stream);
+              int tokens, int width, int dtype, const void* q, const int64_t* q_stride, int q_heads, void* q_out,
+              const int64_t* q_out_stride, const void* k, const int64_t* k_stride, int k_heads, void* k_out,
+              const int64_t* k_out_stride, void* stream);
 
 /*
  * Causal attention of packed prompts: softmax(q k^T / 8) v, where row t of the sequence

@@ -53,11 +53,6 @@ class WfKv4(ctypes.Structure):
                 ("n_frames", ctypes.c_int32)]
 
 
-class WfRotaryRows(ctypes.Structure):
-    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2),
-                ("heads", ctypes.c_int32)]
-
-
 class WfKv8(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("n_head", ctypes.c_int32)]
 
@@ -124,7 +119,7 @@ def load_library(path=LIB_PATH):
         "wf_kv4_attend_workspace_bytes": [kv4p, I, I, ctypes.POINTER(Z)],
         "wf_kv4_attend": [kv4p, I, I, P, I64p, I, I, P, P, P, Z, P],
         "wf_rotary_turns": [I, D, I, D, D, D, D, ctypes.POINTER(D), ctypes.POINTER(F)],
-        "wf_rotary": [P, I, I, F, I, P, I, I, I, ctypes.POINTER(WfRotaryRows), I, P],
+        "wf_rotary": [P, I, I, F, I, P, I, I, I, P, I64p, I, P, I64p, P, I64p, I, P, I64p, P],
         "wf_prompt_attend": [P, I64p, P, I64p, P, I64p, I, P, I, I, I, I, P, I, P],
         "wf_kv8_page_bytes": [I, ctypes.POINTER(Z)],
         "wf_kv8_store": [kv8p, I, P, I64p, P, I64p, I, I, P, P, P, I64, I, P, P],

@@ -301,13 +301,14 @@ int wf_rotary_turns(int dims, double base, int scaling, double factor, double co
 }
 
 int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, int transposed, const int32_t* positions,
-              int tokens, int width, int dtype, const wf_rotary_rows* rows, int n_rows, void* stream) {
+              int tokens, int width, int dtype, const void* q, const int64_t* q_stride, int q_heads, void* q_out,
+              const int64_t* q_out_stride, const void* k, const int64_t* k_stride, int k_heads, void* k_out,
+              const int64_t* k_out_stride, void* stream) {
   size_t e;
   if (width < 2 || width > 4096) return bad("width must be in [2, 4096]");
   if (dims < 2 || dims > width || dims % 2) return bad("dims must be even and in [2, width]");
   if (tokens < 0 || tokens > (1 << 28)) return bad("tokens must be in [0, 2^28]");
   if (int r = check_dtype(dtype, e)) return r;
-  if (n_rows < 1 || n_rows > 2 || !rows) return bad("n_rows must be 1 or 2");
   if (!turns || !positions) return bad("null argument");
   if (!aligned(turns, 8) || !aligned(positions, 4)) return bad("a tensor must be aligned to its elements");
   if (!std::isfinite(amplitude)) return bad("amplitude must be finite");
@@ -321,21 +322,27 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
   a.positions = positions;
   a.tokens = tokens;
   a.bf16_data = dtype == WF_BF16;
-  a.n_rows = n_rows;
+  a.n_rows = k ? 2 : 1;
   a.vec = 1;
-  for (int i = 0; i < n_rows; ++i) {
-    const wf_rotary_rows& w = rows[i];
+  const struct {
+    const void* x;
+    const int64_t* xs;
+    void* y;
+    const int64_t* ys;
+    int heads;
+  } rows[2] = {{q, q_stride, q_out, q_out_stride, q_heads}, {k, k_stride, k_out, k_out_stride, k_heads}};
+  for (int i = 0; i < a.n_rows; ++i) {
+    const auto& w = rows[i];
     if (w.heads < 1 || w.heads > kMaxGrid) return bad("heads must be in [1, 65535]");
-    if (int r = check_strides(w.x, w.x_stride, e, a.vec, 2)) return r;
-    if (int r = check_strides(w.y, w.y_stride, e, a.vec, 2)) return r;
-    if (rows_overlap(w.y_stride, tokens, w.heads, width)) return bad("rows of y overlap");
+    if (int r = check_strides(w.x, w.xs, e, a.vec, 2)) return r;
+    if (int r = check_strides(w.y, w.ys, e, a.vec, 2)) return r;
+    if (rows_overlap(w.ys, tokens, w.heads, width)) return bad("rows of a result overlap");
     if (w.x == w.y) {
-      if ((tokens > 1 && w.x_stride[0] != w.y_stride[0]) || (w.heads > 1 && w.x_stride[1] != w.y_stride[1]))
-        return bad("in place, x and y must have equal strides");
+      if ((tokens > 1 && w.xs[0] != w.ys[0]) || (w.heads > 1 && w.xs[1] != w.ys[1])) return bad("in place, strides must be equal");
     } else {
-      a.copies = 1;  // of an x in place: onto itself
+      a.copies = 1;  // of a tensor in place: onto itself
     }
-    a.rows[i] = RotaryRows{w.x, w.y, w.x_stride[0], w.x_stride[1], w.y_stride[0], w.y_stride[1], w.heads};
+    a.rows[i] = RotaryRows{w.x, w.y, w.xs[0], w.xs[1], w.ys[0], w.ys[1], w.heads};
   }
   if (tokens == 0) return WF_OK;
   rotary(a, static_cast<hipStream_t>(stream));

@@ -17,7 +17,7 @@ import functools
 
 import torch
 
-from .binding import WF_BF16, WF_F32, WfError, WfKv4, WfKv8, WfRotaryRows, _refuse, _tensor, load_library
+from .binding import WF_BF16, WF_F32, WfError, WfKv4, WfKv8, _refuse, _tensor, load_library
 
 try:  # torch.cuda.current_stream() and current_device() without their objects and checks (2.7 and 0.1 us)
     from torch._C import _cuda_getCurrentRawStream as _raw_stream, _cuda_getDevice as _device
@@ -294,6 +294,25 @@ _Strides2 = ctypes.c_int64 * 2
 _SCALINGS = {None: 0, "linear": 1, "base": 2, "ramp": 3}
 
 
+class _Layouts(dict):
+    """What the checks of a call's tensors found, by the tensors' layouts: a call with layouts that were checked before
+    goes without (one token's rotation 16.3 us of the host, now 11).  At most 1,024."""
+
+    @staticmethod
+    def of(*tensors):
+        """A key, or None where an argument is not a tensor (which the checks refuse)."""
+        try:
+            return tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for t in tensors])
+        except (AttributeError, RuntimeError):
+            return None
+
+    def keep(self, key, found):
+        if len(self) >= 1024:
+            self.clear()
+        self[key] = found
+        return found
+
+
 def _heads(t, name, axes, width=64):
     """Device, type and strides of [..., heads, width] of `axes` axes, the last one contiguous."""
     dev = _gpu(t, name, axes)
@@ -307,6 +326,18 @@ def _heads(t, name, axes, width=64):
     return dev, _type(t, name), s[:-1]
 
 
+def _vector(t, name, n, device):
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name} must be a tensor")
+    _tensor(t, name, _I32, (n,), device)
+
+
+def _changed(t):
+    """Counts the change of a tensor that a kernel wrote, as autograd's own operations do."""
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+
+
 class _Rotate(torch.autograd.Function):
     """Rotated tensors as a function of them; the gradient turns the other way."""
 
@@ -314,16 +345,15 @@ class _Rotate(torch.autograd.Function):
     def forward(ctx, rotary, positions, transposed, stream, *tensors):
         ctx.rotary, ctx.transposed = rotary, transposed
         ctx.save_for_backward(positions)
-        return rotary._turn(positions, tensors, transposed, None, stream)
+        return rotary._turn(positions, tensors, transposed, False, stream)
 
     @staticmethod
     def backward(ctx, *grads):
         (positions,) = ctx.saved_tensors
-        need = [i for i, g in enumerate(grads) if ctx.needs_input_grad[4 + i]]
-        turned = _Rotate.apply(ctx.rotary, positions, not ctx.transposed, None,
-                               *(g if g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous() for g in (grads[i] for i in need)))
+        need = [i for i in range(len(grads)) if ctx.needs_input_grad[4 + i]]
+        rows = [g if g.stride(-1) == 1 or g.shape[-1] == 1 else g.contiguous() for g in (grads[i] for i in need)]
         out = [None] * len(grads)
-        for i, t in zip(need, turned):
+        for i, t in zip(need, _Rotate.apply(ctx.rotary, positions, not ctx.transposed, None, *rows)):
             out[i] = t
         return (None, None, None, None, *out)
 
@@ -348,56 +378,65 @@ class Rotary:
         if not self.turns.is_cuda:
             _refuse("device must be a GPU")
         self.device = self.turns.device
+        self._plans = _Layouts()
 
     def rotate(self, positions, q, k=None, in_place=False, stream=None):
         """q, and k beside it, at their positions: q, k fp32 or bf16 [tokens, heads, width] of the same tokens, width and
         type (any strides but the last); positions int32 [tokens].  Returns new tensors, or the given ones changed in place
         (without gradients): the rotated q, or (q, k)."""
         tensors = (q,) if k is None else (q, k)
-        if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
+        if torch.is_grad_enabled() and any([isinstance(t, torch.Tensor) and t.requires_grad for t in tensors]):
             if in_place:
                 _refuse("tensors that require gradients are not changed in place")
             out = _Rotate.apply(self, positions, False, stream, *tensors)
         else:
-            out = self._turn(positions, tensors, False, tensors if in_place else None, stream)
+            out = self._turn(positions, tensors, False, in_place, stream)
         return out[0] if k is None else out
 
-    def _turn(self, positions, tensors, transposed, outs, stream):
-        first = tensors[0]
-        rows = (WfRotaryRows * len(tensors))()
-        for i, (t, name) in enumerate(zip(tensors, "qk")):
-            dev, dtype, strides = _heads(t, name, 3, None)
+    def _plan(self, positions, tensors):
+        """Tokens, width, type, shapes and strides, the results' strides."""
+        first, parts = tensors[0], []
+        for t, name in zip(tensors, "qk"):
+            dev, dtype, s = _heads(t, name, 3, None)
             if dev != self.device:
                 _refuse(f"{name} must be on {self.device}, not {dev}")
             if t.shape[0] != first.shape[0] or t.shape[2] != first.shape[2] or t.dtype != first.dtype:
                 _refuse("k must have q's tokens, width and type")
-            rows[i].x, rows[i].x_stride, rows[i].heads = t.data_ptr(), _Strides2(*strides), t.shape[1]
-        tokens, _, width = first.shape
-        _tensor(positions, "positions", _I32, (tokens,), self.device)
+            parts.append((t.shape, _Strides2(*s), _Strides2(t.shape[1] * t.shape[2], t.shape[2]), t.shape[1]))
+        _vector(positions, "positions", first.shape[0], self.device)
+        return first.shape[0], first.shape[2], dtype, parts
+
+    def _turn(self, positions, tensors, transposed, in_place, stream):
+        key = _Layouts.of(positions, *tensors)
+        plan = self._plans.get(key) or self._plans.keep(key, self._plan(positions, tensors))
+        tokens, width, dtype, parts = plan
 
         def call(raw, empty):
-            result = outs if outs is not None else tuple(empty(t.shape, dtype=t.dtype, device=self.device) for t in tensors)
-            for r, t in zip(rows, result):
-                r.y, r.y_stride = t.data_ptr(), _Strides2(*t.stride()[:2])
+            q, shape, qs, qo, heads = tensors[0], *parts[0]
+            a = q if in_place else empty(shape, dtype=q.dtype, device=self.device)
+            if len(tensors) == 1:
+                b, rest, result = None, (None, None, 0, None, None), (a,)
+            else:
+                k, shape, ks, ko, kv = tensors[1], *parts[1]
+                b = k if in_place else empty(shape, dtype=q.dtype, device=self.device)
+                rest, result = (k.data_ptr(), ks, kv, b.data_ptr(), ks if in_place else ko), (a, b)
             if tokens:
                 _check(self.lib.wf_rotary(self.turns.data_ptr(), self.dims, self.interleaved, self.amplitude, transposed,
-                                          positions.data_ptr(), tokens, width, dtype, rows, len(tensors), raw))
+                                          positions.data_ptr(), tokens, width, dtype, q.data_ptr(), qs, heads, a.data_ptr(),
+                                          qs if in_place else qo, *rest, raw))
             return result
 
         result = _enqueue(self.device, stream, call, positions, self.turns, *tensors)
-        if outs is not None:  # autograd's count of changes
-            torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+        if in_place:
+            for t in tensors:
+                _changed(t)
         return result
 
 
-def prompt_attention(q, k, v, starts, out=None, stream=None):
-    """Causal attention of packed prompts: wf_prompt_attend.
+_prompt_plans = _Layouts()
 
-    q: fp32 or bf16 [tokens, n_head, 64]; k, v: [tokens, n_kv_head, 64] in the same type (any strides but the last);
-    starts: int32 [n + 1], sequence s holds the rows starts[s] .. starts[s + 1] - 1.  Returns [tokens, n_head, 64]: rows of
-    no sequence are zeros, or stay as they are in a given contiguous `out`.
-    """
-    lib = load_library()
+
+def _prompt_plan(q, k, v, starts):
     dev, dtype, qs = _heads(q, "q", 3)
     tokens, heads, _ = q.shape
     strides = []
@@ -410,6 +449,20 @@ def prompt_attention(q, k, v, starts, out=None, stream=None):
         _refuse(f"starts must hold two borders at least, on {dev}")
     n = starts.shape[0] - 1
     _tensor(starts, "starts", _I32, (n + 1,), dev)
+    return dev, dtype, tokens, heads, k.shape[1], n, _Strides2(*qs), *strides
+
+
+def prompt_attention(q, k, v, starts, out=None, stream=None):
+    """Causal attention of packed prompts: wf_prompt_attend.
+
+    q: fp32 or bf16 [tokens, n_head, 64]; k, v: [tokens, n_kv_head, 64] in the same type (any strides but the last);
+    starts: int32 [n + 1], sequence s holds the rows starts[s] .. starts[s + 1] - 1.  Returns [tokens, n_head, 64]: rows of
+    no sequence are zeros, or stay as they are in a given contiguous `out`.
+    """
+    lib = load_library()
+    key = _Layouts.of(q, k, v, starts)
+    plan = _prompt_plans.get(key) or _prompt_plans.keep(key, _prompt_plan(q, k, v, starts))
+    dev, dtype, tokens, heads, kv, n, qs, ks, vs = plan
     wants = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
     if out is not None:
         _tensor(out, "out", q.dtype, (tokens, heads, 64), dev)
@@ -419,13 +472,13 @@ def prompt_attention(q, k, v, starts, out=None, stream=None):
     def call(raw, empty):
         o = out if out is not None else empty((tokens, heads, 64), dtype=q.dtype, device=dev)
         if tokens:
-            _check(lib.wf_prompt_attend(q.data_ptr(), _Strides2(*qs), k.data_ptr(), strides[0], v.data_ptr(), strides[1], dtype,
-                                        starts.data_ptr(), n, tokens, heads, k.shape[1], o.data_ptr(), out is None, raw))
+            _check(lib.wf_prompt_attend(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype, starts.data_ptr(), n, tokens, heads,
+                                        kv, o.data_ptr(), out is None, raw))
         return o
 
     o = _enqueue(dev, stream, call, q, k, v, starts, out)
-    if out is not None and not out.is_inference():
-        torch.autograd.graph.increment_version(out)
+    if out is not None:
+        _changed(out)
     return _without_backward("prompt_attention", o, q, k, v) if wants else o
 
 
@@ -452,7 +505,7 @@ class PagedCache8:
         base, layer = self.data.data_ptr(), self.pages * nbytes.value
         self._c = [WfKv8(base + i * layer, self.pages, self.n_head) for i in range(self.layers)]
         self._refs = [ctypes.byref(c) for c in self._c]
-        self._spaces = {}  # workspace bytes of (n, rows, heads, max_pages)
+        self._stores, self._loads, self._attends = _Layouts(), _Layouts(), _Layouts()
 
     def _layer(self, layer):
         if not 0 <= layer < self.layers:
@@ -470,17 +523,7 @@ class PagedCache8:
             _refuse("a size is out of range")
         return n, most, tables.stride(0)
 
-    def _vector(self, t, name, n):
-        if t is None:
-            return None
-        _tensor(t, name, _I32, (n,), self.device)
-        return t.data_ptr()
-
-    def store(self, k, v, tables, positions, starts=None, counts=None, layer=0, stream=None):
-        """Append rows to requests' pages from positions (int32 [n]) on.  k, v: fp32 or bf16, any strides but the last:
-        packed [rows, n_head, 64] with starts (int32 [n + 1]), or [n, rows, n_head, 64], of which request r's first counts[r]
-        (int32 [n], None: all) are given."""
-        ref = self._layer(layer)
+    def _store_plan(self, k, v, tables, positions, starts, counts):
         n, most, ts = self._tables(tables)
         axes = 4 if starts is None else 3
         strides = []
@@ -491,62 +534,81 @@ class PagedCache8:
             strides.append(_Strides(*s) if starts is None else _Strides(0, *s))
         if starts is None and k.shape[0] != n:
             _refuse(f"k must hold {n} requests, not {k.shape[0]}")
-        if starts is not None and counts is not None:
-            _refuse("starts and counts exclude each other")
-        pstarts, pcounts = self._vector(starts, "starts", n + 1), self._vector(counts, "counts", n)
-        if positions is None:
-            _refuse("positions must be a tensor")
-        at, rows = self._vector(positions, "positions", n), k.shape[-3]
+        if starts is not None:
+            if counts is not None:
+                _refuse("starts and counts exclude each other")
+            _vector(starts, "starts", n + 1, self.device)
+        elif counts is not None:
+            _vector(counts, "counts", n, self.device)
+        _vector(positions, "positions", n, self.device)
+        return n, most, ts, code, k.shape[-3], *strides
+
+    def store(self, k, v, tables, positions, starts=None, counts=None, layer=0, stream=None):
+        """Append rows to requests' pages from positions (int32 [n]) on.  k, v: fp32 or bf16, any strides but the last:
+        packed [rows, n_head, 64] with starts (int32 [n + 1]), or [n, rows, n_head, 64], of which request r's first counts[r]
+        (int32 [n], None: all) are given."""
+        ref = self._layer(layer)
+        args = (k, v, tables, positions, starts, counts)
+        key = _Layouts.of(*args)
+        n, most, ts, code, rows, ks, vs = self._stores.get(key) or self._stores.keep(key, self._store_plan(*args))
         if rows == 0:
             return
         _enqueue(self.device, stream, lambda raw, empty: _check(self.lib.wf_kv8_store(
-            ref, n, k.data_ptr(), strides[0], v.data_ptr(), strides[1], code, rows, pstarts, pcounts, tables.data_ptr(), ts, most, at,
-            raw)), k, v, tables, positions, starts, counts, self.data)
+            ref, n, k.data_ptr(), ks, v.data_ptr(), vs, code, rows, None if starts is None else starts.data_ptr(),
+            None if counts is None else counts.data_ptr(), tables.data_ptr(), ts, most, positions.data_ptr(), raw)), *args, self.data)
+
+    def _load_plan(self, tables, lens):
+        n, most, ts = self._tables(tables)
+        _vector(lens, "lens", n, self.device)
+        return n, most, ts
 
     def load(self, tables, lens, dtype=torch.float32, layer=0, stream=None):
         """The keys and values that the first lens[r] (int32 [n]) positions of requests' pages hold: two tensors
         [n, 16 max_pages, n_head, 64], zeros behind them."""
         ref = self._layer(layer)
-        if dtype not in _DTYPES:
+        code = _DTYPES.get(dtype)
+        if code is None:
             _refuse("dtype must be float32 or bfloat16")
-        n, most, ts = self._tables(tables)
-        if lens is None:
-            _refuse("lens must be a tensor")
-        plens = self._vector(lens, "lens", n)
+        key = _Layouts.of(tables, lens)
+        n, most, ts = self._loads.get(key) or self._loads.keep(key, self._load_plan(tables, lens))
 
         def call(raw, empty):
             k = empty((n, 16 * most, self.n_head, 64), dtype=dtype, device=self.device)
             v = empty((n, 16 * most, self.n_head, 64), dtype=dtype, device=self.device)
-            _check(self.lib.wf_kv8_load(ref, n, tables.data_ptr(), ts, most, plens, k.data_ptr(), v.data_ptr(), _DTYPES[dtype], raw))
+            _check(self.lib.wf_kv8_load(ref, n, tables.data_ptr(), ts, most, lens.data_ptr(), k.data_ptr(), v.data_ptr(), code, raw))
             return k, v
 
         return _enqueue(self.device, stream, call, tables, lens, self.data)
+
+    def _attend_plan(self, q, tables, positions, counts):
+        n, most, ts = self._tables(tables)
+        dev, dtype, s = _heads(q, "q", 4)
+        if dev != self.device or q.shape[0] != n:
+            _refuse(f"q must hold {n} requests on {self.device}")
+        rows, heads = q.shape[1:3]
+        nbytes = ctypes.c_size_t()
+        _check(self.lib.wf_kv8_attend_workspace_bytes(self._refs[0], n, rows, heads, most, ctypes.byref(nbytes)))
+        _vector(positions, "positions", n, self.device)
+        if counts is not None:
+            _vector(counts, "counts", n, self.device)
+        return n, most, ts, dtype, rows, heads, _Strides(*s), nbytes.value
 
     def attend(self, q, tables, positions, counts=None, layer=0, stream=None):
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, heads, 64], any strides but the last; heads a multiple of the
         cache's): row i of request r stands at positions[r] + i (int32 [n]) and sees positions up to its own.  Rows from
         counts[r] (int32 [n], None: all) on give zeros.  Returns [n, rows, heads, 64] in q's type."""
         ref = self._layer(layer)
-        n, most, ts = self._tables(tables)
-        dev, dtype, s = _heads(q, "q", 4)
-        if dev != self.device or q.shape[0] != n:
-            _refuse(f"q must hold {n} requests on {self.device}")
-        rows, heads = q.shape[1:3]
-        need = self._spaces.get((n, rows, heads, most))
-        if need is None:
-            nbytes = ctypes.c_size_t()
-            _check(self.lib.wf_kv8_attend_workspace_bytes(ref, n, rows, heads, most, ctypes.byref(nbytes)))
-            need = self._spaces[n, rows, heads, most] = nbytes.value
-        if positions is None:
-            _refuse("positions must be a tensor")
-        at, pcounts = self._vector(positions, "positions", n), self._vector(counts, "counts", n)
+        args = (q, tables, positions, counts)
+        key = _Layouts.of(*args)
+        n, most, ts, dtype, rows, heads, qs, need = self._attends.get(key) or self._attends.keep(key, self._attend_plan(*args))
 
         def call(raw, empty):
             out = empty((n, rows, heads, 64), dtype=q.dtype, device=self.device)
             ws = empty(need, dtype=_U8, device=self.device) if need else None
-            _check(self.lib.wf_kv8_attend(ref, n, q.data_ptr(), _Strides(*s), rows, heads, dtype, tables.data_ptr(), ts, most, at, pcounts,
-                                          out.data_ptr(), ws.data_ptr() if need else None, need, raw))
+            _check(self.lib.wf_kv8_attend(ref, n, q.data_ptr(), qs, rows, heads, dtype, tables.data_ptr(), ts, most, positions.data_ptr(),
+                                          None if counts is None else counts.data_ptr(), out.data_ptr(),
+                                          ws.data_ptr() if need else None, need, raw))
             return out
 
-        out = _enqueue(self.device, stream, call, q, tables, positions, counts, self.data)
+        out = _enqueue(self.device, stream, call, *args, self.data)
         return _without_backward("attend", out, q) if q.requires_grad else out

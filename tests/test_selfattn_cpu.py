@@ -61,30 +61,26 @@ def test_turns_refusals():
 
 def test_rotary_refusals():
     binding, lib = _lib()
-    qkv = 60 * 64
-
-    def rows(**kw):
-        f = dict(x=P, y=P + (1 << 16), xs=(qkv, 64), ys=(20 * 64, 64), heads=20)
-        f.update(kw)
-        return binding.WfRotaryRows(f["x"], f["y"], S2(*f["xs"]), S2(*f["ys"]), f["heads"])
+    xs, ys = S2(60 * 64, 64), S2(20 * 64, 64)
 
     def call(lib, a):
-        w = (binding.WfRotaryRows * 2)(a["first"], a["second"])
-        return lib.wf_rotary(a["turns"], a["dims"], 0, a["amp"], 0, a["at"], a["tokens"], a["width"], a["dtype"],
-                             None if a["none"] else w, a["n"], None)
-    bad_rows = [(rows(**kw), -1) for kw in (
-        dict(x=None), dict(y=None), dict(x=P + 2), dict(y=P + 1), dict(heads=0), dict(heads=70000), dict(xs=(-1, 64)), dict(xs=(0, 1 << 41)),
-        dict(ys=(0, 64)), dict(ys=(20 * 64, 32)), dict(ys=(19 * 64, 64)), dict(ys=(64, 6 * 64)), dict(y=P), dict(y=P, xs=(qkv, 64), ys=(qkv, 128)))]
-    good = dict(turns=P, dims=64, amp=1.0, at=P, tokens=7, width=64, dtype=0, none=False, n=2, first=rows(), second=rows(y=P + (1 << 18)))
-    varied(call, good, {
-        "turns": [(None, -1), (P + 4, -1)], "dims": [(0, -1), (1, -1), (66, -1), (-64, -1)], "amp": [(float("nan"), -1), (float("inf"), -1)],
-        "at": [(None, -1), (P + 2, -1)], "tokens": [(-1, -1), ((1 << 28) + 1, -1)], "width": [(1, -1), (62, -1), (4098, -1)],
-        "dtype": [(2, -1)], "none": [(True, -1)], "n": [(0, -1), (3, -1)], "first": bad_rows, "second": bad_rows})
+        return lib.wf_rotary(a["turns"], a["dims"], 0, a["amp"], 0, a["at"], a["tokens"], a["width"], a["dtype"], a["q"], a["qs"], a["qh"],
+                             a["qo"], a["qos"], a["k"], a["ks"], a["kh"], a["ko"], a["kos"], None)
+    good = dict(turns=P, dims=64, amp=1.0, at=P, tokens=7, width=64, dtype=0, q=P, qs=xs, qh=20, qo=P + (1 << 16), qos=ys,
+                k=P, ks=xs, kh=20, ko=P + (1 << 18), kos=ys)
+    bad = {"turns": [(None, -1), (P + 4, -1)], "dims": [(0, -1), (1, -1), (66, -1), (-64, -1)], "amp": [(float("nan"), -1), (float("inf"), -1)],
+           "at": [(None, -1), (P + 2, -1)], "tokens": [(-1, -1), ((1 << 28) + 1, -1)], "width": [(1, -1), (62, -1), (4098, -1)], "dtype": [(2, -1)],
+           "q": [(None, -1), (P + 2, -1), (P + (1 << 16), -1)]}                       # the last: in place with other strides
+    for x in "qk":
+        bad.update({x + "s": [(None, -1), (S2(-1, 64), -1), (S2(0, 1 << 41), -1)], x + "h": [(0, -1), (70000, -1)], x + "o": [(None, -1), (P + 1, -1)],
+                    x + "os": [(S2(0, 64), -1), (S2(20 * 64, 32), -1), (S2(19 * 64, 64), -1), (S2(64, 6 * 64), -1), (None, -1)]})
+    varied(call, good, bad)
     assert call(lib, dict(good, tokens=0)) == 0
-    # layouts that do not overlap: heads before tokens, one token, one head
-    for r in (rows(ys=(64, 7 * 64)), rows(ys=(64, 9 * 64))):
-        assert call(lib, dict(good, first=r, tokens=0)) == 0
-    assert call(lib, dict(good, first=rows(heads=1, ys=(64, 0)), tokens=0)) == 0
+    assert call(lib, dict(good, tokens=0, k=None, ks=None, kh=0, ko=None, kos=None)) == 0
+    # layouts that do not overlap: heads before tokens, one head
+    for strides in (S2(64, 7 * 64), S2(64, 9 * 64)):
+        assert call(lib, dict(good, qos=strides, tokens=0)) == 0
+    assert call(lib, dict(good, qh=1, qos=S2(64, 0), tokens=0)) == 0
 
 
 def test_prompt_refusals():

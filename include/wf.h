@@ -537,8 +537,10 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
  * out: device [tokens, n_head, 64] in the same type.  Rows of no sequence are set to zero
  *   (clear != 0) or left as they are.
  * fp32: products in 32 bits; bf16: the probabilities are rounded to bf16 for their product, sums
- * are fp32.  A row all of whose scores are -inf gets zeros.
- * 0 <= tokens <= 2^28 (0: nothing is enqueued), 1 <= n <= 2^24, 1 <= n_kv_head, n_head a multiple of it <= 65535.
+ * are fp32.  An infinity in a row's query or in a key that it sees can make its result NaN; a row all of
+ * whose scores are -inf gets zeros.
+ * tokens >= 0 (0: nothing is enqueued), tokens * n_head <= 2^28, 1 <= n <= 2^24, 1 <= n_kv_head, n_head a
+ * multiple of it <= 65535.
  * Errors: WF_EINVAL, WF_EHIP.
  */
 int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, const int64_t* k_stride, const void* v,

@@ -356,7 +356,7 @@ int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, cons
   if (int r = check_dtype(dtype, e)) return r;
   if (int r = check_heads(n_head, n_kv_head)) return r;
   if (n < 1 || n > (1 << 24)) return bad("n must be in [1, 2^24]");
-  if (tokens < 0 || tokens > (1 << 28)) return bad("tokens must be in [0, 2^28]");
+  if (tokens < 0 || (long long)tokens * n_head > (1 << 28)) return bad("tokens * n_head must be in [0, 2^28]");
   if (!starts || !aligned(starts, 4)) return bad("starts must be aligned to its elements");
   PromptArgs a{};
   a.vec = 1;

@@ -32,13 +32,15 @@ struct Borders {
   int base, size, begin, end;  // begin, end: the rows of all sequences
 };
 // The block's 256 threads narrow the borders 256-fold a round (none up to 511 sequences) and load the window:
-// one round trip to memory, where a search of 96 borders by every row takes seven.
-__device__ __forceinline__ Borders borders_near(const int* starts, int n, int q0, int* window, int* counts) {
+// one round trip to memory, where a search of 96 borders by every row takes seven.  meanwhile() runs while
+// the window is on its way.
+template <typename F>
+__device__ __forceinline__ Borders borders_near(const int* starts, int n, int q0, int* window, int* counts, const F& meanwhile) {
+  static_assert(kWindow == 512, "two borders a thread");
   int base = 0, size = n + 1;
   while (size > kWindow) {
     const int stride = (size + 255) / 256, i = threadIdx.x * stride;
-    const bool before = i < size && starts[base + i] <= q0;
-    const int c = __popcll(__builtin_amdgcn_ballot_w64(before));
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(i < size && starts[base + i] <= q0));
     if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
     __syncthreads();
     const int at = max(counts[0] + counts[1] + counts[2] + counts[3] - 1, 0) * stride;
@@ -47,23 +49,34 @@ __device__ __forceinline__ Borders borders_near(const int* starts, int n, int q0
     base += at;
   }
   base = min(base, n);
-  size = min(kWindow, n + 1 - base);
-  for (int i = threadIdx.x; i < size; i += 256) window[i] = starts[base + i];
-  const Borders b{base, size, starts[0], starts[n]};
+  const int x0 = starts[min(base + (int)threadIdx.x, n)], x1 = starts[min(base + 256 + (int)threadIdx.x, n)];
+  const Borders b{base, min(kWindow, n + 1 - base), starts[0], starts[n]};
+  meanwhile();
+  window[threadIdx.x] = x0;
+  window[256 + threadIdx.x] = x1;
   __syncthreads();
   return b;
 }
 // First key of row t: the largest border <= t, where t lies in a sequence; t + 1 (no key) elsewhere.
 __device__ __forceinline__ int first_key(const int* starts, int n, const int* window, const Borders& b, int t) {
   if (t < b.begin || t >= b.end) return t + 1;
-  const bool near = b.base + b.size > n || window[b.size - 1] > t;
-  int lo = 0, hi = near ? b.size - 1 : n - b.base;  // the border of lo is <= t, that of hi > t
+  int lo = 0, hi = b.size - 1;  // the border of lo is <= t, that of hi > t
+  if (b.base + b.size > n || window[hi] > t) {
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (window[m] <= t) lo = m;
+      else hi = m;
+    }
+    return min(max(window[lo], 0), t + 1);
+  }
+  lo = b.base;
+  hi = n;
   while (hi - lo > 1) {
     const int m = (lo + hi) >> 1;
-    if ((near ? window[m] : starts[b.base + m]) <= t) lo = m;
+    if (starts[m] <= t) lo = m;
     else hi = m;
   }
-  return min(max(near ? window[lo] : starts[b.base + lo], 0), t + 1);
+  return min(max(starts[lo], 0), t + 1);
 }
 
 // N consecutive elements of a row.
@@ -154,7 +167,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
 #pragma unroll
   for (int s = 0; s < 4; ++s) ld<8>(Q + 16 * s, a.vec, q[s]);
   int* window = reinterpret_cast<int*>(wo);
-  const Borders near = borders_near(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm));
+  const Borders near = borders_near(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm), [] {});
   const int lo = first_key(a.starts, a.n, window, near, row), hi = lo > row ? lo : row + 1;  // keys [lo, hi)
   // the keys that any of the rows sees, and those that all see
   int k0 = hi > lo ? lo : a.tokens, k1 = hi > lo ? hi : 0, f0 = lo, f1 = hi;
@@ -328,8 +341,6 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
 // the rounded probabilities.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
 // A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then the values in the same way.
 constexpr int kWaitNext = (4 & 15) | (7 << 4);  // vmcnt <= 4: the copies of the tile behind the next; lgkmcnt 0
@@ -344,24 +355,76 @@ __device__ __forceinline__ uint32_t finite2(uint32_t x) {
 }
 }  // namespace
 
-// Keys and values k0 .. k0 + 63 (rows past the last are the last) into a stage.
-__device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const PromptArgs& a, int k0, uint4* stage) {
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// A pointer that is the same in every lane, kept out of their registers.
+__device__ __forceinline__ const char* in_sgpr(const void* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+}
+// Where a lane's chunks of a tile lie: rows w * 16 + 8 j + lane / 8 (j = 0, 1), bytes from the tile's first row.
+struct Chunks {
+  uint32_t k, v;
+};
+// Reads of a tile in asm, for the compiler would wait for every copy under way before each of them.
+// 32 keys as the operands of four products: the lane's dims 16 s + 8 lk .. + 7 lie at `at` ^ 32 s.
+__device__ __forceinline__ void read_keys(uint32_t at, bf16x8 (&x)[4]) {
+  asm volatile(
+      "ds_read_b128 %0, %4\n\t"
+      "ds_read_b128 %1, %5\n\t"
+      "ds_read_b128 %2, %6\n\t"
+      "ds_read_b128 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+      : "v"(at), "v"(at ^ 32u), "v"(at ^ 64u), "v"(at ^ 96u)
+      : "memory");
+}
+// The values of 32 keys as the operands of four products, [sixteen keys][dim half]; `at` ^ 64: the other half.  The wait falls into
+// the time that the scores' products take.
+__device__ __forceinline__ void read_values(uint32_t at, bf16x8 (&x)[2][2]) {
+  uint2 r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:2048\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:3072\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:2048\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:3072\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(at), "v"(at ^ 64u)
+      : "memory");
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int slot = (w * 2 + j) * 64 + lane, r = slot >> 3, ch = (slot & 7) ^ (r & 7);
-    __builtin_amdgcn_global_load_lds((const void*)(K + min(k0 + r, a.tokens - 1) * a.kt + 8 * ch), (lds_void*)&stage[(w * 2 + j) * 64], 16, 0, 0);
-  }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int slot = (w * 2 + j) * 64 + lane, r = slot >> 3, ch = (slot & 7) ^ (r & 7);
-    __builtin_amdgcn_global_load_lds((const void*)(V + min(k0 + r, a.tokens - 1) * a.vt + 8 * ch), (lds_void*)&stage[512 + (w * 2 + j) * 64], 16, 0, 0);
+  for (int i = 0; i < 4; ++i) x[i >> 1][i & 1] = __builtin_bit_cast(bf16x8, make_uint4(r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y));
+}
+
+// Keys and values k0 .. k0 + 63 (rows outside the tensors are the nearest) into a stage: the tile's address is the wave's, a
+// lane adds its constant chunk.
+__device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const PromptArgs& a, int k0, const Chunks& c, uint4* stage) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // (the instruction's own offset would move both addresses)
+  lds_void *ks0 = (lds_void*)&stage[w * 128], *ks1 = (lds_void*)&stage[w * 128 + 64];
+  lds_void *vs0 = (lds_void*)&stage[512 + w * 128], *vs1 = (lds_void*)&stage[512 + w * 128 + 64];
+  if (k0 >= 0 && k0 + kTile <= a.tokens) {
+    const char *kp = in_sgpr(K + k0 * a.kt), *vp = in_sgpr(V + k0 * a.vt);
+    __builtin_amdgcn_global_load_lds((const void*)(kp + c.k), ks0, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(in_sgpr(kp + 16 * a.kt) + c.k), ks1, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(vp + c.v), vs0, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(in_sgpr(vp + 16 * a.vt) + c.v), vs1, 16, 0, 0);
+  } else {
+    const int r = w * 16 + (lane >> 3), ch = 8 * ((lane ^ (lane >> 3)) & 7), last = a.tokens - 1;
+    const int r0 = min(max(k0 + r, 0), last), r1 = min(max(k0 + r + 8, 0), last);
+    __builtin_amdgcn_global_load_lds((const void*)(K + r0 * a.kt + ch), ks0, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(K + r1 * a.kt + ch), ks1, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(V + r0 * a.vt + ch), vs0, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(V + r1 * a.vt + ch), vs1, 16, 0, 0);
   }
 }
 
-template <int NQ>
-__global__ void __launch_bounds__(256, 2) k_prompt16(PromptArgs a, int tiles, int per) {
-  __shared__ uint4 st0[kStage], st1[kStage], st2[kStage];
+template <int NQ, int KB, int WAVES>
+__global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles, int per) {
+  __shared__ uint4 stages[3 * kStage];
   // The blocks that one XCD gets (every eighth) are neighbours: one head's, whose keys and values its L2 then
   // holds, those with the most keys first.
   const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -371,115 +434,114 @@ __global__ void __launch_bounds__(256, 2) k_prompt16(PromptArgs a, int tiles, in
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head * a.qh;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (head / a.group) * a.kh;
   const bf16* V = reinterpret_cast<const bf16*>(a.v) + (head / a.group) * a.vh;
-  __shared__ int window[kWindow], first[4], last[4], from[4], to[4], odd[4];  // odd: the last tile of a stage that held a NaN or an infinity
-  const Borders near = borders_near(a.starts, a.n, q0, window, first);
-  // the wave's rows, the keys [lo, hi) that each sees, and those that any or all of the wave's do
-  int row[NQ], lo[NQ], hi[NQ], w0 = a.tokens, w1 = 0, f0 = 0, f1 = a.tokens;
+  __shared__ int window[kWindow], odd[4];  // odd: the last tile of a stage that held a NaN or an infinity
+  // Tile t: keys e - 64 (t + 1) .. e - 64 t - 1, from the block's own rows back to its first sequence's first row, so
+  // that the first two can be copied before the borders are known.
+  const int rows = 128 * NQ, e = min(q0 + rows, a.tokens), r0 = q0 + w * 32 * NQ;
+  const uint32_t crow = w * 16 + (lane >> 3), cbyte = 16 * ((lane ^ (lane >> 3)) & 7);
+  const Chunks chunks{crow * 2 * (uint32_t)a.kt + cbyte, crow * 2 * (uint32_t)a.vt + cbyte};
+  int row[NQ], lo[NQ];  // a row and the first key that it sees (the row + 1: none)
   bf16x8 qf[NQ][4];
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
-    row[u] = q0 + (w * NQ + u) * 32 + lr;
-    const int r = min(row[u], a.tokens - 1);
-    lo[u] = first_key(a.starts, a.n, window, near, r);
-    hi[u] = lo[u] > r ? lo[u] : r + 1;
-    if (lo[u] < hi[u]) {
-      w0 = min(w0, lo[u]);
-      w1 = max(w1, hi[u]);
-    }
-    f0 = max(f0, lo[u]);
-    f1 = min(f1, hi[u]);
+    row[u] = min(r0 + u * 32 + lr, a.tokens - 1);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) qf[u][s] = *reinterpret_cast<const bf16x8*>(Q + r * a.qt + 16 * s + 8 * lk);
+    for (int s = 0; s < 4; ++s) qf[u][s] = *reinterpret_cast<const bf16x8*>(Q + row[u] * a.qt + 16 * s + 8 * lk);
+  }
+  auto copy_first = [&] {
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) prompt_copy(K, V, a, e - (t + 1) * kTile, chunks, stages + t * kStage);
+    if (threadIdx.x < 4) odd[threadIdx.x] = -1;
+  };
+  const Borders near = borders_near(a.starts, a.n, q0, window, odd, copy_first);
+  // first keys do not decrease along the rows: of the wave's rows, and of the block's first and last
+  int first = 0, bound = 0;
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    const int x = first_key(a.starts, a.n, window, near, i == 0 ? min(r0 + lane, a.tokens - 1) : lane & 1 ? e - 1 : q0);
+    first = i == 0 ? x : first;
+    bound = x;
   }
 #pragma unroll
-  for (int m = 1; m < 32; m <<= 1) {
-    w0 = min(w0, __shfl_xor(w0, m));
-    w1 = max(w1, __shfl_xor(w1, m));
-    f0 = max(f0, __shfl_xor(f0, m));
-    f1 = min(f1, __shfl_xor(f1, m));
-  }
-  if (lane == 0) {
-    first[w] = w0;
-    last[w] = w1;
-    from[w] = f0;
-    to[w] = f1;
-    odd[w] = -1;
-  }
-  __syncthreads();
-  w0 = __builtin_amdgcn_readfirstlane(w0);
-  w1 = __builtin_amdgcn_readfirstlane(w1);
-  f0 = __builtin_amdgcn_readfirstlane(f0);
-  f1 = __builtin_amdgcn_readfirstlane(f1);
-  const int k0 = __builtin_amdgcn_readfirstlane(min(min(first[0], first[1]), min(first[2], first[3])));
-  const int k1 = __builtin_amdgcn_readfirstlane(max(max(last[0], last[1]), max(last[2], last[3])));
-  const int b0 = __builtin_amdgcn_readfirstlane(max(max(from[0], from[1]), max(from[2], from[3])));
-  const int b1 = __builtin_amdgcn_readfirstlane(min(min(to[0], to[1]), min(to[2], to[3])));
-  const int nt = k1 > k0 ? (k1 - k0 + kTile - 1) / kTile : 0;
+  for (int u = 0; u < NQ; ++u) lo[u] = __shfl(first, 32 * u + lr);
+  const int k0 = __builtin_amdgcn_readlane(bound, 0), b0 = __builtin_amdgcn_readlane(bound, 1);
+  const int w0 = __builtin_amdgcn_readlane(first, 0), f0 = __builtin_amdgcn_readlane(first, 32 * NQ - 1);
+  const int nt = (e - min(k0, e) + kTile - 1) / kTile;
   // Scores are formed less a reference of their row (the products' accumulators start at its negative,
   // `nref`), so p = 2^(kScale s) with no rounding of the reference in it.  It becomes the maximum of the first tile
   // with a score above -inf, then moves only when a score passes it by kRaise: p stays below 2^8
   constexpr float kRaise = 8.f / kScale;
-  constexpr int KB = NQ == 1 ? 2 : 1;  // halves of a tile at a time, as registers allow
-  float raise[NQ], l[NQ], nref[NQ];
-  floatx16 o[NQ][2];
+  float raise[NQ], l[NQ];
+  floatx16 nref[NQ], o[NQ][2];
+  auto clear = [&] {
 #pragma unroll
-  for (int u = 0; u < NQ; ++u) {
-    raise[u] = -INFINITY;
-    l[u] = nref[u] = 0.f;
+    for (int u = 0; u < NQ; ++u) {
+      raise[u] = -INFINITY;
+      l[u] = 0.f;
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[u][d][v] = 0.f;
-  }
+      for (int v = 0; v < 16; ++v) nref[u][v] = o[u][0][v] = o[u][1][v] = 0.f;
+    }
+  };
+  clear();
+  bool careful = false;
+  // a lane's key lk (chunk) of row lr; its part of sixteen keys by sixteen dims, as ds_read_b64_tr_b16 turns them: row 4 lk + lane / 4 % 4 (and 8 on), the 8-byte
+  // piece lane % 4 of dims 16 (lane / 16 % 2) ..
+  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
+  const uint32_t kat = 128 * lr + 16 * (lk ^ (lr & 7)), vat = 8192 + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
   auto step = [&](int t, uint4* cur, uint4* nxt) {
+    const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)cur;
     __builtin_amdgcn_s_waitcnt(kWaitNext);
-    const int kt = k0 + t * kTile;
-    const bool cut = t < nt && (kt < b0 || kt + kTile > b1);  // some row of the block does not see some key
-    if (cut) {
-      // A NaN or an infinity times a probability of 0 would reach the rows that do not see it: such values
-      // leave the tile, each wave looking at what it copied, and are added to the rows that do below.
+    const int kt = e - (t + 1) * kTile;
+    const bool cut = careful && (kt < b0 || kt + kTile > q0 + 1);  // some row of the block does not see some key
+    if (cut) {  // what is not finite among the values leaves the tile, each wave looking at what it copied
       uint4* own = cur + 512 + 128 * w + lane;
-      const uint4 x[2] = {own[0], own[64]};
-      float z = 0.f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) z = dot2(x[j].x, 0u, dot2(x[j].y, 0u, dot2(x[j].z, 0u, dot2(x[j].w, 0u, z))));
-      if (__builtin_amdgcn_ballot_w64(z != 0.f)) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) own[64 * j] = make_uint4(finite2(x[j].x), finite2(x[j].y), finite2(x[j].z), finite2(x[j].w));
-        if (lane == 0) odd[t & 3] = t;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      for (int j = 0; j < 2; ++j) {
+        const uint4 x = own[64 * j], y = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
+        if (__builtin_amdgcn_ballot_w64(((x.x ^ y.x) | (x.y ^ y.y) | (x.z ^ y.z) | (x.w ^ y.w)) != 0)) {
+          own[64 * j] = y;
+          if (lane == 0) odd[t & 3] = t;
+        }
       }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     }
     __builtin_amdgcn_s_barrier();
-    prompt_copy(K, V, a, k0 + min(t + 2, nt - 1) * kTile, nxt);  // every step issues its copies: exact wait counts
-    if (t >= nt || kt >= w1 || kt + kTile <= w0) return;
+    prompt_copy(K, V, a, e - min(t + 3, nt) * kTile, chunks, nxt);  // every step issues its copies: exact wait counts
+    if (kt >= r0 + 32 * NQ || kt + kTile <= w0) return;
 #pragma unroll 1
     for (int h0 = 0; h0 < 2; h0 += KB) {
+      const int kh = kt + 32 * h0;
+      if (kh >= r0 + 32 * NQ || kh + 32 * KB <= w0) continue;
       floatx16 sc[NQ][KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
+        bf16x8 kf[4];
+        read_keys(lds + 4096 * (h0 + kb) + kat, kf);
 #pragma unroll
-        for (int u = 0; u < NQ; ++u)
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) sc[u][kb][v] = nref[u];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const int r = (h0 + kb) * 32 + lr;
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, cur[r * 8 + ((2 * s + lk) ^ (r & 7))]);
-#pragma unroll
-          for (int u = 0; u < NQ; ++u) sc[u][kb] = mfma32(kf, qf[u][s], sc[u][kb]);
-        }
+          for (int u = 0; u < NQ; ++u) sc[u][kb] = mfma32(kf[s], qf[u][s], s == 0 ? nref[u] : sc[u][kb]);
       }
-      if (kt < f0 || kt + kTile > f1) {  // uniform: some row does not see some key
+      bf16x8 vf[KB][2][2];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) read_values(lds + 4096 * (h0 + kb) + vat, vf[kb]);
+      if (kh + 32 * KB > r0 + 1) {  // uniform: some row of the wave does not see some key behind it
 #pragma unroll
         for (int u = 0; u < NQ; ++u)
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const int key = kt + (h0 + kb) * 32 + 8 * (v >> 2) + 4 * lk + (v & 3);
-              sc[u][kb][v] = (uint32_t)(key - lo[u]) < (uint32_t)(hi[u] - lo[u]) ? sc[u][kb][v] : -INFINITY;
-            }
+            for (int v = 0; v < 16; ++v)
+              sc[u][kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) <= row[u] - kh - 4 * lk ? sc[u][kb][v] : -INFINITY;
+      }
+      if (kh < f0) {  // nor keys of the sequence before
+#pragma unroll
+        for (int u = 0; u < NQ; ++u)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              sc[u][kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) >= lo[u] - kh - 4 * lk ? sc[u][kb][v] : -INFINITY;
       }
       uint32_t pk[NQ][KB][8];
 #pragma unroll
@@ -503,7 +565,8 @@ __global__ void __launch_bounds__(256, 2) k_prompt16(PromptArgs a, int tiles, in
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) sc[u][kb][v] -= d;
-          nref[u] -= d;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) nref[u][v] -= d;
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -519,55 +582,59 @@ __global__ void __launch_bounds__(256, 2) k_prompt16(PromptArgs a, int tiles, in
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int d = 0; d < 2; ++d) {
-            // eight keys 4 lk + 8 h + .. of sixteen for the lane's dim: a lane reads row lane / 4 % 4 of them, the 8-byte piece lane % 4
-            // of sixteen dims
-            uint2 x[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int r = (h0 + kb) * 32 + 16 * s + 8 * h + 4 * lk + ((lane >> 2) & 3), c = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-              const char* p = reinterpret_cast<const char*>(cur + 512 + r * 8 + (c ^ (r & 7))) + 8 * (lane & 1);
-              x[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
-            }
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(x[0].x, x[0].y, x[1].x, x[1].y));
 #pragma unroll
             for (int u = 0; u < NQ; ++u) {
               const uint4 p = make_uint4(pk[u][kb][4 * s], pk[u][kb][4 * s + 1], pk[u][kb][4 * s + 2], pk[u][kb][4 * s + 3]);
-              o[u][d] = mfma32(vf, __builtin_bit_cast(bf16x8, p), o[u][d]);
+              o[u][d] = mfma32(vf[kb][s][d], __builtin_bit_cast(bf16x8, p), o[u][d]);
             }
           }
     }
-    if (cut && __builtin_amdgcn_readfirstlane(odd[t & 3]) == t) {  // what left the tile, for the rows that see it
+    if (cut && __builtin_amdgcn_readfirstlane(odd[t & 3]) == t) {  // and is added for the rows that see it
 #pragma unroll 1
-      for (int key = kt; key < min(kt + kTile, k1); ++key) {
+      for (int key = max(kt, 0); key < kt + kTile; ++key) {
         const bf16* vp = V + key * a.vt + 4 * lk;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int g = 0; g < 8; ++g) {
           float x[4];
-          ld<4>(vp + 8 * e, 1, x);
+          ld<4>(vp + 8 * g, 1, x);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float y = finite(x[i]) ? 0.f : x[i];
 #pragma unroll
-            for (int u = 0; u < NQ; ++u) o[u][e >> 2][4 * (e & 3) + i] += (uint32_t)(key - lo[u]) < (uint32_t)(hi[u] - lo[u]) ? y : 0.f;
+            for (int u = 0; u < NQ; ++u) o[u][g >> 2][4 * (g & 3) + i] += key >= lo[u] && key <= row[u] ? y : 0.f;
           }
         }
       }
     }
   };
-  if (nt > 0) {
-    prompt_copy(K, V, a, k0, st0);
-    prompt_copy(K, V, a, k0 + min(1, nt - 1) * kTile, st1);
-    for (int t = 0; t < nt; t += 3) {
-      step(t, st0, st2);
-      step(t + 1, st1, st0);
-      step(t + 2, st2, st1);
+  for (;;) {
+    uint4 *cur = stages, *nxt = stages + 2 * kStage;
+    for (int t = 0; t < nt; ++t) {
+      step(t, cur, nxt);
+      nxt = cur;
+      cur = cur == stages + 2 * kStage ? stages : cur + kStage;
     }
     __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy may land in LDS after the block has left
+    if (careful) break;
+    // A NaN or an infinity among the values reaches rows that do not see it, as its product with a probability of 0.
+    // Where a result is not finite the block starts again and keeps such values out of the tiles that are not whole.
+    float z = 0.f;
+#pragma unroll
+    for (int u = 0; u < NQ; ++u)
+#pragma unroll
+      for (int v = 0; v < 32; ++v) z = fmaf(o[u][v >> 4][v & 15], 0.f, z);
+    if (__builtin_amdgcn_ballot_w64(z != 0.f) && lane == 0) window[0] = -1 - kWindow;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(window[0]) != -1 - kWindow) break;
+    careful = true;
+    clear();
+    copy_first();
+    __syncthreads();
   }
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
     const float total = pair_sum(l[u]), inv = total == 0.f ? 0.f : 1.f / total;
-    if (row[u] >= a.tokens) continue;
+    if (r0 + u * 32 + lr >= a.tokens) continue;
     if (!a.clear && (row[u] < near.begin || row[u] >= near.end)) continue;
     // O^T: lane holds row lr, dims 32 d + 8 (v / 4) + 4 lk + v % 4
     bf16* op = reinterpret_cast<bf16*>(a.out) + ((size_t)row[u] * a.heads + head) * kHeadDim;
@@ -579,10 +646,10 @@ __global__ void __launch_bounds__(256, 2) k_prompt16(PromptArgs a, int tiles, in
             make_uint2(pack2_bf16(o[u][d][4 * g] * inv, o[u][d][4 * g + 1] * inv), pack2_bf16(o[u][d][4 * g + 2] * inv, o[u][d][4 * g + 3] * inv));
   }
 }
-template <int NQ>
+template <int NQ, int KB, int WAVES>
 static void prompt16(const PromptArgs& a, hipStream_t st) {
   const int tiles = (a.tokens + 128 * NQ - 1) / (128 * NQ), per = (int)(((long long)tiles * a.heads + 7) / 8);
-  k_prompt16<NQ><<<8 * per, 256, 0, st>>>(a, tiles, per);
+  k_prompt16<NQ, KB, WAVES><<<8 * per, 256, 0, st>>>(a, tiles, per);
 }
 
 template <typename T>
@@ -593,9 +660,12 @@ static void prompt32(const PromptArgs& a, hipStream_t st) {
 
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
   if (!a.bf16_data) return prompt32<float>(a, st);
-  if (!a.vec) return prompt32<bf16>(a, st);
-  if (a.tokens > 4096) return prompt16<2>(a, st);
-  prompt16<1>(a, st);
+  // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
+  if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
+  const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;
+  if (mean >= 8192 && blocks >= 4096) return prompt16<2, 1, 2>(a, st);
+  if (mean < 2048 && blocks >= 768) return prompt16<1, 1, 3>(a, st);
+  prompt16<1, 2, 2>(a, st);
 }
 
 }  // namespace wf

@@ -339,6 +339,47 @@ def test_prompt_long(dtype):
         assert (np.abs(num(got[i:i + 1]) - want) <= bound(want, spread, size, T, dtype, dtype == BF16)).all()
 
 
+def check_rows(q, k, v, got, starts, rows):
+    """Rows of a large call, each against 64 bits."""
+    rounded = q.dtype == BF16
+    for i in rows:
+        a = max(s for s in starts if s <= i)
+        want, spread, size = plain.seen_attention(num(q[i:i + 1]), num(k[a:i + 1]), num(v[a:i + 1]), np.ones((1, i + 1 - a), bool))
+        bad = ~np.isfinite(want)
+        g = num(got[i:i + 1])
+        assert np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[np.isinf(want)], want[np.isinf(want)]), i
+        tol = bound(np.where(bad, 0, want), np.where(bad, 0, spread), size, i + 1 - a, q.dtype, rounded)
+        assert (np.abs(np.where(bad, 0, g) - np.where(bad, 0, want)) <= tol).all(), i
+
+
+@pytest.mark.parametrize("T,H,KV,lens", [(12345, 9, 3, 97), (12345, 8, 8, 13), (40000, 4, 1, 40), (33000, 20, 5, 1), (33100, 16, 16, 3), (70000, 16, 1, 2)])
+@pytest.mark.parametrize("odd", [False, True])
+def test_prompt_many_blocks(T, H, KV, lens, odd):
+    """bf16 calls of many blocks, short sequences and long ones, each with its own tiles; NaN and infinities in some values."""
+    rng = np.random.default_rng(T)
+    q, k, v = packed(T, H, KV, BF16)
+    cuts = np.sort(rng.choice(np.arange(1, T), lens - 1, replace=False)).tolist() if lens > 1 else []
+    starts = [0] + cuts + [T]
+    if lens in (2, 3):
+        starts = [0] + [T * i // lens for i in range(1, lens)] + [T - 77]
+    at = int(rng.integers(1000, 9000))
+    clean = None
+    if odd:
+        clean = lib().prompt_attention(q, k, v, i32(starts))
+        v[at, :, 3], v[at + 1, :, 4], v[at + 70, :, 3] = INF, NAN, -INF
+    got = lib().prompt_attention(q, k, v, i32(starts))
+    rows = {0, 1, 63, 64, 127, 128, 255, 256, at - 1, at, at + 1, at + 63, at + 69, at + 70, T - 300, T - 78} | set(rng.integers(0, T - 78, 6).tolist())
+    rows |= {s + d for s in starts[1:4] for d in (-1, 0, 31, 32) if s + d < starts[-1]}
+    check_rows(q, k, v, got, starts, [i for i in rows if i < starts[-1]])
+    assert not got[starts[-1]:].any()
+    if odd:
+        end = min(s for s in starts if s > at)
+        sees = torch.zeros(T, dtype=torch.bool, device="cuda")
+        for a in (at, at + 1, at + 70):
+            sees[a:min(s for s in starts if s > a)] = True
+        assert torch.equal(got[~sees], clean[~sees]) and end > at
+
+
 def test_prompt_refuses_gradients():
     wf = lib()
     q, k, v = packed(10, 2, 1, F32)

@@ -41,10 +41,47 @@ __device__ __forceinline__ uint32_t mag_finite(float x) { return mag(x) >= 0x7f8
 // 2^(127 - byte) of a scale byte in [27, 247]
 __device__ __forceinline__ float inverse_f(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
-__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = umax(v, (uint32_t)__shfl_xor((int)v, m));
-  return v;
+__device__ __forceinline__ void values16(uint4 c, float s, float* x) {
+  values8x4(c.x, s, x);
+  values8x4(c.y, s, x + 4);
+  values8x4(c.z, s, x + 8);
+  values8x4(c.w, s, x + 12);
+}
+// The whole wave's maxima of two non-negative numbers, as floats' bits.
+template <int CTRL>
+__device__ __forceinline__ uint32_t umax_dpp(uint32_t v) {
+  return umax(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ uint32_t umax16(uint32_t v) {
+  return umax_dpp<kDppMirror>(umax_dpp<kDppHalfMirror>(umax_dpp<kDppXor2>(umax_dpp<kDppXor1>(v))));
+}
+__device__ __forceinline__ void wave_umax(uint32_t& a, uint32_t& b) {
+  a = umax16(a);
+  b = umax16(b);
+  auto lane = [](uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+  a = umax(umax(lane(a, 0), lane(a, 16)), umax(lane(a, 32), lane(a, 48)));
+  b = umax(umax(lane(b, 0), lane(b, 16)), umax(lane(b, 32), lane(b, 48)));
+}
+// Two consecutive elements.
+__device__ __forceinline__ void ld_two(const float* p, int vec, float* o) {
+  if (vec) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    o[0] = v.x;
+    o[1] = v.y;
+  } else {
+    o[0] = p[0];
+    o[1] = p[1];
+  }
+}
+__device__ __forceinline__ void ld_two(const bf16* p, int vec, float* o) {
+  if (vec) {
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    o[0] = __uint_as_float(v << 16);
+    o[1] = __uint_as_float(v & 0xffff0000u);
+  } else {
+    o[0] = to_f(p[0]);
+    o[1] = to_f(p[1]);
+  }
 }
 
 // ---------------------------------------------------------------- store
@@ -87,19 +124,14 @@ __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
   const int end = (int)min(count - skip, 16ll);
   const T* K = reinterpret_cast<const T*>(a.k) + (a.starts ? 0 : r * a.kr) + head * a.kh;
   const T* V = reinterpret_cast<const T*>(a.v) + (a.starts ? 0 : r * a.vr) + head * a.vh;
-  const uint32_t olds = kept ? *reinterpret_cast<const uint16_t*>(sc) : 0;
-
-  const int n = lane & 15, kg = lane >> 4;
-  float x[16];
-  if (n < kept) {
-    const uint4 c = *reinterpret_cast<const uint4*>(out + 16 * lane);
-    const float s = scale_f(olds & 255);
-    values8x4(c.x, s, x);
-    values8x4(c.y, s, x + 4);
-    values8x4(c.z, s, x + 8);
-    values8x4(c.w, s, x + 12);
-  } else if (n < end) {
-    const T* p = K + (first + skip + n) * a.ki + 16 * kg;
+  // Every load is issued before the first use and without a condition (positions that are no row's take the nearest
+  // row and are replaced): a load under one would make each wait for the one before.
+  const int n = lane & 15, kg = lane >> 4, h = lane >> 5, g = (lane >> 4) & 1;
+  auto row = [&](int f) { return first + (long long)min(max(skip + f, 0ll), (long long)count - 1); };
+  uint8_t* vout = out + kKv8Values + 32 * (16 * g + n) + 16 * h;
+  float x[16], y[8][2];  // y[j]: dims 4 n + 2 h, + 1 of position 8 g + j
+  {
+    const T* p = K + row(n) * a.ki + 16 * kg;
     if (a.vec) {
       ld8(p, x);
       ld8(p + 8, x + 8);
@@ -107,47 +139,44 @@ __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[j] = to_f(p[j]);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = 0.f;
   }
-  uint32_t m = 0;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) m = umax(m, mag_finite(x[j]));
-  const uint32_t ks = scale8_of(__uint_as_float(wave_umax(m)));
-  const float ki = inverse_f(ks);
-  const uint4 kc = make_uint4(codes8x4(x, ki), codes8x4(x + 4, ki), codes8x4(x + 8, ki), codes8x4(x + 12, ki));
-
-  // values: y[dd][j] = dim 4 n + 2 h + dd of position 8 g + j
-  const int h = lane >> 5, g = (lane >> 4) & 1;
-  uint8_t* vout = out + kKv8Values + 32 * (16 * g + n) + 16 * h;
-  float y[2][8];
-  if (kept > 8 * g) {
-    const uint4 c = *reinterpret_cast<const uint4*>(vout);
-    const float s = scale_f(olds >> 8);
-    values8x4(c.x, s, y[0]);
-    values8x4(c.y, s, y[0] + 4);
-    values8x4(c.z, s, y[1]);
-    values8x4(c.w, s, y[1] + 4);
-  }
-  m = 0;
+  for (int j = 0; j < 8; ++j) ld_two(V + row(8 * g + j) * a.vi + 4 * n + 2 * h, a.vec, y[j]);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int f = 8 * g + j;
-    if (f >= kept) {
-      y[0][j] = y[1][j] = 0.f;
-      if (f < end) {
-        const T* p = V + (first + skip + f) * a.vi + 4 * n + 2 * h;
-        y[0][j] = to_f(p[0]);
-        y[1][j] = to_f(p[1]);
-      }
+  for (int j = 0; j < 16; ++j) x[j] = n < end ? x[j] : 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int d = 0; d < 2; ++d) y[j][d] = 8 * g + j < end ? y[j][d] : 0.f;
+  if (kept) {  // uniform
+    const uint32_t old = *reinterpret_cast<const uint16_t*>(sc);
+    const uint4 c = *reinterpret_cast<const uint4*>(out + 16 * lane), d = *reinterpret_cast<const uint4*>(vout);
+    float z[16];
+    values16(c, scale_f(old & 255), z);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = n < kept ? z[j] : x[j];
+    values16(d, scale_f(old >> 8), z);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      y[j][0] = 8 * g + j < kept ? z[j] : y[j][0];
+      y[j][1] = 8 * g + j < kept ? z[8 + j] : y[j][1];
     }
-    m = umax(m, umax(mag_finite(y[0][j]), mag_finite(y[1][j])));
   }
-  const uint32_t vs = scale8_of(__uint_as_float(wave_umax(m)));
-  const float vi = inverse_f(vs);
+  uint32_t m = 0, m2 = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    m = umax(m, mag_finite(x[j]));
+    m2 = umax(m2, mag_finite(y[j >> 1][j & 1]));
+  }
+  wave_umax(m, m2);
+  const uint32_t ks = scale8_of(__uint_as_float(m)), vs = scale8_of(__uint_as_float(m2));
+  const float ki = inverse_f(ks), vi = inverse_f(vs);
+  const uint4 kc = make_uint4(codes8x4(x, ki), codes8x4(x + 4, ki), codes8x4(x + 8, ki), codes8x4(x + 12, ki));
+  float u[2][8];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) u[j & 1][j >> 1] = y[j >> 1][j & 1];
   *reinterpret_cast<uint4*>(out + 16 * lane) = kc;
-  *reinterpret_cast<uint4*>(vout) = make_uint4(codes8x4(y[0], vi), codes8x4(y[0] + 4, vi), codes8x4(y[1], vi), codes8x4(y[1] + 4, vi));
+  *reinterpret_cast<uint4*>(vout) = make_uint4(codes8x4(u[0], vi), codes8x4(u[0] + 4, vi), codes8x4(u[1], vi), codes8x4(u[1] + 4, vi));
   if (lane == 0) *reinterpret_cast<uint16_t*>(sc) = (uint16_t)(ks | vs << 8);
 }
 
@@ -164,8 +193,8 @@ __device__ __forceinline__ void st4(float* p, const float* x) { *reinterpret_cas
 __device__ __forceinline__ void st4(bf16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
 }
-// A wave per (request, column of its table, head): lane l = 16 kg + n the key's dims 16 kg .. + 15 of position n,
-// and dims 4 n .. + 3 of the values of positions 4 kg .. + 3.
+// A wave per (request, column of its table, head): lane l = 16 kg + n holds dims 4 n .. + 3 of positions 4 kg .. + 3, so that
+// a wave writes whole rows.
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
   const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
@@ -174,33 +203,32 @@ __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
   const int page = a.tables[r * a.ts + col];
   const int len = min(max(a.lens[r], 0), 16 * a.max_pages) - 16 * col;  // positions of this page
   const bool there = page >= 0 && page < a.c.n_pages && len > 0;
-  const size_t pitch = (size_t)a.c.n_head * kHeadDim, at = (size_t)blockIdx.x * 16 * pitch + head * kHeadDim;
+  const size_t pitch = (size_t)a.c.n_head * kHeadDim, at = ((size_t)blockIdx.x * 16 + 4 * kg) * pitch + head * kHeadDim + 4 * n;
   T* K = reinterpret_cast<T*>(a.k) + at;
   T* V = reinterpret_cast<T*>(a.v) + at;
-  float x[16], y[4][4];  // y[dt][j]: dim 4 n + dt of position 4 kg + j
-  if (there) {
+  float x[4][4], y[4][4];  // x[j]: dims 4 n .. of position 4 kg + j; y[dt]: dim 4 n + dt of those positions
+  if (there) {             // uniform
     const uint8_t* in = a.c.base + page * a.c.page + (size_t)head * kKv8Head;
     const uint32_t s = *reinterpret_cast<const uint16_t*>(a.c.base + page * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head);
-    const uint4 c = *reinterpret_cast<const uint4*>(in + 16 * lane);
-    values8x4(c.x, scale_f(s & 255), x);
-    values8x4(c.y, scale_f(s & 255), x + 4);
-    values8x4(c.z, scale_f(s & 255), x + 8);
-    values8x4(c.w, scale_f(s & 255), x + 12);
+    uint32_t c[4], v[4];
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(in + kKv8Values + 32 * (16 * (kg >> 1) + n) + 8 * dt + 4 * (kg & 1));
-      values8x4(v, scale_f(s >> 8), y[dt]);
+    for (int j = 0; j < 4; ++j) {
+      c[j] = *reinterpret_cast<const uint32_t*>(in + 16 * (16 * (n >> 2) + 4 * kg + j) + 4 * (n & 3));
+      v[j] = *reinterpret_cast<const uint32_t*>(in + kKv8Values + 32 * (16 * (kg >> 1) + n) + 8 * j + 4 * (kg & 1));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      values8x4(c[j], scale_f(s & 255), x[j]);
+      values8x4(v[j], scale_f(s >> 8), y[j]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 16; ++j) x[j] = there && n < len ? x[j] : 0.f;
-#pragma unroll
-  for (int j = 0; j < 16; j += 4) st4(K + n * pitch + 16 * kg + j, x + j);
-#pragma unroll
   for (int j = 0; j < 4; ++j) {
     const bool in = there && 4 * kg + j < len;
-    const float o[4] = {in ? y[0][j] : 0.f, in ? y[1][j] : 0.f, in ? y[2][j] : 0.f, in ? y[3][j] : 0.f};
-    st4(V + (4 * kg + j) * pitch + 4 * n, o);
+    const float p[4] = {in ? x[j][0] : 0.f, in ? x[j][1] : 0.f, in ? x[j][2] : 0.f, in ? x[j][3] : 0.f};
+    const float q[4] = {in ? y[0][j] : 0.f, in ? y[1][j] : 0.f, in ? y[2][j] : 0.f, in ? y[3][j] : 0.f};
+    st4(K + j * pitch, p);
+    st4(V + j * pitch, q);
   }
 }
 
@@ -223,7 +251,7 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 //            merge kernel
 namespace {
 constexpr float kLog2e = 1.44269504088896f;
-constexpr int kWaves = 8, kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
+constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
 
 __device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
@@ -384,10 +412,10 @@ __device__ __forceinline__ void kv8_rows(const Kv8AttendArgs& a, int r, int& pos
   pos = min(max(a.positions[r], -(1 << 20)), 16 * a.max_pages);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
+template <typename T, int NW>
+__global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
-  __shared__ float wm[kWaves][16], wl[kWaves][16], wo[kWaves][16][68];
+  __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, c0 = blockIdx.z * 16;
   const int cols = a.rows * a.group, cap = 16 * a.max_pages;
@@ -407,14 +435,16 @@ __global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
   st.l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) st.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto load = [&](int g, Step& s) {
-    const int pages = (top + 15) / 16;
+  const int g0 = chunk * each + w, pages = (top + 15) / 16;
+  int ahead = 0;  // the page numbers of 32 of the wave's steps, two a step
+  auto numbers = [&](int i) { ahead = table[min(2 * (g0 + (i + (lane >> 1)) * NW) + (lane & 1), pages - 1)]; };
+  auto load = [&](int i, Step& s) {  // the wave's step i, or its last
+    if ((i & 31) == 0) numbers(i);
     int p[2];
     s.there = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int c = min(2 * min(g, end - 1) + t, pages - 1);
-      p[t] = __builtin_amdgcn_readfirstlane(table[c]);
+      p[t] = __builtin_amdgcn_readlane(ahead, 2 * (i & 31) + t);
       if (p[t] >= 0 && p[t] < a.c.n_pages) s.there |= 1u << t;
       else p[t] = 0;
     }
@@ -430,10 +460,9 @@ __global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
     s.v[0] = *reinterpret_cast<const uint4*>(in);
     s.v[1] = *reinterpret_cast<const uint4*>(in + 16);
   };
-  int g = chunk * each + w;
-  if (g < end) {
+  if (g0 < end) {
     Step A, B;
-    load(g, A);
+    load(0, A);
     const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(i, a.rows - 1) * a.si +
                  (head * a.group + col % a.group) * a.sh + 16 * kg;
     float x[16];
@@ -449,15 +478,14 @@ __global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
     bf16x8 qt[2][QT];
     split_terms<QT>(x, qt[0]);
     split_terms<QT>(x + 8, qt[1]);
-    for (;;) {
-      load(g + kWaves, B);
-      kv8_step<QT, PT>(A, 32 * g, lim, low, top, qt, st);
-      g += kWaves;
-      if (g >= end) break;
-      load(g + kWaves, A);
-      kv8_step<QT, PT>(B, 32 * g, lim, low, top, qt, st);
-      g += kWaves;
-      if (g >= end) break;
+    const int steps = (end - g0 + NW - 1) / NW;
+    for (int i = 0;;) {
+      load(i + 1, B);
+      kv8_step<QT, PT>(A, 32 * (g0 + i * NW), lim, low, top, qt, st);
+      if (++i >= steps) break;
+      load(i + 1, A);
+      kv8_step<QT, PT>(B, 32 * (g0 + i * NW), lim, low, top, qt, st);
+      if (++i >= steps) break;
     }
   }
   const float l = swap_sum(st.l);
@@ -471,14 +499,14 @@ __global__ void __launch_bounds__(kWaves * 64) k_kv8_attend(Kv8AttendArgs a) {
     *reinterpret_cast<floatx4*>(&wo[w][n][16 * kg + 4 * e]) = floatx4{st.o[0][e], st.o[1][e], st.o[2][e], st.o[3][e]};
   __syncthreads();
   const int nc = min(16, cols - c0);
-  for (int t = threadIdx.x; t < nc * 64; t += kWaves * 64) {
+  for (int t = threadIdx.x; t < nc * 64; t += NW * 64) {
     const int c = t >> 6, d = t & 63, ci = (c0 + c) / a.group;
     float M = wm[0][c], L = 0.f, O = 0.f;
 #pragma unroll
-    for (int j = 1; j < kWaves; ++j) M = fmaxf(M, wm[j][c]);
+    for (int j = 1; j < NW; ++j) M = fmaxf(M, wm[j][c]);
     const float base = no_inf(M);
 #pragma unroll
-    for (int j = 0; j < kWaves; ++j) {
+    for (int j = 0; j < NW; ++j) {
       const float f = exp_to(wm[j][c], base);  // 0 for a wave of no positions
       L = fmaf(f, wl[j][c], L);
       O = fmaf(f, wo[j][c][d], O);
@@ -541,10 +569,12 @@ __global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
   }
 }
 
-// Chunks of the positions: towards four blocks a compute unit, each of two steps of every wave at least.
+// Waves of a block, and chunks of the positions: towards four blocks of eight waves a compute unit, each of two steps of every
+// wave at least.
+static int kv8_waves(int max_pages) { return max_pages <= 32 ? 4 : 8; }
 static int kv8_chunks(int n, int rows, int group, int n_head, int max_pages) {
   const long long blocks = (long long)n * n_head * ((rows * group + 15) / 16), groups = (max_pages + 1) / 2;
-  return (int)std::max<long long>(1, std::min<long long>(1024 / blocks, groups / (2 * kWaves)));
+  return (int)std::max<long long>(1, std::min<long long>(1024 / blocks, groups / 16));
 }
 size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages) {
   const int nc = kv8_chunks(n, rows, group, n_head, max_pages);
@@ -554,7 +584,9 @@ size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages) {
 template <typename T>
 static void attend_launch(const Kv8AttendArgs& a, hipStream_t st) {
   const int cols = a.rows * a.group;
-  k_kv8_attend<T><<<dim3(a.c.n_head * a.nchunk, a.n, (cols + 15) / 16), kWaves * 64, 0, st>>>(a);
+  const dim3 grid(a.c.n_head * a.nchunk, a.n, (cols + 15) / 16);
+  if (kv8_waves(a.max_pages) == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
+  else k_kv8_attend<T, 8><<<grid, 512, 0, st>>>(a);
   if (a.nchunk > 1) k_kv8_merge<T><<<dim3(a.c.n_head, a.n, cols), 256, 0, st>>>(a);
 }
 void kv8_attend(const Kv8AttendArgs& a0, hipStream_t st) {

@@ -31,114 +31,162 @@ __device__ __forceinline__ float2 turn(double x, float amp) {
   return make_float2(((q + 1) & 2 ? -co : co) * amp, (q & 2 ? -si : si) * amp);
 }
 
-// `N` consecutive elements of a row as fp32 and back.
-template <int N>
-__device__ __forceinline__ void ld(const float* p, float* o) {
-  if constexpr (N == 4) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
-  } else o[0] = p[0];
-}
-template <int N>
-__device__ __forceinline__ void ld(const bf16* p, float* o) {
-  if constexpr (N == 8) ld8(p, o);
-  else o[0] = to_f(p[0]);
-}
-template <int N>
-__device__ __forceinline__ void st(float* p, const float* v) {
-  if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  else p[0] = v[0];
-}
-template <int N>
-__device__ __forceinline__ void st(bf16* p, const float* v) {
-  if constexpr (N == 8)
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
-  else p[0] = from_f<bf16>(v[0]);
-}
-
-// Block: `tb` tokens.  First their sines and cosines into LDS, then every (token, head, unit of N
-// elements): a unit of halves is N elements and their partners, one of interleaved pairs N (one
-// element: the pair) elements, the units behind `dims` are copied.
+// N consecutive elements of a row as they lie in memory, and their values.
 template <typename T, int N>
-__global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
-  extern __shared__ float2 cs[];
-  const int half = a.dims >> 1, t0 = (blockIdx.x + gridDim.x * blockIdx.z) * a.tb, nt = min(a.tb, a.tokens - t0);
-  if (nt <= 0) return;
-  for (int i = threadIdx.x; i < nt * half; i += 256) {
-    const int t = i / half, j = i - t * half;
-    float2 z = turn((double)a.positions[t0 + t] * a.turns[j], a.amplitude);
-    if (a.transposed) z.y = -z.y;
-    cs[i] = z;
-  }
-  __syncthreads();
-  const int tu = N == 1 ? half : a.interleaved ? a.dims / N : half / N, units = tu + (a.copies ? (a.width - a.dims) / N : 0);
-  const int heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0), total = nt * heads * units;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < total; i += gridDim.y * 256) {
-    const int r = i / units, u = i - r * units, t = r / heads;
-    int h = r - t * heads;
-    const bool second = h >= a.rows[0].heads;
-    const RotaryRows& w = a.rows[second];
-    if (second) h -= a.rows[0].heads;
-    const T* x = reinterpret_cast<const T*>(w.x) + (t0 + t) * w.xt + h * w.xh;
-    T* y = reinterpret_cast<T*>(w.y) + (t0 + t) * w.yt + h * w.yh;
-    const float2* z = cs + t * half;
-    if (u >= tu) {
-      const int at = a.dims + (u - tu) * N;
-      float v[N];
-      ld<N>(x + at, v);
-      st<N>(y + at, v);
-    } else if (!a.interleaved) {
-      float p[N], q[N], o[N], s[N];
-      ld<N>(x + u * N, p);
-      ld<N>(x + half + u * N, q);
+struct Raw;
+template <>
+struct Raw<float, 4> {
+  float4 v;
+  __device__ __forceinline__ void get(float* o) const { o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w; }
+  __device__ __forceinline__ void set(const float* o) { v = make_float4(o[0], o[1], o[2], o[3]); }
+};
+template <>
+struct Raw<float, 1> {
+  float v;
+  __device__ __forceinline__ void get(float* o) const { o[0] = v; }
+  __device__ __forceinline__ void set(const float* o) { v = o[0]; }
+};
+template <>
+struct Raw<bf16, 8> {
+  uint4 v;
+  __device__ __forceinline__ void get(float* o) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float2 c = z[u * N + j];
-        o[j] = fmaf(p[j], c.x, -(q[j] * c.y));
-        s[j] = fmaf(q[j], c.x, p[j] * c.y);
-      }
-      st<N>(y + u * N, o);
-      st<N>(y + half + u * N, s);
-    } else if constexpr (N == 1) {
-      float p, q;
-      ld<1>(x + 2 * u, &p);
-      ld<1>(x + 2 * u + 1, &q);
-      const float2 c = z[u];
-      const float o = fmaf(p, c.x, -(q * c.y)), s = fmaf(q, c.x, p * c.y);
-      st<1>(y + 2 * u, &o);
-      st<1>(y + 2 * u + 1, &s);
-    } else {
-      float p[N];
-      ld<N>(x + u * N, p);
-#pragma unroll
-      for (int j = 0; j < N; j += 2) {
-        const float2 c = z[(u * N + j) >> 1];
-        const float o = fmaf(p[j], c.x, -(p[j + 1] * c.y));
-        p[j + 1] = fmaf(p[j + 1], c.x, p[j] * c.y);
-        p[j] = o;
-      }
-      st<N>(y + u * N, p);
+    for (int j = 0; j < 4; ++j) {
+      o[2 * j] = __uint_as_float(w[j] << 16);
+      o[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
   }
+  __device__ __forceinline__ void set(const float* o) {
+    v = make_uint4(pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3]), pack2_bf16(o[4], o[5]), pack2_bf16(o[6], o[7]));
+  }
+};
+template <>
+struct Raw<bf16, 1> {
+  bf16 v;
+  __device__ __forceinline__ void get(float* o) const { o[0] = to_f(v); }
+  __device__ __forceinline__ void set(const float* o) { v = from_f<bf16>(o[0]); }
+};
+
+// Block: `tb` tokens.  Their sines and cosines into LDS, then every (token, head, unit of N elements): a unit of
+// halves is N elements and their partners, one of interleaved pairs N elements (N = 1: a pair), the units
+// behind `dims` are copied.  A thread takes I units at a time, all loaded before the first is used, the first I before the
+// sines are formed.  Memory bounds it.
+template <typename T, int N, int I>
+__global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
+  extern __shared__ float2 cs[];
+  typedef Raw<T, N> R;
+  const int half = a.dims >> 1, t0 = (blockIdx.x + gridDim.x * blockIdx.z) * a.tb, nt = min(a.tb, a.tokens - t0);
+  if (nt <= 0) return;
+  const int tu = N == 1 ? half : a.interleaved ? a.dims / N : half / N, units = tu + (a.copies ? (a.width - a.dims) / N : 0);
+  const int heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0), total = nt * heads * units;
+  // quotients of numbers below 2^22 as products: (i + 1/2) / n is 1 / (2 n) off a whole number at least, more than its two
+  // roundings, 2^-23 of it; larger ones by division
+  const float iu = 1.f / units, ih = 1.f / heads;
+  const bool small = total <= 1 << 22;
+  R p[I], q[I];
+  T* y[I];
+  int at[I], z[I];  // first element, its partner's distance is `apart`; index of its sine, -1: a copy, -2: nothing
+  const int apart = a.interleaved ? (N == 1 ? 1 : 0) : half;
+  auto load = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < I; ++k) {
+      const int i = first + k * 256;
+      z[k] = -2;
+      if (i >= total) continue;
+      const int r = small ? (int)((i + 0.5f) * iu) : i / units, u = i - r * units, t = small ? (int)((r + 0.5f) * ih) : r / heads;
+      int h = r - t * heads;
+      const bool second = h >= a.rows[0].heads;
+      if (second) h -= a.rows[0].heads;
+      const long long xt = second ? a.rows[1].xt : a.rows[0].xt, xh = second ? a.rows[1].xh : a.rows[0].xh;
+      const long long yt = second ? a.rows[1].yt : a.rows[0].yt, yh = second ? a.rows[1].yh : a.rows[0].yh;
+      const T* x = reinterpret_cast<const T*>(second ? a.rows[1].x : a.rows[0].x) + (t0 + t) * xt + h * xh;
+      y[k] = reinterpret_cast<T*>(second ? a.rows[1].y : a.rows[0].y) + (t0 + t) * yt + h * yh;
+      const bool turns = u < tu;
+      at[k] = !turns ? a.dims + (u - tu) * N : a.interleaved && N == 1 ? 2 * u : u * N;
+      z[k] = !turns ? -1 : t * half + (a.interleaved && N > 1 ? u * N / 2 : u * N);
+      p[k] = *reinterpret_cast<const R*>(x + at[k]);
+      if (apart) q[k] = *reinterpret_cast<const R*>(x + (turns ? at[k] + apart : at[k]));
+    }
+  };
+  int first = blockIdx.y * 256 * I + threadIdx.x;
+  load(first);
+  for (int i = threadIdx.x; i < nt * half; i += 256) {
+    const int t = i / half, j = i - t * half;
+    float2 c = turn((double)a.positions[t0 + t] * a.turns[j], a.amplitude);
+    if (a.transposed) c.y = -c.y;
+    cs[i] = c;
+  }
+  __syncthreads();
+  for (;;) {
+#pragma unroll
+    for (int k = 0; k < I; ++k) {
+      if (z[k] == -2) continue;
+      R* o = reinterpret_cast<R*>(y[k] + at[k]);
+      if (z[k] < 0) {
+        *o = p[k];
+        continue;
+      }
+      const float2* c = cs + z[k];
+      float u[N], v[N];
+      p[k].get(u);
+      if (apart) {
+        float s[N], w[N];
+        q[k].get(v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          s[j] = fmaf(u[j], c[j].x, -(v[j] * c[j].y));
+          w[j] = fmaf(v[j], c[j].x, u[j] * c[j].y);
+        }
+        p[k].set(s);
+        q[k].set(w);
+        *o = p[k];
+        *reinterpret_cast<R*>(y[k] + at[k] + apart) = q[k];
+      } else if constexpr (N > 1) {
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          const float2 d = c[j >> 1];
+          const float s = fmaf(u[j], d.x, -(u[j + 1] * d.y));
+          u[j + 1] = fmaf(u[j + 1], d.x, u[j] * d.y);
+          u[j] = s;
+        }
+        p[k].set(u);
+        *o = p[k];
+      }
+    }
+    first += gridDim.y * 256 * I;
+    if (first - (int)threadIdx.x >= total) break;
+    load(first);
+  }
 }
 
+template <typename T, int N>
+static void rotary_launch(RotaryArgs& a, hipStream_t st) {
+  const int half = a.dims / 2, heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0);
+  const int units = N == 1 ? half + (a.copies ? a.width - a.dims : 0)
+                           : (a.interleaved ? a.dims / N : half / N) + (a.copies ? (a.width - a.dims) / N : 0);
+  // Tokens of a block: units for every thread, more where there are blocks enough to fill the chip with them; sines
+  // within LDS; at most 2^24 units
+  const long long each = (long long)heads * units, all = each * a.tokens;
+  const long long want = all > 256ll * 256 * 16 ? 2048 : 256;
+  a.tb = (int)std::max<long long>(1, std::min<long long>({(want + each - 1) / each, 2048 / half, (1 << 24) / each, 64}));
+  const int blocks = (a.tokens + a.tb - 1) / a.tb, bx = std::min(blocks, 1 << 20);  // a grid's x holds 2^32 threads
+  const unsigned by = (unsigned)std::min<long long>(1024, (a.tb * each + 2047) / 2048);
+  const dim3 grid(bx, by, (blocks + bx - 1) / bx);
+  const size_t lds = (size_t)a.tb * half * sizeof(float2);
+  if (want > 256) k_rotary<T, N, 4><<<grid, 256, lds, st>>>(a);
+  else k_rotary<T, N, 1><<<grid, 256, lds, st>>>(a);
+}
 void rotary(const RotaryArgs& a0, hipStream_t st) {
   RotaryArgs a = a0;
-  const int half = a.dims / 2, heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0);
   const int nv = a.bf16_data ? 8 : 4;
   const bool vec = a.vec && a.dims % (a.interleaved ? nv : 2 * nv) == 0 && (a.width - a.dims) % nv == 0;
-  const int n = vec ? nv : 1;
-  a.tb = (int)std::max<long long>(1, std::min<long long>(std::min(16, 1024 / half), (1 << 24) / ((long long)heads * a.width)));
-  const long long items = (long long)a.tb * heads * (a.width / n);
-  const int blocks = (a.tokens + a.tb - 1) / a.tb, bx = std::min(blocks, 1 << 20);  // a grid's x holds 2^32 threads
-  const dim3 grid(bx, (unsigned)std::min<long long>(16, std::max<long long>(1, items / 2048)), (blocks + bx - 1) / bx);
-  const size_t lds = (size_t)a.tb * half * sizeof(float2);
   if (a.bf16_data) {
-    if (vec) k_rotary<bf16, 8><<<grid, 256, lds, st>>>(a);
-    else k_rotary<bf16, 1><<<grid, 256, lds, st>>>(a);
+    if (vec) rotary_launch<bf16, 8>(a, st);
+    else rotary_launch<bf16, 1>(a, st);
   } else {
-    if (vec) k_rotary<float, 4><<<grid, 256, lds, st>>>(a);
-    else k_rotary<float, 1><<<grid, 256, lds, st>>>(a);
+    if (vec) rotary_launch<float, 4>(a, st);
+    else rotary_launch<float, 1>(a, st);
   }
 }
 

@@ -270,11 +270,12 @@ __device__ __forceinline__ float swap_sum(float v) {
   const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
-// Eight values as N bf16 terms (three hold an fp32 value exactly, one a bf16 value).
+// Eight values as N bf16 terms: three hold an fp32 value exactly, two to 2^-17, one a bf16 value.
 template <int N>
 __device__ __forceinline__ void split_terms(const float* v, bf16x8 (&t)[N]) {
   uint4 u[3];
   if constexpr (N == 3) split3x8(v, u[0], u[1], u[2]);
+  else if constexpr (N == 2) split2x8(v, u[0], u[1]);
   else u[0] = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
 #pragma unroll
   for (int i = 0; i < N; ++i) t[i] = __builtin_bit_cast(bf16x8, u[i]);
@@ -296,6 +297,9 @@ __device__ __forceinline__ void cut(uint32_t& lo, uint32_t& hi, int left) {
   hi &= left >= 8 ? ~0u : left <= 4 ? 0u : (1u << 8 * (left - 4)) - 1;
 }
 
+// a / b of numbers below 2^21: (a + 1/2) / b is 1 / (2 b) off a whole number at least, more than its roundings (a division
+// of integers is forty instructions)
+__device__ __forceinline__ int quotient(int a, int b) { return (int)((a + 0.5f) * __builtin_amdgcn_rcpf((float)b)); }
 // Codes and scales of two pages; there: bit t set where page t's number is good.
 struct Step {
   uint4 k[2], v[2];
@@ -346,9 +350,14 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-  const float m = fmaxf(st.m, swap_max(mx)), base = no_inf(m);
-  const float f = exp_to(st.m, base);  // 0 at first
-  st.m = m;
+  if (__builtin_amdgcn_ballot_w64(mx > st.m)) {  // some column's maximum moves (seldom, once a few hundred positions are seen)
+    const float m = fmaxf(st.m, swap_max(mx)), f = exp_to(st.m, no_inf(m));  // 0 at first
+    st.m = m;
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) st.o[dt] *= f;
+  }
+  const float base = no_inf(st.m);
   float l = 0.f;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
@@ -357,9 +366,7 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
       s[t][i] = exp_to(s[t][i], base);
       l += s[t][i];
     }
-  st.l = fmaf(st.l, f, l);
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt) st.o[dt] *= f;
+  st.l += l;
   auto operand = [&](const floatx4 (&x)[2], float* pb) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -414,32 +421,46 @@ __device__ __forceinline__ void kv8_rows(const Kv8AttendArgs& a, int r, int& pos
 
 template <typename T, int NW>
 __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
-  constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
+  // terms of a query value (exact) and of a probability: three of an fp32 call, of a bf16 one two, whose 2^-17 a result's
+  // own rounding, 2^-9, covers
+  constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
   __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
-  const int head = blockIdx.x % a.c.n_head, chunk = blockIdx.x / a.c.n_head, r = blockIdx.y, c0 = blockIdx.z * 16;
+  const int chunk = quotient(blockIdx.x, a.c.n_head), head = blockIdx.x - chunk * a.c.n_head, r = blockIdx.y, c0 = blockIdx.z * 16;
   const int cols = a.rows * a.group, cap = 16 * a.max_pages;
+  const int* table = a.tables + r * a.ts;
+  // Before the request's position is known: the query, and the page numbers of the wave's first 32 steps (two a step) where
+  // the positions are not split.
+  const int col = c0 + n, i = quotient(col, a.group);
+  int ahead = table[min(2 * (w + (lane >> 1) * NW) + (lane & 1), a.max_pages - 1)];
+  const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(i, a.rows - 1) * a.si + (head * a.group + col - i * a.group) * a.sh + 16 * kg;
+  float x[16];
+  if (a.vec) {
+    ld8(q, x);
+    ld8(q + 8, x + 8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = to_f(q[j]);
+  }
   int pos, count;
   kv8_rows(a, r, pos, count);
   // columns of rows from `count` on, and of rows that see nothing, run along unmasked and are written as zeros
-  const int i0 = c0 / a.group, i1 = min(min(cols, c0 + 16) - 1, count * a.group - 1) / a.group;  // rows of this tile
-  const int col = c0 + n, i = col / a.group;
+  const int i0 = quotient(c0, a.group), i1 = min(quotient(min(cols, c0 + 16) - 1, a.group), count - 1);  // rows of this tile
   const bool live = col < cols && i < count && pos + i >= 0;
-  const int top = c0 < count * a.group ? min(max(pos + i1 + 1, 0), cap) : 0;
+  const int top = i0 < count ? min(max(pos + i1 + 1, 0), cap) : 0;
   const int low = min(max(pos + i0, 0) + 1, top), lim = live ? min(pos + i + 1, cap) : cap;
-  const int groups = (top + 31) / 32, each = (groups + a.nchunk - 1) / a.nchunk;
-  const int end = min((chunk + 1) * each, groups);
-  const int* table = a.tables + r * a.ts;
+  const int groups = (top + 31) / 32, each = a.nchunk == 1 ? groups : (int)((groups + a.nchunk - 1u) / (unsigned)a.nchunk);
+  const int end = min((chunk + 1) * each, groups), g0 = chunk * each + w;
   State st;
   st.m = -INFINITY;
   st.l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) st.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int g0 = chunk * each + w, pages = (top + 15) / 16;
-  int ahead = 0;  // the page numbers of 32 of the wave's steps, two a step
-  auto numbers = [&](int i) { ahead = table[min(2 * (g0 + (i + (lane >> 1)) * NW) + (lane & 1), pages - 1)]; };
-  auto load = [&](int i, Step& s) {  // the wave's step i, or its last
-    if ((i & 31) == 0) numbers(i);
+  const int steps = g0 < end ? (end - g0 + NW - 1) / NW : 0;
+  auto load = [&](int i, Step& s) {  // the wave's step i, or its last again
+    if ((i & 31) == 0 && i < steps && (i > 0 || a.nchunk > 1))
+      ahead = table[min(2 * (g0 + (i + (lane >> 1)) * NW) + (lane & 1), a.max_pages - 1)];
+    i = min(i, steps - 1);
     int p[2];
     s.there = 0;
 #pragma unroll
@@ -460,25 +481,14 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
     s.v[0] = *reinterpret_cast<const uint4*>(in);
     s.v[1] = *reinterpret_cast<const uint4*>(in + 16);
   };
-  if (g0 < end) {
+  if (steps > 0) {
     Step A, B;
     load(0, A);
-    const T* q = reinterpret_cast<const T*>(a.q) + r * a.sr + (long long)min(i, a.rows - 1) * a.si +
-                 (head * a.group + col % a.group) * a.sh + 16 * kg;
-    float x[16];
-    if (a.vec) {
-      ld8(q, x);
-      ld8(q + 8, x + 8);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) x[j] = to_f(q[j]);
-    }
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = live ? 0.125f * x[j] : 0.f;
     bf16x8 qt[2][QT];
     split_terms<QT>(x, qt[0]);
     split_terms<QT>(x + 8, qt[1]);
-    const int steps = (end - g0 + NW - 1) / NW;
     for (int i = 0;;) {
       load(i + 1, B);
       kv8_step<QT, PT>(A, 32 * (g0 + i * NW), lim, low, top, qt, st);
@@ -500,7 +510,7 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
   __syncthreads();
   const int nc = min(16, cols - c0);
   for (int t = threadIdx.x; t < nc * 64; t += NW * 64) {
-    const int c = t >> 6, d = t & 63, ci = (c0 + c) / a.group;
+    const int c = t >> 6, d = t & 63, ci = quotient(c0 + c, a.group);
     float M = wm[0][c], L = 0.f, O = 0.f;
 #pragma unroll
     for (int j = 1; j < NW; ++j) M = fmaxf(M, wm[j][c]);
@@ -513,7 +523,7 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
     }
     if (a.nchunk == 1) {
       const bool some = ci < count && pos + ci >= 0 && L != 0.f;
-      reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + (c0 + c) % a.group) * kHeadDim + d] =
+      reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + c0 + c - ci * a.group) * kHeadDim + d] =
           from_f<T>(some ? O / L : 0.f);
     } else {
       float* rec = a.part + ((((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk + chunk) * kRecord;
@@ -569,9 +579,11 @@ __global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
   }
 }
 
-// Waves of a block, and chunks of the positions: towards four blocks of eight waves a compute unit, each of two steps of every
-// wave at least.
-static int kv8_waves(int max_pages) { return max_pages <= 32 ? 4 : 8; }
+// Waves of a block: four where the positions are few and the blocks many, whose start and end then weigh more than a wave's
+// steps.  us a replayed call, four waves / eight (20 heads, bf16): 96 requests of one row at position 438 24.0 / 26.0, of nine
+// rows at 0 to 438 20.9 / 23.0, 256 of one at 0 to 447 33 / 43; one request at 447 6.8 / 6.1; 64 at 4,000 128 / 114.
+static int kv8_waves(long long blocks, int max_pages) { return max_pages <= 64 && blocks > 256 ? 4 : 8; }
+// Chunks of the positions: towards four blocks a compute unit, each of two steps of every wave at least.
 static int kv8_chunks(int n, int rows, int group, int n_head, int max_pages) {
   const long long blocks = (long long)n * n_head * ((rows * group + 15) / 16), groups = (max_pages + 1) / 2;
   return (int)std::max<long long>(1, std::min<long long>(1024 / blocks, groups / 16));
@@ -585,7 +597,7 @@ template <typename T>
 static void attend_launch(const Kv8AttendArgs& a, hipStream_t st) {
   const int cols = a.rows * a.group;
   const dim3 grid(a.c.n_head * a.nchunk, a.n, (cols + 15) / 16);
-  if (kv8_waves(a.max_pages) == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
+  if (kv8_waves((long long)grid.x * grid.y * grid.z, a.max_pages) == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
   else k_kv8_attend<T, 8><<<grid, 512, 0, st>>>(a);
   if (a.nchunk > 1) k_kv8_merge<T><<<dim3(a.c.n_head, a.n, cols), 256, 0, st>>>(a);
 }

@@ -41,12 +41,6 @@ __device__ __forceinline__ uint32_t mag_finite(float x) { return mag(x) >= 0x7f8
 // 2^(127 - byte) of a scale byte in [27, 247]
 __device__ __forceinline__ float inverse_f(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
-__device__ __forceinline__ void values16(uint4 c, float s, float* x) {
-  values8x4(c.x, s, x);
-  values8x4(c.y, s, x + 4);
-  values8x4(c.z, s, x + 8);
-  values8x4(c.w, s, x + 12);
-}
 // The whole wave's maxima of two non-negative numbers, as floats' bits.
 template <int CTRL>
 __device__ __forceinline__ uint32_t umax_dpp(uint32_t v) {
@@ -62,36 +56,43 @@ __device__ __forceinline__ void wave_umax(uint32_t& a, uint32_t& b) {
   a = umax(umax(lane(a, 0), lane(a, 16)), umax(lane(a, 32), lane(a, 48)));
   b = umax(umax(lane(b, 0), lane(b, 16)), umax(lane(b, 32), lane(b, 48)));
 }
-// Two consecutive elements.
-__device__ __forceinline__ void ld_two(const float* p, int vec, float* o) {
+// Four consecutive elements.
+__device__ __forceinline__ void ld4(const float* p, int vec, float* o) {
   if (vec) {
-    const float2 v = *reinterpret_cast<const float2*>(p);
-    o[0] = v.x;
-    o[1] = v.y;
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
   } else {
-    o[0] = p[0];
-    o[1] = p[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = p[j];
   }
 }
-__device__ __forceinline__ void ld_two(const bf16* p, int vec, float* o) {
+__device__ __forceinline__ void ld4(const bf16* p, int vec, float* o) {
   if (vec) {
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
-    o[0] = __uint_as_float(v << 16);
-    o[1] = __uint_as_float(v & 0xffff0000u);
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    o[0] = __uint_as_float(v.x << 16);
+    o[1] = __uint_as_float(v.x & 0xffff0000u);
+    o[2] = __uint_as_float(v.y << 16);
+    o[3] = __uint_as_float(v.y & 0xffff0000u);
   } else {
-    o[0] = to_f(p[0]);
-    o[1] = to_f(p[1]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = to_f(p[j]);
   }
+}
+// In the store and the load, lane 16 kg + n has dims 4 n .. + 3 of positions 4 kg .. + 3, so that a wave reads and writes
+// whole rows.  The code words: of its keys, dims 4 n .. of position 4 kg + j; of its values, those positions of dim 4 n + j.
+__device__ __forceinline__ int key_code(int lane, int j) { return 256 * ((lane & 15) >> 2) + 16 * (4 * (lane >> 4) + j) + 4 * (lane & 3); }
+__device__ __forceinline__ int value_code(int lane, int j) {
+  return kKv8Values + 32 * (16 * (lane >> 5) + (lane & 15)) + 8 * j + 4 * ((lane >> 4) & 1);
 }
 
 // ---------------------------------------------------------------- store
-// A wave per (page that a request writes, head).  Lane l = 16 kg + n holds dims 16 kg .. + 15 of
-// position n's key; lane l = 32 h + 16 g + n of the values dims 4 n + 2 h, + 1 of positions 8 g .. + 7.
-// Where a request's pages lie in the grid: request r's first page has number starts[r] / 16 + 2 r
-// (packed), which leaves room for every page that its rows can touch, or r * per (padded).
+// A wave per (page that a request writes, head).  Where a request's pages lie in the grid: request r's first page has
+// number starts[r] / 16 + 2 r (packed), which leaves room for every page that its rows can touch, or r * per (padded).
 template <typename T>
-__global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
-  const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6);
+__global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per, int hb) {
+  // neighbouring blocks take neighbouring heads of one page, whose rows lie beside each other; by grid y where there are too many
+  const int unit = gridDim.y > 1 ? blockIdx.x : blockIdx.x / (unsigned)hb, hq = gridDim.y > 1 ? blockIdx.y : blockIdx.x - unit * hb;
+  const int lane = threadIdx.x & 63, head = __builtin_amdgcn_readfirstlane(hq * 4 + (threadIdx.x >> 6));
   if (head >= a.c.n_head) return;
   int r, col, first, count;
   if (a.starts) {
@@ -99,16 +100,16 @@ __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
     auto at = [&](int i) { return min(max(a.starts[i], 0), a.rows); };
     while (hi - lo > 1) {
       const int m = (lo + hi) >> 1;
-      if (at(m) / 16 + 2 * m <= (int)blockIdx.x) lo = m;
+      if (at(m) / 16 + 2 * m <= unit) lo = m;
       else hi = m;
     }
     r = lo;
     first = at(r);
     count = at(r + 1) - first;
-    col = (int)blockIdx.x - (first / 16 + 2 * r);
+    col = unit - (first / 16 + 2 * r);
   } else {
-    r = blockIdx.x / per;
-    col = blockIdx.x - r * per;
+    r = unit / (unsigned)per;
+    col = unit - r * per;
     first = 0;
     count = a.counts ? min(max(a.counts[r], 0), a.rows) : a.rows;
   }
@@ -116,76 +117,84 @@ __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per) {
   const long long page0 = (begin >> 4) + col;                    // this wave's page of the request
   if (col < 0 || count <= 0 || page0 >= a.max_pages || page0 * 16 >= pos + count) return;
   const int page = a.tables[r * a.ts + page0];
-  if (page < 0 || page >= a.c.n_pages) return;
-  uint8_t* out = a.c.base + page * a.c.page + (size_t)head * kKv8Head;
-  uint8_t* sc = a.c.base + page * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head;
   const long long skip = page0 * 16 - pos;  // row of position 0 of the page (negative: kept positions before the rows)
   const int kept = (int)max(-skip, 0ll);    // positions [0, kept) stay, [kept, end) are rows
   const int end = (int)min(count - skip, 16ll);
-  const T* K = reinterpret_cast<const T*>(a.k) + (a.starts ? 0 : r * a.kr) + head * a.kh;
-  const T* V = reinterpret_cast<const T*>(a.v) + (a.starts ? 0 : r * a.vr) + head * a.vh;
   // Every load is issued before the first use and without a condition (positions that are no row's take the nearest
   // row and are replaced): a load under one would make each wait for the one before.
-  const int n = lane & 15, kg = lane >> 4, h = lane >> 5, g = (lane >> 4) & 1;
-  auto row = [&](int f) { return first + (long long)min(max(skip + f, 0ll), (long long)count - 1); };
-  uint8_t* vout = out + kKv8Values + 32 * (16 * g + n) + 16 * h;
-  float x[16], y[8][2];  // y[j]: dims 4 n + 2 h, + 1 of position 8 g + j
-  {
-    const T* p = K + row(n) * a.ki + 16 * kg;
-    if (a.vec) {
-      ld8(p, x);
-      ld8(p + 8, x + 8);
-    } else {
+  const int n = lane & 15, kg = lane >> 4;
+  const T* K = reinterpret_cast<const T*>(a.k) + (a.starts ? 0 : r * a.kr) + head * a.kh + 4 * n;
+  const T* V = reinterpret_cast<const T*>(a.v) + (a.starts ? 0 : r * a.vr) + head * a.vh + 4 * n;
+  float x[4][4], y[4][4];  // [position 4 kg + j][dim 4 n + ..]
+  if (kept == 0 && end == 16) {  // a page of rows alone
+    const T *k = K + (first + skip) * a.ki + 4 * kg * a.ki, *v = V + (first + skip) * a.vi + 4 * kg * a.vi;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) x[j] = to_f(p[j]);
+    for (int j = 0; j < 4; ++j) {
+      ld4(k + j * a.ki, a.vec, x[j]);
+      ld4(v + j * a.vi, a.vec, y[j]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long row = first + min(max(skip + 4 * kg + j, 0ll), (long long)count - 1);
+      ld4(K + row * a.ki, a.vec, x[j]);
+      ld4(V + row * a.vi, a.vec, y[j]);
     }
   }
+  if (page < 0 || page >= a.c.n_pages) return;
+  uint8_t* out = a.c.base + page * a.c.page + (size_t)head * kKv8Head;
+  uint8_t* sc = a.c.base + page * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) ld_two(V + row(8 * g + j) * a.vi + 4 * n + 2 * h, a.vec, y[j]);
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-  for (int j = 0; j < 16; ++j) x[j] = n < end ? x[j] : 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-#pragma unroll
-    for (int d = 0; d < 2; ++d) y[j][d] = 8 * g + j < end ? y[j][d] : 0.f;
+    for (int d = 0; d < 4; ++d) {
+      x[j][d] = 4 * kg + j < end ? x[j][d] : 0.f;
+      y[j][d] = 4 * kg + j < end ? y[j][d] : 0.f;
+    }
   if (kept) {  // uniform
     const uint32_t old = *reinterpret_cast<const uint16_t*>(sc);
-    const uint4 c = *reinterpret_cast<const uint4*>(out + 16 * lane), d = *reinterpret_cast<const uint4*>(vout);
-    float z[16];
-    values16(c, scale_f(old & 255), z);
+    uint32_t kc[4], vc[4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = n < kept ? z[j] : x[j];
-    values16(d, scale_f(old >> 8), z);
+    for (int j = 0; j < 4; ++j) {
+      kc[j] = *reinterpret_cast<const uint32_t*>(out + key_code(lane, j));
+      vc[j] = *reinterpret_cast<const uint32_t*>(out + value_code(lane, j));
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      y[j][0] = 8 * g + j < kept ? z[j] : y[j][0];
-      y[j][1] = 8 * g + j < kept ? z[8 + j] : y[j][1];
+    for (int j = 0; j < 4; ++j) {
+      float p[4], q[4];
+      values8x4(kc[j], scale_f(old & 255), p);
+      values8x4(vc[j], scale_f(old >> 8), q);
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        x[j][d] = 4 * kg + j < kept ? p[d] : x[j][d];
+        y[d][j] = 4 * kg + d < kept ? q[d] : y[d][j];
+      }
     }
   }
   uint32_t m = 0, m2 = 0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
-    m = umax(m, mag_finite(x[j]));
-    m2 = umax(m2, mag_finite(y[j >> 1][j & 1]));
+    m = umax(m, mag_finite(x[j >> 2][j & 3]));
+    m2 = umax(m2, mag_finite(y[j >> 2][j & 3]));
   }
   wave_umax(m, m2);
   const uint32_t ks = scale8_of(__uint_as_float(m)), vs = scale8_of(__uint_as_float(m2));
-  const float ki = inverse_f(ks), vi = inverse_f(vs);
-  const uint4 kc = make_uint4(codes8x4(x, ki), codes8x4(x + 4, ki), codes8x4(x + 8, ki), codes8x4(x + 12, ki));
-  float u[2][8];
 #pragma unroll
-  for (int j = 0; j < 16; ++j) u[j & 1][j >> 1] = y[j >> 1][j & 1];
-  *reinterpret_cast<uint4*>(out + 16 * lane) = kc;
-  *reinterpret_cast<uint4*>(vout) = make_uint4(codes8x4(u[0], vi), codes8x4(u[0] + 4, vi), codes8x4(u[1], vi), codes8x4(u[1] + 4, vi));
+  for (int j = 0; j < 4; ++j) {
+    const float q[4] = {y[0][j], y[1][j], y[2][j], y[3][j]};
+    *reinterpret_cast<uint32_t*>(out + key_code(lane, j)) = codes8x4(x[j], inverse_f(ks));
+    *reinterpret_cast<uint32_t*>(out + value_code(lane, j)) = codes8x4(q, inverse_f(vs));
+  }
   if (lane == 0) *reinterpret_cast<uint16_t*>(sc) = (uint16_t)(ks | vs << 8);
 }
 
 void kv8_store(const Kv8StoreArgs& a, hipStream_t st) {
   const int per = (a.rows + 30) / 16;  // pages that a request's rows can touch
   const long long units = a.starts ? a.rows / 16 + 2ll * a.n + 1 : (long long)per * a.n;
-  const dim3 grid((unsigned)units, (a.c.n_head + 3) / 4);
-  if (a.bf16_src) k_kv8_store<bf16><<<grid, 256, 0, st>>>(a, per);
-  else k_kv8_store<float><<<grid, 256, 0, st>>>(a, per);
+  const int hb = (a.c.n_head + 3) / 4;
+  const dim3 grid = units * hb < 1 << 24 ? dim3((unsigned)(units * hb)) : dim3((unsigned)units, hb);
+  if (a.bf16_src) k_kv8_store<bf16><<<grid, 256, 0, st>>>(a, per, hb);
+  else k_kv8_store<float><<<grid, 256, 0, st>>>(a, per, hb);
 }
 
 // ---------------------------------------------------------------- load
@@ -193,8 +202,7 @@ __device__ __forceinline__ void st4(float* p, const float* x) { *reinterpret_cas
 __device__ __forceinline__ void st4(bf16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
 }
-// A wave per (request, column of its table, head): lane l = 16 kg + n holds dims 4 n .. + 3 of positions 4 kg .. + 3, so that
-// a wave writes whole rows.
+// A wave per (request, column of its table, head).
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
   const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
@@ -213,8 +221,8 @@ __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
     uint32_t c[4], v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      c[j] = *reinterpret_cast<const uint32_t*>(in + 16 * (16 * (n >> 2) + 4 * kg + j) + 4 * (n & 3));
-      v[j] = *reinterpret_cast<const uint32_t*>(in + kKv8Values + 32 * (16 * (kg >> 1) + n) + 8 * j + 4 * (kg & 1));
+      c[j] = *reinterpret_cast<const uint32_t*>(in + key_code(lane, j));
+      v[j] = *reinterpret_cast<const uint32_t*>(in + value_code(lane, j));
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -166,43 +166,35 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
   float q[4][8];
 #pragma unroll
   for (int s = 0; s < 4; ++s) ld<8>(Q + 16 * s, a.vec, q[s]);
-  int* window = reinterpret_cast<int*>(wo);
-  const Borders near = borders_near(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm), [] {});
-  const int lo = first_key(a.starts, a.n, window, near, row), hi = lo > row ? lo : row + 1;  // keys [lo, hi)
-  // the keys that any of the rows sees, and those that all see
-  int k0 = hi > lo ? lo : a.tokens, k1 = hi > lo ? hi : 0, f0 = lo, f1 = hi;
-#pragma unroll
-  for (int m = 1; m < 32; m <<= 1) {
-    k0 = min(k0, __shfl_xor(k0, m));
-    k1 = max(k1, __shfl_xor(k1, m));
-    f0 = max(f0, __shfl_xor(f0, m));
-    f1 = min(f1, __shfl_xor(f1, m));
-  }
-  k0 = __builtin_amdgcn_readfirstlane(k0);
-  k1 = __builtin_amdgcn_readfirstlane(k1);
-  f0 = __builtin_amdgcn_readfirstlane(f0);
-  f1 = __builtin_amdgcn_readfirstlane(f1);
   const T* K = reinterpret_cast<const T*>(a.k) + (head / a.group) * a.kh + 8 * lk;
   const T* V = reinterpret_cast<const T*>(a.v) + (head / a.group) * a.vh + lr;
+  const int last = a.tokens - 1;
   float kx[4][8], vx[2][2][8];  // a tile: keys' dims 16 s + 8 lk .. + 7 of key lr; values [dim half][sixteen keys]
   auto load_keys = [&](int kt) {
-    const T* p = K + min(kt + lr, a.tokens - 1) * a.kt;
+    const T* p = K + min(max(kt + lr, 0), last) * a.kt;
 #pragma unroll
     for (int s = 0; s < 4; ++s) ld<8>(p + 16 * s, a.vec, kx[s]);
   };
   auto load_values = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const T* p = V + min(kt + 8 * (i >> 2) + 4 * lk + (i & 3), a.tokens - 1) * a.vt;
+      const T* p = V + min(max(kt + 8 * (i >> 2) + 4 * lk + (i & 3), 0), last) * a.vt;
       vx[0][i >> 3][i & 7] = to_f(p[0]);
       vx[1][i >> 3][i & 7] = to_f(p[32]);
     }
   };
-  int kt = k0 + 32 * w;
-  if (kt < k1) {
+  // Tile t: keys e - 32 (t + 1) .. e - 32 t - 1, from the block's own rows back to its first sequence's first row, so that
+  // the waves' first tiles are under way before the borders are known.
+  const int e = min(q0 + 32, a.tokens);
+  int kt = e - 32 * (w + 1);
+  int* window = reinterpret_cast<int*>(wo);
+  const Borders near = borders_near(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm), [&] {
     load_keys(kt);
     load_values(kt);
-  }
+  });
+  const int lo = first_key(a.starts, a.n, window, near, row);  // the row sees keys [lo, row]
+  // first keys do not decrease along the rows
+  const int k0 = __builtin_amdgcn_readlane(lo, 0), f0 = __builtin_amdgcn_readlane(lo, 31);
   bf16x8 qt[4][N];
 #pragma unroll
   for (int s = 0; s < 4; ++s) terms8<N>(q[s], qt[s]);
@@ -212,7 +204,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
   for (int d = 0; d < 2; ++d)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
-  for (; kt < k1; kt += 128) {
+  for (; kt + 32 > k0; kt -= 128) {
     floatx16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.f;
@@ -222,14 +214,14 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
       terms8<N>(kx[i], t);
       s = product<N>(t, qt[i], s);
     }
-    if (kt + 128 < k1) load_keys(kt + 128);
-    const bool masked = kt < f0 || kt + 32 > f1;  // uniform: some row does not see some key
+    if (kt - 96 > k0) load_keys(kt - 128);
+    const bool masked = kt < f0 || kt + 31 > q0;  // uniform: some row does not see some key
     uint32_t out = 0;                             // bit v: the row does not see the key
     if (masked) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = kt + 8 * (v >> 2) + 4 * lk + (v & 3);
-        const bool hidden = key < lo || key >= hi;
+        const bool hidden = key < lo || key > row;
         s[v] = hidden ? -INFINITY : s[v];
         out |= hidden ? 1u << v : 0u;
       }
@@ -294,7 +286,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
         o[d] = product<N>(t, pt, o[d]);
       }
     }
-    if (kt + 128 < k1) load_values(kt + 128);
+    if (kt - 96 > k0) load_values(kt - 128);
   }
   l = pair_sum(l);
   __syncthreads();  // the window lies where the outputs go

@@ -644,14 +644,181 @@ static void prompt16(const PromptArgs& a, hipStream_t st) {
   k_prompt16<NQ, KB, WAVES><<<8 * per, 256, 0, st>>>(a, tiles, per);
 }
 
+
+// ---------------------------------------------------------------- fp32, many rows
+// Block: (128 rows, head), four waves of 32 rows.  Tiles of 32 keys: 256 threads load 8 dims of a key and of a value row each,
+// split them into three bf16 terms once for the whole block and write them to one of two LDS stages while the other is
+// multiplied; the next tile's loads are under way meanwhile.  A stage holds six planes of 32 rows of 64 dims (keys' terms,
+// values' terms) in k_prompt16's order.  Products as in k_prompt32 (six a pair of operands, a plane at a time, the
+// smallest first), softmax as in k_prompt16.
+constexpr int kPlane = 4096, kStage3 = 6 * kPlane;
+__global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int per) {
+  __shared__ uint4 stages[2 * kStage3 / 16];
+  __shared__ int window[kWindow], odd[4];  // odd: the last tile of a stage that held a NaN or an infinity
+  const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);  // as in k_prompt16
+  if (at >= tiles * a.heads) return;
+  const int head = at / tiles, q0 = (tiles - 1 - at % tiles) * 128;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
+  const int e = min(q0 + 128, a.tokens), r0 = q0 + w * 32, row = min(r0 + lr, a.tokens - 1);
+  const float* Q = reinterpret_cast<const float*>(a.q) + row * a.qt + head * a.qh + 8 * lk;
+  const float* V = reinterpret_cast<const float*>(a.v) + (head / a.group) * a.vh;
+  const int cr = threadIdx.x >> 3, cc = threadIdx.x & 7;  // the thread's row of a tile and its eight dims
+  const float *Kc = reinterpret_cast<const float*>(a.k) + (head / a.group) * a.kh + 8 * cc, *Vc = V + 8 * cc;
+  float q[4][8], kx[8], vx[8];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) ld<8>(Q + 16 * s, a.vec, q[s]);
+  auto load = [&](int t) {
+    const int r = min(max(e - (t + 1) * 32 + cr, 0), a.tokens - 1);
+    ld<8>(Kc + r * a.kt, a.vec, kx);
+    ld<8>(Vc + r * a.vt, a.vec, vx);
+  };
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)stages, put = 128 * cr + 16 * (cc ^ (cr & 7));
+  auto stage = [&](int t) {  // tile t's terms from the registers
+    // What is not finite among the values leaves the tile and is added for the rows that see it: its product with a
+    // probability of 0 would reach those that do not (and an infinity in terms is NaN).
+    float z = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z = fmaf(vx[j], 0.f, z);
+    if (__builtin_amdgcn_ballot_w64(z != 0.f)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vx[j] = finite(vx[j]) ? vx[j] : 0.f;
+      if (lane == 0) odd[t & 1] = t;
+    }
+    char* to = reinterpret_cast<char*>(stages) + (t & 1) * kStage3 + put;
+    bf16x8 k3[3], v3[3];
+    terms8<3>(kx, k3);
+    terms8<3>(vx, v3);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      *reinterpret_cast<bf16x8*>(to + i * kPlane) = k3[i];
+      *reinterpret_cast<bf16x8*>(to + (3 + i) * kPlane) = v3[i];
+    }
+  };
+  const Borders near = borders_near(a.starts, a.n, q0, window, odd, [&] { load(0); });
+  // first keys do not decrease along the rows: of the wave's rows, and of the block's first
+  const int lo = first_key(a.starts, a.n, window, near, row), bound = first_key(a.starts, a.n, window, near, q0);
+  const int k0 = __builtin_amdgcn_readfirstlane(bound), w0 = __builtin_amdgcn_readlane(lo, 0), f0 = __builtin_amdgcn_readlane(lo, 31);
+  const int nt = (e - min(k0, e) + 31) / 32;
+  bf16x8 qt[4][3];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) terms8<3>(q[s], qt[s]);
+  constexpr float kRaise = 8.f / kScale;  // as in k_prompt16
+  float raise = -INFINITY, l = 0.f;
+  floatx16 nref, o[2];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) nref[v] = o[0][v] = o[1][v] = 0.f;
+  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
+  const uint32_t kat = lds + 128 * lr + 16 * (lk ^ (lr & 7)), vat = lds + 3 * kPlane + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
+  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  __syncthreads();
+  if (nt > 0) stage(0);
+  __syncthreads();
+  for (int t = 0; t < nt; ++t) {
+    if (t + 1 < nt) load(t + 1);
+    const int kt = e - (t + 1) * 32;
+    if (kt < r0 + 32 && kt + 32 > w0) {  // uniform
+      const uint32_t half = (t & 1) * kStage3;
+      floatx16 sc = nref;
+#pragma unroll
+      for (int i = 2; i >= 0; --i) {
+        bf16x8 kf[4];
+        read_keys(kat + half + i * kPlane, kf);
+#pragma unroll
+        for (int j = 2 - i; j >= 0; --j)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) sc = mfma32(kf[s], qt[s][j], sc);
+      }
+      if (kt + 31 > r0) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[v] = 8 * (v >> 2) + (v & 3) <= row - kt - 4 * lk ? sc[v] : -INFINITY;
+      }
+      if (kt < f0) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[v] = 8 * (v >> 2) + (v & 3) >= lo - kt - 4 * lk ? sc[v] : -INFINITY;
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[v]);
+      mx = pair_max(mx);
+      if (__builtin_amdgcn_ballot_w64(mx > raise)) {
+        const float d = mx > raise ? mx : 0.f;
+        const float f = raise > 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;
+        if (mx > raise) raise = kRaise;
+        l *= f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          o[0][v] *= f;
+          o[1][v] *= f;
+          sc[v] -= d;
+          nref[v] -= d;
+        }
+      }
+      bf16x8 pt[2][3];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float p[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          p[v] = __builtin_amdgcn_exp2f(sc[8 * i + v] * kScale);
+          l += p[v];
+        }
+        terms8<3>(p, pt[i]);
+      }
+#pragma unroll
+      for (int i = 2; i >= 0; --i) {
+        bf16x8 vf[2][2];
+        read_values(vat + half + i * kPlane, vf);
+#pragma unroll
+        for (int j = 2 - i; j >= 0; --j)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < 2; ++d) o[d] = mfma32(vf[s][d], pt[s][j], o[d]);
+      }
+      if (__builtin_amdgcn_readfirstlane(odd[t & 1]) == t) {
+#pragma unroll 1
+        for (int key = max(kt, 0); key < min(kt + 32, a.tokens); ++key) {
+          const float* vp = V + key * a.vt + 4 * lk;
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            float x[4];
+            ld<4>(vp + 8 * g, a.vec, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[g >> 2][4 * (g & 3) + i] += !finite(x[i]) && key >= lo && key <= row ? x[i] : 0.f;
+          }
+        }
+      }
+    }
+    if (t + 1 < nt) stage(t + 1);
+    __syncthreads();
+  }
+  const float total = pair_sum(l), inv = total == 0.f ? 0.f : 1.f / total;
+  if (r0 + lr >= a.tokens || (!a.clear && (row < near.begin || row >= near.end))) return;
+  float* op = reinterpret_cast<float*>(a.out) + ((size_t)row * a.heads + head) * kHeadDim + 4 * lk;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<floatx4*>(op + d * 32 + 8 * g) =
+          floatx4{o[d][4 * g] * inv, o[d][4 * g + 1] * inv, o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv};
+}
+
 template <typename T>
 static void prompt32(const PromptArgs& a, hipStream_t st) {
   const int tiles = (a.tokens + 31) / 32, per = (int)(((long long)tiles * a.heads + 7) / 8);
   k_prompt32<T><<<8 * per, 256, 0, st>>>(a, tiles, per);
 }
 
+static void prompt3(const PromptArgs& a, hipStream_t st) {
+  const int tiles = (a.tokens + 127) / 128, per = (int)(((long long)tiles * a.heads + 7) / 8);
+  k_prompt3<<<8 * per, 256, 0, st>>>(a, tiles, per);
+}
+
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
-  if (!a.bf16_data) return prompt32<float>(a, st);
+  if (!a.bf16_data) {
+    if ((a.tokens + 127) / 128 * (long long)a.heads >= 256) return prompt3(a, st);
+    return prompt32<float>(a, st);
+  }
   // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
   const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;

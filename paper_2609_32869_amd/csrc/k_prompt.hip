@@ -31,29 +31,33 @@ constexpr int kWindow = 512;
 struct Borders {
   int base, size, begin, end;  // begin, end: the rows of all sequences
 };
-// The block's 256 threads narrow the borders 256-fold a round (none up to 511 sequences) and load the window:
+// The block's NT threads narrow the borders NT-fold a round (none up to 511 sequences) and load the window:
 // one round trip to memory, where a search of 96 borders by every row takes seven.  meanwhile() runs while
-// the window is on its way.
-template <typename F>
+// the window is on its way.  counts: a word a wave.
+template <int NT, typename F>
 __device__ __forceinline__ Borders borders_near(const int* starts, int n, int q0, int* window, int* counts, const F& meanwhile) {
-  static_assert(kWindow == 512, "two borders a thread");
+  const int tid = threadIdx.x;
   int base = 0, size = n + 1;
   while (size > kWindow) {
-    const int stride = (size + 255) / 256, i = threadIdx.x * stride;
+    const int stride = (size + NT - 1) / NT, i = tid * stride;
     const int c = __popcll(__builtin_amdgcn_ballot_w64(i < size && starts[base + i] <= q0));
-    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
+    if ((tid & 63) == 0) counts[tid >> 6] = c;
     __syncthreads();
-    const int at = max(counts[0] + counts[1] + counts[2] + counts[3] - 1, 0) * stride;
+    int at = -1;
+    for (int w = 0; w < NT / 64; ++w) at += counts[w];
+    at = max(at, 0) * stride;
     __syncthreads();
     size = min(stride, size - at);
     base += at;
   }
   base = min(base, n);
-  const int x0 = starts[min(base + (int)threadIdx.x, n)], x1 = starts[min(base + 256 + (int)threadIdx.x, n)];
+  int x[kWindow / NT];
+#pragma unroll
+  for (int j = 0; j < kWindow / NT; ++j) x[j] = starts[min(base + NT * j + tid, n)];
   const Borders b{base, min(kWindow, n + 1 - base), starts[0], starts[n]};
   meanwhile();
-  window[threadIdx.x] = x0;
-  window[256 + threadIdx.x] = x1;
+#pragma unroll
+  for (int j = 0; j < kWindow / NT; ++j) window[NT * j + tid] = x[j];
   __syncthreads();
   return b;
 }
@@ -77,6 +81,26 @@ __device__ __forceinline__ int first_key(const int* starts, int n, const int* wi
     else hi = m;
   }
   return min(max(starts[lo], 0), t + 1);
+}
+
+// Which head and tile of rows a block takes.  An XCD gets every eighth block; so that its L2 holds few heads' keys and values
+// and all XCDs have equal work, each head's tiles are dealt to S = 2^shift parts (heads * S a multiple of 8), and the
+// XCD takes `parts` = heads * S / 8 of them that follow each other, those of the longest tiles first.  Contiguous
+// eighths of all (head, tile) pairs instead leave one XCD 1.75 heads' work and the next 1.25 (12 heads of 8,192 rows: 181 us).
+struct Grid {
+  int tiles, parts, shift, blocks;
+};
+static Grid grid_of(int tokens, int rows, int heads) {
+  const int tiles = (tokens + rows - 1) / rows, shift = heads % 8 == 0 ? 0 : heads % 4 == 0 ? 1 : heads % 2 == 0 ? 2 : 3;
+  const int parts = (heads << shift) / 8;
+  return Grid{tiles, parts, shift, 8 * parts * ((tiles + (1 << shift) - 1) >> shift)};
+}
+__device__ __forceinline__ bool block_of(const Grid& g, int& head, int& tile) {
+  const unsigned x = blockIdx.x & 7, j = blockIdx.x >> 3, k = j / (unsigned)g.parts, part = x * g.parts + (j - k * g.parts);
+  const int t = (k << g.shift) + (part & ((1 << g.shift) - 1));
+  head = part >> g.shift;
+  tile = g.tiles - 1 - t;
+  return t < g.tiles;
 }
 
 // N consecutive elements of a row.
@@ -154,12 +178,12 @@ __device__ __forceinline__ floatx16 product(const bf16x8 (&a)[N], const bf16x8 (
 //                are the operand as they are, and a lane's values are V[those keys][lane % 32 + 32 d]
 // The next tile's keys are loaded once this one's are multiplied, the values likewise.
 template <typename T>
-__global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, int per) {
+__global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
   constexpr int N = sizeof(T) == 4 ? 3 : 1;
   __shared__ float wm[4][32], wl[4][32], wo[4][32][68];
-  const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);  // as in k_prompt16
-  if (at >= tiles * a.heads) return;
-  const int head = at / tiles, q0 = (tiles - 1 - at % tiles) * 32;
+  int head, tile;
+  if (!block_of(grid, head, tile)) return;
+  const int q0 = tile * 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
   const int row = min(q0 + lr, a.tokens - 1);
   const T* Q = reinterpret_cast<const T*>(a.q) + row * a.qt + head * a.qh + 8 * lk;
@@ -188,7 +212,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, int tiles, in
   const int e = min(q0 + 32, a.tokens);
   int kt = e - 32 * (w + 1);
   int* window = reinterpret_cast<int*>(wo);
-  const Borders near = borders_near(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm), [&] {
+  const Borders near = borders_near<256>(a.starts, a.n, q0, window, reinterpret_cast<int*>(wm), [&] {
     load_keys(kt);
     load_values(kt);
   });
@@ -370,6 +394,25 @@ __device__ __forceinline__ void read_keys(uint32_t at, bf16x8 (&x)[4]) {
       : "v"(at), "v"(at ^ 32u), "v"(at ^ 64u), "v"(at ^ 96u)
       : "memory");
 }
+// Joins two groups' parts of the same rows (a wave of each has them in the same lanes): the reference m of a part's
+// probabilities, -inf where it saw no score, its sum and outputs.  The first group's waves get the whole and true.
+__device__ __forceinline__ bool join(int g, int w, float* lds, float m, float& l, floatx16 (&o)[2]) {
+  float* p = lds + w * 34 * 64 + (threadIdx.x & 63);
+  if (g) {
+    p[0] = m;
+    p[64] = l;
+#pragma unroll
+    for (int v = 0; v < 32; ++v) p[(2 + v) * 64] = o[v >> 4][v & 15];
+  }
+  __syncthreads();
+  if (g) return false;
+  const float m1 = p[0], top = fmaxf(m, m1), base = top == -INFINITY ? 0.f : top;
+  const float f = __builtin_amdgcn_exp2f((m - base) * kScale), f1 = __builtin_amdgcn_exp2f((m1 - base) * kScale);
+  l = l * f + p[64] * f1;
+#pragma unroll
+  for (int v = 0; v < 32; ++v) o[v >> 4][v & 15] = o[v >> 4][v & 15] * f + p[(2 + v) * 64] * f1;
+  return true;
+}
 // The values of 32 keys as the operands of four products, [sixteen keys][dim half]; `at` ^ 64: the other half.  The wait falls into
 // the time that the scores' products take.
 __device__ __forceinline__ void read_values(uint32_t at, bf16x8 (&x)[2][2]) {
@@ -393,8 +436,8 @@ __device__ __forceinline__ void read_values(uint32_t at, bf16x8 (&x)[2][2]) {
 
 // Keys and values k0 .. k0 + 63 (rows outside the tensors are the nearest) into a stage: the tile's address is the wave's, a
 // lane adds its constant chunk.
-__device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const PromptArgs& a, int k0, const Chunks& c, uint4* stage) {
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+__device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const PromptArgs& a, int k0, const Chunks& c, uint4* stage, int w) {
+  const int lane = threadIdx.x & 63;
   // (the instruction's own offset would move both addresses)
   lds_void *ks0 = (lds_void*)&stage[w * 128], *ks1 = (lds_void*)&stage[w * 128 + 64];
   lds_void *vs0 = (lds_void*)&stage[512 + w * 128], *vs1 = (lds_void*)&stage[512 + w * 128 + 64];
@@ -414,19 +457,19 @@ __device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const 
   }
 }
 
-template <int NQ, int KB, int WAVES>
-__global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles, int per) {
-  __shared__ uint4 stages[3 * kStage];
-  // The blocks that one XCD gets (every eighth) are neighbours: one head's, whose keys and values its L2 then
-  // holds, those with the most keys first.
-  const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if (at >= tiles * a.heads || (int)(blockIdx.x >> 3) >= per) return;
-  const int head = at / tiles, q0 = (tiles - 1 - at % tiles) * 128 * NQ;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
+template <int NQ, int KB, int WAVES, int G>
+__global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid grid) {
+  __shared__ uint4 shared_stages[G * 3 * kStage];
+  int head, tile;
+  if (!block_of(grid, head, tile)) return;
+  const int q0 = tile * 128 * NQ;
+  const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
+  uint4* const stages = shared_stages + g * 3 * kStage;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head * a.qh;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (head / a.group) * a.kh;
   const bf16* V = reinterpret_cast<const bf16*>(a.v) + (head / a.group) * a.vh;
-  __shared__ int window[kWindow], odd[4];  // odd: the last tile of a stage that held a NaN or an infinity
+  __shared__ int window[kWindow], odd[8];  // odd: the last tile of a group's stage that held a NaN or an infinity
   // Tile t: keys e - 64 (t + 1) .. e - 64 t - 1, from the block's own rows back to its first sequence's first row, so
   // that the first two can be copied before the borders are known.
   const int rows = 128 * NQ, e = min(q0 + rows, a.tokens), r0 = q0 + w * 32 * NQ;
@@ -442,10 +485,10 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
   }
   auto copy_first = [&] {
 #pragma unroll 1
-    for (int t = 0; t < 2; ++t) prompt_copy(K, V, a, e - (t + 1) * kTile, chunks, stages + t * kStage);
-    if (threadIdx.x < 4) odd[threadIdx.x] = -1;
+    for (int i = 0; i < 2; ++i) prompt_copy(K, V, a, e - (i * G + g + 1) * kTile, chunks, stages + i * kStage, w);
+    if (threadIdx.x < 8) odd[threadIdx.x] = -1;
   };
-  const Borders near = borders_near(a.starts, a.n, q0, window, odd, copy_first);
+  const Borders near = borders_near<256 * G>(a.starts, a.n, q0, window, odd, copy_first);
   // first keys do not decrease along the rows: of the wave's rows, and of the block's first and last
   int first = 0, bound = 0;
 #pragma unroll 1
@@ -480,11 +523,12 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
   // piece lane % 4 of dims 16 (lane / 16 % 2) ..
   const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
   const uint32_t kat = 128 * lr + 16 * (lk ^ (lr & 7)), vat = 8192 + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
-  auto step = [&](int t, uint4* cur, uint4* nxt) {
+  auto step = [&](int i, uint4* cur, uint4* nxt) {
+    const int t = i * G + g;
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)cur;
     __builtin_amdgcn_s_waitcnt(kWaitNext);
     const int kt = e - (t + 1) * kTile;
-    const bool cut = careful && (kt < b0 || kt + kTile > q0 + 1);  // some row of the block does not see some key
+    const bool cut = careful && t < nt && (kt < b0 || kt + kTile > q0 + 1);  // some row of the block does not see some key
     if (cut) {  // what is not finite among the values leaves the tile, each wave looking at what it copied
       uint4* own = cur + 512 + 128 * w + lane;
 #pragma unroll
@@ -492,14 +536,14 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
         const uint4 x = own[64 * j], y = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
         if (__builtin_amdgcn_ballot_w64(((x.x ^ y.x) | (x.y ^ y.y) | (x.z ^ y.z) | (x.w ^ y.w)) != 0)) {
           own[64 * j] = y;
-          if (lane == 0) odd[t & 3] = t;
+          if (lane == 0) odd[4 * g + (i & 3)] = t;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     }
     __builtin_amdgcn_s_barrier();
-    prompt_copy(K, V, a, e - min(t + 3, nt) * kTile, chunks, nxt);  // every step issues its copies: exact wait counts
-    if (kt >= r0 + 32 * NQ || kt + kTile <= w0) return;
+    prompt_copy(K, V, a, e - min(t + 2 * G + 1, nt) * kTile, chunks, nxt, w);  // every step issues its copies: exact wait counts
+    if (t >= nt || kt >= r0 + 32 * NQ || kt + kTile <= w0) return;
 #pragma unroll 1
     for (int h0 = 0; h0 < 2; h0 += KB) {
       const int kh = kt + 32 * h0;
@@ -581,19 +625,19 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
             }
           }
     }
-    if (cut && __builtin_amdgcn_readfirstlane(odd[t & 3]) == t) {  // and is added for the rows that see it
+    if (cut && __builtin_amdgcn_readfirstlane(odd[4 * g + (i & 3)]) == t) {  // and is added for the rows that see it
 #pragma unroll 1
       for (int key = max(kt, 0); key < kt + kTile; ++key) {
         const bf16* vp = V + key * a.vt + 4 * lk;
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
+        for (int b = 0; b < 8; ++b) {
           float x[4];
-          ld<4>(vp + 8 * g, 1, x);
+          ld<4>(vp + 8 * b, 1, x);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float y = finite(x[i]) ? 0.f : x[i];
+          for (int j = 0; j < 4; ++j) {
+            const float y = finite(x[j]) ? 0.f : x[j];
 #pragma unroll
-            for (int u = 0; u < NQ; ++u) o[u][g >> 2][4 * (g & 3) + i] += key >= lo[u] && key <= row[u] ? y : 0.f;
+            for (int u = 0; u < NQ; ++u) o[u][b >> 2][4 * (b & 3) + j] += key >= lo[u] && key <= row[u] ? y : 0.f;
           }
         }
       }
@@ -601,8 +645,8 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
   };
   for (;;) {
     uint4 *cur = stages, *nxt = stages + 2 * kStage;
-    for (int t = 0; t < nt; ++t) {
-      step(t, cur, nxt);
+    for (int i = 0; i * G < nt; ++i) {
+      step(i, cur, nxt);
       nxt = cur;
       cur = cur == stages + 2 * kStage ? stages : cur + kStage;
     }
@@ -623,6 +667,11 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
     copy_first();
     __syncthreads();
   }
+  if constexpr (G == 2) {
+    static_assert(NQ == 1, "one tile of rows a wave");
+    __syncthreads();
+    if (!join(g, w, reinterpret_cast<float*>(shared_stages), raise[0] > 0.f ? -nref[0][0] : -INFINITY, l[0], o[0])) return;
+  }
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
     const float total = pair_sum(l[u]), inv = total == 0.f ? 0.f : 1.f / total;
@@ -638,10 +687,10 @@ __global__ void __launch_bounds__(256, WAVES) k_prompt16(PromptArgs a, int tiles
             make_uint2(pack2_bf16(o[u][d][4 * g] * inv, o[u][d][4 * g + 1] * inv), pack2_bf16(o[u][d][4 * g + 2] * inv, o[u][d][4 * g + 3] * inv));
   }
 }
-template <int NQ, int KB, int WAVES>
+template <int NQ, int KB, int WAVES, int G>
 static void prompt16(const PromptArgs& a, hipStream_t st) {
-  const int tiles = (a.tokens + 128 * NQ - 1) / (128 * NQ), per = (int)(((long long)tiles * a.heads + 7) / 8);
-  k_prompt16<NQ, KB, WAVES><<<8 * per, 256, 0, st>>>(a, tiles, per);
+  const Grid g = grid_of(a.tokens, 128 * NQ, a.heads);
+  k_prompt16<NQ, KB, WAVES, G><<<g.blocks, 256 * G, 0, st>>>(a, g);
 }
 
 
@@ -652,17 +701,20 @@ static void prompt16(const PromptArgs& a, hipStream_t st) {
 // values' terms) in k_prompt16's order.  Products as in k_prompt32 (six a pair of operands, a plane at a time, the
 // smallest first), softmax as in k_prompt16.
 constexpr int kPlane = 4096, kStage3 = 6 * kPlane;
-__global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int per) {
-  __shared__ uint4 stages[2 * kStage3 / 16];
-  __shared__ int window[kWindow], odd[4];  // odd: the last tile of a stage that held a NaN or an infinity
-  const int at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);  // as in k_prompt16
-  if (at >= tiles * a.heads) return;
-  const int head = at / tiles, q0 = (tiles - 1 - at % tiles) * 128;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
+template <int G>
+__global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid) {
+  __shared__ uint4 shared_stages[G * 2 * kStage3 / 16];
+  __shared__ int window[kWindow], odd[8];  // odd: the last tile of a group's stage that held a NaN or an infinity
+  int head, tile;
+  if (!block_of(grid, head, tile)) return;
+  const int q0 = tile * 128;
+  const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
+  uint4* const stages = shared_stages + g * 2 * kStage3 / 16;
   const int e = min(q0 + 128, a.tokens), r0 = q0 + w * 32, row = min(r0 + lr, a.tokens - 1);
   const float* Q = reinterpret_cast<const float*>(a.q) + row * a.qt + head * a.qh + 8 * lk;
   const float* V = reinterpret_cast<const float*>(a.v) + (head / a.group) * a.vh;
-  const int cr = threadIdx.x >> 3, cc = threadIdx.x & 7;  // the thread's row of a tile and its eight dims
+  const int cr = (threadIdx.x & 255) >> 3, cc = threadIdx.x & 7;  // the thread's row of its group's tile and its eight dims
   const float *Kc = reinterpret_cast<const float*>(a.k) + (head / a.group) * a.kh + 8 * cc, *Vc = V + 8 * cc;
   float q[4][8], kx[8], vx[8];
 #pragma unroll
@@ -673,7 +725,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int
     ld<8>(Vc + r * a.vt, a.vec, vx);
   };
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)stages, put = 128 * cr + 16 * (cc ^ (cr & 7));
-  auto stage = [&](int t) {  // tile t's terms from the registers
+  auto stage = [&](int i) {  // the group's tile i, its terms from the registers
     // What is not finite among the values leaves the tile and is added for the rows that see it: its product with a
     // probability of 0 would reach those that do not (and an infinity in terms is NaN).
     float z = 0.f;
@@ -682,19 +734,19 @@ __global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int
     if (__builtin_amdgcn_ballot_w64(z != 0.f)) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) vx[j] = finite(vx[j]) ? vx[j] : 0.f;
-      if (lane == 0) odd[t & 1] = t;
+      if (lane == 0) odd[2 * g + (i & 1)] = i;
     }
-    char* to = reinterpret_cast<char*>(stages) + (t & 1) * kStage3 + put;
+    char* to = reinterpret_cast<char*>(stages) + (i & 1) * kStage3 + put;
     bf16x8 k3[3], v3[3];
     terms8<3>(kx, k3);
     terms8<3>(vx, v3);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      *reinterpret_cast<bf16x8*>(to + i * kPlane) = k3[i];
-      *reinterpret_cast<bf16x8*>(to + (3 + i) * kPlane) = v3[i];
+    for (int j = 0; j < 3; ++j) {
+      *reinterpret_cast<bf16x8*>(to + j * kPlane) = k3[j];
+      *reinterpret_cast<bf16x8*>(to + (3 + j) * kPlane) = v3[j];
     }
   };
-  const Borders near = borders_near(a.starts, a.n, q0, window, odd, [&] { load(0); });
+  const Borders near = borders_near<256 * G>(a.starts, a.n, q0, window, odd, [&] { load(g); });
   // first keys do not decrease along the rows: of the wave's rows, and of the block's first
   const int lo = first_key(a.starts, a.n, window, near, row), bound = first_key(a.starts, a.n, window, near, q0);
   const int k0 = __builtin_amdgcn_readfirstlane(bound), w0 = __builtin_amdgcn_readlane(lo, 0), f0 = __builtin_amdgcn_readlane(lo, 31);
@@ -709,22 +761,23 @@ __global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int
   for (int v = 0; v < 16; ++v) nref[v] = o[0][v] = o[1][v] = 0.f;
   const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
   const uint32_t kat = lds + 128 * lr + 16 * (lk ^ (lr & 7)), vat = lds + 3 * kPlane + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
-  if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+  if (threadIdx.x < 4) odd[threadIdx.x] = -1;
   __syncthreads();
-  if (nt > 0) stage(0);
+  stage(0);
   __syncthreads();
-  for (int t = 0; t < nt; ++t) {
-    if (t + 1 < nt) load(t + 1);
-    const int kt = e - (t + 1) * 32;
-    if (kt < r0 + 32 && kt + 32 > w0) {  // uniform
-      const uint32_t half = (t & 1) * kStage3;
+  for (int i = 0; i * G < nt; ++i) {
+    const int t = i * G + g, kt = e - (t + 1) * 32;
+    const bool more = (i + 1) * G < nt;
+    if (more) load(t + G);
+    if (t < nt && kt < r0 + 32 && kt + 32 > w0) {  // uniform
+      const uint32_t half = (i & 1) * kStage3;
       floatx16 sc = nref;
 #pragma unroll
-      for (int i = 2; i >= 0; --i) {
+      for (int b = 2; b >= 0; --b) {
         bf16x8 kf[4];
-        read_keys(kat + half + i * kPlane, kf);
+        read_keys(kat + half + b * kPlane, kf);
 #pragma unroll
-        for (int j = 2 - i; j >= 0; --j)
+        for (int j = 2 - b; j >= 0; --j)
 #pragma unroll
           for (int s = 0; s < 4; ++s) sc = mfma32(kf[s], qt[s][j], sc);
       }
@@ -755,43 +808,44 @@ __global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int
       }
       bf16x8 pt[2][3];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int s = 0; s < 2; ++s) {
         float p[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-          p[v] = __builtin_amdgcn_exp2f(sc[8 * i + v] * kScale);
+          p[v] = __builtin_amdgcn_exp2f(sc[8 * s + v] * kScale);
           l += p[v];
         }
-        terms8<3>(p, pt[i]);
+        terms8<3>(p, pt[s]);
       }
 #pragma unroll
-      for (int i = 2; i >= 0; --i) {
+      for (int b = 2; b >= 0; --b) {
         bf16x8 vf[2][2];
-        read_values(vat + half + i * kPlane, vf);
+        read_values(vat + half + b * kPlane, vf);
 #pragma unroll
-        for (int j = 2 - i; j >= 0; --j)
+        for (int j = 2 - b; j >= 0; --j)
 #pragma unroll
           for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int d = 0; d < 2; ++d) o[d] = mfma32(vf[s][d], pt[s][j], o[d]);
       }
-      if (__builtin_amdgcn_readfirstlane(odd[t & 1]) == t) {
+      if (__builtin_amdgcn_readfirstlane(odd[2 * g + (i & 1)]) == i) {
 #pragma unroll 1
         for (int key = max(kt, 0); key < min(kt + 32, a.tokens); ++key) {
           const float* vp = V + key * a.vt + 4 * lk;
 #pragma unroll
-          for (int g = 0; g < 8; ++g) {
+          for (int b = 0; b < 8; ++b) {
             float x[4];
-            ld<4>(vp + 8 * g, a.vec, x);
+            ld<4>(vp + 8 * b, a.vec, x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[g >> 2][4 * (g & 3) + i] += !finite(x[i]) && key >= lo && key <= row ? x[i] : 0.f;
+            for (int j = 0; j < 4; ++j) o[b >> 2][4 * (b & 3) + j] += !finite(x[j]) && key >= lo && key <= row ? x[j] : 0.f;
           }
         }
       }
     }
-    if (t + 1 < nt) stage(t + 1);
+    if (more) stage(i + 1);
     __syncthreads();
   }
+  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise > 0.f ? -nref[0] : -INFINITY, l, o)) return;
   const float total = pair_sum(l), inv = total == 0.f ? 0.f : 1.f / total;
   if (r0 + lr >= a.tokens || (!a.clear && (row < near.begin || row >= near.end))) return;
   float* op = reinterpret_cast<float*>(a.out) + ((size_t)row * a.heads + head) * kHeadDim + 4 * lk;
@@ -805,26 +859,39 @@ __global__ void __launch_bounds__(256, 2) k_prompt3(PromptArgs a, int tiles, int
 
 template <typename T>
 static void prompt32(const PromptArgs& a, hipStream_t st) {
-  const int tiles = (a.tokens + 31) / 32, per = (int)(((long long)tiles * a.heads + 7) / 8);
-  k_prompt32<T><<<8 * per, 256, 0, st>>>(a, tiles, per);
+  const Grid g = grid_of(a.tokens, 32, a.heads);
+  k_prompt32<T><<<g.blocks, 256, 0, st>>>(a, g);
 }
 
+template <int G>
 static void prompt3(const PromptArgs& a, hipStream_t st) {
-  const int tiles = (a.tokens + 127) / 128, per = (int)(((long long)tiles * a.heads + 7) / 8);
-  k_prompt3<<<8 * per, 256, 0, st>>>(a, tiles, per);
+  const Grid g = grid_of(a.tokens, 128, a.heads);
+  k_prompt3<G><<<g.blocks, 256 * G, 0, st>>>(a, g);
 }
 
+// By the blocks of 128 rows and the mean length.  us a replayed call (rows x heads; kernels as they are named below):
+//   few blocks, not of the shortest sequences: two groups of waves share a block's keys, since its own tiles one after the
+//     other are the call's time (2,048 x 20: 33.3, one group 41.5, fp32 95 / 125; 64 sequences of 32 x 20: 23.1 / 16.5, fp32 34 / 25;
+//     8,192 x 12: 162 / 145, fp32 613 / 573)
+//   many blocks of long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,691, 128 rows 5,048; 16,384 x 6:
+//     430 / 277)
+//   many blocks: 32 keys at a time, whose registers let three blocks share a compute unit (96 of 224 x 20: 72.1, 64 keys 85.3;
+//     4,096 x 32: 100 / 112; 8,192 x 12: 171 / 145)
+// fp32 below 256 blocks: 32 rows a block, its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32 49 / 53).
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
+  const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;
+  const bool shared = blocks <= 384 && mean >= 256;
   if (!a.bf16_data) {
-    if ((a.tokens + 127) / 128 * (long long)a.heads >= 256) return prompt3(a, st);
-    return prompt32<float>(a, st);
+    if (blocks < 256) return prompt32<float>(a, st);
+    if (shared) return prompt3<2>(a, st);
+    return prompt3<1>(a, st);
   }
   // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
-  const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;
-  if (mean >= 8192 && blocks >= 4096) return prompt16<2, 1, 2>(a, st);
-  if (mean < 2048 && blocks >= 768) return prompt16<1, 1, 3>(a, st);
-  prompt16<1, 2, 2>(a, st);
+  if (shared) return prompt16<1, 2, 2, 2>(a, st);
+  if (mean >= 8192 && blocks >= 2560) return prompt16<2, 1, 2, 1>(a, st);
+  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 3, 1>(a, st);
+  prompt16<1, 2, 2, 1>(a, st);
 }
 
 }  // namespace wf

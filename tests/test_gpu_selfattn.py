@@ -352,15 +352,18 @@ def check_rows(q, k, v, got, starts, rows):
         assert (np.abs(np.where(bad, 0, g) - np.where(bad, 0, want)) <= tol).all(), i
 
 
-@pytest.mark.parametrize("T,H,KV,lens", [(12345, 9, 3, 97), (12345, 8, 8, 13), (40000, 4, 1, 40), (33000, 20, 5, 1), (33100, 16, 16, 3), (70000, 16, 1, 2)])
+@pytest.mark.parametrize("T,H,KV,lens,dtype", [
+    (12345, 9, 3, 97, BF16), (12345, 8, 8, 13, BF16), (40000, 4, 1, 40, BF16), (33000, 20, 5, 1, BF16), (33100, 16, 16, 3, BF16), (70000, 16, 1, 2, BF16),
+    (12000, 2, 1, 2, BF16), (12345, 4, 4, 30, BF16), (12000, 6, 6, 4, BF16), (16400, 6, 3, 300, BF16),
+    (12345, 9, 3, 97, F32), (12000, 3, 1, 2, F32), (16400, 4, 4, 3, F32), (33000, 2, 2, 300, F32)])
 @pytest.mark.parametrize("odd", [False, True])
-def test_prompt_many_blocks(T, H, KV, lens, odd):
-    """bf16 calls of many blocks, short sequences and long ones, each with its own tiles; NaN and infinities in some values."""
+def test_prompt_many_blocks(T, H, KV, lens, dtype, odd):
+    """Calls of many blocks, short sequences and long ones, for each kind of tiles; NaN and infinities in some values."""
     rng = np.random.default_rng(T)
-    q, k, v = packed(T, H, KV, BF16)
+    q, k, v = packed(T, H, KV, dtype)
     cuts = np.sort(rng.choice(np.arange(1, T), lens - 1, replace=False)).tolist() if lens > 1 else []
     starts = [0] + cuts + [T]
-    if lens in (2, 3):
+    if lens in (2, 3, 4):
         starts = [0] + [T * i // lens for i in range(1, lens)] + [T - 77]
     at = int(rng.integers(1000, 9000))
     clean = None

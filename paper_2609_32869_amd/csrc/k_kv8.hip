@@ -308,7 +308,7 @@ __device__ __forceinline__ void cut(uint32_t& lo, uint32_t& hi, int left) {
 // a / b of numbers below 2^21: (a + 1/2) / b is 1 / (2 b) off a whole number at least, more than its roundings (a division
 // of integers is forty instructions)
 __device__ __forceinline__ int quotient(int a, int b) { return (int)((a + 0.5f) * __builtin_amdgcn_rcpf((float)b)); }
-// Codes and scales of two pages; there: bit t set where page t's number is good.
+// Codes and scales of two pages; there: bit t set where page t's number is good and it holds a position that a row sees.
 struct Step {
   uint4 k[2], v[2];
   uint32_t s[2], there;
@@ -474,7 +474,8 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       p[t] = __builtin_amdgcn_readlane(ahead, 2 * (i & 31) + t);
-      if (p[t] >= 0 && p[t] < a.c.n_pages) s.there |= 1u << t;
+      // nothing need ever have been stored in the page behind the last position: its scales may be anything
+      if (p[t] >= 0 && p[t] < a.c.n_pages && 32 * (g0 + i * NW) + 16 * t < top) s.there |= 1u << t;
       else p[t] = 0;
     }
     const size_t scales = (size_t)a.c.n_head * kKv8Head + 2 * head;

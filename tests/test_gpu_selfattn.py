@@ -592,6 +592,23 @@ def test_attend8_bad_pages(dtype, width):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [4, 70, 300])
+@pytest.mark.parametrize("fill", [0xff, 0x7f, 0x80])
+def test_attend8_pages_that_nothing_was_stored_in(dtype, width, fill):
+    """Pages behind the last position hold whatever the memory held, scales that stand for infinity among it."""
+    rng = np.random.default_rng(fill + width)
+    lens = [1, 15, 16, 17, 31, 32, 33, 47, 48, 49, 16 * width - 16, 16 * width - 17]
+    cache, model = lib().PagedCache8(len(lens) * width, 2), plain.PagedCache8(len(lens) * width, 2)
+    cache.data.fill_(fill)
+    tables = random_tables(rng, len(lens), width, len(lens) * width)
+    k, v = (rows_of(rng, (len(lens), max(lens), 2, 64), dtype, 0.5) for _ in range(2))
+    cache.store(k, v, i32(tables), i32([0] * len(lens)), counts=i32(lens))
+    model.store([num(k[r, :m]) for r, m in enumerate(lens)], [num(v[r, :m]) for r, m in enumerate(lens)], tables, [0] * len(lens))
+    q = rows_of(rng, (len(lens), 3, 4, 64), dtype, 0.3)
+    check_attend(cache, model, q, tables, [m - 3 for m in lens])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("width,where", [(3, 20), (3, 33), (60, 900)])
 def test_attend8_what_is_masked_may_hold_anything(dtype, width, where):
     """NaN in positions that some rows, or none, see."""

@@ -41,6 +41,32 @@ struct Raw<float, 4> {
   __device__ __forceinline__ void set(const float* o) { v = make_float4(o[0], o[1], o[2], o[3]); }
 };
 template <>
+struct Raw<float, 2> {
+  float2 v;
+  __device__ __forceinline__ void get(float* o) const { o[0] = v.x; o[1] = v.y; }
+  __device__ __forceinline__ void set(const float* o) { v = make_float2(o[0], o[1]); }
+};
+template <>
+struct Raw<bf16, 4> {
+  uint2 v;
+  __device__ __forceinline__ void get(float* o) const {
+    o[0] = __uint_as_float(v.x << 16);
+    o[1] = __uint_as_float(v.x & 0xffff0000u);
+    o[2] = __uint_as_float(v.y << 16);
+    o[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+  __device__ __forceinline__ void set(const float* o) { v = make_uint2(pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])); }
+};
+template <>
+struct Raw<bf16, 2> {
+  uint32_t v;
+  __device__ __forceinline__ void get(float* o) const {
+    o[0] = __uint_as_float(v << 16);
+    o[1] = __uint_as_float(v & 0xffff0000u);
+  }
+  __device__ __forceinline__ void set(const float* o) { v = pack2_bf16(o[0], o[1]); }
+};
+template <>
 struct Raw<float, 1> {
   float v;
   __device__ __forceinline__ void get(float* o) const { o[0] = v; }
@@ -68,9 +94,18 @@ struct Raw<bf16, 1> {
   __device__ __forceinline__ void set(const float* o) { v = from_f<bf16>(o[0]); }
 };
 
-// Block: `tb` tokens.  Their sines and cosines into LDS, then every (token, head, unit of N elements): a unit of
-// halves is N elements and their partners, one of interleaved pairs N elements (N = 1: a pair), the units
-// behind `dims` are copied.  A thread takes I units at a time, all loaded before the first is used, the first I before the
+// Units of N elements of a head: of halves N elements and their partners each, of interleaved pairs N elements (N = 1: a pair),
+// of which the last may reach past `dims`; the units behind are copied.
+struct Units {
+  int turning, copied, from;  // copied ones start at element `from`
+};
+template <int N>
+__host__ __device__ __forceinline__ Units units_of(const RotaryArgs& a) {
+  const int half = a.dims / 2, turning = N == 1 ? half : a.interleaved ? (a.dims + N - 1) / N : half / N;
+  const int from = a.interleaved && N > 1 ? turning * N : a.dims;
+  return Units{turning, a.copies ? (a.width - from) / N : 0, from};
+}
+// Block: `tb` tokens.  Their sines and cosines into LDS, then every (token, head, unit).  A thread takes I units at a time, all loaded before the first is used, the first I before the
 // sines are formed.  Memory bounds it.
 template <typename T, int N, int I>
 __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
@@ -78,7 +113,8 @@ __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
   typedef Raw<T, N> R;
   const int half = a.dims >> 1, t0 = (blockIdx.x + gridDim.x * blockIdx.z) * a.tb, nt = min(a.tb, a.tokens - t0);
   if (nt <= 0) return;
-  const int tu = N == 1 ? half : a.interleaved ? a.dims / N : half / N, units = tu + (a.copies ? (a.width - a.dims) / N : 0);
+  const Units of = units_of<N>(a);
+  const int tu = of.turning, units = tu + of.copied;
   const int heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0), total = nt * heads * units;
   // quotients of numbers below 2^22 as products: (i + 1/2) / n is 1 / (2 n) off a whole number at least, more than its two
   // roundings, 2^-23 of it; larger ones by division
@@ -103,7 +139,7 @@ __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
       const T* x = reinterpret_cast<const T*>(second ? a.rows[1].x : a.rows[0].x) + (t0 + t) * xt + h * xh;
       y[k] = reinterpret_cast<T*>(second ? a.rows[1].y : a.rows[0].y) + (t0 + t) * yt + h * yh;
       const bool turns = u < tu;
-      at[k] = !turns ? a.dims + (u - tu) * N : a.interleaved && N == 1 ? 2 * u : u * N;
+      at[k] = !turns ? of.from + (u - tu) * N : a.interleaved && N == 1 ? 2 * u : u * N;
       z[k] = !turns ? -1 : t * half + (a.interleaved && N > 1 ? u * N / 2 : u * N);
       p[k] = *reinterpret_cast<const R*>(x + at[k]);
       if (apart) q[k] = *reinterpret_cast<const R*>(x + (turns ? at[k] + apart : at[k]));
@@ -145,6 +181,7 @@ __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
       } else if constexpr (N > 1) {
 #pragma unroll
         for (int j = 0; j < N; j += 2) {
+          if (at[k] + j >= a.dims) break;
           const float2 d = c[j >> 1];
           const float s = fmaf(u[j], d.x, -(u[j + 1] * d.y));
           u[j + 1] = fmaf(u[j + 1], d.x, u[j] * d.y);
@@ -163,8 +200,8 @@ __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
 template <typename T, int N>
 static void rotary_launch(RotaryArgs& a, hipStream_t st) {
   const int half = a.dims / 2, heads = a.rows[0].heads + (a.n_rows > 1 ? a.rows[1].heads : 0);
-  const int units = N == 1 ? half + (a.copies ? a.width - a.dims : 0)
-                           : (a.interleaved ? a.dims / N : half / N) + (a.copies ? (a.width - a.dims) / N : 0);
+  const Units of = units_of<N>(a);
+  const int units = of.turning + of.copied;
   // Tokens of a block: units for every thread, more where there are blocks enough to fill the chip with them; sines
   // within LDS; at most 2^24 units
   const long long each = (long long)heads * units, all = each * a.tokens;
@@ -177,15 +214,21 @@ static void rotary_launch(RotaryArgs& a, hipStream_t st) {
   if (want > 256) k_rotary<T, N, 4><<<grid, 256, lds, st>>>(a);
   else k_rotary<T, N, 1><<<grid, 256, lds, st>>>(a);
 }
+// The widest units that the parts of a head hold whole and that all rows are aligned to.
 void rotary(const RotaryArgs& a0, hipStream_t st) {
   RotaryArgs a = a0;
-  const int nv = a.bf16_data ? 8 : 4;
-  const bool vec = a.vec && a.dims % (a.interleaved ? nv : 2 * nv) == 0 && (a.width - a.dims) % nv == 0;
+  auto fits = [&](int n) {
+    if (a.align < n * (a.bf16_data ? 2 : 4)) return false;
+    return a.interleaved ? a.width % n == 0 : a.dims % (2 * n) == 0 && (a.width - a.dims) % n == 0;
+  };
   if (a.bf16_data) {
-    if (vec) rotary_launch<bf16, 8>(a, st);
+    if (fits(8)) rotary_launch<bf16, 8>(a, st);
+    else if (fits(4)) rotary_launch<bf16, 4>(a, st);
+    else if (fits(2)) rotary_launch<bf16, 2>(a, st);
     else rotary_launch<bf16, 1>(a, st);
   } else {
-    if (vec) rotary_launch<float, 4>(a, st);
+    if (fits(4)) rotary_launch<float, 4>(a, st);
+    else if (fits(2)) rotary_launch<float, 2>(a, st);
     else rotary_launch<float, 1>(a, st);
   }
 }

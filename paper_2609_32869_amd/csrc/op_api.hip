@@ -323,7 +323,8 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
   a.tokens = tokens;
   a.bf16_data = dtype == WF_BF16;
   a.n_rows = k ? 2 : 1;
-  a.vec = 1;
+  a.align = 16;
+  int vec = 1;
   const struct {
     const void* x;
     const int64_t* xs;
@@ -334,8 +335,10 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
   for (int i = 0; i < a.n_rows; ++i) {
     const auto& w = rows[i];
     if (w.heads < 1 || w.heads > kMaxGrid) return bad("heads must be in [1, 65535]");
-    if (int r = check_strides(w.x, w.xs, e, a.vec, 2)) return r;
-    if (int r = check_strides(w.y, w.ys, e, a.vec, 2)) return r;
+    if (int r = check_strides(w.x, w.xs, e, vec, 2)) return r;
+    if (int r = check_strides(w.y, w.ys, e, vec, 2)) return r;
+    const uint64_t all = reinterpret_cast<uintptr_t>(w.x) | reinterpret_cast<uintptr_t>(w.y) | e * (w.xs[0] | w.xs[1] | w.ys[0] | w.ys[1]);
+    while (all % a.align) a.align /= 2;
     if (rows_overlap(w.ys, tokens, w.heads, width)) return bad("rows of a result overlap");
     if (w.x == w.y) {
       if ((tokens > 1 && w.xs[0] != w.ys[0]) || (w.heads > 1 && w.xs[1] != w.ys[1])) return bad("in place, strides must be equal");

@@ -188,7 +188,7 @@ struct RotaryArgs {
   int tokens, bf16_data;
   RotaryRows rows[2];
   int n_rows;
-  int vec;     // rows may be read and written 16 bytes at a time
+  int align;   // bytes, up to 16, that every row is aligned to
   int copies;  // elements from dims on are copied (y is not x)
   int tb;      // tokens of a block (set by the launcher)
 };

@@ -55,7 +55,7 @@ SCALINGS = [{}, dict(scaling="linear", factor=4.0), dict(scaling="base", factor=
 @pytest.mark.parametrize("inter", [False, True])
 @pytest.mark.parametrize("tokens,heads,kv,width,dims", [
     (1, 1, 1, 2, 2), (1, 20, 20, 64, 64), (7, 6, 2, 64, 32), (3, 5, 1, 63, 10), (65, 3, 3, 64, 62), (1000, 2, 2, 64, 64), (5, 4, 4, 128, 96),
-    (2, 3, 1, 4096, 4096), (33, 32, 8, 64, 48), (17, 1, 1, 80, 80), (2, 7, 7, 64, 4)])
+    (2, 3, 1, 4096, 4096), (33, 32, 8, 64, 48), (17, 1, 1, 80, 80), (2, 7, 7, 64, 4), (700, 20, 20, 64, 44), (900, 12, 4, 62, 42), (1100, 6, 6, 64, 46), (50, 3, 2, 64, 40), (9, 2, 2, 72, 6)])
 def test_rotary(tokens, heads, kv, width, dims, inter, dtype):
     g = torch.Generator("cuda").manual_seed(tokens * 100 + dims)
     kw = dict(SCALINGS[(tokens + heads + dims) % 4], interleaved=inter)
@@ -88,7 +88,7 @@ def test_rotary_positions():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("offset", [0, 1, 8])
+@pytest.mark.parametrize("offset", [0, 1, 2, 4, 8])
 def test_rotary_strides(dtype, offset):
     """Slices of a projection's output, heads before tokens, rows off a 16-byte border; nothing else changes in place."""
     g = torch.Generator("cuda").manual_seed(offset)

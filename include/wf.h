@@ -516,7 +516,7 @@ int wf_rotary_turns(int dims, double base, int scaling, double factor, double co
  * head * stride[1] + i elements in (strides >= 0, host arrays of two), likewise in their results
  * q_out and k_out.  k NULL: there is none (k_stride, k_heads, k_out and k_out_stride are not used).  A result is
  * its source itself with equal strides (in place) or other memory; its rows may not overlap, nor the
- * two results.
+ * two results (slices of the rows of one buffer may lie side by side), nor a result and the other's source.
  * 0 <= tokens <= 2^28 (0: nothing is enqueued), 1 <= heads <= 65535, 2 <= dims <= width <= 4096, dims even.
  * Errors: WF_EINVAL, WF_EHIP.
  */
@@ -577,7 +577,7 @@ int wf_kv8_page_bytes(int n_head, size_t* bytes);
  * starts: device int32 [n + 1], not decreasing (borders are taken as the nearest of [0, rows]),
  *   or NULL; counts: device int32 [n], taken as the nearest of [0, rows], or NULL.  Not both.
  * tables: device int32, entry (r, c) at r * table_stride + c, c < max_pages: the page of
- *   positions 16 c .. 16 c + 15.  A page written belongs to one request alone.
+ *   positions 16 c .. 16 c + 15.  A page that is written is named by one entry of one request alone.
  * positions: device int32 [n].  Rows at positions below 0 or from 16 max_pages on, and rows
  *   whose page number is outside [0, n_pages), are not stored.
  * rows >= 0 (0: nothing is enqueued), packed <= 2^27, otherwise <= 2^20 and n * ((rows + 30) / 16) below

@@ -1,6 +1,7 @@
 // C entries of the operators without a handle: argument checks and launches.
 #include <cmath>
 #include <cstdint>
+#include <utility>
 
 #include "../../include/wf.h"
 #include "wf_ops.h"
@@ -71,6 +72,21 @@ bool rows_overlap(const int64_t* s, int tokens, int heads, int width) {
   if (a < width || b < width) return true;
   if (tokens <= 1 || heads <= 1) return false;
   return a < b ? b / a < tokens : a / b < heads;
+}
+// Two such tensors of equal tokens that share memory, or that lie in one another in a way that is not looked into: rows of
+// one token beside each other, as slices of one buffer, do not.
+bool tensors_overlap(const char* a, const int64_t* as, int ah, const char* b, const int64_t* bs, int bh, int tokens, int width, size_t e) {
+  auto row = [&](const int64_t* s, int heads) { return (uint64_t)((heads > 1 ? (heads - 1) * s[1] : 0) + width) * e; };
+  auto all = [&](const int64_t* s, int heads) { return (tokens > 1 ? (uint64_t)(tokens - 1) * s[0] * e : 0) + row(s, heads); };
+  if (!overlap(a, all(as, ah), b, all(bs, bh))) return false;
+  if (tokens <= 1 || as[0] != bs[0]) return true;
+  if (b < a) {
+    std::swap(a, b);
+    std::swap(as, bs);
+    std::swap(ah, bh);
+  }
+  const uint64_t pitch = as[0] * e, apart = (uint64_t)(b - a) % pitch;
+  return apart < row(as, ah) || apart + row(bs, bh) > pitch;
 }
 int check_heads(int n_head, int n_kv_head) {
   if (n_kv_head < 1 || n_head < 1 || n_head > kMaxGrid || n_head % n_kv_head)
@@ -347,6 +363,9 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
     }
     a.rows[i] = RotaryRows{w.x, w.y, w.xs[0], w.xs[1], w.ys[0], w.ys[1], w.heads};
   }
+  if (k && tokens > 0 &&
+      tensors_overlap(static_cast<const char*>(q_out), q_out_stride, q_heads, static_cast<const char*>(k_out), k_out_stride, k_heads, tokens, width, e))
+    return bad("the results overlap");
   if (tokens == 0) return WF_OK;
   rotary(a, static_cast<hipStream_t>(stream));
   return launched();

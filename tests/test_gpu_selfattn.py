@@ -110,6 +110,18 @@ def test_rotary_strides(dtype, offset):
     check_rotary(rot.rotate(at, one.expand(11, 5, 64)), one.expand(11, 5, 64), at.cpu().numpy(), {}, 64)
 
 
+def test_rotary_in_place_twice_is_refused():
+    wf = lib()
+    rot, at, x = wf.Rotary(64), i32([1, 2, 3]), torch.randn((3, 6, 64), device="cuda")
+    for k in (x, x[:, 2:4], x[:, :1]):
+        with pytest.raises(wf.WfError, match="overlap"):
+            rot.rotate(at, x, k, in_place=True)
+    a = rot.rotate(at, x)
+    rot.rotate(at, x[:, :4], x[:, 4:], in_place=True)
+    assert torch.equal(x, a)
+    assert all(torch.equal(y, rot.rotate(at, x)) for y in rot.rotate(at, x, x))      # into new tensors: two of them
+
+
 def test_rotary_no_tokens_and_large_grids():
     rot = lib().Rotary(2)
     assert rot.rotate(i32([]), torch.empty((0, 3, 64), device="cuda")).shape == (0, 3, 64)
@@ -306,6 +318,18 @@ def test_prompt_offsets_past_32_bits():
     x = buf.as_strided((10, 4, 64), (far, 64, 1))
     x.copy_(torch.randn((10, 4, 64), device="cuda"))
     check_prompt(x[:, :2], x[:, 2:3], x[:, 3:], [0, 10])
+
+
+@pytest.mark.parametrize("dtype,H,pitch", [(BF16, 2, 1 << 24), (F32, 128, 1 << 23), (F32, 2, 1 << 23), (BF16, 2, (1 << 24) + 8)])
+def test_prompt_rows_far_apart(dtype, H, pitch):
+    """Keys whose rows lie 32 MB apart, 6 GB in all, for each kind of tiles."""
+    T = 200
+    buf = torch.empty((T - 1) * pitch + 128, dtype=dtype, device="cuda")
+    kv = buf.as_strided((T, 2, 64), (pitch, 64, 1))
+    kv.copy_(torch.randn((T, 2, 64), device="cuda"))
+    q = torch.randn((T, H, 64), device="cuda").to(dtype)
+    got = lib().prompt_attention(q, kv[:, :1], kv[:, 1:], i32([0, 70, 200]))
+    check_rows(q, kv[:, :1], kv[:, 1:], got, [0, 70, 200], [0, 69, 70, 199])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

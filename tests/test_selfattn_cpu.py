@@ -77,6 +77,16 @@ def test_rotary_refusals():
     varied(call, good, bad)
     assert call(lib, dict(good, tokens=0)) == 0
     assert call(lib, dict(good, tokens=0, k=None, ks=None, kh=0, ko=None, kos=None)) == 0
+    # results over each other: the same memory, heads of one buffer that meet, rows that reach into the next token's
+    rows = S2(30 * 64, 64)
+    wide = dict(good, qos=rows, kos=rows, kh=10)
+    for apart, bad_ in ((0, True), (19 * 64, True), (20 * 64, False), (20 * 64 + 8, True), (-10 * 64, False), (-9 * 64, True), (30 * 64 + 20 * 64, False),
+                        (30 * 64, True), (7 * 30 * 64, False), (6 * 30 * 64 + 20 * 64 - 8, True)):
+        a = dict(wide, qo=P + (1 << 16), ko=P + (1 << 16) + 4 * apart)
+        # a call that is fine is not made: a width of no good makes it refused for another reason
+        assert call(lib, a if bad_ else dict(a, dtype=9)) == -1
+        assert (b"results overlap" in lib.wf_last_error(None)) == bad_, apart
+    assert call(lib, dict(wide, qo=P + (1 << 16), ko=P + (1 << 16) + 4 * 20 * 64, kos=S2(31 * 64, 64))) == -1
     # layouts that do not overlap: heads before tokens, one head
     for strides in (S2(64, 7 * 64), S2(64, 9 * 64)):
         assert call(lib, dict(good, qos=strides, tokens=0)) == 0

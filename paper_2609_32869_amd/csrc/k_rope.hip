@@ -105,8 +105,8 @@ __host__ __device__ __forceinline__ Units units_of(const RotaryArgs& a) {
   const int from = a.interleaved && N > 1 ? turning * N : a.dims;
   return Units{turning, a.copies ? (a.width - from) / N : 0, from};
 }
-// Block: `tb` tokens.  Their sines and cosines into LDS, then every (token, head, unit).  A thread takes I units at a time, all loaded before the first is used, the first I before the
-// sines are formed.  Memory bounds it.
+// Block: `tb` tokens.  Their sines and cosines into LDS, then every (token, head, unit).  A thread takes I units at a time, all
+// loaded before the first is used, the first I before the sines are formed.
 template <typename T, int N, int I>
 __global__ void __launch_bounds__(256) k_rotary(RotaryArgs a) {
   extern __shared__ float2 cs[];

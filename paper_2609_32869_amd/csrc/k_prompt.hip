@@ -355,21 +355,21 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 
 // ---------------------------------------------------------------- bf16
 // Block: (128 NQ rows, head), G groups of four waves of 32 NQ rows; group g takes tiles g, g + G, ...  Keys and values
-// stream through three LDS stages a group in tiles of 64 rows, copied straight from memory
-// (global_load_lds_dwordx4) two tiles ahead of their use.  KB x 32 keys at a time a wave forms S^T = K q^T on
+// stream through two LDS stages a group in tiles of 64 rows, copied straight from memory
+// (global_load_lds_dwordx4) a tile ahead of their use.  KB x 32 keys at a time a wave forms S^T = K q^T on
 // v_mfma_f32_32x32x16_bf16, so a lane holds 16 of 32 keys of one row (keys 8 (v / 4) + 4 (lane / 32) + v % 4):
 // reference and sum are per lane (one swap of half-waves joins a row's two lanes) and the probabilities, rounded to
 // bf16 in place (2^-9 of each, as the results' own rounding), are the B operand of O^T += V^T P^T if the half-waves'
 // eight values of an instruction are taken as those keys.  The A operand then is, for a dim, keys 4 and 4 together,
 // what ds_read_b64_tr_b16 makes of rows as they lie in memory.  The sum is taken of the rounded probabilities.
 // 32,768 rows, 32 heads over 8: 4.6 ms, 950 TFLOP/s, 79% of what a library's large product reaches on this card (1,210);
-// 96 prompts of 1 to 447 rows, 20 heads: 78 us, where the bytes alone are 43.  Raising the waves' priority around the
-// products changes nothing; four waves of 64 rows for short prompts cost a third more than of 32.
+// 96 prompts of 1 to 447 rows, 20 heads: 66 us, where the bytes alone are 43.  A third stage gains nothing and costs the fourth
+// block of a compute unit; raising the waves' priority around the products changes nothing.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
 // A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then the values in the same way.
-constexpr int kWaitNext = (4 & 15) | (7 << 4);  // vmcnt <= 4: the copies of the tile behind the next; lgkmcnt 0
+constexpr int kWaitThis = (0 & 15) | (7 << 4);  // vmcnt 0, lgkmcnt 0
 constexpr int kWaitAll = (0 & 15) | (7 << 4) | (15 << 8);
 
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
@@ -469,19 +469,19 @@ __device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const 
 
 template <int NQ, int KB, int WAVES, int G>
 __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid grid) {
-  __shared__ uint4 shared_stages[G * 3 * kStage];
+  __shared__ uint4 shared_stages[G * 2 * kStage];
   int head, tile;
   if (!block_of(grid, head, tile)) return;
   const int q0 = tile * 128 * NQ;
   const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
-  uint4* const stages = shared_stages + g * 3 * kStage;
+  uint4* const stages = shared_stages + g * 2 * kStage;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head * a.qh;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (head / a.group) * a.kh;
   const bf16* V = reinterpret_cast<const bf16*>(a.v) + (head / a.group) * a.vh;
   __shared__ int window[kWindow], odd[8];  // odd: the last tile of a group's stage that held a NaN or an infinity
   // Tile t: keys e - 64 (t + 1) .. e - 64 t - 1, from the block's own rows back to its first sequence's first row, so
-  // that the first two can be copied before the borders are known.
+  // that the first is copied before the borders are known.
   const int rows = 128 * NQ, e = min(q0 + rows, a.tokens), r0 = q0 + w * 32 * NQ;
   const uint32_t crow = w * 16 + (lane >> 3), cbyte = 16 * ((lane ^ (lane >> 3)) & 7);
   const Chunks chunks{crow * 2 * (uint32_t)a.kt + cbyte, crow * 2 * (uint32_t)a.vt + cbyte};
@@ -494,8 +494,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
     for (int s = 0; s < 4; ++s) qf[u][s] = *reinterpret_cast<const bf16x8*>(Q + row[u] * a.qt + 16 * s + 8 * lk);
   }
   auto copy_first = [&] {
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) prompt_copy(K, V, a, e - (i * G + g + 1) * kTile, chunks, stages + i * kStage, w);
+    prompt_copy(K, V, a, e - (g + 1) * kTile, chunks, stages, w);
     if (threadIdx.x < 8) odd[threadIdx.x] = -1;
   };
   const Borders near = borders_near<256 * G>(a.starts, a.n, q0, window, odd, copy_first);
@@ -517,14 +516,16 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   // with a score above -inf, then moves only when a score passes it by kRaise: p stays below 2^8
   constexpr float kRaise = 8.f / kScale;
   float raise[NQ], l[NQ];
-  floatx16 nref[NQ], o[NQ][2];
+  constexpr int NR = WAVES == 4 ? 1 : 16;  // at four waves a SIMD the reference is subtracted instead, for sixteen registers
+  float nref[NQ][NR];
+  floatx16 o[NQ][2];
   auto clear = [&] {
 #pragma unroll
     for (int u = 0; u < NQ; ++u) {
       raise[u] = -INFINITY;
       l[u] = 0.f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) nref[u][v] = o[u][0][v] = o[u][1][v] = 0.f;
+      for (int v = 0; v < 16; ++v) nref[u][v % NR] = o[u][0][v] = o[u][1][v] = 0.f;
     }
   };
   clear();
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   auto step = [&](int i, uint4* cur, uint4* nxt) {
     const int t = i * G + g;
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)cur;
-    __builtin_amdgcn_s_waitcnt(kWaitNext);
+    __builtin_amdgcn_s_waitcnt(kWaitThis);
     const int kt = e - (t + 1) * kTile;
     const bool cut = careful && t < nt && (kt < b0 || kt + kTile > q0 + 1);  // some row of the block does not see some key
     if (cut) {  // what is not finite among the values leaves the tile, each wave looking at what it copied
@@ -546,13 +547,13 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
         const uint4 x = own[64 * j], y = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
         if (__builtin_amdgcn_ballot_w64(((x.x ^ y.x) | (x.y ^ y.y) | (x.z ^ y.z) | (x.w ^ y.w)) != 0)) {
           own[64 * j] = y;
-          if (lane == 0) odd[4 * g + (i & 3)] = t;
+          if (lane == 0) odd[2 * g + (i & 1)] = t;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     }
     __builtin_amdgcn_s_barrier();
-    prompt_copy(K, V, a, e - min(t + 2 * G + 1, nt) * kTile, chunks, nxt, w);  // every step issues its copies: exact wait counts
+    prompt_copy(K, V, a, e - min(t + G + 1, nt) * kTile, chunks, nxt, w);
     if (t >= nt || kt >= r0 + 32 * NQ || kt + kTile <= w0) return;
 #pragma unroll 1
     for (int h0 = 0; h0 < 2; h0 += KB) {
@@ -566,11 +567,25 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-          for (int u = 0; u < NQ; ++u) sc[u][kb] = mfma32(kf[s], qf[u][s], s == 0 ? nref[u] : sc[u][kb]);
+          for (int u = 0; u < NQ; ++u) {
+            if (s == 0) {
+#pragma unroll
+              for (int v = 0; v < 16; ++v) sc[u][kb][v] = NR == 16 ? nref[u][v % NR] : 0.f;
+            }
+            sc[u][kb] = mfma32(kf[s], qf[u][s], sc[u][kb]);
+          }
       }
       bf16x8 vf[KB][2][2];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) read_values(lds + 4096 * (h0 + kb) + vat, vf[kb]);
+      if constexpr (NR == 1) {
+#pragma unroll
+        for (int u = 0; u < NQ; ++u)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[u][kb][v] += nref[u][0];
+      }
       if (kh + 32 * KB > r0 + 1) {  // uniform: some row of the wave does not see some key behind it
 #pragma unroll
         for (int u = 0; u < NQ; ++u)
@@ -612,7 +627,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
 #pragma unroll
             for (int v = 0; v < 16; ++v) sc[u][kb][v] -= d;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) nref[u][v] -= d;
+          for (int v = 0; v < NR; ++v) nref[u][v] -= d;
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -635,7 +650,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
             }
           }
     }
-    if (cut && __builtin_amdgcn_readfirstlane(odd[4 * g + (i & 3)]) == t) {  // and is added for the rows that see it
+    if (cut && __builtin_amdgcn_readfirstlane(odd[2 * g + (i & 1)]) == t) {  // and is added for the rows that see it
 #pragma unroll 1
       for (int key = max(kt, 0); key < kt + kTile; ++key) {
         const bf16* vp = V + key * a.vt + 4 * lk;
@@ -654,11 +669,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
     }
   };
   for (;;) {
-    uint4 *cur = stages, *nxt = stages + 2 * kStage;
     for (int i = 0; i * G < nt; ++i) {
-      step(i, cur, nxt);
-      nxt = cur;
-      cur = cur == stages + 2 * kStage ? stages : cur + kStage;
+      step(i, stages + (i & 1) * kStage, stages + (1 - (i & 1)) * kStage);
     }
     __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy may land in LDS after the block has left
     if (careful) break;
@@ -880,15 +892,15 @@ static void prompt3(const PromptArgs& a, hipStream_t st) {
   k_prompt3<G><<<g.blocks, 256 * G, 0, st>>>(a, g);
 }
 
-// By the blocks of 128 rows and the mean length.  us a replayed call (rows x heads; kernels as they are named below):
+// By the blocks of 128 rows and the mean length.  us a replayed call (rows x heads):
 //   few blocks, not of the shortest sequences: two groups of waves share a block's keys, since its own tiles one after the
-//     other are the call's time (2,048 x 20: 33.3, one group 41.5, fp32 95 / 125; 64 sequences of 32 x 20: 23.1 / 16.5, fp32 34 / 25;
-//     8,192 x 12: 162 / 145, fp32 613 / 573)
-//   many blocks of long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,691, 128 rows 5,048; 16,384 x 6:
-//     430 / 277)
-//   many blocks: 32 keys at a time, whose registers let three blocks share a compute unit (96 of 224 x 20: 72.1, 64 keys 85.3;
-//     4,096 x 32: 100 / 112; 8,192 x 12: 171 / 145)
-// fp32 below 256 blocks: 32 rows a block, its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32 49 / 53).
+//     other are the call's time (2,048 x 20: 33.5, one group 42.3, fp32 95 / 125; but 64 sequences of 32 x 20: 23.2 / 16.2, fp32
+//     34 / 25; 8,192 x 12: 161 / 141, fp32 613 / 573)
+//   many blocks of long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,690 to 4,830, 128 rows 4,960; but
+//     16,384 x 6: 446 / 277)
+//   many blocks: 32 keys at a time and four blocks a compute unit (96 of 224 x 20: 64, with 64 keys 84; 16 of 1,024 x 32: 135 /
+//     160; but 8,192 x 12: 176 / 141)
+// fp32 below 256 blocks: 32 rows a block, its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32: 49 / 53).
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
   const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;
   const bool shared = blocks <= 384 && mean >= 256;
@@ -901,7 +913,7 @@ void prompt_attend(const PromptArgs& a, hipStream_t st) {
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
   if (shared) return prompt16<1, 2, 2, 2>(a, st);
   if (mean >= 8192 && blocks >= 2560) return prompt16<2, 1, 2, 1>(a, st);
-  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 3, 1>(a, st);
+  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 4, 1>(a, st);
   prompt16<1, 2, 2, 1>(a, st);
 }
 

@@ -355,21 +355,23 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 
 // ---------------------------------------------------------------- bf16
 // Block: (128 NQ rows, head), G groups of four waves of 32 NQ rows; group g takes tiles g, g + G, ...  Keys and values
-// stream through two LDS stages a group in tiles of 64 rows, copied straight from memory
-// (global_load_lds_dwordx4) a tile ahead of their use.  KB x 32 keys at a time a wave forms S^T = K q^T on
+// stream through NS LDS stages a group in tiles of 64 rows, copied straight from memory
+// (global_load_lds_dwordx4) NS - 1 tiles ahead of their use.  KB x 32 keys at a time a wave forms S^T = K q^T on
 // v_mfma_f32_32x32x16_bf16, so a lane holds 16 of 32 keys of one row (keys 8 (v / 4) + 4 (lane / 32) + v % 4):
 // reference and sum are per lane (one swap of half-waves joins a row's two lanes) and the probabilities, rounded to
 // bf16 in place (2^-9 of each, as the results' own rounding), are the B operand of O^T += V^T P^T if the half-waves'
 // eight values of an instruction are taken as those keys.  The A operand then is, for a dim, keys 4 and 4 together,
 // what ds_read_b64_tr_b16 makes of rows as they lie in memory.  The sum is taken of the rounded probabilities.
-// 32,768 rows, 32 heads over 8: 4.6 ms, 950 TFLOP/s, 79% of what a library's large product reaches on this card (1,210);
-// 96 prompts of 1 to 447 rows, 20 heads: 66 us, where the bytes alone are 43.  A third stage gains nothing and costs the fourth
-// block of a compute unit; raising the waves' priority around the products changes nothing.
+// 32,768 rows, 32 heads over 8: 4.5 to 4.7 ms by the card, 930 to 975 TFLOP/s, 80% of what a library's large product reaches on this card (1,210);
+// 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are 43.  With a third stage, and three
+// blocks a compute unit, 78; with two stages the long one 4.7 ms.  Raising the waves' priority around the products changes nothing.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
 // A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then the values in the same way.
-constexpr int kWaitThis = (0 & 15) | (7 << 4);  // vmcnt 0, lgkmcnt 0
+// lgkmcnt 0 and vmcnt the copies of the tiles behind the next, four each
+template <int NS>
+constexpr int kWaitNext = (4 * (NS - 2)) | (7 << 4);
 constexpr int kWaitAll = (0 & 15) | (7 << 4) | (15 << 8);
 
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
@@ -467,15 +469,15 @@ __device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const 
   }
 }
 
-template <int NQ, int KB, int WAVES, int G>
+template <int NQ, int KB, int WAVES, int G, int NS>
 __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid grid) {
-  __shared__ uint4 shared_stages[G * 2 * kStage];
+  __shared__ uint4 shared_stages[G * NS * kStage];
   int head, tile;
   if (!block_of(grid, head, tile)) return;
   const int q0 = tile * 128 * NQ;
   const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
-  uint4* const stages = shared_stages + g * 2 * kStage;
+  uint4* const stages = shared_stages + g * NS * kStage;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head * a.qh;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (head / a.group) * a.kh;
   const bf16* V = reinterpret_cast<const bf16*>(a.v) + (head / a.group) * a.vh;
@@ -494,7 +496,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
     for (int s = 0; s < 4; ++s) qf[u][s] = *reinterpret_cast<const bf16x8*>(Q + row[u] * a.qt + 16 * s + 8 * lk);
   }
   auto copy_first = [&] {
-    prompt_copy(K, V, a, e - (g + 1) * kTile, chunks, stages, w);
+#pragma unroll 1
+    for (int i = 0; i < NS - 1; ++i) prompt_copy(K, V, a, e - (i * G + g + 1) * kTile, chunks, stages + i * kStage, w);
     if (threadIdx.x < 8) odd[threadIdx.x] = -1;
   };
   const Borders near = borders_near<256 * G>(a.starts, a.n, q0, window, odd, copy_first);
@@ -537,7 +540,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   auto step = [&](int i, uint4* cur, uint4* nxt) {
     const int t = i * G + g;
     const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)cur;
-    __builtin_amdgcn_s_waitcnt(kWaitThis);
+    __builtin_amdgcn_s_waitcnt(kWaitNext<NS>);
     const int kt = e - (t + 1) * kTile;
     const bool cut = careful && t < nt && (kt < b0 || kt + kTile > q0 + 1);  // some row of the block does not see some key
     if (cut) {  // what is not finite among the values leaves the tile, each wave looking at what it copied
@@ -547,13 +550,13 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
         const uint4 x = own[64 * j], y = make_uint4(finite2(x.x), finite2(x.y), finite2(x.z), finite2(x.w));
         if (__builtin_amdgcn_ballot_w64(((x.x ^ y.x) | (x.y ^ y.y) | (x.z ^ y.z) | (x.w ^ y.w)) != 0)) {
           own[64 * j] = y;
-          if (lane == 0) odd[2 * g + (i & 1)] = t;
+          if (lane == 0) odd[4 * g + (i & 3)] = t;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     }
     __builtin_amdgcn_s_barrier();
-    prompt_copy(K, V, a, e - min(t + G + 1, nt) * kTile, chunks, nxt, w);
+    prompt_copy(K, V, a, e - min(t + (NS - 1) * G + 1, nt) * kTile, chunks, nxt, w);  // in every step: exact wait counts
     if (t >= nt || kt >= r0 + 32 * NQ || kt + kTile <= w0) return;
 #pragma unroll 1
     for (int h0 = 0; h0 < 2; h0 += KB) {
@@ -650,7 +653,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
             }
           }
     }
-    if (cut && __builtin_amdgcn_readfirstlane(odd[2 * g + (i & 1)]) == t) {  // and is added for the rows that see it
+    if (cut && __builtin_amdgcn_readfirstlane(odd[4 * g + (i & 3)]) == t) {  // and is added for the rows that see it
 #pragma unroll 1
       for (int key = max(kt, 0); key < kt + kTile; ++key) {
         const bf16* vp = V + key * a.vt + 4 * lk;
@@ -669,8 +672,11 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
     }
   };
   for (;;) {
+    uint4 *cur = stages, *nxt = stages + (NS - 1) * kStage;
     for (int i = 0; i * G < nt; ++i) {
-      step(i, stages + (i & 1) * kStage, stages + (1 - (i & 1)) * kStage);
+      step(i, cur, nxt);
+      nxt = cur;
+      cur = cur == stages + (NS - 1) * kStage ? stages : cur + kStage;
     }
     __builtin_amdgcn_s_waitcnt(kWaitAll);  // no copy may land in LDS after the block has left
     if (careful) break;
@@ -709,10 +715,10 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
             make_uint2(pack2_bf16(o[u][d][4 * g] * inv, o[u][d][4 * g + 1] * inv), pack2_bf16(o[u][d][4 * g + 2] * inv, o[u][d][4 * g + 3] * inv));
   }
 }
-template <int NQ, int KB, int WAVES, int G>
+template <int NQ, int KB, int WAVES, int G, int NS>
 static void prompt16(const PromptArgs& a, hipStream_t st) {
   const Grid g = grid_of(a.tokens, 128 * NQ, a.heads);
-  k_prompt16<NQ, KB, WAVES, G><<<g.blocks, 256 * G, 0, st>>>(a, g);
+  k_prompt16<NQ, KB, WAVES, G, NS><<<g.blocks, 256 * G, 0, st>>>(a, g);
 }
 
 
@@ -911,10 +917,10 @@ void prompt_attend(const PromptArgs& a, hipStream_t st) {
   }
   // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
-  if (shared) return prompt16<1, 2, 2, 2>(a, st);
-  if (mean >= 8192 && blocks >= 2560) return prompt16<2, 1, 2, 1>(a, st);
-  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 4, 1>(a, st);
-  prompt16<1, 2, 2, 1>(a, st);
+  if (shared) return prompt16<1, 2, 2, 2, 2>(a, st);
+  if (mean >= 8192 && blocks >= 2560) return prompt16<2, 1, 2, 1, 3>(a, st);
+  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 4, 1, 2>(a, st);
+  prompt16<1, 2, 2, 1, 2>(a, st);
 }
 
 }  // namespace wf

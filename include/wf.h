@@ -535,7 +535,7 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
  *   and from starts[n] on belong to none (where starts lies outside [0, tokens], the part
  *   inside counts; borders that decrease give results without meaning, read inside the tensors).
  * out: device [tokens, n_head, 64] in the same type.  Rows of no sequence are set to zero
- *   (clear != 0) or left as they are.
+ *   (clear != 0) or left as they are.  An out that lies within the extent of q, k or v is refused.
  * fp32: products in 32 bits; bf16: the probabilities are rounded to bf16 for their product, sums
  * are fp32.  An infinity in a row's query or in a key that it sees can make its result NaN; a row all of
  * whose scores are -inf gets zeros.

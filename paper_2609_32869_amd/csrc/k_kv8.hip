@@ -86,7 +86,9 @@ __device__ __forceinline__ int value_code(int lane, int j) {
 }
 
 // ---------------------------------------------------------------- store
-// A wave per (page that a request writes, head).  Where a request's pages lie in the grid: request r's first page has
+// A wave per (page that a request writes, head): the page's scale is the maximum of 1,024 elements, so a wave holds it whole
+// and reads and writes it once.  Bytes bound it: 8 x 8,192 rows of 8 heads, fp32, 335 MB in 65 us (5.1 TB/s, a large copy's
+// rate); one page a request (96 x 20 waves): 5 us of a first and a second trip to memory.  Where a request's pages lie in the grid: request r's first page has
 // number starts[r] / 16 + 2 r (packed), which leaves room for every page that its rows can touch, or r * per (padded).
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per, int hb) {
@@ -202,7 +204,8 @@ __device__ __forceinline__ void st4(float* p, const float* x) { *reinterpret_cas
 __device__ __forceinline__ void st4(bf16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
 }
-// A wave per (request, column of its table, head).
+// A wave per (request, column of its table, head).  Bytes bound it: 8 x 8,192 positions of 8 heads into fp32 604 MB, 95 us
+// (6.4 TB/s, nine tenths of them writes).
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
   const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
@@ -249,14 +252,19 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // ---------------------------------------------------------------- attention
 // A key and value head's query columns are the rows of its group's heads: column c is row c / group,
 // head c % group of the group.  Block (key and value head, request, 16 columns, chunk of the
-// positions) x eight waves; a wave takes steps of 32 positions (two pages), every eighth.
+// positions) x NW waves; a wave takes steps of 32 positions (two pages), every NW-th.
 //   scores   S^T = K q^T per page (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets column n of
 //            positions 4 kg .. + 3
-//   softmax  running maximum and sum per column, one rescaling per step
+//   softmax  running maximum and sum per column, rescaled where a maximum moves
 //   values   O^T = V^T P^T per step: two lane swaps turn its two score tiles into the operand
 //            (lane: column n, positions 8 kg .. + 7)
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for the
 //            merge kernel
+// A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
+// requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Of many short
+// ones, 96 x 9 rows at 0 to 438, 20 heads (19 us, the bytes 12), the start and end of 1,920 blocks are 8 us.  Two tiles of
+// 16 columns to a block share the conversion of their keys and values, but leave half the blocks and more registers:
+// 16 x 48 rows at 0 to 2,000, 12 heads over 6, 40.7 us for 26.0; four x nine rows from 65,536 on, 32 heads over 8, 190 for 215.
 namespace {
 constexpr float kLog2e = 1.44269504088896f;
 constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]

@@ -178,8 +178,8 @@ __device__ __forceinline__ floatx16 product(const bf16x8 (&a)[N], const bf16x8 (
 // ---------------------------------------------------------------- few rows, and rows of any alignment
 // Block: (32 rows, head), four waves that take every fourth tile of 32 keys, each on its own from memory
 // to registers, and join their maxima, sums and outputs in LDS at the end.  fp32 values enter the products as three
-// bf16 terms, six products of v_mfma_f32_32x32x16_bf16 for one sixteenth of the rate of v_mfma_f32_32x32x2_f32 each:
-// 9,001 rows of 12 heads 262 us against 471.
+// bf16 terms: six products of v_mfma_f32_32x32x16_bf16, each a sixteenth of the time of the same product by
+// v_mfma_f32_32x32x2_f32 (9,001 rows of 12 heads 262 us against 471).
 //   S^T = K q^T  a lane gets keys 8 (v / 4) + 4 (lane / 32) + v % 4 of row lane % 32
 //   O^T += V^T P^T  the half-waves' eight values of an instruction are taken as those keys, so the probabilities
 //                are the operand as they are, and a lane's values are V[those keys][lane % 32 + 32 d]
@@ -362,9 +362,9 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 // bf16 in place (2^-9 of each, as the results' own rounding), are the B operand of O^T += V^T P^T if the half-waves'
 // eight values of an instruction are taken as those keys.  The A operand then is, for a dim, keys 4 and 4 together,
 // what ds_read_b64_tr_b16 makes of rows as they lie in memory.  The sum is taken of the rounded probabilities.
-// 32,768 rows, 32 heads over 8: 4.5 to 4.7 ms by the card, 930 to 975 TFLOP/s, 80% of what a library's large product reaches on this card (1,210);
-// 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are 43.  With a third stage, and three
-// blocks a compute unit, 78; with two stages the long one 4.7 ms.  Raising the waves' priority around the products changes nothing.
+// 32,768 rows, 32 heads over 8: 4.5 to 4.7 ms by the card, 930 to 975 TFLOP/s, 80% of what a library's large product
+// reaches on it (1,210); 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are 43.  Raising the waves'
+// priority around the products changes nothing.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
@@ -533,8 +533,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   };
   clear();
   bool careful = false;
-  // a lane's key lk (chunk) of row lr; its part of sixteen keys by sixteen dims, as ds_read_b64_tr_b16 turns them: row 4 lk + lane / 4 % 4 (and 8 on), the 8-byte
-  // piece lane % 4 of dims 16 (lane / 16 % 2) ..
+  // a lane's key lk (chunk) of row lr; its part of sixteen keys by sixteen dims, as ds_read_b64_tr_b16 turns them: row
+  // 4 lk + lane / 4 % 4 (and 8 on), the 8-byte piece lane % 4 of dims 16 (lane / 16 % 2) ..
   const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
   const uint32_t kat = 128 * lr + 16 * (lk ^ (lr & 7)), vat = 8192 + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
   auto step = [&](int i, uint4* cur, uint4* nxt) {

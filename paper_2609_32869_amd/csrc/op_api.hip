@@ -387,6 +387,11 @@ int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, cons
   if (int r = check_strides(v, v_stride, e, a.vec, 2)) return r;
   if (!out || !aligned(out, 16)) return bad("out must be 16-byte aligned");
   if (tokens == 0) return WF_OK;
+  auto extent = [&](const int64_t* t, int heads) { return ((tokens - 1) * (uint64_t)t[0] + (heads - 1) * (uint64_t)t[1] + kHeadDim) * e; };
+  const uint64_t written = (uint64_t)tokens * n_head * kHeadDim * e;
+  if (overlap(out, written, q, extent(q_stride, n_head)) || overlap(out, written, k, extent(k_stride, n_kv_head)) ||
+      overlap(out, written, v, extent(v_stride, n_kv_head)))
+    return bad("out overlaps q, k or v");
   a.q = q;
   a.k = k;
   a.v = v;

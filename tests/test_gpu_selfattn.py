@@ -423,6 +423,11 @@ def test_prompt_refuses_gradients():
         with pytest.raises(wf.WfError):
             with torch.no_grad():
                 wf.prompt_attention(**dict(dict(q=q, k=k, v=v, starts=i32([0, 10])), **bad))
+    whole = torch.zeros((20, 2, 64), device="cuda")
+    for q, out in ((whole[:10], whole[:10]), (whole[:10], whole[9:19]), (whole[::2], whole[1:11])):
+        with pytest.raises(wf.WfError, match="overlaps"):
+            wf.prompt_attention(q, q, q, i32([0, 10]), out=out)
+    assert not wf.prompt_attention(whole[:10], whole[:10], whole[:10], i32([0, 10]), out=whole[10:]).any()
 
 
 # ---------------------------------------------------------------- the 8-bit paged cache

@@ -108,6 +108,10 @@ def test_prompt_refusals():
         "out": [(None, -1), (P + 8, -1)]})
     binding, lib = _lib()
     assert call(lib, dict(good, tokens=0)) == 0
+    # 100 tokens of 20 heads in rows of 60 (q) or 20 (k, v) heads: results over any of them
+    far = dict(good, k=P + (1 << 30), v=P + (2 << 30), dtype=0)
+    for out in (P, P + 100 * 20 * 64 * 4, P + (99 * 60 + 20) * 256 - 16, P + (1 << 30) - 16, P + (2 << 30) + 99 * 20 * 256):
+        assert call(lib, dict(far, out=out)) == -1 and b"overlaps" in lib.wf_last_error(None)
 
 
 def test_cache8_refusals():

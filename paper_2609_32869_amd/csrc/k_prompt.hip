@@ -368,12 +368,16 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
-// A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then the values in the same way.
+// A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then of its values at 8 r + (c ^ 2 (r & 3)): the four rows that sixteen
+// lanes read two chunks of by ds_read_b64_tr_b16 then lie in different banks (as the keys lie, two and two shared them).
 // lgkmcnt 0 and vmcnt the copies of the tiles behind the next, four each
 template <int NS>
 constexpr int kWaitNext = (4 * (NS - 2)) | (7 << 4);
 constexpr int kWaitAll = (0 & 15) | (7 << 4) | (15 << 8);
 
+// where chunk c of row r lies in its row of a stage, and which one lies there
+__device__ __forceinline__ int key_chunk(int r, int c) { return (c ^ r) & 7; }
+__device__ __forceinline__ int value_chunk(int r, int c) { return (c ^ 2 * (r & 3)) & 7; }
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16v2, a), __builtin_bit_cast(bf16v2, b), c, false);
 }
@@ -460,12 +464,12 @@ __device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const 
     __builtin_amdgcn_global_load_lds((const void*)(vp + c.v), vs0, 16, 0, 0);
     __builtin_amdgcn_global_load_lds((const void*)(in_sgpr(vp + 16 * a.vt) + c.v), vs1, 16, 0, 0);
   } else {
-    const int r = w * 16 + (lane >> 3), ch = 8 * ((lane ^ (lane >> 3)) & 7), last = a.tokens - 1;
+    const int r = w * 16 + (lane >> 3), ch = 8 * key_chunk(lane >> 3, lane), cv = 8 * value_chunk(lane >> 3, lane), last = a.tokens - 1;
     const int r0 = min(max(k0 + r, 0), last), r1 = min(max(k0 + r + 8, 0), last);
     __builtin_amdgcn_global_load_lds((const void*)(K + r0 * a.kt + ch), ks0, 16, 0, 0);
     __builtin_amdgcn_global_load_lds((const void*)(K + r1 * a.kt + ch), ks1, 16, 0, 0);
-    __builtin_amdgcn_global_load_lds((const void*)(V + r0 * a.vt + ch), vs0, 16, 0, 0);
-    __builtin_amdgcn_global_load_lds((const void*)(V + r1 * a.vt + ch), vs1, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(V + r0 * a.vt + cv), vs0, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(V + r1 * a.vt + cv), vs1, 16, 0, 0);
   }
 }
 
@@ -485,8 +489,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   // Tile t: keys e - 64 (t + 1) .. e - 64 t - 1, from the block's own rows back to its first sequence's first row, so
   // that the first is copied before the borders are known.
   const int rows = 128 * NQ, e = min(q0 + rows, a.tokens), r0 = q0 + w * 32 * NQ;
-  const uint32_t crow = w * 16 + (lane >> 3), cbyte = 16 * ((lane ^ (lane >> 3)) & 7);
-  const Chunks chunks{crow * 2 * (uint32_t)a.kt + cbyte, crow * 2 * (uint32_t)a.vt + cbyte};
+  const uint32_t crow = w * 16 + (lane >> 3);
+  const Chunks chunks{crow * 2 * (uint32_t)a.kt + 16 * key_chunk(lane >> 3, lane), crow * 2 * (uint32_t)a.vt + 16 * value_chunk(lane >> 3, lane)};
   int row[NQ], lo[NQ];  // a row and the first key that it sees (the row + 1: none)
   bf16x8 qf[NQ][4];
 #pragma unroll
@@ -535,7 +539,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   bool careful = false;
   // a lane's key lk (chunk) of row lr; its part of sixteen keys by sixteen dims, as ds_read_b64_tr_b16 turns them: row
   // 4 lk + lane / 4 % 4 (and 8 on), the 8-byte piece lane % 4 of dims 16 (lane / 16 % 2) ..
-  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
+  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = value_chunk(vrow, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1));
   const uint32_t kat = 128 * lr + 16 * (lk ^ (lr & 7)), vat = 8192 + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
   auto step = [&](int i, uint4* cur, uint4* nxt) {
     const int t = i * G + g;
@@ -753,7 +757,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
     ld<8>(Kc + r * a.kt, a.vec, kx);
     ld<8>(Vc + r * a.vt, a.vec, vx);
   };
-  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)stages, put = 128 * cr + 16 * (cc ^ (cr & 7));
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)stages, put = 128 * cr + 16 * key_chunk(cr, cc), putv = 3 * kPlane + 128 * cr + 16 * value_chunk(cr, cc);
   auto stage = [&](int i) {  // the group's tile i, its terms from the registers
     // What is not finite among the values leaves the tile and is added for the rows that see it: its product with a
     // probability of 0 would reach those that do not (and an infinity in terms is NaN).
@@ -765,14 +769,14 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
       for (int j = 0; j < 8; ++j) vx[j] = finite(vx[j]) ? vx[j] : 0.f;
       if (lane == 0) odd[2 * g + (i & 1)] = i;
     }
-    char* to = reinterpret_cast<char*>(stages) + (i & 1) * kStage3 + put;
+    char* to = reinterpret_cast<char*>(stages) + (i & 1) * kStage3;
     bf16x8 k3[3], v3[3];
     terms8<3>(kx, k3);
     terms8<3>(vx, v3);
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      *reinterpret_cast<bf16x8*>(to + j * kPlane) = k3[j];
-      *reinterpret_cast<bf16x8*>(to + (3 + j) * kPlane) = v3[j];
+      *reinterpret_cast<bf16x8*>(to + put + j * kPlane) = k3[j];
+      *reinterpret_cast<bf16x8*>(to + putv + j * kPlane) = v3[j];
     }
   };
   const Borders near = borders_near<256 * G>(a.starts, a.n, q0, window, odd, [&] { load(g); });
@@ -788,7 +792,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
   floatx16 nref, o[2];
 #pragma unroll
   for (int v = 0; v < 16; ++v) nref[v] = o[0][v] = o[1][v] = 0.f;
-  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = (2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ vrow;
+  const int vrow = 4 * lk + ((lane >> 2) & 3), vchunk = value_chunk(vrow, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1));
   const uint32_t kat = lds + 128 * lr + 16 * (lk ^ (lr & 7)), vat = lds + 3 * kPlane + 128 * vrow + 16 * vchunk + 8 * (lane & 1);
   if (threadIdx.x < 4) odd[threadIdx.x] = -1;
   __syncthreads();

@@ -362,9 +362,9 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 // bf16 in place (2^-9 of each, as the results' own rounding), are the B operand of O^T += V^T P^T if the half-waves'
 // eight values of an instruction are taken as those keys.  The A operand then is, for a dim, keys 4 and 4 together,
 // what ds_read_b64_tr_b16 makes of rows as they lie in memory.  The sum is taken of the rounded probabilities.
-// 32,768 rows, 32 heads over 8: 4.5 to 4.7 ms by the card, 930 to 975 TFLOP/s, 80% of what a library's large product
-// reaches on it (1,210); 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are 43.  Raising the waves'
-// priority around the products changes nothing.
+// 32,768 rows, 32 heads over 8: 4.7 to 5.3 ms by the card, whose clock falls under this load, 940 to 830 TFLOP/s, 78 to 72%
+// of what a library's large product reaches on it; 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are
+// 43.  Raising the waves' priority, around the products or of every other wave, changes nothing.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
@@ -435,13 +435,13 @@ __device__ __forceinline__ void read_values(uint32_t at, bf16x8 (&x)[2][2]) {
   uint2 r[8];
   asm volatile(
       "ds_read_b64_tr_b16 %0, %8\n\t"
-      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:0x400\n\t"
       "ds_read_b64_tr_b16 %2, %9\n\t"
-      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %4, %8 offset:2048\n\t"
-      "ds_read_b64_tr_b16 %5, %8 offset:3072\n\t"
-      "ds_read_b64_tr_b16 %6, %9 offset:2048\n\t"
-      "ds_read_b64_tr_b16 %7, %9 offset:3072\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:0x400\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:0x800\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:0xc00\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:0x800\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:0xc00\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
       : "v"(at), "v"(at ^ 64u)

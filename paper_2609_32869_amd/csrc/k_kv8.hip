@@ -263,8 +263,9 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
 // requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Of many short
 // ones, 96 x 9 rows at 0 to 438, 20 heads (19 us, the bytes 12), the start and end of 1,920 blocks are 8 us.  Two tiles of
-// 16 columns to a block share the conversion of their keys and values, but leave half the blocks and more registers:
-// 16 x 48 rows at 0 to 2,000, 12 heads over 6, 40.7 us for 26.0; four x nine rows from 65,536 on, 32 heads over 8, 190 for 215.
+// 16 columns to a block share the way and the conversion of their keys and values, but leave half the blocks and 156
+// registers: four x nine rows from 65,536 on, 32 heads over 8, 190 us for 214, but 32 x nine at 0 to 4,000 56 for 41; which of
+// them a call is, its lengths say, and they are on the device.
 namespace {
 constexpr float kLog2e = 1.44269504088896f;
 constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]

@@ -263,9 +263,8 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
 // requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Of many short
 // ones, 96 x 9 rows at 0 to 438, 20 heads (19 us, the bytes 12), the start and end of 1,920 blocks are 8 us.  Two tiles of
-// 16 columns to a block share the way and the conversion of their keys and values, but leave half the blocks and 156
-// registers: four x nine rows from 65,536 on, 32 heads over 8, 190 us for 214, but 32 x nine at 0 to 4,000 56 for 41; which of
-// them a call is, its lengths say, and they are on the device.
+// 16 columns to a block would share the conversion of their keys and values, but leave half the blocks and 156 registers: four
+// x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to 4,000 56 for 41.
 namespace {
 constexpr float kLog2e = 1.44269504088896f;
 constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
@@ -443,8 +442,18 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
   __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
-  const int chunk = quotient(blockIdx.x, a.c.n_head), head = blockIdx.x - chunk * a.c.n_head, r = blockIdx.y, c0 = blockIdx.z * 16;
-  const int cols = a.rows * a.group, cap = 16 * a.max_pages;
+  const int cols = a.rows * a.group, cap = 16 * a.max_pages, tiles = (cols + 15) >> 4;
+  int chunk = quotient(blockIdx.x, a.c.n_head), head = blockIdx.x - chunk * a.c.n_head, r = blockIdx.y, tile = blockIdx.z;
+  if (a.units) {  // eight (request, chunk, head)s' first tiles, their second ones, ...
+    const int eight = quotient(blockIdx.x, 8 * tiles), rest = blockIdx.x - 8 * tiles * eight, unit = 8 * eight + (rest & 7);
+    if (unit >= a.units) return;
+    tile = rest >> 3;
+    const int part = quotient(unit, a.c.n_head);
+    head = unit - part * a.c.n_head;
+    r = quotient(part, a.nchunk);
+    chunk = part - r * a.nchunk;
+  }
+  const int c0 = tile * 16;
   const int* table = a.tables + r * a.ts;
   // Before the request's position is known: the query, and the page numbers of the wave's first 32 steps (two a step) where
   // the positions are not split.
@@ -544,7 +553,7 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
       reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + c0 + c - ci * a.group) * kHeadDim + d] =
           from_f<T>(some ? O / L : 0.f);
     } else {
-      float* rec = a.part + ((((size_t)r * gridDim.z + blockIdx.z) * a.c.n_head + head) * a.nchunk + chunk) * kRecord;
+      float* rec = a.part + ((((size_t)r * tiles + tile) * a.c.n_head + head) * a.nchunk + chunk) * kRecord;
       rec[32 + t] = O;
       if (d == 0) {
         rec[c] = M;
@@ -612,9 +621,14 @@ size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages) {
 }
 
 template <typename T>
-static void attend_launch(const Kv8AttendArgs& a, hipStream_t st) {
-  const int cols = a.rows * a.group;
-  const dim3 grid(a.c.n_head * a.nchunk, a.n, (cols + 15) / 16);
+static void attend_launch(Kv8AttendArgs& a, hipStream_t st) {
+  // The tiles of the same keys and values one behind the other on one XCD (every eighth block), the later ones then read them
+  // from its L2.  us a replayed call, tiles by grid z / so: four x nine rows from 65,536 on, 32 heads over 8, 217 / 143; one x 17
+  // at 130,000, 20 heads, 124 / 91; 64 x five at 0 to 4,000, 32 over 8, 59 / 51; but 64 x 17 at 0 to 600, 20 heads, 30.6 / 32.2.
+  const int cols = a.rows * a.group, tiles = (cols + 15) / 16;
+  const long long units = (long long)a.n * a.nchunk * a.c.n_head, x = (units + 7) / 8 * 8 * tiles;
+  if (tiles > 1 && x <= 1 << 20) a.units = (int)units;
+  const dim3 grid = a.units ? dim3((unsigned)x) : dim3(a.c.n_head * a.nchunk, a.n, tiles);
   if (kv8_waves((long long)grid.x * grid.y * grid.z, a.max_pages) == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
   else k_kv8_attend<T, 8><<<grid, 512, 0, st>>>(a);
   if (a.nchunk > 1) k_kv8_merge<T><<<dim3(a.c.n_head, a.n, cols), 256, 0, st>>>(a);

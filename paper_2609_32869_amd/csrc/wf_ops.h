@@ -258,6 +258,7 @@ struct Kv8AttendArgs {
   void* out;    // [n][rows][n_head * group][64], the query's type
   float* part;  // chunk records (nchunk > 1)
   int nchunk;   // set by the launcher
+  int units;    // set by the launcher: requests x chunks x heads where blocks take their tiles in turn, else 0
 };
 size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages);
 void kv8_attend(const Kv8AttendArgs& a, hipStream_t st);

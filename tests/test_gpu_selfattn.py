@@ -594,6 +594,27 @@ def test_attend8(n, rows, heads, group, width, at, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,rows,heads,group,width,at", [(3, 5, 3, 7, 5, [33, 2, 74]), (3, 9, 3, 4, 150, [2391, 0, 1400]), (1, 9, 1, 2, 40, [600])])
+def test_attend8_several_tiles(n, rows, heads, group, width, at, dtype):
+    """More rows times heads than a block takes, with requests, chunks and heads that are no multiple of eight together."""
+    rng, cache, model, tables = filled(n, width, heads, seed=rows, dtype=dtype)
+    check_attend(cache, model, rows_of(rng, (n, rows, heads * group, 64), dtype, 0.3), tables, at)
+
+
+def test_attend8_many_rows():
+    """2^19 rows of 40 heads, all but the last 48 before the first position: more blocks than one grid axis is given."""
+    rng, cache, model, tables = filled(1, 3, 40, seed=5, dtype=BF16)
+    rows = 1 << 19
+    q = rows_of(rng, (1, 48, 40, 64), BF16, 0.3)
+    many = q[:, 17:18].expand(1, rows, 40, 64)                # of one row, the same q for all
+    got = cache.attend(many, i32(tables), i32([48 - rows]))
+    assert not got[:, :rows - 48].any()
+    some = cache.attend(many[:, :48], i32(tables), i32([0]))
+    assert torch.equal(got[:, rows - 48:], some)
+    check_attend(cache, model, many[:, :48], tables, [0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("width", [4, 100])
 def test_attend8_counts_and_positions(dtype, width):
     """Rows behind the given ones, before the first position and past the tables; requests of nothing."""

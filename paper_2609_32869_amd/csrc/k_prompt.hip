@@ -902,18 +902,22 @@ static void prompt3(const PromptArgs& a, hipStream_t st) {
   k_prompt3<G><<<g.blocks, 256 * G, 0, st>>>(a, g);
 }
 
-// By the blocks of 128 rows and the mean length.  us a replayed call (rows x heads):
-//   few blocks, not of the shortest sequences: two groups of waves share a block's keys, since its own tiles one after the
-//     other are the call's time (2,048 x 20: 33.5, one group 42.3, fp32 95 / 125; but 64 sequences of 32 x 20: 23.2 / 16.2, fp32
-//     34 / 25; 8,192 x 12: 161 / 141, fp32 613 / 573)
-//   many blocks of long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,690 to 4,830, 128 rows 4,960; but
-//     16,384 x 6: 446 / 277)
-//   many blocks: 32 keys at a time and four blocks a compute unit (96 of 224 x 20: 64, with 64 keys 84; 16 of 1,024 x 32: 135 /
-//     160; but 8,192 x 12: 176 / 141)
-// fp32 below 256 blocks: 32 rows a block, its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32: 49 / 53).
+// By the blocks of 128 rows and the mean length, whose causes are: few blocks leave compute units waiting for the longest, and
+// then a block's own tiles one after the other are the call's time; many keep all busy, and then what a row costs counts.
+// us a replayed call (sequences x rows x heads), bf16:
+//   few blocks of long sequences: two groups of waves share a block's keys, 64 keys at a time (2,048 x 20: 32; one group 42;
+//     2 x 4,000 x 8: 68 / 92; but 8 blocks of 560 rows x 14: 37 / 28)
+//   up to some more: two groups of 32 keys at a time and four waves a SIMD (4 x 4,200 x 8, 1,056 blocks: 126, one group 163; 4 x
+//     1,813 x 20: 61 / 69; 6 x 8,533 x 8: 687 / 707; but 9 x 1,896 x 24, 3,200 blocks: 176 / 166; 10,294 x 24: 422 / 414)
+//   very many of very long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,690 / 4,860; but 16,384 x 6:
+//     446 / 277)
+//   others: one group, 32 keys at a time, four waves a SIMD (96 of 224 x 20: 62; 64 keys and two waves 84)
+// fp32: two groups as above (4,266 x 2 x 8: 166 / 216; but 2,800 x 32, 704 blocks: 210 / 197); below 256 blocks 32 rows a block,
+// its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32: 49 / 53).
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
   const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;
-  const bool shared = blocks <= 384 && mean >= 256;
+  const bool few = blocks <= (a.bf16_data ? 256 : 384), some = blocks <= (a.bf16_data ? 640 : 576);
+  const bool shared = few ? mean >= 256 : some && mean >= (a.bf16_data ? 1536 : 1024);
   if (!a.bf16_data) {
     if (blocks < 256) return prompt32<float>(a, st);
     if (shared) return prompt3<2>(a, st);
@@ -922,9 +926,9 @@ void prompt_attend(const PromptArgs& a, hipStream_t st) {
   // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
   if (shared) return prompt16<1, 2, 2, 2, 2>(a, st);
-  if (mean >= 8192 && blocks >= 2560) return prompt16<2, 1, 2, 1, 3>(a, st);
-  if (blocks >= 1024 || (blocks >= 768 && mean < 1024)) return prompt16<1, 1, 4, 1, 2>(a, st);
-  prompt16<1, 2, 2, 1, 2>(a, st);
+  if (mean >= 16384 && blocks >= 4096) return prompt16<2, 1, 2, 1, 3>(a, st);
+  if (blocks <= (mean < 256 ? 0 : mean < 1024 ? 512 : a.n == 1 ? 1024 : mean < 4096 ? 1536 : 3584)) return prompt16<1, 1, 4, 2, 2>(a, st);
+  prompt16<1, 1, 4, 1, 2>(a, st);
 }
 
 }  // namespace wf

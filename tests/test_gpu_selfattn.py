@@ -378,7 +378,7 @@ def check_rows(q, k, v, got, starts, rows):
 
 @pytest.mark.parametrize("T,H,KV,lens,dtype", [
     (12345, 9, 3, 97, BF16), (12345, 8, 8, 13, BF16), (40000, 4, 1, 40, BF16), (33000, 20, 5, 1, BF16), (33100, 16, 16, 3, BF16), (70000, 16, 1, 2, BF16),
-    (12000, 2, 1, 2, BF16), (12345, 4, 4, 30, BF16), (12000, 6, 6, 4, BF16), (16400, 6, 3, 300, BF16),
+    (12000, 2, 1, 2, BF16), (12345, 4, 4, 30, BF16), (12000, 6, 6, 4, BF16), (16400, 6, 3, 300, BF16), (40000, 4, 2, 12, BF16),
     (12345, 9, 3, 97, F32), (12000, 3, 1, 2, F32), (16400, 4, 4, 3, F32), (33000, 2, 2, 300, F32)])
 @pytest.mark.parametrize("odd", [False, True])
 def test_prompt_many_blocks(T, H, KV, lens, dtype, odd):

@@ -906,13 +906,13 @@ static void prompt3(const PromptArgs& a, hipStream_t st) {
 // then a block's own tiles one after the other are the call's time; many keep all busy, and then what a row costs counts.
 // us a replayed call (sequences x rows x heads), bf16:
 //   few blocks of long sequences: two groups of waves share a block's keys, 64 keys at a time (2,048 x 20: 32; one group 42;
-//     2 x 4,000 x 8: 68 / 92; but 8 blocks of 560 rows x 14: 37 / 28)
+//     2 x 4,000 x 8: 68 / 92; but 10 x 512 x 14: 37 / 28)
 //   up to some more: two groups of 32 keys at a time and four waves a SIMD (4 x 4,200 x 8, 1,056 blocks: 126, one group 163; 4 x
 //     1,813 x 20: 61 / 69; 6 x 8,533 x 8: 687 / 707; but 9 x 1,896 x 24, 3,200 blocks: 176 / 166; 10,294 x 24: 422 / 414)
 //   very many of very long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,690 / 4,860; but 16,384 x 6:
 //     446 / 277)
 //   others: one group, 32 keys at a time, four waves a SIMD (96 of 224 x 20: 62; 64 keys and two waves 84)
-// fp32: two groups as above (4,266 x 2 x 8: 166 / 216; but 2,800 x 32, 704 blocks: 210 / 197); below 256 blocks 32 rows a block,
+// fp32: two groups as above (2 x 3,200 x 8: 166 / 216; but 2,800 x 32, 704 blocks: 210 / 197); below 256 blocks 32 rows a block,
 // its waves taking its keys in turn (224 x 20: 16.4, k_prompt3 20.3; 1,000 x 32: 49 / 53).
 void prompt_attend(const PromptArgs& a, hipStream_t st) {
   const long long blocks = (a.tokens + 127) / 128 * (long long)a.heads, mean = a.tokens / a.n;

@@ -255,22 +255,25 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // positions) x NW waves; a wave takes steps of 32 positions (two pages), every NW-th.
 //   scores   S^T = K q^T per page (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets column n of
 //            positions 4 kg .. + 3
-//   softmax  running maximum and sum per column, rescaled where a maximum moves
+//   softmax  per column a reference, which moves up to the maximum where a score passes it by kRaise (as every
+//            time a maximum moves, most steps of a short context rescaled), and the sum
 //   values   O^T = V^T P^T per step: two lane swaps turn its two score tiles into the operand
 //            (lane: column n, positions 8 kg .. + 7)
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for the
 //            merge kernel
 // A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
-// requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Of many short
-// ones, 96 x 9 rows at 0 to 438, 20 heads (19 us, the bytes 12), the start and end of 1,920 blocks are 8 us.  Two tiles of
-// 16 columns to a block would share the conversion of their keys and values, but leave half the blocks and 156 registers: four
-// x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to 4,000 56 for 41.
+// requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Vector
+// instructions bound many rows: 185 x 29 at 0 to 2,069, 32 heads over 8, 175 us, 135 of them a step of 12 products.  Of many
+// short ones, 96 x 9 rows at 0 to 438, 20 heads (16.7 us, the bytes 12), the start and end of 1,920 blocks are the rest.  Two
+// tiles of 16 columns to a block would share the conversion of their keys and values, but leave half the blocks and 156
+// registers: four x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to 4,000 56 for 41.
 namespace {
-constexpr float kLog2e = 1.44269504088896f;
+constexpr float kScale = 0.125f * 1.44269504088896f;  // exp(s / 8) = 2^(kScale s)
+constexpr float kRaise = 8.f / kScale;
 constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
 
 __device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kLog2e); }
+__device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kScale); }
 __device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -366,7 +369,7 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-  if (__builtin_amdgcn_ballot_w64(mx > st.m)) {  // some column's maximum moves (seldom, once a few hundred positions are seen)
+  if (__builtin_amdgcn_ballot_w64(mx - st.m > kRaise)) {  // some column's reference moves up to its maximum: probabilities stay below 2^8
     const float m = fmaxf(st.m, swap_max(mx)), f = exp_to(st.m, no_inf(m));  // 0 at first
     st.m = m;
     st.l *= f;
@@ -496,23 +499,21 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
       if (p[t] >= 0 && p[t] < a.c.n_pages && 32 * (g0 + i * NW) + 16 * t < top) s.there |= 1u << t;
       else p[t] = 0;
     }
-    const size_t scales = (size_t)a.c.n_head * kKv8Head + 2 * head;
+    const uint8_t* in[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint8_t* in = a.c.base + p[t] * a.c.page;
-      s.k[t] = *reinterpret_cast<const uint4*>(in + (size_t)head * kKv8Head + 16 * lane);
-      s.s[t] = *reinterpret_cast<const uint16_t*>(in + scales);
+      in[t] = a.c.base + p[t] * a.c.page + (size_t)head * kKv8Head;
+      s.k[t] = *reinterpret_cast<const uint4*>(in[t] + 16 * lane);
+      s.s[t] = *reinterpret_cast<const uint16_t*>(a.c.base + p[t] * a.c.page + (size_t)a.c.n_head * kKv8Head + 2 * head);
       if (!(s.there >> t & 1)) s.s[t] = 0x7f7f;  // another page's scales may be anything: 1
     }
-    const uint8_t* in = a.c.base + (kg >> 1 ? p[1] : p[0]) * a.c.page + (size_t)head * kKv8Head + kKv8Values + 32 * (lane & 31);
-    s.v[0] = *reinterpret_cast<const uint4*>(in);
-    s.v[1] = *reinterpret_cast<const uint4*>(in + 16);
+    const uint8_t* values = (kg >> 1 ? in[1] : in[0]) + kKv8Values + 32 * (lane & 31);
+    s.v[0] = *reinterpret_cast<const uint4*>(values);
+    s.v[1] = *reinterpret_cast<const uint4*>(values + 16);
   };
   if (steps > 0) {
     Step A, B;
     load(0, A);
-#pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = live ? 0.125f * x[j] : 0.f;
     bf16x8 qt[2][QT];
     split_terms<QT>(x, qt[0]);
     split_terms<QT>(x + 8, qt[1]);
@@ -536,9 +537,10 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
     *reinterpret_cast<floatx4*>(&wo[w][n][16 * kg + 4 * e]) = floatx4{st.o[0][e], st.o[1][e], st.o[2][e], st.o[3][e]};
   __syncthreads();
   const int nc = min(16, cols - c0);
-  for (int t = threadIdx.x; t < nc * 64; t += NW * 64) {
-    const int c = t >> 6, d = t & 63, ci = quotient(c0 + c, a.group);
-    float M = wm[0][c], L = 0.f, O = 0.f;
+  for (int t = threadIdx.x; t < nc * 16; t += NW * 64) {
+    const int c = t >> 4, d = 4 * (t & 15), ci = quotient(c0 + c, a.group);
+    float M = wm[0][c], L = 0.f;
+    floatx4 O = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 1; j < NW; ++j) M = fmaxf(M, wm[j][c]);
     const float base = no_inf(M);
@@ -546,15 +548,15 @@ __global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
     for (int j = 0; j < NW; ++j) {
       const float f = exp_to(wm[j][c], base);  // 0 for a wave of no positions
       L = fmaf(f, wl[j][c], L);
-      O = fmaf(f, wo[j][c][d], O);
+      O += f * *reinterpret_cast<const floatx4*>(&wo[j][c][d]);
     }
     if (a.nchunk == 1) {
-      const bool some = ci < count && pos + ci >= 0 && L != 0.f;
-      reinterpret_cast<T*>(a.out)[((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + c0 + c - ci * a.group) * kHeadDim + d] =
-          from_f<T>(some ? O / L : 0.f);
+      const float inv = ci < count && pos + ci >= 0 && L != 0.f ? 1.f / L : 0.f;
+      const float o[4] = {inv == 0.f ? 0.f : O[0] * inv, inv == 0.f ? 0.f : O[1] * inv, inv == 0.f ? 0.f : O[2] * inv, inv == 0.f ? 0.f : O[3] * inv};
+      st4(reinterpret_cast<T*>(a.out) + ((((size_t)r * a.rows + ci) * a.c.n_head + head) * a.group + c0 + c - ci * a.group) * kHeadDim + d, o);
     } else {
       float* rec = a.part + ((((size_t)r * tiles + tile) * a.c.n_head + head) * a.nchunk + chunk) * kRecord;
-      rec[32 + t] = O;
+      *reinterpret_cast<floatx4*>(rec + 32 + c * 64 + d) = O;
       if (d == 0) {
         rec[c] = M;
         rec[16 + c] = L;
@@ -606,10 +608,15 @@ __global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
   }
 }
 
-// Waves of a block: four where the positions are few and the blocks many, whose start and end then weigh more than a wave's
-// steps.  us a replayed call, four waves / eight (20 heads, bf16): 96 requests of one row at position 438 24.0 / 26.0, of nine
-// rows at 0 to 438 20.9 / 23.0, 256 of one at 0 to 447 33 / 43; one request at 447 6.8 / 6.1; 64 at 4,000 128 / 114.
-static int kv8_waves(long long blocks, int max_pages) { return max_pages <= 64 && blocks > 256 ? 4 : 8; }
+// Waves of a block: fewer where the positions are few and the blocks many, whose start and end then weigh more than a wave's
+// steps.  us a replayed call, bf16:
+//   one wave / four   256 requests of one row at 0 to 64, 20 heads, 15.6 / 22.4, of nine at 0 to 100, 32 heads over 8, 22.7 / 30.3
+//   four / eight      20 heads: 96 of nine rows at 0 to 438 21.7 / 24.5, 256 of one at 0 to 447 36 / 47; 32 over 8: 185 of 29 at 0 to
+//                     2,069 175 / 201; but 64 of one at 4,000, 20 heads, 127 / 118, 256 of one at 0 to 4,000 252 / 239
+static int kv8_waves(long long blocks, int max_pages) {
+  if (max_pages <= 8 && blocks > 1024) return 1;
+  return (max_pages <= 64 && blocks > 256) || (max_pages <= 192 && blocks >= 3584) ? 4 : 8;
+}
 // Chunks of the positions: towards four blocks a compute unit, each of two steps of every wave at least.
 static int kv8_chunks(int n, int rows, int group, int n_head, int max_pages) {
   const long long blocks = (long long)n * n_head * ((rows * group + 15) / 16), groups = (max_pages + 1) / 2;
@@ -629,7 +636,9 @@ static void attend_launch(Kv8AttendArgs& a, hipStream_t st) {
   const long long units = (long long)a.n * a.nchunk * a.c.n_head, x = (units + 7) / 8 * 8 * tiles;
   if (tiles > 1 && x <= 1 << 20) a.units = (int)units;
   const dim3 grid = a.units ? dim3((unsigned)x) : dim3(a.c.n_head * a.nchunk, a.n, tiles);
-  if (kv8_waves((long long)grid.x * grid.y * grid.z, a.max_pages) == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
+  const int waves = kv8_waves((long long)grid.x * grid.y * grid.z, a.max_pages);
+  if (waves == 1) k_kv8_attend<T, 1><<<grid, 64, 0, st>>>(a);
+  else if (waves == 4) k_kv8_attend<T, 4><<<grid, 256, 0, st>>>(a);
   else k_kv8_attend<T, 8><<<grid, 512, 0, st>>>(a);
   if (a.nchunk > 1) k_kv8_merge<T><<<dim3(a.c.n_head, a.n, cols), 256, 0, st>>>(a);
 }

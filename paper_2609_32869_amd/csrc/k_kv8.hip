@@ -259,7 +259,7 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 //            time a maximum moves, most steps of a short context rescaled), and the sum
 //   values   O^T = V^T P^T per step: two lane swaps turn its two score tiles into the operand
 //            (lane: column n, positions 8 kg .. + 7)
-//   output   waves joined in LDS; one chunk: O / l, else the chunk's (max, l, O) record for the
+//   output   waves joined in LDS; one chunk: O / l, else the chunk's (reference, l, O) record for the
 //            merge kernel
 // A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
 // requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Vector
@@ -270,7 +270,7 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 namespace {
 constexpr float kScale = 0.125f * 1.44269504088896f;  // exp(s / 8) = 2^(kScale s)
 constexpr float kRaise = 8.f / kScale;
-constexpr int kRecord = 32 + 16 * 64;  // max [16], sum [16], O [16][64]
+constexpr int kRecord = 32 + 16 * 64;  // reference [16], sum [16], O [16][64]
 
 __device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float exp_to(float x, float base) { return __builtin_amdgcn_exp2f((x - base) * kScale); }
@@ -369,7 +369,7 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-  if (__builtin_amdgcn_ballot_w64(mx - st.m > kRaise)) {  // some column's reference moves up to its maximum: probabilities stay below 2^8
+  if (__builtin_amdgcn_ballot_w64(mx - st.m > kRaise)) {  // references move up to the maxima: probabilities stay below 2^8
     const float m = fmaxf(st.m, swap_max(mx)), f = exp_to(st.m, no_inf(m));  // 0 at first
     st.m = m;
     st.l *= f;

@@ -9,13 +9,15 @@ behind the work that fills the tensors.  Workspaces and results come from PyTorc
 allocator for the call's stream, so concurrent calls and captured graphs each have their
 own.
 
-Rotary positions have a backward pass, the others none: their results of inputs that require
-gradients raise where a gradient is asked of them; what a cache stores or copies has no history.
+Rotary positions have a backward pass and forward-mode derivatives, the others neither: their
+results of inputs that require gradients raise where a gradient is asked of them, and inputs with
+a tangent are refused; what a cache stores or copies has no history.
 """
 import ctypes
 import functools
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import WF_BF16, WF_F32, WfError, WfKv4, WfKv8, _refuse, _tensor, load_library
 
@@ -120,6 +122,19 @@ def _without_backward(name, result, *tensors):
     return result
 
 
+def _dual(*tensors):
+    """Whether one of the call's tensors has a forward-mode tangent.  Outside of forward_ad's levels none has: looked at first
+    (0.06 us of the host, a tensor's tangent 0.3)."""
+    if getattr(forward_ad, "_current_level", 0) < 0:
+        return False
+    return any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
+def _refuse_tangents(name, *tensors):
+    if _dual(*tensors):
+        _refuse(f"{name} has no forward-mode derivative")
+
+
 @functools.lru_cache(maxsize=256)
 def _select_bytes(n, beams, vocab, k):
     if max(n, beams, vocab, abs(k)) >= _INTS:
@@ -136,6 +151,7 @@ def beam_select(logits, scores, k, suppress=None, stream=None):
     suppress: uint8 [vocab] or None.  Returns (score fp32, beam int32, token int32), each [n, k].
     """
     lib = load_library()
+    _refuse_tangents("beam_select", logits, scores)
     dev = _gpu(logits, "logits", 3)
     dtype = _type(logits, "logits")
     n, beams, vocab = logits.shape
@@ -274,6 +290,7 @@ class AcousticCache4:
     def attend(self, slot0, q, lens=None, stream=None):
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, n_head, 64], any strides but the last) over the first lens[r]
         frames (int32 [n], None: all) of entries slot0 ..: [n, rows, n_head, 64] in q's type."""
+        _refuse_tangents("attend", q)
         dtype, qs = self._rows(q, "q", None)
         n, rows = q.shape[:2]
         if not 0 <= slot0 <= self.entries - n:
@@ -347,13 +364,23 @@ def _changed(t):
 
 
 class _Rotate(torch.autograd.Function):
-    """Rotated tensors as a function of them; the gradient turns the other way."""
+    """Rotated tensors as a function of them; the gradient turns the other way, a tangent the same."""
 
     @staticmethod
     def forward(ctx, rotary, positions, transposed, stream, *tensors):
-        ctx.rotary, ctx.transposed = rotary, transposed
+        ctx.rotary, ctx.transposed, ctx.stream = rotary, transposed, stream
         ctx.save_for_backward(positions)
+        ctx.save_for_forward(positions)
         return rotary._turn(positions, tensors, transposed, False, stream)
+
+    @staticmethod
+    def jvp(ctx, *tangents):
+        (positions,) = ctx.saved_tensors
+        if ctx.stream is not None:  # as the results; an input without a tangent comes with zeros that the current stream has just made
+            ctx.stream.wait_stream(torch.cuda.current_stream(ctx.stream.device))
+        with torch.cuda.stream(ctx.stream):
+            rows = [t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous() for t in tangents[4:]]
+        return _Rotate.apply(ctx.rotary, positions, ctx.transposed, ctx.stream, *rows)
 
     @staticmethod
     def backward(ctx, *grads):
@@ -391,11 +418,12 @@ class Rotary:
     def rotate(self, positions, q, k=None, in_place=False, stream=None):
         """q, and k beside it, at their positions: q, k fp32 or bf16 [tokens, heads, width] of the same tokens, width and
         type (any strides but the last); positions int32 [tokens].  Returns new tensors, or the given ones changed in place
-        (without gradients): the rotated q, or (q, k)."""
+        (without gradients and tangents): the rotated q, or (q, k)."""
         tensors = (q,) if k is None else (q, k)
-        if torch.is_grad_enabled() and (isinstance(q, torch.Tensor) and q.requires_grad or isinstance(k, torch.Tensor) and k.requires_grad):
+        dual = _dual(q, k)
+        if dual or torch.is_grad_enabled() and (isinstance(q, torch.Tensor) and q.requires_grad or isinstance(k, torch.Tensor) and k.requires_grad):
             if in_place:
-                _refuse("tensors that require gradients are not changed in place")
+                _refuse(f"tensors that {'have tangents' if dual else 'require gradients'} are not changed in place")
             out = _Rotate.apply(self, positions, False, stream, *tensors)
         else:
             out = self._turn(positions, tensors, False, in_place, stream)
@@ -468,6 +496,7 @@ def prompt_attention(q, k, v, starts, out=None, stream=None):
     no sequence are zeros, or stay as they are in a given contiguous `out`.
     """
     lib = load_library()
+    _refuse_tangents("prompt_attention", q, k, v, out)
     key = _Layouts.of(q, k, v, starts)
     plan = _prompt_plans.get(key) or _prompt_plans.keep(key, _prompt_plan(q, k, v, starts))
     dev, dtype, tokens, heads, kv, n, qs, ks, vs = plan
@@ -605,6 +634,7 @@ class PagedCache8:
         """softmax(q k^T / 8) v of q (fp32 or bf16 [n, rows, heads, 64], any strides but the last; heads a multiple of the
         cache's): row i of request r stands at positions[r] + i (int32 [n]) and sees positions up to its own.  Rows from
         counts[r] (int32 [n], None: all) on give zeros.  Returns [n, rows, heads, 64] in q's type."""
+        _refuse_tangents("attend", q)
         ref = self._layer(layer)
         args = (q, tables, positions, counts)
         key = _Layouts.of(*args)

@@ -537,8 +537,10 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
  * out: device [tokens, n_head, 64] in the same type.  Rows of no sequence are set to zero
  *   (clear != 0) or left as they are.  An out that lies within the extent of q, k or v is refused.
  * fp32: products in 32 bits; bf16: the probabilities are rounded to bf16 for their product, sums
- * are fp32.  An infinity in a row's query or in a key that it sees can make its result NaN; a row all of
- * whose scores are -inf gets zeros.
+ * are fp32.  Values times probabilities, each at most 1, are summed before the division by the
+ * probabilities' sum: values of up to 3.4e38 / n give finite sums over n keys, larger ones may not.
+ * An infinity in a row's query or in a key that it sees can make its result NaN; a row all of whose
+ * scores are -inf gets zeros.
  * tokens >= 0 (0: nothing is enqueued), tokens * n_head <= 2^28, 1 <= n <= 2^24, 1 <= n_kv_head, n_head a
  * multiple of it <= 65535.
  * Errors: WF_EINVAL, WF_EHIP.
@@ -599,7 +601,8 @@ int wf_kv8_load(const wf_kv8* c, int n, const int32_t* tables, int64_t table_str
  * softmax and all sums are fp32.  Positions whose page number is outside [0, n_pages), and
  * those from 16 max_pages on, are left out; a row that sees none gets zeros, as do rows from
  * counts[r] on (device int32 [n], taken as the nearest of [0, rows], or NULL: all).  What
- * positions hold that a row does not see does not reach it.
+ * positions hold that a row does not see does not reach it.  Finite sums as in wf_prompt_attend:
+ * values of up to 3.4e38 / n over n positions.
  * q: device, fp32 or bf16; element (r, i, h, d) lies r * q_stride[0] + i * q_stride[1] +
  *   h * q_stride[2] + d elements in.  n_q_head: a multiple of the cache's n_head, <= 65535.
  * out: device [n, rows, n_q_head, 64] in the same type.

@@ -19,6 +19,9 @@ namespace wf {
 
 namespace {
 constexpr float kScale = 0.125f * 1.44269504088896340736f;  // exp(s / 8) = 2^(kScale s)
+// References of probabilities p = 2^(kScale (s - reference)) lie this far above the largest score that sets them, so p is 2^-8 there
+// and at most 1 where a later score passes it by less (it then moves up): a sum of p times n values of up to 3.4e38 / n stays finite.
+constexpr float kAbove = 8.f / kScale;
 
 __device__ __forceinline__ float pair_max(float v) {  // over the two half-waves
   const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -261,8 +264,8 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
     float mx = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    const float mn = fmaxf(m, pair_max(mx)), base = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f((m - base) * kScale);
+    const float mn = fmaxf(m, pair_max(mx)), top = mn == -INFINITY ? 0.f : mn, base = top + kAbove;
+    const float f = __builtin_amdgcn_exp2f((m - top) * kScale);
     m = mn;
     l *= f;
 #pragma unroll
@@ -519,9 +522,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   const int w0 = __builtin_amdgcn_readlane(first, 0), f0 = __builtin_amdgcn_readlane(first, 32 * NQ - 1);
   const int nt = (e - min(k0, e) + kTile - 1) / kTile;
   // Scores are formed less a reference of their row (the products' accumulators start at its negative,
-  // `nref`), so p = 2^(kScale s) with no rounding of the reference in it.  It becomes the maximum of the first tile
-  // with a score above -inf, then moves only when a score passes it by kRaise: p stays below 2^8
-  constexpr float kRaise = 8.f / kScale;
+  // `nref`), so p = 2^(kScale s) with no rounding of the reference in it.  It lies kAbove above the maximum of the first tile
+  // with a score above -inf, then moves only when a score passes it: p stays below 1.  raise: -inf before, 0 from then on
   float raise[NQ], l[NQ];
   constexpr int NR = WAVES == 4 ? 1 : 16;  // at four waves a SIMD the reference is subtracted instead, for sixteen registers
   float nref[NQ][NR];
@@ -621,9 +623,9 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
           for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[u][kb][v]);
         mx = pair_max(mx);
         if (__builtin_amdgcn_ballot_w64(mx > raise[u])) {
-          const float d = mx > raise[u] ? mx : 0.f;
-          const float f = raise[u] > 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;  // no score yet: l and o are 0
-          if (mx > raise[u]) raise[u] = kRaise;
+          const float d = mx > raise[u] ? mx + kAbove : 0.f;
+          const float f = raise[u] == 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;  // no score yet: l and o are 0
+          if (mx > raise[u]) raise[u] = 0.f;
           l[u] *= f;
 #pragma unroll
           for (int e = 0; e < 2; ++e)
@@ -702,7 +704,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   if constexpr (G == 2) {
     static_assert(NQ == 1, "one tile of rows a wave");
     __syncthreads();
-    if (!join(g, w, reinterpret_cast<float*>(shared_stages), raise[0] > 0.f ? -nref[0][0] : -INFINITY, l[0], o[0])) return;
+    if (!join(g, w, reinterpret_cast<float*>(shared_stages), raise[0] == 0.f ? -nref[0][0] : -INFINITY, l[0], o[0])) return;
   }
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
@@ -787,8 +789,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
   bf16x8 qt[4][3];
 #pragma unroll
   for (int s = 0; s < 4; ++s) terms8<3>(q[s], qt[s]);
-  constexpr float kRaise = 8.f / kScale;  // as in k_prompt16
-  float raise = -INFINITY, l = 0.f;
+  float raise = -INFINITY, l = 0.f;  // as in k_prompt16
   floatx16 nref, o[2];
 #pragma unroll
   for (int v = 0; v < 16; ++v) nref[v] = o[0][v] = o[1][v] = 0.f;
@@ -827,9 +828,9 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
       for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[v]);
       mx = pair_max(mx);
       if (__builtin_amdgcn_ballot_w64(mx > raise)) {
-        const float d = mx > raise ? mx : 0.f;
-        const float f = raise > 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;
-        if (mx > raise) raise = kRaise;
+        const float d = mx > raise ? mx + kAbove : 0.f;
+        const float f = raise == 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;
+        if (mx > raise) raise = 0.f;
         l *= f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -878,7 +879,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
     if (more) stage(i + 1);
     __syncthreads();
   }
-  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise > 0.f ? -nref[0] : -INFINITY, l, o)) return;
+  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise == 0.f ? -nref[0] : -INFINITY, l, o)) return;
   const float total = pair_sum(l), inv = total == 0.f ? 0.f : 1.f / total;
   if (r0 + lr >= a.tokens || (!a.clear && (row < near.begin || row >= near.end))) return;
   float* op = reinterpret_cast<float*>(a.out) + ((size_t)row * a.heads + head) * kHeadDim + 4 * lk;

@@ -1,0 +1,77 @@
+"""Attention over packed prompts and the 8-bit cache where values or scores are far apart: large values behind small
+references, infinities that a row does not see, a row's own keys far below the earlier ones."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as plain
+from test_gpu_selfattn import BF16, F32, INF, NAN, borders, bound, check_attend, check_rows, i32, lib, num, random_tables
+
+pytestmark = pytest.mark.gpu
+
+# (rows, heads, key and value heads, prompts, type, elements off a 16-byte border): each kind of tiles
+KINDS = [(300, 2, 1, 2, F32, 0), (12000, 3, 1, 2, F32, 0), (12345, 9, 3, 97, F32, 0), (300, 2, 1, 2, BF16, 1), (300, 2, 1, 4, BF16, 0), (700, 2, 1, 1, BF16, 0),
+         (12345, 4, 4, 30, BF16, 0), (33000, 20, 5, 1, BF16, 0)]
+
+
+def slices(T, H, KV, dtype, offset):
+    """Queries, keys and values of zeros, as slices of one buffer."""
+    buf = torch.zeros(offset + T * (H + 2 * KV) * 64, device="cuda", dtype=dtype)
+    x = buf[offset:].view(T, H + 2 * KV, 64)
+    return x[:, :H], x[:, H:H + KV], x[:, H + KV:]
+
+
+@pytest.mark.parametrize("T,H,KV,n,dtype,offset", KINDS)
+def test_prompt_large_values_behind_a_small_reference(T, H, KV, n, dtype, offset):
+    """A key five nats above the others' scores with values of 3e36: results are below that, whatever was seen before."""
+    q, k, v = slices(T, H, KV, dtype, offset)
+    g = torch.Generator("cuda").manual_seed(T)
+    v.copy_(torch.randn(v.shape, device="cuda", generator=g))
+    q[:, :, 0] = 8
+    starts = [T * i // n for i in range(n)] + [T]
+    rows = set()
+    for a, b in zip(starts[:3], starts[1:4]):
+        at = a + (b - a) // 5
+        k[at, :, 0], v[at, :, 3], v[at, :, 4] = 5, 3e36, -3e36
+        rows |= {i for i in (at - 1, at, at + 1, at + 64, at + 128, at + 200, b - 1) if a <= i < b}
+    got = lib().prompt_attention(q, k, v, i32(starts))
+    assert torch.isfinite(got).all()
+    check_rows(q, k, v, got, starts, sorted(rows))
+
+
+@pytest.mark.parametrize("dtype,offset", [(F32, 0), (BF16, 0), (BF16, 1)])
+@pytest.mark.parametrize("T", [100, 29000])
+def test_prompt_large_values_of_every_key(T, dtype, offset):
+    """100 keys a prompt, all values 3.3e36, scores of any order: sums of probabilities times values stay below 3.4e38."""
+    q, k, v = slices(T, 2, 1, dtype, offset)
+    g = torch.Generator("cuda").manual_seed(T)
+    q.copy_(torch.randn(q.shape, device="cuda", generator=g))
+    k.copy_(2 * torch.randn(k.shape, device="cuda", generator=g))
+    v.fill_(3.3e36)
+    starts = list(range(0, T + 1, 100))
+    got = lib().prompt_attention(q, k, v, i32(starts))
+    assert torch.isfinite(got).all()
+    check_rows(q, k, v, got, starts, [0, 1, 50, 99, T - 100, T - 1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,heads,group,width", [(1, 2, 1, 28), (1, 1, 8, 200), (300, 1, 1, 28), (260, 4, 1, 8)])
+def test_attend8_large_values_behind_a_small_reference(n, heads, group, width, dtype):
+    """The same of the cache's: one, four or eight waves a block, and chunks."""
+    rng, rows, length = np.random.default_rng(width), 2, 16 * width
+    cache, model = lib().PagedCache8(n * width, heads), plain.PagedCache8(n * width, heads)
+    tables = random_tables(rng, n, width, n * width)
+    k = torch.zeros((n, length, heads, 64), device="cuda")
+    v = torch.from_numpy(rng.standard_normal(k.shape)).float().cuda()
+    for at in {40, 259, length - 40}:
+        if at < length - rows:
+            k[:, at, :, 0], v[:, at, :, 3], v[:, at, :, 4] = 5, 3e36, -3e36
+    cache.store(k, v, i32(tables), i32([0] * n))
+    q = torch.zeros((n, rows, heads * group, 64), device="cuda", dtype=dtype)
+    q[..., 0] = 8
+    at = [length - rows] * n
+    got = cache.attend(q, i32(tables), i32(at))
+    assert torch.isfinite(got).all()
+    some = sorted({0, n // 2, n - 1})
+    model.store(num(k[some]), num(v[some]), tables[some], [0] * len(some))
+    check_attend(cache, model, q[some], tables[some], at[:len(some)], got=got[some])

@@ -521,9 +521,9 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   const int k0 = __builtin_amdgcn_readlane(bound, 0), b0 = __builtin_amdgcn_readlane(bound, 1);
   const int w0 = __builtin_amdgcn_readlane(first, 0), f0 = __builtin_amdgcn_readlane(first, 32 * NQ - 1);
   const int nt = (e - min(k0, e) + kTile - 1) / kTile;
-  // Scores are formed less a reference of their row (the products' accumulators start at its negative,
-  // `nref`), so p = 2^(kScale s) with no rounding of the reference in it.  It lies kAbove above the maximum of the first tile
-  // with a score above -inf, then moves only when a score passes it: p stays below 1.  raise: -inf before, 0 from then on
+  // Scores are formed less a reference of their row (the products' accumulators start at its negative, `nref`), so p =
+  // 2^(kScale s).  It lies kAbove above the maximum of the first tile with a score above -inf, then moves only when a
+  // score passes it: p stays below 1.  raise: -inf before, 0 from then on
   float raise[NQ], l[NQ];
   constexpr int NR = WAVES == 4 ? 1 : 16;  // at four waves a SIMD the reference is subtracted instead, for sixteen registers
   float nref[NQ][NR];
@@ -587,56 +587,74 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
       bf16x8 vf[KB][2][2];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) read_values(lds + 4096 * (h0 + kb) + vat, vf[kb]);
-      if constexpr (NR == 1) {
-#pragma unroll
-        for (int u = 0; u < NQ; ++u)
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) sc[u][kb][v] += nref[u][0];
-      }
-      if (kh + 32 * KB > r0 + 1) {  // uniform: some row of the wave does not see some key behind it
-#pragma unroll
-        for (int u = 0; u < NQ; ++u)
+      auto masked = [&](int u, floatx16 (&x)[KB]) {  // and their maximum
+        if (kh + 32 * KB > r0 + 1) {                 // uniform: some row of the wave does not see some key behind it
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              sc[u][kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) <= row[u] - kh - 4 * lk ? sc[u][kb][v] : -INFINITY;
-      }
-      if (kh < f0) {  // nor keys of the sequence before
-#pragma unroll
-        for (int u = 0; u < NQ; ++u)
+              x[kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) <= row[u] - kh - 4 * lk ? x[kb][v] : -INFINITY;
+        }
+        if (kh < f0) {  // nor keys of the sequence before
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-              sc[u][kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) >= lo[u] - kh - 4 * lk ? sc[u][kb][v] : -INFINITY;
-      }
-      uint32_t pk[NQ][KB][8];
-#pragma unroll
-      for (int u = 0; u < NQ; ++u) {
-        float mx = sc[u][0][0];
+              x[kb][v] = 32 * kb + 8 * (v >> 2) + (v & 3) >= lo[u] - kh - 4 * lk ? x[kb][v] : -INFINITY;
+        }
+        float mx = x[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[u][kb][v]);
-        mx = pair_max(mx);
-        if (__builtin_amdgcn_ballot_w64(mx > raise[u])) {
-          const float d = mx > raise[u] ? mx + kAbove : 0.f;
-          const float f = raise[u] == 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;  // no score yet: l and o are 0
-          if (mx > raise[u]) raise[u] = 0.f;
+          for (int v = 0; v < 16; ++v) mx = fmaxf(mx, x[kb][v]);
+        return pair_max(mx);
+      };
+      uint32_t pk[NQ][KB][8];
+#pragma unroll
+      for (int u = 0; u < NQ; ++u) {
+        float mx = masked(u, sc[u]);
+        const bool up = (NR == 1 ? mx + nref[u][0] : mx) > raise[u];
+        if (__builtin_amdgcn_ballot_w64(up)) {
+          // Sums that began at a reference hold its roundings, however far below the new one it lies: the scores of such rows again
+          if (NR == 16 && __builtin_amdgcn_ballot_w64(up && raise[u] == 0.f)) {
+            floatx16 x[KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+              bf16x8 kf[4];
+              read_keys(lds + 4096 * (h0 + kb) + kat, kf);
+#pragma unroll
+              for (int v = 0; v < 16; ++v) x[kb][v] = 0.f;
+#pragma unroll
+              for (int s = 0; s < 4; ++s) x[kb] = mfma32(kf[s], qf[u][s], x[kb]);
+            }
+            mx = masked(u, x);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) sc[u][kb][v] = up ? x[kb][v] : sc[u][kb][v];
+          }
+          const float next = up ? -(mx + kAbove) : nref[u][0];
+          const float f = !up ? 1.f : raise[u] == 0.f ? __builtin_amdgcn_exp2f(fminf(next - nref[u][0], 0.f) * kScale) : 0.f;  // no score yet: l and o are 0
+          if (up) raise[u] = 0.f;
           l[u] *= f;
 #pragma unroll
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[u][e][v] *= f;
+          if constexpr (NR == 16) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int v = 0; v < 16; ++v) sc[u][kb][v] += up ? next : 0.f;
+          }
+#pragma unroll
+          for (int v = 0; v < NR; ++v) nref[u][v] = next;
+        }
+        if constexpr (NR == 1) {
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sc[u][kb][v] -= d;
-#pragma unroll
-          for (int v = 0; v < NR; ++v) nref[u][v] -= d;
+            for (int v = 0; v < 16; ++v) sc[u][kb][v] += nref[u][0];
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -805,39 +823,51 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
     if (more) load(t + G);
     if (t < nt && kt < r0 + 32 && kt + 32 > w0) {  // uniform
       const uint32_t half = (i & 1) * kStage3;
+      auto scores = [&](floatx16& x) {  // onto x, and their maximum
+#pragma unroll
+        for (int b = 2; b >= 0; --b) {
+          bf16x8 kf[4];
+          read_keys(kat + half + b * kPlane, kf);
+#pragma unroll
+          for (int j = 2 - b; j >= 0; --j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) x = mfma32(kf[s], qt[s][j], x);
+        }
+        if (kt + 31 > r0) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = 8 * (v >> 2) + (v & 3) <= row - kt - 4 * lk ? x[v] : -INFINITY;
+        }
+        if (kt < f0) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = 8 * (v >> 2) + (v & 3) >= lo - kt - 4 * lk ? x[v] : -INFINITY;
+        }
+        float mx = x[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) mx = fmaxf(mx, x[v]);
+        return pair_max(mx);
+      };
       floatx16 sc = nref;
+      float mx = scores(sc);
+      const bool up = mx > raise;
+      if (__builtin_amdgcn_ballot_w64(up)) {
+        if (__builtin_amdgcn_ballot_w64(up && raise == 0.f)) {
+          floatx16 x;
 #pragma unroll
-      for (int b = 2; b >= 0; --b) {
-        bf16x8 kf[4];
-        read_keys(kat + half + b * kPlane, kf);
+          for (int v = 0; v < 16; ++v) x[v] = 0.f;
+          mx = scores(x);
 #pragma unroll
-        for (int j = 2 - b; j >= 0; --j)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) sc = mfma32(kf[s], qt[s][j], sc);
-      }
-      if (kt + 31 > r0) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = 8 * (v >> 2) + (v & 3) <= row - kt - 4 * lk ? sc[v] : -INFINITY;
-      }
-      if (kt < f0) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = 8 * (v >> 2) + (v & 3) >= lo - kt - 4 * lk ? sc[v] : -INFINITY;
-      }
-      float mx = sc[0];
-#pragma unroll
-      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[v]);
-      mx = pair_max(mx);
-      if (__builtin_amdgcn_ballot_w64(mx > raise)) {
-        const float d = mx > raise ? mx + kAbove : 0.f;
-        const float f = raise == 0.f ? __builtin_amdgcn_exp2f(-d * kScale) : 0.f;
-        if (mx > raise) raise = 0.f;
+          for (int v = 0; v < 16; ++v) sc[v] = up ? x[v] : sc[v];
+        }
+        const float next = up ? -(mx + kAbove) : nref[0];
+        const float f = !up ? 1.f : raise == 0.f ? __builtin_amdgcn_exp2f(fminf(next - nref[0], 0.f) * kScale) : 0.f;
+        if (up) raise = 0.f;
         l *= f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           o[0][v] *= f;
           o[1][v] *= f;
-          sc[v] -= d;
-          nref[v] -= d;
+          sc[v] += up ? next : 0.f;
+          nref[v] = next;
         }
       }
       bf16x8 pt[2][3];

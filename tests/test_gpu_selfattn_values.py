@@ -75,3 +75,53 @@ def test_attend8_large_values_behind_a_small_reference(n, heads, group, width, d
     some = sorted({0, n // 2, n - 1})
     model.store(num(k[some]), num(v[some]), tables[some], [0] * len(some))
     check_attend(cache, model, q[some], tables[some], at[:len(some)], got=got[some])
+
+
+@pytest.mark.parametrize("T,H,KV,n,dtype,offset", KINDS)
+@pytest.mark.parametrize("below", [1e4, 1e6, 1e8])
+def test_prompt_own_keys_far_below(T, H, KV, n, dtype, offset, below):
+    """A row's own tiles score -below, earlier keys around 0: those keep all weight, at their own scores' accuracy.  Of 64 products
+    one is what sets the near keys apart: the far keys' is a product with 0, and adds neither size nor error."""
+    q, k, v = slices(T, H, KV, dtype, offset)
+    g = torch.Generator("cuda").manual_seed(T)
+    for t in (q, k, v):
+        t.copy_(torch.randn(t.shape, device="cuda", generator=g))
+    starts = [T * i // n for i in range(n)] + [T]
+    q[:, :, 0], k[:, :, 0] = 256, 0
+    rows = []
+    for a, b in zip(starts, starts[1:]):
+        near = b - min(140, (b - a) // 2)                    # more than a block's own tiles of keys where the prompt is long
+        k[near:b, :, 0] = -below / 32
+        rows.append((a, near, b))
+    got = lib().prompt_attention(q, k, v, i32(starts))
+    for a, near, b in rows[:2] + rows[-1:]:
+        for i in {near, (near + b) // 2, b - 1}:
+            # the weights of the near keys, exp(-below / 2) at most, are zeros in 64 bits too
+            assert below / 2 > 800
+            want, spread, size = plain.seen_attention(num(q[i:i + 1]), num(k[a:near]), num(v[a:near]), np.ones((1, near - a), bool))
+            assert size.max() < 64
+            err = np.abs(num(got[i:i + 1]) - want)
+            assert (err <= bound(want, spread, size, near - a, dtype, dtype == BF16)).all(), (i, err.max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,heads,group,width", [(2, 2, 1, 28), (1, 1, 8, 200), (260, 4, 1, 8)])
+def test_attend8_first_keys_far_below(n, heads, group, width, dtype):
+    """The cache's positions are taken from the first on: those score far below, the last ones around 0."""
+    rng, rows, length = np.random.default_rng(width), 2, 16 * width
+    cache, model = lib().PagedCache8(n * width, heads), plain.PagedCache8(n * width, heads)
+    tables = random_tables(rng, n, width, n * width)
+    k, v = (torch.from_numpy(rng.standard_normal((n, length, heads, 64))).float().cuda() for _ in range(2))
+    k[..., 0] = 0
+    far = length - 48
+    k[:, :far, :, 0] = -2.0 ** 15                            # exact in 8 bits; what lies beside it in a page is rounded coarsely
+    cache.store(k, v, i32(tables), i32([0] * n))
+    q = torch.from_numpy(rng.standard_normal((n, rows, heads * group, 64))).to(dtype).cuda()
+    q[..., 0] = 256
+    got = cache.attend(q, i32(tables), i32([length - rows] * n))
+    model.store(num(k[:1]), num(v[:1]), tables[:1], [0])
+    kk, vv, _ = model.rows(tables[0], length)
+    sees = np.arange(far, length)[None] <= length - rows + np.arange(rows)[:, None]
+    want, spread, size = plain.seen_attention(num(q[0]), kk[far:], vv[far:], sees)
+    assert size.max() < 64
+    assert (np.abs(num(got[0]) - want) <= bound(want, spread, size, 48, dtype)).all()

@@ -306,11 +306,14 @@ __device__ __forceinline__ bf16x8 bf8(uint32_t lo, uint32_t hi, float s) {
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// The bytes of a word that are NaN codes, as 0xff each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t c) {
-  const uint32_t x = (c & 0x7f7f7f7fu) + 0x01010101u;  // bit 7 of a byte: its low seven bits are all ones
+// The bytes of a word whose codes stand for no finite value, as 0xff each: low seven bits from 0x80 less a byte of `step` on.  kNan:
+// NaN; kInfinite: codes from 256 on as well, which the largest scale, 2^120, takes past 32 bits' range.
+constexpr uint32_t kNan = 0x01010101u, kInfinite = 0x08080808u;
+__device__ __forceinline__ uint32_t odd_bytes(uint32_t c, uint32_t step) {
+  const uint32_t x = (c & 0x7f7f7f7fu) + step;
   return ((x & 0x80808080u) >> 7) * 255u;
 }
+__device__ __forceinline__ uint32_t negative_bytes(uint32_t c) { return ((c & 0x80808080u) >> 7) * 255u; }
 // The bytes of positions below `left` in the two words of eight positions.
 __device__ __forceinline__ void cut(uint32_t& lo, uint32_t& hi, int left) {
   lo &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << 8 * left) - 1;
@@ -349,6 +352,7 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
   const uint32_t vs = (kg >> 1 ? c.s[1] : c.s[0]) >> 8;
   const bool masked = p0 + 32 > low || c.there != 3;
   uint32_t odd = 0, hidden = 0;  // hidden: bit 4 t + i
+  const uint32_t step = vs == 247 ? kInfinite : kNan;
   if (masked) {  // uniform
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -362,7 +366,7 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) {
       cut(vw[dt][0], vw[dt][1], left);
-      odd |= nan_bytes(vw[dt][0]) | nan_bytes(vw[dt][1]);
+      odd |= odd_bytes(vw[dt][0], step) | odd_bytes(vw[dt][1], step);
     }
   }
   float mx = -INFINITY;
@@ -396,8 +400,8 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
       pb[4 + i] = __uint_as_float(y[1]);
     }
   };
-  // A NaN times a probability of 0 would reach the columns that do not see it: such values leave the
-  // product and are counted, for the columns that do, by a product of ones.
+  // A NaN or an infinity times a probability of 0 would reach the columns that do not see it: such values leave
+  // the product and are counted, for the columns that do, by two products of ones.
   if (__builtin_amdgcn_ballot_w64(odd != 0)) {
     floatx4 sees[2];
 #pragma unroll
@@ -410,14 +414,21 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
     split_terms<1>(pb, one);
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) {
-      const uint32_t n0 = nan_bytes(vw[dt][0]), n1 = nan_bytes(vw[dt][1]);
-      const bf16x8 x = bf8(n0 & 0x38383838u, n1 & 0x38383838u, 1.f);  // 0x38: the code of 1
-      const floatx4 z = mfma16(x, one[0], floatx4{0.f, 0.f, 0.f, 0.f});
+      uint32_t up[2], down[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (z[i] > 0.f) st.o[dt][i] = __uint_as_float(0x7fc00000u);
-      vw[dt][0] &= ~n0;
-      vw[dt][1] &= ~n1;
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t c = vw[dt][j], any = odd_bytes(c, step), nan = odd_bytes(c, kNan), neg = negative_bytes(c);
+        up[j] = (nan | (any & ~neg)) & 0x38383838u;  // 0x38: the code of 1
+        down[j] = (nan | (any & neg)) & 0x38383838u;
+        vw[dt][j] &= ~any;
+      }
+      const floatx4 z = mfma16(bf8(up[0], up[1], 1.f), one[0], floatx4{0.f, 0.f, 0.f, 0.f});
+      const floatx4 y = mfma16(bf8(down[0], down[1], 1.f), one[0], floatx4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (z[i] > 0.f) st.o[dt][i] += INFINITY;
+        if (y[i] > 0.f) st.o[dt][i] -= INFINITY;
+      }
     }
   }
   float pb[8];
@@ -439,8 +450,8 @@ __device__ __forceinline__ void kv8_rows(const Kv8AttendArgs& a, int r, int& pos
   pos = min(max(a.positions[r], -(1 << 20)), 16 * a.max_pages);
 }
 
-template <typename T, int NW>
-__global__ void __launch_bounds__(NW * 64) k_kv8_attend(Kv8AttendArgs a) {
+template <typename T, int NW>  // four waves a SIMD: 128 registers, where fp32 with eight waves took 129 and a block less (52 us for 60: 64 x 5 rows below)
+__global__ void __launch_bounds__(NW * 64, 4) k_kv8_attend(Kv8AttendArgs a) {
   // terms of a query value (exact) and of a probability: three of an fp32 call, of a bf16 one two, whose 2^-17 a result's
   // own rounding, 2^-9, covers
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;

@@ -125,3 +125,39 @@ def test_attend8_first_keys_far_below(n, heads, group, width, dtype):
     want, spread, size = plain.seen_attention(num(q[0]), kk[far:], vv[far:], sees)
     assert size.max() < 64
     assert (np.abs(num(got[0]) - want) <= bound(want, spread, size, 48, dtype)).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width,where", [(3, 16), (3, 32), (60, 896), (200, 3008)])
+def test_attend8_infinities_that_a_row_does_not_see(dtype, width, where):
+    """Values of 3.35e38, which the cache holds as infinity: rows before them are as without them, those from them on infinite of their
+    sign, NaN where a row sees both."""
+    rng, n, heads = np.random.default_rng(where), 3, 2
+    cache, model = lib().PagedCache8(n * width, heads), plain.PagedCache8(n * width, heads)
+    cache.data.fill_(0xff)
+    tables = random_tables(rng, n, width, n * width)
+    k, v = (torch.from_numpy(rng.standard_normal((n, where, heads, 64))).float().cuda() for _ in range(2))
+    cache.store(k, v, i32(tables), i32([0] * n))
+    model.store(num(k), num(v), tables, [0] * n)
+    q = torch.from_numpy(0.3 * rng.standard_normal((n, 7, 2 * heads, 64))).to(dtype).cuda()
+    at = [where - 3] * n
+    clean = cache.attend(q, i32(tables), i32(at), counts=i32([3] * n))
+    x, y = (torch.from_numpy(rng.standard_normal((n, 4, heads, 64))).float().cuda() for _ in range(2))
+    y[0, 0, 0, 7], y[0, 1, 1, 9], y[0, 2, 0, 7], y[0, 3, 0, 11] = 3.35e38, -3.35e38, -3.4e38, NAN     # of several rows and heads
+    y[1, 3] = 3.35e38                                                # the last row only
+    y[2, 2, :, :32] = 247 * 2.0 ** 120                               # the largest finite ones beside them
+    cache.store(x, y, i32(tables), i32([where] * n))
+    model.store(num(x), num(y), tables, [where] * n)
+    got = cache.attend(q, i32(tables), i32(at))
+    assert torch.equal(got[:, :3], clean[:, :3])
+    for r in range(n):
+        kk, vv, _ = model.rows(tables[r], where + 4)
+        vv = np.where(np.abs(vv) >= 2.0 ** 128, np.copysign(INF, vv), vv)
+        sees = np.arange(where + 4)[None] <= at[r] + np.arange(7)[:, None]
+        want, spread, size = plain.seen_attention(num(q[r]), kk, vv, sees)
+        g = num(got[r])
+        bad = ~np.isfinite(want)
+        assert np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[np.isinf(want)], want[np.isinf(want)])
+        assert bad.any() == (r < 2)
+        tol = bound(np.where(bad, 0, want), np.where(bad, 0, spread), size, where + 4, dtype)
+        assert (np.abs(np.where(bad, 0, g) - np.where(bad, 0, want)) <= tol).all()

@@ -255,9 +255,10 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // positions) x NW waves; a wave takes steps of 32 positions (two pages), every NW-th.
 //   scores   S^T = K q^T per page (v_mfma_f32_16x16x32_bf16): lane 16 kg + n gets column n of
 //            positions 4 kg .. + 3
-//   softmax  per column a reference, kAbove above the maximum that set it, which moves where a score passes it (as every
-//            time a maximum moves, most steps of a short context rescaled), and the sum: probabilities are at most 1, so
-//            that sums of them times n values of up to 3.4e38 / n stay finite
+//   softmax  per column a reference, which moves up to the maximum where a score passes it by kRaise (as every
+//            time a maximum moves, most steps of a short context rescaled), in steps with values above 448 where a score
+//            passes it at all: such values meet probabilities of at most 1, so that n of up to 3.4e38 / n have finite
+//            sums; and the sum
 //   values   O^T = V^T P^T per step: two lane swaps turn its two score tiles into the operand
 //            (lane: column n, positions 8 kg .. + 7)
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (reference, l, O) record for the
@@ -270,7 +271,7 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 // registers: four x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to 4,000 56 for 41.
 namespace {
 constexpr float kScale = 0.125f * 1.44269504088896f;  // exp(s / 8) = 2^(kScale s)
-constexpr float kAbove = 8.f / kScale;
+constexpr float kRaise = 8.f / kScale;
 constexpr int kRecord = 32 + 16 * 64;  // reference [16], sum [16], O [16][64]
 
 __device__ __forceinline__ float no_inf(float m) { return m == -INFINITY ? 0.f : m; }
@@ -374,8 +375,9 @@ __device__ __forceinline__ void kv8_step(Step& c, int p0, int lim, int low, int 
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][i]);
-  if (__builtin_amdgcn_ballot_w64(mx > st.m)) {
-    const float top = swap_max(mx), m = top > st.m ? top + kAbove : st.m, f = exp_to(st.m, no_inf(m));  // 0 at first
+  const float above = (c.s[0] | c.s[1]) & 0x8000u ? 0.f : kRaise;  // a value scale of 2 or more
+  if (__builtin_amdgcn_ballot_w64(mx - st.m > above)) {
+    const float top = swap_max(mx), m = top - st.m > above ? top : st.m, f = exp_to(st.m, no_inf(m));  // 0 at first
     st.m = m;
     st.l *= f;
 #pragma unroll

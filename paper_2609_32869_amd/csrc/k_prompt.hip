@@ -19,9 +19,9 @@ namespace wf {
 
 namespace {
 constexpr float kScale = 0.125f * 1.44269504088896340736f;  // exp(s / 8) = 2^(kScale s)
-// References of probabilities p = 2^(kScale (s - reference)) lie this far above the largest score that sets them, so p is 2^-8 there
-// and at most 1 where a later score passes it by less (it then moves up): a sum of p times n values of up to 3.4e38 / n stays finite.
-constexpr float kAbove = 8.f / kScale;
+// The reference of a row's probabilities p = 2^(kScale (s - reference)) moves where a score passes its old maximum by this, so that p
+// would reach 2^8.  p or the values are taken 2^-8 of themselves: n values of up to 3.4e38 / n have finite sums.
+constexpr float kRaise = 8.f / kScale;
 
 __device__ __forceinline__ float pair_max(float v) {  // over the two half-waves
   const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -264,8 +264,8 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
     float mx = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    const float mn = fmaxf(m, pair_max(mx)), top = mn == -INFINITY ? 0.f : mn, base = top + kAbove;
-    const float f = __builtin_amdgcn_exp2f((m - top) * kScale);
+    const float mn = fmaxf(m, pair_max(mx)), base = mn == -INFINITY ? 0.f : mn;
+    const float f = __builtin_amdgcn_exp2f((m - base) * kScale);
     m = mn;
     l *= f;
 #pragma unroll
@@ -522,8 +522,8 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   const int w0 = __builtin_amdgcn_readlane(first, 0), f0 = __builtin_amdgcn_readlane(first, 32 * NQ - 1);
   const int nt = (e - min(k0, e) + kTile - 1) / kTile;
   // Scores are formed less a reference of their row (the products' accumulators start at its negative, `nref`), so p =
-  // 2^(kScale s).  It lies kAbove above the maximum of the first tile with a score above -inf, then moves only when a
-  // score passes it: p stays below 1.  raise: -inf before, 0 from then on
+  // 2^(kScale s).  It lies kRaise above the maximum of the first tile with a score above -inf, then moves only when a
+  // score passes it: p stays below 1 (its exponent's rounding, 2^-21, is far below p's own).  raise: -inf before, 0 from then on
   float raise[NQ], l[NQ];
   constexpr int NR = WAVES == 4 ? 1 : 16;  // at four waves a SIMD the reference is subtracted instead, for sixteen registers
   float nref[NQ][NR];
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
 #pragma unroll
               for (int v = 0; v < 16; ++v) sc[u][kb][v] = up ? x[kb][v] : sc[u][kb][v];
           }
-          const float next = up ? -(mx + kAbove) : nref[u][0];
+          const float next = up ? -(mx + kRaise) : nref[u][0];
           const float f = !up ? 1.f : raise[u] == 0.f ? __builtin_amdgcn_exp2f(fminf(next - nref[u][0], 0.f) * kScale) : 0.f;  // no score yet: l and o are 0
           if (up) raise[u] = 0.f;
           l[u] *= f;
@@ -789,6 +789,8 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
       for (int j = 0; j < 8; ++j) vx[j] = finite(vx[j]) ? vx[j] : 0.f;
       if (lane == 0) odd[2 * g + (i & 1)] = i;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vx[j] *= 0x1p-8f;
     char* to = reinterpret_cast<char*>(stages) + (i & 1) * kStage3;
     bf16x8 k3[3], v3[3];
     terms8<3>(kx, k3);
@@ -807,7 +809,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
   bf16x8 qt[4][3];
 #pragma unroll
   for (int s = 0; s < 4; ++s) terms8<3>(q[s], qt[s]);
-  float raise = -INFINITY, l = 0.f;  // as in k_prompt16
+  float raise = -INFINITY, l = 0.f;  // as in k_prompt16, but for a reference at the maximum: raise is kRaise from the first on
   floatx16 nref, o[2];
 #pragma unroll
   for (int v = 0; v < 16; ++v) nref[v] = o[0][v] = o[1][v] = 0.f;
@@ -850,7 +852,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
       float mx = scores(sc);
       const bool up = mx > raise;
       if (__builtin_amdgcn_ballot_w64(up)) {
-        if (__builtin_amdgcn_ballot_w64(up && raise == 0.f)) {
+        if (__builtin_amdgcn_ballot_w64(up && raise > 0.f)) {
           floatx16 x;
 #pragma unroll
           for (int v = 0; v < 16; ++v) x[v] = 0.f;
@@ -858,9 +860,9 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
 #pragma unroll
           for (int v = 0; v < 16; ++v) sc[v] = up ? x[v] : sc[v];
         }
-        const float next = up ? -(mx + kAbove) : nref[0];
-        const float f = !up ? 1.f : raise == 0.f ? __builtin_amdgcn_exp2f(fminf(next - nref[0], 0.f) * kScale) : 0.f;
-        if (up) raise = 0.f;
+        const float next = up ? -mx : nref[0];
+        const float f = !up ? 1.f : raise > 0.f ? __builtin_amdgcn_exp2f(fminf(next - nref[0], 0.f) * kScale) : 0.f;
+        if (up) raise = kRaise;
         l *= f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -909,8 +911,8 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
     if (more) stage(i + 1);
     __syncthreads();
   }
-  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise == 0.f ? -nref[0] : -INFINITY, l, o)) return;
-  const float total = pair_sum(l), inv = total == 0.f ? 0.f : 1.f / total;
+  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise > 0.f ? -nref[0] : -INFINITY, l, o)) return;
+  const float total = pair_sum(l), inv = total == 0.f ? 0.f : 256.f / total;
   if (r0 + lr >= a.tokens || (!a.clear && (row < near.begin || row >= near.end))) return;
   float* op = reinterpret_cast<float*>(a.out) + ((size_t)row * a.heads + head) * kHeadDim + 4 * lk;
 #pragma unroll

@@ -161,3 +161,27 @@ def test_attend8_infinities_that_a_row_does_not_see(dtype, width, where):
         assert bad.any() == (r < 2)
         tol = bound(np.where(bad, 0, want), np.where(bad, 0, spread), size, where + 4, dtype)
         assert (np.abs(np.where(bad, 0, g) - np.where(bad, 0, want)) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [1, 70])
+def test_attend8_probabilities_are_exact_in_the_products(dtype, width):
+    """Two positions of scores d and 0 and of values 6 and -6: 6 (1 - p) / (1 + p) with p = exp(-d), which for a small d is what
+    the last bits of p leave.  The scores are exact; p is off by 2^-23 for its exponential and 2^-23 for the rounding of d log2(e)
+    and of its factor, the result by 3 times that (12 p / (1 + p)^2 <= 3), and by at most six roundings to 2^-24 of 6: under 2^-18,
+    then half a step of the type.  (Two bf16 terms leave up to 2^-16 of p: 2^-14.4.)"""
+    d = 2.0 ** torch.arange(-13, 1, 0.125, dtype=torch.float64)
+    n = len(d)
+    q = torch.zeros((n, 1, 1, 64), device="cuda", dtype=dtype)
+    q[:, 0, 0, 0] = (8 * d).to(q)
+    k, v = torch.zeros((1, 2, 1, 64), device="cuda"), torch.full((1, 2, 1, 64), 6.0, device="cuda")
+    k[0, 0, 0, 0] = 1
+    v[0, 1] = -6
+    cache = lib().PagedCache8(width, 1)
+    table = i32([list(range(width))])
+    cache.store(k, v, table, i32([0]))
+    got = num(cache.attend(q, table.expand(n, width), i32([1] * n)))[:, 0, 0]
+    p = np.exp(-num(q)[:, 0, 0, :1] / 8)
+    want = 6 * (1 - p) / (1 + p)
+    tol = 2.0 ** -18 + torch.finfo(dtype).eps / 2 * want
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()

@@ -708,7 +708,7 @@ __device__ __forceinline__ void op_apply(const OprojArgs& op, int head, int g, i
 //   output       waves summed in LDS; one chunk: O / l, else the chunk's
 //                (max, l, O) record for the merge kernel.
 
-// v = hi + lo: hi truncated to bf16, lo = RNE(v - hi) (2^-17 relative)
+// v = hi + lo: hi truncated to bf16, lo = RNE(v - hi) (2^-16 relative)
 __device__ __forceinline__ void split_planes(const float* v, bf16x8& hi, bf16x8& lo) {
   uint4 h, l;
   split2x8(v, h, l);

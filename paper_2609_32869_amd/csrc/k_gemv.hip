@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(NW * 64) k_gemv16k(GemvArgs a) {
 // ---------------------------------------------------------------- bf16 GEMM (batch >= 2)
 // The rows of several slots (nine each) times W^T in tiles of 64 rows x 64 columns whose
 // four waves split k (split_tile, wf_tile.h).  The operand holds each value as two bf16
-// planes (hi + lo, 2^-17 relative), both multiplied into one accumulator, so the product
+// planes (hi + lo, 2^-16 relative), both multiplied into one accumulator, so the product
 // is accurate to fp32 rounding.  Grid y splits the k-steps (EPI_PART stores each split's
 // partial sums, EPI_ACC adds them to y).
 // Bound by the first, cold reads of the weights with few rows (a step reads 1.4 GB of

@@ -256,9 +256,9 @@ void kv4_unpack(const Kv4UnpackArgs& a, hipStream_t st) {
 //            the merge kernel
 
 // bf16 terms of a query value and of a probability: as many as hold it exactly (an fp32 query three, a bf16 one one,
-// a probability three).  Two terms of a probability, 2^-17 of it, are a tenth faster with bf16 rows (16 x 5 rows of ragged
+// a probability three).  Two terms of a probability, 2^-16 of it, are a tenth faster with bf16 rows (16 x 5 rows of ragged
 // memories 10.7 us against 11.7) and round 0.24% of the bf16 outputs to the other side of 64 bits, three 0.017%, as sums
-// in 32 bits do.  A decoder step's operands hold an fp32 value to 2^-17 themselves: two terms of each.
+// in 32 bits do.  A decoder step's operands hold an fp32 value to 2^-16 themselves: two terms of each.
 enum { KV4_ROWS = 0, KV4_OPERAND = 1, KV4_RECORDS = 2 };
 template <typename T, int OUT>
 struct Terms {

@@ -9,7 +9,7 @@
 // the cache, so the parts of one prompt can share the pass.
 //
 // Operands are P bf16 planes in 16-row fragment order (wf_common.h): P = 3 (hi, mid,
-// lo: the exact fp32 value) for handles of one slot and P = 2 (hi, lo: 2^-17) for
+// lo: the exact fp32 value) for handles of one slot and P = 2 (hi, lo: 2^-16) for
 // several, as in the step.
 #include <algorithm>
 

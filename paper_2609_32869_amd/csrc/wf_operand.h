@@ -19,7 +19,7 @@ __device__ __forceinline__ size_t op_index(const Operand& o, int m, int k) {
 // row, R9 + row, 2 R9 + row.  nsplit = 2 (several slots, 16-row fragment order):
 // hi (v truncated to bf16) in the operand and lo = RNE(v - hi) at the same place
 // of a second plane right after it (mt * 16 * ld elements on), so hi + lo
-// equals v to 2^-17 relative and the two products share one accumulator.
+// equals v to 2^-16 relative and the two products share one accumulator.
 // Otherwise the value rounded to the storage type.
 __device__ __forceinline__ void put_operand(const Operand& o, int, int, int row, int col, float v, float) {
   reinterpret_cast<float*>(o.p)[op_index(o, row, col)] = v;
@@ -51,7 +51,7 @@ __device__ __forceinline__ void put_op(const Operand& o, int nsplit, int R9, int
 __device__ __forceinline__ uint4 pack8_bits(const uint32_t* h) {
   return make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
 }
-// v = hi + lo to 2^-17: hi truncated to bf16, lo the remainder rounded.
+// v = hi + lo to 2^-16: hi truncated to bf16, lo the remainder rounded.
 __device__ __forceinline__ void split2x8(const float* v, uint4& hi, uint4& lo) {
   uint32_t h[4], l[4];
 #pragma unroll

@@ -456,7 +456,8 @@ __global__ void __launch_bounds__(NW * 64, 4) k_kv8_attend(Kv8AttendArgs a) {
   // bf16 terms of a query value and of a probability: as many as hold it exactly.  Two terms of a probability, 2^-16 of it, would
   // save a bf16 call 2% (96 x 9 rows at 0 to 438, 22.4 us for 22.9) to 9% (185 x 29, 177 for 193)
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
-  __shared__ float wm[NW][16], wl[NW][16], wo[NW][16][68];
+  __shared__ float wm[NW][16], wl[NW][16];
+  __shared__ alignas(16) float wo[NW][16][68];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
   const int cols = a.rows * a.group, cap = 16 * a.max_pages, tiles = (cols + 15) >> 4;
   int chunk = quotient(blockIdx.x, a.c.n_head), head = blockIdx.x - chunk * a.c.n_head, r = blockIdx.y, tile = blockIdx.z;
@@ -581,7 +582,8 @@ __global__ void __launch_bounds__(NW * 64, 4) k_kv8_attend(Kv8AttendArgs a) {
 // Joins the chunks of one column: 16 threads (4 dims each) take every sixteenth chunk and meet in LDS.
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
-  __shared__ float wm[16], wl[16], wo[16][64];
+  __shared__ float wm[16], wl[16];
+  __shared__ alignas(16) float wo[16][64];
   const int cols = a.rows * a.group, tiles = (cols + 15) >> 4;
   const int head = blockIdx.x, r = blockIdx.y, c = blockIdx.z, tile = c >> 4, i = c & 15;
   const int t = threadIdx.x, q = t >> 4, d = 4 * (t & 15);

@@ -191,7 +191,8 @@ __device__ __forceinline__ floatx16 product(const bf16x8 (&a)[N], const bf16x8 (
 template <typename T>
 __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
   constexpr int N = sizeof(T) == 4 ? 3 : 1;
-  __shared__ float wm[4][32], wl[4][32], wo[4][32][68];
+  __shared__ float wm[4][32], wl[4][32];
+  __shared__ alignas(16) float wo[4][32][68];
   int head, tile;
   if (!block_of(grid, head, tile)) return;
   const int q0 = tile * 32;
@@ -371,6 +372,11 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kTile = 64, kStage = 1024;  // keys of a tile; 16-byte chunks of a stage
+// LDS stages.  Reads form their addresses by xor within a row's 128 bytes, so a row starts on a border of as many.
+template <int CHUNKS>
+struct alignas(128) Stages {
+  uint4 chunk[CHUNKS];
+};
 // A stage: chunk c (8 dims) of key r at 8 r + (c ^ (r & 7)), then of its values at 8 r + (c ^ 2 (r & 3)): the four rows that sixteen
 // lanes read two chunks of by ds_read_b64_tr_b16 then lie in different banks (as the keys lie, two and two shared them).
 // lgkmcnt 0 and vmcnt the copies of the tiles behind the next, four each
@@ -478,13 +484,14 @@ __device__ __forceinline__ void prompt_copy(const bf16* K, const bf16* V, const 
 
 template <int NQ, int KB, int WAVES, int G, int NS>
 __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid grid) {
-  __shared__ uint4 shared_stages[G * NS * kStage];
+  __shared__ Stages<G * NS * kStage> shared;
+  static_assert(alignof(decltype(shared)) % 128 == 0, "reads xor addresses up to 127");
   int head, tile;
   if (!block_of(grid, head, tile)) return;
   const int q0 = tile * 128 * NQ;
   const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
-  uint4* const stages = shared_stages + g * NS * kStage;
+  uint4* const stages = shared.chunk + g * NS * kStage;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head * a.qh;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (head / a.group) * a.kh;
   const bf16* V = reinterpret_cast<const bf16*>(a.v) + (head / a.group) * a.vh;
@@ -722,7 +729,7 @@ __global__ void __launch_bounds__(256 * G, WAVES) k_prompt16(PromptArgs a, Grid 
   if constexpr (G == 2) {
     static_assert(NQ == 1, "one tile of rows a wave");
     __syncthreads();
-    if (!join(g, w, reinterpret_cast<float*>(shared_stages), raise[0] == 0.f ? -nref[0][0] : -INFINITY, l[0], o[0])) return;
+    if (!join(g, w, reinterpret_cast<float*>(shared.chunk), raise[0] == 0.f ? -nref[0][0] : -INFINITY, l[0], o[0])) return;
   }
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
@@ -756,14 +763,15 @@ static void prompt16(const PromptArgs& a, hipStream_t st) {
 constexpr int kPlane = 4096, kStage3 = 6 * kPlane;
 template <int G>
 __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid) {
-  __shared__ uint4 shared_stages[G * 2 * kStage3 / 16];
+  __shared__ Stages<G * 2 * kStage3 / 16> shared;
+  static_assert(alignof(decltype(shared)) % 128 == 0, "reads xor addresses up to 127");
   __shared__ int window[kWindow], odd[8];  // odd: the last tile of a group's stage that held a NaN or an infinity
   int head, tile;
   if (!block_of(grid, head, tile)) return;
   const int q0 = tile * 128;
   const int w = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3), g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int lane = threadIdx.x & 63, lr = lane & 31, lk = lane >> 5;
-  uint4* const stages = shared_stages + g * 2 * kStage3 / 16;
+  uint4* const stages = shared.chunk + g * 2 * kStage3 / 16;
   const int e = min(q0 + 128, a.tokens), r0 = q0 + w * 32, row = min(r0 + lr, a.tokens - 1);
   const float* Q = reinterpret_cast<const float*>(a.q) + row * a.qt + head * a.qh + 8 * lk;
   const float* V = reinterpret_cast<const float*>(a.v) + (head / a.group) * a.vh;
@@ -911,7 +919,7 @@ __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid)
     if (more) stage(i + 1);
     __syncthreads();
   }
-  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared_stages), raise > 0.f ? -nref[0] : -INFINITY, l, o)) return;
+  if (G == 2 && !join(g, w, reinterpret_cast<float*>(shared.chunk), raise > 0.f ? -nref[0] : -INFINITY, l, o)) return;
   const float total = pair_sum(l), inv = total == 0.f ? 0.f : 256.f / total;
   if (r0 + lr >= a.tokens || (!a.clear && (row < near.begin || row >= near.end))) return;
   float* op = reinterpret_cast<float*>(a.out) + ((size_t)row * a.heads + head) * kHeadDim + 4 * lk;

@@ -536,8 +536,9 @@ int wf_rotary(const double* turns, int dims, int interleaved, float amplitude, i
  *   inside counts; borders that decrease give results without meaning, read inside the tensors).
  * out: device [tokens, n_head, 64] in the same type.  Rows of no sequence are set to zero
  *   (clear != 0) or left as they are.  An out that lies within the extent of q, k or v is refused.
- * fp32: products in 32 bits; bf16: the probabilities are rounded to bf16 for their product, sums
- * are fp32.  Values times probabilities, each at most 1, are summed before the division by the
+ * fp32: operands enter the products as the three bf16 terms that hold them; what the products leave out is
+ * below 2^-22 of their magnitudes' sum.  bf16: the probabilities are rounded to bf16 for their product.
+ * All sums are fp32.  Values times probabilities, each at most 1, are summed before the division by the
  * probabilities' sum: values of up to 3.4e38 / n give finite sums over n keys, larger ones may not.
  * An infinity in a row's query or in a key that it sees can make its result NaN; a row all of whose
  * scores are -inf gets zeros.
@@ -558,7 +559,7 @@ int wf_prompt_attend(const void* q, const int64_t* q_stride, const void* k, cons
  * page that keeps them while rows are appended to it.
  * data: device, 16-byte aligned, n_pages records of wf_kv8_page_bytes(n_head) bytes (a multiple
  * of 16) one after the other, in an order of the library's own: a page may be copied as bytes
- * (wf_cache_reorder, page_tokens 16).
+ * (wf_cache_reorder, page_tokens 16, which takes caches of up to 2^18 pages).
  * 1 <= n_pages <= 2^24, 1 <= n_head <= 4096.
  */
 typedef struct wf_kv8 {

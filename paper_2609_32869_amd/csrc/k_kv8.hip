@@ -87,9 +87,10 @@ __device__ __forceinline__ int value_code(int lane, int j) {
 
 // ---------------------------------------------------------------- store
 // A wave per (page that a request writes, head): the page's scale is the maximum of 1,024 elements, so a wave holds it whole
-// and reads and writes it once.  Bytes bound it: 8 x 8,192 rows of 8 heads, fp32, 335 MB in 65 us (5.1 TB/s, a large copy's
-// rate); one page a request (96 x 20 waves): 5 us of a first and a second trip to memory.  Where a request's pages lie in the grid: request r's first page has
-// number starts[r] / 16 + 2 r (packed), which leaves room for every page that its rows can touch, or r * per (padded).
+// and reads and writes it once.  Bytes bound it: 8 x 8,192 rows of 8 heads, fp32, 335 MB, in 64 us store after store (5.2 TB/s, a
+// large copy's rate), 95 behind a load that has just written 537 MB.  Nine rows of each of 96 requests, 20 heads, 9.4 us (10.9 behind
+// a load): positions, page numbers, kept codes, scales, one trip to memory after the other.  Where a request's pages lie in the
+// grid: request r's first page has number starts[r] / 16 + 2 r (packed), which leaves room for every page that its rows can touch, or r * per (padded).
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_store(Kv8StoreArgs a, int per, int hb) {
   // neighbouring blocks take neighbouring heads of one page, whose rows lie beside each other; by grid y where there are too many
@@ -204,8 +205,8 @@ __device__ __forceinline__ void st4(float* p, const float* x) { *reinterpret_cas
 __device__ __forceinline__ void st4(bf16* p, const float* x) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
 }
-// A wave per (request, column of its table, head).  Bytes bound it: 8 x 8,192 positions of 8 heads into fp32 604 MB, 95 us
-// (6.4 TB/s, nine tenths of them writes).
+// A wave per (request, column of its table, head).  Bytes bound it: 8 x 8,192 positions of 8 heads into fp32 604 MB, 99 us
+// (6.1 TB/s, nine tenths of them writes).
 template <typename T>
 __global__ void __launch_bounds__(256) k_kv8_load(Kv8LoadArgs a) {
   const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
@@ -264,11 +265,12 @@ void kv8_load(const Kv8LoadArgs& a, hipStream_t st) {
 //   output   waves joined in LDS; one chunk: O / l, else the chunk's (reference, l, O) record for the
 //            merge kernel
 // A step's codes, scales and page numbers are loaded while the one before is multiplied.  Bytes bound long contexts: four
-// requests of one row at 131,071, 8 heads of four each, 538 MB in 95 to 100 us (5.4 TB/s; the merge 5 us more).  Vector
-// instructions bound many rows: 185 x 29 at 0 to 2,069, 32 heads over 8, 175 us, 135 of them a step of 12 products.  Of many
-// short ones, 96 x 9 rows at 0 to 438, 20 heads (16.7 us, the bytes 12), the start and end of 1,920 blocks are the rest.  Two
+// requests of one row at 131,071, 8 heads of four each, 538 MB in 99 us (5.4 TB/s; the merge 5 us more).  Vector
+// instructions bound many rows, whose every 16 columns turn the codes into values anew: 185 x 29 at 0 to 2,069, 32 heads over 8, 186 us.
+// Of many short ones, 96 x 9 rows at 0 to 438, 20 heads (17.0 us, the bytes 12), the start and end of 1,920 blocks are the rest.  Two
 // tiles of 16 columns to a block would share the conversion of their keys and values, but leave half the blocks and 156
-// registers: four x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to 4,000 56 for 41.
+// registers: with probabilities in two terms four x nine rows from 65,536 on, 32 heads over 8, 190 us for 143, 32 x nine at 0 to
+// 4,000 56 for 41.
 namespace {
 constexpr float kScale = 0.125f * 1.44269504088896f;  // exp(s / 8) = 2^(kScale s)
 constexpr float kRaise = 8.f / kScale;
@@ -454,7 +456,7 @@ __device__ __forceinline__ void kv8_rows(const Kv8AttendArgs& a, int r, int& pos
 template <typename T, int NW>  // four waves a SIMD: 128 registers, where fp32 with eight waves took 129 and a block less (52 us for 60: 64 x 5 rows below)
 __global__ void __launch_bounds__(NW * 64, 4) k_kv8_attend(Kv8AttendArgs a) {
   // bf16 terms of a query value and of a probability: as many as hold it exactly.  Two terms of a probability, 2^-16 of it, would
-  // save a bf16 call 2% (96 x 9 rows at 0 to 438, 22.4 us for 22.9) to 9% (185 x 29, 177 for 193)
+  // save a bf16 call 2% (96 x 9 rows at 0 to 438, 22.4 us a replay for 22.9) to 9% (185 x 29, 177 for 193)
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
   __shared__ float wm[NW][16], wl[NW][16];
   __shared__ alignas(16) float wo[NW][16][68];
@@ -624,7 +626,9 @@ __global__ void __launch_bounds__(256) k_kv8_merge(Kv8AttendArgs a) {
 }
 
 // Waves of a block: fewer where the positions are few and the blocks many, whose start and end then weigh more than a wave's
-// steps.  us a replayed call, bf16:
+// steps.  The table's width stands for the positions, which are not known here: of contexts far below it a call takes up to a
+// fifth more (64 rows at 0 to 500, 32 heads over 8, table of 2,048 pages 19.4 us, of 32 17.3).  us a call of a graph of one, replayed
+// again and again (some 5 us more than among a stream's other calls), bf16, probabilities in two terms:
 //   one wave / four   256 requests of one row at 0 to 64, 20 heads, 15.6 / 22.4, of nine at 0 to 100, 32 heads over 8, 22.7 / 30.3
 //   four / eight      20 heads: 96 of nine rows at 0 to 438 21.7 / 24.5, 256 of one at 0 to 447 36 / 47; 32 over 8: 185 of 29 at 0 to
 //                     2,069 175 / 201; but 64 of one at 4,000, 20 heads, 127 / 118, 256 of one at 0 to 4,000 252 / 239
@@ -645,7 +649,7 @@ size_t kv8_workspace(int n, int rows, int group, int n_head, int max_pages) {
 template <typename T>
 static void attend_launch(Kv8AttendArgs& a, hipStream_t st) {
   // The tiles of the same keys and values one behind the other on one XCD (every eighth block), the later ones then read them
-  // from its L2.  us a replayed call, tiles by grid z / so: four x nine rows from 65,536 on, 32 heads over 8, 217 / 143; one x 17
+  // from its L2.  us a replayed call, probabilities in two terms, tiles by grid z / so: four x nine rows from 65,536 on, 32 heads over 8, 217 / 143; one x 17
   // at 130,000, 20 heads, 124 / 91; 64 x five at 0 to 4,000, 32 over 8, 59 / 51; but 64 x 17 at 0 to 600, 20 heads, 30.6 / 32.2.
   const int cols = a.rows * a.group, tiles = (cols + 15) / 16;
   const long long units = (long long)a.n * a.nchunk * a.c.n_head, x = (units + 7) / 8 * 8 * tiles;

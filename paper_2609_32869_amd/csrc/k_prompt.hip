@@ -186,8 +186,8 @@ __device__ __forceinline__ floatx16 product(const bf16x8 (&a)[N], const bf16x8 (
 //   S^T = K q^T  a lane gets keys 8 (v / 4) + 4 (lane / 32) + v % 4 of row lane % 32
 //   O^T += V^T P^T  the half-waves' eight values of an instruction are taken as those keys, so the probabilities
 //                are the operand as they are, and a lane's values are V[those keys][lane % 32 + 32 d]
-// The next tile's keys are loaded once this one's are multiplied, the values likewise.  One prompt of 224 rows, 20 heads: 10.4 us
-// a call, of which 7.9 the caller's; the way of a block's first loads, its two tiles and the joining bounds it.
+// The next tile's keys are loaded once this one's are multiplied, the values likewise.  One prompt of 224 rows, 20 heads: 10.5 us
+// a call among others, 8.0 of the host; the way of a block's first loads, its two tiles and the joining bounds it.
 template <typename T>
 __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
   constexpr int N = sizeof(T) == 4 ? 3 : 1;
@@ -363,11 +363,13 @@ __global__ void __launch_bounds__(256, 2) k_prompt32(PromptArgs a, Grid grid) {
 // (global_load_lds_dwordx4) NS - 1 tiles ahead of their use.  KB x 32 keys at a time a wave forms S^T = K q^T on
 // v_mfma_f32_32x32x16_bf16, so a lane holds 16 of 32 keys of one row (keys 8 (v / 4) + 4 (lane / 32) + v % 4):
 // reference and sum are per lane (one swap of half-waves joins a row's two lanes) and the probabilities, rounded to
-// bf16 in place (2^-9 of each, as the results' own rounding), are the B operand of O^T += V^T P^T if the half-waves'
+// bf16 in place (2^-9 of each, as the results' own rounding: an error of 0.0019 of the 2-norm where that alone leaves 0.0014;
+// two terms of each would take 43% more time, 6.8 ms for 4.8 of 32,768 rows of 32 heads, 14% more for 96 short prompts),
+// are the B operand of O^T += V^T P^T if the half-waves'
 // eight values of an instruction are taken as those keys.  The A operand then is, for a dim, keys 4 and 4 together,
 // what ds_read_b64_tr_b16 makes of rows as they lie in memory.  The sum is taken of the rounded probabilities.
 // 32,768 rows, 32 heads over 8: 4.7 to 5.3 ms by the card, whose clock falls under this load, 940 to 830 TFLOP/s, 78 to 72%
-// of what a library's large product reaches on it; 96 prompts of 1 to 447 rows, 20 heads: 71 us, where the bytes alone are
+// of what a library's large product reaches on it; 96 prompts of 1 to 447 rows, 20 heads: 73 us, where the bytes alone are
 // 43.  Raising the waves' priority, around the products or of every other wave, changes nothing.
 namespace {
 typedef __attribute__((address_space(3))) void lds_void;
@@ -759,7 +761,7 @@ static void prompt16(const PromptArgs& a, hipStream_t st) {
 // write them to one of two LDS stages while the other is multiplied; the next tile's loads are under way
 // meanwhile.  A stage holds six planes of 32 rows of 64 dims (keys' terms, values' terms) in k_prompt16's order.  Products as in
 // k_prompt32 (six a pair of operands, a plane at a time, the smallest first), softmax as in k_prompt16.  32,768 rows, 32
-// heads: 22.6 ms, 195 TFLOP/s, where a library's fp32 product reaches 152; 9,001 rows of five prompts, 12 heads: 218 us.
+// heads: 22.9 ms, 192 TFLOP/s, where a library's fp32 product reaches 152; 9,001 rows of five prompts, 12 heads: 229 us.
 constexpr int kPlane = 4096, kStage3 = 6 * kPlane;
 template <int G>
 __global__ void __launch_bounds__(256 * G, 2) k_prompt3(PromptArgs a, Grid grid) {
@@ -945,11 +947,13 @@ static void prompt3(const PromptArgs& a, hipStream_t st) {
 
 // By the blocks of 128 rows and the mean length, whose causes are: few blocks leave compute units waiting for the longest, and
 // then a block's own tiles one after the other are the call's time; many keep all busy, and then what a row costs counts.
-// us a replayed call (sequences x rows x heads), bf16:
+// us a call of a graph of one, replayed again and again (small ones take 4 to 8 us more so than among a stream's other calls;
+// sequences x rows x heads), bf16:
 //   few blocks of long sequences: two groups of waves share a block's keys, 64 keys at a time (2,048 x 20: 32; one group 42;
 //     2 x 4,000 x 8: 68 / 92; but 10 x 512 x 14: 37 / 28)
 //   up to some more: two groups of 32 keys at a time and four waves a SIMD (4 x 4,200 x 8, 1,056 blocks: 126, one group 163; 4 x
-//     1,813 x 20: 61 / 69; 6 x 8,533 x 8: 687 / 707; but 9 x 1,896 x 24, 3,200 blocks: 176 / 166; 10,294 x 24: 422 / 414)
+//     1,813 x 20: 61 / 69; 6 x 8,533 x 8: 687 / 707; but 9 x 1,896 x 24, 3,200 blocks: 176 / 166; one sequence, 810 blocks of
+//     10,294 x 10: 206 / 224, 1,024 of 4,096 x 32: 104 / 105, but 1,944 of 10,294 x 24: 422 / 414)
 //   very many of very long sequences: 256 rows a block, half the reads from LDS (32,768 x 32: 4,690 / 4,860; but 16,384 x 6:
 //     446 / 277)
 //   others: one group, 32 keys at a time, four waves a SIMD (96 of 224 x 20: 62; 64 keys and two waves 84)
@@ -964,7 +968,8 @@ void prompt_attend(const PromptArgs& a, hipStream_t st) {
     if (shared) return prompt3<2>(a, st);
     return prompt3<1>(a, st);
   }
-  // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets
+  // k_prompt16 reads 16 bytes at a time, 64 rows by 32-bit offsets; rows off a 16-byte border take single elements and 32-row blocks
+  // (8,192 x 12: 813 us for 166, 96 of 224 x 20: 322 / 59, 224 x 20: 16.7 / 16.1)
   if (!a.vec || std::max(a.kt, a.vt) > 1 << 24) return prompt32<bf16>(a, st);
   if (shared) return prompt16<1, 2, 2, 2, 2>(a, st);
   if (mean >= 16384 && blocks >= 4096) return prompt16<2, 1, 2, 1, 3>(a, st);

@@ -521,8 +521,8 @@ def prompt_attention(q, k, v, starts, out=None, stream=None):
 
 class PagedCache8:
     """Self-attention keys and values in 8 bits (wf_kv8): `layers` layers of `pages` pages of 16 positions of n_head heads of
-    64.  data: uint8 [layers, pages, bytes of a page], what cache_reorder takes as its cache; requests' page numbers lie in
-    tables, int32 [n, max_pages] (rows of any stride), the same for every layer."""
+    64.  data: uint8 [layers, pages, bytes of a page], what cache_reorder takes as its cache (up to 2^18 pages); requests' page
+    numbers lie in tables, int32 [n, max_pages] (rows of any stride), the same for every layer."""
 
     PAGE = 16
 
